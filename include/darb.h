@@ -23,8 +23,8 @@
  *  - The caller owns every buffer it passes; a handle owns the encoded matrix
  *    and any scratch it allocates, and releases both in darb_destroy.
  *  - Work is enqueued on the caller's stream.  Only darb_encode, darb_import,
- *    darb_export, darb_sync_status, darb_rnn_reserve and darb_destroy
- *    synchronise; the product, step and sequence calls are asynchronous.
+ *    darb_export, darb_sync_status, darb_rnn_reserve, darb_adamw_create and the
+ *    two destroy calls synchronise; the others are asynchronous.
  *    darb_spmm allocates nothing; the step calls on large matrices or batches
  *    use scratch owned by the handle (darb_rnn_reserve sizes it up front).
  *  - Only two opt-in calls take scratch from the device's stream-ordered
@@ -67,8 +67,16 @@ typedef enum {
 
 typedef enum { DARB_F32 = 0, DARB_BF16 = 1 } darb_dtype_t;
 
+/* How the activations of a call lie in memory.  DARB_TOKEN_ROWS: token t is a row
+ * of contiguous features at t * ld.  DARB_TOKEN_COLUMNS: features x tokens, feature
+ * f of token t at f * ld + t -- the layout that darb_spmm and the steps read and write. */
+typedef enum { DARB_TOKEN_ROWS = 0, DARB_TOKEN_COLUMNS = 1 } darb_layout_t;
+
 /* Largest block size the format stores (offsets take at most 8 bits). */
 #define DARB_MAX_BLOCK 256
+
+/* Most alternatives that darb_token_logprobs lists for a token. */
+#define DARB_MAX_TOP 32
 
 /*
  * Density-adaptive block-size rule (Sec. 3.2, the worked example with matrix
@@ -371,6 +379,170 @@ DARB_API darb_status_t darb_lstm_step_noalloc(darb_handle_t h, int64_t I, int64_
  * later step calls allocate nothing (e.g. before capturing them in a CUDA
  * graph).  Synchronises the device.  Errors: INVALID_ARG, OOM, CUDA.          */
 DARB_API darb_status_t darb_rnn_reserve(darb_handle_t h, int64_t max_batch);
+
+/*
+ * What a model answers with, scored: for each token the log probability of the
+ * entry that was given, the entropy of the distribution and its k most probable
+ * entries, from the logits in one pass (the perplexity that Sec. 4.1 reports
+ * is exp of the mean negative log probability).  With x the token's logits,
+ *   lse = log sum_v exp(x_v),  log p_v = x_v - lse,  entropy = -sum_v p_v log p_v.
+ *   logits   device, tokens x vocab in `layout`, fp32 or bf16 (dtype), leading
+ *            dimension ld (>= vocab for token rows, >= tokens for token columns)
+ *   targets  device int64[tokens]: the entry whose log probability is wanted;
+ *            negative: none (log probability 0); vocab or more: NaN.  NULL if
+ *            logprob is NULL, and only then
+ *   k        0 <= k <= min(DARB_MAX_TOP, vocab)
+ *   logprob, entropy, lse   device fp32[tokens]; each may be NULL
+ *   top_logprob, top_index  device fp32 / int32 [tokens x k], most probable
+ *            first, equal logits by index (NaN counts as the largest); NULL
+ *            allowed when k == 0
+ * A logit of -inf is a masked entry (p = 0).  A token whose entries are all -inf
+ * has lse and log probabilities of -inf and an entropy of 0.  A token with a NaN or
+ * +inf among its logits has NaN results (its top_index stands).  All sums are
+ * fp32 and in a fixed order.  tokens == 0 does nothing.
+ * No output may overlap another buffer of the call.  Asynchronous on `stream`;
+ * allocates nothing; one launch.
+ * Errors: DARB_ERR_INVALID_ARG; DARB_ERR_UNSUPPORTED (more than 2^27 tokens,
+ * 2^30 entries, or 2^48 elements from the first to the last logit); DARB_ERR_CUDA.
+ */
+DARB_API darb_status_t darb_token_logprobs(const void *logits, darb_dtype_t dtype, darb_layout_t layout,
+                                           int64_t tokens, int64_t vocab, int64_t ld, const int64_t *targets,
+                                           int32_t k, float *logprob, float *entropy, float *lse,
+                                           float *top_logprob, int32_t *top_index, cudaStream_t stream);
+
+/*
+ * The gradient of darb_token_logprobs with respect to the logits: with a and b
+ * the incoming gradients of log probability and entropy,
+ *   d_logits_v = a ([v = target] - p_v) - b p_v (log p_v + entropy).
+ * (The gradient of the mean loss over n tokens has a = -1/n.)
+ *   logits, targets   as in the forward call; lse, entropy its results
+ *   d_logprob, d_entropy   device fp32[tokens]; NULL: no such gradient (targets
+ *            may then be NULL, and without d_entropy entropy may be NULL)
+ *   d_logits device, tokens x vocab in `layout`, of the logits' dtype, leading
+ *            dimension ld_grad; may be the logits themselves (same pointer and
+ *            leading dimension), otherwise it may not overlap another buffer
+ * A token without a target gets no gradient of its log probability, a token
+ * whose entries are all -inf none at all; a target of vocab or more gives NaN.
+ * Asynchronous on `stream`; allocates nothing; one launch.
+ * Errors: as darb_token_logprobs.
+ */
+DARB_API darb_status_t darb_token_logprobs_grad(const void *logits, darb_dtype_t dtype, darb_layout_t layout,
+                                                int64_t tokens, int64_t vocab, int64_t ld, const int64_t *targets,
+                                                const float *lse, const float *entropy, const float *d_logprob,
+                                                const float *d_entropy, void *d_logits, int64_t ld_grad,
+                                                cudaStream_t stream);
+
+/*
+ * Layer norm over the features of each token (the normalisation between the
+ * layers that the library multiplies):
+ *   mean = sum_f x_f / F,  rstd = 1 / sqrt(sum_f (x_f - mean)^2 / F + eps),
+ *   y_f = (x_f - mean) * rstd * gamma_f + beta_f.
+ *   x, y     device, fp32 or bf16 (dtype), leading dimensions ld_x, ld_y.  Token
+ *            rows: tokens x features, steps = 1.  Token columns: `steps` matrices
+ *            of features x tokens one after the other (matrix s at
+ *            s * features * ld), as the sequence calls write them
+ *   gamma, beta   device fp32[features]; NULL: 1 and 0
+ *   mean, rstd    device fp32[steps x tokens]: the statistics the backward pass
+ *            needs; each may be NULL
+ * The mean and the centred squares are summed in fp32, the squares after the mean
+ * is known.  y may be x itself (same pointer and leading dimension); no other
+ * overlap of an output is allowed.  No tokens: nothing is done.
+ * Asynchronous on `stream`; allocates nothing; one launch.
+ * Errors: DARB_ERR_INVALID_ARG (also a negative or NaN eps); DARB_ERR_UNSUPPORTED
+ * (sizes as darb_token_logprobs, features up to 2^24); DARB_ERR_CUDA.
+ */
+DARB_API darb_status_t darb_layer_norm(const void *x, darb_dtype_t dtype, darb_layout_t layout, int64_t steps,
+                                       int64_t tokens, int64_t features, int64_t ld_x, const float *gamma,
+                                       const float *beta, float eps, void *y, int64_t ld_y, float *mean, float *rstd,
+                                       cudaStream_t stream);
+
+/*
+ * The backward pass of darb_layer_norm.  With xh = (x - mean) * rstd and
+ * g = dy * gamma, per token
+ *   dx_f = rstd * (g_f - sum g / F - xh_f * sum(g xh) / F),
+ * and over all tokens dgamma_f = sum dy_f xh_f, dbeta_f = sum dy_f.
+ *   dy, x, dx   device, of one dtype and layout, with leading dimensions of
+ *            their own; dx may be dy itself (same pointer and leading dimension)
+ *   gamma    device fp32[features] or NULL (1)
+ *   mean, rstd  what the forward pass wrote
+ *   dgamma, dbeta  device fp32[features], overwritten (with zeros when there
+ *            are no tokens); both NULL: not wanted
+ *   work     device scratch of darb_layer_norm_grad_work bytes, 16-byte aligned, the
+ *            caller's; not used (NULL allowed) when dgamma and dbeta are NULL
+ * The sums over the tokens are fp32, in an order fixed by the sizes and alignments.
+ * Asynchronous on `stream`; allocates nothing.  Errors: as darb_layer_norm.
+ */
+DARB_API darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x,
+                                            darb_dtype_t dtype, darb_layout_t layout, int64_t steps, int64_t tokens,
+                                            int64_t features, const float *gamma, const float *mean,
+                                            const float *rstd, void *dx, int64_t ld_dx, float *dgamma, float *dbeta,
+                                            void *work, cudaStream_t stream);
+
+/* Bytes of scratch that darb_layer_norm_grad needs on the current device.
+ * Errors: DARB_ERR_INVALID_ARG (sizes, null output).                          */
+DARB_API darb_status_t darb_layer_norm_grad_work(darb_layout_t layout, int64_t steps, int64_t tokens, int64_t features,
+                                                 int64_t *bytes);
+
+/* Elements that share a scale where darb_adamw_step holds states in 8 bits. */
+#define DARB_ADAMW_BLOCK 256
+
+typedef struct darb_adamw_s *darb_adamw_t;
+
+/*
+ * A plan for AdamW steps over n tensors at once (the update of the dense weights
+ * between two re-encodes of Sec. 4's prune-retrain loop).  All tensors are dense
+ * and the caller's; they have to stay where they are while the plan lives.
+ *   numel    host int64[n], 0 allowed
+ *   params   host array of n device pointers, fp32, updated by every step
+ *   m, v     host arrays of n device pointers, the moments.  m_scale and v_scale
+ *            NULL: fp32, m and v.  Otherwise e4m3 codes (one byte an element) of m
+ *            and of sqrt(v), with
+ *   m_scale, v_scale  host arrays of n device pointers, fp32, one value for every
+ *            DARB_ADAMW_BLOCK elements of the tensor (the last block may be
+ *            short); an element is code * scale.  Zero codes and scales are zero
+ *            moments
+ *   copies   host array of n device pointers (NULL entries allowed), bf16: the
+ *            updated parameter rounded, e.g. for darb_reencode; NULL: none
+ *   gtype    type of the gradients
+ * No two of the buffers may overlap.  Allocates the plan's tables on the current
+ * device, runs on `stream` and synchronises it.
+ * Errors: DARB_ERR_INVALID_ARG; DARB_ERR_UNSUPPORTED (2^31 chunks of 4096
+ * elements or more); DARB_ERR_OOM; DARB_ERR_CUDA.
+ */
+DARB_API darb_status_t darb_adamw_create(int32_t n, const int64_t *numel, float *const *params, void *const *m,
+                                         void *const *v, float *const *m_scale, float *const *v_scale,
+                                         void *const *copies, darb_dtype_t gtype, darb_adamw_t *out,
+                                         cudaStream_t stream);
+
+/*
+ * One step: with g' = g * *grad_scale and t = step,
+ *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *   p = p (1 - lr weight_decay)
+ *       - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
+ *   grads    host array of n device pointers of the plan's gradient type; a NULL
+ *            entry leaves its tensor and states as they are
+ *   grad_scale  device fp32 scalar (what clipping by the norm gives), or NULL: 1
+ *   step     t >= 1
+ *   seed     of the states' rounding in 8 bits; another one for every step (the
+ *            step itself, for instance).  The same inputs and seed give the same
+ *            results.  Not used with fp32 states
+ * Each operation above is one IEEE fp32 operation; in 8 bits the update uses m
+ * and v before they are rounded, and a block's scale is its largest magnitude /
+ * 448, the codes rounded up or down at random so that the mean is kept (a root
+ * that is not zero keeps a code that is not zero).  A NaN or infinity reaches its
+ * own element, and in 8 bits the states of its block.
+ * Asynchronous on `stream`; allocates nothing; one launch for every 448 tensors.
+ * Steps of one plan must be ordered on one stream.
+ * Errors: DARB_ERR_INVALID_ARG (an unknown plan, a step below 1, lr, eps or
+ * weight_decay negative or not finite, a beta outside [0, 1), a gradient that
+ * overlaps its tensor's buffers); DARB_ERR_CUDA.
+ */
+DARB_API darb_status_t darb_adamw_step(darb_adamw_t plan, const void *const *grads, const float *grad_scale,
+                                       int64_t step, uint64_t seed, double lr, double beta1, double beta2, double eps,
+                                       double weight_decay, cudaStream_t stream);
+
+/* Release a plan (not its tensors); NULL is a no-op.  Waits for the device.    */
+DARB_API darb_status_t darb_adamw_destroy(darb_adamw_t plan);
 
 typedef struct {
     int64_t rows, cols;

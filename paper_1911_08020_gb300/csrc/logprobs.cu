@@ -1,0 +1,826 @@
+// logprobs.cu -- the log probability of given tokens under their logits, the
+// entropy of the distribution and its k largest entries, in one pass over the
+// logits; and the gradient of log probability and entropy (darb_token_logprobs,
+// darb_token_logprobs_grad): what turns a layer's product into the perplexity
+// that Sec. 4.1 reports and into the loss of its
+// retraining.
+//
+// For a token with logits x_v:  M = max x,  s = sum exp(x_v - M),
+//   lse = M + log s,   log p_v = x_v - lse,
+//   H   = -sum p log p = log s - (sum exp(x_v - M) (x_v - M)) / s.
+// The kernels work in base 2: with the reference r = M log2(e), rounded once
+// and used by every term, d_v = x_v log2(e) - r is one FMA, e_v = 2^d_v one
+// instruction, and lse = (r + log2 s) ln 2.  A partial result is (M, s, t) with
+// s = sum e_v and t = sum e_v d_v; two of them join by
+//   f = 2^(r1 - r),  s += f s1,  t += f (t1 + s1 (r1 - r)).
+//
+// Masks.  Logits are clamped from below at -2^15 before use, so that a masked
+// entry (-inf, the type's lowest value, -1e9) adds 2^-huge = 0 to s and to t
+// instead of 0 * inf, and so that d of the largest logit is never far from 0
+// (the rounding of r is at most 2^-24 of 2^15 log2(e)).  A token whose largest
+// logit is not within +-2^14 (every entry masked, or enormous logits) is done
+// again in plain fp32 differences x - M ("wide"), which hold for any finite
+// logits.  NaN survives every maximum (max.NaN), so a NaN logit makes the
+// token's results NaN.
+#include "launch.cuh"
+#include "tma.cuh"
+#include "tokens.cuh"
+#include "trace.h"
+
+#include <cooperative_groups.h>
+
+#include <algorithm>
+#include <cmath>
+
+namespace cg = cooperative_groups;
+
+namespace darb {
+
+int sm_count();
+
+namespace {
+
+constexpr float kMasked = -0x1p15f;   // logits are read as at least this (exact in bf16)
+constexpr float kWide = 0x1p14f;      // the largest logit of a token that takes the fast path, in magnitude
+constexpr int kMaxTop = DARB_MAX_TOP;
+constexpr int kCandidates = 256;    // candidates for the k largest that are gathered at once
+constexpr int kMaxSplit = 8;        // CTAs that share a token
+
+struct ScoreArgs {
+    const void *x;
+    int64_t ld;
+    int64_t tokens;
+    int32_t vocab;
+    int32_t k;
+    const int64_t *targets;   // or null
+    float *logprob, *entropy, *lse, *top_logprob;   // or null
+    int32_t *top_index;
+};
+
+// A partial result over some of a token's logits.
+struct Part {
+    float m, s, t;
+};
+__device__ __forceinline__ Part empty_part() { return {kMasked, 0.0f, 0.0f}; }
+__device__ __forceinline__ Part rescaled(const Part &p, float m) {
+    const float d = p.m * kLog2e - m * kLog2e;
+    const float f = exp2_fast(d);
+    return {m, f * p.s, f * (p.t + p.s * d)};
+}
+__device__ __forceinline__ Part warp_join(Part p) {
+    float m = p.m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    p = rescaled(p, m);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        p.s += __shfl_xor_sync(0xFFFFFFFFu, p.s, o);
+        p.t += __shfl_xor_sync(0xFFFFFFFFu, p.t, o);
+    }
+    return p;
+}
+
+// Logits in order of value: larger logits have larger keys, NaN the largest,
+// +0 and -0 one key.  Below it the index, inverted: ties go to the lowest.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t b = __float_as_uint(x);
+    if (x != x) return 0xFFFFFFFFu;
+    if (x == 0.0f) return 0x80000000u;
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) {
+    if (o == 0xFFFFFFFFu) return __uint_as_float(0x7FC00000u);
+    return __uint_as_float((o & 0x80000000u) ? o ^ 0x80000000u : ~o);
+}
+__device__ __forceinline__ uint64_t key_of(float x, int32_t index) {
+    return (uint64_t(order_of(x)) << 32) | uint32_t(0xFFFFFFFFu - uint32_t(index));
+}
+__device__ __forceinline__ int32_t index_of(uint64_t key) { return int32_t(0xFFFFFFFFu - uint32_t(key)); }
+
+// What every output of a token is made from.
+struct Token {
+    float r;       // log2 units: the reference, (finite) M log2(e)
+    float m;       // M itself, for wide tokens
+    float log2s;   // log2 s
+    float t_s;     // t / s
+    bool wide, empty;
+    __device__ float logprob(float x) const {
+        if (empty) return -INFINITY;
+        return (wide ? (x - m) * kLog2e - log2s : fmaf(x, kLog2e, -r) - log2s) * kLn2;
+    }
+    __device__ float entropy() const { return empty ? 0.0f : (log2s - t_s) * kLn2; }
+    __device__ float lse() const { return empty ? -INFINITY : wide ? m + log2s * kLn2 : (r + log2s) * kLn2; }
+};
+__device__ __forceinline__ Token token_of(const Part &p) {
+    return {p.m * kLog2e, p.m, log2f(p.s), p.t / p.s, false, false};
+}
+// Whether a token's fast partial result does not stand (a NaN one does).
+__device__ __forceinline__ bool is_wide(float m) { return m < -kWide || m > kWide; }
+
+__device__ __forceinline__ float target_logprob(const Token &tok, int64_t target, int32_t vocab, float x) {
+    if (target < 0) return 0.0f;
+    if (target >= vocab) return __uint_as_float(0x7FC00000u);
+    return tok.logprob(x);
+}
+
+// ---- a CTA's slow paths over the logits base[i * stride], i in [i0, i1) ----
+
+// Sum, maximum or maximum with NaN over the CTA; every thread gets it.  `buf`:
+// 33 floats of shared memory.
+template <typename Op>
+__device__ float cta_reduce(float v, float *buf, Op op) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    __syncthreads();   // the buffer may still be read by an earlier call
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float a = buf[0];
+        for (unsigned w = 1; w < blockDim.x / 32; ++w) a = op(a, buf[w]);
+        buf[32] = a;
+    }
+    __syncthreads();
+    return buf[32];
+}
+
+// A token in plain differences from its maximum, for logits of any size.
+template <typename T>
+__device__ Token wide_token(const T *base, int64_t stride, int32_t n, float *buf) {
+    float m = -INFINITY;
+    for (int32_t i = threadIdx.x; i < n; i += blockDim.x) m = max_nan(m, widen(base[int64_t(i) * stride]));
+    m = cta_reduce(m, buf, [](float a, float b) { return max_nan(a, b); });
+    if (m == -INFINITY) return {0.0f, m, 0.0f, 0.0f, true, true};
+    float s = 0.0f, t = 0.0f;
+    for (int32_t i = threadIdx.x; i < n; i += blockDim.x) {
+        const float d = widen(base[int64_t(i) * stride]) - m;   // NaN for m = inf and for NaN logits
+        const float l = max_nan(d * kLog2e, -1e3f);
+        const float e = exp2_fast(l);
+        s += e;
+        t += e * l;
+    }
+    s = cta_reduce(s, buf, [](float a, float b) { return a + b; });
+    t = cta_reduce(t, buf, [](float a, float b) { return a + b; });
+    return {0.0f, m, log2f(s), t / s, true, false};
+}
+
+// The min(k, i1 - i0) largest keys, in any order, to sel[0 .. kMaxTop) (0 where
+// there is none), for any logits: the k-th largest key is found 8 bits at a
+// time.  hist: 256 words, ctl: 4 words of shared memory.
+template <typename T>
+__device__ void select_any(const T *base, int64_t stride, int32_t i0, int32_t i1, int k, uint64_t *sel, uint32_t *hist,
+                           uint32_t *ctl) {
+    const int want = min(k, max(0, i1 - i0));
+    __syncthreads();
+    if (threadIdx.x < kMaxTop) sel[threadIdx.x] = 0;
+    if (threadIdx.x == 0) ctl[0] = want, ctl[1] = 0, ctl[2] = 0;   // rank that is left, gathered, done
+    uint64_t prefix = 0;
+    int bits = 0;   // of the prefix
+    if (want > 0) {
+        while (bits < 64) {
+            for (int i = threadIdx.x; i < 256; i += blockDim.x) hist[i] = 0;
+            __syncthreads();
+            const int shift = 64 - bits - 8;
+            // a run of equal digits is added at once: masked entries share theirs
+            uint32_t run_digit = 0, run = 0;
+            for (int32_t i = i0 + int32_t(threadIdx.x); i < i1; i += blockDim.x) {
+                const uint64_t key = key_of(widen(base[int64_t(i) * stride]), i);
+                if (bits > 0 && (key >> (shift + 8)) != prefix) continue;
+                const uint32_t d = uint32_t(key >> shift) & 255u;
+                if (d == run_digit) {
+                    ++run;
+                } else {
+                    if (run) atomicAdd(&hist[run_digit], run);
+                    run_digit = d;
+                    run = 1;
+                }
+            }
+            if (run) atomicAdd(&hist[run_digit], run);
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                uint32_t left = ctl[0];
+                int d = 255;
+                while (d > 0 && hist[d] < left) left -= hist[d--];
+                ctl[0] = left;
+                ctl[3] = uint32_t(d);
+                ctl[2] = hist[d] == left;   // the whole digit is taken
+            }
+            __syncthreads();
+            prefix = (prefix << 8) | ctl[3];
+            bits += 8;
+            if (ctl[2]) break;
+            __syncthreads();
+        }
+        for (int32_t i = i0 + int32_t(threadIdx.x); i < i1; i += blockDim.x) {
+            const uint64_t key = key_of(widen(base[int64_t(i) * stride]), i);
+            if ((key >> (64 - bits)) >= prefix) {
+                const uint32_t p = atomicAdd(&ctl[1], 1u);
+                if (p < kMaxTop) sel[p] = key;
+            }
+        }
+    }
+    __syncthreads();
+}
+
+// The k largest of n keys (all different, but for zeros at the end), in order:
+// every key counts those above it.
+__device__ __forceinline__ void rank_keys(const uint64_t *keys, int n, int k, uint64_t *sorted, int thread, int threads) {
+    for (int i = thread; i < n; i += threads) {
+        const uint64_t key = keys[i];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += keys[j] > key;
+        if (above < k && key != 0) sorted[above] = key;
+    }
+}
+
+// The k-th largest of 32 values, one a lane (equal values rank by lane).
+__device__ __forceinline__ float kth_of_warp(float v, int k) {
+    const int lane = threadIdx.x & 31;
+    int above = 0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        const float o = __shfl_sync(0xFFFFFFFFu, v, j);
+        above += o > v || (o == v && j < lane);
+    }
+    const unsigned at = __ballot_sync(0xFFFFFFFFu, above == k - 1);
+    return __shfl_sync(0xFFFFFFFFu, v, at ? __ffs(at) - 1 : 0);
+}
+
+// ---- token rows ----
+
+// The logits of a block of granules, clamped, and their maximum.
+template <int N>
+__device__ __forceinline__ void clamp_block(uint4 (&q)[N], float &m, float) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        uint32_t *w = reinterpret_cast<uint32_t *>(&q[u]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float c = max_nan(__uint_as_float(w[i]), kMasked);
+            m = max_nan(m, c);
+            w[i] = __float_as_uint(c);
+        }
+    }
+}
+template <int N>
+__device__ __forceinline__ void clamp_block(uint4 (&q)[N], float &m, __nv_bfloat16) {
+    const __nv_bfloat162 lowest = __float2bfloat162_rn(kMasked);
+    __nv_bfloat162 mm = lowest;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        __nv_bfloat162 *w = reinterpret_cast<__nv_bfloat162 *>(&q[u]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = __hmax2_nan(w[i], lowest);
+            mm = __hmax2_nan(mm, w[i]);
+        }
+    }
+    m = max_nan(m, max_nan(__low2float(mm), __high2float(mm)));
+}
+
+template <typename T, int THREADS, int U>
+__global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a) {
+    constexpr int V = kPerGranule<T>;
+    constexpr int W = THREADS / 32;
+    __shared__ Part warp_part[W];
+    __shared__ Part cta_part;
+    __shared__ float thread_max[THREADS];
+    __shared__ uint64_t cand[kCandidates], sel[kMaxTop], sorted[kMaxTop];
+    __shared__ uint32_t hist[256], ctl[4], ncand;
+    __shared__ float buf[33];
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int split = int(cluster.num_blocks()), rank = int(cluster.block_rank());
+    const int64_t token = blockIdx.x / split;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const T *row = static_cast<const T *>(a.x) + token * a.ld;
+    const int head = row_head<T>(row);
+    const int32_t n = a.vocab, granules = int32_t(row_granules<T>(head, n));
+    const int32_t g0 = int32_t(int64_t(granules) * rank / split), g1 = int32_t(int64_t(granules) * (rank + 1) / split);
+    int64_t target = -1;
+    float target_x = 0.0f;
+    if (tid == 0 && rank == 0 && a.targets != nullptr) {
+        target = a.targets[token];
+        if (target >= 0 && target < n) target_x = widen(row[target]);
+    }
+    if (tid == 0) ncand = 0;
+
+    float m = kMasked;
+    float2 s2 = both(0.0f), t2 = both(0.0f);
+    for (int32_t g = g0 + tid; g < g1; g += THREADS * U) {
+        uint4 q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t gu = g + u * THREADS;
+            q[u] = load_granule(row, gu < g1 ? int64_t(gu) * V - head : int64_t(n), n, -INFINITY);
+        }
+        float top = m;
+        clamp_block(q, top, T());
+        {
+            const float d = m * kLog2e - top * kLog2e, f = exp2_fast(d);
+            t2 = mul2(both(f), fma2(s2, both(d), t2));
+            s2 = mul2(both(f), s2);
+            m = top;
+        }
+        const float2 l2 = both(kLog2e), r2 = both(-(m * kLog2e));
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[V];
+            unpack(q[u], v);
+#pragma unroll
+            for (int i = 0; i < V; i += 2) {
+                const float2 d = fma2(make_float2(v[i], v[i + 1]), l2, r2);
+                const float2 e = make_float2(exp2_fast(d.x), exp2_fast(d.y));
+                s2 = add2(s2, e);
+                t2 = fma2(e, d, t2);
+            }
+        }
+    }
+    thread_max[tid] = m;
+    const Part mine = warp_join({m, s2.x + s2.y, t2.x + t2.y});
+    if (lane == 0) warp_part[warp] = mine;
+    __syncthreads();
+    // every warp joins the partial results of all, in the same order
+    const Part all = warp_join(lane < W ? warp_part[lane] : empty_part());
+    if (split > 1 && tid == 0) cta_part = all;
+
+    const int k = a.k;
+    if (k > 0) {
+        // The k-th largest of 32 maxima over disjoint sets of logits is at most the
+        // k-th largest logit, so only logits from there on can be among the k
+        // largest, and only threads whose maximum reaches it look at theirs again.
+        float g = thread_max[lane];
+        for (int w = 1; w < W; ++w) g = max_nan(g, thread_max[w * 32 + lane]);
+        const float bar = kth_of_warp(g, k);
+        const bool plain = bar > kMasked && all.m == all.m;   // the same for all threads
+        if (plain && m >= bar) {
+            for (int32_t gi = g0 + tid; gi < g1; gi += THREADS) {
+                float v[V];
+                const int64_t j0 = int64_t(gi) * V - head;
+                unpack(load_granule(row, j0, n, -INFINITY), v);
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (v[i] >= bar) {
+                        const uint32_t p = atomicAdd(&ncand, 1u);
+                        if (p < kCandidates) cand[p] = key_of(v[i], int32_t(j0 + i));
+                    }
+            }
+        }
+        __syncthreads();
+        int found = int(ncand);
+        if (!plain || found > kCandidates) {
+            const int32_t i0 = max(0, g0 * V - head), i1 = min(n, g1 * V - head);
+            select_any(row, 1, i0, i1, k, sel, hist, ctl);
+            if (tid < kMaxTop) cand[tid] = sel[tid];
+            found = kMaxTop;
+        }
+        if (tid < kMaxTop) sorted[tid] = 0;
+        __syncthreads();
+        rank_keys(cand, found, k, sorted, tid, THREADS);
+    }
+    Part whole = all;
+    if (split > 1) {
+        cluster.sync();
+        if (rank == 0) {
+            whole = empty_part();
+            if (lane < split) whole = *cluster.map_shared_rank(&cta_part, lane);
+            whole = warp_join(whole);
+            const int total = split * k;
+            for (int i = tid; i < total; i += THREADS) cand[i] = cluster.map_shared_rank(sorted, i / k)[i % k];
+        }
+        cluster.sync();   // the other CTAs may leave: nothing reads them any more
+        if (rank != 0) return;
+        if (k > 0) {
+            if (tid < kMaxTop) sorted[tid] = 0;
+            __syncthreads();
+            rank_keys(cand, split * k, k, sorted, tid, THREADS);
+        }
+    }
+    Token tok;
+    if (is_wide(whole.m)) tok = wide_token(row, 1, n, buf);
+    else tok = token_of(whole);
+    if (tid == 0) {
+        if (a.logprob) a.logprob[token] = target_logprob(tok, target, n, target_x);
+        if (a.entropy) a.entropy[token] = tok.entropy();
+        if (a.lse) a.lse[token] = tok.lse();
+    }
+    if (k > 0) {
+        __syncthreads();
+        if (tid < k) {
+            const uint64_t key = sorted[tid];
+            a.top_logprob[token * k + tid] = tok.logprob(value_of(uint32_t(key >> 32)));
+            a.top_index[token * k + tid] = index_of(key);
+        }
+    }
+}
+
+// ---- token columns ----
+
+// A tile of CT columns; thread = (slot, column), the slots of a CTA share the
+// rows of its part of the vocabulary.
+constexpr int kColThreads = 1024;
+constexpr int kColCandidates = 160;   // a column
+constexpr int kColUnroll = 8;
+
+template <int CT>
+struct ColShared {
+    static constexpr int kSlots = kColThreads / CT;
+    Part part[kSlots][CT + 1];
+    Part col[CT];
+    float bar[CT];
+    uint32_t ncand[CT];
+    uint64_t cand[CT][kColCandidates];
+    uint64_t sorted[CT][kMaxTop];
+    uint64_t sel[kMaxTop];
+    uint32_t hist[256], ctl[4];
+    float buf[33];
+    Token tok[CT];
+};
+
+template <typename T, int CT>
+__global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreArgs a) {
+    constexpr int SLOTS = kColThreads / CT, U = kColUnroll;
+    extern __shared__ __align__(16) unsigned char smem[];
+    ColShared<CT> &sh = *reinterpret_cast<ColShared<CT> *>(smem);
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int split = int(cluster.num_blocks()), rank = int(cluster.block_rank());
+    const int64_t c0 = int64_t(blockIdx.x / split) * CT;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int col = tid % CT, slot = tid / CT;
+    const int64_t token = c0 + col;
+    const bool in = token < a.tokens;
+    const T *base = static_cast<const T *>(a.x) + token;   // of this thread's column
+    const int32_t n = a.vocab, k = a.k;
+    const int32_t v0 = int32_t(int64_t(n) * rank / split), v1 = int32_t(int64_t(n) * (rank + 1) / split);
+    if (tid < CT) sh.ncand[tid] = 0;
+
+    float m = kMasked;
+    float2 s2 = both(0.0f), t2 = both(0.0f);
+    if (in) {
+        for (int32_t v = v0 + slot; v < v1; v += SLOTS * U) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int32_t vu = v + u * SLOTS;
+                x[u] = vu < v1 ? widen(base[int64_t(vu) * a.ld]) : -INFINITY;
+            }
+            float top = m;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                x[u] = max_nan(x[u], kMasked);
+                top = max_nan(top, x[u]);
+            }
+            const float d0 = m * kLog2e - top * kLog2e, f = exp2_fast(d0);
+            t2 = mul2(both(f), fma2(s2, both(d0), t2));
+            s2 = mul2(both(f), s2);
+            m = top;
+            const float2 l2 = both(kLog2e), r2 = both(-(m * kLog2e));
+#pragma unroll
+            for (int u = 0; u < U; u += 2) {
+                const float2 d = fma2(make_float2(x[u], x[u + 1]), l2, r2);
+                const float2 e = make_float2(exp2_fast(d.x), exp2_fast(d.y));
+                s2 = add2(s2, e);
+                t2 = fma2(e, d, t2);
+            }
+        }
+    }
+    sh.part[slot][col] = {m, s2.x + s2.y, t2.x + t2.y};
+    __syncthreads();
+    // warp c joins column c (c < CT <= 32 warps), and finds the bar of its k largest
+    if (warp < CT) {
+        Part p = empty_part();
+        float g = kMasked;
+        for (int s = lane; s < SLOTS; s += 32) {
+            const Part q = sh.part[s][warp];
+            g = max_nan(g, q.m);
+            const float mm = max_nan(p.m, q.m);
+            const Part x = rescaled(p, mm), y = rescaled(q, mm);
+            p = {mm, x.s + y.s, x.t + y.t};
+        }
+        p = warp_join(p);
+        if (lane == 0) sh.col[warp] = p;
+        if (k > 0) {
+            const float bar = kth_of_warp(g, k);
+            if (lane == 0) sh.bar[warp] = bar > kMasked && p.m == p.m ? bar : __uint_as_float(0x7FC00000u);
+        }
+    }
+    __syncthreads();
+    if (k > 0) {
+        const float bar = sh.bar[col];   // NaN: no plain choice
+        if (in && m >= bar) {
+            for (int32_t v = v0 + slot; v < v1; v += SLOTS) {
+                const float x = widen(base[int64_t(v) * a.ld]);
+                if (x >= bar) {
+                    const uint32_t p = atomicAdd(&sh.ncand[col], 1u);
+                    if (p < kColCandidates) sh.cand[col][p] = key_of(x, v);
+                }
+            }
+        }
+        for (int i = tid; i < CT * kMaxTop; i += kColThreads) sh.sorted[i / kMaxTop][i % kMaxTop] = 0;
+        __syncthreads();
+        for (int c = 0; c < CT && c0 + c < a.tokens; ++c) {
+            if (sh.bar[c] == sh.bar[c] && sh.ncand[c] <= kColCandidates) continue;
+            select_any(static_cast<const T *>(a.x) + c0 + c, a.ld, v0, v1, k, sh.sel, sh.hist, sh.ctl);
+            if (tid < kMaxTop) sh.cand[c][tid] = sh.sel[tid];
+            if (tid == 0) sh.ncand[c] = kMaxTop;
+            // (the bar is not read again in this loop: the next column has its own)
+        }
+        __syncthreads();
+        if (warp < CT) rank_keys(sh.cand[warp], int(sh.ncand[warp]), k, sh.sorted[warp], lane, 32);
+    }
+    if (split > 1) {
+        cluster.sync();
+        Part p = empty_part();
+        if (rank == 0 && warp < CT) {
+            if (lane < split) p = cluster.map_shared_rank(&sh, lane)->col[warp];
+            for (int i = lane; i < split * k; i += 32)
+                sh.cand[warp][i] = cluster.map_shared_rank(&sh, i / k)->sorted[warp][i % k];
+        }
+        cluster.sync();   // the other CTAs may leave
+        if (rank != 0) return;
+        if (warp < CT) {
+            p = warp_join(p);
+            if (lane == 0) sh.col[warp] = p;
+            if (k > 0) {
+                sh.sorted[warp][lane] = 0;
+                __syncwarp();
+                rank_keys(sh.cand[warp], split * k, k, sh.sorted[warp], lane, 32);
+            }
+        }
+    }
+    __syncthreads();
+    for (int c = 0; c < CT && c0 + c < a.tokens; ++c) {
+        Token tok;
+        if (is_wide(sh.col[c].m)) tok = wide_token(static_cast<const T *>(a.x) + c0 + c, a.ld, n, sh.buf);
+        else if (tid != c) continue;
+        else tok = token_of(sh.col[c]);
+        if (tid == c) sh.tok[c] = tok;
+    }
+    __syncthreads();
+    if (tid < CT && in) {   // slot 0: col == tid
+        const Token tok = sh.tok[tid];
+        if (a.logprob) {
+            const int64_t target = a.targets[token];
+            const float x = target >= 0 && target < n ? widen(base[target * a.ld]) : 0.0f;
+            a.logprob[token] = target_logprob(tok, target, n, x);
+        }
+        if (a.entropy) a.entropy[token] = tok.entropy();
+        if (a.lse) a.lse[token] = tok.lse();
+    }
+    for (int i = tid; i < CT * k; i += kColThreads) {
+        const int c = i / k, j = i % k;
+        if (c0 + c >= a.tokens) break;
+        const uint64_t key = sh.sorted[c][j];
+        a.top_logprob[(c0 + c) * k + j] = sh.tok[c].logprob(value_of(uint32_t(key >> 32)));
+        a.top_index[(c0 + c) * k + j] = index_of(key);
+    }
+}
+
+template <typename T>
+cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream) {
+    constexpr int THREADS = 256, U = 4;
+    int split = 1;
+    while (split < kMaxSplit && a.tokens * split < 2 * sm_count() &&
+           a.vocab / (2 * split) >= THREADS * kPerGranule<T>)
+        split *= 2;
+    return launch_ex(score_rows_kernel<T, THREADS, U>, dim3(unsigned(a.tokens * split)), dim3(THREADS), 0, stream,
+                     unsigned(split), true, a);
+}
+
+template <typename T, int CT>
+cudaError_t launch_score_columns_ct(const ScoreArgs &a, cudaStream_t stream) {
+    const int64_t tiles = (a.tokens + CT - 1) / CT;
+    // the candidates of every CTA of a cluster have to fit a column's list
+    const int most = a.k > 0 ? std::max(1, kColCandidates / a.k) : kMaxSplit;
+    int split = 1;
+    while (split < kMaxSplit && 2 * split <= most && tiles * split < sm_count() && a.vocab / (2 * split) >= 4 * kColThreads / CT)
+        split *= 2;
+    const size_t smem = sizeof(ColShared<CT>);
+    const cudaError_t e = allow_smem(score_columns_kernel<T, CT>, smem);
+    if (e != cudaSuccess) return e;
+    return launch_ex(score_columns_kernel<T, CT>, dim3(unsigned(tiles * split)), dim3(kColThreads), smem, stream,
+                     unsigned(split), true, a);
+}
+
+template <typename T>
+cudaError_t launch_score_columns(const ScoreArgs &a, cudaStream_t stream) {
+    if (a.tokens > 16) return launch_score_columns_ct<T, 32>(a, stream);
+    if (a.tokens > 8) return launch_score_columns_ct<T, 16>(a, stream);
+    if (a.tokens > 4) return launch_score_columns_ct<T, 8>(a, stream);
+    return launch_score_columns_ct<T, 4>(a, stream);
+}
+
+// ---- the gradient ----
+//
+//   dx_v = a ([v = target] - p_v) - b p_v (log p_v + H),
+// a and b the incoming gradients of log probability and entropy, p_v =
+// exp(x_v - lse).  One pass: reads a logit, writes its gradient.
+
+struct GradArgs {
+    const void *x;
+    void *dx;
+    int64_t ld, ldd;
+    int64_t tokens;
+    int32_t vocab;
+    const int64_t *targets;   // or null
+    const float *lse, *entropy, *d_logprob, *d_entropy;   // or null, but lse
+};
+
+// What a token's gradient is made from.
+struct GradToken {
+    float lse, a, b, h;
+    int32_t target;   // -1: none
+};
+__device__ __forceinline__ GradToken grad_token(const GradArgs &g, int64_t token) {
+    GradToken t = {g.lse[token], 0.0f, 0.0f, 0.0f, -1};
+    if (g.d_logprob != nullptr) {
+        const int64_t target = g.targets[token];
+        if (target >= g.vocab) {
+            t.a = __uint_as_float(0x7FC00000u);
+        } else if (target >= 0) {
+            t.a = g.d_logprob[token];
+            t.target = int32_t(target);
+        }
+    }
+    if (g.d_entropy != nullptr) {
+        t.b = g.d_entropy[token];
+        t.h = g.entropy[token];
+    }
+    if (t.lse == -INFINITY) {   // no entry: no distribution, no gradient
+        const bool nan = t.a != t.a;
+        t = {0.0f, nan ? t.a : 0.0f, 0.0f, 0.0f, -1};
+    }
+    return t;
+}
+__device__ __forceinline__ float grad_of(const GradToken &t, float x, int32_t v) {
+    const float l = max_nan(x - t.lse, kMasked);   // log p; a masked entry has p = 0
+    const float p = exp2_fast(l * kLog2e);
+    const float hit = v == t.target ? 1.0f : 0.0f;
+    return fmaf(t.a, hit - p, -t.b * p * (l + t.h));
+}
+
+constexpr int kGradThreads = 256;
+constexpr int kGradUnroll = 4;
+
+// Rows whose logits and gradients start alike past a 16-byte boundary.
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) grad_rows_kernel(const GradArgs a, int32_t parts) {
+    constexpr int V = kPerGranule<T>, U = kGradUnroll;
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    const int64_t token = blockIdx.x / parts;
+    const int32_t part = int32_t(blockIdx.x % parts);
+    const T *row = static_cast<const T *>(a.x) + token * a.ld;
+    T *out = static_cast<T *>(a.dx) + token * a.ldd;
+    const int head = row_head<T>(row);
+    const int32_t n = a.vocab, granules = int32_t(row_granules<T>(head, n));
+    const int32_t g0 = part * (kGradThreads * U) + int32_t(threadIdx.x);
+    uint4 q[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t g = g0 + u * kGradThreads;
+        if (g < granules) q[u] = load_granule<T, false>(row, int64_t(g) * V - head, n, -INFINITY);
+    }
+    const GradToken t = grad_token(a, token);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t g = g0 + u * kGradThreads;
+        if (g >= granules) break;
+        const int64_t j0 = int64_t(g) * V - head;
+        float v[V];
+        unpack(q[u], v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = grad_of(t, v[i], int32_t(j0 + i));
+        store_granule(out, j0, n, v);
+    }
+}
+
+// Any strides: logit v of token t at x[t * ts + v * vs].  Consecutive threads
+// take consecutive elements of the contiguous axis.
+template <typename T, bool COLUMNS>
+__global__ void __launch_bounds__(kGradThreads) grad_any_kernel(const GradArgs a, int32_t parts) {
+    constexpr int U = 8;
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    const T *x = static_cast<const T *>(a.x);
+    T *dx = static_cast<T *>(a.dx);
+    if constexpr (COLUMNS) {
+        // 32 columns x 8 rows of threads, U rows each
+        const int64_t token = int64_t(blockIdx.x / parts) * 32 + (threadIdx.x & 31);
+        if (token >= a.tokens) return;
+        const int64_t v0 = int64_t(blockIdx.x % parts) * (8 * U) + (threadIdx.x >> 5);
+        float v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (v0 + 8 * u < a.vocab) v[u] = widen(x[(v0 + 8 * u) * a.ld + token]);
+        const GradToken t = grad_token(a, token);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (v0 + 8 * u < a.vocab) dx[(v0 + 8 * u) * a.ldd + token] = narrow<T>(grad_of(t, v[u], int32_t(v0 + 8 * u)));
+    } else {
+        const int64_t token = blockIdx.x / parts;
+        const int64_t v0 = int64_t(blockIdx.x % parts) * (kGradThreads * U) + threadIdx.x;
+        const T *row = x + token * a.ld;
+        T *out = dx + token * a.ldd;
+        float v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (v0 + u * kGradThreads < a.vocab) v[u] = widen(row[v0 + u * kGradThreads]);
+        const GradToken t = grad_token(a, token);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (v0 + u * kGradThreads < a.vocab)
+                out[v0 + u * kGradThreads] = narrow<T>(grad_of(t, v[u], int32_t(v0 + u * kGradThreads)));
+    }
+}
+
+template <typename T>
+cudaError_t launch_grad(const GradArgs &a, darb_layout_t layout, cudaStream_t stream) {
+    const auto grid = [](int64_t n) { return dim3(unsigned(n)); };
+    if (layout == DARB_TOKEN_COLUMNS) {
+        const int32_t parts = int32_t((a.vocab + 63) / 64);
+        const int64_t blocks = (a.tokens + 31) / 32 * parts;
+        if (blocks > INT32_MAX) return cudaErrorNotSupported;
+        return launch_ex(grad_any_kernel<T, true>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
+    }
+    // logits and gradients of every row start alike past a 16-byte boundary
+    const bool alike = row_head<T>(a.x) == row_head<T>(a.dx) && (a.tokens == 1 || (a.ld - a.ldd) * int64_t(sizeof(T)) % 16 == 0);
+    const int64_t per = alike ? int64_t(kGradThreads) * kGradUnroll * kPerGranule<T> : int64_t(kGradThreads) * 8;
+    const int32_t parts = int32_t((a.vocab + kPerGranule<T> - 1 + per - 1) / per);
+    const int64_t blocks = a.tokens * parts;
+    if (blocks > INT32_MAX) return cudaErrorNotSupported;
+    if (alike) return launch_ex(grad_rows_kernel<T>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
+    return launch_ex(grad_any_kernel<T, false>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
+}
+
+darb_status_t status_of(cudaError_t e) {
+    if (e == cudaSuccess) return DARB_OK;
+    cudaGetLastError();
+    return e == cudaErrorNotSupported ? DARB_ERR_UNSUPPORTED : DARB_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace darb
+
+using namespace darb;
+
+extern "C" {
+
+darb_status_t darb_token_logprobs(const void *logits, darb_dtype_t dtype, darb_layout_t layout, int64_t tokens,
+                                  int64_t vocab, int64_t ld, const int64_t *targets, int32_t k, float *logprob,
+                                  float *entropy, float *lse, float *top_logprob, int32_t *top_index,
+                                  cudaStream_t stream) {
+    DARB_TRACE("darb_token_logprobs");
+    if (!token_dtype(dtype) || !token_layout(layout) || tokens < 0 || vocab <= 0 || k < 0 || k > DARB_MAX_TOP || k > vocab)
+        return DARB_ERR_INVALID_ARG;
+    if (ld < (layout == DARB_TOKEN_ROWS ? vocab : tokens)) return DARB_ERR_INVALID_ARG;
+    if (tokens == 0) return DARB_OK;
+    if (logits == nullptr || !aligned_to(logits, dtype_size(dtype)) || (targets == nullptr) != (logprob == nullptr) ||
+        !aligned_to(targets, 8) || !aligned_to(logprob, 4) || !aligned_to(entropy, 4) || !aligned_to(lse, 4))
+        return DARB_ERR_INVALID_ARG;
+    if (k > 0 && (top_logprob == nullptr || top_index == nullptr || !aligned_to(top_logprob, 4) || !aligned_to(top_index, 4)))
+        return DARB_ERR_INVALID_ARG;
+    if (tokens > kMaxTokens || vocab > kMaxFeatures) return DARB_ERR_UNSUPPORTED;
+    const int64_t span = token_span(layout, 1, tokens, vocab, ld);
+    if (span < 0) return DARB_ERR_UNSUPPORTED;
+    const Range outs[] = {{logprob, tokens * 4}, {entropy, tokens * 4}, {lse, tokens * 4}, {k ? top_logprob : nullptr, tokens * k * 4},
+                          {k ? top_index : nullptr, tokens * k * 4}};
+    const Range ins[] = {{logits, span * int64_t(dtype_size(dtype))}, {targets, tokens * 8}};
+    if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
+    const ScoreArgs a = {logits, ld, tokens, int32_t(vocab), k, targets, logprob, entropy, lse, top_logprob, top_index};
+    if (layout == DARB_TOKEN_ROWS)
+        return status_of(dtype == DARB_BF16 ? launch_score_rows<__nv_bfloat16>(a, stream) : launch_score_rows<float>(a, stream));
+    return status_of(dtype == DARB_BF16 ? launch_score_columns<__nv_bfloat16>(a, stream) : launch_score_columns<float>(a, stream));
+}
+
+darb_status_t darb_token_logprobs_grad(const void *logits, darb_dtype_t dtype, darb_layout_t layout, int64_t tokens,
+                                       int64_t vocab, int64_t ld, const int64_t *targets, const float *lse,
+                                       const float *entropy, const float *d_logprob, const float *d_entropy,
+                                       void *d_logits, int64_t ld_grad, cudaStream_t stream) {
+    DARB_TRACE("darb_token_logprobs_grad");
+    if (!token_dtype(dtype) || !token_layout(layout) || tokens < 0 || vocab <= 0) return DARB_ERR_INVALID_ARG;
+    const int64_t least = layout == DARB_TOKEN_ROWS ? vocab : tokens;
+    if (ld < least || ld_grad < least) return DARB_ERR_INVALID_ARG;
+    if (tokens == 0) return DARB_OK;
+    const size_t es = dtype_size(dtype);
+    if (logits == nullptr || d_logits == nullptr || lse == nullptr || !aligned_to(logits, es) || !aligned_to(d_logits, es) ||
+        !aligned_to(lse, 4) || !aligned_to(entropy, 4) || !aligned_to(d_logprob, 4) || !aligned_to(d_entropy, 4) ||
+        !aligned_to(targets, 8))
+        return DARB_ERR_INVALID_ARG;
+    if ((d_logprob != nullptr && targets == nullptr) || (d_entropy != nullptr && entropy == nullptr)) return DARB_ERR_INVALID_ARG;
+    if (tokens > kMaxTokens || vocab > kMaxFeatures) return DARB_ERR_UNSUPPORTED;
+    const int64_t span = token_span(layout, 1, tokens, vocab, ld), span_grad = token_span(layout, 1, tokens, vocab, ld_grad);
+    if (span < 0 || span_grad < 0) return DARB_ERR_UNSUPPORTED;
+    // the gradient may take the logits' place: every element is read before it is written
+    const bool in_place = logits == d_logits && ld == ld_grad;
+    const Range outs[] = {{d_logits, span_grad * int64_t(es)}};
+    const Range ins[] = {{in_place ? nullptr : logits, span * int64_t(es)}, {targets, tokens * 8}, {lse, tokens * 4},
+                         {entropy, tokens * 4}, {d_logprob, tokens * 4}, {d_entropy, tokens * 4}};
+    if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
+    const GradArgs a = {logits, d_logits, ld, ld_grad, tokens, int32_t(vocab), targets, lse, entropy, d_logprob, d_entropy};
+    return status_of(dtype == DARB_BF16 ? launch_grad<__nv_bfloat16>(a, layout, stream) : launch_grad<float>(a, layout, stream));
+}
+
+}  // extern "C"

@@ -11,6 +11,7 @@ import ctypes
 import os
 import threading
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import numpy as np
 
@@ -20,7 +21,10 @@ LIB_PATH = os.path.join(_PKG, "libdarb.so")
 OK, ERR_INVALID_ARG, ERR_NONFINITE, ERR_OOM, ERR_CUDA, ERR_TIMEOUT, ERR_UNSUPPORTED = range(7)
 F32, BF16 = 0, 1
 PATH_AUTO, PATH_CUDA_CORES, PATH_TENSOR_CORES = 0, 1, 2
+TOKEN_ROWS, TOKEN_COLUMNS = 0, 1
 MAX_BLOCK = 256
+MAX_TOP = 32
+ADAMW_BLOCK = 256
 
 _lock = threading.Lock()
 _lib = None
@@ -75,6 +79,17 @@ def lib():
                 "darb_import": [P, P, P, ctypes.c_int, I64, I64, P, S],
                 "darb_destroy": [P],
                 "darb_set_pdl": [ctypes.c_int],
+                "darb_token_logprobs": [P, ctypes.c_int, ctypes.c_int, I64, I64, I64, P, I32, P, P, P, P, P, S],
+                "darb_token_logprobs_grad": [P, ctypes.c_int, ctypes.c_int, I64, I64, I64, P, P, P, P, P, P, I64, S],
+                "darb_layer_norm": [P, ctypes.c_int, ctypes.c_int, I64, I64, I64, I64, P, P, ctypes.c_float, P, I64,
+                                    P, P, S],
+                "darb_layer_norm_grad": [P, I64, P, I64, ctypes.c_int, ctypes.c_int, I64, I64, I64, P, P, P, P, I64,
+                                         P, P, P, S],
+                "darb_layer_norm_grad_work": [ctypes.c_int, I64, I64, I64, P],
+                "darb_adamw_create": [I32, P, P, P, P, P, P, P, ctypes.c_int, P, S],
+                "darb_adamw_step": [P, P, P, I64, ctypes.c_uint64, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                                    ctypes.c_double, ctypes.c_double, S],
+                "darb_adamw_destroy": [P],
             }
             for name, args in sig.items():
                 fn = getattr(L, name)
@@ -372,3 +387,311 @@ def darb_destroy(h: Handle | None):
 def darb_set_pdl(enabled: bool):
     """Launch the library's kernels with (default) or without programmatic dependent launch."""
     _check(lib().darb_set_pdl(1 if enabled else 0), "darb_set_pdl")
+
+
+# ---- scoring and training around a pruned layer ----
+
+def _refuse(call: str, what: str):
+    raise DarbError(ERR_INVALID_ARG, f"{call}: {what}")
+
+
+def _value_code(t, call: str, name: str) -> int:
+    """The type code of a CUDA tensor of activations."""
+    torch = _torch or _load_torch()
+    if not t.is_cuda:
+        _refuse(call, f"{name} must be a CUDA tensor")
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    _refuse(call, f"{name} must be float32 or bfloat16")
+
+
+def _vector(t, n: int, dtype, call: str, name: str) -> int | None:
+    """The pointer of a dense CUDA vector of n values, or None."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        _refuse(call, f"{name} must be a contiguous CUDA {dtype} tensor of {n} values")
+    return t.data_ptr()
+
+
+def _new(shape, dtype, device, stream):
+    """A new tensor, kept from reuse while `stream` (if it is not the current one) may still work on it."""
+    t = _torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(_torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+    return t
+
+
+def _tokens(t, dim: int, call: str, name: str) -> tuple[int, int, int, int, int]:
+    """(layout, steps, tokens, features, ld) of a tensor whose features lie along `dim`: 2-D with
+    either axis contiguous, or 3-D (steps, features, tokens) with contiguous tokens."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 2:
+        if dim not in (-2, -1, 0, 1):
+            _refuse(call, f"no axis {dim}")
+        f, n = (shape[1], shape[0]) if dim % 2 else shape
+        fs, ns = (strides[1], strides[0]) if dim % 2 else strides
+        if fs == 1 or f == 1:
+            return TOKEN_ROWS, 1, n, f, ns if n > 1 else f
+        if ns == 1 or n == 1:
+            return TOKEN_COLUMNS, 1, n, f, fs
+        _refuse(call, f"an axis of {name} must be contiguous")
+    if len(shape) != 3 or dim not in (1, -2):
+        _refuse(call, f"{name} must be 2-D, or 3-D (steps, features, tokens) with dim=1")
+    steps, f, n = shape
+    ld = strides[1] if f > 1 else strides[0] if steps > 1 else n
+    if (n > 1 and strides[2] != 1) or (steps > 1 and strides[0] != f * ld):
+        _refuse(call, f"{name} must have contiguous tokens and steps one after the other")
+    return TOKEN_COLUMNS, steps, n, f, ld
+
+
+def _same_tokens(t, like, dim: int, layout: int, call: str, name: str) -> int:
+    """The leading dimension of a tensor of the shape, type and layout of another."""
+    if not t.is_cuda or t.dtype != like.dtype or t.shape != like.shape:
+        _refuse(call, f"{name} must be a CUDA tensor of the input's shape and type")
+    strides = t.stride()
+    f, n = (t.shape[dim], t.shape[1 - dim % 2 if t.dim() == 2 else 2])
+    fs, ns = (strides[dim], strides[1 - dim % 2 if t.dim() == 2 else 2])
+    steps = 1 if t.dim() == 2 else t.shape[0]
+    if layout == TOKEN_ROWS:
+        if f > 1 and fs != 1:
+            _refuse(call, f"{name} must have contiguous features, as the input")
+        return ns if n > 1 else f
+    ld = fs if f > 1 else strides[0] if steps > 1 else n
+    if (n > 1 and ns != 1) or (steps > 1 and strides[0] != f * ld):
+        _refuse(call, f"{name} must have contiguous tokens, as the input")
+    return ld
+
+
+class TokenLogprobs(NamedTuple):
+    """Results of darb_token_logprobs: float32 (tokens,) and, of the k alternatives, float32 and int32 (tokens, k)."""
+    logprob: object
+    entropy: object
+    lse: object
+    top_logprob: object
+    top_index: object
+
+    @staticmethod
+    def empty(tokens: int, k: int = 0, device="cuda", stream=None) -> "TokenLogprobs":
+        """Buffers for the results of `tokens` tokens, to be passed as `out`."""
+        torch = _torch or _load_torch()
+        f32 = [_new((tokens,), torch.float32, device, stream) for _ in range(3)]
+        return TokenLogprobs(*f32, _new((tokens, k), torch.float32, device, stream),
+                             _new((tokens, k), torch.int32, device, stream))
+
+
+def darb_token_logprobs(logits, targets=None, k: int = 0, dim: int = -1, out: TokenLogprobs | None = None,
+                        stream=None) -> TokenLogprobs:
+    """Log probability of the given entries, entropy, log of the sum of exponentials and the k most
+    probable entries of each token, from its logits.
+
+    logits: 2-D float32 or bfloat16, the vocabulary along `dim` (-1: tokens x vocab; 0: vocab x tokens,
+    what darb_spmm returns), either axis contiguous.  targets: int64 (tokens,), negative for none; without
+    targets there is no logprob.  out: buffers to write (entries may be None: not wanted)."""
+    call = "darb_token_logprobs"
+    code = _value_code(logits, call, "logits")
+    if logits.dim() != 2:
+        _refuse(call, "logits must be 2-D")
+    if k < 0:
+        _refuse(call, "k must not be negative")
+    layout, _, n, v, ld = _tokens(logits, dim, call, "logits")
+    torch = _torch
+    if out is None:
+        out = TokenLogprobs.empty(n, k, logits.device, stream)
+        if targets is None:
+            out = out._replace(logprob=None)
+    f32 = torch.float32
+    logprob = None if targets is None else _vector(out.logprob, n, f32, call, "logprob")
+    top = (_vector(out.top_logprob, n * k, f32, call, "top_logprob"),
+           _vector(out.top_index, n * k, torch.int32, call, "top_index")) if k else (None, None)
+    _check(lib().darb_token_logprobs(logits.data_ptr(), code, layout, n, v, ld,
+                                     None if logprob is None else _vector(targets, n, torch.int64, call, "targets"), k, logprob,
+                                     _vector(out.entropy, n, f32, call, "entropy"), _vector(out.lse, n, f32, call, "lse"),
+                                     *top, _stream(stream)), call)
+    return out
+
+
+def darb_token_logprobs_grad(logits, targets, lse, d_logprob, entropy=None, d_entropy=None, dim: int = -1, out=None,
+                             stream=None):
+    """The gradient with respect to the logits, given those of log probability (d_logprob) and entropy
+    (d_entropy); lse and entropy are the forward call's.  out: a tensor of the logits' shape, type and
+    layout, or the logits themselves; a new one if None."""
+    call = "darb_token_logprobs_grad"
+    code = _value_code(logits, call, "logits")
+    if logits.dim() != 2:
+        _refuse(call, "logits must be 2-D")
+    layout, _, n, v, ld = _tokens(logits, dim, call, "logits")
+    torch = _torch
+    if out is None:
+        out = _new((n, v) if layout == TOKEN_ROWS else (v, n), logits.dtype, logits.device, stream)
+        if (layout == TOKEN_ROWS) != (dim % 2 == 1):
+            out = out.t()
+    ld_out = _same_tokens(out, logits, dim, layout, call, "out")
+    f32 = torch.float32
+    _check(lib().darb_token_logprobs_grad(logits.data_ptr(), code, layout, n, v, ld,
+                                          _vector(targets, n, torch.int64, call, "targets"), _vector(lse, n, f32, call, "lse"),
+                                          _vector(entropy, n, f32, call, "entropy"),
+                                          _vector(d_logprob, n, f32, call, "d_logprob"),
+                                          _vector(d_entropy, n, f32, call, "d_entropy"), out.data_ptr(), ld_out,
+                                          _stream(stream)), call)
+    return out
+
+
+def darb_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, dim: int = -1, y=None, mean=None, rstd=None,
+                    stream=None):
+    """(y, mean, rstd): layer norm over the features of each token, which lie along `dim`.
+
+    x: float32 or bfloat16, 2-D with either axis contiguous (dim=-1: tokens x features; dim=0: features x
+    tokens, as the steps write h) or 3-D (steps, features, tokens) with dim=1, as the sequence calls write
+    h_seq.  gamma, beta: float32 (features,) or None.  y may be x; mean and rstd: float32, a value a token."""
+    call = "darb_layer_norm"
+    code = _value_code(x, call, "x")
+    layout, steps, n, f, ld = _tokens(x, dim, call, "x")
+    f32 = _torch.float32
+    if y is None:
+        y = _new_like(x, dim, layout, steps, n, f, stream)
+    lead = (steps, n) if x.dim() == 3 else (n,)
+    if mean is None:
+        mean = _new(lead, f32, x.device, stream)
+    if rstd is None:
+        rstd = _new(lead, f32, x.device, stream)
+    _check(lib().darb_layer_norm(x.data_ptr(), code, layout, steps, n, f, ld, _vector(gamma, f, f32, call, "gamma"),
+                                 _vector(beta, f, f32, call, "beta"), eps, y.data_ptr(),
+                                 _same_tokens(y, x, dim, layout, call, "y"), _vector(mean, steps * n, f32, call, "mean"),
+                                 _vector(rstd, steps * n, f32, call, "rstd"), _stream(stream)), call)
+    return y, mean, rstd
+
+
+def _new_like(x, dim: int, layout: int, steps: int, n: int, f: int, stream):
+    """A dense tensor of x's shape and type whose contiguous axis is x's."""
+    if x.dim() == 3:
+        return _new((steps, f, n), x.dtype, x.device, stream)
+    t = _new((n, f) if layout == TOKEN_ROWS else (f, n), x.dtype, x.device, stream)
+    return t if (layout == TOKEN_ROWS) == (dim % 2 == 1) else t.t()
+
+
+def darb_layer_norm_grad(dy, x, gamma, mean, rstd, dim: int = -1, dx=None, dgamma=None, dbeta=None, weights: bool = True,
+                         work=None, stream=None):
+    """(dx, dgamma, dbeta): the backward pass of darb_layer_norm (dx may be dy).  weights=False leaves
+    dgamma and dbeta out (None).  work: scratch of darb_layer_norm_grad_work bytes, a new one if None."""
+    call = "darb_layer_norm_grad"
+    code = _value_code(x, call, "x")
+    layout, steps, n, f, ld = _tokens(x, dim, call, "x")
+    f32 = _torch.float32
+    if dx is None:
+        dx = _new_like(x, dim, layout, steps, n, f, stream)
+    pg = pb = pw = None
+    if weights:
+        if dgamma is None:
+            dgamma = _new((f,), f32, x.device, stream)
+        if dbeta is None:
+            dbeta = _new((f,), f32, x.device, stream)
+        pg, pb = _vector(dgamma, f, f32, call, "dgamma"), _vector(dbeta, f, f32, call, "dbeta")
+        need = darb_layer_norm_grad_work(layout, steps, n, f)
+        if work is None:
+            work = _new((need,), _torch.uint8, x.device, stream)
+        elif not work.is_cuda or not work.is_contiguous() or work.numel() * work.element_size() < need:
+            _refuse(call, f"work must be a contiguous CUDA tensor of {need} bytes")
+        pw = work.data_ptr()
+    else:
+        dgamma = dbeta = None
+    _check(lib().darb_layer_norm_grad(dy.data_ptr(), _same_tokens(dy, x, dim, layout, call, "dy"), x.data_ptr(), ld, code,
+                                      layout, steps, n, f, _vector(gamma, f, f32, call, "gamma"),
+                                      _vector(mean, steps * n, f32, call, "mean"), _vector(rstd, steps * n, f32, call, "rstd"),
+                                      dx.data_ptr(), _same_tokens(dx, x, dim, layout, call, "dx"), pg, pb, pw,
+                                      _stream(stream)), call)
+    return dx, dgamma, dbeta
+
+
+def darb_layer_norm_grad_work(layout: int, steps: int, tokens: int, features: int) -> int:
+    """Bytes of scratch that darb_layer_norm_grad needs (layout: TOKEN_ROWS or TOKEN_COLUMNS)."""
+    need = ctypes.c_int64()
+    _check(lib().darb_layer_norm_grad_work(layout, steps, tokens, features, ctypes.byref(need)),
+           "darb_layer_norm_grad_work")
+    return need.value
+
+
+class AdamW:
+    """A plan of darb_adamw_create (owned; free with darb_adamw_destroy).  Holds on to its tensors."""
+
+    def __init__(self, ptr: int, tensors, numels, grad_dtype):
+        self.ptr, self.tensors, self.numels, self.grad_dtype = ptr, tensors, numels, grad_dtype
+        self.pointers = (ctypes.c_void_p * len(numels))()
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        darb_adamw_destroy(self)
+
+
+def darb_adamw_create(params, m, v, m_scale=None, v_scale=None, copies=None, grad_dtype=None, stream=None) -> AdamW:
+    """A plan for AdamW steps over the float32 CUDA tensors `params`, all tensors contiguous.
+
+    m, v: the moments, float32 of the parameters' sizes; or, with m_scale and v_scale (float32, one value
+    for every ADAMW_BLOCK elements of a tensor), float8_e4m3fn (or uint8) codes of m and of sqrt(v).
+    copies: bfloat16 tensors (or None) that receive the rounded parameters, e.g. for darb_reencode.
+    grad_dtype: float32 (default) or bfloat16."""
+    call = "darb_adamw_create"
+    torch = _torch or _load_torch()
+    params, m, v = list(params), list(m), list(v)
+    n = len(params)
+    lists = [params, m, v] + [None if t is None else list(t) for t in (m_scale, v_scale, copies)]
+    if any(t is not None and len(t) != n for t in lists):
+        _refuse(call, "one state (and scale and copy) for every parameter")
+    if (m_scale is None) != (v_scale is None):
+        _refuse(call, "m_scale and v_scale go together")
+    codes = (torch.float8_e4m3fn, torch.uint8)
+    states = codes if m_scale is not None else (torch.float32,)
+    grad_dtype = torch.float32 if grad_dtype is None else grad_dtype
+    if grad_dtype not in (torch.float32, torch.bfloat16):
+        _refuse(call, "grad_dtype must be float32 or bfloat16")
+    kinds = [(torch.float32,), states, states, (torch.float32,), (torch.float32,), (torch.bfloat16,)]
+    names = ("params", "m", "v", "m_scale", "v_scale", "copies")
+    numels = [p.numel() for p in params]
+    pointers = []
+    for name, tensors, dtypes in zip(names, lists, kinds):
+        if tensors is None:
+            pointers.append(None)
+            continue
+        for t, size in zip(tensors, numels):
+            if t is None and name == "copies":
+                continue
+            want = -(-size // ADAMW_BLOCK) if name.endswith("scale") else size
+            if not t.is_cuda or t.dtype not in dtypes or t.numel() != want or not t.is_contiguous():
+                _refuse(call, f"{name} must be contiguous CUDA tensors of {' or '.join(map(str, dtypes))}, {want} values here")
+        pointers.append((ctypes.c_void_p * n)(*[None if t is None else t.data_ptr() for t in tensors]))
+    out = ctypes.c_void_p()
+    _check(lib().darb_adamw_create(n, (ctypes.c_int64 * n)(*numels), *pointers, BF16 if grad_dtype == torch.bfloat16 else F32,
+                                   ctypes.byref(out), _stream(stream)), call)
+    return AdamW(out.value, lists, numels, grad_dtype)
+
+
+def darb_adamw_step(plan: AdamW, grads, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                    weight_decay: float = 0.01, grad_scale=None, seed: int | None = None, stream=None):
+    """One step (step >= 1) with the gradients `grads` of the plan's tensors (None: that tensor is left as it
+    is).  grad_scale: float32 CUDA scalar that multiplies every gradient.  seed: of the rounding of states in
+    8 bits, the step itself if None."""
+    call = "darb_adamw_step"
+    pointers, dtype = plan.pointers, plan.grad_dtype
+    if len(grads) != len(plan.numels):
+        _refuse(call, "one gradient for every parameter")
+    for i, (g, n) in enumerate(zip(grads, plan.numels)):
+        if g is None:
+            pointers[i] = None
+            continue
+        if g.dtype != dtype or not g.is_cuda or g.numel() != n or not g.is_contiguous():
+            _refuse(call, f"gradient {i} must be a contiguous CUDA {dtype} tensor of {n} values")
+        pointers[i] = g.data_ptr()
+    _check(lib().darb_adamw_step(plan.ptr, pointers, _vector(grad_scale, 1, (_torch or _load_torch()).float32, call, "grad_scale"),
+                                 step, (step if seed is None else seed) & 0xFFFFFFFFFFFFFFFF, lr, beta1, beta2, eps,
+                                 weight_decay, _stream(stream)), call)
+
+
+def darb_adamw_destroy(plan: AdamW | None):
+    if plan is None or plan.ptr is None:
+        return
+    _check(lib().darb_adamw_destroy(plan.ptr), "darb_adamw_destroy")
+    plan.ptr = None
