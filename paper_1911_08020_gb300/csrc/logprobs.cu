@@ -57,13 +57,15 @@ struct ScoreArgs {
     int32_t *top_index;
 };
 
-// A partial result over some of a token's logits.
+// A partial result over some of a token's logits: its largest (clamped) logit,
+// and the sums relative to r = reference(m).
 struct Part {
     float m, s, t;
 };
 __device__ __forceinline__ Part empty_part() { return {kMasked, 0.0f, 0.0f}; }
+__device__ __forceinline__ float reference(float m) { return __fmul_rn(m, kLog2e); }
 __device__ __forceinline__ Part rescaled(const Part &p, float m) {
-    const float d = p.m * kLog2e - m * kLog2e;
+    const float d = __fsub_rn(reference(p.m), reference(m));
     const float f = exp2_fast(d);
     return {m, f * p.s, f * (p.t + p.s * d)};
 }
@@ -78,6 +80,28 @@ __device__ __forceinline__ Part warp_join(Part p) {
         p.t += __shfl_xor_sync(0xFFFFFFFFu, p.t, o);
     }
     return p;
+}
+
+// A thread's running sums, and one block of N of its logits (clamped, the
+// largest of them `top`) added to them: the block is summed by itself first, so
+// that no addition chain is longer than a block plus the number of blocks.
+struct Running {
+    float m, r;
+    float2 s, t;
+};
+__device__ __forceinline__ Running no_sums() { return {kMasked, kMasked * kLog2e, {0.0f, 0.0f}, {0.0f, 0.0f}}; }
+__device__ __forceinline__ void rebase(Running &a, float top) {
+    a.m = max_nan(a.m, top);
+    const float r = reference(a.m), d = __fsub_rn(a.r, r), f = exp2_fast(d);
+    a.t = mul2(both(f), fma2(a.s, both(d), a.t));
+    a.s = mul2(both(f), a.s);
+    a.r = r;
+}
+__device__ __forceinline__ void add_pair(float2 x, float r, float2 &s, float2 &t) {
+    const float2 d = fma2(x, both(kLog2e), both(-r));
+    const float2 e = make_float2(exp2_fast(d.x), exp2_fast(d.y));
+    s = add2(s, e);
+    t = fma2(e, d, t);
 }
 
 // Logits in order of value: larger logits have larger keys, NaN the largest,
@@ -112,7 +136,7 @@ struct Token {
     __device__ float lse() const { return empty ? -INFINITY : wide ? m + log2s * kLn2 : (r + log2s) * kLn2; }
 };
 __device__ __forceinline__ Token token_of(const Part &p) {
-    return {p.m * kLog2e, p.m, log2f(p.s), p.t / p.s, false, false};
+    return {reference(p.m), p.m, log2f(p.s), p.t / p.s, false, false};
 }
 // Whether a token's fast partial result does not stand (a NaN one does).
 __device__ __forceinline__ bool is_wide(float m) { return m < -kWide || m > kWide; }
@@ -277,15 +301,28 @@ __device__ __forceinline__ void clamp_block(uint4 (&q)[N], float &m, __nv_bfloat
     m = max_nan(m, max_nan(__low2float(mm), __high2float(mm)));
 }
 
+// The blocks that a thread's share of the logits is cut into: `rounds` rounds of
+// U granules, `per_slot` of them sharing a slot of the table of maxima.
+struct Blocks {
+    int32_t slots, per_slot;
+};
+inline Blocks blocks_of(int64_t rounds, int most) {
+    const int64_t per = std::max<int64_t>(1, (rounds + most - 1) / most);
+    return {int32_t((rounds + per - 1) / per), int32_t(per)};
+}
+constexpr int kRowSlots = 32;   // of the table of maxima, at most
+
+constexpr int kItems = 256;   // blocks that may hold one of the k largest, at most
+
 template <typename T, int THREADS, int U>
-__global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a) {
+__global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, const Blocks blocks) {
     constexpr int V = kPerGranule<T>;
     constexpr int W = THREADS / 32;
-    __shared__ Part warp_part[W];
-    __shared__ Part cta_part;
-    __shared__ float thread_max[THREADS];
+    extern __shared__ float block_max[];   // [slots][THREADS], for k > 0
+    __shared__ Part warp_part[W], cta_part;
+    __shared__ float thread_max[THREADS], s_bar;
     __shared__ uint64_t cand[kCandidates], sel[kMaxTop], sorted[kMaxTop];
-    __shared__ uint32_t hist[256], ctl[4], ncand;
+    __shared__ uint32_t items[kItems], hist[256], ctl[4], nitems, ncand;
     __shared__ float buf[33];
     pdl_wait_previous();
     pdl_launch_dependents();
@@ -295,107 +332,139 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a) 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const T *row = static_cast<const T *>(a.x) + token * a.ld;
     const int head = row_head<T>(row);
-    const int32_t n = a.vocab, granules = int32_t(row_granules<T>(head, n));
+    const int32_t n = a.vocab, granules = int32_t(row_granules<T>(head, n)), k = a.k;
     const int32_t g0 = int32_t(int64_t(granules) * rank / split), g1 = int32_t(int64_t(granules) * (rank + 1) / split);
+    const auto fetch = [&](int32_t g) {
+        return load_granule(row, g < g1 ? int64_t(g) * V - head : int64_t(n), n, -INFINITY);
+    };
+    uint4 next[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = fetch(g0 + tid + u * THREADS);
     int64_t target = -1;
     float target_x = 0.0f;
-    if (tid == 0 && rank == 0 && a.targets != nullptr) {
-        target = a.targets[token];
-        if (target >= 0 && target < n) target_x = widen(row[target]);
+    if (tid == 0) {
+        nitems = ncand = 0;
+        if (rank == 0 && a.targets != nullptr) {
+            target = a.targets[token];
+            if (target >= 0 && target < n) target_x = widen(row[target]);
+        }
     }
-    if (tid == 0) ncand = 0;
 
-    float m = kMasked;
-    float2 s2 = both(0.0f), t2 = both(0.0f);
-    for (int32_t g = g0 + tid; g < g1; g += THREADS * U) {
+    Running sum = no_sums();
+    int slot = 0, in_slot = 0;
+    float slot_max = kMasked;
+    for (int32_t g = g0 + tid; g - tid < g1; g += THREADS * U) {
         uint4 q[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t gu = g + u * THREADS;
-            q[u] = load_granule(row, gu < g1 ? int64_t(gu) * V - head : int64_t(n), n, -INFINITY);
+        for (int u = 0; u < U; ++u) q[u] = next[u];
+        if (g - tid + THREADS * U < g1) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) next[u] = fetch(g + THREADS * U + u * THREADS);
         }
-        float top = m;
+        float top = kMasked;
         clamp_block(q, top, T());
-        {
-            const float d = m * kLog2e - top * kLog2e, f = exp2_fast(d);
-            t2 = mul2(both(f), fma2(s2, both(d), t2));
-            s2 = mul2(both(f), s2);
-            m = top;
+        if (k > 0) {
+            slot_max = max_nan(slot_max, top);
+            if (++in_slot == blocks.per_slot) {
+                block_max[slot++ * THREADS + tid] = slot_max;
+                slot_max = kMasked;
+                in_slot = 0;
+            }
         }
-        const float2 l2 = both(kLog2e), r2 = both(-(m * kLog2e));
+        rebase(sum, top);
+        float2 s2 = both(0.0f), t2 = both(0.0f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float v[V];
             unpack(q[u], v);
 #pragma unroll
-            for (int i = 0; i < V; i += 2) {
-                const float2 d = fma2(make_float2(v[i], v[i + 1]), l2, r2);
-                const float2 e = make_float2(exp2_fast(d.x), exp2_fast(d.y));
-                s2 = add2(s2, e);
-                t2 = fma2(e, d, t2);
-            }
+            for (int i = 0; i < V; i += 2) add_pair(make_float2(v[i], v[i + 1]), sum.r, s2, t2);
         }
+        sum.s = add2(sum.s, s2);
+        sum.t = add2(sum.t, t2);
     }
-    thread_max[tid] = m;
-    const Part mine = warp_join({m, s2.x + s2.y, t2.x + t2.y});
+    if (k > 0) {
+        if (in_slot > 0) block_max[slot++ * THREADS + tid] = slot_max;
+        thread_max[tid] = sum.m;
+    }
+    const Part mine = warp_join({sum.m, sum.s.x + sum.s.y, sum.t.x + sum.t.y});
     if (lane == 0) warp_part[warp] = mine;
     __syncthreads();
-    // every warp joins the partial results of all, in the same order
-    const Part all = warp_join(lane < W ? warp_part[lane] : empty_part());
-    if (split > 1 && tid == 0) cta_part = all;
-
-    const int k = a.k;
+    Part all;   // of the CTA; warp 0 has it
+    if (warp == 0) {
+        all = warp_join(lane < W ? warp_part[lane] : empty_part());
+        if (lane == 0) cta_part = all;
+        if (k > 0) {
+            // The k-th largest of 32 maxima over disjoint sets of logits is at most the
+            // k-th largest logit, so only blocks that reach it can hold one of the k largest.
+            float g = thread_max[lane];
+#pragma unroll
+            for (int w = 1; w < W; ++w) g = max_nan(g, thread_max[w * 32 + lane]);
+            const float bar = kth_of_warp(g, k);
+            if (lane == 0) s_bar = bar > kMasked && all.m == all.m ? bar : __uint_as_float(0x7FC00000u);
+        }
+    }
     if (k > 0) {
-        // The k-th largest of 32 maxima over disjoint sets of logits is at most the
-        // k-th largest logit, so only logits from there on can be among the k
-        // largest, and only threads whose maximum reaches it look at theirs again.
-        float g = thread_max[lane];
-        for (int w = 1; w < W; ++w) g = max_nan(g, thread_max[w * 32 + lane]);
-        const float bar = kth_of_warp(g, k);
-        const bool plain = bar > kMasked && all.m == all.m;   // the same for all threads
-        if (plain && m >= bar) {
-            for (int32_t gi = g0 + tid; gi < g1; gi += THREADS) {
+        __syncthreads();
+        const float bar = s_bar;   // NaN: the maxima say nothing
+        if (sum.m >= bar)
+            for (int i = 0; i < slot; ++i)
+                if (block_max[i * THREADS + tid] >= bar) {
+                    const uint32_t p = atomicAdd(&nitems, 1u);
+                    if (p < kItems) items[p] = uint32_t(i * THREADS + tid);
+                }
+        __syncthreads();
+        int found = int(nitems);
+        const bool listed = bar == bar && found <= kItems;
+        if (listed) {
+            // the granules of the listed blocks, all at once
+            const int per = U * blocks.per_slot;
+            for (int i = tid; i < found * per; i += THREADS) {
+                const int32_t item = int32_t(items[i / per]), j = i % per;
+                const int32_t g = g0 + ((item / THREADS) * blocks.per_slot + j / U) * (THREADS * U) + (j % U) * THREADS + item % THREADS;
+                if (g >= g1) continue;
                 float v[V];
-                const int64_t j0 = int64_t(gi) * V - head;
+                const int64_t j0 = int64_t(g) * V - head;
                 unpack(load_granule(row, j0, n, -INFINITY), v);
 #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (v[i] >= bar) {
+                for (int e = 0; e < V; ++e)
+                    if (v[e] >= bar) {
                         const uint32_t p = atomicAdd(&ncand, 1u);
-                        if (p < kCandidates) cand[p] = key_of(v[i], int32_t(j0 + i));
+                        if (p < kCandidates) cand[p] = key_of(v[e], int32_t(j0 + e));
                     }
             }
+            if (tid < kMaxTop) sorted[tid] = 0;
+            __syncthreads();
+            found = int(ncand);
         }
-        __syncthreads();
-        int found = int(ncand);
-        if (!plain || found > kCandidates) {
+        if (!listed || found > kCandidates) {
             const int32_t i0 = max(0, g0 * V - head), i1 = min(n, g1 * V - head);
             select_any(row, 1, i0, i1, k, sel, hist, ctl);
-            if (tid < kMaxTop) cand[tid] = sel[tid];
+            if (tid < kMaxTop) cand[tid] = sel[tid], sorted[tid] = 0;
             found = kMaxTop;
+            __syncthreads();
         }
-        if (tid < kMaxTop) sorted[tid] = 0;
-        __syncthreads();
         rank_keys(cand, found, k, sorted, tid, THREADS);
     }
-    Part whole = all;
     if (split > 1) {
         cluster.sync();
         if (rank == 0) {
-            whole = empty_part();
-            if (lane < split) whole = *cluster.map_shared_rank(&cta_part, lane);
-            whole = warp_join(whole);
-            const int total = split * k;
-            for (int i = tid; i < total; i += THREADS) cand[i] = cluster.map_shared_rank(sorted, i / k)[i % k];
+            if (warp == 0) {
+                all = empty_part();
+                if (lane < split) all = *cluster.map_shared_rank(&cta_part, lane);
+                all = warp_join(all);
+            }
+            for (int i = tid; i < split * k; i += THREADS) cand[i] = cluster.map_shared_rank(sorted, i / k)[i % k];
         }
         cluster.sync();   // the other CTAs may leave: nothing reads them any more
         if (rank != 0) return;
-        if (k > 0) {
-            if (tid < kMaxTop) sorted[tid] = 0;
-            __syncthreads();
-            rank_keys(cand, split * k, k, sorted, tid, THREADS);
-        }
+        if (warp == 0 && lane == 0) cta_part = all;
+        if (tid < kMaxTop) sorted[tid] = 0;
+        __syncthreads();
+        rank_keys(cand, split * k, k, sorted, tid, THREADS);
     }
+    __syncthreads();
+    const Part whole = cta_part;
     Token tok;
     if (is_wide(whole.m)) tok = wide_token(row, 1, n, buf);
     else tok = token_of(whole);
@@ -404,13 +473,10 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a) 
         if (a.entropy) a.entropy[token] = tok.entropy();
         if (a.lse) a.lse[token] = tok.lse();
     }
-    if (k > 0) {
-        __syncthreads();
-        if (tid < k) {
-            const uint64_t key = sorted[tid];
-            a.top_logprob[token * k + tid] = tok.logprob(value_of(uint32_t(key >> 32)));
-            a.top_index[token * k + tid] = index_of(key);
-        }
+    if (tid < k) {
+        const uint64_t key = sorted[tid];
+        a.top_logprob[token * k + tid] = tok.logprob(value_of(uint32_t(key >> 32)));
+        a.top_index[token * k + tid] = index_of(key);
     }
 }
 
@@ -421,6 +487,8 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a) 
 constexpr int kColThreads = 1024;
 constexpr int kColCandidates = 160;   // a column
 constexpr int kColUnroll = 8;
+constexpr int kColSlots = 8;          // of the table of maxima, at most
+constexpr int kColItems = 1024;       // blocks that may hold one of the k largest
 
 template <int CT>
 struct ColShared {
@@ -435,10 +503,13 @@ struct ColShared {
     uint32_t hist[256], ctl[4];
     float buf[33];
     Token tok[CT];
+    uint32_t nitems;
+    uint32_t items[kColItems];
+    float block_max[kColSlots][kColThreads];
 };
 
 template <typename T, int CT>
-__global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreArgs a) {
+__global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreArgs a, const Blocks blocks) {
     constexpr int SLOTS = kColThreads / CT, U = kColUnroll;
     extern __shared__ __align__(16) unsigned char smem[];
     ColShared<CT> &sh = *reinterpret_cast<ColShared<CT> *>(smem);
@@ -454,39 +525,44 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
     const T *base = static_cast<const T *>(a.x) + token;   // of this thread's column
     const int32_t n = a.vocab, k = a.k;
     const int32_t v0 = int32_t(int64_t(n) * rank / split), v1 = int32_t(int64_t(n) * (rank + 1) / split);
+    const auto fetch = [&](int32_t v) { return in && v < v1 ? widen(base[int64_t(v) * a.ld]) : -INFINITY; };
+    float next[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = fetch(v0 + slot + u * SLOTS);
     if (tid < CT) sh.ncand[tid] = 0;
+    if (tid == 0) sh.nitems = 0;
 
-    float m = kMasked;
-    float2 s2 = both(0.0f), t2 = both(0.0f);
-    if (in) {
-        for (int32_t v = v0 + slot; v < v1; v += SLOTS * U) {
-            float x[U];
+    Running sum = no_sums();
+    int block = 0, in_block = 0;
+    float slot_max = kMasked;
+    for (int32_t v = v0; v < v1; v += SLOTS * U) {
+        float x[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int32_t vu = v + u * SLOTS;
-                x[u] = vu < v1 ? widen(base[int64_t(vu) * a.ld]) : -INFINITY;
-            }
-            float top = m;
+        for (int u = 0; u < U; ++u) x[u] = max_nan(next[u], kMasked);
+        if (v + SLOTS * U < v1) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                x[u] = max_nan(x[u], kMasked);
-                top = max_nan(top, x[u]);
-            }
-            const float d0 = m * kLog2e - top * kLog2e, f = exp2_fast(d0);
-            t2 = mul2(both(f), fma2(s2, both(d0), t2));
-            s2 = mul2(both(f), s2);
-            m = top;
-            const float2 l2 = both(kLog2e), r2 = both(-(m * kLog2e));
+            for (int u = 0; u < U; ++u) next[u] = fetch(v + slot + (U + u) * SLOTS);
+        }
+        float top = x[0];
 #pragma unroll
-            for (int u = 0; u < U; u += 2) {
-                const float2 d = fma2(make_float2(x[u], x[u + 1]), l2, r2);
-                const float2 e = make_float2(exp2_fast(d.x), exp2_fast(d.y));
-                s2 = add2(s2, e);
-                t2 = fma2(e, d, t2);
+        for (int u = 1; u < U; ++u) top = max_nan(top, x[u]);
+        if (k > 0) {
+            slot_max = max_nan(slot_max, top);
+            if (++in_block == blocks.per_slot) {
+                sh.block_max[block++][tid] = slot_max;
+                slot_max = kMasked;
+                in_block = 0;
             }
         }
+        rebase(sum, top);
+        float2 s2 = both(0.0f), t2 = both(0.0f);
+#pragma unroll
+        for (int u = 0; u < U; u += 2) add_pair(make_float2(x[u], x[u + 1]), sum.r, s2, t2);
+        sum.s = add2(sum.s, s2);
+        sum.t = add2(sum.t, t2);
     }
-    sh.part[slot][col] = {m, s2.x + s2.y, t2.x + t2.y};
+    if (in_block > 0) sh.block_max[block++][tid] = slot_max;
+    sh.part[slot][col] = {sum.m, sum.s.x + sum.s.y, sum.t.x + sum.t.y};
     __syncthreads();
     // warp c joins column c (c < CT <= 32 warps), and finds the bar of its k largest
     if (warp < CT) {
@@ -508,24 +584,35 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
     }
     __syncthreads();
     if (k > 0) {
-        const float bar = sh.bar[col];   // NaN: no plain choice
-        if (in && m >= bar) {
-            for (int32_t v = v0 + slot; v < v1; v += SLOTS) {
-                const float x = widen(base[int64_t(v) * a.ld]);
-                if (x >= bar) {
-                    const uint32_t p = atomicAdd(&sh.ncand[col], 1u);
-                    if (p < kColCandidates) sh.cand[col][p] = key_of(x, v);
+        const float bar = sh.bar[col];   // NaN: the maxima say nothing
+        if (in && sum.m >= bar)
+            for (int i = 0; i < block; ++i)
+                if (sh.block_max[i][tid] >= bar) {
+                    const uint32_t p = atomicAdd(&sh.nitems, 1u);
+                    if (p < kColItems) sh.items[p] = uint32_t(i * kColThreads + tid);
+                }
+        for (int i = tid; i < CT * kMaxTop; i += kColThreads) sh.sorted[i / kMaxTop][i % kMaxTop] = 0;
+        __syncthreads();
+        const bool listed = sh.nitems <= kColItems;
+        if (listed) {
+            const int per = U * blocks.per_slot, total = int(sh.nitems) * per;
+            for (int i = tid; i < total; i += kColThreads) {
+                const int32_t item = int32_t(sh.items[i / per]), j = i % per, t = item % kColThreads, c = t % CT;
+                const int32_t v = v0 + ((item / kColThreads) * blocks.per_slot + j / U) * (SLOTS * U) + (j % U) * SLOTS + t / CT;
+                if (v >= v1) continue;
+                const float x = widen(static_cast<const T *>(a.x)[int64_t(v) * a.ld + c0 + c]);
+                if (x >= sh.bar[c]) {
+                    const uint32_t p = atomicAdd(&sh.ncand[c], 1u);
+                    if (p < kColCandidates) sh.cand[c][p] = key_of(x, v);
                 }
             }
         }
-        for (int i = tid; i < CT * kMaxTop; i += kColThreads) sh.sorted[i / kMaxTop][i % kMaxTop] = 0;
         __syncthreads();
         for (int c = 0; c < CT && c0 + c < a.tokens; ++c) {
-            if (sh.bar[c] == sh.bar[c] && sh.ncand[c] <= kColCandidates) continue;
+            if (listed && sh.bar[c] == sh.bar[c] && sh.ncand[c] <= kColCandidates) continue;
             select_any(static_cast<const T *>(a.x) + c0 + c, a.ld, v0, v1, k, sh.sel, sh.hist, sh.ctl);
             if (tid < kMaxTop) sh.cand[c][tid] = sh.sel[tid];
-            if (tid == 0) sh.ncand[c] = kMaxTop;
-            // (the bar is not read again in this loop: the next column has its own)
+            if (tid == 0) sh.ncand[c] = kMaxTop;   // read by all before select_any's barriers
         }
         __syncthreads();
         if (warp < CT) rank_keys(sh.cand[warp], int(sh.ncand[warp]), k, sh.sorted[warp], lane, 32);
@@ -585,8 +672,13 @@ cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream) {
     while (split < kMaxSplit && a.tokens * split < 2 * sm_count() &&
            a.vocab / (2 * split) >= THREADS * kPerGranule<T>)
         split *= 2;
-    return launch_ex(score_rows_kernel<T, THREADS, U>, dim3(unsigned(a.tokens * split)), dim3(THREADS), 0, stream,
-                     unsigned(split), true, a);
+    const int64_t granules = row_granules<T>(kPerGranule<T> - 1, a.vocab) / split + 1;   // of a CTA, at most
+    const Blocks blocks = blocks_of((granules + THREADS * U - 1) / (THREADS * U), kRowSlots);
+    const size_t smem = a.k > 0 ? size_t(blocks.slots) * THREADS * 4 : 0;
+    const cudaError_t e = allow_smem(score_rows_kernel<T, THREADS, U>, smem);
+    if (e != cudaSuccess) return e;
+    return launch_ex(score_rows_kernel<T, THREADS, U>, dim3(unsigned(a.tokens * split)), dim3(THREADS), smem, stream,
+                     unsigned(split), true, a, blocks);
 }
 
 template <typename T, int CT>
@@ -597,11 +689,14 @@ cudaError_t launch_score_columns_ct(const ScoreArgs &a, cudaStream_t stream) {
     int split = 1;
     while (split < kMaxSplit && 2 * split <= most && tiles * split < sm_count() && a.vocab / (2 * split) >= 4 * kColThreads / CT)
         split *= 2;
+    const int64_t rows = a.vocab / split + 1;   // of a CTA, at most
+    constexpr int per_round = kColThreads / CT * kColUnroll;
+    const Blocks blocks = blocks_of((rows + per_round - 1) / per_round, kColSlots);
     const size_t smem = sizeof(ColShared<CT>);
     const cudaError_t e = allow_smem(score_columns_kernel<T, CT>, smem);
     if (e != cudaSuccess) return e;
     return launch_ex(score_columns_kernel<T, CT>, dim3(unsigned(tiles * split)), dim3(kColThreads), smem, stream,
-                     unsigned(split), true, a);
+                     unsigned(split), true, a, blocks);
 }
 
 template <typename T>
