@@ -245,18 +245,45 @@ __device__ void select_any(const T *base, int64_t stride, int32_t i0, int32_t i1
     __syncthreads();
 }
 
-// The k largest of n keys (all different, but for zeros at the end), in order:
-// every key counts those above it.
-__device__ __forceinline__ void rank_keys(const uint64_t *keys, int n, int k, uint64_t *sorted, int thread, int threads) {
-    for (int i = thread; i < n; i += threads) {
-        const uint64_t key = keys[i];
-        int above = 0;
-        for (int j = 0; j < n; ++j) above += keys[j] > key;
-        if (above < k && key != 0) sorted[above] = key;
+// The k largest of n keys in order, to sorted[0 .. kMaxTop) (the keys all
+// different, but for zeros, which are none; zeros where there are fewer), by one
+// warp.  Up to 64 keys: every lane counts the keys above its own.  More: the
+// largest of all lanes' largest, k times, by two 32-bit maxima over the warp.
+__device__ __forceinline__ void warp_sort(const uint64_t *keys, int n, int k, uint64_t *sorted) {
+    const int lane = threadIdx.x & 31;
+    if (n <= 64) {
+        const uint64_t lo = lane < n ? keys[lane] : 0, hi = lane + 32 < n ? keys[lane + 32] : 0;
+        int above_lo = 0, above_hi = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) {
+            const uint64_t o = keys[j];
+            above_lo += o > lo;
+            above_hi += o > hi;
+        }
+        sorted[lane] = 0;
+        __syncwarp();
+        if (lo != 0 && above_lo < k) sorted[above_lo] = lo;
+        if (hi != 0 && above_hi < k) sorted[above_hi] = hi;
+    } else {
+        uint64_t best = 0, mine = 0;
+        for (int i = lane; i < n; i += 32) best = keys[i] > best ? keys[i] : best;
+        for (int j = 0; j < k; ++j) {
+            const uint32_t hi = __reduce_max_sync(0xFFFFFFFFu, uint32_t(best >> 32));
+            const uint32_t lo = __reduce_max_sync(0xFFFFFFFFu, uint32_t(best >> 32) == hi ? uint32_t(best) : 0u);
+            const uint64_t top = (uint64_t(hi) << 32) | lo;
+            if (lane == j) mine = top;
+            if (best == top) {
+                best = 0;
+                for (int i = lane; i < n; i += 32) best = keys[i] < top && keys[i] > best ? keys[i] : best;
+            }
+        }
+        sorted[lane] = mine;
     }
+    __syncwarp();
 }
 
-// The k-th largest of 32 values, one a lane (equal values rank by lane).
+// The k-th largest of 32 values, one a lane (equal values rank by lane); NaN if
+// one of them is.
 __device__ __forceinline__ float kth_of_warp(float v, int k) {
     const int lane = threadIdx.x & 31;
     int above = 0;
@@ -266,7 +293,8 @@ __device__ __forceinline__ float kth_of_warp(float v, int k) {
         above += o > v || (o == v && j < lane);
     }
     const unsigned at = __ballot_sync(0xFFFFFFFFu, above == k - 1);
-    return __shfl_sync(0xFFFFFFFFu, v, at ? __ffs(at) - 1 : 0);
+    const float kth = __shfl_sync(0xFFFFFFFFu, v, at ? __ffs(at) - 1 : 0);
+    return __any_sync(0xFFFFFFFFu, v != v) ? __uint_as_float(0x7FC00000u) : kth;
 }
 
 // ---- token rows ----
@@ -334,12 +362,23 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
     const int head = row_head<T>(row);
     const int32_t n = a.vocab, granules = int32_t(row_granules<T>(head, n)), k = a.k;
     const int32_t g0 = int32_t(int64_t(granules) * rank / split), g1 = int32_t(int64_t(granules) * (rank + 1) / split);
-    const auto fetch = [&](int32_t g) {
-        return load_granule(row, g < g1 ? int64_t(g) * V - head : int64_t(n), n, -INFINITY);
+    // a round's granules: at once where all of them lie in the row and in this CTA's share
+    const int32_t whole0 = head > 0 ? 1 : 0, whole1 = (head + n) / V;
+    const uint4 *aligned = reinterpret_cast<const uint4 *>(row - head);
+    const auto fetch = [&](uint4 (&q)[U], int32_t g) {
+        if (g >= whole0 && g + THREADS * U <= min(g1, whole1)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) q[u] = __ldg(aligned + g + u * THREADS + tid);
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t gu = g + u * THREADS + tid;
+            q[u] = load_granule(row, gu < g1 ? int64_t(gu) * V - head : int64_t(n), n, -INFINITY);
+        }
     };
     uint4 next[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = fetch(g0 + tid + u * THREADS);
+    fetch(next, g0);
     int64_t target = -1;
     float target_x = 0.0f;
     if (tid == 0) {
@@ -353,14 +392,11 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
     Running sum = no_sums();
     int slot = 0, in_slot = 0;
     float slot_max = kMasked;
-    for (int32_t g = g0 + tid; g - tid < g1; g += THREADS * U) {
+    for (int32_t g = g0; g < g1; g += THREADS * U) {
         uint4 q[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) q[u] = next[u];
-        if (g - tid + THREADS * U < g1) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) next[u] = fetch(g + THREADS * U + u * THREADS);
-        }
+        if (g + THREADS * U < g1) fetch(next, g + THREADS * U);
         float top = kMasked;
         clamp_block(q, top, T());
         if (k > 0) {
@@ -394,15 +430,14 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
     if (warp == 0) {
         all = warp_join(lane < W ? warp_part[lane] : empty_part());
         if (lane == 0) cta_part = all;
-        if (k > 0) {
-            // The k-th largest of 32 maxima over disjoint sets of logits is at most the
-            // k-th largest logit, so only blocks that reach it can hold one of the k largest.
-            float g = thread_max[lane];
+    } else if (warp == 1 && k > 0) {
+        // The k-th largest of 32 maxima over disjoint sets of logits is at most the
+        // k-th largest logit, so only blocks that reach it can hold one of the k largest.
+        float g = thread_max[lane];
 #pragma unroll
-            for (int w = 1; w < W; ++w) g = max_nan(g, thread_max[w * 32 + lane]);
-            const float bar = kth_of_warp(g, k);
-            if (lane == 0) s_bar = bar > kMasked && all.m == all.m ? bar : __uint_as_float(0x7FC00000u);
-        }
+        for (int w = 1; w < W; ++w) g = max_nan(g, thread_max[w * 32 + lane]);
+        const float bar = kth_of_warp(g, k);
+        if (lane == 0) s_bar = bar > kMasked ? bar : __uint_as_float(0x7FC00000u);
     }
     if (k > 0) {
         __syncthreads();
@@ -433,18 +468,17 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
                         if (p < kCandidates) cand[p] = key_of(v[e], int32_t(j0 + e));
                     }
             }
-            if (tid < kMaxTop) sorted[tid] = 0;
             __syncthreads();
             found = int(ncand);
         }
         if (!listed || found > kCandidates) {
             const int32_t i0 = max(0, g0 * V - head), i1 = min(n, g1 * V - head);
             select_any(row, 1, i0, i1, k, sel, hist, ctl);
-            if (tid < kMaxTop) cand[tid] = sel[tid], sorted[tid] = 0;
+            if (tid < kMaxTop) cand[tid] = sel[tid];
             found = kMaxTop;
             __syncthreads();
         }
-        rank_keys(cand, found, k, sorted, tid, THREADS);
+        if (warp == 0) warp_sort(cand, found, k, sorted);
     }
     if (split > 1) {
         cluster.sync();
@@ -459,9 +493,8 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
         cluster.sync();   // the other CTAs may leave: nothing reads them any more
         if (rank != 0) return;
         if (warp == 0 && lane == 0) cta_part = all;
-        if (tid < kMaxTop) sorted[tid] = 0;
         __syncthreads();
-        rank_keys(cand, split * k, k, sorted, tid, THREADS);
+        if (warp == 0 && k > 0) warp_sort(cand, split * k, k, sorted);
     }
     __syncthreads();
     const Part whole = cta_part;
@@ -579,7 +612,7 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
         if (lane == 0) sh.col[warp] = p;
         if (k > 0) {
             const float bar = kth_of_warp(g, k);
-            if (lane == 0) sh.bar[warp] = bar > kMasked && p.m == p.m ? bar : __uint_as_float(0x7FC00000u);
+            if (lane == 0) sh.bar[warp] = bar > kMasked ? bar : __uint_as_float(0x7FC00000u);
         }
     }
     __syncthreads();
@@ -591,7 +624,6 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
                     const uint32_t p = atomicAdd(&sh.nitems, 1u);
                     if (p < kColItems) sh.items[p] = uint32_t(i * kColThreads + tid);
                 }
-        for (int i = tid; i < CT * kMaxTop; i += kColThreads) sh.sorted[i / kMaxTop][i % kMaxTop] = 0;
         __syncthreads();
         const bool listed = sh.nitems <= kColItems;
         if (listed) {
@@ -608,14 +640,16 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
             }
         }
         __syncthreads();
-        for (int c = 0; c < CT && c0 + c < a.tokens; ++c) {
-            if (listed && sh.bar[c] == sh.bar[c] && sh.ncand[c] <= kColCandidates) continue;
-            select_any(static_cast<const T *>(a.x) + c0 + c, a.ld, v0, v1, k, sh.sel, sh.hist, sh.ctl);
-            if (tid < kMaxTop) sh.cand[c][tid] = sh.sel[tid];
-            if (tid == 0) sh.ncand[c] = kMaxTop;   // read by all before select_any's barriers
-        }
+        const auto short_way = [&](int c) { return listed && sh.bar[c] == sh.bar[c] && sh.ncand[c] <= kColCandidates; };
+        if (__syncthreads_or(tid < CT && in && !short_way(tid)))
+            for (int c = 0; c < CT && c0 + c < a.tokens; ++c) {
+                if (short_way(c)) continue;
+                select_any(static_cast<const T *>(a.x) + c0 + c, a.ld, v0, v1, k, sh.sel, sh.hist, sh.ctl);
+                if (tid < kMaxTop) sh.cand[c][tid] = sh.sel[tid];
+                if (tid == 0) sh.ncand[c] = kMaxTop;   // all have asked: select_any has barriers
+            }
         __syncthreads();
-        if (warp < CT) rank_keys(sh.cand[warp], int(sh.ncand[warp]), k, sh.sorted[warp], lane, 32);
+        if (warp < CT) warp_sort(sh.cand[warp], int(sh.ncand[warp]), k, sh.sorted[warp]);
     }
     if (split > 1) {
         cluster.sync();
@@ -630,21 +664,19 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
         if (warp < CT) {
             p = warp_join(p);
             if (lane == 0) sh.col[warp] = p;
-            if (k > 0) {
-                sh.sorted[warp][lane] = 0;
-                __syncwarp();
-                rank_keys(sh.cand[warp], split * k, k, sh.sorted[warp], lane, 32);
-            }
+            __syncwarp();
+            if (k > 0) warp_sort(sh.cand[warp], split * k, k, sh.sorted[warp]);
         }
     }
     __syncthreads();
-    for (int c = 0; c < CT && c0 + c < a.tokens; ++c) {
-        Token tok;
-        if (is_wide(sh.col[c].m)) tok = wide_token(static_cast<const T *>(a.x) + c0 + c, a.ld, n, sh.buf);
-        else if (tid != c) continue;
-        else tok = token_of(sh.col[c]);
-        if (tid == c) sh.tok[c] = tok;
-    }
+    const bool wide = tid < CT && in && is_wide(sh.col[tid].m);
+    if (tid < CT && in && !wide) sh.tok[tid] = token_of(sh.col[tid]);
+    if (__syncthreads_or(wide))
+        for (int c = 0; c < CT && c0 + c < a.tokens; ++c) {
+            if (!is_wide(sh.col[c].m)) continue;
+            const Token tok = wide_token(static_cast<const T *>(a.x) + c0 + c, a.ld, n, sh.buf);
+            if (tid == c) sh.tok[c] = tok;
+        }
     __syncthreads();
     if (tid < CT && in) {   // slot 0: col == tid
         const Token tok = sh.tok[tid];
@@ -665,13 +697,9 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
     }
 }
 
-template <typename T>
-cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream) {
-    constexpr int THREADS = 256, U = 4;
-    int split = 1;
-    while (split < kMaxSplit && a.tokens * split < 2 * sm_count() &&
-           a.vocab / (2 * split) >= THREADS * kPerGranule<T>)
-        split *= 2;
+template <typename T, int THREADS>
+cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream, int split) {
+    constexpr int U = 4;
     const int64_t granules = row_granules<T>(kPerGranule<T> - 1, a.vocab) / split + 1;   // of a CTA, at most
     const Blocks blocks = blocks_of((granules + THREADS * U - 1) / (THREADS * U), kRowSlots);
     const size_t smem = a.k > 0 ? size_t(blocks.slots) * THREADS * 4 : 0;
@@ -679,6 +707,16 @@ cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
     return launch_ex(score_rows_kernel<T, THREADS, U>, dim3(unsigned(a.tokens * split)), dim3(THREADS), smem, stream,
                      unsigned(split), true, a, blocks);
+}
+
+template <typename T>
+cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream) {
+    const bool short_rows = row_granules<T>(0, a.vocab) <= 8192;
+    if (a.tokens >= 4 * sm_count() && short_rows) return launch_score_rows<T, 128>(a, stream, 1);
+    int split = 1;
+    while (split < kMaxSplit && a.tokens * split < 2 * sm_count() && a.vocab / (2 * split) >= 256 * kPerGranule<T>)
+        split *= 2;
+    return launch_score_rows<T, 256>(a, stream, split);
 }
 
 template <typename T, int CT>
@@ -701,9 +739,13 @@ cudaError_t launch_score_columns_ct(const ScoreArgs &a, cudaStream_t stream) {
 
 template <typename T>
 cudaError_t launch_score_columns(const ScoreArgs &a, cudaStream_t stream) {
-    if (a.tokens > 16) return launch_score_columns_ct<T, 32>(a, stream);
-    if (a.tokens > 8) return launch_score_columns_ct<T, 16>(a, stream);
-    if (a.tokens > 4) return launch_score_columns_ct<T, 8>(a, stream);
+    int ct = 32;
+    // narrower tiles where the wider leave SMs idle, down to the 32 bytes that memory moves at a time
+    while (ct > 4 && (a.tokens <= ct / 2 || (ct * int(sizeof(T)) > 32 && (a.tokens + ct / 2 - 1) / (ct / 2) * kMaxSplit <= sm_count())))
+        ct /= 2;
+    if (ct == 32) return launch_score_columns_ct<T, 32>(a, stream);
+    if (ct == 16) return launch_score_columns_ct<T, 16>(a, stream);
+    if (ct == 8) return launch_score_columns_ct<T, 8>(a, stream);
     return launch_score_columns_ct<T, 4>(a, stream);
 }
 
