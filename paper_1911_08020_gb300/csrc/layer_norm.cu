@@ -10,14 +10,15 @@
 // Both passes are bound by memory: x (and dy) are read once, y (or dx) written
 // once, and a token stays in registers between its sums and its output.
 //
-// Token rows.  A row is read as granules (tokens.cuh).  A group of threads
-// (GROUP) owns a row, VPT granules a thread; the CTAs are persistent and take
-// rows a multiple of 8 apart, so that all rows of a group start alike past a
-// 16-byte boundary whatever the leading dimension: a thread then owns the same
-// features in every row, and keeps their gamma and beta, and in the backward
-// pass their sums over its rows, in registers.  Those sums go to scratch once
-// at the end, one partial result a group, and a second small kernel adds them
-// in a fixed order.
+// Token rows.  A row is read as granules (tokens.cuh) by the threads of a CTA,
+// VPT granules a thread.  The CTAs are persistent and take rows a multiple of 8
+// apart, so that all rows of a CTA start alike past a 16-byte boundary whatever
+// the leading dimension: a thread then owns the same features in every row, and
+// keeps their gamma and beta, and in the backward pass their sums over its
+// rows, in registers.  Those sums go to scratch once at the end, one partial
+// result a CTA, and a second small kernel adds them in a fixed order.  Rows
+// arrive through a ring of bulk copies in shared memory: the bytes in flight do
+// not depend on how many registers the threads leave for occupancy.
 //
 // Token columns.  A CTA takes 32 tokens of a step and a share of the features,
 // lane = token; the CTAs of a cluster share a tile and exchange their sums
@@ -62,180 +63,292 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// The sums of N values over the threads of a group (a warp, or the CTA); every
-// thread gets them.  buf: 2 x N x 32 floats of shared memory, its halves used
-// in turn so that one barrier a call is enough.
-template <int GROUP, int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], float *buf, int &turn) {
+constexpr int kSumWarps = 16;   // warps of a CTA that shares a sum, at most
+
+// The sums of N values over the threads of the CTA; every thread gets them.
+// buf: 2 x N x kSumWarps floats of shared memory, zeros at first; its halves are
+// used in turn, so that one barrier a call is enough.
+template <int N>
+__device__ __forceinline__ void cta_sum(float (&v)[N], float *buf, int &turn) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-    if constexpr (GROUP > 32) {
-        constexpr int W = GROUP / 32;
-        float *b = buf + (turn & 1) * (N * 32);
-        turn ^= 1;
-        const int lane = threadIdx.x & 31;
-        if (lane == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) b[i * 32 + (threadIdx.x >> 5)] = v[i];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < W ? b[i * 32 + lane] : 0.0f);
+    const int warps = int(blockDim.x) >> 5;
+    if (warps == 1) {
+        __syncwarp();
+        return;
     }
+    float *b = buf + turn * (N * kSumWarps);
+    turn ^= 1;
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) b[i * kSumWarps + (threadIdx.x >> 5)] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float4 q = *reinterpret_cast<const float4 *>(b + i * kSumWarps);
+        v[i] = (q.x + q.y) + (q.z + q.w);
+        for (int w = 4; w < warps; w += 4) {
+            const float4 p = *reinterpret_cast<const float4 *>(b + i * kSumWarps + w);
+            v[i] += (p.x + p.y) + (p.z + p.w);
+        }
+    }
+}
+__device__ __forceinline__ void clear_sums(float *buf, int floats) {
+    for (int i = threadIdx.x; i < floats; i += blockDim.x) buf[i] = 0.0f;
+    __syncthreads();
 }
 
 // ---- token rows ----
 
-template <int GROUP>
-struct RowsOf {
-    static constexpr int kPerCta = GROUP == 32 ? 8 : 1;   // rows at a time
-    static constexpr int kThreads = GROUP * kPerCta;
+// Rows of `n` values from `base` on, `ld` apart, as the ring copies them: of a
+// row's granules those that lie in the tensor as a whole.  (The first of the
+// first row and the last of the last can stick out of it; a granule that two
+// rows share is copied for both, and each masks the other's values.)
+template <typename T>
+struct RowCopies {
+    const T *base, *end;
+    int64_t ld, count;
+    int32_t n;
+    __device__ RowCopies(const void *p, int64_t ld_, int64_t rows, int32_t n_)
+        : base(static_cast<const T *>(p)), end(base + (rows - 1) * ld_ + n_), ld(ld_), count(rows), n(n_) {}
+    // granules [c0, c1) of row r are copied; `first`: address of granule 0
+    __device__ __forceinline__ const T *range(int64_t r, int &c0, int &c1) const {
+        const T *row = base + r * ld;
+        const int head = row_head<T>(row);
+        const T *first = row - head;
+        c1 = int(row_granules<T>(head, n));
+        c0 = first < base ? 1 : 0;
+        if (first + c1 * kPerGranule<T> > end) --c1;
+        return first;
+    }
+    // Start the copy of row r into `stage`; returns its bytes.
+    __device__ __forceinline__ uint32_t copy(int64_t r, unsigned char *stage, uint64_t *bar) const {
+        int c0, c1;
+        const T *first = range(r, c0, c1);
+        if (c1 <= c0) return 0;
+        bulk_g2s(stage + c0 * 16, first + c0 * kPerGranule<T>, uint32_t(c1 - c0) * 16, bar);
+        return uint32_t(c1 - c0) * 16;
+    }
+    __device__ __forceinline__ uint32_t bytes(int64_t r) const {
+        int c0, c1;
+        range(r, c0, c1);
+        return c1 > c0 ? uint32_t(c1 - c0) * 16 : 0;
+    }
 };
 
-template <typename T, int GROUP, int VPT>
-__global__ void __launch_bounds__(RowsOf<GROUP>::kThreads) norm_rows_kernel(const NormArgs a) {
-    constexpr int V = kPerGranule<T>, PER = RowsOf<GROUP>::kPerCta;
-    __shared__ float buf[2 * 32];
+// The granules of a thread: for every row of a CTA at the same features.
+template <typename T, int VPT>
+struct Owned {
+    static constexpr int V = kPerGranule<T>;
+    int32_t f0;        // first feature of granule u: f0 + u * step
+    int32_t step, n;
+    __device__ __forceinline__ int32_t feature(int u) const { return f0 + u * step; }
+    __device__ __forceinline__ bool whole(int u) const { return feature(u) >= 0 && feature(u) + V <= n; }
+    __device__ __forceinline__ bool in(int u, int e) const { return feature(u) + e >= 0 && feature(u) + e < n; }
+
+    // The granules of a row as pairs, 0 outside the row.  `stage`: this thread's
+    // granule 0 of the row as copied.
+    __device__ __forceinline__ void load(const RowCopies<T> &rows, int64_t r, const unsigned char *stage, bool arrived,
+                                         float2 (&v)[VPT][V / 2]) const {
+        const bool inner = r >= 8 && r + 8 < rows.count;   // all its granules are copied: 8 values are 16 bytes or more
+#pragma unroll
+        for (int u = 0; u < VPT; ++u) {
+            float w[V];
+            if (whole(u)) {
+                unpack(*reinterpret_cast<const uint4 *>(stage + u * step * int(sizeof(T))), w);
+            } else if (feature(u) < n && inner) {
+                unpack(*reinterpret_cast<const uint4 *>(stage + u * step * int(sizeof(T))), w);
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (!in(u, e)) w[e] = 0.0f;
+            } else {
+                unpack(load_granule<T, false>(rows.base + r * rows.ld, feature(u), n, 0.0f), w);
+            }
+#pragma unroll
+            for (int e = 0; e < V; e += 2) v[u][e / 2] = make_float2(w[e], w[e + 1]);
+        }
+        if (!arrived) v[0][0].x = __uint_as_float(0x7FC00000u);   // a copy that never came: the row is NaN
+    }
+    __device__ __forceinline__ void store(T *row, const float2 (&v)[VPT][V / 2]) const {
+#pragma unroll
+        for (int u = 0; u < VPT; ++u) {
+            float w[V];
+#pragma unroll
+            for (int e = 0; e < V; e += 2) w[e] = v[u][e / 2].x, w[e + 1] = v[u][e / 2].y;
+            if (whole(u)) *reinterpret_cast<uint4 *>(row + feature(u)) = pack(w);
+            else store_granule(row, feature(u), n, w);
+        }
+    }
+    // Values of a vector over the features, 0 outside.
+    template <typename F>
+    __device__ __forceinline__ void gather(F at, float2 (&v)[VPT][V / 2]) const {
+#pragma unroll
+        for (int u = 0; u < VPT; ++u)
+#pragma unroll
+            for (int e = 0; e < V; e += 2)
+                v[u][e / 2] = make_float2(in(u, e) ? at(feature(u) + e) : 0.0f, in(u, e + 1) ? at(feature(u) + e + 1) : 0.0f);
+    }
+};
+
+constexpr int kRowThreads = 512;   // threads that share a row, at most
+
+template <typename T, int VPT, int STAGES>
+__global__ void __launch_bounds__(kRowThreads) norm_rows_kernel(const NormArgs a, int32_t stage_bytes) {
+    constexpr int V = kPerGranule<T>, H = V / 2;
+    extern __shared__ __align__(16) unsigned char ring[];
+    __shared__ __align__(16) float buf[2 * kSumWarps];
+    __shared__ uint64_t full[STAGES];
+    const int t = threadIdx.x, threads = blockDim.x;
+    if (t == 0) {
+        for (int s = 0; s < STAGES; ++s) mbar_init(&full[s], 1);
+        fence_mbar_init();
+    }
     pdl_wait_previous();
     pdl_launch_dependents();
-    const int t = threadIdx.x % GROUP;
+    const int64_t stride = gridDim.x, r0 = blockIdx.x;
+    if (r0 >= a.tokens) return;
     const int32_t n = a.features;
+    const RowCopies<T> rows(a.x, a.ld_x, a.tokens, n);
+    const auto issue = [&](int64_t r, int s) {
+        mbar_arrive_expect_tx(&full[s], rows.bytes(r));
+        rows.copy(r, ring + s * stage_bytes, &full[s]);
+    };
+    if (t == 0)
+        for (int s = 0; s < STAGES; ++s)
+            if (r0 + s * stride < a.tokens) issue(r0 + s * stride, s);
     const float inv_n = __fdiv_rn(1.0f, float(n));
-    int turn = 0;
-    const int64_t stride = int64_t(gridDim.x) * PER;
-    int64_t r = int64_t(blockIdx.x) * PER + threadIdx.x / GROUP;
-    if (r >= a.tokens) return;
-    const T *x = static_cast<const T *>(a.x);
+    // all rows of this CTA start alike
+    const Owned<T, VPT> own = {t * V - row_head<T>(rows.base + r0 * a.ld_x), threads * V, n};
+    float2 gm[VPT][H], bt[VPT][H];
+    own.gather([&](int32_t f) { return gamma_at(a, f); }, gm);
+    own.gather([&](int32_t f) { return beta_at(a, f); }, bt);
+    clear_sums(buf, 2 * kSumWarps);
     T *y = static_cast<T *>(a.out);
-    const int head = row_head<T>(x + r * a.ld_x);   // of every row of this group
-    float gm[VPT][V], bt[VPT][V];
-#pragma unroll
-    for (int u = 0; u < VPT; ++u)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const int32_t f = (u * GROUP + t) * V - head + e;
-            const bool in = f >= 0 && f < n;
-            gm[u][e] = in ? gamma_at(a, f) : 0.0f;
-            bt[u][e] = in ? beta_at(a, f) : 0.0f;
-        }
-    uint4 next[VPT];
-#pragma unroll
-    for (int u = 0; u < VPT; ++u)
-        next[u] = load_granule<T, false>(x + r * a.ld_x, (u * GROUP + t) * V - head, n, 0.0f);
-    for (; r < a.tokens; r += stride) {
-        float v[VPT][V];
-#pragma unroll
-        for (int u = 0; u < VPT; ++u) unpack(next[u], v[u]);
-        if (r + stride < a.tokens) {
-#pragma unroll
-            for (int u = 0; u < VPT; ++u)
-                next[u] = load_granule<T, false>(x + (r + stride) * a.ld_x, (u * GROUP + t) * V - head, n, 0.0f);
-        }
-        float s[1] = {0.0f};
+    int turn = 0, stage = 0;
+    uint32_t parity = 0;
+    bool arrived = true;
+    for (int64_t r = r0; r < a.tokens; r += stride) {
+        float2 v[VPT][H], s2 = both(0.0f);
+        arrived = arrived && mbar_wait(&full[stage], parity);
+        own.load(rows, r, ring + stage * stage_bytes + t * 16, arrived, v);
 #pragma unroll
         for (int u = 0; u < VPT; ++u)
 #pragma unroll
-            for (int e = 0; e < V; ++e) s[0] += v[u][e];   // 0 outside the row
-        group_sum<GROUP>(s, buf, turn);
+            for (int e = 0; e < H; ++e) s2 = add2(s2, v[u][e]);
+        float s[1] = {s2.x + s2.y};
+        cta_sum(s, buf, turn);   // every thread has read the stage
+        if (t == 0 && arrived && r + STAGES * stride < a.tokens) issue(r + STAGES * stride, stage);
+        if (++stage == STAGES) stage = 0, parity ^= 1;
         const float mean = s[0] * inv_n;
-        s[0] = 0.0f;
+        s2 = both(0.0f);
 #pragma unroll
-        for (int u = 0; u < VPT; ++u)
+        for (int u = 0; u < VPT; ++u) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const int32_t f = (u * GROUP + t) * V - head + e;
-                const float c = v[u][e] - mean;
-                v[u][e] = c;
-                s[0] += f >= 0 && f < n ? c * c : 0.0f;
+            for (int e = 0; e < H; ++e) v[u][e] = add2(v[u][e], both(-mean));
+            if (!own.whole(u)) {
+#pragma unroll
+                for (int e = 0; e < H; ++e) {
+                    if (!own.in(u, 2 * e)) v[u][e].x = 0.0f;
+                    if (!own.in(u, 2 * e + 1)) v[u][e].y = 0.0f;
+                }
             }
-        group_sum<GROUP>(s, buf, turn);
+#pragma unroll
+            for (int e = 0; e < H; ++e) s2 = fma2(v[u][e], v[u][e], s2);
+        }
+        s[0] = s2.x + s2.y;
+        cta_sum(s, buf, turn);
         const float rstd = inverse_root(s[0] * inv_n + a.eps);
         if (t == 0) {
             if (a.mean) a.mean[r] = mean;
             if (a.rstd) a.rstd[r] = rstd;
         }
 #pragma unroll
-        for (int u = 0; u < VPT; ++u) {
+        for (int u = 0; u < VPT; ++u)
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[u][e] = fmaf(v[u][e] * rstd, gm[u][e], bt[u][e]);
-            store_granule(y + r * a.ld_out, (u * GROUP + t) * V - head, n, v[u]);
-        }
+            for (int e = 0; e < H; ++e) v[u][e] = fma2(mul2(v[u][e], both(rstd)), gm[u][e], bt[u][e]);
+        own.store(y + r * a.ld_out, v);
     }
 }
 
-template <typename T, int GROUP, int VPT>
-__global__ void __launch_bounds__(RowsOf<GROUP>::kThreads) back_rows_kernel(const NormArgs a) {
-    constexpr int V = kPerGranule<T>, PER = RowsOf<GROUP>::kPerCta;
-    __shared__ float buf[2 * 2 * 32];
+template <typename T, int VPT, int STAGES>
+__global__ void __launch_bounds__(kRowThreads) back_rows_kernel(const NormArgs a, int32_t stage_bytes) {
+    constexpr int V = kPerGranule<T>, H = V / 2;
+    extern __shared__ __align__(16) unsigned char ring[];   // a stage: a row of x, a row of dy
+    __shared__ __align__(16) float buf[2 * 2 * kSumWarps];
+    __shared__ uint64_t full[STAGES];
+    const int t = threadIdx.x, threads = blockDim.x;
+    if (t == 0) {
+        for (int s = 0; s < STAGES; ++s) mbar_init(&full[s], 1);
+        fence_mbar_init();
+    }
     pdl_wait_previous();
     pdl_launch_dependents();
-    const int t = threadIdx.x % GROUP;
-    const int32_t n = a.features;
-    const float inv_n = __fdiv_rn(1.0f, float(n));
-    int turn = 0;
-    const int64_t stride = int64_t(gridDim.x) * PER;
-    const int64_t group = int64_t(blockIdx.x) * PER + threadIdx.x / GROUP;
-    const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
-    T *dx = static_cast<T *>(a.out);
-    const int head = row_head<T>(x + group * a.ld_x);
-    float gm[VPT][V], sg[VPT][V], sb[VPT][V];
-#pragma unroll
-    for (int u = 0; u < VPT; ++u)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const int32_t f = (u * GROUP + t) * V - head + e;
-            gm[u][e] = f >= 0 && f < n ? gamma_at(a, f) : 0.0f;
-            sg[u][e] = sb[u][e] = 0.0f;
-        }
-    uint4 nx[VPT], nd[VPT];
-    float mean_next = 0.0f, rstd_next = 0.0f;
-    const auto fetch = [&](int64_t r) {
-#pragma unroll
-        for (int u = 0; u < VPT; ++u) {
-            nx[u] = load_granule<T>(x + r * a.ld_x, (u * GROUP + t) * V - head, n, 0.0f);
-            nd[u] = load_granule<T, false>(dy + r * a.ld_dy, (u * GROUP + t) * V - head, n, 0.0f);
-        }
-        mean_next = __ldg(a.mean + r);
-        rstd_next = __ldg(a.rstd + r);
+    const int32_t n = a.features, half = stage_bytes / 2;
+    const RowCopies<T> xs(a.x, a.ld_x, a.tokens, n), ds(a.dy, a.ld_dy, a.tokens, n);
+    const int64_t stride = gridDim.x, r0 = blockIdx.x;
+    const auto issue = [&](int64_t r, int s) {
+        mbar_arrive_expect_tx(&full[s], xs.bytes(r) + ds.bytes(r));
+        xs.copy(r, ring + s * stage_bytes, &full[s]);
+        ds.copy(r, ring + s * stage_bytes + half, &full[s]);
     };
-    if (group < a.tokens) fetch(group);
-    for (int64_t r = group; r < a.tokens; r += stride) {
-        float xh[VPT][V], d[VPT][V];
+    if (t == 0)
+        for (int s = 0; s < STAGES; ++s)
+            if (r0 + s * stride < a.tokens) issue(r0 + s * stride, s);
+    const float inv_n = __fdiv_rn(1.0f, float(n));
+    const Owned<T, VPT> own = {t * V - row_head<T>(xs.base + r0 * a.ld_x), threads * V, n};
+    float2 gm[VPT][H], sg[VPT][H], sb[VPT][H];
+    own.gather([&](int32_t f) { return gamma_at(a, f); }, gm);
+    own.gather([](int32_t) { return 0.0f; }, sg);
+    own.gather([](int32_t) { return 0.0f; }, sb);
+    clear_sums(buf, 2 * 2 * kSumWarps);
+    T *dx = static_cast<T *>(a.out);
+    int turn = 0, stage = 0;
+    uint32_t parity = 0;
+    bool arrived = true;
+    float mean_next = 0.0f, rstd_next = 0.0f;
+    if (r0 < a.tokens) mean_next = __ldg(a.mean + r0), rstd_next = __ldg(a.rstd + r0);
+    for (int64_t r = r0; r < a.tokens; r += stride) {
+        float2 xh[VPT][H], d[VPT][H], s0 = both(0.0f), s1 = both(0.0f);
         const float mean = mean_next, rstd = rstd_next;
-#pragma unroll
-        for (int u = 0; u < VPT; ++u) unpack(nx[u], xh[u]), unpack(nd[u], d[u]);
-        if (r + stride < a.tokens) fetch(r + stride);
-        float s[2] = {0.0f, 0.0f};
+        if (r + stride < a.tokens) mean_next = __ldg(a.mean + r + stride), rstd_next = __ldg(a.rstd + r + stride);
+        arrived = arrived && mbar_wait(&full[stage], parity);
+        const unsigned char *at = ring + stage * stage_bytes + t * 16;
+        own.load(xs, r, at, arrived, xh);
+        own.load(ds, r, at + half, arrived, d);   // 0 outside the row: adds nothing to any sum
 #pragma unroll
         for (int u = 0; u < VPT; ++u)
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const int32_t f = (u * GROUP + t) * V - head + e;
-                xh[u][e] = f >= 0 && f < n ? (xh[u][e] - mean) * rstd : 0.0f;
-                sg[u][e] = fmaf(d[u][e], xh[u][e], sg[u][e]);
-                sb[u][e] += d[u][e];
-                d[u][e] *= gm[u][e];
-                s[0] += d[u][e];
-                s[1] = fmaf(d[u][e], xh[u][e], s[1]);
+            for (int e = 0; e < H; ++e) {
+                xh[u][e] = mul2(add2(xh[u][e], both(-mean)), both(rstd));
+                sg[u][e] = fma2(d[u][e], xh[u][e], sg[u][e]);
+                sb[u][e] = add2(sb[u][e], d[u][e]);
+                d[u][e] = mul2(d[u][e], gm[u][e]);
+                s0 = add2(s0, d[u][e]);
+                s1 = fma2(d[u][e], xh[u][e], s1);
             }
-        group_sum<GROUP>(s, buf, turn);
+        float s[2] = {s0.x + s0.y, s1.x + s1.y};
+        cta_sum(s, buf, turn);   // every thread has read the stage
+        if (t == 0 && arrived && r + STAGES * stride < a.tokens) issue(r + STAGES * stride, stage);
+        if (++stage == STAGES) stage = 0, parity ^= 1;
         const float c0 = s[0] * inv_n, c1 = s[1] * inv_n;
 #pragma unroll
-        for (int u = 0; u < VPT; ++u) {
+        for (int u = 0; u < VPT; ++u)
 #pragma unroll
-            for (int e = 0; e < V; ++e) d[u][e] = rstd * (d[u][e] - c0 - xh[u][e] * c1);
-            store_granule(dx + r * a.ld_out, (u * GROUP + t) * V - head, n, d[u]);
-        }
+            for (int e = 0; e < H; ++e)
+                d[u][e] = mul2(fma2(xh[u][e], both(-c1), add2(d[u][e], both(-c0))), both(rstd));
+        own.store(dx + r * a.ld_out, d);
     }
     if (a.partial != nullptr) {
-        float *p = a.partial + group * 2 * int64_t(n);
+        float *p = a.partial + r0 * 2 * int64_t(n);
 #pragma unroll
         for (int u = 0; u < VPT; ++u)
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const int32_t f = (u * GROUP + t) * V - head + e;
-                if (f >= 0 && f < n) p[f] = sg[u][e], p[n + f] = sb[u][e];
-            }
+            for (int e = 0; e < V; ++e)
+                if (own.in(u, e)) {
+                    p[own.feature(u) + e] = e & 1 ? sg[u][e / 2].y : sg[u][e / 2].x;
+                    p[n + own.feature(u) + e] = e & 1 ? sb[u][e / 2].y : sb[u][e / 2].x;
+                }
     }
 }
 
@@ -263,7 +376,8 @@ constexpr int kAnyThreads = 256;
 
 template <typename T>
 __global__ void __launch_bounds__(kAnyThreads) norm_any_kernel(const NormArgs a) {
-    __shared__ float buf[2 * 32];
+    __shared__ __align__(16) float buf[2 * kSumWarps];
+    clear_sums(buf, 2 * kSumWarps);
     pdl_wait_previous();
     pdl_launch_dependents();
     const int64_t r = blockIdx.x;
@@ -273,14 +387,14 @@ __global__ void __launch_bounds__(kAnyThreads) norm_any_kernel(const NormArgs a)
     int turn = 0;
     float s[1] = {0.0f};
     for (int32_t f = threadIdx.x; f < n; f += kAnyThreads) s[0] += widen(x[f]);
-    group_sum<kAnyThreads>(s, buf, turn);
+    cta_sum(s, buf, turn);
     const float mean = s[0] / float(n);
     s[0] = 0.0f;
     for (int32_t f = threadIdx.x; f < n; f += kAnyThreads) {
         const float c = widen(x[f]) - mean;
         s[0] = fmaf(c, c, s[0]);
     }
-    group_sum<kAnyThreads>(s, buf, turn);
+    cta_sum(s, buf, turn);
     const float rstd = inverse_root(s[0] / float(n) + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[r] = mean;
@@ -292,7 +406,8 @@ __global__ void __launch_bounds__(kAnyThreads) norm_any_kernel(const NormArgs a)
 
 template <typename T>
 __global__ void __launch_bounds__(kAnyThreads) back_any_kernel(const NormArgs a) {
-    __shared__ float buf[2 * 2 * 32];
+    __shared__ __align__(16) float buf[2 * 2 * kSumWarps];
+    clear_sums(buf, 2 * 2 * kSumWarps);
     pdl_wait_previous();
     pdl_launch_dependents();
     const int64_t r = blockIdx.x;
@@ -307,7 +422,7 @@ __global__ void __launch_bounds__(kAnyThreads) back_any_kernel(const NormArgs a)
         s[0] += g;
         s[1] = fmaf(g, (widen(x[f]) - mean) * rstd, s[1]);
     }
-    group_sum<kAnyThreads>(s, buf, turn);
+    cta_sum(s, buf, turn);
     const float c0 = s[0] / float(n), c1 = s[1] / float(n);
     for (int32_t f = threadIdx.x; f < n; f += kAnyThreads) {
         const float xh = (widen(x[f]) - mean) * rstd;
@@ -455,22 +570,41 @@ __global__ void zero_kernel(float *a, float *b, int32_t n) {
 
 // ---- choice of kernels ----
 
-// Threads that share a row of token rows, and granules a thread: the fewest
-// threads that hold the row at `most` granules a thread (0: none do).
+// Granules of a row, at most: one more where rows can start past a boundary.
 template <typename T>
-int row_group(int64_t features, int most) {
-    const int64_t granules = row_granules<T>(kPerGranule<T> - 1, features);   // at the worst alignment
-    for (int g = 32; g <= 1024; g *= 2)
-        if (granules <= int64_t(g) * most) return g;
-    return 0;
+int64_t most_granules(const void *p, int64_t ld, int64_t rows, int64_t features) {
+    const bool aligned = aligned_to(p, 16) && (rows == 1 || ld * int64_t(sizeof(T)) % 16 == 0);
+    return row_granules<T>(aligned ? 0 : kPerGranule<T> - 1, features);
 }
 
-// The CTAs of the persistent row kernels: a multiple of 8, so that the rows of
-// a group start alike.
-int64_t row_grid(int64_t rows, int per_cta, int ctas_per_sm) {
-    const int64_t want = (rows + per_cta - 1) / per_cta;
-    const int64_t most = std::max<int64_t>(8, int64_t(sm_count()) * ctas_per_sm / 8 * 8);
-    return std::min(most, (want + 7) / 8 * 8);
+// How a persistent row kernel runs: the threads of a CTA (0: the row is too
+// long for it), the CTAs (a multiple of 8, so that the rows of one start
+// alike), and a stage of its ring.
+struct RowPlan {
+    int threads;
+    int64_t grid;
+    int32_t stage_bytes;
+};
+template <typename Kernel>
+RowPlan row_plan(Kernel kernel, int64_t granules, int vpt, int copies, int stages, int64_t rows) {
+    RowPlan p = {};
+    const int64_t threads = ((granules + vpt - 1) / vpt + 31) / 32 * 32;
+    p.stage_bytes = int32_t(std::min<int64_t>(granules, int64_t(kRowThreads) * vpt)) * 16 * copies;
+    const size_t smem = size_t(p.stage_bytes) * stages;
+    // (the kernel's own shared memory counts against the limit that needs no asking)
+    if (threads > kRowThreads || allow_smem(kernel, smem + 1024) != cudaSuccess) return p;
+    const int64_t per_sm = per_device(reinterpret_cast<const void *>(kernel), int64_t(threads) << 32 | int64_t(smem), [&]() -> long long {
+        int n = 0;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, int(threads), smem) != cudaSuccess) {
+            cudaGetLastError();
+            n = 0;
+        }
+        return n;
+    });
+    if (per_sm <= 0) return p;
+    p.threads = int(threads);
+    p.grid = std::min<int64_t>(std::max<int64_t>(8, per_sm * sm_count() / 8 * 8), (rows + 7) / 8 * 8);
+    return p;
 }
 
 // Whether rows of `a` and `b` start alike past a 16-byte boundary.
@@ -479,18 +613,8 @@ bool alike(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows,
            (rows == 1 || (lda - ldb) * int64_t(es) % 16 == 0);
 }
 
-template <typename T, int GROUP, int VPT>
-cudaError_t launch_norm_group(const NormArgs &a, cudaStream_t stream) {
-    using R = RowsOf<GROUP>;
-    const int64_t grid = row_grid(a.tokens, R::kPerCta, std::max(1, 1536 / R::kThreads));
-    return launch_ex(norm_rows_kernel<T, GROUP, VPT>, dim3(unsigned(grid)), dim3(R::kThreads), 0, stream, 1, true, a);
-}
-template <typename T>
-constexpr int kNormVpt = sizeof(T) == 2 ? 2 : 4;
-
 template <typename T>
 cudaError_t launch_norm(const NormArgs &a, darb_layout_t layout, cudaStream_t stream) {
-    constexpr int VPT = kNormVpt<T>;
     if (layout == DARB_TOKEN_COLUMNS) {
         const int64_t tiles = (a.tokens + 31) / 32, all = tiles * a.steps;
         int split = 1;
@@ -499,15 +623,13 @@ cudaError_t launch_norm(const NormArgs &a, darb_layout_t layout, cudaStream_t st
         return launch_ex(norm_columns_kernel<T>, dim3(unsigned(all * split)), dim3(kColThreads), 0, stream,
                          unsigned(split), true, a, int32_t(tiles));
     }
-    const int group = alike(a.x, a.ld_x, a.out, a.ld_out, a.tokens, sizeof(T)) ? row_group<T>(a.features, VPT) : 0;
-    switch (group) {
-        case 32: return launch_norm_group<T, 32, VPT>(a, stream);
-        case 64: return launch_norm_group<T, 64, VPT>(a, stream);
-        case 128: return launch_norm_group<T, 128, VPT>(a, stream);
-        case 256: return launch_norm_group<T, 256, VPT>(a, stream);
-        case 512: return launch_norm_group<T, 512, VPT>(a, stream);
-        case 1024: return launch_norm_group<T, 1024, VPT>(a, stream);
-        default: break;
+    if (alike(a.x, a.ld_x, a.out, a.ld_out, a.tokens, sizeof(T))) {
+        constexpr int VPT = sizeof(T) == 2 ? 2 : 4, STAGES = 4;
+        const auto kernel = norm_rows_kernel<T, VPT, STAGES>;
+        const RowPlan p = row_plan(kernel, most_granules<T>(a.x, a.ld_x, a.tokens, a.features), VPT, 1, STAGES, a.tokens);
+        if (p.threads > 0)
+            return launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * STAGES, stream, 1, true, a,
+                             p.stage_bytes);
     }
     return launch_ex(norm_any_kernel<T>, dim3(unsigned(a.tokens)), dim3(kAnyThreads), 0, stream, 1, true, a);
 }
@@ -518,17 +640,8 @@ int64_t most_partials(darb_layout_t layout, int64_t steps, int64_t tokens) {
     return std::min<int64_t>((tokens + 63) / 64 * 64, int64_t(sm_count()) * 32);
 }
 
-template <typename T, int GROUP, int VPT>
-cudaError_t launch_back_group(const NormArgs &a, int64_t *partials, cudaStream_t stream) {
-    using R = RowsOf<GROUP>;
-    const int64_t grid = row_grid(a.tokens, R::kPerCta, std::max(1, 1024 / R::kThreads));
-    *partials = grid * R::kPerCta;
-    return launch_ex(back_rows_kernel<T, GROUP, VPT>, dim3(unsigned(grid)), dim3(R::kThreads), 0, stream, 1, true, a);
-}
-
 template <typename T>
 cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, float *dbeta, cudaStream_t stream) {
-    constexpr int VPT = sizeof(T) == 2 ? 1 : 2;
     cudaError_t e = cudaSuccess;
     int64_t partials = 0;
     if (layout == DARB_TOKEN_COLUMNS) {
@@ -542,22 +655,27 @@ cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, 
     } else {
         const bool same = alike(a.x, a.ld_x, a.out, a.ld_out, a.tokens, sizeof(T)) &&
                           alike(a.x, a.ld_x, a.dy, a.ld_dy, a.tokens, sizeof(T));
-        switch (same ? row_group<T>(a.features, VPT) : 0) {
-            case 32: e = launch_back_group<T, 32, VPT>(a, &partials, stream); break;
-            case 64: e = launch_back_group<T, 64, VPT>(a, &partials, stream); break;
-            case 128: e = launch_back_group<T, 128, VPT>(a, &partials, stream); break;
-            case 256: e = launch_back_group<T, 256, VPT>(a, &partials, stream); break;
-            case 512: e = launch_back_group<T, 512, VPT>(a, &partials, stream); break;
-            case 1024: e = launch_back_group<T, 1024, VPT>(a, &partials, stream); break;
-            default:
-                if (a.partial != nullptr) {
-                    partials = std::min<int64_t>(a.tokens, std::min<int64_t>(64, most_partials(layout, a.steps, a.tokens)));
-                    e = launch_ex(row_sums_kernel<T>, dim3(unsigned((a.features + kAnyThreads - 1) / kAnyThreads), unsigned(partials)),
-                                  dim3(kAnyThreads), 0, stream, 1, true, a);
-                }
-                if (e == cudaSuccess)
-                    e = launch_ex(back_any_kernel<T>, dim3(unsigned(a.tokens)), dim3(kAnyThreads), 0, stream, 1, true, a);
-                break;
+        constexpr int STAGES = 3;
+        const int64_t granules = most_granules<T>(a.x, a.ld_x, a.tokens, a.features);
+        const auto rows = [&](auto kernel, int vpt) {
+            const RowPlan p = row_plan(kernel, granules, vpt, 2, STAGES, a.tokens);
+            if (p.threads == 0) return cudaErrorNotSupported;
+            partials = p.grid;
+            return launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * STAGES, stream, 1, true, a,
+                             p.stage_bytes);
+        };
+        e = same ? rows(back_rows_kernel<T, 2, STAGES>, 2) : cudaErrorNotSupported;
+        if constexpr (sizeof(T) == 4)
+            if (same && e == cudaErrorNotSupported) e = rows(back_rows_kernel<T, 4, STAGES>, 4);
+        if (e == cudaErrorNotSupported) {
+            e = cudaSuccess;
+            if (a.partial != nullptr) {
+                partials = std::min<int64_t>(a.tokens, std::min<int64_t>(64, most_partials(layout, a.steps, a.tokens)));
+                e = launch_ex(row_sums_kernel<T>, dim3(unsigned((a.features + kAnyThreads - 1) / kAnyThreads), unsigned(partials)),
+                              dim3(kAnyThreads), 0, stream, 1, true, a);
+            }
+            if (e == cudaSuccess)
+                e = launch_ex(back_any_kernel<T>, dim3(unsigned(a.tokens)), dim3(kAnyThreads), 0, stream, 1, true, a);
         }
     }
     if (e == cudaSuccess && a.partial != nullptr)
