@@ -50,8 +50,12 @@ struct NormArgs {
     const float *gamma, *beta;   // or null
     float eps;
     float *mean, *rstd;          // forward: written (or null); backward: read
-    float *partial;              // backward: scratch, [partials][2][features], or null
+    float *partial;              // backward: scratch, [partials][2][partial_width], or null
 };
+
+// Floats of one half of a partial result: the features, moved by less than a
+// granule, in whole granules.
+__host__ __device__ __forceinline__ int64_t partial_width(int32_t features) { return (int64_t(features) + 7 + 7) / 8 * 8; }
 
 __device__ __forceinline__ float gamma_at(const NormArgs &a, int32_t f) { return a.gamma ? __ldg(a.gamma + f) : 1.0f; }
 __device__ __forceinline__ float beta_at(const NormArgs &a, int32_t f) { return a.beta ? __ldg(a.beta + f) : 0.0f; }
@@ -150,44 +154,55 @@ struct Owned {
     // The granules of a row as pairs, 0 outside the row.  `stage`: this thread's
     // granule 0 of the row as copied.
     __device__ __forceinline__ void load(const RowCopies<T> &rows, int64_t r, const unsigned char *stage, bool arrived,
-                                         float2 (&v)[VPT][V / 2]) const {
+                                         Pair (&v)[VPT][V / 2]) const {
         const bool inner = r >= 8 && r + 8 < rows.count;   // all its granules are copied: 8 values are 16 bytes or more
 #pragma unroll
         for (int u = 0; u < VPT; ++u) {
-            float w[V];
             if (whole(u)) {
-                unpack(*reinterpret_cast<const uint4 *>(stage + u * step * int(sizeof(T))), w);
+                unpack(*reinterpret_cast<const uint4 *>(stage + u * step * int(sizeof(T))), v[u]);
             } else if (feature(u) < n && inner) {
-                unpack(*reinterpret_cast<const uint4 *>(stage + u * step * int(sizeof(T))), w);
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    if (!in(u, e)) w[e] = 0.0f;
+                unpack(*reinterpret_cast<const uint4 *>(stage + u * step * int(sizeof(T))), v[u]);
+                clear_outside(u, v[u]);
             } else {
-                unpack(load_granule<T, false>(rows.base + r * rows.ld, feature(u), n, 0.0f), w);
+                unpack(load_granule<T, false>(rows.base + r * rows.ld, feature(u), n, 0.0f), v[u]);
             }
-#pragma unroll
-            for (int e = 0; e < V; e += 2) v[u][e / 2] = make_float2(w[e], w[e + 1]);
         }
-        if (!arrived) v[0][0].x = __uint_as_float(0x7FC00000u);   // a copy that never came: the row is NaN
+        if (!arrived) v[0][0] = both(__uint_as_float(0x7FC00000u));   // a copy that never came: the row is NaN
     }
-    __device__ __forceinline__ void store(T *row, const float2 (&v)[VPT][V / 2]) const {
+    __device__ __forceinline__ void clear_outside(int u, Pair (&v)[V / 2]) const {
+#pragma unroll
+        for (int e = 0; e < V; e += 2) v[e / 2] = pair(in(u, e) ? low(v[e / 2]) : 0.0f, in(u, e + 1) ? high(v[e / 2]) : 0.0f);
+    }
+    __device__ __forceinline__ void store(T *row, const Pair (&v)[VPT][V / 2]) const {
 #pragma unroll
         for (int u = 0; u < VPT; ++u) {
-            float w[V];
+            if (whole(u)) {
+                *reinterpret_cast<uint4 *>(row + feature(u)) = pack(v[u]);
+            } else {
+                float w[V];
 #pragma unroll
-            for (int e = 0; e < V; e += 2) w[e] = v[u][e / 2].x, w[e + 1] = v[u][e / 2].y;
-            if (whole(u)) *reinterpret_cast<uint4 *>(row + feature(u)) = pack(w);
-            else store_granule(row, feature(u), n, w);
+                for (int e = 0; e < V; e += 2) w[e] = low(v[u][e / 2]), w[e + 1] = high(v[u][e / 2]);
+                store_granule(row, feature(u), n, w);
+            }
         }
     }
-    // Values of a vector over the features, 0 outside.
-    template <typename F>
-    __device__ __forceinline__ void gather(F at, float2 (&v)[VPT][V / 2]) const {
+    // Values of a vector over the features (null: `none`), 0 outside.
+    __device__ __forceinline__ void gather(const float *p, float none, Pair (&v)[VPT][V / 2]) const {
 #pragma unroll
-        for (int u = 0; u < VPT; ++u)
+        for (int u = 0; u < VPT; ++u) {
+            if (p != nullptr && whole(u) && (reinterpret_cast<uintptr_t>(p + feature(u)) & 15) == 0) {
 #pragma unroll
-            for (int e = 0; e < V; e += 2)
-                v[u][e / 2] = make_float2(in(u, e) ? at(feature(u) + e) : 0.0f, in(u, e + 1) ? at(feature(u) + e + 1) : 0.0f);
+                for (int e = 0; e < V; e += 4) {
+                    const float4 q = __ldg(reinterpret_cast<const float4 *>(p + feature(u) + e));
+                    v[u][e / 2] = pair(q.x, q.y);
+                    v[u][e / 2 + 1] = pair(q.z, q.w);
+                }
+            } else {
+                const auto at = [&](int e) { return !in(u, e) ? 0.0f : p == nullptr ? none : __ldg(p + feature(u) + e); };
+#pragma unroll
+                for (int e = 0; e < V; e += 2) v[u][e / 2] = pair(at(e), at(e + 1));
+            }
+        }
     }
 };
 
@@ -220,23 +235,23 @@ __global__ void __launch_bounds__(kRowThreads) norm_rows_kernel(const NormArgs a
     const float inv_n = __fdiv_rn(1.0f, float(n));
     // all rows of this CTA start alike
     const Owned<T, VPT> own = {t * V - row_head<T>(rows.base + r0 * a.ld_x), threads * V, n};
-    float2 gm[VPT][H], bt[VPT][H];
-    own.gather([&](int32_t f) { return gamma_at(a, f); }, gm);
-    own.gather([&](int32_t f) { return beta_at(a, f); }, bt);
+    Pair gm[VPT][H], bt[VPT][H];
+    own.gather(a.gamma, 1.0f, gm);
+    own.gather(a.beta, 0.0f, bt);
     clear_sums(buf, 2 * kSumWarps);
     T *y = static_cast<T *>(a.out);
     int turn = 0, stage = 0;
     uint32_t parity = 0;
     bool arrived = true;
     for (int64_t r = r0; r < a.tokens; r += stride) {
-        float2 v[VPT][H], s2 = both(0.0f);
+        Pair v[VPT][H], s2 = both(0.0f);
         arrived = arrived && mbar_wait(&full[stage], parity);
         own.load(rows, r, ring + stage * stage_bytes + t * 16, arrived, v);
 #pragma unroll
         for (int u = 0; u < VPT; ++u)
 #pragma unroll
             for (int e = 0; e < H; ++e) s2 = add2(s2, v[u][e]);
-        float s[1] = {s2.x + s2.y};
+        float s[1] = {across(s2)};
         cta_sum(s, buf, turn);   // every thread has read the stage
         if (t == 0 && arrived && r + STAGES * stride < a.tokens) issue(r + STAGES * stride, stage);
         if (++stage == STAGES) stage = 0, parity ^= 1;
@@ -246,17 +261,11 @@ __global__ void __launch_bounds__(kRowThreads) norm_rows_kernel(const NormArgs a
         for (int u = 0; u < VPT; ++u) {
 #pragma unroll
             for (int e = 0; e < H; ++e) v[u][e] = add2(v[u][e], both(-mean));
-            if (!own.whole(u)) {
-#pragma unroll
-                for (int e = 0; e < H; ++e) {
-                    if (!own.in(u, 2 * e)) v[u][e].x = 0.0f;
-                    if (!own.in(u, 2 * e + 1)) v[u][e].y = 0.0f;
-                }
-            }
+            if (!own.whole(u)) own.clear_outside(u, v[u]);
 #pragma unroll
             for (int e = 0; e < H; ++e) s2 = fma2(v[u][e], v[u][e], s2);
         }
-        s[0] = s2.x + s2.y;
+        s[0] = across(s2);
         cta_sum(s, buf, turn);
         const float rstd = inverse_root(s[0] * inv_n + a.eps);
         if (t == 0) {
@@ -297,10 +306,12 @@ __global__ void __launch_bounds__(kRowThreads) back_rows_kernel(const NormArgs a
             if (r0 + s * stride < a.tokens) issue(r0 + s * stride, s);
     const float inv_n = __fdiv_rn(1.0f, float(n));
     const Owned<T, VPT> own = {t * V - row_head<T>(xs.base + r0 * a.ld_x), threads * V, n};
-    float2 gm[VPT][H], sg[VPT][H], sb[VPT][H];
-    own.gather([&](int32_t f) { return gamma_at(a, f); }, gm);
-    own.gather([](int32_t) { return 0.0f; }, sg);
-    own.gather([](int32_t) { return 0.0f; }, sb);
+    Pair gm[VPT][H], sg[VPT][H], sb[VPT][H];
+    own.gather(a.gamma, 1.0f, gm);
+#pragma unroll
+    for (int u = 0; u < VPT; ++u)
+#pragma unroll
+        for (int e = 0; e < H; ++e) sg[u][e] = sb[u][e] = both(0.0f);
     clear_sums(buf, 2 * 2 * kSumWarps);
     T *dx = static_cast<T *>(a.out);
     int turn = 0, stage = 0;
@@ -309,7 +320,7 @@ __global__ void __launch_bounds__(kRowThreads) back_rows_kernel(const NormArgs a
     float mean_next = 0.0f, rstd_next = 0.0f;
     if (r0 < a.tokens) mean_next = __ldg(a.mean + r0), rstd_next = __ldg(a.rstd + r0);
     for (int64_t r = r0; r < a.tokens; r += stride) {
-        float2 xh[VPT][H], d[VPT][H], s0 = both(0.0f), s1 = both(0.0f);
+        Pair xh[VPT][H], d[VPT][H], s0 = both(0.0f), s1 = both(0.0f);
         const float mean = mean_next, rstd = rstd_next;
         if (r + stride < a.tokens) mean_next = __ldg(a.mean + r + stride), rstd_next = __ldg(a.rstd + r + stride);
         arrived = arrived && mbar_wait(&full[stage], parity);
@@ -327,7 +338,7 @@ __global__ void __launch_bounds__(kRowThreads) back_rows_kernel(const NormArgs a
                 s0 = add2(s0, d[u][e]);
                 s1 = fma2(d[u][e], xh[u][e], s1);
             }
-        float s[2] = {s0.x + s0.y, s1.x + s1.y};
+        float s[2] = {across(s0), across(s1)};
         cta_sum(s, buf, turn);   // every thread has read the stage
         if (t == 0 && arrived && r + STAGES * stride < a.tokens) issue(r + STAGES * stride, stage);
         if (++stage == STAGES) stage = 0, parity ^= 1;
@@ -340,35 +351,45 @@ __global__ void __launch_bounds__(kRowThreads) back_rows_kernel(const NormArgs a
         own.store(dx + r * a.ld_out, d);
     }
     if (a.partial != nullptr) {
-        float *p = a.partial + r0 * 2 * int64_t(n);
+        // as the thread holds them: feature f at f + the head of this CTA's rows
+        const int64_t width = partial_width(n);
+        float *p = a.partial + r0 * 2 * width;
 #pragma unroll
         for (int u = 0; u < VPT; ++u)
+            if (own.feature(u) < n) {
+                float4 *g = reinterpret_cast<float4 *>(p + (u * threads + t) * V), *b = reinterpret_cast<float4 *>(p + width + (u * threads + t) * V);
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                if (own.in(u, e)) {
-                    p[own.feature(u) + e] = e & 1 ? sg[u][e / 2].y : sg[u][e / 2].x;
-                    p[n + own.feature(u) + e] = e & 1 ? sb[u][e / 2].y : sb[u][e / 2].x;
+                for (int e = 0; e < H; e += 2) {
+                    g[e / 2] = make_float4(low(sg[u][e]), high(sg[u][e]), low(sg[u][e + 1]), high(sg[u][e + 1]));
+                    b[e / 2] = make_float4(low(sb[u][e]), high(sb[u][e]), low(sb[u][e + 1]), high(sb[u][e + 1]));
                 }
+            }
     }
 }
 
-// out[i] = sum over p of partial[p][i], i in [0, 2F): 32 values a CTA, the
-// partial results shared by its warps, joined in order.
+// dgamma and dbeta from the partial results: 32 features of one of them a CTA,
+// the partial results shared by its warps, joined in order.  Where rows p of
+// the kernel that made them start `base` + p * `step` bytes from a 16-byte
+// boundary, feature f lies that many elements further.
 __global__ void __launch_bounds__(1024) sum_partials_kernel(const float *partial, int32_t partials, int32_t features,
-                                                            float *dgamma, float *dbeta) {
+                                                            uint32_t base, uint32_t step, uint32_t size, float *dgamma,
+                                                            float *dbeta) {
     __shared__ float s[32][33];
     pdl_wait_previous();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const int64_t width = 2 * int64_t(features), i = int64_t(blockIdx.x) * 32 + lane;
+    const int64_t width = partial_width(features);
+    const int32_t f = int32_t(blockIdx.x) * 32 + lane;
+    const float *at = partial + blockIdx.y * width + f;
     float v = 0.0f;
-    if (i < width)
-        for (int32_t p = w; p < partials; p += 32) v += partial[p * width + i];
+    if (f < features)
+        for (int32_t p = w; p < partials; p += 32)
+            v += at[int64_t(p) * 2 * width + ((base + uint32_t(p) * step) & 15u) / size];
     s[w][lane] = v;
     __syncthreads();
-    v = warp_sum(s[lane][w]);   // of value blockIdx.x * 32 + w
-    const int64_t j = int64_t(blockIdx.x) * 32 + w;
-    if (lane == 0 && j < width) (j < features ? dgamma + j : dbeta + (j - features))[0] = v;
+    v = warp_sum(s[lane][w]);   // of feature blockIdx.x * 32 + w
+    const int32_t j = int32_t(blockIdx.x) * 32 + w;
+    if (lane == 0 && j < features) (blockIdx.y ? dbeta : dgamma)[j] = v;
 }
 
 // Rows of any length and alignment: a CTA a row, read again for every sum.
@@ -446,9 +467,9 @@ __global__ void __launch_bounds__(kAnyThreads) row_sums_kernel(const NormArgs a)
         sg = fmaf(d, (widen(x[r * a.ld_x]) - __ldg(a.mean + r)) * __ldg(a.rstd + r), sg);
         sb += d;
     }
-    float *p = a.partial + int64_t(blockIdx.y) * 2 * n;
+    float *p = a.partial + int64_t(blockIdx.y) * 2 * partial_width(n);
     p[f] = sg;
-    p[n + f] = sb;
+    p[partial_width(n) + f] = sb;
 }
 
 // ---- token columns ----
@@ -543,9 +564,9 @@ __global__ void __launch_bounds__(kColThreads) back_columns_kernel(const NormArg
             // the feature's sums over this tile's tokens, one partial result a tile
             const float sg = warp_sum(d * xh), sb = warp_sum(d);
             if (lane == 0) {
-                float *p = a.partial + tile * 2 * n;
+                float *p = a.partial + tile * 2 * partial_width(n);
                 p[f] = sg;
-                p[n + f] = sb;
+                p[partial_width(n) + f] = sb;
             }
         }
         const float g = d * gamma_at(a, f);
@@ -644,6 +665,7 @@ template <typename T>
 cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, float *dbeta, cudaStream_t stream) {
     cudaError_t e = cudaSuccess;
     int64_t partials = 0;
+    uint32_t base = 0, step = 0;   // of the partial results' rows, in bytes
     if (layout == DARB_TOKEN_COLUMNS) {
         const int64_t tiles = (a.tokens + 31) / 32, all = tiles * a.steps;
         int split = 1;
@@ -661,6 +683,8 @@ cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, 
             const RowPlan p = row_plan(kernel, granules, vpt, 2, STAGES, a.tokens);
             if (p.threads == 0) return cudaErrorNotSupported;
             partials = p.grid;
+            base = uint32_t(reinterpret_cast<uintptr_t>(a.x));
+            step = uint32_t(a.ld_x * int64_t(sizeof(T)));
             return launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * STAGES, stream, 1, true, a,
                              p.stage_bytes);
         };
@@ -679,8 +703,9 @@ cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, 
         }
     }
     if (e == cudaSuccess && a.partial != nullptr)
-        e = launch_ex(sum_partials_kernel, dim3(unsigned((2 * int64_t(a.features) + 31) / 32)), dim3(1024), 0, stream, 1, true,
-                      static_cast<const float *>(a.partial), int32_t(partials), a.features, dgamma, dbeta);
+        e = launch_ex(sum_partials_kernel, dim3(unsigned((a.features + 31) / 32), 2), dim3(1024), 0, stream, 1, true,
+                      static_cast<const float *>(a.partial), int32_t(partials), a.features, base, step, uint32_t(sizeof(T)),
+                      dgamma, dbeta);
     return e;
 }
 
@@ -741,7 +766,7 @@ darb_status_t darb_layer_norm_grad_work(darb_layout_t layout, int64_t steps, int
     if (bytes == nullptr) return DARB_ERR_INVALID_ARG;
     const darb_status_t st = check_norm(DARB_F32, layout, steps, tokens, features);
     if (st != DARB_OK) return st == DARB_ERR_UNSUPPORTED ? st : DARB_ERR_INVALID_ARG;
-    *bytes = most_partials(layout, steps, tokens) * 2 * features * 4;
+    *bytes = most_partials(layout, steps, tokens) * 2 * partial_width(int32_t(features)) * 4;
     return DARB_OK;
 }
 
@@ -773,7 +798,7 @@ darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x,
     const bool in_place = dx == dy && ld_dx == ld_dy;
     const int64_t all = steps * tokens;
     const Range outs[] = {{dx, no * int64_t(es)}, {dgamma, features * 4}, {dbeta, features * 4},
-                          {dgamma ? work : nullptr, most_partials(layout, steps, tokens) * 8 * features}};
+                          {dgamma ? work : nullptr, most_partials(layout, steps, tokens) * 8 * partial_width(int32_t(features))}};
     const Range ins[] = {{in_place ? nullptr : dy, nd * int64_t(es)}, {x, nx * int64_t(es)}, {gamma, features * 4},
                          {mean, all * 4}, {rstd, all * 4}};
     if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;

@@ -87,9 +87,9 @@ __device__ __forceinline__ Part warp_join(Part p) {
 // that no addition chain is longer than a block plus the number of blocks.
 struct Running {
     float m, r;
-    float2 s, t;
+    Pair s, t;
 };
-__device__ __forceinline__ Running no_sums() { return {kMasked, kMasked * kLog2e, {0.0f, 0.0f}, {0.0f, 0.0f}}; }
+__device__ __forceinline__ Running no_sums() { return {kMasked, reference(kMasked), both(0.0f), both(0.0f)}; }
 __device__ __forceinline__ void rebase(Running &a, float top) {
     a.m = max_nan(a.m, top);
     const float r = reference(a.m), d = __fsub_rn(a.r, r), f = exp2_fast(d);
@@ -97,9 +97,9 @@ __device__ __forceinline__ void rebase(Running &a, float top) {
     a.s = mul2(both(f), a.s);
     a.r = r;
 }
-__device__ __forceinline__ void add_pair(float2 x, float r, float2 &s, float2 &t) {
-    const float2 d = fma2(x, both(kLog2e), both(-r));
-    const float2 e = make_float2(exp2_fast(d.x), exp2_fast(d.y));
+__device__ __forceinline__ void add_pair(Pair x, float r, Pair &s, Pair &t) {
+    const Pair d = fma2(x, both(kLog2e), both(-r));
+    const Pair e = pair(exp2_fast(low(d)), exp2_fast(high(d)));
     s = add2(s, e);
     t = fma2(e, d, t);
 }
@@ -408,13 +408,13 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
             }
         }
         rebase(sum, top);
-        float2 s2 = both(0.0f), t2 = both(0.0f);
+        Pair s2 = both(0.0f), t2 = both(0.0f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            float v[V];
+            Pair v[V / 2];
             unpack(q[u], v);
 #pragma unroll
-            for (int i = 0; i < V; i += 2) add_pair(make_float2(v[i], v[i + 1]), sum.r, s2, t2);
+            for (int i = 0; i < V / 2; ++i) add_pair(v[i], sum.r, s2, t2);
         }
         sum.s = add2(sum.s, s2);
         sum.t = add2(sum.t, t2);
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
         if (in_slot > 0) block_max[slot++ * THREADS + tid] = slot_max;
         thread_max[tid] = sum.m;
     }
-    const Part mine = warp_join({sum.m, sum.s.x + sum.s.y, sum.t.x + sum.t.y});
+    const Part mine = warp_join({sum.m, across(sum.s), across(sum.t)});
     if (lane == 0) warp_part[warp] = mine;
     __syncthreads();
     Part all;   // of the CTA; warp 0 has it
@@ -588,14 +588,14 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
             }
         }
         rebase(sum, top);
-        float2 s2 = both(0.0f), t2 = both(0.0f);
+        Pair s2 = both(0.0f), t2 = both(0.0f);
 #pragma unroll
-        for (int u = 0; u < U; u += 2) add_pair(make_float2(x[u], x[u + 1]), sum.r, s2, t2);
+        for (int u = 0; u < U; u += 2) add_pair(pair(x[u], x[u + 1]), sum.r, s2, t2);
         sum.s = add2(sum.s, s2);
         sum.t = add2(sum.t, t2);
     }
     if (in_block > 0) sh.block_max[block++][tid] = slot_max;
-    sh.part[slot][col] = {sum.m, sum.s.x + sum.s.y, sum.t.x + sum.t.y};
+    sh.part[slot][col] = {sum.m, across(sum.s), across(sum.t)};
     __syncthreads();
     // warp c joins column c (c < CT <= 32 warps), and finds the bar of its k largest
     if (warp < CT) {

@@ -116,29 +116,61 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     return y;
 }
 
-// Two fp32 values in a register pair: each half is one IEEE operation.
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 r;
-    asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n"
-        " add.rn.f32x2 z, x, y;\n mov.b64 {%0, %1}, z;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+// Two fp32 values in a register pair; an operation on pairs is one instruction,
+// each half of it one IEEE operation.
+struct Pair {
+    unsigned long long bits;
+};
+__device__ __forceinline__ Pair pair(float x, float y) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.bits) : "f"(x), "f"(y));
+    return p;
+}
+__device__ __forceinline__ Pair both(float v) { return pair(v, v); }
+__device__ __forceinline__ float low(Pair p) { return __uint_as_float(uint32_t(p.bits)); }
+__device__ __forceinline__ float high(Pair p) { return __uint_as_float(uint32_t(p.bits >> 32)); }
+__device__ __forceinline__ float across(Pair p) { return low(p) + high(p); }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
     return r;
 }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 r;
-    asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n"
-        " mul.rn.f32x2 z, x, y;\n mov.b64 {%0, %1}, z;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
     return r;
 }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 r;
-    asm("{\n .reg .b64 x, y, z, w;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n"
-        " fma.rn.f32x2 w, x, y, z;\n mov.b64 {%0, %1}, w;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
     return r;
 }
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// A granule as pairs, and back.
+__device__ __forceinline__ void unpack(const uint4 &q, Pair (&v)[2]) {
+    v[0].bits = uint64_t(q.x) | uint64_t(q.y) << 32;
+    v[1].bits = uint64_t(q.z) | uint64_t(q.w) << 32;
+}
+__device__ __forceinline__ void unpack(const uint4 &q, Pair (&v)[4]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = widen2(w[i]);
+        v[i] = pair(f.x, f.y);
+    }
+}
+__device__ __forceinline__ uint4 pack(const Pair (&v)[2]) {
+    return make_uint4(uint32_t(v[0].bits), uint32_t(v[0].bits >> 32), uint32_t(v[1].bits), uint32_t(v[1].bits >> 32));
+}
+__device__ __forceinline__ uint4 pack(const Pair (&v)[4]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(low(v[i]), high(v[i]));
+        w[i] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 
 // ---- host side: argument checks ----
 inline bool token_dtype(darb_dtype_t t) { return t == DARB_F32 || t == DARB_BF16; }
