@@ -206,10 +206,12 @@ struct Owned {
     }
 };
 
-constexpr int kRowThreads = 512;   // threads that share a row, at most
+// Threads that share a row, at most, by the granules that each has: what leaves
+// it the registers for them.
+constexpr int row_threads(int vpt) { return vpt > 2 ? 256 : 512; }
 
 template <typename T, int VPT, int STAGES>
-__global__ void __launch_bounds__(kRowThreads) norm_rows_kernel(const NormArgs a, int32_t stage_bytes) {
+__global__ void __launch_bounds__(row_threads(VPT)) norm_rows_kernel(const NormArgs a, int32_t stage_bytes) {
     constexpr int V = kPerGranule<T>, H = V / 2;
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ __align__(16) float buf[2 * kSumWarps];
@@ -281,7 +283,7 @@ __global__ void __launch_bounds__(kRowThreads) norm_rows_kernel(const NormArgs a
 }
 
 template <typename T, int VPT, int STAGES>
-__global__ void __launch_bounds__(kRowThreads) back_rows_kernel(const NormArgs a, int32_t stage_bytes) {
+__global__ void __launch_bounds__(row_threads(VPT)) back_rows_kernel(const NormArgs a, int32_t stage_bytes) {
     constexpr int V = kPerGranule<T>, H = V / 2;
     extern __shared__ __align__(16) unsigned char ring[];   // a stage: a row of x, a row of dy
     __shared__ __align__(16) float buf[2 * 2 * kSumWarps];
@@ -610,10 +612,10 @@ template <typename Kernel>
 RowPlan row_plan(Kernel kernel, int64_t granules, int vpt, int copies, int stages, int64_t rows) {
     RowPlan p = {};
     const int64_t threads = ((granules + vpt - 1) / vpt + 31) / 32 * 32;
-    p.stage_bytes = int32_t(std::min<int64_t>(granules, int64_t(kRowThreads) * vpt)) * 16 * copies;
+    p.stage_bytes = int32_t(std::min<int64_t>(granules, int64_t(row_threads(vpt)) * vpt)) * 16 * copies;
     const size_t smem = size_t(p.stage_bytes) * stages;
     // (the kernel's own shared memory counts against the limit that needs no asking)
-    if (threads > kRowThreads || allow_smem(kernel, smem + 1024) != cudaSuccess) return p;
+    if (threads > row_threads(vpt) || allow_smem(kernel, smem + 1024) != cudaSuccess) return p;
     const int64_t per_sm = per_device(reinterpret_cast<const void *>(kernel), int64_t(threads) << 32 | int64_t(smem), [&]() -> long long {
         int n = 0;
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, int(threads), smem) != cudaSuccess) {
@@ -645,12 +647,18 @@ cudaError_t launch_norm(const NormArgs &a, darb_layout_t layout, cudaStream_t st
                          unsigned(split), true, a, int32_t(tiles));
     }
     if (alike(a.x, a.ld_x, a.out, a.ld_out, a.tokens, sizeof(T))) {
-        constexpr int VPT = sizeof(T) == 2 ? 2 : 4, STAGES = 4;
-        const auto kernel = norm_rows_kernel<T, VPT, STAGES>;
-        const RowPlan p = row_plan(kernel, most_granules<T>(a.x, a.ld_x, a.tokens, a.features), VPT, 1, STAGES, a.tokens);
-        if (p.threads > 0)
+        constexpr int STAGES = 4;
+        const int64_t granules = most_granules<T>(a.x, a.ld_x, a.tokens, a.features);
+        const auto rows = [&](auto kernel, int vpt) {
+            const RowPlan p = row_plan(kernel, granules, vpt, 1, STAGES, a.tokens);
+            if (p.threads == 0) return cudaErrorNotSupported;
             return launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * STAGES, stream, 1, true, a,
                              p.stage_bytes);
+        };
+        cudaError_t e = rows(norm_rows_kernel<T, 4, STAGES>, 4);
+        if constexpr (sizeof(T) == 4)
+            if (e == cudaErrorNotSupported) e = rows(norm_rows_kernel<T, 8, STAGES>, 8);
+        if (e != cudaErrorNotSupported) return e;
     }
     return launch_ex(norm_any_kernel<T>, dim3(unsigned(a.tokens)), dim3(kAnyThreads), 0, stream, 1, true, a);
 }
@@ -688,9 +696,9 @@ cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, 
             return launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * STAGES, stream, 1, true, a,
                              p.stage_bytes);
         };
-        e = same ? rows(back_rows_kernel<T, 2, STAGES>, 2) : cudaErrorNotSupported;
+        e = same ? rows(back_rows_kernel<T, 4, STAGES>, 4) : cudaErrorNotSupported;
         if constexpr (sizeof(T) == 4)
-            if (same && e == cudaErrorNotSupported) e = rows(back_rows_kernel<T, 4, STAGES>, 4);
+            if (same && e == cudaErrorNotSupported) e = rows(back_rows_kernel<T, 8, STAGES>, 8);
         if (e == cudaErrorNotSupported) {
             e = cudaSuccess;
             if (a.partial != nullptr) {
