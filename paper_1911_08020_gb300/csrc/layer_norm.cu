@@ -20,9 +20,12 @@
 // arrive through a ring of bulk copies in shared memory: the bytes in flight do
 // not depend on how many registers the threads leave for occupancy.
 //
-// Token columns.  A CTA takes 32 tokens of a step and a share of the features,
-// lane = token; the CTAs of a cluster share a tile and exchange their sums
-// through distributed shared memory.
+// Token columns.  A CTA takes a tile of CT tokens of a step and a share of the
+// features; thread = (slot, token), so that a row of the tile is one contiguous
+// run, and a thread reads kColBatch of its rows at a time.  The CTAs of a cluster
+// share a tile and exchange their sums once through distributed shared memory.
+// A share of one batch a thread stays in registers between the sums and the
+// output; larger ones are read again, from L1 or L2.
 #include "launch.cuh"
 #include "tma.cuh"
 #include "tokens.cuh"
@@ -32,6 +35,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace cg = cooperative_groups;
 
@@ -476,112 +480,234 @@ __global__ void __launch_bounds__(kAnyThreads) row_sums_kernel(const NormArgs a)
 
 // ---- token columns ----
 
-constexpr int kColThreads = 1024;   // 32 tokens x 32 slots
+constexpr int kColThreads = 512;
 constexpr int kColWarps = kColThreads / 32;
-constexpr int kColSplit = 8;        // CTAs that share a tile, at most
+constexpr int kColBatch = 16;
+constexpr int kColSplit = 8;   // CTAs that share a tile, at most
 
-// Sums of N values over the slots of a column and the CTAs of the cluster, for
-// the column of the thread's lane.  part: [N][32][33], sum: [N][32] floats of
-// shared memory.
-template <int N>
-__device__ __forceinline__ void column_sum(float (&v)[N], float (*part)[32][33], float (*sum)[32], cg::cluster_group &cluster) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int split = int(cluster.num_blocks());
+// The rows of a thread: features f0 + slot + i * SLOTS, in batches.
+template <typename T, int CT>
+struct ColShare {
+    static constexpr int SLOTS = kColThreads / CT, U = kColBatch;
+    int32_t first, end;   // features of the thread: first, first + SLOTS, ... below end
+    __device__ __forceinline__ int count() const { return first < end ? (end - first + SLOTS - 1) / SLOTS : 0; }
+    __device__ __forceinline__ int32_t feature(int batch, int u) const { return first + (batch * U + u) * SLOTS; }
+    __device__ __forceinline__ void load(const T *x, int64_t ld, int batch, bool in, float (&v)[U]) const {
 #pragma unroll
-    for (int i = 0; i < N; ++i) part[i][warp][lane] = v[i];
+        for (int u = 0; u < U; ++u) {
+            const int32_t f = feature(batch, u);
+            v[u] = in && f < end ? widen(x[f * ld]) : 0.0f;
+        }
+    }
+};
+
+template <typename T, int CT>
+__global__ void __launch_bounds__(kColThreads) norm_columns_kernel(const NormArgs a, int32_t tiles) {
+    using Share = ColShare<T, CT>;
+    constexpr int SLOTS = Share::SLOTS, U = Share::U;
+    __shared__ float p_mean[SLOTS][CT + 1], p_m2[SLOTS][CT + 1];
+    __shared__ float2 s_part[CT], s_stat[CT];   // (mean, centred squares) of this CTA; (mean, rstd) of the token
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int split = int(cluster.num_blocks()), rank = int(cluster.block_rank());
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = threadIdx.x % CT, slot = threadIdx.x / CT;
+    const int64_t tile = blockIdx.x / split, step = tile / tiles, c = (tile % tiles) * CT + col;
+    const bool in = c < a.tokens;
+    const int32_t n = a.features;
+    const auto start = [&](int q) { return int32_t(int64_t(n) * q / split); };
+    const int32_t f0 = start(rank), f1 = start(rank + 1);
+    const Share share = {f0 + slot, f1};
+    const T *x = static_cast<const T *>(a.x) + step * n * a.ld_x + c;
+    T *y = static_cast<T *>(a.out) + step * n * a.ld_out + c;
+    const int rows = share.count(), batches = (rows + U - 1) / U;
+    // mean and centred squares of the thread's rows, a batch at a time joined to those before
+    float v[U], mean = 0.0f, m2 = 0.0f;
+    for (int b = 0; b < batches; ++b) {
+        share.load(x, a.ld_x, b, in, v);
+        const int have = min(U, rows - b * U);
+        float s = 0.0f, q = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) s += v[u];
+        const float bm = s / float(have);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float d = u < have ? v[u] - bm : 0.0f;
+            q = fmaf(d, d, q);
+        }
+        const float part = float(have) / float(b * U + have), d = bm - mean;
+        mean = fmaf(d, part, mean);
+        m2 += q + d * d * (float(b * U) * part);
+    }
+    p_mean[slot][col] = mean;
+    p_m2[slot][col] = m2;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float s = warp_sum(part[i][lane][warp]);   // of column `warp`
-        if (lane == 0) sum[i][warp] = s;
+    // a warp joins the slots of a column: the mean first, then the squares about it
+    for (int k = warp; k < CT; k += kColWarps) {
+        const int32_t m = f1 - f0;
+        float sum = 0.0f;
+        for (int s = lane; s < SLOTS; s += 32) sum = fmaf(float(s < m ? (m - s + SLOTS - 1) / SLOTS : 0), p_mean[s][k], sum);
+        const float all = m > 0 ? warp_sum(sum) / float(m) : 0.0f;
+        float q = 0.0f;
+        for (int s = lane; s < SLOTS; s += 32) {
+            const float d = p_mean[s][k] - all;
+            if (s < m) q += fmaf(d * d, float((m - s + SLOTS - 1) / SLOTS), p_m2[s][k]);
+        }
+        q = warp_sum(q);
+        if (lane == 0) s_part[k] = make_float2(all, q);
     }
     if (split > 1) cluster.sync();
     else __syncthreads();
+    if (threadIdx.x < CT) {
+        float sum = 0.0f, q = 0.0f;
+        float2 parts[kColSplit];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float s = 0.0f;
-        if (split > 1) {
-            for (int q = 0; q < split; ++q) s += cluster.map_shared_rank(&sum[i][0], q)[lane];
+        for (int r = 0; r < kColSplit; ++r)
+            if (r < split) {
+                parts[r] = *cluster.map_shared_rank(&s_part[threadIdx.x], r);
+                sum = fmaf(parts[r].x, float(start(r + 1) - start(r)), sum);
+            }
+        const float all = sum / float(n);
+#pragma unroll
+        for (int r = 0; r < kColSplit; ++r)
+            if (r < split) {
+                const float d = parts[r].x - all;
+                q += fmaf(d * d, float(start(r + 1) - start(r)), parts[r].y);
+            }
+        const float rstd = inverse_root(q / float(n) + a.eps);
+        s_stat[threadIdx.x] = make_float2(all, rstd);
+        if (rank == 0 && in) {   // slot 0
+            if (a.mean) a.mean[step * a.tokens + c] = all;
+            if (a.rstd) a.rstd[step * a.tokens + c] = rstd;
+        }
+    }
+    __syncthreads();
+    const float2 stat = s_stat[col];
+    for (int b = 0; b < batches; ++b) {
+        if (batches > 1) share.load(x, a.ld_x, b, in, v);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t f = share.feature(b, u);
+            if (in && f < f1) y[f * a.ld_out] = narrow<T>(fmaf((v[u] - stat.x) * stat.y, gamma_at(a, f), beta_at(a, f)));
+        }
+    }
+    if (split > 1) cluster.sync();   // its sums may still be read
+}
+
+// Sums over the CT lanes of a tile of N values a lane, N a power of two: in each
+// step a lane hands half of its values to the lane across and adds what it gets
+// to the other half, so that N values cost about N shuffles.  Afterwards v[0 ..
+// left) are the sums of values first, first + 1, ...
+template <int CT, int N>
+__device__ __forceinline__ void reduce_scatter(float (&v)[N], int &first, int &left) {
+    first = 0;
+    int m = N;
+#pragma unroll
+    for (int o = CT / 2; o > 0; o >>= 1) {
+        const bool upper = (threadIdx.x & o) != 0;
+        if (m > 1) {
+            m /= 2;
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i)
+                if (i < m) {
+                    const float mine = upper ? v[i + m] : v[i], other = upper ? v[i] : v[i + m];
+                    v[i] = mine + __shfl_xor_sync(0xFFFFFFFFu, other, o);
+                }
+            first += upper ? m : 0;
         } else {
-            s = sum[i][lane];
+            v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], o);
         }
-        v[i] = s;
     }
-    if (split > 1) cluster.sync();   // the sums may be written again, or the CTA leave
+    left = m;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kColThreads) norm_columns_kernel(const NormArgs a, int32_t tiles) {
-    __shared__ float part[1][32][33], sum[1][32];
-    pdl_wait_previous();
-    pdl_launch_dependents();
-    cg::cluster_group cluster = cg::this_cluster();
-    const int split = int(cluster.num_blocks()), rank = int(cluster.block_rank());
-    const int lane = threadIdx.x & 31, slot = threadIdx.x >> 5;
-    const int64_t tile = blockIdx.x / split, step = tile / tiles, c = (tile % tiles) * 32 + lane;
-    const bool in = c < a.tokens;
-    const int32_t n = a.features, f0 = int32_t(int64_t(n) * rank / split), f1 = int32_t(int64_t(n) * (rank + 1) / split);
-    const T *x = static_cast<const T *>(a.x) + step * n * a.ld_x + c;
-    T *y = static_cast<T *>(a.out) + step * n * a.ld_out + c;
-    float s[1] = {0.0f};
-    if (in)
-        for (int32_t f = f0 + slot; f < f1; f += kColWarps) s[0] += widen(x[f * a.ld_x]);
-    column_sum(s, part, sum, cluster);
-    const float mean = s[0] / float(n);
-    s[0] = 0.0f;
-    if (in)
-        for (int32_t f = f0 + slot; f < f1; f += kColWarps) {
-            const float d = widen(x[f * a.ld_x]) - mean;
-            s[0] = fmaf(d, d, s[0]);
-        }
-    column_sum(s, part, sum, cluster);
-    const float rstd = inverse_root(s[0] / float(n) + a.eps);
-    if (!in) return;
-    if (rank == 0 && slot == 0) {
-        if (a.mean) a.mean[step * a.tokens + c] = mean;
-        if (a.rstd) a.rstd[step * a.tokens + c] = rstd;
-    }
-    for (int32_t f = f0 + slot; f < f1; f += kColWarps)
-        y[f * a.ld_out] = narrow<T>(fmaf((widen(x[f * a.ld_x]) - mean) * rstd, gamma_at(a, f), beta_at(a, f)));
-}
-
-template <typename T>
+template <typename T, int CT>
 __global__ void __launch_bounds__(kColThreads) back_columns_kernel(const NormArgs a, int32_t tiles) {
-    __shared__ float part[2][32][33], sum[2][32];
+    using Share = ColShare<T, CT>;
+    constexpr int SLOTS = Share::SLOTS, U = Share::U;
+    __shared__ float p_g[SLOTS][CT + 1], p_gx[SLOTS][CT + 1];
+    __shared__ float2 s_part[CT], s_sum[CT];   // sums of (g, g xh): of this CTA, and of the token over F
     pdl_wait_previous();
     pdl_launch_dependents();
     cg::cluster_group cluster = cg::this_cluster();
     const int split = int(cluster.num_blocks()), rank = int(cluster.block_rank());
-    const int lane = threadIdx.x & 31, slot = threadIdx.x >> 5;
-    const int64_t tile = blockIdx.x / split, step = tile / tiles, c = (tile % tiles) * 32 + lane;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = threadIdx.x % CT, slot = threadIdx.x / CT;
+    const int64_t tile = blockIdx.x / split, step = tile / tiles, c = (tile % tiles) * CT + col;
     const bool in = c < a.tokens;
     const int32_t n = a.features, f0 = int32_t(int64_t(n) * rank / split), f1 = int32_t(int64_t(n) * (rank + 1) / split);
+    const Share share = {f0 + slot, f1};
     const T *x = static_cast<const T *>(a.x) + step * n * a.ld_x + c, *dy = static_cast<const T *>(a.dy) + step * n * a.ld_dy + c;
     T *dx = static_cast<T *>(a.out) + step * n * a.ld_out + c;
     const float mean = in ? a.mean[step * a.tokens + c] : 0.0f, rstd = in ? a.rstd[step * a.tokens + c] : 0.0f;
-    float s[2] = {0.0f, 0.0f};
-    for (int32_t f = f0 + slot; f < f1; f += kColWarps) {
-        const float d = in ? widen(dy[f * a.ld_dy]) : 0.0f, xh = in ? (widen(x[f * a.ld_x]) - mean) * rstd : 0.0f;
-        if (a.partial != nullptr) {
-            // the feature's sums over this tile's tokens, one partial result a tile
-            const float sg = warp_sum(d * xh), sb = warp_sum(d);
-            if (lane == 0) {
-                float *p = a.partial + tile * 2 * partial_width(n);
-                p[f] = sg;
-                p[partial_width(n) + f] = sb;
-            }
+    // (as many batches in every thread: the sums over the lanes need all of them)
+    const int batches = (f1 - f0 + SLOTS * U - 1) / (SLOTS * U);
+    float xv[U], dv[U], sg = 0.0f, sgx = 0.0f;
+    for (int b = 0; b < batches; ++b) {
+        share.load(x, a.ld_x, b, in, xv);
+        share.load(dy, a.ld_dy, b, in, dv);   // 0 outside: adds nothing
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t f = share.feature(b, u);
+            xv[u] = in && f < f1 ? (xv[u] - mean) * rstd : 0.0f;
+            const float g = dv[u] * (f < f1 ? gamma_at(a, f) : 0.0f);
+            sg += g;
+            sgx = fmaf(g, xv[u], sgx);
         }
-        const float g = d * gamma_at(a, f);
-        s[0] += g;
-        s[1] = fmaf(g, xh, s[1]);
+        if (a.partial != nullptr) {
+            // the features' sums over this tile's tokens, one partial result a tile
+            float w[2 * U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) w[u] = dv[u] * xv[u], w[U + u] = dv[u];
+            int first, left;
+            reduce_scatter<CT>(w, first, left);
+            float *p = a.partial + tile * 2 * partial_width(n);
+#pragma unroll
+            for (int i = 0; i < 2 * U / (CT < 2 * U ? CT : 2 * U); ++i)
+                if (i < left) {
+                    const int k = first + i;
+                    const int32_t f = share.feature(b, k % U);
+                    if (f < f1) p[(k < U ? 0 : partial_width(n)) + f] = w[i];
+                }
+        }
     }
-    column_sum(s, part, sum, cluster);
-    if (!in) return;
-    const float c0 = s[0] / float(n), c1 = s[1] / float(n);
-    for (int32_t f = f0 + slot; f < f1; f += kColWarps) {
-        const float xh = (widen(x[f * a.ld_x]) - mean) * rstd;
-        dx[f * a.ld_out] = narrow<T>(rstd * (widen(dy[f * a.ld_dy]) * gamma_at(a, f) - c0 - xh * c1));
+    p_g[slot][col] = sg;
+    p_gx[slot][col] = sgx;
+    __syncthreads();
+    for (int k = warp; k < CT; k += kColWarps) {
+        float s0 = 0.0f, s1 = 0.0f;
+        for (int s = lane; s < SLOTS; s += 32) s0 += p_g[s][k], s1 += p_gx[s][k];
+        s0 = warp_sum(s0), s1 = warp_sum(s1);
+        if (lane == 0) s_part[k] = make_float2(s0, s1);
     }
+    if (split > 1) cluster.sync();
+    else __syncthreads();
+    if (threadIdx.x < CT) {
+        float s0 = 0.0f, s1 = 0.0f;
+        float2 parts[kColSplit];
+#pragma unroll
+        for (int r = 0; r < kColSplit; ++r)
+            if (r < split) parts[r] = *cluster.map_shared_rank(&s_part[threadIdx.x], r);
+#pragma unroll
+        for (int r = 0; r < kColSplit; ++r)
+            if (r < split) s0 += parts[r].x, s1 += parts[r].y;
+        s_sum[threadIdx.x] = make_float2(s0 / float(n), s1 / float(n));
+    }
+    __syncthreads();
+    const float2 sum = s_sum[col];
+    for (int b = 0; b < batches; ++b) {
+        if (batches > 1) {
+            share.load(x, a.ld_x, b, in, xv);
+            share.load(dy, a.ld_dy, b, in, dv);
+#pragma unroll
+            for (int u = 0; u < U; ++u) xv[u] = (xv[u] - mean) * rstd;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t f = share.feature(b, u);
+            if (in && f < f1) dx[f * a.ld_out] = narrow<T>(rstd * (dv[u] * gamma_at(a, f) - sum.x - xv[u] * sum.y));
+        }
+    }
+    if (split > 1) cluster.sync();   // its sums may still be read
 }
 
 __global__ void zero_kernel(float *a, float *b, int32_t n) {
@@ -636,16 +762,38 @@ bool alike(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows,
            (rows == 1 || (lda - ldb) * int64_t(es) % 16 == 0);
 }
 
+// Tokens of a tile of token columns: 32, or fewer where there are fewer, and
+// where wider tiles would leave SMs idle, down to the 32 bytes that memory
+// moves at a time.
+int col_tile(int64_t steps, int64_t tokens, size_t es) {
+    int ct = 32;
+    while (ct > 4 && (tokens <= ct / 2 || (ct * int(es) > 32 && steps * ((tokens + ct / 2 - 1) / (ct / 2)) * kColSplit <= sm_count())))
+        ct /= 2;
+    return ct;
+}
+
+// Calls f with the tile width as a constant, the tiles of a step and the CTAs
+// that share a tile.
+template <typename T, typename F>
+cudaError_t with_col_tile(const NormArgs &a, F f) {
+    const int ct = col_tile(a.steps, a.tokens, sizeof(T));
+    const int64_t tiles = (a.tokens + ct - 1) / ct, all = tiles * a.steps;
+    int split = 1;
+    while (split < kColSplit && all * split < 2 * sm_count() && a.features / (2 * split) >= 2 * kColThreads / ct) split *= 2;
+    if (all * split > INT32_MAX) return cudaErrorNotSupported;
+    const dim3 grid(unsigned(all * split));
+    if (ct == 32) return f(std::integral_constant<int, 32>(), grid, unsigned(split), int32_t(tiles));
+    if (ct == 16) return f(std::integral_constant<int, 16>(), grid, unsigned(split), int32_t(tiles));
+    if (ct == 8) return f(std::integral_constant<int, 8>(), grid, unsigned(split), int32_t(tiles));
+    return f(std::integral_constant<int, 4>(), grid, unsigned(split), int32_t(tiles));
+}
+
 template <typename T>
 cudaError_t launch_norm(const NormArgs &a, darb_layout_t layout, cudaStream_t stream) {
-    if (layout == DARB_TOKEN_COLUMNS) {
-        const int64_t tiles = (a.tokens + 31) / 32, all = tiles * a.steps;
-        int split = 1;
-        while (split < kColSplit && all * split < sm_count() && a.features / (2 * split) >= 64) split *= 2;
-        if (all * split > INT32_MAX) return cudaErrorNotSupported;
-        return launch_ex(norm_columns_kernel<T>, dim3(unsigned(all * split)), dim3(kColThreads), 0, stream,
-                         unsigned(split), true, a, int32_t(tiles));
-    }
+    if (layout == DARB_TOKEN_COLUMNS)
+        return with_col_tile<T>(a, [&](auto ct, dim3 grid, unsigned split, int32_t tiles) {
+            return launch_ex(norm_columns_kernel<T, ct.value>, grid, dim3(kColThreads), 0, stream, split, true, a, tiles);
+        });
     if (alike(a.x, a.ld_x, a.out, a.ld_out, a.tokens, sizeof(T))) {
         constexpr int STAGES = 4;
         const int64_t granules = most_granules<T>(a.x, a.ld_x, a.tokens, a.features);
@@ -665,7 +813,12 @@ cudaError_t launch_norm(const NormArgs &a, darb_layout_t layout, cudaStream_t st
 
 // Partial results of the sums over the tokens, at most (of any kernel).
 int64_t most_partials(darb_layout_t layout, int64_t steps, int64_t tokens) {
-    if (layout == DARB_TOKEN_COLUMNS) return steps * ((tokens + 31) / 32);
+    if (layout == DARB_TOKEN_COLUMNS && tokens == 1)   // may be taken as rows
+        return std::max(steps, most_partials(DARB_TOKEN_ROWS, 1, steps));
+    if (layout == DARB_TOKEN_COLUMNS) {
+        const int64_t ct = std::min(col_tile(steps, tokens, 2), col_tile(steps, tokens, 4));
+        return steps * ((tokens + ct - 1) / ct);
+    }
     return std::min<int64_t>((tokens + 63) / 64 * 64, int64_t(sm_count()) * 32);
 }
 
@@ -675,13 +828,10 @@ cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, 
     int64_t partials = 0;
     uint32_t base = 0, step = 0;   // of the partial results' rows, in bytes
     if (layout == DARB_TOKEN_COLUMNS) {
-        const int64_t tiles = (a.tokens + 31) / 32, all = tiles * a.steps;
-        int split = 1;
-        while (split < kColSplit && all * split < sm_count() && a.features / (2 * split) >= 64) split *= 2;
-        if (all * split > INT32_MAX) return cudaErrorNotSupported;
-        partials = all;
-        e = launch_ex(back_columns_kernel<T>, dim3(unsigned(all * split)), dim3(kColThreads), 0, stream,
-                      unsigned(split), true, a, int32_t(tiles));
+        e = with_col_tile<T>(a, [&](auto ct, dim3 grid, unsigned split, int32_t tiles) {
+            partials = a.steps * tiles;
+            return launch_ex(back_columns_kernel<T, ct.value>, grid, dim3(kColThreads), 0, stream, split, true, a, tiles);
+        });
     } else {
         const bool same = alike(a.x, a.ld_x, a.out, a.ld_out, a.tokens, sizeof(T)) &&
                           alike(a.x, a.ld_x, a.dy, a.ld_dy, a.tokens, sizeof(T));
@@ -732,6 +882,16 @@ darb_status_t check_norm(darb_dtype_t dtype, darb_layout_t layout, int64_t steps
     if (tokens > kMaxTokens || steps > kMaxTokens || features > kMaxNormFeatures) return DARB_ERR_UNSUPPORTED;
     return DARB_OK;
 }
+// One token a step, its features one after the other: a row a step.
+bool is_rows(darb_layout_t layout, int64_t tokens, int64_t ld0, int64_t ld1, int64_t ld2) {
+    return layout == DARB_TOKEN_COLUMNS && tokens == 1 && ld0 == 1 && ld1 == 1 && ld2 == 1;
+}
+void as_rows(NormArgs &a, darb_layout_t &layout) {
+    layout = DARB_TOKEN_ROWS;
+    a.tokens = a.steps;
+    a.steps = 1;
+    a.ld_x = a.ld_dy = a.ld_out = a.features;
+}
 bool good_ld(darb_layout_t layout, int64_t tokens, int64_t features, int64_t ld) {
     return ld >= (layout == DARB_TOKEN_ROWS ? features : tokens);
 }
@@ -766,6 +926,7 @@ darb_status_t darb_layer_norm(const void *x, darb_dtype_t dtype, darb_layout_t l
     NormArgs a = {};
     a.x = x, a.out = y, a.ld_x = ld_x, a.ld_out = ld_y, a.steps = steps, a.tokens = tokens, a.features = int32_t(features);
     a.gamma = gamma, a.beta = beta, a.eps = eps, a.mean = mean, a.rstd = rstd;
+    if (is_rows(layout, tokens, ld_x, ld_y, 1)) as_rows(a, layout);
     return status_of(dtype == DARB_BF16 ? launch_norm<__nv_bfloat16>(a, layout, stream) : launch_norm<float>(a, layout, stream));
 }
 
@@ -815,6 +976,7 @@ darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x,
     a.steps = steps, a.tokens = tokens, a.features = int32_t(features), a.gamma = gamma;
     a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
     a.partial = dgamma ? static_cast<float *>(work) : nullptr;
+    if (is_rows(layout, tokens, ld_x, ld_dy, ld_dx)) as_rows(a, layout);
     return status_of(dtype == DARB_BF16 ? launch_back<__nv_bfloat16>(a, layout, dgamma, dbeta, stream)
                                         : launch_back<float>(a, layout, dgamma, dbeta, stream));
 }

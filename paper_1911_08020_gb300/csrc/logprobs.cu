@@ -926,6 +926,7 @@ darb_status_t darb_token_logprobs(const void *logits, darb_dtype_t dtype, darb_l
                           {k ? top_index : nullptr, tokens * k * 4}};
     const Range ins[] = {{logits, span * int64_t(dtype_size(dtype))}, {targets, tokens * 8}};
     if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
+    if (layout == DARB_TOKEN_COLUMNS && tokens == 1 && ld == 1) layout = DARB_TOKEN_ROWS;   // (a single row: ld is not used)
     const ScoreArgs a = {logits, ld, tokens, int32_t(vocab), k, targets, logprob, entropy, lse, top_logprob, top_index};
     if (layout == DARB_TOKEN_ROWS)
         return status_of(dtype == DARB_BF16 ? launch_score_rows<__nv_bfloat16>(a, stream) : launch_score_rows<float>(a, stream));
@@ -956,6 +957,7 @@ darb_status_t darb_token_logprobs_grad(const void *logits, darb_dtype_t dtype, d
     const Range ins[] = {{in_place ? nullptr : logits, span * int64_t(es)}, {targets, tokens * 8}, {lse, tokens * 4},
                          {entropy, tokens * 4}, {d_logprob, tokens * 4}, {d_entropy, tokens * 4}};
     if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
+    if (layout == DARB_TOKEN_COLUMNS && tokens == 1 && ld == 1 && ld_grad == 1) layout = DARB_TOKEN_ROWS;
     const GradArgs a = {logits, d_logits, ld, ld_grad, tokens, int32_t(vocab), targets, lse, entropy, d_logprob, d_entropy};
     return status_of(dtype == DARB_BF16 ? launch_grad<__nv_bfloat16>(a, layout, stream) : launch_grad<float>(a, layout, stream));
 }
