@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(kAnyThreads) row_sums_kernel(const NormArgs a)
 
 constexpr int kColThreads = 512;
 constexpr int kColWarps = kColThreads / 32;
-constexpr int kColBatch = 16;
+constexpr int kColBatch = 8;
 constexpr int kColSplit = 8;   // CTAs that share a tile, at most
 
 // The rows of a thread: features f0 + slot + i * SLOTS, in batches.
@@ -492,11 +492,35 @@ struct ColShare {
     int32_t first, end;   // features of the thread: first, first + SLOTS, ... below end
     __device__ __forceinline__ int count() const { return first < end ? (end - first + SLOTS - 1) / SLOTS : 0; }
     __device__ __forceinline__ int32_t feature(int batch, int u) const { return first + (batch * U + u) * SLOTS; }
-    __device__ __forceinline__ void load(const T *x, int64_t ld, int batch, bool in, float (&v)[U]) const {
+    __device__ __forceinline__ bool full(int batch) const { return feature(batch, U - 1) < end; }
+    // A batch's values of x (row f at x + f * ld; 0 past the end).
+    __device__ __forceinline__ void load(const T *x, int64_t ld, int batch, float (&v)[U]) const {
+        const T *p = x + int64_t(feature(batch, 0)) * ld;
+        const int64_t stride = SLOTS * ld;
+        if (full(batch)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t f = feature(batch, u);
-            v[u] = in && f < end ? widen(x[f * ld]) : 0.0f;
+            for (int u = 0; u < U; ++u, p += stride) v[u] = widen(*p);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u, p += stride) v[u] = feature(batch, u) < end ? widen(*p) : 0.0f;
+        }
+    }
+    // The same of a vector over the features; null: `none`.
+    __device__ __forceinline__ void load(const float *g, float none, int batch, float (&v)[U]) const {
+        const float *p = g + feature(batch, 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = g == nullptr ? none : feature(batch, u) < end ? __ldg(p + u * SLOTS) : 0.0f;
+    }
+    __device__ __forceinline__ void store(T *y, int64_t ld, int batch, const float (&v)[U]) const {
+        T *p = y + int64_t(feature(batch, 0)) * ld;
+        const int64_t stride = SLOTS * ld;
+        if (full(batch)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u, p += stride) *p = narrow<T>(v[u]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u, p += stride)
+                if (feature(batch, u) < end) *p = narrow<T>(v[u]);
         }
     }
 };
@@ -518,13 +542,14 @@ __global__ void __launch_bounds__(kColThreads) norm_columns_kernel(const NormArg
     const auto start = [&](int q) { return int32_t(int64_t(n) * q / split); };
     const int32_t f0 = start(rank), f1 = start(rank + 1);
     const Share share = {f0 + slot, f1};
-    const T *x = static_cast<const T *>(a.x) + step * n * a.ld_x + c;
+    // (past the last token: the last one's values, for nobody)
+    const T *x = static_cast<const T *>(a.x) + step * n * a.ld_x + (in ? c : a.tokens - 1);
     T *y = static_cast<T *>(a.out) + step * n * a.ld_out + c;
     const int rows = share.count(), batches = (rows + U - 1) / U;
     // mean and centred squares of the thread's rows, a batch at a time joined to those before
     float v[U], mean = 0.0f, m2 = 0.0f;
     for (int b = 0; b < batches; ++b) {
-        share.load(x, a.ld_x, b, in, v);
+        share.load(x, a.ld_x, b, v);
         const int have = min(U, rows - b * U);
         float s = 0.0f, q = 0.0f;
 #pragma unroll
@@ -584,24 +609,25 @@ __global__ void __launch_bounds__(kColThreads) norm_columns_kernel(const NormArg
     __syncthreads();
     const float2 stat = s_stat[col];
     for (int b = 0; b < batches; ++b) {
-        if (batches > 1) share.load(x, a.ld_x, b, in, v);
+        float gm[U], bt[U];
+        if (batches > 1) share.load(x, a.ld_x, b, v);
+        share.load(a.gamma, 1.0f, b, gm);
+        share.load(a.beta, 0.0f, b, bt);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t f = share.feature(b, u);
-            if (in && f < f1) y[f * a.ld_out] = narrow<T>(fmaf((v[u] - stat.x) * stat.y, gamma_at(a, f), beta_at(a, f)));
-        }
+        for (int u = 0; u < U; ++u) v[u] = fmaf((v[u] - stat.x) * stat.y, gm[u], bt[u]);
+        if (in) share.store(y, a.ld_out, b, v);
     }
     if (split > 1) cluster.sync();   // its sums may still be read
 }
 
 // Sums over the CT lanes of a tile of N values a lane, N a power of two: in each
 // step a lane hands half of its values to the lane across and adds what it gets
-// to the other half, so that N values cost about N shuffles.  Afterwards v[0 ..
-// left) are the sums of values first, first + 1, ...
+// to the other half, so that N values cost about N shuffles.  Afterwards v[0],
+// v[1], ... (N / CT of them, one at least) are the sums of values first, first +
+// 1, ...; returns first.
 template <int CT, int N>
-__device__ __forceinline__ void reduce_scatter(float (&v)[N], int &first, int &left) {
-    first = 0;
-    int m = N;
+__device__ __forceinline__ int reduce_scatter(float (&v)[N]) {
+    int first = 0, m = N;
 #pragma unroll
     for (int o = CT / 2; o > 0; o >>= 1) {
         const bool upper = (threadIdx.x & o) != 0;
@@ -618,7 +644,7 @@ __device__ __forceinline__ void reduce_scatter(float (&v)[N], int &first, int &l
             v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], o);
         }
     }
-    left = m;
+    return first;
 }
 
 template <typename T, int CT>
@@ -636,20 +662,23 @@ __global__ void __launch_bounds__(kColThreads) back_columns_kernel(const NormArg
     const bool in = c < a.tokens;
     const int32_t n = a.features, f0 = int32_t(int64_t(n) * rank / split), f1 = int32_t(int64_t(n) * (rank + 1) / split);
     const Share share = {f0 + slot, f1};
-    const T *x = static_cast<const T *>(a.x) + step * n * a.ld_x + c, *dy = static_cast<const T *>(a.dy) + step * n * a.ld_dy + c;
+    // (past the last token: the last one's values, whose dy counts as 0)
+    const int64_t cc = in ? c : a.tokens - 1;
+    const T *x = static_cast<const T *>(a.x) + step * n * a.ld_x + cc, *dy = static_cast<const T *>(a.dy) + step * n * a.ld_dy + cc;
     T *dx = static_cast<T *>(a.out) + step * n * a.ld_out + c;
-    const float mean = in ? a.mean[step * a.tokens + c] : 0.0f, rstd = in ? a.rstd[step * a.tokens + c] : 0.0f;
+    const float mean = a.mean[step * a.tokens + cc], rstd = a.rstd[step * a.tokens + cc];
     // (as many batches in every thread: the sums over the lanes need all of them)
     const int batches = (f1 - f0 + SLOTS * U - 1) / (SLOTS * U);
-    float xv[U], dv[U], sg = 0.0f, sgx = 0.0f;
+    float xv[U], dv[U], gm[U], sg = 0.0f, sgx = 0.0f;
     for (int b = 0; b < batches; ++b) {
-        share.load(x, a.ld_x, b, in, xv);
-        share.load(dy, a.ld_dy, b, in, dv);   // 0 outside: adds nothing
+        share.load(x, a.ld_x, b, xv);
+        share.load(dy, a.ld_dy, b, dv);   // 0 past the end: adds nothing
+        share.load(a.gamma, 1.0f, b, gm);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int32_t f = share.feature(b, u);
-            xv[u] = in && f < f1 ? (xv[u] - mean) * rstd : 0.0f;
-            const float g = dv[u] * (f < f1 ? gamma_at(a, f) : 0.0f);
+            xv[u] = (xv[u] - mean) * rstd;
+            if (!in) dv[u] = 0.0f;
+            const float g = dv[u] * gm[u];
             sg += g;
             sgx = fmaf(g, xv[u], sgx);
         }
@@ -658,16 +687,14 @@ __global__ void __launch_bounds__(kColThreads) back_columns_kernel(const NormArg
             float w[2 * U];
 #pragma unroll
             for (int u = 0; u < U; ++u) w[u] = dv[u] * xv[u], w[U + u] = dv[u];
-            int first, left;
-            reduce_scatter<CT>(w, first, left);
+            const int first = reduce_scatter<CT>(w);
             float *p = a.partial + tile * 2 * partial_width(n);
 #pragma unroll
-            for (int i = 0; i < 2 * U / (CT < 2 * U ? CT : 2 * U); ++i)
-                if (i < left) {
-                    const int k = first + i;
-                    const int32_t f = share.feature(b, k % U);
-                    if (f < f1) p[(k < U ? 0 : partial_width(n)) + f] = w[i];
-                }
+            for (int i = 0; i < 2 * U / (CT < 2 * U ? CT : 2 * U); ++i) {
+                const int k = first + i;
+                const int32_t f = share.feature(b, k % U);
+                if (f < f1) p[(k < U ? 0 : partial_width(n)) + f] = w[i];
+            }
         }
     }
     p_g[slot][col] = sg;
@@ -696,16 +723,15 @@ __global__ void __launch_bounds__(kColThreads) back_columns_kernel(const NormArg
     const float2 sum = s_sum[col];
     for (int b = 0; b < batches; ++b) {
         if (batches > 1) {
-            share.load(x, a.ld_x, b, in, xv);
-            share.load(dy, a.ld_dy, b, in, dv);
+            share.load(x, a.ld_x, b, xv);
+            share.load(dy, a.ld_dy, b, dv);
+            share.load(a.gamma, 1.0f, b, gm);
 #pragma unroll
             for (int u = 0; u < U; ++u) xv[u] = (xv[u] - mean) * rstd;
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t f = share.feature(b, u);
-            if (in && f < f1) dx[f * a.ld_out] = narrow<T>(rstd * (dv[u] * gamma_at(a, f) - sum.x - xv[u] * sum.y));
-        }
+        for (int u = 0; u < U; ++u) dv[u] = rstd * (dv[u] * gm[u] - sum.x - xv[u] * sum.y);
+        if (in) share.store(dx, a.ld_out, b, dv);
     }
     if (split > 1) cluster.sync();   // its sums may still be read
 }
