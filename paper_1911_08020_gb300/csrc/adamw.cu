@@ -71,63 +71,81 @@ struct StepArgs {
     const void *grads[kGradPointers];
 };
 
-__device__ __forceinline__ void update(float &p, float g, float &m, float &v, float &root, const StepArgs &a) {
-    m = __fadd_rn(__fmul_rn(m, a.b1), __fmul_rn(g, a.c1));
-    v = __fadd_rn(__fmul_rn(v, a.b2), __fmul_rn(__fmul_rn(g, g), a.c2));
-    root = __fsqrt_rn(v);
-    const float denom = __fadd_rn(__fmul_rn(root, a.root_scale), a.eps);
-    p = __fsub_rn(__fmul_rn(p, a.decay), __fdiv_rn(__fmul_rn(m, a.step_size), denom));
+// What a step multiplies by, twice each for pairs.
+struct Factors {
+    Pair b1, c1, b2, c2, decay, step, root_scale, eps, grad_scale;
+    __device__ explicit Factors(const StepArgs &a, float scale)
+        : b1(both(a.b1)), c1(both(a.c1)), b2(both(a.b2)), c2(both(a.c2)), decay(both(a.decay)), step(both(-a.step_size)),
+          root_scale(both(a.root_scale)), eps(both(a.eps)), grad_scale(both(scale)) {}
+};
+
+// A pair's sum in two scalar additions: the assembler contracts a paired product
+// and a paired sum into one rounding, whatever is asked of it.
+__device__ __forceinline__ Pair plus(Pair a, Pair b) { return pair(__fadd_rn(low(a), low(b)), __fadd_rn(high(a), high(b))); }
+
+__device__ __forceinline__ void update(Pair &p, Pair g, Pair &m, Pair &v, Pair &root, const Factors &k) {
+    g = mul2(g, k.grad_scale);
+    m = plus(mul2(m, k.b1), mul2(g, k.c1));
+    v = plus(mul2(v, k.b2), mul2(mul2(g, g), k.c2));
+    root = pair(__fsqrt_rn(low(v)), __fsqrt_rn(high(v)));
+    const Pair denom = plus(mul2(root, k.root_scale), k.eps), num = mul2(m, k.step);   // (the step is negative here)
+    p = plus(mul2(p, k.decay), pair(__fdiv_rn(low(num), low(denom)), __fdiv_rn(high(num), high(denom))));
 }
 
 // Elements i .. i + 8 of a tensor as fp32 (VEC: i is a multiple of 8 and the
 // tensor 16-byte aligned; else zeros from n on).
 template <bool VEC, typename T>
-__device__ __forceinline__ void load8(const T *t, int64_t i, int64_t n, float (&v)[8]) {
+__device__ __forceinline__ void load8(const T *t, int64_t i, int64_t n, Pair (&v)[4]) {
     if (VEC) {
         if constexpr (sizeof(T) == 4) {
-            const uint4 lo = *reinterpret_cast<const uint4 *>(t + i), hi = *reinterpret_cast<const uint4 *>(t + i + 4);
-            v[0] = __uint_as_float(lo.x), v[1] = __uint_as_float(lo.y), v[2] = __uint_as_float(lo.z), v[3] = __uint_as_float(lo.w);
-            v[4] = __uint_as_float(hi.x), v[5] = __uint_as_float(hi.y), v[6] = __uint_as_float(hi.z), v[7] = __uint_as_float(hi.w);
+            Pair lo[2], hi[2];
+            unpack(*reinterpret_cast<const uint4 *>(t + i), lo);
+            unpack(*reinterpret_cast<const uint4 *>(t + i + 4), hi);
+            v[0] = lo[0], v[1] = lo[1], v[2] = hi[0], v[3] = hi[1];
         } else {
             unpack(*reinterpret_cast<const uint4 *>(t + i), v);
         }
     } else {
+        float w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = i + e < n ? widen(t[i + e]) : 0.0f;
+        for (int e = 0; e < 8; ++e) w[e] = i + e < n ? widen(t[i + e]) : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = pair(w[2 * e], w[2 * e + 1]);
     }
 }
 template <bool VEC, typename T>
-__device__ __forceinline__ void store8(T *t, int64_t i, int64_t n, const float (&v)[8]) {
+__device__ __forceinline__ void store8(T *t, int64_t i, int64_t n, const Pair (&v)[4]) {
     if (VEC) {
         if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4 *>(t + i) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4 *>(t + i + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            const Pair lo[2] = {v[0], v[1]}, hi[2] = {v[2], v[3]};
+            *reinterpret_cast<uint4 *>(t + i) = pack(lo);
+            *reinterpret_cast<uint4 *>(t + i + 4) = pack(hi);
         } else {
             *reinterpret_cast<uint4 *>(t + i) = pack(v);
         }
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (i + e < n) t[i + e] = narrow<T>(v[e]);
+            if (i + e < n) t[i + e] = narrow<T>(e & 1 ? high(v[e / 2]) : low(v[e / 2]));
     }
 }
 
 // e4m3 codes to fp32 (exact), two at a time.
-__device__ __forceinline__ float2 decode2(uint16_t codes) {
+__device__ __forceinline__ Pair decode2(uint16_t codes) {
     uint32_t h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(codes));
-    float2 f;
-    asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %2;\n cvt.f32.f16 %0, lo;\n cvt.f32.f16 %1, hi;\n}"
-        : "=f"(f.x), "=f"(f.y) : "r"(h));
-    return f;
+    float lo, hi;
+    asm("{\n .reg .b16 x, y;\n mov.b32 {x, y}, %2;\n cvt.f32.f16 %0, x;\n cvt.f32.f16 %1, y;\n}" : "=f"(lo), "=f"(hi) : "r"(h));
+    return pair(lo, hi);
 }
-__device__ __forceinline__ uint16_t encode2(float lo, float hi) {   // values that codes have
+// The code of a value that codes have, or of NaN.
+__device__ __forceinline__ uint32_t encode(float v) {
     uint16_t c;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(hi), "f"(lo));
-    return c;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(0.0f), "f"(v));
+    return c & 0xFFu;
 }
 template <bool VEC>
-__device__ __forceinline__ void load_codes(const uint8_t *t, int64_t i, int64_t n, float scale, float (&v)[8]) {
+__device__ __forceinline__ void load_codes(const uint8_t *t, int64_t i, int64_t n, float scale, Pair (&v)[4]) {
     uint32_t w[2] = {0, 0};
     if (VEC) {
         const uint2 q = *reinterpret_cast<const uint2 *>(t + i);
@@ -138,62 +156,64 @@ __device__ __forceinline__ void load_codes(const uint8_t *t, int64_t i, int64_t 
             if (i + e < n) w[e >> 2] |= uint32_t(t[i + e]) << (8 * (e & 3));
     }
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-        const float2 f = decode2(uint16_t(w[e >> 2] >> (8 * (e & 3))));
-        v[e] = __fmul_rn(f.x, scale);
-        v[e + 1] = __fmul_rn(f.y, scale);
-    }
+    for (int e = 0; e < 4; ++e) v[e] = mul2(decode2(uint16_t(w[e >> 1] >> (16 * (e & 1)))), both(scale));
 }
 template <bool VEC>
-__device__ __forceinline__ void store_codes(uint8_t *t, int64_t i, int64_t n, const float (&c)[8]) {
-    uint32_t w[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-        w[h] = uint32_t(encode2(c[4 * h], c[4 * h + 1])) | uint32_t(encode2(c[4 * h + 2], c[4 * h + 3])) << 16;
+__device__ __forceinline__ void store_codes(uint8_t *t, int64_t i, int64_t n, const uint32_t (&c)[8]) {
+    const uint32_t lo = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, hi = c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24;
     if (VEC) {
-        *reinterpret_cast<uint2 *>(t + i) = make_uint2(w[0], w[1]);
+        *reinterpret_cast<uint2 *>(t + i) = make_uint2(lo, hi);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (i + e < n) t[i + e] = uint8_t(w[e >> 2] >> (8 * (e & 3)));
+            if (i + e < n) t[i + e] = uint8_t(c[e]);
     }
 }
 
-// Two random numbers of 16 bits for element `number` of a step.
-__device__ __forceinline__ uint32_t noise_of(uint32_t number, uint32_t key) {
-    uint32_t z = number * 0x9E3779B1u + key;
+// Two random numbers of 16 bits for element `number` of a step, from
+// number * kNumberFactor + key.
+constexpr uint32_t kNumberFactor = 0x9E3779B1u;
+__device__ __forceinline__ uint32_t noise_of(uint32_t z) {
     z = (z ^ (z >> 15)) * 0x6A09E667u;
     z = (z ^ (z >> 13)) * 0xBB67AE85u;
     return z ^ (z >> 16);
 }
 
-// x (at most 448 in magnitude, but for rounding) to the value of a code next to
-// it, away from zero with the probability of its distance from the other one.
-__device__ __forceinline__ float random_code(float x, uint32_t noise16) {
+// The code of |x| (at most 448, but for rounding; not NaN): the code below or
+// the one above it, above with the probability of its distance from the lower
+// one.  noise: 16 random bits times 16, plus 8.  Adding it to a value's bits
+// carries into the three bits of fraction that a code keeps as often as the
+// bits below them say; below 2^-6 the codes are 2^-9 apart, as they are from
+// 2^-6 to 2^-5, so smaller values are moved there and back.
+__device__ __forceinline__ uint32_t random_code(float x, uint32_t noise) {
     const float a = fabsf(x);
-    // below 2^-6 the codes are 2^-9 apart, as they are from 2^-6 to 2^-5
-    const float shift = a < 0x1p-6f ? 0x1p-6f : 0.0f;
-    const uint32_t bits = (__float_as_uint(__fadd_rn(a, shift)) + (noise16 << 4) + 8u) & 0xFFF00000u;
-    const float c = fminf(__fsub_rn(__uint_as_float(bits), shift), 448.0f);
-    return copysignf(a == a ? c : a, x);
+    const bool small = a < 0x1p-6f;
+    const uint32_t bits = __float_as_uint(__fadd_rn(a, small ? 0x1p-6f : 0.0f)) + noise;
+    // fp32 exponents count from 127 and codes' from 7: 120 << 3; a moved value is 1 << 3 too high
+    return min((bits >> 20) - (small ? 968u : 960u), 126u);
 }
 
-// The scale of a block from the lanes' values, and its inverse (0 where the
-// block's values are below the smallest normal scale: their codes are 0).
-__device__ __forceinline__ float block_scale(const float (&v)[8], float &inverse) {
-    // magnitudes order as their bits, NaN above all
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-    top = __reduce_max_sync(0xFFFFFFFFu, top);
+// The scale of a block whose largest magnitude has the bits `top`, and its
+// inverse (0 where the scale would not be normal: the block's codes are 0).
+__device__ __forceinline__ float block_scale(uint32_t top, float &inverse) {
     const float scale = __fmul_rn(__uint_as_float(top), float(1.0 / 448.0));
     inverse = scale >= FLT_MIN ? __fdiv_rn(1.0f, scale) : 0.0f;
     return scale;
 }
 
+// The largest magnitude's bits over a block (magnitudes order as their bits,
+// NaN above all).
+__device__ __forceinline__ uint32_t block_top(const Pair (&v)[4]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        top = max(top, max(__float_as_uint(low(v[e])) & 0x7FFFFFFFu, __float_as_uint(high(v[e])) & 0x7FFFFFFFu));
+    return __reduce_max_sync(0xFFFFFFFFu, top);
+}
+
 template <typename G, bool CODES, bool VEC>
-__device__ __forceinline__ void step8(const Tensor &t, const G *grad, int64_t i, float grad_scale, const StepArgs &a) {
-    float p[8], g[8], m[8], v[8], root[8];
+__device__ __forceinline__ void step8(const Tensor &t, const G *grad, int64_t i, const Factors &k, uint32_t key) {
+    Pair p[4], g[4], m[4], v[4], root[4];
     const int64_t block = i / kBlock;
     load8<VEC>(t.p, i, t.n, p);
     load8<VEC>(grad, i, t.n, g);
@@ -201,32 +221,52 @@ __device__ __forceinline__ void step8(const Tensor &t, const G *grad, int64_t i,
         load_codes<VEC>(static_cast<const uint8_t *>(t.m), i, t.n, t.m_scale[block], m);
         load_codes<VEC>(static_cast<const uint8_t *>(t.v), i, t.n, t.v_scale[block], v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], v[e]);
+        for (int e = 0; e < 4; ++e) v[e] = mul2(v[e], v[e]);
     } else {
         load8<VEC>(static_cast<const float *>(t.m), i, t.n, m);
         load8<VEC>(static_cast<const float *>(t.v), i, t.n, v);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) update(p[e], __fmul_rn(g[e], grad_scale), m[e], v[e], root[e], a);
+    for (int e = 0; e < 4; ++e) update(p[e], g[e], m[e], v[e], root[e], k);
     store8<VEC>(t.p, i, t.n, p);
     if (t.copy != nullptr) store8<VEC>(t.copy, i, t.n, p);
     if constexpr (CODES) {
         if (!VEC) {   // elements past the end are no part of the block
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (i + e >= t.n) m[e] = root[e] = 0.0f;
+            for (int e = 0; e < 4; ++e) {
+                m[e] = pair(i + 2 * e < t.n ? low(m[e]) : 0.0f, i + 2 * e + 1 < t.n ? high(m[e]) : 0.0f);
+                root[e] = pair(i + 2 * e < t.n ? low(root[e]) : 0.0f, i + 2 * e + 1 < t.n ? high(root[e]) : 0.0f);
+            }
         }
         float mi, ri;
-        const float ms = block_scale(m, mi), rs = block_scale(root, ri);
+        const uint32_t m_top = block_top(m), r_top = block_top(root);
+        const float ms = block_scale(m_top, mi), rs = block_scale(r_top, ri);
+        const uint32_t first = (uint32_t(t.first) + uint32_t(i)) * kNumberFactor + key;
+        uint32_t mc[8], rc[8];
+        if (max(m_top, r_top) < 0x7F800000u) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t z = noise_of(uint32_t(t.first + i) + e, a.key);
-            m[e] = random_code(__fmul_rn(m[e], mi), z >> 16);
-            const float c = random_code(__fmul_rn(root[e], ri), z & 0xFFFFu);
-            root[e] = root[e] > 0.0f && c == 0.0f ? 0x1p-9f : c;
+            for (int e = 0; e < 8; ++e) {
+                const Pair xm = mul2(m[e / 2], both(mi)), xr = mul2(root[e / 2], both(ri));
+                const float x = e & 1 ? high(xm) : low(xm), y = e & 1 ? high(xr) : low(xr), r = e & 1 ? high(root[e / 2]) : low(root[e / 2]);
+                const uint32_t z = noise_of(first + uint32_t(e) * kNumberFactor);
+                mc[e] = random_code(x, ((z >> 12) & 0xFFFF0u) | 8u) | (__float_as_uint(x) >> 24 & 0x80u);
+                const uint32_t c = random_code(y, (z * 16u + 8u) & 0xFFFFFu);
+                rc[e] = r > 0.0f ? max(c, 1u) : c;   // the least code is 2^-9
+            }
+        } else {
+            // an infinity or NaN: the scale is one too, and every element with it
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = __fmul_rn(e & 1 ? high(m[e / 2]) : low(m[e / 2]), mi), r = e & 1 ? high(root[e / 2]) : low(root[e / 2]);
+                const float y = __fmul_rn(r, ri);
+                const uint32_t z = noise_of(first + uint32_t(e) * kNumberFactor);
+                mc[e] = x != x ? encode(x) : random_code(x, ((z >> 12) & 0xFFFF0u) | 8u) | (__float_as_uint(x) >> 24 & 0x80u);
+                const uint32_t c = y != y ? encode(y) : random_code(y, (z * 16u + 8u) & 0xFFFFFu);
+                rc[e] = r > 0.0f ? max(c, 1u) : c;
+            }
         }
-        store_codes<VEC>(static_cast<uint8_t *>(t.m), i, t.n, m);
-        store_codes<VEC>(static_cast<uint8_t *>(t.v), i, t.n, root);
+        store_codes<VEC>(static_cast<uint8_t *>(t.m), i, t.n, mc);
+        store_codes<VEC>(static_cast<uint8_t *>(t.v), i, t.n, rc);
         if ((threadIdx.x & 31) == 0 && block * kBlock < t.n) {
             t.m_scale[block] = ms;
             t.v_scale[block] = rs;
@@ -238,14 +278,14 @@ __device__ __forceinline__ void step8(const Tensor &t, const G *grad, int64_t i,
 }
 
 template <typename G, bool CODES>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ StepArgs a) {
+__global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_constant__ StepArgs a) {
     const Chunk c = a.chunks[blockIdx.x];   // the tables are the plan's: complete before any step
     const Tensor t = a.tensors[c.tensor];
     const G *grad = static_cast<const G *>(a.grads[c.tensor - a.first_tensor]);
     pdl_wait_previous();
     pdl_launch_dependents();
     if (grad == nullptr) return;   // a tensor without a gradient stays as it is
-    const float grad_scale = a.grad_scale ? *a.grad_scale : 1.0f;
+    const Factors k(a, a.grad_scale ? *a.grad_scale : 1.0f);
     const bool aligned = ((reinterpret_cast<uintptr_t>(t.p) | reinterpret_cast<uintptr_t>(grad) |
                            reinterpret_cast<uintptr_t>(t.copy)) & 15) == 0 &&
                          ((reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v)) & (CODES ? 7 : 15)) == 0;
@@ -255,8 +295,8 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
          i += kAdamThreads * kPerLane) {
         // a warp takes one block of 256: whole and aligned, or element by element
         const int64_t block_end = i - (threadIdx.x & 31) * kPerLane + kBlock;
-        if (aligned && block_end <= t.n) step8<G, CODES, true>(t, grad, i, grad_scale, a);
-        else step8<G, CODES, false>(t, grad, i < t.n ? i : t.n, grad_scale, a);
+        if (aligned && block_end <= t.n) step8<G, CODES, true>(t, grad, i, k, a.key);
+        else step8<G, CODES, false>(t, grad, i < t.n ? i : t.n, k, a.key);
     }
 }
 
