@@ -506,7 +506,7 @@ typedef struct darb_adamw_s *darb_adamw_t;
  *   gtype    type of the gradients
  * No two of the buffers may overlap.  Allocates the plan's tables on the current
  * device, runs on `stream` and synchronises it.
- * Errors: DARB_ERR_INVALID_ARG; DARB_ERR_UNSUPPORTED (2^31 chunks of 4096
+ * Errors: DARB_ERR_INVALID_ARG; DARB_ERR_UNSUPPORTED (2^31 chunks of 2048
  * elements or more); DARB_ERR_OOM; DARB_ERR_CUDA.
  */
 DARB_API darb_status_t darb_adamw_create(int32_t n, const int64_t *numel, float *const *params, void *const *m,

@@ -19,11 +19,12 @@
 // same on every run.  A root that is not zero keeps a code that is not zero, so
 // that no update is divided by eps alone.
 //
-// The step is bound by memory (28 bytes an element with fp32 gradients and states):
-// a CTA takes one chunk of kChunkElems consecutive elements of one tensor, so
-// that tensors of any sizes share the machine evenly; which chunk of which
-// tensor is looked up in a table made with the plan.  A warp takes a whole
-// block of 256, 8 elements a lane, so that a block's maximum is one reduction.
+// The step is bound by memory (28 bytes an element with fp32 gradients and
+// states).  The unit of work is a chunk of kChunkElems consecutive elements of
+// one tensor, so that tensors of any sizes share the machine evenly; which chunk
+// of which tensor is looked up in a table made with the plan.  A warp takes a
+// whole block of 256, 8 elements a lane, so that a block's maximum is one
+// reduction.
 #include "launch.cuh"
 #include "tma.cuh"
 #include "tokens.cuh"
@@ -39,11 +40,14 @@
 #include <vector>
 
 namespace darb {
+
+int sm_count();
+
 namespace {
 
 constexpr int kBlock = DARB_ADAMW_BLOCK;
 constexpr int kAdamThreads = 256;
-constexpr int kChunkElems = 4096;
+constexpr int kChunkElems = 2048;
 constexpr int kPerLane = kBlock / 32;
 constexpr int kGradPointers = 448;   // tensors of a launch: the pointers fit in 4 KB of arguments
 static_assert(kChunkElems % (kAdamThreads * kPerLane) == 0, "whole blocks of every warp in a chunk");
@@ -159,14 +163,13 @@ __device__ __forceinline__ void load_codes(const uint8_t *t, int64_t i, int64_t 
     for (int e = 0; e < 4; ++e) v[e] = mul2(decode2(uint16_t(w[e >> 1] >> (16 * (e & 1)))), both(scale));
 }
 template <bool VEC>
-__device__ __forceinline__ void store_codes(uint8_t *t, int64_t i, int64_t n, const uint32_t (&c)[8]) {
-    const uint32_t lo = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, hi = c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24;
+__device__ __forceinline__ void store_codes(uint8_t *t, int64_t i, int64_t n, const uint32_t (&c)[2]) {
     if (VEC) {
-        *reinterpret_cast<uint2 *>(t + i) = make_uint2(lo, hi);
+        *reinterpret_cast<uint2 *>(t + i) = make_uint2(c[0], c[1]);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (i + e < n) t[i + e] = uint8_t(c[e]);
+            if (i + e < n) t[i + e] = uint8_t(c[e / 4] >> (8 * (e & 3)));
     }
 }
 
@@ -179,36 +182,83 @@ __device__ __forceinline__ uint32_t noise_of(uint32_t z) {
     return z ^ (z >> 16);
 }
 
-// The code of |x| (at most 448, but for rounding; not NaN): the code below or
-// the one above it, above with the probability of its distance from the lower
-// one.  noise: 16 random bits times 16, plus 8.  Adding it to a value's bits
-// carries into the three bits of fraction that a code keeps as often as the
-// bits below them say; below 2^-6 the codes are 2^-9 apart, as they are from
-// 2^-6 to 2^-5, so smaller values are moved there and back.
-__device__ __forceinline__ uint32_t random_code(float x, uint32_t noise) {
-    const float a = fabsf(x);
-    const bool small = a < 0x1p-6f;
-    const uint32_t bits = __float_as_uint(__fadd_rn(a, small ? 0x1p-6f : 0.0f)) + noise;
-    // fp32 exponents count from 127 and codes' from 7: 120 << 3; a moved value is 1 << 3 too high
-    return min((bits >> 20) - (small ? 968u : 960u), 126u);
+// The code of a (at most 448, but for rounding; not negative, not NaN): the code
+// below or the one above it, above with the probability of its distance from the
+// lower one.  noise: 16 random bits times 16, plus 8.  Adding it to a value's
+// bits carries into the three bits of fraction that a code keeps as often as
+// the bits below them say.  Below 2^-6 the codes are 2^-9 apart, as they are from
+// 2^-6 to 2^-5, so smaller values are moved there; and halved, which makes the
+// exponent field of both kinds the code's own but for the different bias.
+__device__ __forceinline__ uint32_t random_code(float a, uint32_t noise) {
+    if (a < 0x1p-6f) a = fmaf(a, 0.5f, 0x1p-7f);   // (a + 2^-6) / 2, rounded as the sum is
+    return min((__float_as_uint(a) + (noise - (120u << 23))) >> 20, 126u);
 }
 
-// The scale of a block whose largest magnitude has the bits `top`, and its
-// inverse (0 where the scale would not be normal: the block's codes are 0).
-__device__ __forceinline__ float block_scale(uint32_t top, float &inverse) {
-    const float scale = __fmul_rn(__uint_as_float(top), float(1.0 / 448.0));
+// The scale of a block whose largest magnitude is `top`, and its inverse (0
+// where the scale would not be normal: the block's codes are 0).
+__device__ __forceinline__ float block_scale(float top, float &inverse) {
+    const float scale = __fmul_rn(top, float(1.0 / 448.0));
     inverse = scale >= FLT_MIN ? __fdiv_rn(1.0f, scale) : 0.0f;
     return scale;
 }
 
-// The largest magnitude's bits over a block (magnitudes order as their bits,
-// NaN above all).
-__device__ __forceinline__ uint32_t block_top(const Pair (&v)[4]) {
-    uint32_t top = 0;
+// The largest magnitude over a block (NaN if there is one): magnitudes order as
+// their bits, NaN above all.
+__device__ __forceinline__ float block_top(const Pair (&v)[4]) {
+    float top = max_nan(fabsf(low(v[0])), fabsf(high(v[0])));
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        top = max(top, max(__float_as_uint(low(v[e])) & 0x7FFFFFFFu, __float_as_uint(high(v[e])) & 0x7FFFFFFFu));
-    return __reduce_max_sync(0xFFFFFFFFu, top);
+    for (int e = 1; e < 4; ++e) top = max_nan(top, max_nan(fabsf(low(v[e])), fabsf(high(v[e]))));
+    return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top) & 0x7FFFFFFFu));
+}
+
+// Bytes b of four words, in one.
+template <int B>
+__device__ __forceinline__ uint32_t bytes_of(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
+    return __byte_perm(__byte_perm(w0, w1, B | (B + 4) << 4), __byte_perm(w2, w3, B | (B + 4) << 4), 0x5410);
+}
+
+// The codes and scales of a block's new m and roots: 8 of its elements a lane,
+// whose numbers are first, first + 1, ..., the last four GAP further.
+template <int GAP>
+__device__ __forceinline__ void encode_block(const Pair (&m)[4], const Pair (&root)[4], uint32_t first, uint32_t key, uint32_t (&mc)[2],
+                                             uint32_t (&rc)[2], float &ms, float &rs) {
+    float mi, ri;
+    const float m_top = block_top(m), r_top = block_top(root);
+    ms = block_scale(m_top, mi), rs = block_scale(r_top, ri);
+    const uint32_t z0 = first * kNumberFactor + key;
+    const bool finite = m_top < INFINITY && r_top < INFINITY;   // the same for the block
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float x[4], y[4];
+        uint32_t cm[4], cr[4];
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+            const Pair xm = mul2(m[2 * h + e / 2], both(mi)), xr = mul2(root[2 * h + e / 2], both(ri));
+            x[e] = low(xm), x[e + 1] = high(xm);
+            y[e] = low(xr), y[e + 1] = high(xr);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t z = noise_of(z0 + uint32_t(4 * h + e + h * GAP) * kNumberFactor);
+            cm[e] = random_code(fabsf(x[e]), ((z >> 12) & 0xFFFF0u) | 8u);
+            cr[e] = random_code(y[e], (z * 16u + 8u) & 0xFFFFFu);
+            if (!finite) {   // the scale is an infinity or NaN, and every element of the block with it
+                if (x[e] != x[e]) cm[e] = encode(x[e]);
+                if (y[e] != y[e]) cr[e] = encode(y[e]);
+            }
+        }
+        const uint32_t sign = bytes_of<3>(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+        mc[h] = bytes_of<0>(cm[0], cm[1], cm[2], cm[3]) | (sign & 0x80808080u);
+        rc[h] = bytes_of<0>(cr[0], cr[1], cr[2], cr[3]);
+        // a zero byte: a root that is not zero has the least code, 2^-9
+        if (((rc[h] - 0x01010101u) & ~rc[h] & 0x80808080u) != 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float r = e & 1 ? high(root[2 * h + e / 2]) : low(root[2 * h + e / 2]);
+                if (r > 0.0f && cr[e] == 0) rc[h] |= 1u << (8 * e);
+            }
+        }
+    }
 }
 
 template <typename G, bool CODES, bool VEC>
@@ -238,33 +288,9 @@ __device__ __forceinline__ void step8(const Tensor &t, const G *grad, int64_t i,
                 root[e] = pair(i + 2 * e < t.n ? low(root[e]) : 0.0f, i + 2 * e + 1 < t.n ? high(root[e]) : 0.0f);
             }
         }
-        float mi, ri;
-        const uint32_t m_top = block_top(m), r_top = block_top(root);
-        const float ms = block_scale(m_top, mi), rs = block_scale(r_top, ri);
-        const uint32_t first = (uint32_t(t.first) + uint32_t(i)) * kNumberFactor + key;
-        uint32_t mc[8], rc[8];
-        if (max(m_top, r_top) < 0x7F800000u) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const Pair xm = mul2(m[e / 2], both(mi)), xr = mul2(root[e / 2], both(ri));
-                const float x = e & 1 ? high(xm) : low(xm), y = e & 1 ? high(xr) : low(xr), r = e & 1 ? high(root[e / 2]) : low(root[e / 2]);
-                const uint32_t z = noise_of(first + uint32_t(e) * kNumberFactor);
-                mc[e] = random_code(x, ((z >> 12) & 0xFFFF0u) | 8u) | (__float_as_uint(x) >> 24 & 0x80u);
-                const uint32_t c = random_code(y, (z * 16u + 8u) & 0xFFFFFu);
-                rc[e] = r > 0.0f ? max(c, 1u) : c;   // the least code is 2^-9
-            }
-        } else {
-            // an infinity or NaN: the scale is one too, and every element with it
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x = __fmul_rn(e & 1 ? high(m[e / 2]) : low(m[e / 2]), mi), r = e & 1 ? high(root[e / 2]) : low(root[e / 2]);
-                const float y = __fmul_rn(r, ri);
-                const uint32_t z = noise_of(first + uint32_t(e) * kNumberFactor);
-                mc[e] = x != x ? encode(x) : random_code(x, ((z >> 12) & 0xFFFF0u) | 8u) | (__float_as_uint(x) >> 24 & 0x80u);
-                const uint32_t c = y != y ? encode(y) : random_code(y, (z * 16u + 8u) & 0xFFFFFu);
-                rc[e] = r > 0.0f ? max(c, 1u) : c;
-            }
-        }
+        uint32_t mc[2], rc[2];
+        float ms, rs;
+        encode_block<0>(m, root, uint32_t(t.first) + uint32_t(i), key, mc, rc, ms, rs);
         store_codes<VEC>(static_cast<uint8_t *>(t.m), i, t.n, mc);
         store_codes<VEC>(static_cast<uint8_t *>(t.v), i, t.n, rc);
         if ((threadIdx.x & 31) == 0 && block * kBlock < t.n) {
@@ -277,7 +303,28 @@ __device__ __forceinline__ void step8(const Tensor &t, const G *grad, int64_t i,
     }
 }
 
+// Whether whole blocks of a tensor can be read and written 16 (codes: 8) bytes at a time.
+template <bool CODES>
+__device__ __forceinline__ bool is_aligned(const Tensor &t, const void *grad) {
+    return ((reinterpret_cast<uintptr_t>(t.p) | reinterpret_cast<uintptr_t>(grad) | reinterpret_cast<uintptr_t>(t.copy)) & 15) == 0 &&
+           ((reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v)) & (CODES ? 7 : 15)) == 0;
+}
+
+// A warp's share of a chunk, straight from memory: one block of 256 at a time,
+// whole and aligned, or element by element.
 template <typename G, bool CODES>
+__device__ __forceinline__ void step_chunk(const Tensor &t, const G *grad, int64_t start, int warp, const Factors &k, uint32_t key) {
+    const int64_t end = t.n - start < kChunkElems ? t.n : start + kChunkElems;
+    const bool aligned = is_aligned<CODES>(t, grad);
+    for (int64_t b = start + int64_t(warp) * kBlock; b < end; b += kAdamThreads / 32 * kBlock) {
+        const int64_t i = b + (threadIdx.x & 31) * kPerLane;
+        if (aligned && b + kBlock <= t.n) step8<G, CODES, true>(t, grad, i, k, key);
+        else step8<G, CODES, false>(t, grad, i < t.n ? i : t.n, k, key);
+    }
+}
+
+// States in fp32: a CTA a chunk.
+template <typename G>
 __global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_constant__ StepArgs a) {
     const Chunk c = a.chunks[blockIdx.x];   // the tables are the plan's: complete before any step
     const Tensor t = a.tensors[c.tensor];
@@ -286,18 +333,165 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_con
     pdl_launch_dependents();
     if (grad == nullptr) return;   // a tensor without a gradient stays as it is
     const Factors k(a, a.grad_scale ? *a.grad_scale : 1.0f);
-    const bool aligned = ((reinterpret_cast<uintptr_t>(t.p) | reinterpret_cast<uintptr_t>(grad) |
-                           reinterpret_cast<uintptr_t>(t.copy)) & 15) == 0 &&
-                         ((reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v)) & (CODES ? 7 : 15)) == 0;
-    const int64_t start = int64_t(c.chunk) * kChunkElems;
-    const int64_t end = t.n - start < kChunkElems ? t.n : start + kChunkElems;
-    for (int64_t i = start + int64_t(threadIdx.x) * kPerLane; i - (threadIdx.x & 31) * kPerLane < end;
-         i += kAdamThreads * kPerLane) {
-        // a warp takes one block of 256: whole and aligned, or element by element
-        const int64_t block_end = i - (threadIdx.x & 31) * kPerLane + kBlock;
-        if (aligned && block_end <= t.n) step8<G, CODES, true>(t, grad, i, k, a.key);
-        else step8<G, CODES, false>(t, grad, i < t.n ? i : t.n, k, a.key);
+    step_chunk<G, false>(t, grad, int64_t(c.chunk) * kChunkElems, threadIdx.x >> 5, k, a.key);
+}
+
+// States in codes.  An element takes some 90 instructions for its 18 bytes, so
+// the loads have to run ahead of the arithmetic: persistent CTAs, whose last
+// warp copies chunk after chunk into a ring of stages (whole aligned chunks;
+// others are left where they are), and whose 8 other warps take a block each.
+constexpr int kStages = 4;
+template <typename G>
+struct Stage {
+    alignas(16) float p[kChunkElems];
+    alignas(16) G g[kChunkElems];
+    alignas(16) uint8_t m[kChunkElems], v[kChunkElems];
+    alignas(16) float m_scale[kChunkElems / kBlock], v_scale[kChunkElems / kBlock];
+    alignas(16) Tensor t;
+    const G *grad;
+    int64_t start;
+    int32_t staged;
+};
+
+// Four consecutive elements from shared memory.
+__device__ __forceinline__ void quad(const float *p, Pair &a, Pair &b) {
+    Pair v[2];
+    unpack(*reinterpret_cast<const uint4 *>(p), v);
+    a = v[0], b = v[1];
+}
+__device__ __forceinline__ void quad(const __nv_bfloat16 *p, Pair &a, Pair &b) {
+    const uint2 q = *reinterpret_cast<const uint2 *>(p);
+    const float2 x = widen2(q.x), y = widen2(q.y);
+    a = pair(x.x, x.y), b = pair(y.x, y.y);
+}
+__device__ __forceinline__ void quad(const uint8_t *p, float scale, Pair &a, Pair &b) {
+    const uint32_t q = *reinterpret_cast<const uint32_t *>(p);
+    a = mul2(decode2(uint16_t(q)), both(scale)), b = mul2(decode2(uint16_t(q >> 16)), both(scale));
+}
+
+template <typename G>
+__global__ void __launch_bounds__(kAdamThreads + 32, 2) adamw_codes_kernel(const __grid_constant__ StepArgs a, int32_t chunks) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    Stage<G> *ring = reinterpret_cast<Stage<G> *>(smem);
+    __shared__ uint64_t full[kStages], empty[kStages];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], kAdamThreads / 32);
+        }
+        fence_mbar_init();
     }
+    __syncthreads();
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    int stage = 0;
+    uint32_t parity = 0;
+    if (warp == kAdamThreads / 32) {
+        if (lane != 0) return;
+        for (int32_t c = blockIdx.x, it = 0; c < chunks; c += gridDim.x, ++it) {
+            const Chunk ch = a.chunks[c];
+            const Tensor t = a.tensors[ch.tensor];
+            const G *grad = static_cast<const G *>(a.grads[ch.tensor - a.first_tensor]);
+            const int64_t start = int64_t(ch.chunk) * kChunkElems, block = start / kBlock;
+            if (it >= kStages && !mbar_wait(&empty[stage], parity ^ 1)) return;
+            Stage<G> &s = ring[stage];
+            s.t = t;
+            s.grad = grad;
+            s.start = start;
+            s.staged = grad != nullptr && start + kChunkElems <= t.n && is_aligned<true>(t, grad) &&
+                       ((reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v) | reinterpret_cast<uintptr_t>(t.m_scale) |
+                         reinterpret_cast<uintptr_t>(t.v_scale)) & 15) == 0;
+            if (s.staged) {
+                mbar_arrive_expect_tx(&full[stage], sizeof(s.p) + sizeof(s.g) + sizeof(s.m) + sizeof(s.v) + sizeof(s.m_scale) + sizeof(s.v_scale));
+                bulk_g2s(s.p, t.p + start, sizeof(s.p), &full[stage]);
+                bulk_g2s(s.g, grad + start, sizeof(s.g), &full[stage]);
+                bulk_g2s(s.m, static_cast<const uint8_t *>(t.m) + start, sizeof(s.m), &full[stage]);
+                bulk_g2s(s.v, static_cast<const uint8_t *>(t.v) + start, sizeof(s.v), &full[stage]);
+                bulk_g2s(s.m_scale, t.m_scale + block, sizeof(s.m_scale), &full[stage]);
+                bulk_g2s(s.v_scale, t.v_scale + block, sizeof(s.v_scale), &full[stage]);
+            } else {
+                mbar_arrive(&full[stage]);
+            }
+            if (++stage == kStages) stage = 0, parity ^= 1;
+        }
+        return;
+    }
+    const Factors k(a, a.grad_scale ? *a.grad_scale : 1.0f);
+    static_assert(kChunkElems == kAdamThreads / 32 * kBlock, "a block a warp");
+    for (int32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+        if (!mbar_wait(&full[stage], parity)) return;   // a copy that never came
+        const Stage<G> &s = ring[stage];
+        if (s.staged) {
+            // a lane has 4 elements of either half of the block
+            const int at = warp * kBlock + 4 * lane;
+            Pair p[4], g[4], m[4], v[4], root[4];
+            const float m_scale = s.m_scale[warp], v_scale = s.v_scale[warp];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                quad(s.p + at + 128 * h, p[2 * h], p[2 * h + 1]);
+                quad(s.g + at + 128 * h, g[2 * h], g[2 * h + 1]);
+                quad(s.m + at + 128 * h, m_scale, m[2 * h], m[2 * h + 1]);
+                quad(s.v + at + 128 * h, v_scale, v[2 * h], v[2 * h + 1]);
+            }
+            const int64_t i = s.start + at, block = s.start / kBlock + warp;
+            float *tp = s.t.p + i;
+            __nv_bfloat16 *tc = s.t.copy;
+            uint8_t *tm = static_cast<uint8_t *>(s.t.m) + i, *tv = static_cast<uint8_t *>(s.t.v) + i;
+            float *tms = s.t.m_scale + block, *tvs = s.t.v_scale + block;
+            const uint32_t first = uint32_t(s.t.first) + uint32_t(i);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty[stage]);   // the warp has read its part
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = mul2(v[e], v[e]);
+                update(p[e], g[e], m[e], v[e], root[e], k);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const Pair q[2] = {p[2 * h], p[2 * h + 1]};
+                *reinterpret_cast<uint4 *>(tp + 128 * h) = pack(q);
+                if (tc != nullptr) {
+                    const __nv_bfloat162 x = __floats2bfloat162_rn(low(q[0]), high(q[0])), y = __floats2bfloat162_rn(low(q[1]), high(q[1]));
+                    *reinterpret_cast<uint2 *>(tc + i + 128 * h) =
+                        make_uint2(*reinterpret_cast<const uint32_t *>(&x), *reinterpret_cast<const uint32_t *>(&y));
+                }
+            }
+            uint32_t mc[2], rc[2];
+            float ms, rs;
+            encode_block<124>(m, root, first, a.key, mc, rc, ms, rs);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                *reinterpret_cast<uint32_t *>(tm + 128 * h) = mc[h];
+                *reinterpret_cast<uint32_t *>(tv + 128 * h) = rc[h];
+            }
+            if (lane == 0) *tms = ms, *tvs = rs;
+        } else {
+            const Tensor t = s.t;
+            const G *grad = s.grad;
+            const int64_t start = s.start;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty[stage]);
+            if (grad != nullptr) step_chunk<G, true>(t, grad, start, warp, k, a.key);
+        }
+        if (++stage == kStages) stage = 0, parity ^= 1;
+    }
+}
+
+template <typename G>
+cudaError_t launch_step(const StepArgs &a, bool codes, int64_t chunks, cudaStream_t stream) {
+    if (!codes) return launch_ex(adamw_kernel<G>, dim3(unsigned(chunks)), dim3(kAdamThreads), 0, stream, 1, true, a);
+    const auto kernel = adamw_codes_kernel<G>;
+    constexpr size_t smem = kStages * sizeof(Stage<G>);
+    const cudaError_t e = allow_smem(kernel, smem + 1024);
+    if (e != cudaSuccess) return e;
+    const int64_t per_sm = per_device(reinterpret_cast<const void *>(kernel), 0, [&]() -> long long {
+        int n = 0;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kAdamThreads + 32, smem) != cudaSuccess) cudaGetLastError();
+        return std::max(n, 1);
+    });
+    return launch_ex(kernel, dim3(unsigned(std::min(chunks, per_sm * sm_count()))), dim3(kAdamThreads + 32), smem, stream, 1, true, a,
+                     int32_t(chunks));
 }
 
 }  // namespace
@@ -470,9 +664,8 @@ darb_status_t darb_adamw_step(darb_adamw_t plan, const void *const *grads, const
         a.chunks = plan->d_chunks + plan->first_chunk[t0];
         a.first_tensor = t0;
         for (int32_t i = t0; i < t1; ++i) a.grads[i - t0] = grads[i];
-        const auto kernel = plan->gtype == DARB_BF16 ? (plan->codes ? adamw_kernel<__nv_bfloat16, true> : adamw_kernel<__nv_bfloat16, false>)
-                                                     : (plan->codes ? adamw_kernel<float, true> : adamw_kernel<float, false>);
-        if (launch_ex(kernel, dim3(unsigned(chunks)), dim3(kAdamThreads), 0, stream, 1, true, a) != cudaSuccess) {
+        if ((plan->gtype == DARB_BF16 ? launch_step<__nv_bfloat16>(a, plan->codes, chunks, stream)
+                                      : launch_step<float>(a, plan->codes, chunks, stream)) != cudaSuccess) {
             cudaGetLastError();
             return DARB_ERR_CUDA;
         }
