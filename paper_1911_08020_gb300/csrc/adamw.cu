@@ -217,16 +217,12 @@ __device__ __forceinline__ uint32_t bytes_of(uint32_t w0, uint32_t w1, uint32_t 
     return __byte_perm(__byte_perm(w0, w1, B | (B + 4) << 4), __byte_perm(w2, w3, B | (B + 4) << 4), 0x5410);
 }
 
-// The codes and scales of a block's new m and roots: 8 of its elements a lane,
-// whose numbers are first, first + 1, ..., the last four GAP further.
-template <int GAP>
-__device__ __forceinline__ void encode_block(const Pair (&m)[4], const Pair (&root)[4], uint32_t first, uint32_t key, uint32_t (&mc)[2],
-                                             uint32_t (&rc)[2], float &ms, float &rs) {
-    float mi, ri;
-    const float m_top = block_top(m), r_top = block_top(root);
-    ms = block_scale(m_top, mi), rs = block_scale(r_top, ri);
-    const uint32_t z0 = first * kNumberFactor + key;
-    const bool finite = m_top < INFINITY && r_top < INFINITY;   // the same for the block
+// The codes of a lane's 8 elements of a block, given the inverse scales.  z0:
+// of the first element's noise; the last four elements are GAP further.  FINITE:
+// no infinity or NaN in the block.
+template <int GAP, bool FINITE>
+__device__ __forceinline__ void encode_lane(const Pair (&m)[4], const Pair (&root)[4], float mi, float ri, uint32_t z0, uint32_t (&mc)[2],
+                                            uint32_t (&rc)[2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         float x[4], y[4];
@@ -242,7 +238,7 @@ __device__ __forceinline__ void encode_block(const Pair (&m)[4], const Pair (&ro
             const uint32_t z = noise_of(z0 + uint32_t(4 * h + e + h * GAP) * kNumberFactor);
             cm[e] = random_code(fabsf(x[e]), ((z >> 12) & 0xFFFF0u) | 8u);
             cr[e] = random_code(y[e], (z * 16u + 8u) & 0xFFFFFu);
-            if (!finite) {   // the scale is an infinity or NaN, and every element of the block with it
+            if (!FINITE) {   // the scale is an infinity or NaN, and every element of the block with it
                 if (x[e] != x[e]) cm[e] = encode(x[e]);
                 if (y[e] != y[e]) cr[e] = encode(y[e]);
             }
@@ -259,6 +255,19 @@ __device__ __forceinline__ void encode_block(const Pair (&m)[4], const Pair (&ro
             }
         }
     }
+}
+
+// The codes and scales of a block's new m and roots: 8 of its elements a lane,
+// whose numbers are first, first + 1, ..., the last four GAP further.
+template <int GAP>
+__device__ __forceinline__ void encode_block(const Pair (&m)[4], const Pair (&root)[4], uint32_t first, uint32_t key, uint32_t (&mc)[2],
+                                             uint32_t (&rc)[2], float &ms, float &rs) {
+    float mi, ri;
+    const float m_top = block_top(m), r_top = block_top(root);
+    ms = block_scale(m_top, mi), rs = block_scale(r_top, ri);
+    const uint32_t z0 = first * kNumberFactor + key;
+    if (m_top < INFINITY && r_top < INFINITY) encode_lane<GAP, true>(m, root, mi, ri, z0, mc, rc);   // the same for the warp
+    else encode_lane<GAP, false>(m, root, mi, ri, z0, mc, rc);
 }
 
 template <typename G, bool CODES, bool VEC>

@@ -765,9 +765,10 @@ struct GradArgs {
     const float *lse, *entropy, *d_logprob, *d_entropy;   // or null, but lse
 };
 
-// What a token's gradient is made from.
+// What a token's gradient is made from:  dx_v = a [v = target] - p_v (b log p_v + c),
+// c = a + b H.
 struct GradToken {
-    float lse, a, b, h;
+    float lse, a, b, c;
     int32_t target;   // -1: none
 };
 __device__ __forceinline__ GradToken grad_token(const GradArgs &g, int64_t token) {
@@ -781,21 +782,33 @@ __device__ __forceinline__ GradToken grad_token(const GradArgs &g, int64_t token
             t.target = int32_t(target);
         }
     }
+    t.c = t.a;
     if (g.d_entropy != nullptr) {
         t.b = g.d_entropy[token];
-        t.h = g.entropy[token];
+        t.c = fmaf(t.b, g.entropy[token], t.a);
     }
-    if (t.lse == -INFINITY) {   // no entry: no distribution, no gradient
-        const bool nan = t.a != t.a;
-        t = {0.0f, nan ? t.a : 0.0f, 0.0f, 0.0f, -1};
-    }
+    if (t.lse == -INFINITY) t = {0.0f, 0.0f, 0.0f, t.a == t.a ? 0.0f : t.a, -1};   // no entry: no distribution, no gradient
     return t;
 }
-__device__ __forceinline__ float grad_of(const GradToken &t, float x, int32_t v) {
-    const float l = max_nan(x - t.lse, kMasked);   // log p; a masked entry has p = 0
-    const float p = exp2_fast(l * kLog2e);
-    const float hit = v == t.target ? 1.0f : 0.0f;
-    return fmaf(t.a, hit - p, -t.b * p * (l + t.h));
+
+// N logits of one token, from v0 on `step` apart, to their gradients.  A masked
+// entry has p = 0; log p is held above -2^15 or so, so that it adds 0 there.
+template <int N>
+__device__ __forceinline__ void grad_of(const GradToken &t, Pair (&x)[N], int32_t v0, int32_t step) {
+    const Pair lse = both(-t.lse), log2e = both(kLog2e), b = both(-t.b), c = both(-t.c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        Pair l = add2(x[i], lse);
+        l = pair(max_nan(low(l), kMasked), max_nan(high(l), kMasked));
+        const Pair d = mul2(l, log2e);
+        x[i] = mul2(pair(exp2_fast(low(d)), exp2_fast(high(d))), fma2(l, b, c));
+    }
+    const uint32_t at = uint32_t(t.target - v0);
+    if (t.target >= 0 && at < uint32_t(2 * N * step)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            x[i] = pair(low(x[i]) + (at == uint32_t(2 * i * step) ? t.a : 0.0f), high(x[i]) + (at == uint32_t((2 * i + 1) * step) ? t.a : 0.0f));
+    }
 }
 
 constexpr int kGradThreads = 256;
@@ -813,64 +826,64 @@ __global__ void __launch_bounds__(kGradThreads) grad_rows_kernel(const GradArgs 
     T *out = static_cast<T *>(a.dx) + token * a.ldd;
     const int head = row_head<T>(row);
     const int32_t n = a.vocab, granules = int32_t(row_granules<T>(head, n));
-    const int32_t g0 = part * (kGradThreads * U) + int32_t(threadIdx.x);
-    uint4 q[U];
+    const int32_t first = part * (kGradThreads * U), g0 = first + int32_t(threadIdx.x);
+    // (plain loads: the gradient may take the logits' place)
+    if (first >= (head > 0 ? 1 : 0) && first + kGradThreads * U <= (head + n) / V) {   // granules all in the row
+        const uint4 *in = reinterpret_cast<const uint4 *>(row - head) + g0;
+        uint4 *to = reinterpret_cast<uint4 *>(out - head) + g0;
+        uint4 q[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int32_t g = g0 + u * kGradThreads;
-        if (g < granules) q[u] = load_granule<T, false>(row, int64_t(g) * V - head, n, -INFINITY);
+        for (int u = 0; u < U; ++u) q[u] = in[u * kGradThreads];
+        const GradToken t = grad_token(a, token);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            Pair v[V / 2];
+            unpack(q[u], v);
+            grad_of(t, v, (g0 + u * kGradThreads) * V - head, 1);
+            to[u * kGradThreads] = pack(v);
+        }
+        return;
     }
     const GradToken t = grad_token(a, token);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int32_t g = g0 + u * kGradThreads;
-        if (g >= granules) break;
+    for (int32_t g = g0; g < min(granules, first + kGradThreads * U); g += kGradThreads) {
         const int64_t j0 = int64_t(g) * V - head;
-        float v[V];
-        unpack(q[u], v);
+        Pair v[V / 2];
+        unpack(load_granule<T, false>(row, j0, n, -INFINITY), v);
+        grad_of(t, v, int32_t(j0), 1);
+        float w[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = grad_of(t, v[i], int32_t(j0 + i));
-        store_granule(out, j0, n, v);
+        for (int i = 0; i < V / 2; ++i) w[2 * i] = low(v[i]), w[2 * i + 1] = high(v[i]);
+        store_granule(out, j0, n, w);
     }
 }
 
-// Any strides: logit v of token t at x[t * ts + v * vs].  Consecutive threads
-// take consecutive elements of the contiguous axis.
+// Rows that do not start alike, and columns: consecutive threads take
+// consecutive elements of the contiguous axis, U of them each.
 template <typename T, bool COLUMNS>
 __global__ void __launch_bounds__(kGradThreads) grad_any_kernel(const GradArgs a, int32_t parts) {
     constexpr int U = 8;
     pdl_wait_previous();
     pdl_launch_dependents();
-    const T *x = static_cast<const T *>(a.x);
-    T *dx = static_cast<T *>(a.dx);
-    if constexpr (COLUMNS) {
-        // 32 columns x 8 rows of threads, U rows each
-        const int64_t token = int64_t(blockIdx.x / parts) * 32 + (threadIdx.x & 31);
-        if (token >= a.tokens) return;
-        const int64_t v0 = int64_t(blockIdx.x % parts) * (8 * U) + (threadIdx.x >> 5);
-        float v[U];
+    // columns: 32 tokens x 8 rows of threads; rows: one token
+    const int64_t token = COLUMNS ? int64_t(blockIdx.x / parts) * 32 + (threadIdx.x & 31) : blockIdx.x / parts;
+    if (token >= a.tokens) return;
+    const int32_t part = int32_t(blockIdx.x % parts), step = COLUMNS ? kGradThreads / 32 : kGradThreads;
+    const int32_t v0 = part * (step * U) + int32_t(COLUMNS ? threadIdx.x >> 5 : threadIdx.x);
+    const T *x = static_cast<const T *>(a.x) + (COLUMNS ? v0 * a.ld + token : token * a.ld + v0);
+    T *dx = static_cast<T *>(a.dx) + (COLUMNS ? v0 * a.ldd + token : token * a.ldd + v0);
+    const int64_t by = COLUMNS ? step * a.ld : step, by_out = COLUMNS ? step * a.ldd : step;
+    const bool whole = v0 + (U - 1) * step < a.vocab;
+    Pair v[U / 2];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v0 + 8 * u < a.vocab) v[u] = widen(x[(v0 + 8 * u) * a.ld + token]);
-        const GradToken t = grad_token(a, token);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v0 + 8 * u < a.vocab) dx[(v0 + 8 * u) * a.ldd + token] = narrow<T>(grad_of(t, v[u], int32_t(v0 + 8 * u)));
-    } else {
-        const int64_t token = blockIdx.x / parts;
-        const int64_t v0 = int64_t(blockIdx.x % parts) * (kGradThreads * U) + threadIdx.x;
-        const T *row = x + token * a.ld;
-        T *out = dx + token * a.ldd;
-        float v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v0 + u * kGradThreads < a.vocab) v[u] = widen(row[v0 + u * kGradThreads]);
-        const GradToken t = grad_token(a, token);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v0 + u * kGradThreads < a.vocab)
-                out[v0 + u * kGradThreads] = narrow<T>(grad_of(t, v[u], int32_t(v0 + u * kGradThreads)));
+    for (int u = 0; u < U; u += 2) {
+        const float lo = whole || v0 + u * step < a.vocab ? widen(x[u * by]) : 0.0f;
+        v[u / 2] = pair(lo, whole || v0 + (u + 1) * step < a.vocab ? widen(x[(u + 1) * by]) : 0.0f);
     }
+    const GradToken t = grad_token(a, token);
+    grad_of(t, v, v0, step);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (whole || v0 + u * step < a.vocab) dx[u * by_out] = narrow<T>(u & 1 ? high(v[u / 2]) : low(v[u / 2]));
 }
 
 template <typename T>
