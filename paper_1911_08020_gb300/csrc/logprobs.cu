@@ -31,6 +31,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace cg = cooperative_groups;
 
@@ -886,13 +887,60 @@ __global__ void __launch_bounds__(kGradThreads) grad_any_kernel(const GradArgs a
         if (whole || v0 + u * step < a.vocab) dx[u * by_out] = narrow<T>(u & 1 ? high(v[u / 2]) : low(v[u / 2]));
 }
 
+// Columns whose rows can be read two tokens at a time: 64 tokens x 8 rows of
+// threads, U rows each, a pair the same entry of two tokens.
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) grad_columns_kernel(const GradArgs a, int32_t parts) {
+    constexpr int U = 8, ROWS = kGradThreads / 32;
+    using Two = typename std::conditional<sizeof(T) == 4, uint2, uint32_t>::type;
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    const int64_t token = int64_t(blockIdx.x / parts) * 64 + 2 * (threadIdx.x & 31);
+    if (token >= a.tokens) return;
+    const int32_t v0 = int32_t(blockIdx.x % parts) * (ROWS * U) + int32_t(threadIdx.x >> 5);
+    const T *x = static_cast<const T *>(a.x) + v0 * a.ld + token;
+    T *dx = static_cast<T *>(a.dx) + v0 * a.ldd + token;
+    const int64_t by = ROWS * a.ld, by_out = ROWS * a.ldd;
+    if (token + 1 == a.tokens || v0 + (U - 1) * ROWS >= a.vocab) {   // one by one
+        for (int k = 0; k < 2 && token + k < a.tokens; ++k) {
+            const GradToken t = grad_token(a, token + k);
+            for (int32_t u = 0, v = v0; v < a.vocab && u < U; ++u, v += ROWS) {
+                Pair g[1] = {both(widen(x[u * by + k]))};
+                grad_of(t, g, v, a.vocab);   // (the second value is nobody's)
+                dx[u * by_out + k] = narrow<T>(low(g[0]));
+            }
+        }
+        return;
+    }
+    Two q[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u, x += by) q[u] = *reinterpret_cast<const Two *>(x);
+    const GradToken t0 = grad_token(a, token), t1 = grad_token(a, token + 1);
+    const Pair lse = pair(-t0.lse, -t1.lse), log2e = both(kLog2e), b = pair(-t0.b, -t1.b), c = pair(-t0.c, -t1.c);
+#pragma unroll
+    for (int u = 0; u < U; ++u, dx += by_out) {
+        Pair l;
+        if constexpr (sizeof(T) == 4) l = pair(__uint_as_float(q[u].x), __uint_as_float(q[u].y));
+        else l = pair(widen2(q[u]).x, widen2(q[u]).y);
+        l = add2(l, lse);
+        l = pair(max_nan(low(l), kMasked), max_nan(high(l), kMasked));
+        const Pair d = mul2(l, log2e), g = mul2(pair(exp2_fast(low(d)), exp2_fast(high(d))), fma2(l, b, c));
+        const int32_t v = v0 + u * ROWS;
+        const float g0 = low(g) + (v == t0.target ? t0.a : 0.0f), g1 = high(g) + (v == t1.target ? t1.a : 0.0f);
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float2 *>(dx) = make_float2(g0, g1);
+        else *reinterpret_cast<__nv_bfloat162 *>(dx) = __floats2bfloat162_rn(g0, g1);
+    }
+}
+
 template <typename T>
 cudaError_t launch_grad(const GradArgs &a, darb_layout_t layout, cudaStream_t stream) {
     const auto grid = [](int64_t n) { return dim3(unsigned(n)); };
     if (layout == DARB_TOKEN_COLUMNS) {
         const int32_t parts = int32_t((a.vocab + 63) / 64);
-        const int64_t blocks = (a.tokens + 31) / 32 * parts;
+        const bool pairs = a.tokens > 32 && a.ld % 2 == 0 && a.ldd % 2 == 0 && aligned_to(a.x, 2 * sizeof(T)) && aligned_to(a.dx, 2 * sizeof(T));
+        const int64_t blocks = (pairs ? (a.tokens + 63) / 64 : (a.tokens + 31) / 32) * parts;
         if (blocks > INT32_MAX) return cudaErrorNotSupported;
+        if (pairs) return launch_ex(grad_columns_kernel<T>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
         return launch_ex(grad_any_kernel<T, true>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
     }
     // logits and gradients of every row start alike past a 16-byte boundary
