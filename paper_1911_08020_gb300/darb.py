@@ -8,6 +8,7 @@ the library's CUDA kernels; if ``libdarb.so`` is missing or a call fails, a
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 from dataclasses import dataclass
@@ -447,11 +448,13 @@ def _tokens(t, dim: int, call: str, name: str) -> tuple[int, int, int, int, int]
     return TOKEN_COLUMNS, steps, n, f, ld
 
 
-def _same_tokens(t, like, dim: int, layout: int, call: str, name: str) -> int:
-    """The leading dimension of a tensor of the shape, type and layout of another."""
+def _same_tokens(t, like, ld: int, dim: int, layout: int, call: str, name: str) -> int:
+    """The leading dimension of a tensor of the shape, type and layout of another, whose own is `ld`."""
     if not t.is_cuda or t.dtype != like.dtype or t.shape != like.shape:
         _refuse(call, f"{name} must be a CUDA tensor of the input's shape and type")
     strides = t.stride()
+    if strides == like.stride():
+        return ld
     f, n = (t.shape[dim], t.shape[1 - dim % 2 if t.dim() == 2 else 2])
     fs, ns = (strides[dim], strides[1 - dim % 2 if t.dim() == 2 else 2])
     steps = 1 if t.dim() == 2 else t.shape[0]
@@ -528,7 +531,7 @@ def darb_token_logprobs_grad(logits, targets, lse, d_logprob, entropy=None, d_en
         out = _new((n, v) if layout == TOKEN_ROWS else (v, n), logits.dtype, logits.device, stream)
         if (layout == TOKEN_ROWS) != (dim % 2 == 1):
             out = out.t()
-    ld_out = _same_tokens(out, logits, dim, layout, call, "out")
+    ld_out = _same_tokens(out, logits, ld, dim, layout, call, "out")
     f32 = torch.float32
     _check(lib().darb_token_logprobs_grad(logits.data_ptr(), code, layout, n, v, ld,
                                           _vector(targets, n, torch.int64, call, "targets"), _vector(lse, n, f32, call, "lse"),
@@ -559,7 +562,7 @@ def darb_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, dim: int = -1, 
         rstd = _new(lead, f32, x.device, stream)
     _check(lib().darb_layer_norm(x.data_ptr(), code, layout, steps, n, f, ld, _vector(gamma, f, f32, call, "gamma"),
                                  _vector(beta, f, f32, call, "beta"), eps, y.data_ptr(),
-                                 _same_tokens(y, x, dim, layout, call, "y"), _vector(mean, steps * n, f32, call, "mean"),
+                                 _same_tokens(y, x, ld, dim, layout, call, "y"), _vector(mean, steps * n, f32, call, "mean"),
                                  _vector(rstd, steps * n, f32, call, "rstd"), _stream(stream)), call)
     return y, mean, rstd
 
@@ -589,7 +592,7 @@ def darb_layer_norm_grad(dy, x, gamma, mean, rstd, dim: int = -1, dx=None, dgamm
         if dbeta is None:
             dbeta = _new((f,), f32, x.device, stream)
         pg, pb = _vector(dgamma, f, f32, call, "dgamma"), _vector(dbeta, f, f32, call, "dbeta")
-        need = darb_layer_norm_grad_work(layout, steps, n, f)
+        need = _work_bytes(layout, steps, n, f, _torch.cuda.current_device())
         if work is None:
             work = _new((need,), _torch.uint8, x.device, stream)
         elif not work.is_cuda or not work.is_contiguous() or work.numel() * work.element_size() < need:
@@ -597,10 +600,10 @@ def darb_layer_norm_grad(dy, x, gamma, mean, rstd, dim: int = -1, dx=None, dgamm
         pw = work.data_ptr()
     else:
         dgamma = dbeta = None
-    _check(lib().darb_layer_norm_grad(dy.data_ptr(), _same_tokens(dy, x, dim, layout, call, "dy"), x.data_ptr(), ld, code,
+    _check(lib().darb_layer_norm_grad(dy.data_ptr(), _same_tokens(dy, x, ld, dim, layout, call, "dy"), x.data_ptr(), ld, code,
                                       layout, steps, n, f, _vector(gamma, f, f32, call, "gamma"),
                                       _vector(mean, steps * n, f32, call, "mean"), _vector(rstd, steps * n, f32, call, "rstd"),
-                                      dx.data_ptr(), _same_tokens(dx, x, dim, layout, call, "dx"), pg, pb, pw,
+                                      dx.data_ptr(), _same_tokens(dx, x, ld, dim, layout, call, "dx"), pg, pb, pw,
                                       _stream(stream)), call)
     return dx, dgamma, dbeta
 
@@ -611,6 +614,11 @@ def darb_layer_norm_grad_work(layout: int, steps: int, tokens: int, features: in
     _check(lib().darb_layer_norm_grad_work(layout, steps, tokens, features, ctypes.byref(need)),
            "darb_layer_norm_grad_work")
     return need.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _work_bytes(layout: int, steps: int, tokens: int, features: int, device: int) -> int:
+    return darb_layer_norm_grad_work(layout, steps, tokens, features)
 
 
 class AdamW:
