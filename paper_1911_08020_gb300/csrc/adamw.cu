@@ -627,7 +627,7 @@ darb_status_t darb_adamw_create(int32_t n, const int64_t *numel, float *const *p
             std::lock_guard<std::mutex> lk(g_plans_mu);
             g_plans.insert(plan);
         }
-    } catch (const std::bad_alloc &) {
+    } catch (...) {   // std::bad_alloc, or a vector asked for more than it can hold
         st = DARB_ERR_OOM;
     }
     if (st != DARB_OK) {
@@ -673,11 +673,11 @@ darb_status_t darb_adamw_step(darb_adamw_t plan, const void *const *grads, const
         a.chunks = plan->d_chunks + plan->first_chunk[t0];
         a.first_tensor = t0;
         for (int32_t i = t0; i < t1; ++i) a.grads[i - t0] = grads[i];
-        if ((plan->gtype == DARB_BF16 ? launch_step<__nv_bfloat16>(a, plan->codes, chunks, stream)
-                                      : launch_step<float>(a, plan->codes, chunks, stream)) != cudaSuccess) {
-            cudaGetLastError();
-            return DARB_ERR_CUDA;
-        }
+        const darb_status_t st = enqueue([&] {
+            return plan->gtype == DARB_BF16 ? launch_step<__nv_bfloat16>(a, plan->codes, chunks, stream)
+                                            : launch_step<float>(a, plan->codes, chunks, stream);
+        });
+        if (st != DARB_OK) return st;
     }
     return DARB_OK;
 }

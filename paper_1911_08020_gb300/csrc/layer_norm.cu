@@ -792,8 +792,9 @@ bool alike(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows,
 // where wider tiles would leave SMs idle, down to the 32 bytes that memory
 // moves at a time.
 int col_tile(int64_t steps, int64_t tokens, size_t es) {
+    const int sms = sm_count();
     int ct = 32;
-    while (ct > 4 && (tokens <= ct / 2 || (ct * int(es) > 32 && steps * ((tokens + ct / 2 - 1) / (ct / 2)) * kColSplit <= sm_count())))
+    while (ct > 4 && (tokens <= ct / 2 || (ct * int(es) > 32 && steps * ((tokens + ct / 2 - 1) / (ct / 2)) * kColSplit <= sms)))
         ct /= 2;
     return ct;
 }
@@ -806,8 +807,9 @@ cudaError_t with_col_tile(const NormArgs &a, F f) {
     const int64_t tiles = (a.tokens + ct - 1) / ct, all = tiles * a.steps;
     // more CTAs a tile while each thread keeps half a batch of features (1500 x 20:
     // 5.5 us; with a quarter of one 6.7, with a whole one 6.0)
+    const int sms = sm_count();
     int split = 1;
-    while (split < kColSplit && all * split < 2 * sm_count() && a.features / (2 * split) >= kColBatch / 2 * kColThreads / ct) split *= 2;
+    while (split < kColSplit && all * split < 2 * sms && a.features / (2 * split) >= kColBatch / 2 * kColThreads / ct) split *= 2;
     if (all * split > INT32_MAX) return cudaErrorNotSupported;
     const dim3 grid(unsigned(all * split));
     if (ct == 32) return f(std::integral_constant<int, 32>(), grid, unsigned(split), int32_t(tiles));
@@ -895,10 +897,12 @@ cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, 
     return e;
 }
 
-darb_status_t status_of(cudaError_t e) {
-    if (e == cudaSuccess) return DARB_OK;
-    cudaGetLastError();
-    return e == cudaErrorNotSupported ? DARB_ERR_UNSUPPORTED : DARB_ERR_CUDA;
+// The scratch of the backward pass: its partial results.
+darb_status_t work_bytes(darb_layout_t layout, int64_t steps, int64_t tokens, int64_t features, int64_t *bytes) {
+    return enqueue([&] {
+        *bytes = most_partials(layout, steps, tokens) * 2 * partial_width(int32_t(features)) * int64_t(sizeof(float));
+        return cudaSuccess;
+    });
 }
 
 constexpr int64_t kMaxNormFeatures = int64_t(1) << 24;   // below 2^24 a count is exact in fp32
@@ -955,7 +959,7 @@ darb_status_t darb_layer_norm(const void *x, darb_dtype_t dtype, darb_layout_t l
     a.x = x, a.out = y, a.ld_x = ld_x, a.ld_out = ld_y, a.steps = steps, a.tokens = tokens, a.features = int32_t(features);
     a.gamma = gamma, a.beta = beta, a.eps = eps, a.mean = mean, a.rstd = rstd;
     if (is_rows(layout, tokens, ld_x, ld_y, 1)) as_rows(a, layout);
-    return status_of(dtype == DARB_BF16 ? launch_norm<__nv_bfloat16>(a, layout, stream) : launch_norm<float>(a, layout, stream));
+    return enqueue([&] { return dtype == DARB_BF16 ? launch_norm<__nv_bfloat16>(a, layout, stream) : launch_norm<float>(a, layout, stream); });
 }
 
 darb_status_t darb_layer_norm_grad_work(darb_layout_t layout, int64_t steps, int64_t tokens, int64_t features, int64_t *bytes) {
@@ -963,8 +967,7 @@ darb_status_t darb_layer_norm_grad_work(darb_layout_t layout, int64_t steps, int
     if (bytes == nullptr) return DARB_ERR_INVALID_ARG;
     const darb_status_t st = check_norm(DARB_F32, layout, steps, tokens, features);
     if (st != DARB_OK) return st == DARB_ERR_UNSUPPORTED ? st : DARB_ERR_INVALID_ARG;
-    *bytes = most_partials(layout, steps, tokens) * 2 * partial_width(int32_t(features)) * 4;
-    return DARB_OK;
+    return work_bytes(layout, steps, tokens, features, bytes);
 }
 
 darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, darb_dtype_t dtype,
@@ -981,8 +984,10 @@ darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x,
     if (steps * tokens == 0) {
         if (dgamma == nullptr) return DARB_OK;
         if (ranges_overlap(dgamma, features * 4, dbeta, features * 4)) return DARB_ERR_INVALID_ARG;
-        return status_of(launch_ex(zero_kernel, dim3(unsigned((features + 255) / 256)), dim3(256), 0, stream, 1, true, dgamma,
-                                   dbeta, int32_t(features)));
+        return enqueue([&] {
+            return launch_ex(zero_kernel, dim3(unsigned((features + 255) / 256)), dim3(256), 0, stream, 1, true, dgamma, dbeta,
+                             int32_t(features));
+        });
     }
     const size_t es = dtype_size(dtype);
     if (dy == nullptr || x == nullptr || dx == nullptr || mean == nullptr || rstd == nullptr || !aligned_to(dy, es) ||
@@ -994,8 +999,11 @@ darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x,
     if (nd < 0 || nx < 0 || no < 0) return DARB_ERR_UNSUPPORTED;
     const bool in_place = dx == dy && ld_dx == ld_dy;
     const int64_t all = steps * tokens;
+    int64_t scratch = 0;
+    st = work_bytes(layout, steps, tokens, features, &scratch);
+    if (st != DARB_OK) return st;
     const Range outs[] = {{dx, no * int64_t(es)}, {dgamma, features * 4}, {dbeta, features * 4},
-                          {dgamma ? work : nullptr, most_partials(layout, steps, tokens) * 8 * partial_width(int32_t(features))}};
+                          {dgamma ? work : nullptr, scratch}};
     const Range ins[] = {{in_place ? nullptr : dy, nd * int64_t(es)}, {x, nx * int64_t(es)}, {gamma, features * 4},
                          {mean, all * 4}, {rstd, all * 4}};
     if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
@@ -1005,8 +1013,10 @@ darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x,
     a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
     a.partial = dgamma ? static_cast<float *>(work) : nullptr;
     if (is_rows(layout, tokens, ld_x, ld_dy, ld_dx)) as_rows(a, layout);
-    return status_of(dtype == DARB_BF16 ? launch_back<__nv_bfloat16>(a, layout, dgamma, dbeta, stream)
-                                        : launch_back<float>(a, layout, dgamma, dbeta, stream));
+    return enqueue([&] {
+        return dtype == DARB_BF16 ? launch_back<__nv_bfloat16>(a, layout, dgamma, dbeta, stream)
+                                  : launch_back<float>(a, layout, dgamma, dbeta, stream);
+    });
 }
 
 }  // extern "C"

@@ -733,13 +733,14 @@ cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream, int split
 
 template <typename T>
 cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream) {
+    const int sms = sm_count();
     const bool short_rows = row_granules<T>(0, a.vocab) <= 8192;
-    if (a.tokens >= 4 * sm_count() && short_rows) return launch_score_rows<T, 128>(a, stream, 1);
+    if (a.tokens >= 4 * sms && short_rows) return launch_score_rows<T, 128>(a, stream, 1);
     // CTAs for every SM, while a thread keeps two granules (a vocabulary of 32000 in
     // bf16: one token 6.0 us, with one granule 6.4, with four 6.5; 50 tokens of 31856
     // in fp32 on 200 CTAs 9.4, on 400 11.8)
     int split = 1;
-    while (split < kMaxSplit && a.tokens * split < sm_count() && a.vocab / (2 * split) >= 2 * 256 * kPerGranule<T>) split *= 2;
+    while (split < kMaxSplit && a.tokens * split < sms && a.vocab / (2 * split) >= 2 * 256 * kPerGranule<T>) split *= 2;
     return launch_score_rows<T, 256>(a, stream, split);
 }
 
@@ -748,8 +749,9 @@ cudaError_t launch_score_columns_ct(const ScoreArgs &a, cudaStream_t stream) {
     const int64_t tiles = (a.tokens + CT - 1) / CT;
     // the candidates of every CTA of a cluster have to fit a column's list
     const int most = a.k > 0 ? std::max(1, kColCandidates / a.k) : kMaxSplit;
+    const int sms = sm_count();
     int split = 1;
-    while (split < kMaxSplit && 2 * split <= most && tiles * split < sm_count() && a.vocab / (2 * split) >= 4 * kColThreads / CT)
+    while (split < kMaxSplit && 2 * split <= most && tiles * split < sms && a.vocab / (2 * split) >= 4 * kColThreads / CT)
         split *= 2;
     const int64_t rows = a.vocab / split + 1;   // of a CTA, at most
     constexpr int per_round = kColThreads / CT * kColUnroll;
@@ -763,9 +765,10 @@ cudaError_t launch_score_columns_ct(const ScoreArgs &a, cudaStream_t stream) {
 
 template <typename T>
 cudaError_t launch_score_columns(const ScoreArgs &a, cudaStream_t stream) {
+    const int sms = sm_count();
     int ct = 32;
     // narrower tiles where the wider leave SMs idle, down to the 32 bytes that memory moves at a time
-    while (ct > 4 && (a.tokens <= ct / 2 || (ct * int(sizeof(T)) > 32 && (a.tokens + ct / 2 - 1) / (ct / 2) * kMaxSplit <= sm_count())))
+    while (ct > 4 && (a.tokens <= ct / 2 || (ct * int(sizeof(T)) > 32 && (a.tokens + ct / 2 - 1) / (ct / 2) * kMaxSplit <= sms)))
         ct /= 2;
     if (ct == 32) return launch_score_columns_ct<T, 32>(a, stream);
     if (ct == 16) return launch_score_columns_ct<T, 16>(a, stream);
@@ -976,12 +979,6 @@ cudaError_t launch_grad(const GradArgs &a, darb_layout_t layout, cudaStream_t st
     return launch_ex(grad_any_kernel<T, false>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
 }
 
-darb_status_t status_of(cudaError_t e) {
-    if (e == cudaSuccess) return DARB_OK;
-    cudaGetLastError();
-    return e == cudaErrorNotSupported ? DARB_ERR_UNSUPPORTED : DARB_ERR_CUDA;
-}
-
 }  // namespace
 }  // namespace darb
 
@@ -1013,8 +1010,8 @@ darb_status_t darb_token_logprobs(const void *logits, darb_dtype_t dtype, darb_l
     if (layout == DARB_TOKEN_COLUMNS && tokens == 1 && ld == 1) layout = DARB_TOKEN_ROWS;   // (a single row: ld is not used)
     const ScoreArgs a = {logits, ld, tokens, int32_t(vocab), k, targets, logprob, entropy, lse, top_logprob, top_index};
     if (layout == DARB_TOKEN_ROWS)
-        return status_of(dtype == DARB_BF16 ? launch_score_rows<__nv_bfloat16>(a, stream) : launch_score_rows<float>(a, stream));
-    return status_of(dtype == DARB_BF16 ? launch_score_columns<__nv_bfloat16>(a, stream) : launch_score_columns<float>(a, stream));
+        return enqueue([&] { return dtype == DARB_BF16 ? launch_score_rows<__nv_bfloat16>(a, stream) : launch_score_rows<float>(a, stream); });
+    return enqueue([&] { return dtype == DARB_BF16 ? launch_score_columns<__nv_bfloat16>(a, stream) : launch_score_columns<float>(a, stream); });
 }
 
 darb_status_t darb_token_logprobs_grad(const void *logits, darb_dtype_t dtype, darb_layout_t layout, int64_t tokens,
@@ -1043,7 +1040,7 @@ darb_status_t darb_token_logprobs_grad(const void *logits, darb_dtype_t dtype, d
     if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
     if (layout == DARB_TOKEN_COLUMNS && tokens == 1 && ld == 1 && ld_grad == 1) layout = DARB_TOKEN_ROWS;
     const GradArgs a = {logits, d_logits, ld, ld_grad, tokens, int32_t(vocab), targets, lse, entropy, d_logprob, d_entropy};
-    return status_of(dtype == DARB_BF16 ? launch_grad<__nv_bfloat16>(a, layout, stream) : launch_grad<float>(a, layout, stream));
+    return enqueue([&] { return dtype == DARB_BF16 ? launch_grad<__nv_bfloat16>(a, layout, stream) : launch_grad<float>(a, layout, stream); });
 }
 
 }  // extern "C"

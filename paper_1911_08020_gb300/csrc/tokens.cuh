@@ -14,6 +14,7 @@
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <new>
 
 #include "darb.h"
 
@@ -172,7 +173,25 @@ __device__ __forceinline__ uint4 pack(const Pair (&v)[4]) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// ---- host side: argument checks ----
+// ---- host side ----
+
+// The status of what `launch` returns (a cudaError_t).  No exception leaves a C
+// entry: the tables of kernel attributes can run out of host memory.
+template <typename F>
+darb_status_t enqueue(F launch) noexcept {
+    cudaError_t e;
+    try {
+        e = launch();
+    } catch (const std::bad_alloc &) {
+        return DARB_ERR_OOM;
+    } catch (...) {
+        return DARB_ERR_CUDA;
+    }
+    if (e == cudaSuccess) return DARB_OK;
+    cudaGetLastError();
+    return e == cudaErrorNotSupported ? DARB_ERR_UNSUPPORTED : DARB_ERR_CUDA;
+}
+
 inline bool token_dtype(darb_dtype_t t) { return t == DARB_F32 || t == DARB_BF16; }
 inline bool token_layout(darb_layout_t l) { return l == DARB_TOKEN_ROWS || l == DARB_TOKEN_COLUMNS; }
 inline size_t dtype_size(darb_dtype_t t) { return t == DARB_BF16 ? 2 : 4; }

@@ -262,3 +262,21 @@ def test_the_binding_refuses():
     darb.darb_adamw_destroy(plan)   # nothing left to do
     with pytest.raises(darb.DarbError):
         step(G)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+def test_a_tensor_of_more_elements_than_32_bits_count(codes):
+    n = (1 << 31) + 5000
+    tail = 1000
+    E = torch.float8_e4m3fn
+    P = torch.zeros(n, device="cuda")
+    G = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    G[-tail:] = torch.randn(tail, device="cuda").bfloat16()
+    new = (lambda: torch.zeros(n, dtype=torch.uint8, device="cuda").view(E)) if codes else (lambda: torch.zeros(n, device="cuda"))
+    scales = [[torch.zeros(-(-n // 256), device="cuda")] for _ in range(2)] if codes else []
+    with darb.darb_adamw_create([P], [new()], [new()], *scales, grad_dtype=torch.bfloat16) as plan:
+        darb.darb_adamw_step(plan, [G], 1, **HYPER)
+        torch.cuda.synchronize()
+        g, z = G[-tail:].float().cpu().numpy(), np.zeros(tail, F)
+        np.testing.assert_array_equal(P[-tail:].cpu().numpy(), step32(z, g, z, z, 1.0, 1, **HYPER)[0])
+        assert P[:-tail].count_nonzero() == 0

@@ -228,3 +228,27 @@ def test_the_binding_refuses():
         with pytest.raises(darb.DarbError) as e:
             f()
         assert e.value.status == darb.ERR_INVALID_ARG, i
+
+
+@pytest.mark.parametrize("layout", ["rows", "columns"])
+def test_tokens_further_apart_than_32_bits_count(layout):
+    n, f = (3, 800) if layout == "rows" else (40, 70)
+    ld = (1 << 31) + 24 if layout == "rows" else (1 << 26) + 3
+    lines, width = (n, f) if layout == "rows" else (f, n)
+    flat = torch.empty((lines - 1) * ld + width, dtype=torch.bfloat16, device="cuda")
+    t = flat.as_strided((lines, width), (ld, 1))
+    dim = -1 if layout == "rows" else 0
+    x = torch.randn(n, f, device="cuda").bfloat16()
+    put = x if layout == "rows" else x.t().contiguous()
+    ga = torch.randn(f, device="cuda")
+    y, mean, rstd = darb.darb_layer_norm(put, ga, dim=dim)
+    t.copy_(put)
+    _, mean2, rstd2 = darb.darb_layer_norm(t, ga, dim=dim, y=t)
+    assert torch.allclose(mean, mean2, rtol=0, atol=1e-6) and torch.allclose(rstd, rstd2, rtol=1e-5)
+    assert torch.allclose(t.float(), y.float(), rtol=2.0 ** -7, atol=1e-6)
+    dy = torch.randn(lines, width, device="cuda").bfloat16()
+    want = darb.darb_layer_norm_grad(dy, put, ga, mean, rstd, dim=dim)
+    t.copy_(dy)
+    got = darb.darb_layer_norm_grad(t, put, ga, mean, rstd, dim=dim, dx=t)
+    for a, b in zip(got, want):
+        assert torch.allclose(a.float(), b.float(), rtol=2.0 ** -7, atol=1e-4)

@@ -362,3 +362,24 @@ def test_the_binding_refuses():
         with pytest.raises(darb.DarbError) as e:
             f()
         assert e.value.status == darb.ERR_INVALID_ARG, i
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_logits_further_apart_than_32_bits_count(layout):
+    """Rows (or entries) whose offsets in elements and in bytes pass 2^32."""
+    n, v = (3, 1000) if layout == "rows" else (40, 70)
+    ld = (1 << 31) + 24 if layout == "rows" else (1 << 26) + 3
+    lines, width = (n, v) if layout == "rows" else (v, n)
+    flat = torch.empty((lines - 1) * ld + width, dtype=torch.bfloat16, device="cuda")
+    t = flat.as_strided((lines, width), (ld, 1))
+    x = torch.from_numpy(np.random.default_rng(1).standard_normal((n, v)).astype(np.float32)).cuda().bfloat16()
+    t.copy_(x if layout == "rows" else x.t())
+    dim = -1 if layout == "rows" else 0
+    tg = torch.arange(n, device="cuda")
+    want, got = darb.darb_token_logprobs(x, tg, 5), darb.darb_token_logprobs(t, tg, 5, dim=dim)
+    assert torch.equal(got.top_index, want.top_index)
+    assert torch.allclose(got.logprob, want.logprob, rtol=0, atol=1e-5) and torch.allclose(got.entropy, want.entropy, rtol=0, atol=1e-4)
+    d = torch.ones(n, device="cuda")
+    a = darb.darb_token_logprobs_grad(x, tg, want.lse, d)
+    b = darb.darb_token_logprobs_grad(t, tg, want.lse, d, dim=dim, out=t)
+    assert torch.allclose(a.float(), (b if layout == "rows" else b.t()).float(), rtol=2.0 ** -7, atol=1e-7)
