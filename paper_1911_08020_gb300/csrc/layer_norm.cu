@@ -210,12 +210,13 @@ struct Owned {
     }
 };
 
-// Threads that share a row, at most, by the granules that each has: what leaves
-// it the registers for them.
-constexpr int row_threads(int vpt) { return vpt > 2 ? 256 : 512; }
+// Threads that share a row, at most.  Kernels for rows of up to kHalfThreads
+// are held to the registers of which an SM has enough for two CTAs.
+constexpr int kRowThreads = 512, kHalfThreads = 288;
+constexpr int ctas_of(int most) { return most > kHalfThreads ? 1 : 2; }
 
-template <typename T, int VPT, int STAGES>
-__global__ void __launch_bounds__(row_threads(VPT)) norm_rows_kernel(const NormArgs a, int32_t stage_bytes) {
+template <typename T, int VPT, int STAGES, int MOST>
+__global__ void __launch_bounds__(MOST, ctas_of(MOST)) norm_rows_kernel(const NormArgs a, int32_t stage_bytes) {
     constexpr int V = kPerGranule<T>, H = V / 2;
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ __align__(16) float buf[2 * kSumWarps];
@@ -286,8 +287,9 @@ __global__ void __launch_bounds__(row_threads(VPT)) norm_rows_kernel(const NormA
     }
 }
 
-template <typename T, int VPT, int STAGES>
-__global__ void __launch_bounds__(row_threads(VPT)) back_rows_kernel(const NormArgs a, int32_t stage_bytes) {
+// SUMS: with the sums over the tokens.
+template <typename T, int VPT, int STAGES, int MOST, bool SUMS>
+__global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const NormArgs a, int32_t stage_bytes) {
     constexpr int V = kPerGranule<T>, H = V / 2;
     extern __shared__ __align__(16) unsigned char ring[];   // a stage: a row of x, a row of dy
     __shared__ __align__(16) float buf[2 * 2 * kSumWarps];
@@ -312,12 +314,14 @@ __global__ void __launch_bounds__(row_threads(VPT)) back_rows_kernel(const NormA
             if (r0 + s * stride < a.tokens) issue(r0 + s * stride, s);
     const float inv_n = __fdiv_rn(1.0f, float(n));
     const Owned<T, VPT> own = {t * V - row_head<T>(xs.base + r0 * a.ld_x), threads * V, n};
-    Pair gm[VPT][H], sg[VPT][H], sb[VPT][H];
+    Pair gm[VPT][H], sg[SUMS ? VPT : 1][H], sb[SUMS ? VPT : 1][H];
     own.gather(a.gamma, 1.0f, gm);
+    if constexpr (SUMS) {
 #pragma unroll
-    for (int u = 0; u < VPT; ++u)
+        for (int u = 0; u < VPT; ++u)
 #pragma unroll
-        for (int e = 0; e < H; ++e) sg[u][e] = sb[u][e] = both(0.0f);
+            for (int e = 0; e < H; ++e) sg[u][e] = sb[u][e] = both(0.0f);
+    }
     clear_sums(buf, 2 * 2 * kSumWarps);
     T *dx = static_cast<T *>(a.out);
     int turn = 0, stage = 0;
@@ -338,8 +342,10 @@ __global__ void __launch_bounds__(row_threads(VPT)) back_rows_kernel(const NormA
 #pragma unroll
             for (int e = 0; e < H; ++e) {
                 xh[u][e] = mul2(add2(xh[u][e], both(-mean)), both(rstd));
-                sg[u][e] = fma2(d[u][e], xh[u][e], sg[u][e]);
-                sb[u][e] = add2(sb[u][e], d[u][e]);
+                if constexpr (SUMS) {
+                    sg[u][e] = fma2(d[u][e], xh[u][e], sg[u][e]);
+                    sb[u][e] = add2(sb[u][e], d[u][e]);
+                }
                 d[u][e] = mul2(d[u][e], gm[u][e]);
                 s0 = add2(s0, d[u][e]);
                 s1 = fma2(d[u][e], xh[u][e], s1);
@@ -356,7 +362,7 @@ __global__ void __launch_bounds__(row_threads(VPT)) back_rows_kernel(const NormA
                 d[u][e] = mul2(fma2(xh[u][e], both(-c1), add2(d[u][e], both(-c0))), both(rstd));
         own.store(dx + r * a.ld_out, d);
     }
-    if (a.partial != nullptr) {
+    if (SUMS && a.partial != nullptr) {
         // as the thread holds them: feature f at f + the head of this CTA's rows
         const int64_t width = partial_width(n);
         float *p = a.partial + r0 * 2 * width;
@@ -457,11 +463,60 @@ __global__ void __launch_bounds__(kAnyThreads) back_any_kernel(const NormArgs a)
     }
 }
 
-// The sums over the tokens p, p + partials, ... of token rows, one partial
-// result a blockIdx.y; a thread a feature.  Runs before dx is written: dx may
+// The sums over the tokens p, p + partials, ... of token rows that start alike,
+// one partial result a blockIdx.y (a multiple of 8 in all): a thread a granule,
+// for rows too long to sum where dx is made.  Runs before dx is written: dx may
 // be dy.
 template <typename T>
 __global__ void __launch_bounds__(kAnyThreads) row_sums_kernel(const NormArgs a) {
+    constexpr int V = kPerGranule<T>, H = V / 2, U = 4;
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    const int32_t n = a.features;
+    const int64_t r0 = blockIdx.y, stride = gridDim.y;
+    const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
+    const int head = row_head<T>(x + r0 * a.ld_x);
+    const int32_t g = int32_t(blockIdx.x) * kAnyThreads + int32_t(threadIdx.x), f = g * V - head;
+    if (f >= n) return;
+    Pair sg[H], sb[H];
+#pragma unroll
+    for (int e = 0; e < H; ++e) sg[e] = sb[e] = both(0.0f);
+    for (int64_t r = r0; r < a.tokens; r += U * stride) {
+        uint4 qx[U], qd[U];
+        float mean[U], rstd[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = r + u * stride;
+            const bool in = at < a.tokens;
+            qx[u] = in ? load_granule(x + at * a.ld_x, f, n, 0.0f) : make_uint4(0, 0, 0, 0);
+            qd[u] = in ? load_granule(dy + at * a.ld_dy, f, n, 0.0f) : make_uint4(0, 0, 0, 0);   // 0 adds nothing
+            mean[u] = in ? __ldg(a.mean + at) : 0.0f;
+            rstd[u] = in ? __ldg(a.rstd + at) : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            Pair xv[H], d[H];
+            unpack(qx[u], xv);
+            unpack(qd[u], d);
+#pragma unroll
+            for (int e = 0; e < H; ++e) {
+                sg[e] = fma2(d[e], mul2(add2(xv[e], both(-mean[u])), both(rstd[u])), sg[e]);
+                sb[e] = add2(sb[e], d[e]);
+            }
+        }
+    }
+    float *p = a.partial + r0 * 2 * partial_width(n);
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (f + e >= 0 && f + e < n) {
+            p[f + e] = e & 1 ? high(sg[e / 2]) : low(sg[e / 2]);
+            p[partial_width(n) + f + e] = e & 1 ? high(sb[e / 2]) : low(sb[e / 2]);
+        }
+}
+
+// The same for rows that do not start alike: a thread a feature.
+template <typename T>
+__global__ void __launch_bounds__(kAnyThreads) any_sums_kernel(const NormArgs a) {
     pdl_wait_previous();
     pdl_launch_dependents();
     const int32_t f = int32_t(blockIdx.x) * kAnyThreads + int32_t(threadIdx.x), n = a.features;
@@ -476,6 +531,137 @@ __global__ void __launch_bounds__(kAnyThreads) row_sums_kernel(const NormArgs a)
     float *p = a.partial + int64_t(blockIdx.y) * 2 * partial_width(n);
     p[f] = sg;
     p[partial_width(n) + f] = sb;
+}
+
+// ---- narrow token rows ----
+//
+// Rows of at most 32 granules: LANES lanes of a warp own a row, one granule
+// each, so a warp takes 32 / LANES rows at a time; the next rows are loaded while
+// these are summed.  Rows of a lane group are a multiple of 8 apart, as above.
+constexpr int kNarrowThreads = 256;
+
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+
+template <typename T, int LANES>
+__global__ void __launch_bounds__(kNarrowThreads) norm_narrow_kernel(const NormArgs a) {
+    constexpr int V = kPerGranule<T>, H = V / 2, GROUPS = kNarrowThreads / LANES;
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    const int32_t n = a.features;
+    const float inv_n = __fdiv_rn(1.0f, float(n));
+    const int64_t stride = int64_t(gridDim.x) * GROUPS, r0 = int64_t(blockIdx.x) * GROUPS + threadIdx.x / LANES;
+    const T *x = static_cast<const T *>(a.x);
+    T *y = static_cast<T *>(a.out);
+    const Owned<T, 1> own = {int32_t(threadIdx.x % LANES) * V - row_head<T>(x + r0 * a.ld_x), 0, n};
+    Pair gm[1][H], bt[1][H];
+    own.gather(a.gamma, 1.0f, gm);
+    own.gather(a.beta, 0.0f, bt);
+    const int64_t rounds = (a.tokens - 1) / stride + 1;   // the same for all lanes of a warp
+    const auto fetch = [&](int64_t r) {
+        return r < a.tokens ? load_granule<T, false>(x + r * a.ld_x, own.f0, n, 0.0f) : make_uint4(0, 0, 0, 0);
+    };
+    uint4 next = fetch(r0);
+    int64_t r = r0;
+    for (int64_t i = 0; i < rounds; ++i, r += stride) {
+        Pair v[1][H];
+        unpack(next, v[0]);
+        if (i + 1 < rounds) next = fetch(r + stride);
+        Pair s = v[0][0];
+#pragma unroll
+        for (int e = 1; e < H; ++e) s = add2(s, v[0][e]);
+        const float mean = lanes_sum<LANES>(across(s)) * inv_n;
+#pragma unroll
+        for (int e = 0; e < H; ++e) v[0][e] = add2(v[0][e], both(-mean));
+        if (!own.whole(0)) own.clear_outside(0, v[0]);
+        s = mul2(v[0][0], v[0][0]);
+#pragma unroll
+        for (int e = 1; e < H; ++e) s = fma2(v[0][e], v[0][e], s);
+        const float rstd = inverse_root(lanes_sum<LANES>(across(s)) * inv_n + a.eps);
+        if (r < a.tokens) {
+            if (threadIdx.x % LANES == 0) {
+                if (a.mean) a.mean[r] = mean;
+                if (a.rstd) a.rstd[r] = rstd;
+            }
+#pragma unroll
+            for (int e = 0; e < H; ++e) v[0][e] = fma2(mul2(v[0][e], both(rstd)), gm[0][e], bt[0][e]);
+            own.store(y + r * a.ld_out, v);
+        }
+    }
+}
+
+template <typename T, int LANES>
+__global__ void __launch_bounds__(kNarrowThreads) back_narrow_kernel(const NormArgs a) {
+    constexpr int V = kPerGranule<T>, H = V / 2, GROUPS = kNarrowThreads / LANES;
+    __shared__ float sums[2][LANES * V];   // of the CTA's rows
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    const int32_t n = a.features;
+    const float inv_n = __fdiv_rn(1.0f, float(n));
+    const int group = threadIdx.x / LANES;
+    const int64_t stride = int64_t(gridDim.x) * GROUPS, r0 = int64_t(blockIdx.x) * GROUPS + group;
+    const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
+    T *dx = static_cast<T *>(a.out);
+    const Owned<T, 1> own = {int32_t(threadIdx.x % LANES) * V - row_head<T>(x + r0 * a.ld_x), 0, n};
+    Pair gm[1][H], sg[H], sb[H];
+    own.gather(a.gamma, 1.0f, gm);
+#pragma unroll
+    for (int e = 0; e < H; ++e) sg[e] = sb[e] = both(0.0f);
+    const int64_t rounds = (a.tokens - 1) / stride + 1;
+    uint4 nx, nd;
+    float mean_next, rstd_next;
+    const auto fetch = [&](int64_t r) {
+        const bool in = r < a.tokens;
+        nx = in ? load_granule(x + r * a.ld_x, own.f0, n, 0.0f) : make_uint4(0, 0, 0, 0);
+        nd = in ? load_granule<T, false>(dy + r * a.ld_dy, own.f0, n, 0.0f) : make_uint4(0, 0, 0, 0);   // 0 adds nothing
+        mean_next = in ? __ldg(a.mean + r) : 0.0f;
+        rstd_next = in ? __ldg(a.rstd + r) : 0.0f;
+    };
+    fetch(r0);
+    int64_t r = r0;
+    for (int64_t i = 0; i < rounds; ++i, r += stride) {
+        Pair xh[H], d[1][H], s0 = both(0.0f), s1 = both(0.0f);
+        const float mean = mean_next, rstd = rstd_next;
+        unpack(nx, xh);
+        unpack(nd, d[0]);
+        if (i + 1 < rounds) fetch(r + stride);
+#pragma unroll
+        for (int e = 0; e < H; ++e) {
+            xh[e] = mul2(add2(xh[e], both(-mean)), both(rstd));
+            sg[e] = fma2(d[0][e], xh[e], sg[e]);
+            sb[e] = add2(sb[e], d[0][e]);
+            d[0][e] = mul2(d[0][e], gm[0][e]);
+            s0 = add2(s0, d[0][e]);
+            s1 = fma2(d[0][e], xh[e], s1);
+        }
+        const float c0 = lanes_sum<LANES>(across(s0)) * inv_n, c1 = lanes_sum<LANES>(across(s1)) * inv_n;
+        if (r < a.tokens) {
+#pragma unroll
+            for (int e = 0; e < H; ++e) d[0][e] = mul2(fma2(xh[e], both(-c1), add2(d[0][e], both(-c0))), both(rstd));
+            own.store(dx + r * a.ld_out, d);
+        }
+    }
+    if (a.partial == nullptr) return;
+    // the groups' sums, one after the other: a fixed order
+    for (int i = threadIdx.x; i < 2 * LANES * V; i += kNarrowThreads) (&sums[0][0])[i] = 0.0f;
+    __syncthreads();
+    for (int k = 0; k < GROUPS; ++k) {
+        if (group == k) {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (own.in(0, e)) {
+                    sums[0][own.f0 + e] += e & 1 ? high(sg[e / 2]) : low(sg[e / 2]);
+                    sums[1][own.f0 + e] += e & 1 ? high(sb[e / 2]) : low(sb[e / 2]);
+                }
+        }
+        __syncthreads();
+    }
+    float *p = a.partial + int64_t(blockIdx.x) * 2 * partial_width(n);
+    for (int i = threadIdx.x; i < n; i += kNarrowThreads) p[i] = sums[0][i], p[partial_width(n) + i] = sums[1][i];
 }
 
 // ---- token columns ----
@@ -761,13 +947,14 @@ struct RowPlan {
     int32_t stage_bytes;
 };
 template <typename Kernel>
-RowPlan row_plan(Kernel kernel, int64_t granules, int vpt, int copies, int stages, int64_t rows) {
+RowPlan row_plan(Kernel kernel, int64_t granules, int vpt, int most, int copies, int stages, int64_t rows) {
     RowPlan p = {};
     const int64_t threads = ((granules + vpt - 1) / vpt + 31) / 32 * 32;
-    p.stage_bytes = int32_t(std::min<int64_t>(granules, int64_t(row_threads(vpt)) * vpt)) * 16 * copies;
+    if (threads > most) return p;
+    p.stage_bytes = int32_t(granules) * 16 * copies;
     const size_t smem = size_t(p.stage_bytes) * stages;
     // (the kernel's own shared memory counts against the limit that needs no asking)
-    if (threads > row_threads(vpt) || allow_smem(kernel, smem + 1024) != cudaSuccess) return p;
+    if (allow_smem(kernel, smem + 1024) != cudaSuccess) return p;
     const int64_t per_sm = per_device(reinterpret_cast<const void *>(kernel), int64_t(threads) << 32 | int64_t(smem), [&]() -> long long {
         int n = 0;
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, int(threads), smem) != cudaSuccess) {
@@ -780,6 +967,19 @@ RowPlan row_plan(Kernel kernel, int64_t granules, int vpt, int copies, int stage
     p.threads = int(threads);
     p.grid = std::min<int64_t>(std::max<int64_t>(8, per_sm * sm_count() / 8 * 8), (rows + 7) / 8 * 8);
     return p;
+}
+
+// Rows of up to 32 granules: calls f with the lanes of a row as a constant and
+// the grid; cudaErrorNotSupported for longer rows.
+template <typename F>
+cudaError_t narrow_rows(const NormArgs &a, int64_t granules, F f) {
+    if (granules > 32) return cudaErrorNotSupported;
+    const int lanes = granules > 16 ? 32 : granules > 8 ? 16 : 8;
+    const int64_t want = (a.tokens * lanes + kNarrowThreads - 1) / kNarrowThreads;
+    const dim3 grid(unsigned(std::min<int64_t>(want, 4 * int64_t(sm_count()))));
+    if (lanes == 32) return f(std::integral_constant<int, 32>(), grid);
+    if (lanes == 16) return f(std::integral_constant<int, 16>(), grid);
+    return f(std::integral_constant<int, 8>(), grid);
 }
 
 // Whether rows of `a` and `b` start alike past a 16-byte boundary.
@@ -825,17 +1025,22 @@ cudaError_t launch_norm(const NormArgs &a, darb_layout_t layout, cudaStream_t st
             return launch_ex(norm_columns_kernel<T, ct.value>, grid, dim3(kColThreads), 0, stream, split, true, a, tiles);
         });
     if (alike(a.x, a.ld_x, a.out, a.ld_out, a.tokens, sizeof(T))) {
-        constexpr int STAGES = 4;
+        // 32 features a thread
+        constexpr int VPT = sizeof(T) == 2 ? 4 : 8;
         const int64_t granules = most_granules<T>(a.x, a.ld_x, a.tokens, a.features);
-        const auto rows = [&](auto kernel, int vpt) {
-            const RowPlan p = row_plan(kernel, granules, vpt, 1, STAGES, a.tokens);
-            if (p.threads == 0) return cudaErrorNotSupported;
-            return launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * STAGES, stream, 1, true, a,
-                             p.stage_bytes);
+        cudaError_t e = narrow_rows(a, granules, [&](auto lanes, dim3 grid) {
+            return launch_ex(norm_narrow_kernel<T, lanes.value>, grid, dim3(kNarrowThreads), 0, stream, 1, true, a);
+        });
+        const auto rows = [&](auto kernel, int vpt, int most, int stages) {
+            if (e != cudaErrorNotSupported) return;
+            const RowPlan p = row_plan(kernel, granules, vpt, most, 1, stages, a.tokens);
+            if (p.threads > 0)
+                e = launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * stages, stream, 1, true, a,
+                              p.stage_bytes);
         };
-        cudaError_t e = rows(norm_rows_kernel<T, 4, STAGES>, 4);
-        if constexpr (sizeof(T) == 4)
-            if (e == cudaErrorNotSupported) e = rows(norm_rows_kernel<T, 8, STAGES>, 8);
+        rows(norm_rows_kernel<T, VPT / 2, 4, 128>, VPT / 2, 128, 4);
+        rows(norm_rows_kernel<T, VPT, 4, 256>, VPT, 256, 4);
+        rows(norm_rows_kernel<T, VPT, 3, kRowThreads>, VPT, kRowThreads, 3);
         if (e != cudaErrorNotSupported) return e;
     }
     return launch_ex(norm_any_kernel<T>, dim3(unsigned(a.tokens)), dim3(kAnyThreads), 0, stream, 1, true, a);
@@ -865,25 +1070,51 @@ cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, 
     } else {
         const bool same = alike(a.x, a.ld_x, a.out, a.ld_out, a.tokens, sizeof(T)) &&
                           alike(a.x, a.ld_x, a.dy, a.ld_dy, a.tokens, sizeof(T));
-        constexpr int STAGES = 3;
+        // 16 features a thread, whose sums it keeps; 32 where the sums are a kernel of their own
+        constexpr int VPT = sizeof(T) == 2 ? 2 : 4;
         const int64_t granules = most_granules<T>(a.x, a.ld_x, a.tokens, a.features);
-        const auto rows = [&](auto kernel, int vpt) {
-            const RowPlan p = row_plan(kernel, granules, vpt, 2, STAGES, a.tokens);
-            if (p.threads == 0) return cudaErrorNotSupported;
-            partials = p.grid;
+        const auto shifted = [&] {   // partial results as the threads of aligned granules hold them
             base = uint32_t(reinterpret_cast<uintptr_t>(a.x));
             step = uint32_t(a.ld_x * int64_t(sizeof(T)));
-            return launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * STAGES, stream, 1, true, a,
-                             p.stage_bytes);
         };
-        e = same ? rows(back_rows_kernel<T, 4, STAGES>, 4) : cudaErrorNotSupported;
-        if constexpr (sizeof(T) == 4)
-            if (same && e == cudaErrorNotSupported) e = rows(back_rows_kernel<T, 8, STAGES>, 8);
+        e = cudaErrorNotSupported;
+        if (same)
+            e = narrow_rows(a, granules, [&](auto lanes, dim3 grid) {
+                partials = grid.x;
+                return launch_ex(back_narrow_kernel<T, lanes.value>, grid, dim3(kNarrowThreads), 0, stream, 1, true, a);
+            });
+        const auto rows = [&](auto kernel, int vpt, int most, int stages) {
+            if (!same || e != cudaErrorNotSupported) return;
+            const RowPlan p = row_plan(kernel, granules, vpt, most, 2, stages, a.tokens);
+            if (p.threads == 0) return;
+            partials = p.grid;
+            shifted();
+            e = launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * stages, stream, 1, true, a,
+                          p.stage_bytes);
+        };
+        rows(back_rows_kernel<T, VPT, 3, 256, true>, VPT, 256, 3);
+        rows(back_rows_kernel<T, VPT, 3, kHalfThreads, true>, VPT, kHalfThreads, 3);
+        rows(back_rows_kernel<T, VPT, 3, kRowThreads, true>, VPT, kRowThreads, 3);
+        if (same && e == cudaErrorNotSupported) {
+            const auto kernel = back_rows_kernel<T, 2 * VPT, 2, kRowThreads, false>;
+            const RowPlan p = row_plan(kernel, granules, 2 * VPT, kRowThreads, 2, 2, a.tokens);
+            if (p.threads > 0) {
+                e = cudaSuccess;
+                if (a.partial != nullptr) {
+                    const int64_t tiles = (granules + kAnyThreads - 1) / kAnyThreads;
+                    partials = std::min((a.tokens + 7) / 8 * 8, std::max<int64_t>(8, 6 * int64_t(sm_count()) / tiles / 8 * 8));
+                    e = launch_ex(row_sums_kernel<T>, dim3(unsigned(tiles), unsigned(partials)), dim3(kAnyThreads), 0, stream, 1, true, a);
+                }
+                if (e == cudaSuccess)
+                    e = launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * 2, stream, 1, true, a,
+                                  p.stage_bytes);
+            }
+        }
         if (e == cudaErrorNotSupported) {
             e = cudaSuccess;
             if (a.partial != nullptr) {
                 partials = std::min<int64_t>(a.tokens, std::min<int64_t>(64, most_partials(layout, a.steps, a.tokens)));
-                e = launch_ex(row_sums_kernel<T>, dim3(unsigned((a.features + kAnyThreads - 1) / kAnyThreads), unsigned(partials)),
+                e = launch_ex(any_sums_kernel<T>, dim3(unsigned((a.features + kAnyThreads - 1) / kAnyThreads), unsigned(partials)),
                               dim3(kAnyThreads), 0, stream, 1, true, a);
             }
             if (e == cudaSuccess)
