@@ -153,6 +153,7 @@ struct Owned {
     int32_t step, n;
     __device__ __forceinline__ int32_t feature(int u) const { return f0 + u * step; }
     __device__ __forceinline__ bool whole(int u) const { return feature(u) >= 0 && feature(u) + V <= n; }
+    __device__ __forceinline__ bool partial(int u) const { return !whole(u) && feature(u) < n; }   // (else: past the row)
     __device__ __forceinline__ bool in(int u, int e) const { return feature(u) + e >= 0 && feature(u) + e < n; }
 
     // The granules of a row as pairs, 0 outside the row.  `stage`: this thread's
@@ -164,8 +165,8 @@ struct Owned {
         for (int u = 0; u < VPT; ++u) {
             if (whole(u)) {
                 unpack(*reinterpret_cast<const uint4 *>(stage + u * step * int(sizeof(T))), v[u]);
-            } else if (feature(u) < n && inner) {
-                unpack(*reinterpret_cast<const uint4 *>(stage + u * step * int(sizeof(T))), v[u]);
+            } else if (inner || !partial(u)) {
+                if (partial(u)) unpack(*reinterpret_cast<const uint4 *>(stage + u * step * int(sizeof(T))), v[u]);
                 clear_outside(u, v[u]);
             } else {
                 unpack(load_granule<T, false>(rows.base + r * rows.ld, feature(u), n, 0.0f), v[u]);
@@ -174,6 +175,11 @@ struct Owned {
         if (!arrived) v[0][0] = both(__uint_as_float(0x7FC00000u));   // a copy that never came: the row is NaN
     }
     __device__ __forceinline__ void clear_outside(int u, Pair (&v)[V / 2]) const {
+        if (!partial(u)) {
+#pragma unroll
+            for (int e = 0; e < V / 2; ++e) v[e] = both(0.0f);
+            return;
+        }
 #pragma unroll
         for (int e = 0; e < V; e += 2) v[e / 2] = pair(in(u, e) ? low(v[e / 2]) : 0.0f, in(u, e + 1) ? high(v[e / 2]) : 0.0f);
     }
@@ -182,7 +188,7 @@ struct Owned {
         for (int u = 0; u < VPT; ++u) {
             if (whole(u)) {
                 *reinterpret_cast<uint4 *>(row + feature(u)) = pack(v[u]);
-            } else {
+            } else if (partial(u)) {
                 float w[V];
 #pragma unroll
                 for (int e = 0; e < V; e += 2) w[e] = low(v[u][e / 2]), w[e + 1] = high(v[u][e / 2]);
