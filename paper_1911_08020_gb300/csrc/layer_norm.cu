@@ -1044,8 +1044,8 @@ cudaError_t launch_norm(const NormArgs &a, darb_layout_t layout, cudaStream_t st
                 e = launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * stages, stream, 1, true, a,
                               p.stage_bytes);
         };
-        rows(norm_rows_kernel<T, VPT / 2, 4, 128>, VPT / 2, 128, 4);
-        rows(norm_rows_kernel<T, VPT, 4, 256>, VPT, 256, 4);
+        rows(norm_rows_kernel<T, VPT / 2, 3, 128>, VPT / 2, 128, 3);
+        rows(norm_rows_kernel<T, VPT, 3, 256>, VPT, 256, 3);
         rows(norm_rows_kernel<T, VPT, 3, kRowThreads>, VPT, kRowThreads, 3);
         if (e != cudaErrorNotSupported) return e;
     }
