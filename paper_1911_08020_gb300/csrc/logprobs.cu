@@ -520,6 +520,7 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
 // rows of its part of the vocabulary.
 constexpr int kColThreads = 1024;
 constexpr int kColCandidates = 256;   // a column (k = 32: some 130)
+static_assert(kColCandidates >= kMaxSplit * kMaxTop, "what a cluster hands on");
 constexpr int kColUnroll = 8;
 constexpr int kColSlots = 16;         // of the table of maxima, at most
 static_assert(kColSlots * kColThreads <= 65536, "a block's place fits an item");
@@ -530,6 +531,7 @@ struct ColShared {
     static constexpr int kSlots = kColThreads / CT;
     Part part[kSlots][CT + 1];
     Part col[CT];
+    float top[CT][32];          // maxima of 32 disjoint sets of a column's logits
     float bar[CT];
     uint32_t ncand[CT];
     uint64_t cand[CT][kColCandidates];
@@ -608,7 +610,7 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
     if (in_block > 0) sh.block_max[block++][tid] = __float2bfloat16_ru(slot_max);
     sh.part[slot][col] = {sum.m, across(sum.s), across(sum.t)};
     __syncthreads();
-    // warp c joins column c (c < CT <= 32 warps), and finds the bar of its k largest
+    // warp c joins column c (c < CT <= 32 warps)
     if (warp < CT) {
         Part p = empty_part();
         float g = kMasked;
@@ -621,13 +623,25 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
         }
         p = warp_join(p);
         if (lane == 0) sh.col[warp] = p;
+        sh.top[warp][lane] = g;
+    }
+    // The bar of a column is that of all CTAs of the cluster: few logits reach it.
+    if (split > 1) cluster.sync();
+    else __syncthreads();
+    Part whole = empty_part();   // of the column, in rank 0's warp of it
+    if (warp < CT) {
+        if (rank == 0 && lane < split) whole = cluster.map_shared_rank(&sh, lane)->col[warp];
         if (k > 0) {
+            float g = kMasked;
+#pragma unroll
+            for (int q = 0; q < kMaxSplit; ++q)
+                if (q < split) g = max_nan(g, cluster.map_shared_rank(&sh, q)->top[warp][lane]);
             const float bar = kth_of_warp(g, k);
             if (lane == 0) sh.bar[warp] = bar > kMasked ? bar : __uint_as_float(0x7FC00000u);
         }
     }
-    __syncthreads();
     if (k > 0) {
+        __syncthreads();
         const float bar = sh.bar[col];   // NaN: the maxima say nothing
         if (in && sum.m >= bar)
             for (int i = 0; i < block; ++i)
@@ -671,23 +685,44 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
                 if (tid == 0) sh.ncand[c] = kMaxTop;   // all have asked: select_any has barriers
             }
         __syncthreads();
-        if (warp < CT) warp_sort(sh.cand[warp], int(sh.ncand[warp]), k, sh.sorted[warp]);
+        // a CTA of a cluster hands on at most kMaxTop candidates of a column
+        if (warp < CT && (split == 1 || sh.ncand[warp] > kMaxTop)) {
+            warp_sort(sh.cand[warp], int(sh.ncand[warp]), k, sh.sorted[warp]);
+            if (split > 1) {
+                sh.cand[warp][lane] = sh.sorted[warp][lane];
+                if (lane == 0) sh.ncand[warp] = kMaxTop;
+            }
+        }
     }
     if (split > 1) {
         cluster.sync();
-        Part p = empty_part();
-        if (rank == 0 && warp < CT) {
-            if (lane < split) p = cluster.map_shared_rank(&sh, lane)->col[warp];
-            for (int i = lane; i < split * k; i += 32)
-                sh.cand[warp][i] = cluster.map_shared_rank(&sh, i / k)->sorted[warp][i % k];
+        uint64_t keys[kMaxSplit];
+        uint32_t from[kMaxSplit], total = 0;
+        if (rank == 0 && warp < CT && k > 0) {
+            uint32_t n_q[kMaxSplit];
+#pragma unroll
+            for (int q = 0; q < kMaxSplit; ++q) {
+                n_q[q] = q < split ? cluster.map_shared_rank(&sh, q)->ncand[warp] : 0;
+                keys[q] = q < split ? cluster.map_shared_rank(&sh, q)->cand[warp][lane] : 0;
+            }
+#pragma unroll
+            for (int q = 0; q < kMaxSplit; ++q) {
+                from[q] = uint32_t(lane) < n_q[q] ? total + lane : 0xFFFFFFFFu;
+                total += n_q[q];
+            }
         }
-        cluster.sync();   // the other CTAs may leave
+        cluster.sync();   // the other CTAs may leave, and the lists be written
         if (rank != 0) return;
         if (warp < CT) {
-            p = warp_join(p);
-            if (lane == 0) sh.col[warp] = p;
-            __syncwarp();
-            if (k > 0) warp_sort(sh.cand[warp], split * k, k, sh.sorted[warp]);
+            whole = warp_join(whole);
+            if (lane == 0) sh.col[warp] = whole;
+            if (k > 0) {
+#pragma unroll
+                for (int q = 0; q < kMaxSplit; ++q)
+                    if (from[q] != 0xFFFFFFFFu) sh.cand[warp][from[q]] = keys[q];
+                __syncwarp();
+                warp_sort(sh.cand[warp], int(total), k, sh.sorted[warp]);
+            }
         }
     }
     __syncthreads();
@@ -747,12 +782,13 @@ cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream) {
 template <typename T, int CT>
 cudaError_t launch_score_columns_ct(const ScoreArgs &a, cudaStream_t stream) {
     const int64_t tiles = (a.tokens + CT - 1) / CT;
-    // the candidates of every CTA of a cluster have to fit a column's list
-    const int most = a.k > 0 ? std::max(1, kColCandidates / a.k) : kMaxSplit;
+    // a CTA takes an SM: the split whose CTAs fill their waves best, the smaller of
+    // equals (1011 columns of 25568 bf16, 32 tiles: 4 CTAs a tile in one wave, not 8 in two)
     const int sms = sm_count();
     int split = 1;
-    while (split < kMaxSplit && 2 * split <= most && tiles * split < sms && a.vocab / (2 * split) >= 4 * kColThreads / CT)
-        split *= 2;
+    const auto cost = [&](int s) { return double((tiles * s + sms - 1) / sms) / s; };
+    for (int s = 2; s <= kMaxSplit; s *= 2)
+        if (a.vocab / s >= 4 * kColThreads / CT && cost(s) < 0.95 * cost(split)) split = s;
     const int64_t rows = a.vocab / split + 1;   // of a CTA, at most
     constexpr int per_round = kColThreads / CT * kColUnroll;
     const Blocks blocks = blocks_of((rows + per_round - 1) / per_round, kColSlots);
