@@ -44,8 +44,9 @@ namespace {
 constexpr float kMasked = -0x1p15f;   // logits are read as at least this (exact in bf16)
 constexpr float kWide = 0x1p14f;      // the largest logit of a token that takes the fast path, in magnitude
 constexpr int kMaxTop = DARB_MAX_TOP;
-constexpr int kCandidates = 256;    // candidates for the k largest that are gathered at once
+constexpr int kCandidates = 256;    // candidates for the k largest that are gathered at once (k = 32: some 130)
 constexpr int kMaxSplit = 8;        // CTAs that share a token
+static_assert(kCandidates >= kMaxSplit * kMaxTop, "what a cluster hands on");
 
 struct ScoreArgs {
     const void *x;
@@ -343,20 +344,20 @@ constexpr int kRowSlots = 32;   // of the table of maxima, at most
 
 constexpr int kItems = 256;   // blocks that may hold one of the k largest, at most
 
-template <typename T, int THREADS, int U>
+template <typename T, int THREADS, int U, bool CLUSTER>
 __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, const Blocks blocks) {
     constexpr int V = kPerGranule<T>;
     constexpr int W = THREADS / 32;
     extern __shared__ float block_max[];   // [slots][THREADS], for k > 0
-    __shared__ Part warp_part[W], cta_part;
-    __shared__ float thread_max[THREADS], s_bar;
+    __shared__ Part warp_part[W], cta_part, token_part;
+    __shared__ float thread_max[THREADS], s_top[32], s_bar;
     __shared__ uint64_t cand[kCandidates], sel[kMaxTop], sorted[kMaxTop];
     __shared__ uint32_t items[kItems], hist[256], ctl[4], nitems, ncand;
     __shared__ float buf[33];
     pdl_wait_previous();
     pdl_launch_dependents();
     cg::cluster_group cluster = cg::this_cluster();
-    const int split = int(cluster.num_blocks()), rank = int(cluster.block_rank());
+    const int split = CLUSTER ? int(cluster.num_blocks()) : 1, rank = CLUSTER ? int(cluster.block_rank()) : 0;
     const int64_t token = blockIdx.x / split;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const T *row = static_cast<const T *>(a.x) + token * a.ld;
@@ -427,21 +428,37 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
     const Part mine = warp_join({sum.m, across(sum.s), across(sum.t)});
     if (lane == 0) warp_part[warp] = mine;
     __syncthreads();
-    Part all;   // of the CTA; warp 0 has it
+    // Warp 0 joins the sums; warp 1 finds the bar: the k-th largest of 32 maxima
+    // over disjoint sets of the token's logits is at most the k-th largest logit, so
+    // only blocks that reach it can hold one of the k largest.
+    Part all = empty_part();
+    float g = kMasked;
     if (warp == 0) {
         all = warp_join(lane < W ? warp_part[lane] : empty_part());
-        if (lane == 0) cta_part = all;
+        if (lane == 0) (CLUSTER ? cta_part : token_part) = all;
     } else if (warp == 1 && k > 0) {
-        // The k-th largest of 32 maxima over disjoint sets of logits is at most the
-        // k-th largest logit, so only blocks that reach it can hold one of the k largest.
-        float g = thread_max[lane];
+        g = thread_max[lane];
 #pragma unroll
         for (int w = 1; w < W; ++w) g = max_nan(g, thread_max[w * 32 + lane]);
+        if (CLUSTER) s_top[lane] = g;
+    }
+    if (CLUSTER) {
+        cluster.sync();
+        if (warp == 0 && rank == 0) {
+            all = warp_join(lane < split ? *cluster.map_shared_rank(&cta_part, lane) : empty_part());
+            if (lane == 0) token_part = all;
+        } else if (warp == 1 && k > 0) {
+#pragma unroll
+            for (int q = 0; q < kMaxSplit; ++q)
+                if (q < split) g = max_nan(g, cluster.map_shared_rank(s_top, q)[lane]);
+        }
+    }
+    if (warp == 1 && k > 0) {
         const float bar = kth_of_warp(g, k);
         if (lane == 0) s_bar = bar > kMasked ? bar : __uint_as_float(0x7FC00000u);
     }
+    __syncthreads();
     if (k > 0) {
-        __syncthreads();
         const float bar = s_bar;   // NaN: the maxima say nothing
         if (sum.m >= bar)
             for (int i = 0; i < slot; ++i)
@@ -450,17 +467,16 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
                     if (p < kItems) items[p] = uint32_t(i * THREADS + tid);
                 }
         __syncthreads();
-        int found = int(nitems);
-        const bool listed = bar == bar && found <= kItems;
-        if (listed) {
+        const int listed = int(nitems);
+        if (listed <= kItems) {
             // the granules of the listed blocks, all at once
             const int per = U * blocks.per_slot;
-            for (int i = tid; i < found * per; i += THREADS) {
+            for (int i = tid; i < listed * per; i += THREADS) {
                 const int32_t item = int32_t(items[i / per]), j = i % per;
-                const int32_t g = g0 + ((item / THREADS) * blocks.per_slot + j / U) * (THREADS * U) + (j % U) * THREADS + item % THREADS;
-                if (g >= g1) continue;
+                const int32_t gi = g0 + ((item / THREADS) * blocks.per_slot + j / U) * (THREADS * U) + (j % U) * THREADS + item % THREADS;
+                if (gi >= g1) continue;
                 float v[V];
-                const int64_t j0 = int64_t(g) * V - head;
+                const int64_t j0 = int64_t(gi) * V - head;
                 unpack(load_granule(row, j0, n, -INFINITY), v);
 #pragma unroll
                 for (int e = 0; e < V; ++e)
@@ -469,38 +485,58 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
                         if (p < kCandidates) cand[p] = key_of(v[e], int32_t(j0 + e));
                     }
             }
-            __syncthreads();
-            found = int(ncand);
         }
-        if (!listed || found > kCandidates) {
+        __syncthreads();
+        int found = int(ncand);
+        if (!(bar == bar) || listed > kItems || found > kCandidates) {
             const int32_t i0 = max(0, g0 * V - head), i1 = min(n, g1 * V - head);
             select_any(row, 1, i0, i1, k, sel, hist, ctl);
             if (tid < kMaxTop) cand[tid] = sel[tid];
             found = kMaxTop;
+            if (tid == 0) ncand = found;
             __syncthreads();
         }
-        if (warp == 0) warp_sort(cand, found, k, sorted);
-    }
-    if (split > 1) {
-        cluster.sync();
-        if (rank == 0) {
-            if (warp == 0) {
-                all = empty_part();
-                if (lane < split) all = *cluster.map_shared_rank(&cta_part, lane);
-                all = warp_join(all);
+        if (CLUSTER) {
+            // a CTA hands on at most kMaxTop candidates
+            if (warp == 0 && found > kMaxTop) {
+                warp_sort(cand, found, k, sorted);
+                cand[lane] = sorted[lane];
+                if (lane == 0) ncand = kMaxTop;
             }
-            for (int i = tid; i < split * k; i += THREADS) cand[i] = cluster.map_shared_rank(sorted, i / k)[i % k];
+            cluster.sync();
+            uint64_t keys[kMaxSplit];
+            uint32_t from[kMaxSplit], total = 0;
+            if (rank == 0 && warp == 0) {
+                uint32_t n_q[kMaxSplit];
+#pragma unroll
+                for (int q = 0; q < kMaxSplit; ++q) {
+                    n_q[q] = q < split ? *cluster.map_shared_rank(&ncand, q) : 0;
+                    keys[q] = q < split ? cluster.map_shared_rank(cand, q)[lane] : 0;
+                }
+#pragma unroll
+                for (int q = 0; q < kMaxSplit; ++q) {
+                    from[q] = uint32_t(lane) < n_q[q] ? total + lane : 0xFFFFFFFFu;
+                    total += n_q[q];
+                }
+            }
+            cluster.sync();   // the other CTAs may leave, and the lists be written
+            if (rank == 0 && warp == 0) {
+#pragma unroll
+                for (int q = 0; q < kMaxSplit; ++q)
+                    if (from[q] != 0xFFFFFFFFu) cand[from[q]] = keys[q];
+                __syncwarp();
+                found = int(total);
+            }
         }
-        cluster.sync();   // the other CTAs may leave: nothing reads them any more
-        if (rank != 0) return;
-        if (warp == 0 && lane == 0) cta_part = all;
-        __syncthreads();
-        if (warp == 0 && k > 0) warp_sort(cand, split * k, k, sorted);
+        if (warp == 0 && rank == 0) warp_sort(cand, found, k, sorted);
+    } else if (CLUSTER) {
+        cluster.sync();   // the sums have been read
     }
-    __syncthreads();
-    const Part whole = cta_part;
+    if (rank != 0) return;
+    const Part whole = token_part;
     Token tok;
-    if (is_wide(whole.m)) tok = wide_token(row, 1, n, buf);
+    if (is_wide(whole.m)) tok = wide_token(row, 1, n, buf);   // the same for the CTA
+    else if (warp > 0) return;
     else tok = token_of(whole);
     if (tid == 0) {
         if (a.logprob) a.logprob[token] = target_logprob(tok, target, n, target_x);
@@ -520,7 +556,7 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
 // rows of its part of the vocabulary.
 constexpr int kColThreads = 1024;
 constexpr int kColCandidates = 256;   // a column (k = 32: some 130)
-static_assert(kColCandidates >= kMaxSplit * kMaxTop, "what a cluster hands on");
+static_assert(kColCandidates >= kMaxSplit * kMaxTop, "as above");
 constexpr int kColUnroll = 8;
 constexpr int kColSlots = 16;         // of the table of maxima, at most
 static_assert(kColSlots * kColThreads <= 65536, "a block's place fits an item");
@@ -754,29 +790,32 @@ __global__ void __launch_bounds__(kColThreads) score_columns_kernel(const ScoreA
     }
 }
 
-template <typename T, int THREADS>
+template <typename T, int THREADS, bool CLUSTER>
 cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream, int split) {
     constexpr int U = 4;
+    const auto kernel = score_rows_kernel<T, THREADS, U, CLUSTER>;
     const int64_t granules = row_granules<T>(kPerGranule<T> - 1, a.vocab) / split + 1;   // of a CTA, at most
     const Blocks blocks = blocks_of((granules + THREADS * U - 1) / (THREADS * U), kRowSlots);
     const size_t smem = a.k > 0 ? size_t(blocks.slots) * THREADS * 4 : 0;
-    const cudaError_t e = allow_smem(score_rows_kernel<T, THREADS, U>, smem);
+    const cudaError_t e = allow_smem(kernel, smem + 8 * 1024);   // (and the kernel's own)
     if (e != cudaSuccess) return e;
-    return launch_ex(score_rows_kernel<T, THREADS, U>, dim3(unsigned(a.tokens * split)), dim3(THREADS), smem, stream,
-                     unsigned(split), true, a, blocks);
+    return launch_ex(kernel, dim3(unsigned(a.tokens * split)), dim3(THREADS), smem, stream, unsigned(split), true, a, blocks);
 }
 
 template <typename T>
 cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream) {
     const int sms = sm_count();
+    // Rows of up to 128 KB on CTAs of 128 threads, so that fewer warps wait while a
+    // token's sums are joined (4096 x 32000 bf16: 52 us, with 256 threads 63); longer
+    // ones need the loads of 256 (1023 x 128001 fp32: 88, with 128 threads 137).
     const bool short_rows = row_granules<T>(0, a.vocab) <= 8192;
-    if (a.tokens >= 4 * sms && short_rows) return launch_score_rows<T, 128>(a, stream, 1);
+    if (a.tokens >= 4 * sms && short_rows) return launch_score_rows<T, 128, false>(a, stream, 1);
     // CTAs for every SM, while a thread keeps two granules (a vocabulary of 32000 in
     // bf16: one token 6.0 us, with one granule 6.4, with four 6.5; 50 tokens of 31856
     // in fp32 on 200 CTAs 9.4, on 400 11.8)
     int split = 1;
     while (split < kMaxSplit && a.tokens * split < sms && a.vocab / (2 * split) >= 2 * 256 * kPerGranule<T>) split *= 2;
-    return launch_score_rows<T, 256>(a, stream, split);
+    return split > 1 ? launch_score_rows<T, 256, true>(a, stream, split) : launch_score_rows<T, 256, false>(a, stream, 1);
 }
 
 template <typename T, int CT>

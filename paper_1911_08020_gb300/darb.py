@@ -592,7 +592,7 @@ def darb_layer_norm_grad(dy, x, gamma, mean, rstd, dim: int = -1, dx=None, dgamm
         if dbeta is None:
             dbeta = _new((f,), f32, x.device, stream)
         pg, pb = _vector(dgamma, f, f32, call, "dgamma"), _vector(dbeta, f, f32, call, "dbeta")
-        need = _work_bytes(layout, steps, n, f, _torch.cuda.current_device())
+        need = _work_bytes(layout, steps, n, f, x.get_device())
         if work is None:
             work = _new((need,), _torch.uint8, x.device, stream)
         elif not work.is_cuda or not work.is_contiguous() or work.numel() * work.element_size() < need:
