@@ -27,9 +27,9 @@
  *    two destroy calls synchronise; the others are asynchronous.
  *    darb_spmm allocates nothing; the step calls on large matrices or batches
  *    use scratch owned by the handle (darb_rnn_reserve sizes it up front).
- *  - Only two opt-in calls take scratch from the device's stream-ordered
- *    memory pool: darb_spmm_ex with DARB_PATH_TENSOR_CORES and the sequence
- *    calls.  They return it to the pool on the same stream.  The first such
+ *  - Only these calls take scratch from the device's stream-ordered memory
+ *    pool: darb_spmm_ex with DARB_PATH_TENSOR_CORES, the sequence calls, and
+ *    darb_layer_norm_grad where it is given none.  They return it to the pool on the same stream.  The first such
  *    call on a device raises the release threshold of the device's current
  *    pool to 1 GiB if it is lower, so that freed scratch stays mapped across
  *    synchronisations; darb_spmm never touches the pool.
@@ -468,9 +468,11 @@ DARB_API darb_status_t darb_layer_norm(const void *x, darb_dtype_t dtype, darb_l
  *   dgamma, dbeta  device fp32[features], overwritten (with zeros when there
  *            are no tokens); both NULL: not wanted
  *   work     device scratch of darb_layer_norm_grad_work bytes, 16-byte aligned, the
- *            caller's; not used (NULL allowed) when dgamma and dbeta are NULL
+ *            caller's; NULL: taken from the device's stream-ordered memory pool for
+ *            the duration of the call.  Not used when dgamma and dbeta are NULL
  * The sums over the tokens are fp32, in an order fixed by the sizes and alignments.
- * Asynchronous on `stream`; allocates nothing.  Errors: as darb_layer_norm.
+ * Asynchronous on `stream`; allocates nothing else.  Errors: as darb_layer_norm,
+ * and DARB_ERR_OOM if the pool cannot supply the scratch.
  */
 DARB_API darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x,
                                             darb_dtype_t dtype, darb_layout_t layout, int64_t steps, int64_t tokens,

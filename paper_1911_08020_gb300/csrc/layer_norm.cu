@@ -42,6 +42,7 @@ namespace cg = cooperative_groups;
 namespace darb {
 
 int sm_count();
+cudaError_t stream_alloc(void **p, size_t bytes, cudaStream_t stream);
 
 namespace {
 
@@ -1230,7 +1231,7 @@ darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x,
     if (dy == nullptr || x == nullptr || dx == nullptr || mean == nullptr || rstd == nullptr || !aligned_to(dy, es) ||
         !aligned_to(x, es) || !aligned_to(dx, es) || !aligned_to(gamma, 4) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
         return DARB_ERR_INVALID_ARG;
-    if (dgamma != nullptr && (work == nullptr || !aligned_to(work, 16))) return DARB_ERR_INVALID_ARG;
+    if (dgamma != nullptr && !aligned_to(work, 16)) return DARB_ERR_INVALID_ARG;
     const int64_t nd = token_span(layout, steps, tokens, features, ld_dy), nx = token_span(layout, steps, tokens, features, ld_x),
                   no = token_span(layout, steps, tokens, features, ld_dx);
     if (nd < 0 || nx < 0 || no < 0) return DARB_ERR_UNSUPPORTED;
@@ -1250,9 +1251,20 @@ darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x,
     a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
     a.partial = dgamma ? static_cast<float *>(work) : nullptr;
     if (is_rows(layout, tokens, ld_x, ld_dy, ld_dx)) as_rows(a, layout);
+    const bool borrow = dgamma != nullptr && work == nullptr;
     return enqueue([&] {
-        return dtype == DARB_BF16 ? launch_back<__nv_bfloat16>(a, layout, dgamma, dbeta, stream)
-                                  : launch_back<float>(a, layout, dgamma, dbeta, stream);
+        cudaError_t e = cudaSuccess;
+        if (borrow) {
+            e = stream_alloc(reinterpret_cast<void **>(&a.partial), size_t(scratch), stream);
+            if (e != cudaSuccess) return e;
+        }
+        e = dtype == DARB_BF16 ? launch_back<__nv_bfloat16>(a, layout, dgamma, dbeta, stream)
+                               : launch_back<float>(a, layout, dgamma, dbeta, stream);
+        if (borrow) {
+            const cudaError_t f = cudaFreeAsync(a.partial, stream);
+            if (e == cudaSuccess) e = f;
+        }
+        return e;
     });
 }
 

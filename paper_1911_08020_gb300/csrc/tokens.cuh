@@ -189,6 +189,7 @@ darb_status_t enqueue(F launch) noexcept {
     }
     if (e == cudaSuccess) return DARB_OK;
     cudaGetLastError();
+    if (e == cudaErrorMemoryAllocation) return DARB_ERR_OOM;
     return e == cudaErrorNotSupported ? DARB_ERR_UNSUPPORTED : DARB_ERR_CUDA;
 }
 

@@ -8,7 +8,6 @@ the library's CUDA kernels; if ``libdarb.so`` is missing or a call fails, a
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 import threading
 from dataclasses import dataclass
@@ -578,7 +577,8 @@ def _new_like(x, dim: int, layout: int, steps: int, n: int, f: int, stream):
 def darb_layer_norm_grad(dy, x, gamma, mean, rstd, dim: int = -1, dx=None, dgamma=None, dbeta=None, weights: bool = True,
                          work=None, stream=None):
     """(dx, dgamma, dbeta): the backward pass of darb_layer_norm (dx may be dy).  weights=False leaves
-    dgamma and dbeta out (None).  work: scratch of darb_layer_norm_grad_work bytes, a new one if None."""
+    dgamma and dbeta out (None).  work: scratch of darb_layer_norm_grad_work bytes; from the
+    device's memory pool if None."""
     call = "darb_layer_norm_grad"
     code = _value_code(x, call, "x")
     layout, steps, n, f, ld = _tokens(x, dim, call, "x")
@@ -592,12 +592,11 @@ def darb_layer_norm_grad(dy, x, gamma, mean, rstd, dim: int = -1, dx=None, dgamm
         if dbeta is None:
             dbeta = _new((f,), f32, x.device, stream)
         pg, pb = _vector(dgamma, f, f32, call, "dgamma"), _vector(dbeta, f, f32, call, "dbeta")
-        need = _work_bytes(layout, steps, n, f, x.get_device())
-        if work is None:
-            work = _new((need,), _torch.uint8, x.device, stream)
-        elif not work.is_cuda or not work.is_contiguous() or work.numel() * work.element_size() < need:
-            _refuse(call, f"work must be a contiguous CUDA tensor of {need} bytes")
-        pw = work.data_ptr()
+        if work is not None:
+            need = darb_layer_norm_grad_work(layout, steps, n, f)
+            if not work.is_cuda or not work.is_contiguous() or work.numel() * work.element_size() < need:
+                _refuse(call, f"work must be a contiguous CUDA tensor of {need} bytes")
+            pw = work.data_ptr()
     else:
         dgamma = dbeta = None
     _check(lib().darb_layer_norm_grad(dy.data_ptr(), _same_tokens(dy, x, ld, dim, layout, call, "dy"), x.data_ptr(), ld, code,
@@ -614,11 +613,6 @@ def darb_layer_norm_grad_work(layout: int, steps: int, tokens: int, features: in
     _check(lib().darb_layer_norm_grad_work(layout, steps, tokens, features, ctypes.byref(need)),
            "darb_layer_norm_grad_work")
     return need.value
-
-
-@functools.lru_cache(maxsize=1024)
-def _work_bytes(layout: int, steps: int, tokens: int, features: int, device: int) -> int:
-    return darb_layer_norm_grad_work(layout, steps, tokens, features)
 
 
 class AdamW:

@@ -208,6 +208,9 @@ def test_no_tokens_no_weights_and_repeats():
     b = darb.darb_layer_norm_grad(dy, x, None, mean, rstd, stream=s)
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(a, b))
+    need = darb.darb_layer_norm_grad_work(darb.TOKEN_ROWS, 1, 999, 777)
+    own = darb.darb_layer_norm_grad(dy, x, None, mean, rstd, work=torch.empty(need, dtype=torch.uint8, device="cuda"))
+    assert all(torch.equal(p, q) for p, q in zip(a, own))          # scratch of the caller's, or of the pool
     c = darb.darb_layer_norm_grad(dy, x, None, mean, rstd, weights=False)
     assert torch.equal(c[0], a[0]) and c[1] is None and c[2] is None
 
@@ -252,3 +255,31 @@ def test_tokens_further_apart_than_32_bits_count(layout):
     got = darb.darb_layer_norm_grad(t, put, ga, mean, rstd, dim=dim, dx=t)
     for a, b in zip(got, want):
         assert torch.allclose(a.float(), b.float(), rtol=2.0 ** -7, atol=1e-4)
+
+
+def test_a_pool_without_room_is_reported(monkeypatch):
+    x = torch.randn(64, 256, device="cuda")
+    y, mean, rstd = darb.darb_layer_norm(x)
+    monkeypatch.setenv("DARB_TEST_POOL_LIMIT", "1000")
+    with pytest.raises(darb.DarbError) as e:
+        darb.darb_layer_norm_grad(y, x, None, mean, rstd)
+    assert e.value.status == darb.ERR_OOM
+    darb.darb_layer_norm_grad(y, x, None, mean, rstd, weights=False)   # needs none
+    torch.cuda.synchronize()
+
+
+def test_captured_in_a_graph():
+    x, dy = torch.randn(3, 70, 20, device="cuda"), torch.randn(3, 70, 20, device="cuda")
+    ga = torch.randn(70, device="cuda")
+    want = darb.darb_layer_norm(x, ga, dim=1)
+    back = darb.darb_layer_norm_grad(dy, x, ga, want[1], want[2], dim=1)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        got = darb.darb_layer_norm(x, ga, dim=1)
+        got_back = darb.darb_layer_norm_grad(dy, x, ga, got[1], got[2], dim=1)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(want + back, got + got_back))

@@ -79,7 +79,7 @@ def test_layer_norm_grad_refusals(L):
         return L.darb_layer_norm_grad(a["dy"], a["ldd"], a["x"], a["ld"], a["dt"], a["lay"], a["s"], a["n"], a["f"], a["g"], a["mean"],
                                       a["rstd"], a["dx"], a["ldo"], a["dg"], a["db"], a["work"], None)
 
-    for kw in (dict(dy=None), dict(x=None), dict(dx=None), dict(mean=None), dict(rstd=None), dict(dg=None), dict(db=None), dict(work=None),
+    for kw in (dict(dy=None), dict(x=None), dict(dx=None), dict(mean=None), dict(rstd=None), dict(dg=None), dict(db=None),
                dict(work=W + 4), dict(dx=Y), dict(dx=X, ldo=101), dict(dg=6 << 20), dict(dg=X), dict(work=X), dict(ldd=99), dict(ldo=99),
                dict(f=-1), dict(s=0x7FFFFFFF)):
         assert call(**kw) == INVALID, kw
