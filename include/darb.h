@@ -23,8 +23,9 @@
  *  - The caller owns every buffer it passes; a handle owns the encoded matrix
  *    and any scratch it allocates, and releases both in darb_destroy.
  *  - Work is enqueued on the caller's stream.  Only darb_encode, darb_import,
- *    darb_export, darb_sync_status, darb_rnn_reserve, darb_adamw_create and the
- *    two destroy calls synchronise; the others are asynchronous.
+ *    darb_export, darb_sync_status, darb_rnn_reserve, darb_adamw_create,
+ *    darb_adamw_sync_status and the two destroy calls synchronise; the others are
+ *    asynchronous.
  *    darb_spmm allocates nothing; the step calls on large matrices or batches
  *    use scratch owned by the handle (darb_rnn_reserve sizes it up front).
  *  - Only these calls take scratch from the device's stream-ordered memory
@@ -447,6 +448,8 @@ DARB_API darb_status_t darb_token_logprobs_grad(const void *logits, darb_dtype_t
  * The mean and the centred squares are summed in fp32, the squares after the mean
  * is known.  y may be x itself (same pointer and leading dimension); no other
  * overlap of an output is allowed.  No tokens: nothing is done.
+ * A bounded device wait that gave up (DARB_ERR_TIMEOUT elsewhere; it has no handle
+ * to be reported through) leaves NaN in the tokens it was for.
  * Asynchronous on `stream`; allocates nothing; one launch.
  * Errors: DARB_ERR_INVALID_ARG (also a negative or NaN eps); DARB_ERR_UNSUPPORTED
  * (sizes as darb_token_logprobs, features up to 2^24); DARB_ERR_CUDA.
@@ -542,6 +545,11 @@ DARB_API darb_status_t darb_adamw_create(int32_t n, const int64_t *numel, float 
 DARB_API darb_status_t darb_adamw_step(darb_adamw_t plan, const void *const *grads, const float *grad_scale,
                                        int64_t step, uint64_t seed, double lr, double beta1, double beta2, double eps,
                                        double weight_decay, cudaStream_t stream);
+
+/* Synchronise `stream` and report what the plan's steps recorded since the last
+ * call, then clear it: DARB_ERR_TIMEOUT if a bounded device wait for a bulk copy
+ * gave up (the tensors are then not all updated), else DARB_OK.                */
+DARB_API darb_status_t darb_adamw_sync_status(darb_adamw_t plan, cudaStream_t stream);
 
 /* Release a plan (not its tensors); NULL is a no-op.  Waits for the device.    */
 DARB_API darb_status_t darb_adamw_destroy(darb_adamw_t plan);

@@ -68,6 +68,7 @@ struct StepArgs {
     const Tensor *tensors;
     const Chunk *chunks;
     const float *grad_scale;   // or null
+    int32_t *status;           // the plan's, of waits that gave up
     float b1, c1, b2, c2;      // c = 1 - b
     float decay, step_size, root_scale, eps;
     uint32_t key;
@@ -403,7 +404,10 @@ __global__ void __launch_bounds__(kAdamThreads + 32, 2) adamw_codes_kernel(const
             const Tensor t = a.tensors[ch.tensor];
             const G *grad = static_cast<const G *>(a.grads[ch.tensor - a.first_tensor]);
             const int64_t start = int64_t(ch.chunk) * kChunkElems, block = start / kBlock;
-            if (it >= kStages && !mbar_wait(&empty[stage], parity ^ 1)) return;
+            if (it >= kStages && !mbar_wait(&empty[stage], parity ^ 1)) {
+                atomicOr(a.status, kStatusTimeout);
+                return;   // (every copy so far has been waited for, or will be by the other warps)
+            }
             Stage<G> &s = ring[stage];
             s.t = t;
             s.grad = grad;
@@ -429,7 +433,11 @@ __global__ void __launch_bounds__(kAdamThreads + 32, 2) adamw_codes_kernel(const
     const Factors k(a, a.grad_scale ? *a.grad_scale : 1.0f);
     static_assert(kChunkElems == kAdamThreads / 32 * kBlock, "a block a warp");
     for (int32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        if (!mbar_wait(&full[stage], parity)) return;   // a copy that never came
+        if (!mbar_wait(&full[stage], parity)) {   // a copy that never came
+            if (lane == 0) atomicOr(a.status, kStatusTimeout);
+            mbar_wait(&full[stage], parity);      // one more second for it to land before the CTA leaves
+            return;
+        }
         const Stage<G> &s = ring[stage];
         if (s.staged) {
             // a lane has 4 elements of either half of the block
@@ -516,6 +524,7 @@ struct darb_adamw_s {
     void *dmem = nullptr;
     const darb::Tensor *d_tensors = nullptr;
     const darb::Chunk *d_chunks = nullptr;
+    int32_t *d_status = nullptr;
 };
 
 namespace {
@@ -578,7 +587,8 @@ darb_status_t build_plan(darb_adamw_s *plan, int32_t n, const int64_t *numel, fl
     if (chunks.empty()) return DARB_OK;
     const char *fail = std::getenv("DARB_FAIL_ALLOC");   // test hook, as for the library's other allocations
     if (fail != nullptr && fail[0] == '1') return DARB_ERR_OOM;
-    const size_t o_chunks = (plan->tensors.size() * sizeof(Tensor) + 255) / 256 * 256;
+    // the status word, the tensors, the chunks
+    const size_t o_tensors = 256, o_chunks = o_tensors + (plan->tensors.size() * sizeof(Tensor) + 255) / 256 * 256;
     const cudaError_t e = cudaMalloc(&plan->dmem, o_chunks + chunks.size() * sizeof(Chunk));
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -586,9 +596,12 @@ darb_status_t build_plan(darb_adamw_s *plan, int32_t n, const int64_t *numel, fl
         return e == cudaErrorMemoryAllocation ? DARB_ERR_OOM : DARB_ERR_CUDA;
     }
     char *d = static_cast<char *>(plan->dmem);
-    plan->d_tensors = reinterpret_cast<const Tensor *>(d);
+    plan->d_status = reinterpret_cast<int32_t *>(d);
+    plan->d_tensors = reinterpret_cast<const Tensor *>(d + o_tensors);
     plan->d_chunks = reinterpret_cast<const Chunk *>(d + o_chunks);
-    cudaError_t c = cudaMemcpyAsync(d, plan->tensors.data(), plan->tensors.size() * sizeof(Tensor), cudaMemcpyHostToDevice, stream);
+    cudaError_t c = cudaMemsetAsync(d, 0, 4, stream);
+    if (c == cudaSuccess)
+        c = cudaMemcpyAsync(d + o_tensors, plan->tensors.data(), plan->tensors.size() * sizeof(Tensor), cudaMemcpyHostToDevice, stream);
     if (c == cudaSuccess)
         c = cudaMemcpyAsync(d + o_chunks, chunks.data(), chunks.size() * sizeof(Chunk), cudaMemcpyHostToDevice, stream);
     // the chunks leave with this call, and steps may come on any stream
@@ -660,6 +673,7 @@ darb_status_t darb_adamw_step(darb_adamw_t plan, const void *const *grads, const
     StepArgs a;
     a.tensors = plan->d_tensors;
     a.grad_scale = grad_scale;
+    a.status = plan->d_status;
     a.b1 = float(beta1), a.c1 = float(1.0 - beta1), a.b2 = float(beta2), a.c2 = float(1.0 - beta2);
     a.decay = float(1.0 - lr * weight_decay);
     a.step_size = float(lr / (1.0 - std::pow(beta1, double(step))));
@@ -680,6 +694,21 @@ darb_status_t darb_adamw_step(darb_adamw_t plan, const void *const *grads, const
         if (st != DARB_OK) return st;
     }
     return DARB_OK;
+}
+
+darb_status_t darb_adamw_sync_status(darb_adamw_t plan, cudaStream_t stream) {
+    DARB_TRACE("darb_adamw_sync_status");
+    if (!live_plan(plan)) return DARB_ERR_INVALID_ARG;
+    if (plan->d_status == nullptr) return DARB_OK;   // nothing to update
+    int32_t bits = 0;
+    cudaError_t e = cudaMemcpyAsync(&bits, plan->d_status, 4, cudaMemcpyDeviceToHost, stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(plan->d_status, 0, 4, stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return DARB_ERR_CUDA;
+    }
+    return bits & kStatusTimeout ? DARB_ERR_TIMEOUT : DARB_OK;
 }
 
 darb_status_t darb_adamw_destroy(darb_adamw_t plan) {

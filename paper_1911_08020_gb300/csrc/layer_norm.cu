@@ -146,6 +146,9 @@ struct RowCopies {
     }
 };
 
+// A wait that gives up (after a second, and once more so that the copy can land)
+// makes the row NaN; the CTA then copies and waits no more.
+
 // The granules of a thread: for every row of a CTA at the same features.
 template <typename T, int VPT>
 struct Owned {
@@ -259,7 +262,7 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) norm_rows_kernel(const No
     bool arrived = true;
     for (int64_t r = r0; r < a.tokens; r += stride) {
         Pair v[VPT][H], s2 = both(0.0f);
-        arrived = arrived && mbar_wait(&full[stage], parity);
+        arrived = arrived && (mbar_wait(&full[stage], parity) || mbar_wait(&full[stage], parity));
         own.load(rows, r, ring + stage * stage_bytes + t * 16, arrived, v);
 #pragma unroll
         for (int u = 0; u < VPT; ++u)
@@ -340,7 +343,7 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const No
         Pair xh[VPT][H], d[VPT][H], s0 = both(0.0f), s1 = both(0.0f);
         const float mean = mean_next, rstd = rstd_next;
         if (r + stride < a.tokens) mean_next = __ldg(a.mean + r + stride), rstd_next = __ldg(a.rstd + r + stride);
-        arrived = arrived && mbar_wait(&full[stage], parity);
+        arrived = arrived && (mbar_wait(&full[stage], parity) || mbar_wait(&full[stage], parity));
         const unsigned char *at = ring + stage * stage_bytes + t * 16;
         own.load(xs, r, at, arrived, xh);
         own.load(ds, r, at + half, arrived, d);   // 0 outside the row: adds nothing to any sum

@@ -89,6 +89,7 @@ def lib():
                 "darb_adamw_create": [I32, P, P, P, P, P, P, P, ctypes.c_int, P, S],
                 "darb_adamw_step": [P, P, P, I64, ctypes.c_uint64, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                     ctypes.c_double, ctypes.c_double, S],
+                "darb_adamw_sync_status": [P, S],
                 "darb_adamw_destroy": [P],
             }
             for name, args in sig.items():
@@ -690,6 +691,11 @@ def darb_adamw_step(plan: AdamW, grads, step: int, lr: float, beta1: float = 0.9
     _check(lib().darb_adamw_step(plan.ptr, pointers, _vector(grad_scale, 1, (_torch or _load_torch()).float32, call, "grad_scale"),
                                  step, (step if seed is None else seed) & 0xFFFFFFFFFFFFFFFF, lr, beta1, beta2, eps,
                                  weight_decay, _stream(stream)), call)
+
+
+def darb_adamw_sync_status(plan: AdamW, stream=None):
+    """Synchronise and raise if a step's bounded wait gave up."""
+    _check(lib().darb_adamw_sync_status(plan.ptr, _stream(stream)), "darb_adamw_sync_status")
 
 
 def darb_adamw_destroy(plan: AdamW | None):

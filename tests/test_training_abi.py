@@ -118,6 +118,8 @@ def test_adamw_refusals(L, monkeypatch):
         h = list(hyper)
         h[i] = float(bad)
         assert L.darb_adamw_step(plan, g, None, 1, 0, *h, None) == INVALID
+    assert L.darb_adamw_sync_status(plan, None) == OK
     assert L.darb_adamw_destroy(plan) == OK
+    assert L.darb_adamw_sync_status(plan, None) == INVALID
     assert L.darb_adamw_step(plan, g, None, 1, 0, *hyper, None) == INVALID and L.darb_adamw_destroy(plan) == INVALID
     assert L.darb_adamw_destroy(None) == OK
