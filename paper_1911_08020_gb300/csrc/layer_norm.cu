@@ -704,8 +704,16 @@ struct ColShare {
     // The same of a vector over the features; null: `none`.
     __device__ __forceinline__ void load(const float *g, float none, int batch, float (&v)[U]) const {
         const float *p = g + feature(batch, 0);
+        if (g == nullptr) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = g == nullptr ? none : feature(batch, u) < end ? __ldg(p + u * SLOTS) : 0.0f;
+            for (int u = 0; u < U; ++u) v[u] = none;
+        } else if (full(batch)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = __ldg(p + u * SLOTS);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = feature(batch, u) < end ? __ldg(p + u * SLOTS) : 0.0f;
+        }
     }
     __device__ __forceinline__ void store(T *y, int64_t ld, int batch, const float (&v)[U]) const {
         T *p = y + int64_t(feature(batch, 0)) * ld;
@@ -749,14 +757,16 @@ __global__ void __launch_bounds__(kColThreads) norm_columns_kernel(const NormArg
         const int have = min(U, rows - b * U);
         float s = 0.0f, q = 0.0f;
 #pragma unroll
-        for (int u = 0; u < U; ++u) s += v[u];
-        const float bm = s / float(have);
+        for (int u = 0; u < U; ++u) s += v[u];   // 0 past the end
+        const float bm = have == U ? s * (1.0f / U) : s / float(have);
+        if (have == U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const float d = u < have ? v[u] - bm : 0.0f;
-            q = fmaf(d, d, q);
+            for (int u = 0; u < U; ++u) q = fmaf(v[u] - bm, v[u] - bm, q);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) q = u < have ? fmaf(v[u] - bm, v[u] - bm, q) : q;
         }
-        const float part = float(have) / float(b * U + have), d = bm - mean;
+        const float part = __fdividef(float(have), float(b * U + have)), d = bm - mean;
         mean = fmaf(d, part, mean);
         m2 += q + d * d * (float(b * U) * part);
     }
