@@ -448,6 +448,15 @@ def _tokens(t, dim: int, call: str, name: str) -> tuple[int, int, int, int, int]
     return TOKEN_COLUMNS, steps, n, f, ld
 
 
+def _single_token(layout: int, n: int, f: int, ld: int, x, others, dim: int) -> tuple[int, int]:
+    """(layout, ld) of one token's features x, which can be taken as a row if they are contiguous, but have
+    to be taken as a column where those of another tensor of the call are not."""
+    if n == 1 and layout == TOKEN_ROWS and x.dim() == 2:
+        if any(t is not None and t.dim() == 2 and t.stride()[dim] != 1 for t in others):
+            return TOKEN_COLUMNS, x.stride()[dim] if f > 1 else 1
+    return layout, ld
+
+
 def _same_tokens(t, like, ld: int, dim: int, layout: int, call: str, name: str) -> int:
     """The leading dimension of a tensor of the shape, type and layout of another, whose own is `ld`."""
     if not t.is_cuda or t.dtype != like.dtype or t.shape != like.shape:
@@ -531,6 +540,7 @@ def darb_token_logprobs_grad(logits, targets, lse, d_logprob, entropy=None, d_en
         out = _new((n, v) if layout == TOKEN_ROWS else (v, n), logits.dtype, logits.device, stream)
         if (layout == TOKEN_ROWS) != (dim % 2 == 1):
             out = out.t()
+    layout, ld = _single_token(layout, n, v, ld, logits, (out,), dim)
     ld_out = _same_tokens(out, logits, ld, dim, layout, call, "out")
     f32 = torch.float32
     _check(lib().darb_token_logprobs_grad(logits.data_ptr(), code, layout, n, v, ld,
@@ -555,6 +565,7 @@ def darb_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, dim: int = -1, 
     f32 = _torch.float32
     if y is None:
         y = _new_like(x, dim, layout, steps, n, f, stream)
+    layout, ld = _single_token(layout, n, f, ld, x, (y,), dim)
     lead = (steps, n) if x.dim() == 3 else (n,)
     if mean is None:
         mean = _new(lead, f32, x.device, stream)
@@ -586,6 +597,7 @@ def darb_layer_norm_grad(dy, x, gamma, mean, rstd, dim: int = -1, dx=None, dgamm
     f32 = _torch.float32
     if dx is None:
         dx = _new_like(x, dim, layout, steps, n, f, stream)
+    layout, ld = _single_token(layout, n, f, ld, x, (dy, dx), dim)
     pg = pb = pw = None
     if weights:
         if dgamma is None:

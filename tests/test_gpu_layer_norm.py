@@ -283,3 +283,19 @@ def test_captured_in_a_graph():
         graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(want + back, got + got_back))
+
+
+@pytest.mark.parametrize("strides", [(1, 1, 1), (1, 4, 1), (3, 1, 2), (1, 1, 5), (2, 3, 4)])
+def test_one_column_of_wider_matrices(strides):
+    f = 150
+    a, b, c = (torch.zeros(f, s, device="cuda")[:, :1] for s in strides)
+    a.copy_(torch.randn(f, 1, device="cuda"))
+    ga = torch.randn(f, device="cuda")
+    row = a.t().contiguous()
+    y, mean, rstd = darb.darb_layer_norm(row, ga)
+    got = darb.darb_layer_norm(a, ga, dim=0, y=b)
+    assert torch.allclose(got[0].t(), y, rtol=1e-5, atol=1e-6)
+    want = darb.darb_layer_norm_grad(y, row, ga, mean, rstd)
+    back = darb.darb_layer_norm_grad(b, a, ga, mean, rstd, dim=0, dx=c)
+    assert torch.allclose(back[0].t(), want[0], rtol=1e-4, atol=1e-5)
+    assert torch.allclose(back[1], want[1], rtol=1e-4, atol=1e-5) and torch.allclose(back[2], want[2], rtol=1e-4, atol=1e-5)

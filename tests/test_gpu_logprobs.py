@@ -383,3 +383,19 @@ def test_logits_further_apart_than_32_bits_count(layout):
     a = darb.darb_token_logprobs_grad(x, tg, want.lse, d)
     b = darb.darb_token_logprobs_grad(t, tg, want.lse, d, dim=dim, out=t)
     assert torch.allclose(a.float(), (b if layout == "rows" else b.t()).float(), rtol=2.0 ** -7, atol=1e-7)
+
+
+@pytest.mark.parametrize("strides", [(1, 1), (1, 4), (3, 1), (5, 2)])
+def test_one_column_of_wider_matrices(strides):
+    """One token: dense features here, features a leading dimension apart there."""
+    v = 300
+    a, b = (torch.zeros(v, s, device="cuda")[:, :1] for s in strides)
+    a.copy_(torch.randn(v, 1, device="cuda"))
+    tg, d = torch.tensor([7], device="cuda"), torch.ones(1, device="cuda")
+    row = a.t().contiguous()
+    fwd = darb.darb_token_logprobs(a, tg, 3, dim=0)
+    want = darb.darb_token_logprobs(row, tg, 3)
+    assert torch.equal(fwd.top_index, want.top_index) and torch.allclose(fwd.logprob, want.logprob, rtol=0, atol=1e-5)
+    got = darb.darb_token_logprobs_grad(a, tg, want.lse, d, dim=0, out=b)
+    assert got.data_ptr() == b.data_ptr()
+    assert torch.allclose(got.t(), darb.darb_token_logprobs_grad(row, tg, want.lse, d), rtol=1e-5, atol=1e-7)
