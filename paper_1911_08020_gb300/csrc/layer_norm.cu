@@ -736,7 +736,7 @@ struct ColShare {
 };
 
 // Latency and instructions, not memory: 1500 x 20 fp32 5.5 us, 35 steps of it
-// 10.4; 60 x 10852 x 26 fp32 59 us (2.3 TB/s).
+// 10.4; 60 x 10852 x 26 fp32 53 us (2.6 TB/s).
 template <typename T, int CT>
 __global__ void __launch_bounds__(kColThreads) norm_columns_kernel(const NormArgs a, int32_t tiles) {
     using Share = ColShare<T, CT>;
@@ -862,7 +862,7 @@ __device__ __forceinline__ int reduce_scatter(float (&v)[N]) {
 }
 
 // 35 x 1500 x 20 fp32 11.5 us with the kernel that adds the partial results;
-// 60 x 10852 x 26 fp32 80 us (2.5 TB/s).
+// 60 x 10852 x 26 fp32 81 us (2.5 TB/s).
 template <typename T, int CT>
 __global__ void __launch_bounds__(kColThreads) back_columns_kernel(const NormArgs a, int32_t tiles) {
     using Share = ColShare<T, CT>;
@@ -1036,10 +1036,12 @@ cudaError_t with_col_tile(const NormArgs &a, F f) {
     const int ct = col_tile(a.steps, a.tokens, sizeof(T));
     const int64_t tiles = (a.tokens + ct - 1) / ct, all = tiles * a.steps;
     // more CTAs a tile while each thread keeps half a batch of features (1500 x 20:
-    // 5.5 us; with a quarter of one 6.7, with a whole one 6.0)
+    // 5.5 us; with a quarter of one 6.7, with a whole one 6.0) and until every SM has
+    // one: beyond that they make a second wave (64 x 300 x 99 bf16 on 256 CTAs 8.2 us,
+    // on 512 14.7; 60 x 10852 x 26 fp32 on 240 CTAs 53, on 480 60)
     const int sms = sm_count();
     int split = 1;
-    while (split < kColSplit && all * split < 2 * sms && a.features / (2 * split) >= kColBatch / 2 * kColThreads / ct) split *= 2;
+    while (split < kColSplit && all * split < sms && a.features / (2 * split) >= kColBatch / 2 * kColThreads / ct) split *= 2;
     if (all * split > INT32_MAX) return cudaErrorNotSupported;
     const dim3 grid(unsigned(all * split));
     if (ct == 32) return f(std::integral_constant<int, 32>(), grid, unsigned(split), int32_t(tiles));
