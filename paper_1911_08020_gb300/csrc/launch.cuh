@@ -110,6 +110,43 @@ cudaError_t allow_smem(void (*kernel)(KArgs...), size_t bytes) {
     return cudaSuccess;
 }
 
+// Clusters of 1, 2, 4 and 8 CTAs of a kernel that the device holds at a time.  (Clusters
+// of 8 CTAs that take an SM each: 15 on 152 SMs, as they do not cross the SMs'
+// groups.)
+struct ClusterRoom {
+    int of[4];
+};
+template <typename... KArgs>
+ClusterRoom cluster_room(void (*kernel)(KArgs...), int threads, size_t smem) {
+    const void *fn = reinterpret_cast<const void *>(kernel);
+    const long long v = per_device(fn, 1ll << 62 | (long long)threads << 32 | (long long)smem, [&]() -> long long {
+        long long all = 0;
+        for (int i = 0; i < 4; ++i) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(8);
+            cfg.blockDim = dim3(static_cast<unsigned>(threads));
+            cfg.dynamicSmemBytes = smem;
+            cudaLaunchAttribute at[1];
+            at[0].id = cudaLaunchAttributeClusterDimension;
+            at[0].val.clusterDim.x = 1u << i;
+            at[0].val.clusterDim.y = 1;
+            at[0].val.clusterDim.z = 1;
+            cfg.attrs = at;
+            cfg.numAttrs = 1;
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess) {
+                cudaGetLastError();
+                n = 0;
+            }
+            all |= static_cast<long long>(n < 1 ? 1 : n > 0x7FFF ? 0x7FFF : n) << (16 * i);
+        }
+        return all;
+    });
+    ClusterRoom r;
+    for (int i = 0; i < 4; ++i) r.of[i] = static_cast<int>(v >> (16 * i) & 0xFFFF);
+    return r;
+}
+
 // cuTensorMapEncodeTiled from the driver (through the runtime, so that the
 // library does not link libcuda); nullptr if unavailable.
 inline PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {

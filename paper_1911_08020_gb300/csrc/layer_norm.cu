@@ -736,7 +736,7 @@ struct ColShare {
 };
 
 // Latency and instructions, not memory: 1500 x 20 fp32 5.5 us, 35 steps of it
-// 10.4; 60 x 10852 x 26 fp32 53 us (2.6 TB/s).
+// 8.9; 60 x 10852 x 26 fp32 53 us (2.6 TB/s).
 template <typename T, int CT>
 __global__ void __launch_bounds__(kColThreads) norm_columns_kernel(const NormArgs a, int32_t tiles) {
     using Share = ColShare<T, CT>;
@@ -861,7 +861,7 @@ __device__ __forceinline__ int reduce_scatter(float (&v)[N]) {
     return first;
 }
 
-// 35 x 1500 x 20 fp32 11.5 us with the kernel that adds the partial results;
+// 35 x 1500 x 20 fp32 10.0 us with the kernel that adds the partial results;
 // 60 x 10852 x 26 fp32 81 us (2.5 TB/s).
 template <typename T, int CT>
 __global__ void __launch_bounds__(kColThreads) back_columns_kernel(const NormArgs a, int32_t tiles) {
@@ -1035,13 +1035,23 @@ template <typename T, typename F>
 cudaError_t with_col_tile(const NormArgs &a, F f) {
     const int ct = col_tile(a.steps, a.tokens, sizeof(T));
     const int64_t tiles = (a.tokens + ct - 1) / ct, all = tiles * a.steps;
-    // more CTAs a tile while each thread keeps half a batch of features (1500 x 20:
-    // 5.5 us; with a quarter of one 6.7, with a whole one 6.0) and until every SM has
-    // one: beyond that they make a second wave (64 x 300 x 99 bf16 on 256 CTAs 8.2 us,
-    // on 512 14.7; 60 x 10852 x 26 fp32 on 240 CTAs 53, on 480 60)
-    const int sms = sm_count();
-    int split = 1;
-    while (split < kColSplit && all * split < sms && a.features / (2 * split) >= kColBatch / 2 * kColThreads / ct) split *= 2;
+    // The split with the least time, while each thread keeps half a batch of features
+    // (1500 x 20: 5.5 us; with a quarter of one 6.7, with a whole one 6.0): waves of
+    // clusters, two CTAs an SM, each with a fixed part and its rows, in units of a row of
+    // 32 tokens (8 ns).  CTAs that share an SM are slower: 64 x 300 x 99 bf16 on 256 CTAs
+    // 8.2 us, on 512 14.7; 35 x 1500 x 20 fp32 on 140 8.9, on 280 10.4; 60 x 10852 x 26 on
+    // 240 53, on 480 60.  (The backward kernel and other tiles have as much room.)
+    const ClusterRoom room = cluster_room(norm_columns_kernel<T, 32>, kColThreads, 0);
+    static_assert(kColSplit == 8, "the clusters that room is known of");
+    const auto cost = [&](int i) {
+        const int64_t waves = (all + room.of[i] - 1) / room.of[i];
+        const double rows = double(a.features >> i) * ct / 32;
+        return double(waves) * (500 + (2 * all > room.of[i] ? 325 + 1.25 * rows : rows));
+    };
+    int best = 0;
+    for (int i = 1; i < 4; ++i)
+        if (a.features >> i >= kColBatch / 2 * kColThreads / ct && cost(i) < cost(best)) best = i;
+    const int split = 1 << best;
     if (all * split > INT32_MAX) return cudaErrorNotSupported;
     const dim3 grid(unsigned(all * split));
     if (ct == 32) return f(std::integral_constant<int, 32>(), grid, unsigned(split), int32_t(tiles));

@@ -836,19 +836,27 @@ cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream) {
 template <typename T, int CT>
 cudaError_t launch_score_columns_ct(const ScoreArgs &a, cudaStream_t stream) {
     const int64_t tiles = (a.tokens + CT - 1) / CT;
-    // a CTA takes an SM: the split whose CTAs fill their waves best, the smaller of
-    // equals (1011 columns of 25568 bf16, 32 tiles: 4 CTAs a tile in one wave, not 8 in two)
-    const int sms = sm_count();
-    int split = 1;
-    const auto cost = [&](int s) { return double((tiles * s + sms - 1) / sms) / s; };
-    for (int s = 2; s <= kMaxSplit; s *= 2)
-        if (a.vocab / s >= 4 * kColThreads / CT && cost(s) < 0.95 * cost(split)) split = s;
-    const int64_t rows = a.vocab / split + 1;   // of a CTA, at most
-    constexpr int per_round = kColThreads / CT * kColUnroll;
-    const Blocks blocks = blocks_of((rows + per_round - 1) / per_round, kColSlots);
     const size_t smem = sizeof(ColShared<CT>);
     const cudaError_t e = allow_smem(score_columns_kernel<T, CT>, smem);
     if (e != cudaSuccess) return e;
+    // A CTA takes an SM.  The split with the least time: waves of clusters, each with a
+    // fixed part (the joins, the candidates, in a cluster its exchanges) and its rows, in
+    // units of a row of 32 columns (2.6 ns).  4000 x 3000 fp32, k = 5: 94 CTAs 20 us, in
+    // clusters of 8 76; 37462 x 566: clusters of 4 30.5, of 8 (two waves) 35.
+    const ClusterRoom room = cluster_room(score_columns_kernel<T, CT>, kColThreads, smem);
+    static_assert(kMaxSplit == 8, "the clusters that room is known of");
+    const auto cost = [&](int i) {
+        const int64_t waves = (tiles + room.of[i] - 1) / room.of[i];
+        const double fixed = a.k > 0 ? (i > 0 ? 3800 : 3000) : (i > 0 ? 1700 : 1150);
+        return double(waves) * (fixed + double(a.vocab >> i) * CT / 32);
+    };
+    int best = 0;
+    for (int i = 1; i < 4; ++i)
+        if (a.vocab >> i >= 4 * kColThreads / CT && cost(i) < cost(best)) best = i;
+    const int split = 1 << best;
+    const int64_t rows = a.vocab / split + 1;   // of a CTA, at most
+    constexpr int per_round = kColThreads / CT * kColUnroll;
+    const Blocks blocks = blocks_of((rows + per_round - 1) / per_round, kColSlots);
     return launch_ex(score_columns_kernel<T, CT>, dim3(unsigned(tiles * split)), dim3(kColThreads), smem, stream,
                      unsigned(split), true, a, blocks);
 }
