@@ -351,7 +351,7 @@ constexpr int kRowSlots = 32;   // of the table of maxima, at most
 // blocks that reach the bar are read again.
 //   4096 x 32000 bf16: 41.5 us (6.3 TB/s), k = 5 49, k = 20 53
 //   1023 x 128001 fp32: 78 us (6.7 TB/s), k = 20 86-88
-//   1 x 32000 bf16: 3.3 us, k = 8 6.5
+//   1 x 32000 bf16: 3.4 us, k = 8 5.6
 constexpr int kItems = 256;   // blocks that may hold one of the k largest, at most
 
 template <typename T, int THREADS, int U, bool CLUSTER>
@@ -819,18 +819,26 @@ cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream, int split
 
 template <typename T>
 cudaError_t launch_score_rows(const ScoreArgs &a, cudaStream_t stream) {
-    const int sms = sm_count();
-    // Rows of up to 128 KB on CTAs of 128 threads, so that fewer warps wait while a
-    // token's sums are joined (4096 x 32000 bf16: 52 us, with 256 threads 63); longer
-    // ones need the loads of 256 (1023 x 128001 fp32: 88, with 128 threads 137).
-    const bool short_rows = row_granules<T>(0, a.vocab) <= 8192;
-    if (a.tokens >= 4 * sms && short_rows) return launch_score_rows<T, 128, false>(a, stream, 1);
-    // CTAs for every SM, while a thread keeps two granules (a vocabulary of 32000 in
-    // bf16: one token 6.0 us, with one granule 6.4, with four 6.5; 50 tokens of 31856
-    // in fp32 on 200 CTAs 9.4, on 400 11.8)
+    const int64_t sms = sm_count(), granules = row_granules<T>(0, a.vocab);
+    // A cluster where it saves more reading than its exchanges cost (k = 5: one token of
+    // 32000 bf16 alone 5.5 us, in a cluster 6.7; of 128000 10.3 and 7.0), while there are SMs
+    // without a CTA, or with one that has much to read (130 x 128000 fp32: 2 a token 19.2 us, 4 16.5).
     int split = 1;
-    while (split < kMaxSplit && a.tokens * split < sms && a.vocab / (2 * split) >= 2 * 256 * kPerGranule<T>) split *= 2;
-    return split > 1 ? launch_score_rows<T, 256, true>(a, stream, split) : launch_score_rows<T, 256, false>(a, stream, 1);
+    if (granules > (a.k > 0 ? 14000 : 6000))
+        while (split < kMaxSplit && (a.tokens * split < sms || (a.tokens * split < 2 * sms && granules / split > 8192))) split *= 2;
+    if (split > 1) return launch_score_rows<T, 256, true>(a, stream, split);
+    // Fewer threads a token leave less waiting for the joins of its sums, and more tokens
+    // at a time on an SM; too few, and the loads in flight are too few.  Rows of one round
+    // of 64 threads (8000 x 1000 bf16: 12.1 us, with 128 threads 21.6), or of some rounds
+    // with many tokens (8000 x 5000 bf16 19.7, with 128 28.2; 1000 x 10000 fp32 10.4, with 128 8.9):
+    if (granules <= 256 || (granules > 512 && granules <= 2048 && a.tokens >= 8 * sms))
+        return launch_score_rows<T, 64, false>(a, stream, 1);
+    // of up to 128 KB with 128 (4096 x 32000 bf16: 52 us, with 256 63; 400 x 11201 fp32 4.1 and
+    // 4.8; but 600 x 32000 fp32 16.0 and 13.8), longer ones with 256 (1023 x 128001 fp32: 88, with 128 137).
+    if (granules <= 512 || (granules <= 2048 && a.tokens >= sms) || (granules <= 4096 && a.tokens >= 2 * sms) ||
+        (granules <= 8192 && a.tokens >= 4 * sms))
+        return launch_score_rows<T, 128, false>(a, stream, 1);
+    return launch_score_rows<T, 256, false>(a, stream, 1);
 }
 
 template <typename T, int CT>
