@@ -394,29 +394,46 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const No
     }
 }
 
-// dgamma and dbeta from the partial results: 32 features of one of them a CTA,
-// the partial results shared by its warps, joined in order.  Where rows p of
-// the kernel that made them start `base` + p * `step` bytes from a 16-byte
-// boundary, feature f lies that many elements further.
+// dgamma and dbeta from the partial results: 32 features of one of them a CTA, or
+// a cluster where features are few and partial results many, those shared by its
+// warps, joined in order.  Where rows p of the kernel that made them start `base` +
+// p * `step` bytes from a 16-byte boundary, feature f lies that many elements
+// further.  2432 partial results of 200 features (16000 rows, fp32): the call takes
+// 20.2 us with clusters of 8, 24.6 without; 704 of 700 features 8.9 and 7.7.
+constexpr int kSumSplit = 8;
+
+template <bool CLUSTER>
 __global__ void __launch_bounds__(1024) sum_partials_kernel(const float *partial, int32_t partials, int32_t features,
                                                             uint32_t base, uint32_t step, uint32_t size, float *dgamma,
                                                             float *dbeta) {
-    __shared__ float s[32][33];
+    __shared__ float s[32][33], part[32];
     pdl_wait_previous();
     pdl_launch_dependents();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int split = CLUSTER ? int(cluster.num_blocks()) : 1, rank = CLUSTER ? int(cluster.block_rank()) : 0;
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int32_t f0 = int32_t(blockIdx.x) / split * 32;
     const int64_t width = partial_width(features);
-    const int32_t f = int32_t(blockIdx.x) * 32 + lane;
-    const float *at = partial + blockIdx.y * width + f;
+    const float *at = partial + blockIdx.y * width + f0 + lane;
+    const auto value = [&](int32_t p) { return at[int64_t(p) * 2 * width + (((base + uint32_t(p) * step) & 15u) / size)]; };
     float v = 0.0f;
-    if (f < features)
-        for (int32_t p = w; p < partials; p += 32)
-            v += at[int64_t(p) * 2 * width + ((base + uint32_t(p) * step) & 15u) / size];
+    if (f0 + lane < features)
+        for (int32_t p = w + 32 * rank; p < partials; p += 32 * split) v += value(p);
     s[w][lane] = v;
     __syncthreads();
-    v = warp_sum(s[lane][w]);   // of feature blockIdx.x * 32 + w
-    const int32_t j = int32_t(blockIdx.x) * 32 + w;
-    if (lane == 0 && j < features) (blockIdx.y ? dbeta : dgamma)[j] = v;
+    v = warp_sum(s[lane][w]);   // of feature f0 + w
+    if constexpr (!CLUSTER) {
+        if (lane == 0 && f0 + w < features) (blockIdx.y ? dbeta : dgamma)[f0 + w] = v;
+        return;
+    }
+    if (lane == 0) part[w] = v;
+    cluster.sync();
+    if (rank == 0 && threadIdx.x < 32) {
+        v = 0.0f;
+        for (int r = 0; r < split; ++r) v += cluster.map_shared_rank(part, r)[lane];
+        if (f0 + lane < features) (blockIdx.y ? dbeta : dgamma)[f0 + lane] = v;
+    }
+    cluster.sync();   // its sums may still be read
 }
 
 // Rows of any length and alignment: a CTA a row, read again for every sum.
@@ -1163,10 +1180,15 @@ cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, 
                 e = launch_ex(back_any_kernel<T>, dim3(unsigned(a.tokens)), dim3(kAnyThreads), 0, stream, 1, true, a);
         }
     }
-    if (e == cudaSuccess && a.partial != nullptr)
-        e = launch_ex(sum_partials_kernel, dim3(unsigned((a.features + 31) / 32), 2), dim3(1024), 0, stream, 1, true,
-                      static_cast<const float *>(a.partial), int32_t(partials), a.features, base, step, uint32_t(sizeof(T)),
-                      dgamma, dbeta);
+    if (e == cudaSuccess && a.partial != nullptr) {
+        const unsigned blocks = unsigned((a.features + 31) / 32);
+        unsigned split = 1;
+        if (partials > 1024)
+            while (split < kSumSplit && partials > 512 * int64_t(split) && 2 * blocks * split < unsigned(sm_count())) split *= 2;
+        e = launch_ex(split > 1 ? sum_partials_kernel<true> : sum_partials_kernel<false>, dim3(blocks * split, 2), dim3(1024), 0,
+                      stream, split, true, static_cast<const float *>(a.partial), int32_t(partials), a.features, base, step,
+                      uint32_t(sizeof(T)), dgamma, dbeta);
+    }
     return e;
 }
 

@@ -299,3 +299,15 @@ def test_one_column_of_wider_matrices(strides):
     back = darb.darb_layer_norm_grad(b, a, ga, mean, rstd, dim=0, dx=c)
     assert torch.allclose(back[0].t(), want[0], rtol=1e-4, atol=1e-5)
     assert torch.allclose(back[1], want[1], rtol=1e-4, atol=1e-5) and torch.allclose(back[2], want[2], rtol=1e-4, atol=1e-5)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,f,pad", [(3000, 300, 0), (2600, 210, 3), (2500, 515, 1), (1300, 1030, 0)])
+def test_many_partial_results(n, f, pad, dtype):
+    run_case(1, n, f, "rows", dtype, pad=pad)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("s,n,f", [(40, 33, 600), (64, 99, 70), (10, 100, 700), (20, 37, 520), (9, 25, 1100)])
+def test_column_tiles_of_every_split(s, n, f, dtype):
+    run_case(s, n, f, "steps", dtype)

@@ -399,3 +399,17 @@ def test_one_column_of_wider_matrices(strides):
     got = darb.darb_token_logprobs_grad(a, tg, want.lse, d, dim=0, out=b)
     assert got.data_ptr() == b.data_ptr()
     assert torch.allclose(got.t(), darb.darb_token_logprobs_grad(row, tg, want.lse, d), rtol=1e-5, atol=1e-7)
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,v", [(400, 1001), (160, 2100), (1300, 4200), (2500, 600), (320, 13000), (620, 7001), (4, 120001),
+                                 (155, 60000)])
+def test_scores_of_every_split(n, v, dtype, layout):
+    """Few and many threads a token, one CTA and several."""
+    g = np.random.default_rng(n + v)
+    x = 3.0 * g.standard_normal((n, v)).astype(np.float32)
+    x[g.random((n, v)) < 0.1] = -np.inf
+    targets = g.integers(0, v, n)
+    for k in (0, 6):
+        check(x, layout, dtype, targets, k)
