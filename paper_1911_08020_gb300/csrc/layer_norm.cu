@@ -299,13 +299,18 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) norm_rows_kernel(const No
     }
 }
 
-// SUMS: with the sums over the tokens, 16 features a thread; without them 32.
+// SUMS: the sums over the tokens in registers, 16 features a thread; in shared
+// memory (of the thread that owns the features), 32; or none, 32.
 //   8192 x 4096 bf16: 43 us with the kernel that adds the partial results (4.7
 //   TB/s; 5.9 a row); x 4104, with a third fewer rows in flight: 61
-//   2700 x 12288 fp32 (sums in row_sums_kernel, which reads x and dy again): 113 us
-template <typename T, int VPT, int STAGES, int MOST, bool SUMS>
+//   sums in shared memory (in row_sums_kernel, which reads x and dy again):
+//   1000 x 12000 bf16 37 us (50), 2700 x 12288 fp32 114 (127)
+enum Sums { kNoSums, kRegisterSums, kSharedSums };
+
+template <typename T, int VPT, int STAGES, int MOST, Sums SUMS>
 __global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const NormArgs a, int32_t stage_bytes) {
     constexpr int V = kPerGranule<T>, H = V / 2;
+    constexpr bool REGISTERS = SUMS == kRegisterSums, SHARED = SUMS == kSharedSums;
     extern __shared__ __align__(16) unsigned char ring[];   // a stage: a row of x, a row of dy
     __shared__ __align__(16) float buf[2 * 2 * kSumWarps];
     __shared__ uint64_t full[STAGES];
@@ -329,9 +334,18 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const No
             if (r0 + s * stride < a.tokens) issue(r0 + s * stride, s);
     const float inv_n = __fdiv_rn(1.0f, float(n));
     const Owned<T, VPT> own = {t * V - row_head<T>(xs.base + r0 * a.ld_x), threads * V, n};
-    Pair gm[VPT][H], sg[SUMS ? VPT : 1][H], sb[SUMS ? VPT : 1][H];
+    Pair gm[VPT][H], sg[REGISTERS ? VPT : 1][H], sb[REGISTERS ? VPT : 1][H];
     own.gather(a.gamma, 1.0f, gm);
-    if constexpr (SUMS) {
+    // granule g of the row: V sums for dgamma, V for dbeta, at 16 bytes a thread
+    float4 *sums = reinterpret_cast<float4 *>(ring + STAGES * stage_bytes) + t;
+    const auto place = [&](int u, int q) { return (u * (V / 2) + q) * threads; };   // q: V / 4 words of one sum, V / 4 of the other
+    if constexpr (SHARED) {
+#pragma unroll
+        for (int u = 0; u < VPT; ++u)
+#pragma unroll
+            for (int q = 0; q < V / 2; ++q) sums[place(u, q)] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    if constexpr (REGISTERS) {
 #pragma unroll
         for (int u = 0; u < VPT; ++u)
 #pragma unroll
@@ -357,9 +371,19 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const No
 #pragma unroll
             for (int e = 0; e < H; ++e) {
                 xh[u][e] = mul2(add2(xh[u][e], both(-mean)), both(rstd));
-                if constexpr (SUMS) {
+                if constexpr (REGISTERS) {
                     sg[u][e] = fma2(d[u][e], xh[u][e], sg[u][e]);
                     sb[u][e] = add2(sb[u][e], d[u][e]);
+                }
+                if constexpr (SHARED) {
+                    if (e % 2 == 0) {
+                        float4 &g = sums[place(u, e / 2)], &b = sums[place(u, V / 4 + e / 2)];
+                        const Pair x1 = mul2(add2(xh[u][e + 1], both(-mean)), both(rstd)), d0 = d[u][e], d1 = d[u][e + 1];
+                        const Pair g0 = fma2(d0, xh[u][e], pair(g.x, g.y)), g1 = fma2(d1, x1, pair(g.z, g.w));
+                        const Pair b0 = add2(d0, pair(b.x, b.y)), b1 = add2(d1, pair(b.z, b.w));
+                        g = make_float4(low(g0), high(g0), low(g1), high(g1));
+                        b = make_float4(low(b0), high(b0), low(b1), high(b1));
+                    }
                 }
                 d[u][e] = mul2(d[u][e], gm[u][e]);
                 s0 = add2(s0, d[u][e]);
@@ -377,7 +401,7 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const No
                 d[u][e] = mul2(fma2(xh[u][e], both(-c1), add2(d[u][e], both(-c0))), both(rstd));
         own.store(dx + r * a.ld_out, d);
     }
-    if (SUMS && a.partial != nullptr) {
+    if (SUMS != kNoSums && a.partial != nullptr) {
         // as the thread holds them: feature f at f + the head of this CTA's rows
         const int64_t width = partial_width(n);
         float *p = a.partial + r0 * 2 * width;
@@ -387,6 +411,12 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const No
                 float4 *g = reinterpret_cast<float4 *>(p + (u * threads + t) * V), *b = reinterpret_cast<float4 *>(p + width + (u * threads + t) * V);
 #pragma unroll
                 for (int e = 0; e < H; e += 2) {
+                    if constexpr (SHARED) {
+                        g[e / 2] = sums[place(u, e / 2)];
+                        b[e / 2] = sums[place(u, V / 4 + e / 2)];
+                        continue;
+                    }
+                    if constexpr (!REGISTERS) continue;
                     g[e / 2] = make_float4(low(sg[u][e]), high(sg[u][e]), low(sg[u][e + 1]), high(sg[u][e + 1]));
                     b[e / 2] = make_float4(low(sb[u][e]), high(sb[u][e]), low(sb[u][e + 1]), high(sb[u][e + 1]));
                 }
@@ -992,14 +1022,16 @@ struct RowPlan {
     int threads;
     int64_t grid;
     int32_t stage_bytes;
+    size_t smem;
 };
 template <typename Kernel>
-RowPlan row_plan(Kernel kernel, int64_t granules, int vpt, int most, int copies, int stages, int64_t rows) {
+RowPlan row_plan(Kernel kernel, int64_t granules, int vpt, int most, int copies, int stages, int64_t rows, int granule_sums = 0) {
     RowPlan p = {};
     const int64_t threads = ((granules + vpt - 1) / vpt + 31) / 32 * 32;
     if (threads > most) return p;
     p.stage_bytes = int32_t(granules) * 16 * copies;
-    const size_t smem = size_t(p.stage_bytes) * stages;
+    const size_t smem = size_t(p.stage_bytes) * stages + size_t(threads) * vpt * granule_sums;
+    p.smem = smem;
     // (the kernel's own shared memory counts against the limit that needs no asking)
     if (allow_smem(kernel, smem + 1024) != cudaSuccess) return p;
     const int64_t per_sm = per_device(reinterpret_cast<const void *>(kernel), int64_t(threads) << 32 | int64_t(smem), [&]() -> long long {
@@ -1151,11 +1183,22 @@ cudaError_t launch_back(const NormArgs &a, darb_layout_t layout, float *dgamma, 
             e = launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * stages, stream, 1, true, a,
                           p.stage_bytes);
         };
-        rows(back_rows_kernel<T, VPT, 3, 256, true>, VPT, 256, 3);
-        rows(back_rows_kernel<T, VPT, 3, kHalfThreads, true>, VPT, kHalfThreads, 3);
-        rows(back_rows_kernel<T, VPT, 3, kRowThreads, true>, VPT, kRowThreads, 3);
+        rows(back_rows_kernel<T, VPT, 3, 256, kRegisterSums>, VPT, 256, 3);
+        rows(back_rows_kernel<T, VPT, 3, kHalfThreads, kRegisterSums>, VPT, kHalfThreads, 3);
+        rows(back_rows_kernel<T, VPT, 3, kRowThreads, kRegisterSums>, VPT, kRowThreads, 3);
+        if (same && e == cudaErrorNotSupported && a.partial != nullptr) {
+            // a stage of x and dy next to the sums: two where they fit
+            constexpr int STAGES = sizeof(T) == 2 ? 2 : 1;
+            const auto kernel = back_rows_kernel<T, 2 * VPT, STAGES, kRowThreads, kSharedSums>;
+            const RowPlan p = row_plan(kernel, granules, 2 * VPT, kRowThreads, 2, STAGES, a.tokens, kPerGranule<T> * 8);
+            if (p.threads > 0) {
+                partials = p.grid;
+                shifted();
+                e = launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), p.smem, stream, 1, true, a, p.stage_bytes);
+            }
+        }
         if (same && e == cudaErrorNotSupported) {
-            const auto kernel = back_rows_kernel<T, 2 * VPT, 2, kRowThreads, false>;
+            const auto kernel = back_rows_kernel<T, 2 * VPT, 2, kRowThreads, kNoSums>;
             const RowPlan p = row_plan(kernel, granules, 2 * VPT, kRowThreads, 2, 2, a.tokens);
             if (p.threads > 0) {
                 e = cudaSuccess;

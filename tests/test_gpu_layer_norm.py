@@ -311,3 +311,9 @@ def test_many_partial_results(n, f, pad, dtype):
 @pytest.mark.parametrize("s,n,f", [(40, 33, 600), (64, 99, 70), (10, 100, 700), (20, 37, 520), (9, 25, 1100)])
 def test_column_tiles_of_every_split(s, n, f, dtype):
     run_case(s, n, f, "steps", dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,f,pad", [(200, 12288, 0), (170, 9001, 0), (330, 8500, 3), (9, 14500, 1), (40, 16000, 0)])
+def test_long_rows(n, f, pad, dtype):
+    run_case(1, n, f, "rows", dtype, pad=pad)
