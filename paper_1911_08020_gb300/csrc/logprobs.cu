@@ -949,9 +949,9 @@ constexpr int kGradUnroll = 4;
 
 // Rows whose logits and gradients start alike past a 16-byte boundary: four
 // granules a thread in flight.  Bound by memory: 4096 x 32000 bf16 with an entropy
-// gradient 87 us (6.0 TB/s; 96 before the arithmetic was paired).
-template <typename T>
-__global__ void __launch_bounds__(kGradThreads) grad_rows_kernel(const GradArgs a, int32_t parts) {
+// gradient 78 us (6.8 TB/s).
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS) grad_rows_kernel(const GradArgs a, int32_t parts) {
     constexpr int V = kPerGranule<T>, U = kGradUnroll;
     pdl_wait_previous();
     pdl_launch_dependents();
@@ -961,34 +961,52 @@ __global__ void __launch_bounds__(kGradThreads) grad_rows_kernel(const GradArgs 
     T *out = static_cast<T *>(a.dx) + token * a.ldd;
     const int head = row_head<T>(row);
     const int32_t n = a.vocab, granules = int32_t(row_granules<T>(head, n));
-    const int32_t first = part * (kGradThreads * U), g0 = first + int32_t(threadIdx.x);
+    const int32_t first = part * (THREADS * U), g0 = first + int32_t(threadIdx.x);
     // (plain loads: the gradient may take the logits' place)
-    if (first >= (head > 0 ? 1 : 0) && first + kGradThreads * U <= (head + n) / V) {   // granules all in the row
+    if (first >= (head > 0 ? 1 : 0) && first + THREADS * U <= (head + n) / V) {   // granules all in the row
         const uint4 *in = reinterpret_cast<const uint4 *>(row - head) + g0;
         uint4 *to = reinterpret_cast<uint4 *>(out - head) + g0;
         uint4 q[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) q[u] = in[u * kGradThreads];
+        for (int u = 0; u < U; ++u) q[u] = in[u * THREADS];
         const GradToken t = grad_token(a, token);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             Pair v[V / 2];
             unpack(q[u], v);
-            grad_of(t, v, (g0 + u * kGradThreads) * V - head, 1);
-            to[u * kGradThreads] = pack(v);
+            grad_of(t, v, (g0 + u * THREADS) * V - head, 1);
+            to[u * THREADS] = pack(v);
         }
         return;
     }
-    const GradToken t = grad_token(a, token);
-    for (int32_t g = g0; g < min(granules, first + kGradThreads * U); g += kGradThreads) {
-        const int64_t j0 = int64_t(g) * V - head;
-        Pair v[V / 2];
-        unpack(load_granule<T, false>(row, j0, n, -INFINITY), v);
-        grad_of(t, v, int32_t(j0), 1);
-        float w[V];
+    // Parts with an end of the row, or past it: four granules in flight as well in
+    // bf16; in fp32 one, as that leaves 32 registers a thread and not 48, and more threads
+    // (2000 x 5000: 14.0 us, with four 16.1; bf16, 5000 x 5000: 27.6 and 17.6).
+    constexpr int B = sizeof(T) == 4 ? 1 : U;
+    const GradToken t = B == 1 ? grad_token(a, token) : GradToken{};
+#pragma unroll 1
+    for (int b = 0; b < U / B; ++b) {
+        const int32_t at = g0 + b * B * THREADS;
+        uint4 q[B];
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) w[2 * i] = low(v[i]), w[2 * i + 1] = high(v[i]);
-        store_granule(out, j0, n, w);
+        for (int u = 0; u < B; ++u) {
+            const int32_t g = at + u * THREADS;
+            if (g < granules) q[u] = load_granule<T, false>(row, int64_t(g) * V - head, n, -INFINITY);
+        }
+        const GradToken own = B == 1 ? t : grad_token(a, token);   // (after the loads)
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+            const int32_t g = at + u * THREADS;
+            if (g >= granules) return;
+            const int64_t j0 = int64_t(g) * V - head;
+            Pair v[V / 2];
+            unpack(q[u], v);
+            grad_of(own, v, int32_t(j0), 1);
+            float w[V];
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) w[2 * i] = low(v[i]), w[2 * i + 1] = high(v[i]);
+            store_granule(out, j0, n, w);
+        }
     }
 }
 
@@ -1080,11 +1098,29 @@ cudaError_t launch_grad(const GradArgs &a, darb_layout_t layout, cudaStream_t st
     }
     // logits and gradients of every row start alike past a 16-byte boundary
     const bool alike = row_head<T>(a.x) == row_head<T>(a.dx) && (a.tokens == 1 || (a.ld - a.ldd) * int64_t(sizeof(T)) % 16 == 0);
-    const int64_t per = alike ? int64_t(kGradThreads) * kGradUnroll * kPerGranule<T> : int64_t(kGradThreads) * 8;
-    const int32_t parts = int32_t((a.vocab + kPerGranule<T> - 1 + per - 1) / per);
+    if (alike) {
+        const int64_t granules = row_granules<T>(kPerGranule<T> - 1, a.vocab);
+        const auto rows = [&](auto threads) {
+            const int64_t parts = (granules + threads.value * kGradUnroll - 1) / (threads.value * kGradUnroll);
+            if (a.tokens * parts > INT32_MAX) return cudaErrorNotSupported;
+            return launch_ex(grad_rows_kernel<T, threads.value>, grid(a.tokens * parts), dim3(threads.value), 0, stream, 1, true, a,
+                             int32_t(parts));
+        };
+        // Small CTAs: the loads of one in the time of another's stores.  bf16: one part a row
+        // or 64 threads (1896 x 2783: 4.3 us, with 64 5.3, with 256 5.5; 4096 x 32000 78, with
+        // 256 87).  fp32: 64 for many short rows (3230 x 1656: 9.4 us, with 256 11.1; 700 x 10000
+        // 11.4 and 10.5; 100 x 1000 2.4 and 1.7).
+        if constexpr (sizeof(T) == 2) {
+            if (granules > 256 && granules <= 512) return rows(std::integral_constant<int, 128>());
+            return rows(std::integral_constant<int, 64>());
+        } else {
+            if (granules <= 512 && a.tokens >= 4 * sm_count()) return rows(std::integral_constant<int, 64>());
+            return rows(std::integral_constant<int, kGradThreads>());
+        }
+    }
+    const int32_t parts = int32_t((a.vocab + kGradThreads * 8 - 1) / (kGradThreads * 8));
     const int64_t blocks = a.tokens * parts;
     if (blocks > INT32_MAX) return cudaErrorNotSupported;
-    if (alike) return launch_ex(grad_rows_kernel<T>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
     return launch_ex(grad_any_kernel<T, false>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
 }
 
