@@ -1018,9 +1018,11 @@ __global__ void __launch_bounds__(kGradThreads) grad_any_kernel(const GradArgs a
     pdl_wait_previous();
     pdl_launch_dependents();
     // columns: 32 tokens x 8 rows of threads; rows: one token
-    const int64_t token = COLUMNS ? int64_t(blockIdx.x / parts) * 32 + (threadIdx.x & 31) : blockIdx.x / parts;
+    // (columns: consecutive CTAs take neighbouring tokens of the same rows)
+    const int32_t tiles = COLUMNS ? int32_t((a.tokens + 31) / 32) : 1;
+    const int64_t token = COLUMNS ? int64_t(blockIdx.x % tiles) * 32 + (threadIdx.x & 31) : blockIdx.x / parts;
     if (token >= a.tokens) return;
-    const int32_t part = int32_t(blockIdx.x % parts), step = COLUMNS ? kGradThreads / 32 : kGradThreads;
+    const int32_t part = int32_t(COLUMNS ? blockIdx.x / tiles : blockIdx.x % parts), step = COLUMNS ? kGradThreads / 32 : kGradThreads;
     const int32_t v0 = part * (step * U) + int32_t(COLUMNS ? threadIdx.x >> 5 : threadIdx.x);
     const T *x = static_cast<const T *>(a.x) + (COLUMNS ? v0 * a.ld + token : token * a.ld + v0);
     T *dx = static_cast<T *>(a.dx) + (COLUMNS ? v0 * a.ldd + token : token * a.ldd + v0);
@@ -1039,39 +1041,20 @@ __global__ void __launch_bounds__(kGradThreads) grad_any_kernel(const GradArgs a
         if (whole || v0 + u * step < a.vocab) dx[u * by_out] = narrow<T>(u & 1 ? high(v[u / 2]) : low(v[u / 2]));
 }
 
-// Columns whose rows can be read two tokens at a time: 64 tokens x 8 rows of
-// threads, U rows each, a pair the same entry of two tokens.  700 x 10000 fp32
-// 11.3 us (5.0 TB/s), 226 x 22765 bf16 6.3 us (one token at a time 9.6).
-template <typename T>
-__global__ void __launch_bounds__(kGradThreads) grad_columns_kernel(const GradArgs a, int32_t parts) {
-    constexpr int U = 8, ROWS = kGradThreads / 32;
+// Rows v0, v0 + ROWS, ... of two neighbouring tokens, N of them, or with GUARD those
+// below the vocabulary's end.
+template <typename T, int N, int ROWS, bool GUARD>
+__device__ __forceinline__ void grad_pairs(const GradArgs &a, int64_t token, const T *x, T *dx, int64_t by, int64_t by_out, int32_t v0) {
     using Two = typename std::conditional<sizeof(T) == 4, uint2, uint32_t>::type;
-    pdl_wait_previous();
-    pdl_launch_dependents();
-    const int64_t token = int64_t(blockIdx.x / parts) * 64 + 2 * (threadIdx.x & 31);
-    if (token >= a.tokens) return;
-    const int32_t v0 = int32_t(blockIdx.x % parts) * (ROWS * U) + int32_t(threadIdx.x >> 5);
-    const T *x = static_cast<const T *>(a.x) + v0 * a.ld + token;
-    T *dx = static_cast<T *>(a.dx) + v0 * a.ldd + token;
-    const int64_t by = ROWS * a.ld, by_out = ROWS * a.ldd;
-    if (token + 1 == a.tokens || v0 + (U - 1) * ROWS >= a.vocab) {   // one by one
-        for (int k = 0; k < 2 && token + k < a.tokens; ++k) {
-            const GradToken t = grad_token(a, token + k);
-            for (int32_t u = 0, v = v0; v < a.vocab && u < U; ++u, v += ROWS) {
-                Pair g[1] = {both(widen(x[u * by + k]))};
-                grad_of(t, g, v, a.vocab);   // (the second value is nobody's)
-                dx[u * by_out + k] = narrow<T>(low(g[0]));
-            }
-        }
-        return;
-    }
-    Two q[U];
+    Two q[N];
 #pragma unroll
-    for (int u = 0; u < U; ++u, x += by) q[u] = *reinterpret_cast<const Two *>(x);
+    for (int u = 0; u < N; ++u, x += by)
+        if (!GUARD || v0 + u * ROWS < a.vocab) q[u] = *reinterpret_cast<const Two *>(x);
     const GradToken t0 = grad_token(a, token), t1 = grad_token(a, token + 1);
     const Pair lse = pair(-t0.lse, -t1.lse), log2e = both(kLog2e), b = pair(-t0.b, -t1.b), c = pair(-t0.c, -t1.c);
 #pragma unroll
-    for (int u = 0; u < U; ++u, dx += by_out) {
+    for (int u = 0; u < N; ++u, dx += by_out) {
+        if (GUARD && v0 + u * ROWS >= a.vocab) return;
         Pair l;
         if constexpr (sizeof(T) == 4) l = pair(__uint_as_float(q[u].x), __uint_as_float(q[u].y));
         else l = pair(widen2(q[u]).x, widen2(q[u]).y);
@@ -1082,6 +1065,41 @@ __global__ void __launch_bounds__(kGradThreads) grad_columns_kernel(const GradAr
         const float g0 = low(g) + (v == t0.target ? t0.a : 0.0f), g1 = high(g) + (v == t1.target ? t1.a : 0.0f);
         if constexpr (sizeof(T) == 4) *reinterpret_cast<float2 *>(dx) = make_float2(g0, g1);
         else *reinterpret_cast<__nv_bfloat162 *>(dx) = __floats2bfloat162_rn(g0, g1);
+    }
+}
+
+// Columns whose rows can be read two tokens at a time: 64 tokens x 8 rows of
+// threads, U rows each, a pair the same entry of two tokens.  Consecutive CTAs
+// take neighbouring tokens, so that whole rows are read at about the same time.
+// 700 x 10000 fp32 10.5 us (5.4 TB/s), 300 x 128000 fp32 45 (6.8 TB/s; consecutive
+// CTAs down the rows of the same tokens: 65), 860 x 50000 bf16 35 (39).
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) grad_columns_kernel(const GradArgs a, int32_t parts) {
+    constexpr int U = 8, ROWS = kGradThreads / 32;
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    // (consecutive CTAs take neighbouring tokens of the same rows)
+    const int32_t tiles = int32_t((a.tokens + 63) / 64);
+    const int64_t token = int64_t(blockIdx.x % tiles) * 64 + 2 * (threadIdx.x & 31);
+    if (token >= a.tokens) return;
+    const int32_t v0 = int32_t(blockIdx.x / tiles) * (ROWS * U) + int32_t(threadIdx.x >> 5);
+    const T *x = static_cast<const T *>(a.x) + v0 * a.ld + token;
+    T *dx = static_cast<T *>(a.dx) + v0 * a.ldd + token;
+    const int64_t by = ROWS * a.ld, by_out = ROWS * a.ldd;
+    if (token + 1 == a.tokens) {   // the last one, alone
+        const GradToken t = grad_token(a, token);
+        for (int32_t u = 0, v = v0; v < a.vocab && u < U; ++u, v += ROWS) {
+            Pair g[1] = {both(widen(x[u * by]))};
+            grad_of(t, g, v, a.vocab);   // (the second value is nobody's)
+            dx[u * by_out] = narrow<T>(low(g[0]));
+        }
+        return;
+    }
+    if (v0 + (U - 1) * ROWS < a.vocab) {
+        grad_pairs<T, U, ROWS, false>(a, token, x, dx, by, by_out, v0);
+    } else {   // (fewer at a time: the registers are the other way's)
+        for (int32_t u = 0; u < U && v0 + u * ROWS < a.vocab; u += U / 4)
+            grad_pairs<T, U / 4, ROWS, true>(a, token, x + u * by, dx + u * by_out, by, by_out, v0 + u * ROWS);
     }
 }
 
