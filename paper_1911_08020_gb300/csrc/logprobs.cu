@@ -1013,7 +1013,7 @@ __global__ void __launch_bounds__(THREADS) grad_rows_kernel(const GradArgs a, in
 // Rows that do not start alike, and columns: consecutive threads take
 // consecutive elements of the contiguous axis, U of them each.
 template <typename T, bool COLUMNS>
-__global__ void __launch_bounds__(kGradThreads) grad_any_kernel(const GradArgs a, int32_t parts) {
+__global__ void __launch_bounds__(kGradThreads) grad_any_kernel(const GradArgs a, int32_t parts) {   // (parts of a row; columns need none)
     constexpr int U = 8;
     pdl_wait_previous();
     pdl_launch_dependents();
@@ -1074,7 +1074,7 @@ __device__ __forceinline__ void grad_pairs(const GradArgs &a, int64_t token, con
 // 700 x 10000 fp32 10.5 us (5.4 TB/s), 300 x 128000 fp32 45 (6.8 TB/s; consecutive
 // CTAs down the rows of the same tokens: 65), 860 x 50000 bf16 35 (39).
 template <typename T>
-__global__ void __launch_bounds__(kGradThreads) grad_columns_kernel(const GradArgs a, int32_t parts) {
+__global__ void __launch_bounds__(kGradThreads) grad_columns_kernel(const GradArgs a) {
     constexpr int U = 8, ROWS = kGradThreads / 32;
     pdl_wait_previous();
     pdl_launch_dependents();
@@ -1111,7 +1111,7 @@ cudaError_t launch_grad(const GradArgs &a, darb_layout_t layout, cudaStream_t st
         const bool pairs = a.tokens > 32 && a.ld % 2 == 0 && a.ldd % 2 == 0 && aligned_to(a.x, 2 * sizeof(T)) && aligned_to(a.dx, 2 * sizeof(T));
         const int64_t blocks = (pairs ? (a.tokens + 63) / 64 : (a.tokens + 31) / 32) * parts;
         if (blocks > INT32_MAX) return cudaErrorNotSupported;
-        if (pairs) return launch_ex(grad_columns_kernel<T>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
+        if (pairs) return launch_ex(grad_columns_kernel<T>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a);
         return launch_ex(grad_any_kernel<T, true>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
     }
     // logits and gradients of every row start alike past a 16-byte boundary
