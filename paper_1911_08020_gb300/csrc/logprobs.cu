@@ -342,7 +342,7 @@ inline Blocks blocks_of(int64_t rounds, int most) {
 constexpr int kRowSlots = 32;   // of the table of maxima, at most
 
 // One read of the logits; bound by memory, and with alternatives by the barriers
-// of the joins.  A CTA, or a cluster where there are fewer tokens than SMs, takes a
+// of the joins.  A CTA, or a cluster where rows are long and tokens few, takes a
 // token.  The main loop keeps one maximum, one reference and two pairs of sums a
 // thread: a block of U granules is clamped and its maximum taken (in bf16 two
 // logits an instruction), the sums are moved to the new reference once a block,
