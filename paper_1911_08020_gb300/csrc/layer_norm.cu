@@ -1129,7 +1129,11 @@ cudaError_t launch_norm(const NormArgs &a, darb_layout_t layout, cudaStream_t st
                 e = launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * stages, stream, 1, true, a,
                               p.stage_bytes);
         };
-        rows(norm_rows_kernel<T, VPT / 2, 3, 128>, VPT / 2, 128, 3);
+        // 16 features a thread, while that leaves enough rows at a time on an SM: 12000 x 2500
+        // bf16 (160 threads) 33 us, with 32 features 41; 8000 x 4096 fp32 43 and 48; 300 x 4096
+        // bf16 3.3 and 4.0; but 8191 x 4096 bf16 34 and 30, 10000 x 3300 48 and 41
+        const bool wide = sizeof(T) == 4 || a.tokens <= 2 * int64_t(sm_count());
+        rows(norm_rows_kernel<T, VPT / 2, 3, kHalfThreads>, VPT / 2, wide ? kHalfThreads : 160, 3);
         rows(norm_rows_kernel<T, VPT, 3, 256>, VPT, 256, 3);
         rows(norm_rows_kernel<T, VPT, 3, kRowThreads>, VPT, kRowThreads, 3);
         if (e != cudaErrorNotSupported) return e;
