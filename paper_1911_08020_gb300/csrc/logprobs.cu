@@ -134,7 +134,8 @@ struct Token {
         return (wide ? (x - m) * kLog2e - log2s : fmaf(x, kLog2e, -r) - log2s) * kLn2;
     }
     __device__ float entropy() const { return empty ? 0.0f : (log2s - t_s) * kLn2; }
-    __device__ float lse() const { return empty ? -INFINITY : wide ? m + log2s * kLn2 : (r + log2s) * kLn2; }
+    // r is m log2(e) but for its rounding, which belongs to log2s: one rounding at the size of m is left
+    __device__ float lse() const { return empty ? -INFINITY : fmaf(wide ? log2s : log2s + fmaf(-m, kLog2e, r), kLn2, m); }
 };
 __device__ __forceinline__ Token token_of(const Part &p) {
     return {reference(p.m), p.m, log2f(p.s), p.t / p.s, false, false};
@@ -898,6 +899,17 @@ struct GradArgs {
     const float *lse, *entropy, *d_logprob, *d_entropy;   // or null, but lse
 };
 
+// lse is one fp32 number: half a unit in its last place is 2^-16 below 512, and
+// p_v as far off (relative to itself; the logits of trained models are within
+// +-100, where it is 2^-18).  Past 512 it is more, and from 2^24 on lse says nothing
+// of log sum exp(x - M) any more.  The sums of such a token are taken again from its
+// logits, as differences from their maximum.  A single CTA (of columns, a warp) does
+// that and writes the whole token, as the gradient may take the logits' place: the
+// others that share the token leave it alone.  Asking costs ordinary columns some 0.1 to
+// 0.3 us, rows less.
+constexpr float kWideLse = 512.0f;
+__device__ __forceinline__ bool is_wide_lse(float lse) { return __builtin_expect(fabsf(lse) > kWideLse, false); }   // (of a token with an entry)
+
 // What a token's gradient is made from:  dx_v = a [v = target] - p_v (b log p_v + c),
 // c = a + b H.
 struct GradToken {
@@ -924,6 +936,61 @@ __device__ __forceinline__ GradToken grad_token(const GradArgs &g, int64_t token
     return t;
 }
 
+// A wide token: its maximum and log2 of its sum.
+struct WideToken {
+    float m, log2s;
+    __device__ float grad(const GradToken &t, float x, int32_t v) const {
+        const float d = max_nan((x - m) * kLog2e, kMasked) - log2s;
+        const float g = m == -INFINITY ? 0.0f * t.c : exp2_fast(d) * fmaf(d * kLn2, -t.b, -t.c);
+        return v == t.target ? g + t.a : g;
+    }
+};
+
+// The gradient of one wide row by the CTA.  (Not inlined: the kernels' registers
+// are for their own way.)
+template <typename T, typename Args>
+__device__ __noinline__ void wide_row(Args a, int64_t token, const T *x, int64_t step, T *dx, int64_t step_out) {
+    __shared__ float buf[33];
+    const GradToken t = grad_token(a, token);
+    const Token tok = wide_token(x, step, a.vocab, buf);
+    const WideToken k = {tok.m, tok.log2s};
+    for (int32_t i = threadIdx.x; i < a.vocab; i += blockDim.x) dx[int64_t(i) * step_out] = narrow<T>(k.grad(t, widen(x[int64_t(i) * step]), i));
+}
+
+// The wide tokens of a tile of 32 columns (PAIRS: and those that are read with one),
+// by a CTA of its own: a warp takes 4 of them and 8 rows at a time.
+constexpr int kGradThreads = 256;
+template <typename T, bool PAIRS>
+__device__ __noinline__ void wide_tile(const GradArgs a, int64_t tile) {
+    static_assert(kGradThreads == 256, "8 warps of 4 tokens");
+    const int lane = threadIdx.x & 31;
+    const int64_t token = tile * 32 + (threadIdx.x >> 5) * 4 + (lane & 3);
+    bool wide = token < a.tokens && is_wide_lse(a.lse[token]) && a.lse[token] != -INFINITY;
+    if (PAIRS) {
+        const int other = __shfl_xor_sync(0xFFFFFFFFu, int(wide), 1);   // (all lanes)
+        wide = token < a.tokens && (wide || other != 0);
+    }
+    if (!__any_sync(0xFFFFFFFFu, wide)) return;
+    const T *x = static_cast<const T *>(a.x) + token;
+    T *dx = static_cast<T *>(a.dx) + token;
+    const int32_t n = wide ? a.vocab : 0;   // (a lane without a wide token goes along)
+    float m = -INFINITY, s = 0.0f;
+    for (int32_t v = lane >> 2; v < n; v += 8) m = max_nan(m, widen(x[v * a.ld]));
+#pragma unroll
+    for (int o = 4; o < 32; o *= 2) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    for (int32_t v0 = lane >> 2; v0 < n; v0 += 8 * 256) {   // (256 terms first)
+        float block = 0.0f;
+        for (int32_t v = v0; v < n && v < v0 + 8 * 256; v += 8) block += exp2_fast(max_nan((widen(x[v * a.ld]) - m) * kLog2e, kMasked));
+        s += block;
+    }
+#pragma unroll
+    for (int o = 4; o < 32; o *= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (!wide) return;
+    const GradToken t = grad_token(a, token);
+    const WideToken k = {m, log2f(s)};
+    for (int32_t v = lane >> 2; v < n; v += 8) dx[v * a.ldd] = narrow<T>(k.grad(t, widen(x[v * a.ld]), v));
+}
+
 // N logits of one token, from v0 on `step` apart, to their gradients.  A masked
 // entry has p = 0; log p is held above -2^15 or so, so that it adds 0 there.
 template <int N>
@@ -944,14 +1011,13 @@ __device__ __forceinline__ void grad_of(const GradToken &t, Pair (&x)[N], int32_
     }
 }
 
-constexpr int kGradThreads = 256;
 constexpr int kGradUnroll = 4;
 
 // Rows whose logits and gradients start alike past a 16-byte boundary: four
 // granules a thread in flight.  Bound by memory: 4096 x 32000 bf16 with an entropy
 // gradient 78 us (6.8 TB/s).
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS) grad_rows_kernel(const GradArgs a, int32_t parts) {
+__global__ void __launch_bounds__(THREADS) grad_rows_kernel(const __grid_constant__ GradArgs a, int32_t parts) {
     constexpr int V = kPerGranule<T>, U = kGradUnroll;
     pdl_wait_previous();
     pdl_launch_dependents();
@@ -970,6 +1036,10 @@ __global__ void __launch_bounds__(THREADS) grad_rows_kernel(const GradArgs a, in
 #pragma unroll
         for (int u = 0; u < U; ++u) q[u] = in[u * THREADS];
         const GradToken t = grad_token(a, token);
+        if (is_wide_lse(t.lse)) {
+            if (part == 0) wide_row<T, const GradArgs &>(a, token, row, 1, out, 1);
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             Pair v[V / 2];
@@ -994,6 +1064,10 @@ __global__ void __launch_bounds__(THREADS) grad_rows_kernel(const GradArgs a, in
             if (g < granules) q[u] = load_granule<T, false>(row, int64_t(g) * V - head, n, -INFINITY);
         }
         const GradToken own = B == 1 ? t : grad_token(a, token);   // (after the loads)
+        if (is_wide_lse(own.lse)) {   // (in the first round, and for all threads)
+            if (part == 0) wide_row<T, const GradArgs &>(a, token, row, 1, out, 1);
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < B; ++u) {
             const int32_t g = at + u * THREADS;
@@ -1011,18 +1085,21 @@ __global__ void __launch_bounds__(THREADS) grad_rows_kernel(const GradArgs a, in
 }
 
 // Rows that do not start alike, and columns: consecutive threads take
-// consecutive elements of the contiguous axis, U of them each.
+// consecutive elements of the contiguous axis, U of them each.  32 registers a thread
+// in fp32 (5184 x 175 columns 2.8 us, with 34 3.6), 40 in bf16 (52783 x 30 3.8 us, with 32 4.3).
 template <typename T, bool COLUMNS>
-__global__ void __launch_bounds__(kGradThreads) grad_any_kernel(const GradArgs a, int32_t parts) {   // (parts of a row; columns need none)
+__global__ void __launch_bounds__(kGradThreads, sizeof(T) == 4 ? 8 : 6) grad_any_kernel(const GradArgs a, int32_t parts) {   // (parts of a row; columns need none)
     constexpr int U = 8;
     pdl_wait_previous();
     pdl_launch_dependents();
     // columns: 32 tokens x 8 rows of threads; rows: one token
-    // (columns: consecutive CTAs take neighbouring tokens of the same rows)
+    // (columns: consecutive CTAs take neighbouring tokens of the same rows, after a CTA a tile for its wide tokens)
     const int32_t tiles = COLUMNS ? int32_t((a.tokens + 31) / 32) : 1;
-    const int64_t token = COLUMNS ? int64_t(blockIdx.x % tiles) * 32 + (threadIdx.x & 31) : blockIdx.x / parts;
+    const int32_t cta = COLUMNS ? int32_t(blockIdx.x) - tiles : int32_t(blockIdx.x);
+    if (COLUMNS && cta < 0) return wide_tile<T, false>(a, blockIdx.x);
+    const int64_t token = COLUMNS ? int64_t(cta % tiles) * 32 + (threadIdx.x & 31) : cta / parts;
     if (token >= a.tokens) return;
-    const int32_t part = int32_t(COLUMNS ? blockIdx.x / tiles : blockIdx.x % parts), step = COLUMNS ? kGradThreads / 32 : kGradThreads;
+    const int32_t part = COLUMNS ? cta / tiles : cta % parts, step = COLUMNS ? kGradThreads / 32 : kGradThreads;
     const int32_t v0 = part * (step * U) + int32_t(COLUMNS ? threadIdx.x >> 5 : threadIdx.x);
     const T *x = static_cast<const T *>(a.x) + (COLUMNS ? v0 * a.ld + token : token * a.ld + v0);
     T *dx = static_cast<T *>(a.dx) + (COLUMNS ? v0 * a.ldd + token : token * a.ldd + v0);
@@ -1035,10 +1112,13 @@ __global__ void __launch_bounds__(kGradThreads) grad_any_kernel(const GradArgs a
         v[u / 2] = pair(lo, whole || v0 + (u + 1) * step < a.vocab ? widen(x[(u + 1) * by]) : 0.0f);
     }
     const GradToken t = grad_token(a, token);
+    const bool wide = is_wide_lse(t.lse);
     grad_of(t, v, v0, step);
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (whole || v0 + u * step < a.vocab) dx[u * by_out] = narrow<T>(u & 1 ? high(v[u / 2]) : low(v[u / 2]));
+        if (!wide && (whole || v0 + u * step < a.vocab)) dx[u * by_out] = narrow<T>(u & 1 ? high(v[u / 2]) : low(v[u / 2]));
+    if (!COLUMNS && wide && part == 0)
+        wide_row<T, GradArgs>(a, token, static_cast<const T *>(a.x) + token * a.ld, 1, static_cast<T *>(a.dx) + token * a.ldd, 1);
 }
 
 // Rows v0, v0 + ROWS, ... of two neighbouring tokens, N of them, or with GUARD those
@@ -1052,6 +1132,7 @@ __device__ __forceinline__ void grad_pairs(const GradArgs &a, int64_t token, con
         if (!GUARD || v0 + u * ROWS < a.vocab) q[u] = *reinterpret_cast<const Two *>(x);
     const GradToken t0 = grad_token(a, token), t1 = grad_token(a, token + 1);
     const Pair lse = pair(-t0.lse, -t1.lse), log2e = both(kLog2e), b = pair(-t0.b, -t1.b), c = pair(-t0.c, -t1.c);
+    const bool wide = is_wide_lse(t0.lse) || is_wide_lse(t1.lse);
 #pragma unroll
     for (int u = 0; u < N; ++u, dx += by_out) {
         if (GUARD && v0 + u * ROWS >= a.vocab) return;
@@ -1063,6 +1144,7 @@ __device__ __forceinline__ void grad_pairs(const GradArgs &a, int64_t token, con
         const Pair d = mul2(l, log2e), g = mul2(pair(exp2_fast(low(d)), exp2_fast(high(d))), fma2(l, b, c));
         const int32_t v = v0 + u * ROWS;
         const float g0 = low(g) + (v == t0.target ? t0.a : 0.0f), g1 = high(g) + (v == t1.target ? t1.a : 0.0f);
+        if (wide) continue;
         if constexpr (sizeof(T) == 4) *reinterpret_cast<float2 *>(dx) = make_float2(g0, g1);
         else *reinterpret_cast<__nv_bfloat162 *>(dx) = __floats2bfloat162_rn(g0, g1);
     }
@@ -1074,20 +1156,22 @@ __device__ __forceinline__ void grad_pairs(const GradArgs &a, int64_t token, con
 // 700 x 10000 fp32 10.5 us (5.4 TB/s), 300 x 128000 fp32 45 (6.8 TB/s; consecutive
 // CTAs down the rows of the same tokens: 65), 860 x 50000 bf16 35 (39).
 template <typename T>
-__global__ void __launch_bounds__(kGradThreads) grad_columns_kernel(const GradArgs a) {
+__global__ void __launch_bounds__(kGradThreads, 5) grad_columns_kernel(const GradArgs a) {
     constexpr int U = 8, ROWS = kGradThreads / 32;
     pdl_wait_previous();
     pdl_launch_dependents();
-    // (consecutive CTAs take neighbouring tokens of the same rows)
-    const int32_t tiles = int32_t((a.tokens + 63) / 64);
-    const int64_t token = int64_t(blockIdx.x % tiles) * 64 + 2 * (threadIdx.x & 31);
+    // (consecutive CTAs take neighbouring tokens of the same rows, after one for the wide tokens of every 32)
+    const int32_t tiles = int32_t((a.tokens + 63) / 64), cta = int32_t(blockIdx.x) - int32_t((a.tokens + 31) / 32);
+    if (cta < 0) return wide_tile<T, true>(a, blockIdx.x);
+    const int64_t token = int64_t(cta % tiles) * 64 + 2 * (threadIdx.x & 31);
     if (token >= a.tokens) return;
-    const int32_t v0 = int32_t(blockIdx.x / tiles) * (ROWS * U) + int32_t(threadIdx.x >> 5);
+    const int32_t v0 = cta / tiles * (ROWS * U) + int32_t(threadIdx.x >> 5);
     const T *x = static_cast<const T *>(a.x) + v0 * a.ld + token;
     T *dx = static_cast<T *>(a.dx) + v0 * a.ldd + token;
     const int64_t by = ROWS * a.ld, by_out = ROWS * a.ldd;
     if (token + 1 == a.tokens) {   // the last one, alone
         const GradToken t = grad_token(a, token);
+        if (is_wide_lse(t.lse)) return;
         for (int32_t u = 0, v = v0; v < a.vocab && u < U; ++u, v += ROWS) {
             Pair g[1] = {both(widen(x[u * by]))};
             grad_of(t, g, v, a.vocab);   // (the second value is nobody's)
@@ -1109,7 +1193,7 @@ cudaError_t launch_grad(const GradArgs &a, darb_layout_t layout, cudaStream_t st
     if (layout == DARB_TOKEN_COLUMNS) {
         const int32_t parts = int32_t((a.vocab + 63) / 64);
         const bool pairs = a.tokens > 32 && a.ld % 2 == 0 && a.ldd % 2 == 0 && aligned_to(a.x, 2 * sizeof(T)) && aligned_to(a.dx, 2 * sizeof(T));
-        const int64_t blocks = (pairs ? (a.tokens + 63) / 64 : (a.tokens + 31) / 32) * parts;
+        const int64_t tiles = (a.tokens + 31) / 32, blocks = (pairs ? (a.tokens + 63) / 64 : tiles) * parts + tiles;
         if (blocks > INT32_MAX) return cudaErrorNotSupported;
         if (pairs) return launch_ex(grad_columns_kernel<T>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a);
         return launch_ex(grad_any_kernel<T, true>, grid(blocks), dim3(kGradThreads), 0, stream, 1, true, a, parts);
