@@ -7,9 +7,10 @@ back, one AdamW step updates the dense weights, and the layer is encoded again:
     darb_layer_norm -> darb_spmm -> darb_token_logprobs -> darb_token_logprobs_grad
       -> darb_layer_norm_grad -> darb_adamw_step -> darb_reencode
 
-The products of the backward pass are plain dense ones and pass the pruning straight through: the
-gradient of a pruned weight is that of the weight at its place, so that the best weight of a block
-can change from one encode to the next.
+The products of the backward pass are plain dense ones (library calls).  The gradient of the layer's input
+is that of the pruned layer, whose dense form is the product with the identity.  The gradient of the weights
+passes the pruning straight through: that of a pruned weight is that of the weight at its place, so that
+the best weight of a block can change from one encode to the next.
 """
 from __future__ import annotations
 
@@ -27,6 +28,7 @@ class Head:
     def __init__(self, vocab: int, features: int, block: int, lr: float = 2e-3, states: str = "e4m3", seed: int = 0):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         self.W = torch.randn(vocab, features, generator=gen, device="cuda") / math.sqrt(features)
+        self.eye = torch.eye(features, device="cuda")
         self.gamma, self.beta = torch.ones(features, device="cuda"), torch.zeros(features, device="cuda")
         self.stored = self.W.to(torch.bfloat16)   # what is encoded
         self.handle = darb.darb_encode(self.stored, np.full(vocab, block, np.int32))
@@ -59,7 +61,7 @@ class Head:
         scores = darb.darb_token_logprobs(logits, words, dim=0)
         d_logprob = torch.full_like(scores.logprob, -1.0 / h.shape[1])
         d_logits = darb.darb_token_logprobs_grad(logits, words, scores.lse, d_logprob, dim=0, out=logits)
-        dW, dx = d_logits @ x.t(), self.W.t() @ d_logits
+        dW, dx = d_logits @ x.t(), darb.darb_spmm(self.handle, self.eye).t() @ d_logits
         _, d_gamma, d_beta = darb.darb_layer_norm_grad(dx, h, self.gamma, mean, rstd, dim=0, dx=dx)
         self.step += 1
         darb.darb_adamw_step(self.plan, [dW, d_gamma, d_beta], self.step, self.lr)
