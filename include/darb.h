@@ -399,8 +399,9 @@ DARB_API darb_status_t darb_rnn_reserve(darb_handle_t h, int64_t max_batch);
  *            allowed when k == 0
  * A logit of -inf is a masked entry (p = 0).  A token whose entries are all -inf
  * has lse and log probabilities of -inf and an entropy of 0.  A token with a NaN or
- * +inf among its logits has NaN results (its top_index stands).  All sums are
- * fp32 and in a fixed order.  tokens == 0 does nothing.
+ * +inf among its logits has NaN results (its top_index stands).  No other log
+ * probability is above 0 and no other entropy below it.  All sums are fp32 and in
+ * a fixed order.  tokens == 0 does nothing.
  * No output may overlap another buffer of the call.  Asynchronous on `stream`;
  * allocates nothing; one launch.
  * Errors: DARB_ERR_INVALID_ARG; DARB_ERR_UNSUPPORTED (more than 2^27 tokens,

@@ -125,15 +125,21 @@ __device__ __forceinline__ int32_t index_of(uint64_t key) { return int32_t(0xFFF
 // What every output of a token is made from.
 struct Token {
     float r;       // log2 units: the reference, (finite) M log2(e)
-    float m;       // M itself, for wide tokens
+    float m;       // M itself
     float log2s;   // log2 s
     float t_s;     // t / s
     bool wide, empty;
+    // (the roundings of a token with one entry can leave its log probability above and its
+    // entropy below 0; NaN stays)
     __device__ float logprob(float x) const {
         if (empty) return -INFINITY;
-        return (wide ? (x - m) * kLog2e - log2s : fmaf(x, kLog2e, -r) - log2s) * kLn2;
+        const float l = (wide ? (x - m) * kLog2e - log2s : fmaf(x, kLog2e, -r) - log2s) * kLn2;
+        return l > 0.0f ? 0.0f : l;
     }
-    __device__ float entropy() const { return empty ? 0.0f : (log2s - t_s) * kLn2; }
+    __device__ float entropy() const {
+        const float h = empty ? 0.0f : (log2s - t_s) * kLn2;
+        return h < 0.0f ? 0.0f : h;
+    }
     // r is m log2(e) but for its rounding, which belongs to log2s: one rounding at the size of m is left
     __device__ float lse() const { return empty ? -INFINITY : fmaf(wide ? log2s : log2s + fmaf(-m, kLog2e, r), kLn2, m); }
 };
