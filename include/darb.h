@@ -543,8 +543,8 @@ DARB_API darb_status_t darb_adamw_create(int32_t n, const int64_t *numel, float 
  * Asynchronous on `stream`; allocates nothing; one launch for every 448 tensors.
  * Steps of one plan must be ordered on one stream.
  * Errors: DARB_ERR_INVALID_ARG (an unknown plan, a step below 1, lr, eps or
- * weight_decay negative or not finite, a beta outside [0, 1), a gradient that
- * overlaps its tensor's buffers); DARB_ERR_CUDA.
+ * weight_decay negative or not finite, a beta outside [0, 1), a gradient or
+ * grad_scale that overlaps a buffer of any of the plan's tensors); DARB_ERR_CUDA.
  */
 DARB_API darb_status_t darb_adamw_step(darb_adamw_t plan, const void *const *grads, const float *grad_scale,
                                        int64_t step, uint64_t seed, double lr, double beta1, double beta2, double eps,

@@ -34,6 +34,7 @@
 #include <cfloat>
 #include <cmath>
 #include <cstdlib>
+#include <functional>
 #include <mutex>
 #include <new>
 #include <unordered_set>
@@ -522,6 +523,7 @@ using namespace darb;
 struct darb_adamw_s {
     std::vector<darb::Tensor> tensors;
     std::vector<int64_t> first_chunk;   // of every tensor, and the number of all
+    std::vector<darb::Range> written;   // all buffers that a step writes, in order of address, none twice
     darb_dtype_t gtype = DARB_F32;
     bool codes = false;
     void *dmem = nullptr;
@@ -540,17 +542,25 @@ bool live_plan(const darb_adamw_s *p) {
     return p != nullptr && g_plans.count(p) != 0;
 }
 
-// One past the buffers that tensor i writes, each with its bytes.
+// The buffers that a step writes of a tensor, each with its bytes.
 std::vector<Range> written(const Tensor &t, bool codes) {
     const int64_t blocks = (t.n + kBlock - 1) / kBlock, state = codes ? t.n : t.n * 4;
     return {{t.p, t.n * 4}, {t.m, state}, {t.v, state}, {t.m_scale, blocks * 4}, {t.v_scale, blocks * 4}, {t.copy, t.n * 2}};
+}
+
+// Whether the bytes from p on meet one of the plan's buffers.
+bool meets_written(const darb_adamw_s &plan, const void *p, int64_t bytes) {
+    const auto after = std::upper_bound(plan.written.begin(), plan.written.end(), p,
+                                        [](const void *q, const Range &r) { return std::less<const void *>()(q, r.p); });
+    if (after != plan.written.end() && ranges_overlap(after->p, after->bytes, p, bytes)) return true;
+    return after != plan.written.begin() && ranges_overlap((after - 1)->p, (after - 1)->bytes, p, bytes);
 }
 
 darb_status_t build_plan(darb_adamw_s *plan, int32_t n, const int64_t *numel, float *const *params, void *const *m,
                          void *const *v, float *const *m_scale, float *const *v_scale, void *const *copies,
                          cudaStream_t stream) {
     std::vector<Chunk> chunks;
-    std::vector<Range> all;
+    std::vector<Range> &all = plan->written;
     int64_t first = 0;
     for (int32_t i = 0; i < n; ++i) {
         if (numel[i] < 0) return DARB_ERR_INVALID_ARG;
@@ -584,7 +594,7 @@ darb_status_t build_plan(darb_adamw_s *plan, int32_t n, const int64_t *numel, fl
         plan->tensors.push_back(t);
     }
     plan->first_chunk.push_back(int64_t(chunks.size()));
-    std::sort(all.begin(), all.end(), [](const Range &a, const Range &b) { return a.p < b.p; });
+    std::sort(all.begin(), all.end(), [](const Range &a, const Range &b) { return std::less<const void *>()(a.p, b.p); });
     for (size_t i = 1; i < all.size(); ++i)
         if (ranges_overlap(all[i - 1].p, all[i - 1].bytes, all[i].p, all[i].bytes)) return DARB_ERR_INVALID_ARG;
     if (chunks.empty()) return DARB_OK;
@@ -662,16 +672,13 @@ darb_status_t darb_adamw_step(darb_adamw_t plan, const void *const *grads, const
     if (!(lr >= 0.0 && std::isfinite(lr)) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
         !(eps >= 0.0 && std::isfinite(eps)) || !(weight_decay >= 0.0 && std::isfinite(weight_decay)))
         return DARB_ERR_INVALID_ARG;
+    if (grad_scale != nullptr && meets_written(*plan, grad_scale, 4)) return DARB_ERR_INVALID_ARG;
     const size_t es = dtype_size(plan->gtype);
     const int32_t n = int32_t(plan->tensors.size());
     for (int32_t i = 0; i < n; ++i) {
         const Tensor &t = plan->tensors[i];
         if (grads[i] == nullptr || t.n == 0) continue;
-        if (!aligned_to(grads[i], es)) return DARB_ERR_INVALID_ARG;
-        const int64_t state = plan->codes ? t.n : t.n * 4, g = t.n * int64_t(es);
-        if (ranges_overlap(grads[i], g, t.p, t.n * 4) || ranges_overlap(grads[i], g, t.m, state) ||
-            ranges_overlap(grads[i], g, t.v, state) || ranges_overlap(grads[i], g, t.copy, t.n * 2))
-            return DARB_ERR_INVALID_ARG;
+        if (!aligned_to(grads[i], es) || meets_written(*plan, grads[i], t.n * int64_t(es))) return DARB_ERR_INVALID_ARG;
     }
     StepArgs a;
     a.tensors = plan->d_tensors;
