@@ -488,7 +488,8 @@ DARB_API darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const
                                             void *work, cudaStream_t stream);
 
 /* Bytes of scratch that darb_layer_norm_grad needs on the current device.
- * Errors: DARB_ERR_INVALID_ARG (sizes, null output).                          */
+ * Errors: DARB_ERR_INVALID_ARG (sizes, null output); DARB_ERR_UNSUPPORTED (sizes
+ * that darb_layer_norm_grad does not take).                                   */
 DARB_API darb_status_t darb_layer_norm_grad_work(darb_layout_t layout, int64_t steps, int64_t tokens, int64_t features,
                                                  int64_t *bytes);
 

@@ -1319,7 +1319,9 @@ darb_status_t darb_layer_norm_grad_work(darb_layout_t layout, int64_t steps, int
     DARB_TRACE("darb_layer_norm_grad_work");
     if (bytes == nullptr) return DARB_ERR_INVALID_ARG;
     const darb_status_t st = check_norm(DARB_F32, layout, steps, tokens, features);
-    if (st != DARB_OK) return st == DARB_ERR_UNSUPPORTED ? st : DARB_ERR_INVALID_ARG;
+    if (st != DARB_OK) return st;
+    // (sizes that no call takes, whose scratch need not fit 64 bits)
+    if (token_span(layout, steps, tokens, features, layout == DARB_TOKEN_ROWS ? features : tokens) < 0) return DARB_ERR_UNSUPPORTED;
     return work_bytes(layout, steps, tokens, features, bytes);
 }
 
