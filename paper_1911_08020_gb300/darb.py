@@ -501,7 +501,8 @@ def darb_token_logprobs(logits, targets=None, k: int = 0, dim: int = -1, out: To
 
     logits: 2-D float32 or bfloat16, the vocabulary along `dim` (-1: tokens x vocab; 0: vocab x tokens,
     what darb_spmm returns), either axis contiguous.  targets: int64 (tokens,), negative for none; without
-    targets there is no logprob.  out: buffers to write (entries may be None: not wanted)."""
+    targets there is no logprob.  out: buffers to write (entries may be None: not wanted).  What the call does
+    not compute is None in what it returns, also where `out` has a buffer for it."""
     call = "darb_token_logprobs"
     code = _value_code(logits, call, "logits")
     if logits.dim() != 2:
@@ -512,8 +513,10 @@ def darb_token_logprobs(logits, targets=None, k: int = 0, dim: int = -1, out: To
     torch = _torch
     if out is None:
         out = TokenLogprobs.empty(n, k, logits.device, stream)
-        if targets is None:
-            out = out._replace(logprob=None)
+    elif k == 0 and any(t is not None and t.numel() for t in out[3:]):
+        out = out._replace(top_logprob=None, top_index=None)
+    if targets is None:
+        out = out._replace(logprob=None)
     f32 = torch.float32
     logprob = None if targets is None else _vector(out.logprob, n, f32, call, "logprob")
     top = (_vector(out.top_logprob, n * k, f32, call, "top_logprob"),
