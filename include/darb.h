@@ -70,7 +70,10 @@ typedef enum { DARB_F32 = 0, DARB_BF16 = 1 } darb_dtype_t;
 
 /* How the activations of a call lie in memory.  DARB_TOKEN_ROWS: token t is a row
  * of contiguous features at t * ld.  DARB_TOKEN_COLUMNS: features x tokens, feature
- * f of token t at f * ld + t -- the layout that darb_spmm and the steps read and write. */
+ * f of token t at f * ld + t -- the layout that darb_spmm and the steps read and write.
+ * In the calls that take a layout, matrices of one leading dimension that lie side by side
+ * in a wider buffer do not overlap, nor does a vector that lies between a matrix's lines;
+ * of different leading dimensions everything from the first to the last element counts. */
 typedef enum { DARB_TOKEN_ROWS = 0, DARB_TOKEN_COLUMNS = 1 } darb_layout_t;
 
 /* Largest block size the format stores (offsets take at most 8 bits). */

@@ -1301,12 +1301,12 @@ darb_status_t darb_layer_norm(const void *x, darb_dtype_t dtype, darb_layout_t l
     if (x == nullptr || y == nullptr || !aligned_to(x, es) || !aligned_to(y, es) || !aligned_to(gamma, 4) ||
         !aligned_to(beta, 4) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
         return DARB_ERR_INVALID_ARG;
-    const int64_t nx = token_span(layout, steps, tokens, features, ld_x), ny = token_span(layout, steps, tokens, features, ld_y);
-    if (nx < 0 || ny < 0) return DARB_ERR_UNSUPPORTED;
+    for (const int64_t ld : {ld_x, ld_y})
+        if (token_span(layout, steps, tokens, features, ld) < 0) return DARB_ERR_UNSUPPORTED;
     const bool in_place = x == y && ld_x == ld_y;
     const int64_t all = steps * tokens;
-    const Range outs[] = {{y, ny * int64_t(es)}, {mean, all * 4}, {rstd, all * 4}};
-    const Range ins[] = {{in_place ? nullptr : x, nx * int64_t(es)}, {gamma, features * 4}, {beta, features * 4}};
+    const Range outs[] = {token_range(y, layout, steps, tokens, features, ld_y, es), {mean, all * 4}, {rstd, all * 4}};
+    const Range ins[] = {token_range(in_place ? nullptr : x, layout, steps, tokens, features, ld_x, es), {gamma, features * 4}, {beta, features * 4}};
     if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
     NormArgs a = {};
     a.x = x, a.out = y, a.ld_x = ld_x, a.ld_out = ld_y, a.steps = steps, a.tokens = tokens, a.features = int32_t(features);
@@ -1349,18 +1349,17 @@ darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const void *x,
         !aligned_to(x, es) || !aligned_to(dx, es) || !aligned_to(gamma, 4) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
         return DARB_ERR_INVALID_ARG;
     if (dgamma != nullptr && !aligned_to(work, 16)) return DARB_ERR_INVALID_ARG;
-    const int64_t nd = token_span(layout, steps, tokens, features, ld_dy), nx = token_span(layout, steps, tokens, features, ld_x),
-                  no = token_span(layout, steps, tokens, features, ld_dx);
-    if (nd < 0 || nx < 0 || no < 0) return DARB_ERR_UNSUPPORTED;
+    for (const int64_t ld : {ld_dy, ld_x, ld_dx})
+        if (token_span(layout, steps, tokens, features, ld) < 0) return DARB_ERR_UNSUPPORTED;
     const bool in_place = dx == dy && ld_dx == ld_dy;
     const int64_t all = steps * tokens;
     int64_t scratch = 0;
     st = work_bytes(layout, steps, tokens, features, &scratch);
     if (st != DARB_OK) return st;
-    const Range outs[] = {{dx, no * int64_t(es)}, {dgamma, features * 4}, {dbeta, features * 4},
+    const Range outs[] = {token_range(dx, layout, steps, tokens, features, ld_dx, es), {dgamma, features * 4}, {dbeta, features * 4},
                           {dgamma ? work : nullptr, scratch}};
-    const Range ins[] = {{in_place ? nullptr : dy, nd * int64_t(es)}, {x, nx * int64_t(es)}, {gamma, features * 4},
-                         {mean, all * 4}, {rstd, all * 4}};
+    const Range ins[] = {token_range(in_place ? nullptr : dy, layout, steps, tokens, features, ld_dy, es),
+                         token_range(x, layout, steps, tokens, features, ld_x, es), {gamma, features * 4}, {mean, all * 4}, {rstd, all * 4}};
     if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
     NormArgs a = {};
     a.x = x, a.dy = dy, a.out = dx, a.ld_x = ld_x, a.ld_dy = ld_dy, a.ld_out = ld_dx;

@@ -1254,11 +1254,10 @@ darb_status_t darb_token_logprobs(const void *logits, darb_dtype_t dtype, darb_l
     if (k > 0 && (top_logprob == nullptr || top_index == nullptr || !aligned_to(top_logprob, 4) || !aligned_to(top_index, 4)))
         return DARB_ERR_INVALID_ARG;
     if (tokens > kMaxTokens || vocab > kMaxFeatures) return DARB_ERR_UNSUPPORTED;
-    const int64_t span = token_span(layout, 1, tokens, vocab, ld);
-    if (span < 0) return DARB_ERR_UNSUPPORTED;
+    if (token_span(layout, 1, tokens, vocab, ld) < 0) return DARB_ERR_UNSUPPORTED;
     const Range outs[] = {{logprob, tokens * 4}, {entropy, tokens * 4}, {lse, tokens * 4}, {k ? top_logprob : nullptr, tokens * k * 4},
                           {k ? top_index : nullptr, tokens * k * 4}};
-    const Range ins[] = {{logits, span * int64_t(dtype_size(dtype))}, {targets, tokens * 8}};
+    const Range ins[] = {token_range(logits, layout, 1, tokens, vocab, ld, dtype_size(dtype)), {targets, tokens * 8}};
     if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
     if (layout == DARB_TOKEN_COLUMNS && tokens == 1 && ld == 1) layout = DARB_TOKEN_ROWS;   // (a single row: ld is not used)
     const ScoreArgs a = {logits, ld, tokens, int32_t(vocab), k, targets, logprob, entropy, lse, top_logprob, top_index};
@@ -1283,12 +1282,11 @@ darb_status_t darb_token_logprobs_grad(const void *logits, darb_dtype_t dtype, d
         return DARB_ERR_INVALID_ARG;
     if ((d_logprob != nullptr && targets == nullptr) || (d_entropy != nullptr && entropy == nullptr)) return DARB_ERR_INVALID_ARG;
     if (tokens > kMaxTokens || vocab > kMaxFeatures) return DARB_ERR_UNSUPPORTED;
-    const int64_t span = token_span(layout, 1, tokens, vocab, ld), span_grad = token_span(layout, 1, tokens, vocab, ld_grad);
-    if (span < 0 || span_grad < 0) return DARB_ERR_UNSUPPORTED;
+    if (token_span(layout, 1, tokens, vocab, ld) < 0 || token_span(layout, 1, tokens, vocab, ld_grad) < 0) return DARB_ERR_UNSUPPORTED;
     // the gradient may take the logits' place: every element is read before it is written
     const bool in_place = logits == d_logits && ld == ld_grad;
-    const Range outs[] = {{d_logits, span_grad * int64_t(es)}};
-    const Range ins[] = {{in_place ? nullptr : logits, span * int64_t(es)}, {targets, tokens * 8}, {lse, tokens * 4},
+    const Range outs[] = {token_range(d_logits, layout, 1, tokens, vocab, ld_grad, es)};
+    const Range ins[] = {token_range(in_place ? nullptr : logits, layout, 1, tokens, vocab, ld, es), {targets, tokens * 8}, {lse, tokens * 4},
                          {entropy, tokens * 4}, {d_logprob, tokens * 4}, {d_entropy, tokens * 4}};
     if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
     if (layout == DARB_TOKEN_COLUMNS && tokens == 1 && ld == 1 && ld_grad == 1) layout = DARB_TOKEN_ROWS;

@@ -220,18 +220,39 @@ inline bool ranges_overlap(const void *a, int64_t abytes, const void *b, int64_t
     return x < y + static_cast<uintptr_t>(bbytes) && y < x + static_cast<uintptr_t>(abytes);
 }
 
-// One buffer of a call, for the check that no output meets another buffer.
+// One buffer of a call, for the check that no output meets another buffer: `bytes`
+// from the first to past the last; of a matrix, lines of `width` bytes `pitch` apart.
 struct Range {
     const void *p;
     int64_t bytes;
+    int64_t pitch = 0, width = 0;
 };
+// Activations whose span (token_span) has been found to be allowed.
+inline Range token_range(const void *p, darb_layout_t l, int64_t steps, int64_t tokens, int64_t features, int64_t ld, size_t es) {
+    const int64_t size = static_cast<int64_t>(es), bytes = token_span(l, steps, tokens, features, ld) * size;
+    const int64_t lines = l == DARB_TOKEN_ROWS ? tokens : steps * features;
+    if (lines < 2) return {p, bytes};
+    return {p, bytes, ld * size, (l == DARB_TOKEN_ROWS ? features : tokens) * size};
+}
+// Whether two buffers share a byte.  Lines of one pitch, or a run and lines, lie side by
+// side where either fits between the other's lines (slices of one wide buffer);
+// different pitches are told apart by their first and last bytes alone.
+inline bool buffers_overlap(const Range &a, const Range &b) {
+    if (!ranges_overlap(a.p, a.bytes, b.p, b.bytes)) return false;
+    const int64_t pitch = a.pitch > b.pitch ? a.pitch : b.pitch;
+    if (pitch == 0 || (a.pitch != b.pitch && a.pitch != 0 && b.pitch != 0)) return true;
+    const int64_t wa = a.pitch ? a.width : a.bytes, wb = b.pitch ? b.width : b.bytes;
+    int64_t d = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % pitch;   // of b's lines past a's
+    if (d < 0) d += pitch;
+    return d < wa || d + wb > pitch;
+}
 template <int NO, int NI>
 inline bool outputs_apart(const Range (&outs)[NO], const Range (&ins)[NI]) {
     for (int o = 0; o < NO; ++o) {
         for (int i = 0; i < NI; ++i)
-            if (ranges_overlap(outs[o].p, outs[o].bytes, ins[i].p, ins[i].bytes)) return false;
+            if (buffers_overlap(outs[o], ins[i])) return false;
         for (int p = 0; p < o; ++p)
-            if (ranges_overlap(outs[o].p, outs[o].bytes, outs[p].p, outs[p].bytes)) return false;
+            if (buffers_overlap(outs[o], outs[p])) return false;
     }
     return true;
 }
