@@ -952,15 +952,48 @@ struct WideToken {
     }
 };
 
-// The gradient of one wide row by the CTA.  (Not inlined: the kernels' registers
-// are for their own way.)
+// The gradient of one wide row by the CTA, a granule a thread.  (Not inlined: the
+// kernels' registers are for their own way.)
 template <typename T, typename Args>
-__device__ __noinline__ void wide_row(Args a, int64_t token, const T *x, int64_t step, T *dx, int64_t step_out) {
+__device__ __noinline__ void wide_row(Args a, int64_t token, const T *row, T *out) {
+    constexpr int V = kPerGranule<T>;
     __shared__ float buf[33];
+    const int head = row_head<T>(row);
+    const int32_t n = a.vocab, granules = int32_t(row_granules<T>(head, n));
+    const bool alike = row_head<T>(out) == head;
+    const auto fetch = [&](int32_t g, float (&v)[V]) { unpack(load_granule<T, false>(row, int64_t(g) * V - head, n, -INFINITY), v); };
+    float m = -INFINITY, s = 0.0f;
+    for (int32_t g = threadIdx.x; g < granules; g += blockDim.x) {
+        float v[V];
+        fetch(g, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) m = max_nan(m, v[e]);
+    }
+    m = cta_reduce(m, buf, [](float p, float q) { return max_nan(p, q); });
+    for (int32_t g = threadIdx.x; g < granules; g += blockDim.x) {
+        float v[V], part = 0.0f;
+        fetch(g, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) part += exp2_fast(max_nan((v[e] - m) * kLog2e, kMasked));
+        s += part;
+    }
+    s = cta_reduce(s, buf, [](float p, float q) { return p + q; });
     const GradToken t = grad_token(a, token);
-    const Token tok = wide_token(x, step, a.vocab, buf);
-    const WideToken k = {tok.m, tok.log2s};
-    for (int32_t i = threadIdx.x; i < a.vocab; i += blockDim.x) dx[int64_t(i) * step_out] = narrow<T>(k.grad(t, widen(x[int64_t(i) * step]), i));
+    const WideToken k = {m, log2f(s)};
+    for (int32_t g = threadIdx.x; g < granules; g += blockDim.x) {
+        const int64_t j0 = int64_t(g) * V - head;
+        float v[V];
+        fetch(g, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = k.grad(t, v[e], int32_t(j0 + e));
+        if (alike) {
+            store_granule(out, j0, n, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (j0 + e >= 0 && j0 + e < n) out[j0 + e] = narrow<T>(v[e]);
+        }
+    }
 }
 
 // The wide tokens of a tile of 32 columns (PAIRS: and those that are read with one),
@@ -981,12 +1014,15 @@ __device__ __noinline__ void wide_tile(const GradArgs a, int64_t tile) {
     T *dx = static_cast<T *>(a.dx) + token;
     const int32_t n = wide ? a.vocab : 0;   // (a lane without a wide token goes along)
     float m = -INFINITY, s = 0.0f;
+#pragma unroll 8
     for (int32_t v = lane >> 2; v < n; v += 8) m = max_nan(m, widen(x[v * a.ld]));
 #pragma unroll
     for (int o = 4; o < 32; o *= 2) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
     for (int32_t v0 = lane >> 2; v0 < n; v0 += 8 * 256) {   // (256 terms first)
         float block = 0.0f;
-        for (int32_t v = v0; v < n && v < v0 + 8 * 256; v += 8) block += exp2_fast(max_nan((widen(x[v * a.ld]) - m) * kLog2e, kMasked));
+        const int32_t end = min(n, v0 + 8 * 256);
+#pragma unroll 8
+        for (int32_t v = v0; v < end; v += 8) block += exp2_fast(max_nan((widen(x[v * a.ld]) - m) * kLog2e, kMasked));
         s += block;
     }
 #pragma unroll
@@ -994,7 +1030,16 @@ __device__ __noinline__ void wide_tile(const GradArgs a, int64_t tile) {
     if (!wide) return;
     const GradToken t = grad_token(a, token);
     const WideToken k = {m, log2f(s)};
-    for (int32_t v = lane >> 2; v < n; v += 8) dx[v * a.ldd] = narrow<T>(k.grad(t, widen(x[v * a.ld]), v));
+    constexpr int U = 8;   // (rows in flight: the stores may be where the loads are)
+    for (int32_t v0 = lane >> 2; v0 < n; v0 += 8 * U) {
+        T q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (v0 + 8 * u < n) q[u] = x[(v0 + 8 * u) * a.ld];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (v0 + 8 * u < n) dx[(v0 + 8 * u) * a.ldd] = narrow<T>(k.grad(t, widen(q[u]), v0 + 8 * u));
+    }
 }
 
 // N logits of one token, from v0 on `step` apart, to their gradients.  A masked
@@ -1043,7 +1088,7 @@ __global__ void __launch_bounds__(THREADS) grad_rows_kernel(const __grid_constan
         for (int u = 0; u < U; ++u) q[u] = in[u * THREADS];
         const GradToken t = grad_token(a, token);
         if (is_wide_lse(t.lse)) {
-            if (part == 0) wide_row<T, const GradArgs &>(a, token, row, 1, out, 1);
+            if (part == 0) wide_row<T, const GradArgs &>(a, token, row, out);
             return;
         }
 #pragma unroll
@@ -1071,7 +1116,7 @@ __global__ void __launch_bounds__(THREADS) grad_rows_kernel(const __grid_constan
         }
         const GradToken own = B == 1 ? t : grad_token(a, token);   // (after the loads)
         if (is_wide_lse(own.lse)) {   // (in the first round, and for all threads)
-            if (part == 0) wide_row<T, const GradArgs &>(a, token, row, 1, out, 1);
+            if (part == 0) wide_row<T, const GradArgs &>(a, token, row, out);
             return;
         }
 #pragma unroll
@@ -1124,7 +1169,7 @@ __global__ void __launch_bounds__(kGradThreads, sizeof(T) == 4 ? 8 : 6) grad_any
     for (int u = 0; u < U; ++u)
         if (!wide && (whole || v0 + u * step < a.vocab)) dx[u * by_out] = narrow<T>(u & 1 ? high(v[u / 2]) : low(v[u / 2]));
     if (!COLUMNS && wide && part == 0)
-        wide_row<T, GradArgs>(a, token, static_cast<const T *>(a.x) + token * a.ld, 1, static_cast<T *>(a.dx) + token * a.ldd, 1);
+        wide_row<T, GradArgs>(a, token, static_cast<const T *>(a.x) + token * a.ld, static_cast<T *>(a.dx) + token * a.ldd);
 }
 
 // Rows v0, v0 + ROWS, ... of two neighbouring tokens, N of them, or with GUARD those
