@@ -1139,9 +1139,11 @@ cudaError_t launch_norm(const NormArgs &a, darb_layout_t layout, cudaStream_t st
                 e = launch_ex(kernel, dim3(unsigned(p.grid)), dim3(p.threads), size_t(p.stage_bytes) * stages, stream, 1, true, a,
                               p.stage_bytes);
         };
-        // 16 features a thread, while that leaves enough rows at a time on an SM: 12000 x 2500
-        // bf16 (160 threads) 33 us, with 32 features 41; 8000 x 4096 fp32 43 and 48; 300 x 4096
-        // bf16 3.3 and 4.0; but 8191 x 4096 bf16 34 and 30, 10000 x 3300 48 and 41
+        // 16 features a thread, while that leaves enough rows at a time on an SM.  bf16, with 16
+        // and with 32: up to 160 threads 19531 x 1536 27.6 and 36.1 us, 12000 x 2500 33.1 and 41.1,
+        // 11718 x 2560 28.0 and 33.6; from 192 on 11160 x 2688 35.0 and 32.7, 10190 x 2944
+        // 32.2 and 30.6, 9375 x 3200 39.0 and 34.9, 7324 x 4096 31.2 and 27.8; but 300 x 4096 3.3
+        // and 4.0.  fp32: 8000 x 4096 43 and 48.
         const bool wide = sizeof(T) == 4 || a.tokens <= 2 * int64_t(sm_count());
         rows(norm_rows_kernel<T, VPT / 2, 3, kHalfThreads>, VPT / 2, wide ? kHalfThreads : 160, 3);
         rows(norm_rows_kernel<T, VPT, 3, 256>, VPT, 256, 3);

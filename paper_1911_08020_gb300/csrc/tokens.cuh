@@ -118,7 +118,9 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 
 // Two fp32 values in a register pair; an operation on pairs is one instruction,
-// each half of it one IEEE operation.
+// each half of it one IEEE operation.  But the assembler contracts a product and the
+// sum that it goes into to one rounding, whatever is asked of it: where the two
+// roundings matter, the sum is two scalar additions.
 struct Pair {
     unsigned long long bits;
 };
