@@ -20,7 +20,7 @@ import torch
 
 own = False
 
-LR, BETA, DECAY, NS_EPS = 2e-4, 0.95, 0.01, 1e-7
+LR, BETA, DECAY, NS_EPS = 2e-4, 0.95, 0.01, 1e-7   # a rate for training that starts from trained weights
 NS = (3.4445, -4.7750, 2.0315)   # the coefficients of an iteration, five iterations
 CLIP_LOW, CLIP_HIGH, KL, BONUS = 0.2, 0.28, 0.05, 0.01
 
