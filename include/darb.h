@@ -496,6 +496,63 @@ DARB_API darb_status_t darb_layer_norm_grad(const void *dy, int64_t ld_dy, const
 DARB_API darb_status_t darb_layer_norm_grad_work(darb_layout_t layout, int64_t steps, int64_t tokens, int64_t features,
                                                  int64_t *bytes);
 
+/* What a gate of darb_gated_scan holds: the logit of the share of the old state that
+ * is kept, or that share itself. */
+typedef enum { DARB_GATES_LOGITS = 0, DARB_GATES_VALUES = 1 } darb_gates_t;
+
+/*
+ * A gated linear recurrence over whole sequences: the recurrent layer whose gates do
+ * not need the step before, so that those of all steps are one darb_spmm.  Per channel
+ *   a_t = sigmoid(gate_t) (DARB_GATES_VALUES: gate_t),
+ *   h_t = a_t h_(t-1) + (1 - a_t) x_t   (coupled == 0: a_t h_(t-1) + x_t).
+ *   gate, x, h   device, fp32 or bf16 (dtype).  Element (o, t, i) -- outer, step, inner
+ *            -- is at o * ld + t * step + i, with leading dimensions and steps of their
+ *            own.  What the sequence calls write (steps x features x batch) has inner =
+ *            features * batch; a product of all steps (features x (steps * batch)) has
+ *            outer = features, inner = batch; token rows (batch x steps x features) have
+ *            outer = batch, inner = features.  No two elements of a tensor may share a place
+ *   h0       device fp32[outer x inner], the state before step 0; NULL: 0
+ *   h_last   device fp32[outer x inner], the state after the last step; NULL: not wanted.
+ *            May be h0 itself (a state that is carried from call to call)
+ * The state is fp32 from step to step; h is rounded to its type as it is written.  h may
+ * be x itself (same pointer and strides); no other overlap is allowed.  A logit of -inf
+ * starts anew (a = 0), one of +inf keeps the state as it is (a = 1); a NaN, or an infinite
+ * state that meets a = 0, makes its channel NaN from there on.  Gates above 1 in magnitude are
+ * allowed as long as their products over 512 steps (or until the state is 0) stay finite.
+ * No channels: nothing is done; steps == 0: h_last is h0.
+ * Asynchronous on `stream`; allocates nothing; one launch (steps == 0: a copy).
+ * Errors: DARB_ERR_INVALID_ARG; DARB_ERR_UNSUPPORTED (more than 2^30 steps or channels,
+ * or 2^48 elements from the first to the last of a tensor); DARB_ERR_CUDA.
+ */
+DARB_API darb_status_t darb_gated_scan(const void *gate, int64_t ld_gate, int64_t step_gate, const void *x,
+                                       int64_t ld_x, int64_t step_x, darb_dtype_t dtype, darb_gates_t gates,
+                                       int coupled, int64_t outer, int64_t steps, int64_t inner, const float *h0,
+                                       void *h, int64_t ld_h, int64_t step_h, float *h_last, cudaStream_t stream);
+
+/*
+ * The backward pass of darb_gated_scan.  From the last step to the first, with c what
+ * flows to a step from the one after it (d_last at the end),
+ *   g = dh_t + c,  d_x_t = g (1 - a_t)  (coupled == 0: g),
+ *   d_gate_t = g (h_(t-1) - x_t) a_t (1 - a_t)   (coupled == 0: without x_t;
+ *            DARB_GATES_VALUES: without a_t (1 - a_t)),
+ *   c = a_t g,  and at the end d_h0 = c.
+ *   gate, x, h0, gates, coupled   as in the forward call; h its result
+ *   dh       device, the gradient that comes in at every step, of the same dtype
+ *   d_last   device fp32[outer x inner], the gradient of h_last; NULL: 0
+ *   d_gate, d_x   device, of the same dtype; d_gate may be the gate itself and d_x may be x
+ *            (same pointer and strides)
+ *   d_h0     device fp32[outer x inner]; NULL: not wanted.  May be d_last itself
+ * No other overlap of an output is allowed.  steps == 0: d_h0 is d_last.
+ * Asynchronous on `stream`; allocates nothing; one launch.  Errors: as darb_gated_scan.
+ */
+DARB_API darb_status_t darb_gated_scan_grad(const void *dh, int64_t ld_dh, int64_t step_dh, const void *gate,
+                                            int64_t ld_gate, int64_t step_gate, const void *x, int64_t ld_x,
+                                            int64_t step_x, const void *h, int64_t ld_h, int64_t step_h,
+                                            darb_dtype_t dtype, darb_gates_t gates, int coupled, int64_t outer,
+                                            int64_t steps, int64_t inner, const float *h0, const float *d_last,
+                                            void *d_gate, int64_t ld_dgate, int64_t step_dgate, void *d_x,
+                                            int64_t ld_dx, int64_t step_dx, float *d_h0, cudaStream_t stream);
+
 /* Elements that share a scale where darb_adamw_step holds states in 8 bits. */
 #define DARB_ADAMW_BLOCK 256
 

@@ -22,6 +22,7 @@ OK, ERR_INVALID_ARG, ERR_NONFINITE, ERR_OOM, ERR_CUDA, ERR_TIMEOUT, ERR_UNSUPPOR
 F32, BF16 = 0, 1
 PATH_AUTO, PATH_CUDA_CORES, PATH_TENSOR_CORES = 0, 1, 2
 TOKEN_ROWS, TOKEN_COLUMNS = 0, 1
+GATES_LOGITS, GATES_VALUES = 0, 1
 MAX_BLOCK = 256
 MAX_TOP = 32
 ADAMW_BLOCK = 256
@@ -86,6 +87,10 @@ def lib():
                 "darb_layer_norm_grad": [P, I64, P, I64, ctypes.c_int, ctypes.c_int, I64, I64, I64, P, P, P, P, I64,
                                          P, P, P, S],
                 "darb_layer_norm_grad_work": [ctypes.c_int, I64, I64, I64, P],
+                "darb_gated_scan": [P, I64, I64, P, I64, I64, ctypes.c_int, ctypes.c_int, ctypes.c_int, I64, I64, I64, P, P,
+                                    I64, I64, P, S],
+                "darb_gated_scan_grad": [P, I64, I64, P, I64, I64, P, I64, I64, P, I64, I64, ctypes.c_int, ctypes.c_int,
+                                         ctypes.c_int, I64, I64, I64, P, P, P, I64, I64, P, I64, I64, P, S],
                 "darb_adamw_create": [I32, P, P, P, P, P, P, P, ctypes.c_int, P, S],
                 "darb_adamw_step": [P, P, P, I64, ctypes.c_uint64, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                     ctypes.c_double, ctypes.c_double, S],
@@ -629,6 +634,102 @@ def darb_layer_norm_grad_work(layout: int, steps: int, tokens: int, features: in
     _check(lib().darb_layer_norm_grad_work(layout, steps, tokens, features, ctypes.byref(need)),
            "darb_layer_norm_grad_work")
     return need.value
+
+
+# ---- a gated linear recurrence ----
+
+def _channel_axes(like, others, dim: int, call: str) -> tuple[int, int, int, int, int]:
+    """(outer, steps, inner, outer axis, step axis) of tensors whose steps lie along `dim`: their other axes are
+    one run of contiguous channels where that holds for all of them, else a strided axis and a contiguous one.
+    The outer axis is -1 where there is none."""
+    shape = like.shape
+    nd = len(shape)
+    if nd not in (2, 3) or not -nd <= dim < nd:
+        _refuse(call, "x must be 2-D or 3-D, with its steps along dim")
+    dim %= nd
+    axes = [a for a in range(nd) if a != dim]
+    n = [shape[a] for a in axes]
+    channels = n[0] * (n[1] if nd == 3 else 1)
+    tensors = (like, *others)
+    if nd == 3:
+        if n[0] == 1 or n[1] == 1:
+            axes = axes[n[0] == 1:][:1]
+        elif channels and any(t.stride(axes[0]) != n[1] * t.stride(axes[1]) for t in tensors):
+            if any(t.stride(axes[1]) != 1 for t in tensors):
+                _refuse(call, "the last axis of the channels must be contiguous, or all channels equally far apart")
+            return n[0], shape[dim], n[1], axes[0], dim
+    if channels <= 1 or all(t.stride(axes[-1]) == 1 for t in tensors):
+        return 1, shape[dim], channels, -1, dim
+    return channels, shape[dim], 1, axes[-1], dim
+
+
+def _scan_operand(t, like, outer: int, step: int, call: str, name: str) -> tuple[int, int, int]:
+    """(pointer, leading dimension, step) of a tensor of x's shape and type."""
+    if t.dtype != like.dtype or not t.is_cuda or t.shape != like.shape:
+        _refuse(call, f"{name} must be a CUDA tensor of x's shape and type")
+    strides = t.stride()
+    return t.data_ptr(), strides[outer] if outer >= 0 else 0, strides[step]
+
+
+def _state_shape(x, dim: int):
+    shape = list(x.shape)
+    del shape[dim]
+    return shape
+
+
+def darb_gated_scan(gate, x, h0=None, dim: int = 0, gates: int = GATES_LOGITS, coupled: bool = True, h=None, h_last=None,
+                    stream=None):
+    """(h, h_last): the recurrence h_t = a_t h_(t-1) + (1 - a_t) x_t over the steps along `dim`, every channel for
+    itself, with a_t = sigmoid(gate_t) (GATES_VALUES: gate_t); coupled=False: without the factor 1 - a_t.
+
+    gate, x: float32 or bfloat16, 2-D or 3-D, e.g. (steps, features, batch) with dim=0, as the sequence calls
+    write; a product of all steps, viewed as (features, steps, batch), with dim=1; token rows (batch, steps,
+    features) with dim=1.  Slices of wider tensors are taken as they are.  h0: float32 of x's shape without
+    `dim`, the state before the first step (None: 0).  h: as x, and may be x; h_last: as h0, and may be h0."""
+    call = "darb_gated_scan"
+    code = _value_code(x, call, "x")
+    f32 = _torch.float32
+    if h is None:
+        h = _new(x.shape, x.dtype, x.device, stream)
+    if gate.shape != x.shape or h.shape != x.shape:
+        _refuse(call, "gate and h must have x's shape")
+    outer, steps, inner, oa, sa = _channel_axes(x, (gate, h), dim, call)
+    if h_last is None:
+        h_last = _new(_state_shape(x, sa), f32, x.device, stream)
+    n = outer * inner
+    _check(lib().darb_gated_scan(*_scan_operand(gate, x, oa, sa, call, "gate"), *_scan_operand(x, x, oa, sa, call, "x"), code,
+                                 gates, bool(coupled), outer, steps, inner, _vector(h0, n, f32, call, "h0"),
+                                 *_scan_operand(h, x, oa, sa, call, "h"), _vector(h_last, n, f32, call, "h_last"),
+                                 _stream(stream)), call)
+    return h, h_last
+
+
+def darb_gated_scan_grad(dh, gate, x, h, h0=None, d_last=None, dim: int = 0, gates: int = GATES_LOGITS, coupled: bool = True,
+                         d_gate=None, d_x=None, d_h0=None, stream=None):
+    """(d_gate, d_x, d_h0): the backward pass of darb_gated_scan, given the gradients of h (dh) and of h_last
+    (d_last; None: 0).  h: the forward call's.  d_gate may be gate, d_x may be x, d_h0 may be d_last.  Without
+    h0 there is no d_h0 (None) unless a buffer for it is given."""
+    call = "darb_gated_scan_grad"
+    code = _value_code(x, call, "x")
+    f32 = _torch.float32
+    if d_gate is None:
+        d_gate = _new(x.shape, x.dtype, x.device, stream)
+    if d_x is None:
+        d_x = _new(x.shape, x.dtype, x.device, stream)
+    others = (gate, dh, h, d_gate, d_x)
+    if any(t.shape != x.shape for t in others):
+        _refuse(call, "dh, gate, h, d_gate and d_x must have x's shape")
+    outer, steps, inner, oa, sa = _channel_axes(x, others, dim, call)
+    if d_h0 is None and h0 is not None:
+        d_h0 = _new(_state_shape(x, sa), f32, x.device, stream)
+    n = outer * inner
+    at = [_scan_operand(t, x, oa, sa, call, name) for t, name in ((dh, "dh"), (gate, "gate"), (x, "x"), (h, "h"))]
+    _check(lib().darb_gated_scan_grad(*at[0], *at[1], *at[2], *at[3], code, gates, bool(coupled), outer, steps, inner,
+                                      _vector(h0, n, f32, call, "h0"), _vector(d_last, n, f32, call, "d_last"),
+                                      *_scan_operand(d_gate, x, oa, sa, call, "d_gate"),
+                                      *_scan_operand(d_x, x, oa, sa, call, "d_x"), _vector(d_h0, n, f32, call, "d_h0"),
+                                      _stream(stream)), call)
+    return d_gate, d_x, d_h0
 
 
 class AdamW:
