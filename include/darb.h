@@ -553,6 +553,55 @@ DARB_API darb_status_t darb_gated_scan_grad(const void *dh, int64_t ld_dh, int64
                                             void *d_gate, int64_t ld_dgate, int64_t step_dgate, void *d_x,
                                             int64_t ld_dx, int64_t step_dx, float *d_h0, cudaStream_t stream);
 
+/* Whether darb_policy_loss takes a ratio for every token or one for every sequence
+ * (the exponential of the mean difference of its tokens), and whether every token or
+ * every sequence counts the same in the means. */
+typedef enum { DARB_PER_TOKEN = 0, DARB_PER_SEQUENCE = 1 } darb_per_t;
+
+/*
+ * The clipped policy loss of sequences that a model drew itself, with a KL term and
+ * an entropy bonus, and its gradients in the same call.  It takes what
+ * darb_token_logprobs gives and leaves what darb_token_logprobs_grad takes.  Of the
+ * tokens that count, with r = e^(logprob - old) (or the sequence's), A the sequence's
+ * advantage, x = ref - logprob and w = 1 / (tokens) or 1 / (sequences with a token * tokens
+ * of the sequence):
+ *   policy = -sum w min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
+ *   kl = sum w (e^x - 1 - x),  entropy = sum w H
+ *   loss = policy + kl_coef kl - entropy_coef entropy
+ *   logprob, old_logprob   device fp32[tokens]
+ *   ref_logprob, entropy   device fp32[tokens]; NULL allowed where kl_coef (entropy_coef
+ *            and d_entropy) do without
+ *   mask     device, a byte a token: 0 does not count; NULL: all count.  What the other
+ *            buffers hold at tokens that do not count is not looked at
+ *   advantage  device fp32[sequences]
+ *   offsets  device int64[sequences + 1]: sequence s has the tokens from offsets[s] up
+ *            to offsets[s + 1]; they must not fall, nor be below 0 or above `tokens`
+ *            (else results are not defined, but nothing outside the buffers is touched).
+ *            Tokens before the first and behind the last sequence do not count
+ *   clip_low   0 .. 1 (1: r is not clipped from below); clip_high >= 0 (+inf: not from above)
+ *   stats    device fp32[5]: loss, policy, kl, entropy, and the share of the weight whose
+ *            ratio is clipped; terms without their buffers are 0
+ *   d_logprob, d_entropy   device fp32[tokens]: the gradients of the loss; d_entropy NULL: not
+ *            wanted.  0 at masked tokens; of tokens outside of all sequences left as it was
+ *   work     device scratch of darb_policy_loss_work bytes (16-byte aligned), not to be shared
+ *            by calls that may run at the same time; NULL: from the device's memory pool
+ * Where nothing counts the stats and gradients are 0.  A border is decided as the exact
+ * difference decides it; sums are in a fixed order, over more than 256 tokens in 64 bits.
+ * No output may overlap another buffer.  Asynchronous on `stream`; allocates nothing but work;
+ * one launch up to 4096 tokens, else two or three.
+ * Errors: DARB_ERR_INVALID_ARG; DARB_ERR_UNSUPPORTED (more than 2^27 tokens or sequences);
+ * DARB_ERR_OOM; DARB_ERR_CUDA.
+ */
+DARB_API darb_status_t darb_policy_loss(int64_t tokens, int64_t sequences, const float *logprob,
+                                        const float *old_logprob, const float *ref_logprob, const float *entropy,
+                                        const uint8_t *mask, const float *advantage, const int64_t *offsets,
+                                        double clip_low, double clip_high, double kl_coef, double entropy_coef,
+                                        darb_per_t ratio, darb_per_t mean, float *stats, float *d_logprob,
+                                        float *d_entropy, void *work, cudaStream_t stream);
+
+/* Bytes of scratch that darb_policy_loss needs for so many tokens (0 up to 4096). */
+DARB_API darb_status_t darb_policy_loss_work(int64_t tokens, int64_t *bytes);
+
 /* Elements that share a scale where darb_adamw_step holds states in 8 bits. */
 #define DARB_ADAMW_BLOCK 256
 

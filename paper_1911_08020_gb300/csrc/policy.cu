@@ -1,0 +1,732 @@
+// policy.cu -- the clipped policy loss of drawn answers with a KL term and an
+// entropy bonus, and its gradients (darb_policy_loss): between darb_token_logprobs,
+// whose log probabilities and entropies it takes, and darb_token_logprobs_grad, which
+// takes what it leaves.
+//
+// Per token that counts, with d = logprob - old (or its mean over the token's
+// sequence), r = e^d, A the sequence's advantage and w the token's weight:
+//   loss = sum w (-min(r A, clip(r, 1 - low, 1 + high) A) + kl_coef k - entropy_coef H),
+//   k = e^x - 1 - x with x = ref - logprob,
+//   d_logprob = w (-[not clipped] A r - kl_coef (e^x - 1)),  d_entropy = -entropy_coef w.
+// A mean over a sequence shares its gradient among n tokens and gets it back from as
+// many, so the formula is the same with one ratio a sequence.
+//
+// w needs how many tokens count in a sequence, and in all: the inputs are read twice
+// (mask, and log probabilities where the ratio is the sequence's; then everything).
+// A CTA takes a chunk of consecutive tokens.  Its sequences are found once, by a
+// search of 256 offsets at a time; the place where a sequence starts in the chunk
+// stands for it from then on, so that scratch goes by tokens and any number of empty
+// sequences costs nothing but reading their offsets.  A chunk's sums of a sequence
+// go to that place, those of a sequence from an earlier chunk to the chunk, and who
+// needs the sum of a sequence that spans chunks adds the chunks up, in their order.
+// Up to 4096 tokens are one chunk: one CTA, one launch, no scratch.
+//
+// What bounds it: latency for few tokens, memory for many (25 bytes a token with
+// every term; 64-bit arithmetic is too slow to spend on a token, one operation takes
+// as long as 6 bytes, so differences are pairs of 32-bit numbers where a border needs
+// them exact, and 64 bits hold the sums from a warp on).
+#include "launch.cuh"
+#include "tma.cuh"
+#include "tokens.cuh"
+#include "trace.h"
+
+#include <algorithm>
+#include <cmath>
+#include <limits>
+
+namespace darb {
+
+cudaError_t stream_alloc(void **p, size_t bytes, cudaStream_t stream);
+
+namespace {
+
+constexpr int kE = 8;                       // tokens of a thread
+constexpr int kFew = 4096;                  // tokens of the single CTA
+constexpr int kChunkThreads = 256;
+constexpr int kChunkTokens = kChunkThreads * kE;
+constexpr int kInline = 8192;               // chunks and sequences that every CTA counts itself
+constexpr int kStats = 5;                   // loss, policy, kl, entropy, clipped
+constexpr int kSums = 4;                    // the sums that they come from
+constexpr int kOutside = -2, kNone = -1;    // in place of a sequence
+
+struct PolicyWork {
+    double *slot_sum;     // per token: of the sequence that starts there, what its first chunk has of it
+    double *head_sum;     // per chunk: of the sequence that started before it
+    double *partial;      // per sum and chunk
+    int32_t *slot_count, *head_count;
+    int32_t *head_start;  // where that sequence started; -1: none
+    int32_t *count;       // per chunk: all of its tokens that count
+    long long *norm;      // the tokens, or sequences, that count
+    int32_t *ticket;
+};
+
+struct PolicyArgs {
+    const float *logprob, *old, *ref, *entropy, *advantage;
+    const uint8_t *mask;
+    const int64_t *offsets;
+    float *stats, *d_logprob, *d_entropy;
+    PolicyWork w;
+    int64_t n, sequences, chunks;
+    double log_low, log_high;     // log(1 - low), log(1 + high)
+    float low[3], high[3];        // the same, as sums of 32-bit numbers
+    float used_low, used_high;    // 1 - low, 1 + high
+    float kl_coef, entropy_coef;
+    int32_t per_sequence;         // the mean: every sequence counts the same
+    int32_t counted;              // w.norm has been summed by a launch of its own
+    int32_t vector;
+};
+
+// How many of the offsets are <= at: offsets[0 .. n] do not fall.
+template <int THREADS>
+__device__ __forceinline__ int64_t offsets_upto(const int64_t *offsets, int64_t n, int64_t at) {
+    int64_t lo = 0, hi = n + 1;   // the answer is in [lo, hi]
+    while (hi > lo) {
+        const int64_t span = hi - lo, step = (span + THREADS - 1) / THREADS;
+        // thread i looks at the last of the i-th run of `step` offsets
+        const int64_t i = lo + (int64_t(threadIdx.x) + 1) * step - 1;
+        const int below = __syncthreads_count(i < hi && offsets[i] <= at);
+        lo = min(lo + below * step, hi);
+        hi = min(lo + step - 1, hi);
+    }
+    return lo;
+}
+
+template <int THREADS>
+struct ChunkShared {
+    static constexpr int T = THREADS * kE;
+    int start[T];        // at the first token of a sequence: the sequence; elsewhere kNone
+    int warp_max[THREADS / 32];
+    double scan_sum[THREADS / 32];
+    int scan_count[THREADS / 32], scan_flag[THREADS / 32];
+    int last;            // where the last sequence of the chunk starts
+    int64_t before;      // where the sequence of the first token starts
+};
+
+// Which sequences start where in the chunk at c0; where the last one starts before
+// the thread's tokens (0 in the first thread, where one always stands).
+template <int THREADS>
+__device__ __forceinline__ int find_sequences(const PolicyArgs &a, int64_t c0, ChunkShared<THREADS> &sh) {
+    constexpr int T = THREADS * kE;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    for (int p = tid; p < T; p += THREADS) sh.start[p] = kNone;
+    const int64_t s0 = offsets_upto<THREADS>(a.offsets, a.sequences, c0) - 1;   // (its barriers order the writes above)
+    if (tid == 0) {
+        const bool inside = s0 >= 0 && s0 < a.sequences;
+        sh.start[0] = inside ? int(s0) : kOutside;
+        sh.before = inside ? a.offsets[s0] : c0;
+    }
+    for (int64_t base = s0 + 1;; base += THREADS) {
+        const int64_t s = base + tid;
+        const int64_t at = s <= a.sequences ? a.offsets[s] - c0 : T;
+        const bool in = at < T;
+        if (in && at > 0 && c0 + at < a.n) {
+            if (s == a.sequences) sh.start[at] = kOutside;
+            else if (a.offsets[s + 1] - c0 > at) sh.start[at] = int(s);
+        }
+        if (__syncthreads_count(in) < THREADS) break;
+    }
+    int mine = -1;
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+        if (sh.start[tid * kE + e] != kNone) mine = tid * kE + e;
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(~0u, mine, d);
+        if (lane >= d) mine = max(mine, o);
+    }
+    if (lane == 31) sh.warp_max[warp] = mine;
+    __syncthreads();
+    int before = __shfl_up_sync(~0u, mine, 1);
+    if (lane == 0) before = -1;
+    for (int w = 0; w < warp; ++w) before = max(before, sh.warp_max[w]);
+    if (tid == THREADS - 1) sh.last = max(mine, before);
+    return tid == 0 ? 0 : before;
+}
+
+// kE tokens from i on (`rest` where n ends before them).
+__device__ __forceinline__ void load8(const float *p, int64_t i, int64_t n, bool vector, float (&v)[kE]) {
+    if (vector && i + kE <= n) {
+        const float4 x = __ldg(reinterpret_cast<const float4 *>(p + i)), y = __ldg(reinterpret_cast<const float4 *>(p + i) + 1);
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < kE; ++e) v[e] = i + e < n ? __ldg(p + i + e) : 0.0f;
+}
+// The mask of kE tokens, a bit each.
+__device__ __forceinline__ uint32_t load_mask(const uint8_t *p, int64_t i, int64_t n, bool vector) {
+    uint32_t bits = 0;
+    if (p == nullptr) {
+        return i >= n ? 0u : n - i >= kE ? (1u << kE) - 1 : (1u << int(n - i)) - 1;
+    }
+    if (vector && i + kE <= n) {
+        const uint2 q = __ldg(reinterpret_cast<const uint2 *>(p + i));
+#pragma unroll
+        for (int e = 0; e < kE; ++e) bits |= uint32_t((((e < 4 ? q.x : q.y) >> (8 * (e & 3))) & 255u) != 0) << e;
+        return bits;
+    }
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+        if (i + e < n && __ldg(p + i + e) != 0) bits |= 1u << e;
+    return bits;
+}
+
+// a - b exactly, as a rounded difference and what that leaves.
+__device__ __forceinline__ void difference(float a, float b, float &hi, float &lo) {
+    hi = __fsub_rn(a, b);
+    const float bb = __fsub_rn(a, hi);
+    lo = __fadd_rn(__fsub_rn(a, __fadd_rn(hi, bb)), __fsub_rn(bb, b));
+}
+
+// Whether hi + lo is above (sign +1) or below (-1) the border.
+__device__ __forceinline__ bool past(float hi, float lo, const float (&border)[3], float sign) {
+    if (hi != border[0]) return sign * hi > sign * border[0];
+    if (lo != border[1]) return sign * lo > sign * border[1];
+    return sign * border[2] < 0.0f;
+}
+
+// Of every sequence in the chunk, how many of its tokens count and the sum of their
+// differences: put(start, count, sum) once for each.
+template <int THREADS, bool SUMS, typename Put>
+__device__ __forceinline__ void sequence_sums(const PolicyArgs &a, int64_t c0, int first, uint32_t on, const float (&lp)[kE],
+                                              const float (&old)[kE], ChunkShared<THREADS> &sh, Put put) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    int cur = first, count = 0, head_count = 0;
+    float hi = 0.0f, lo = 0.0f;
+    double head_sum = 0.0;
+    bool flag = false;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+        const int p = tid * kE + e;
+        if (sh.start[p] != kNone && p > 0) {
+            if (!flag) head_count = count, head_sum = SUMS ? double(hi) + double(lo) : 0.0;
+            else put(cur, count, SUMS ? double(hi) + double(lo) : 0.0);
+            flag = true;
+            cur = p, count = 0, hi = 0.0f, lo = 0.0f;
+        }
+        if (on >> e & 1) {
+            ++count;
+            if (SUMS) {
+                // what the difference and the sum round away is summed beside it
+                float d, r, err;
+                difference(lp[e], old[e], d, r);
+                const float sum = __fadd_rn(hi, d), back = __fsub_rn(sum, hi);
+                err = __fadd_rn(__fsub_rn(hi, __fsub_rn(sum, back)), __fsub_rn(d, back));
+                hi = sum;
+                lo = isfinite(sum) ? lo + (err + r) : 0.0f;
+            }
+        }
+    }
+    // from the last start of each thread on, over the threads that have none
+    const int tail_count = count;
+    const double tail_sum = SUMS ? double(hi) + double(lo) : 0.0;
+    int c = tail_count;
+    double s = tail_sum;
+    int f = flag;
+    for (int d = 1; d < 32; d <<= 1) {
+        const int oc = __shfl_up_sync(~0u, c, d), of = __shfl_up_sync(~0u, f, d);
+        const double os = SUMS ? __shfl_up_sync(~0u, s, d) : 0.0;
+        if (lane >= d) {
+            if (!f) c += oc, s = os + s;
+            f |= of;
+        }
+    }
+    if (lane == 31) sh.scan_count[warp] = c, sh.scan_sum[warp] = s, sh.scan_flag[warp] = f;
+    int bc = __shfl_up_sync(~0u, c, 1), bf = __shfl_up_sync(~0u, f, 1);
+    double bs = SUMS ? __shfl_up_sync(~0u, s, 1) : 0.0;
+    if (lane == 0) bc = 0, bf = 0, bs = 0.0;
+    __syncthreads();
+    int wc = 0;
+    double ws = 0.0;   // of the warps before
+    for (int w = 0; w < warp; ++w) {
+        if (sh.scan_flag[w]) wc = sh.scan_count[w], ws = sh.scan_sum[w];
+        else wc += sh.scan_count[w], ws += sh.scan_sum[w];
+    }
+    if (!bf) bc += wc, bs = ws + bs;
+    // the thread's first start ends the sequence before it, the chunk's end the last one
+    if (flag) put(first, bc + head_count, bs + head_sum);
+    if (tid == THREADS - 1) {
+        if (flag) put(cur, tail_count, tail_sum);
+        else put(cur, bc + tail_count, bs + tail_sum);
+    }
+}
+
+__device__ __forceinline__ double warp_sum(double v) {
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
+    return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
+    return v;
+}
+__device__ __forceinline__ long long warp_sum(long long v) {
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
+    return v;
+}
+
+template <int THREADS>
+__device__ __forceinline__ long long block_sum(long long v) {
+    __shared__ long long part[THREADS / 32];
+    v = warp_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0;
+    for (int w = 0; w < THREADS / 32; ++w) v += part[w];
+    return v;
+}
+
+// The part of thread `at` of `threads` of the tokens (or sequences) that count.
+__device__ __forceinline__ long long counted(const PolicyArgs &a, int64_t at, int64_t threads) {
+    const PolicyWork &w = a.w;
+    long long sum = 0;
+    if (!a.per_sequence) {
+        for (int64_t c = at; c < a.chunks; c += threads) sum += w.count[c];
+        return sum;
+    }
+    for (int64_t s = at; s < a.sequences; s += threads) {
+        const int64_t lo = a.offsets[s], hi = a.offsets[s + 1];
+        if (lo >= 0 && lo < hi && lo < a.n) sum += w.slot_count[lo] > 0;
+    }
+    // a sequence none of whose tokens count in its first chunk: the first chunk that has one
+    for (int64_t c = at; c < a.chunks; c += threads) {
+        const int start = w.head_start[c];
+        if (start < 0 || w.head_count[c] == 0) continue;
+        const int64_t own = start / kChunkTokens;
+        bool first = w.slot_count[start] == 0;
+        for (int64_t b = c - 1; b > own && first; --b) first = w.head_count[b] == 0;
+        sum += first;
+    }
+    return sum;
+}
+
+// What a token needs to know of its sequence.
+struct Piece {
+    float weight, advantage;
+    float used, slope;   // of one ratio a sequence: what it is clipped to, and -A r where it is not clipped
+};
+
+template <bool SUMS>
+__device__ __forceinline__ Piece piece_of(const PolicyArgs &a, int64_t s, int count, double sum, long long norm) {
+    Piece p;
+    const long long n = a.per_sequence ? norm * count : norm;
+    p.weight = count > 0 ? 1.0f / __ll2float_rn(n) : 0.0f;
+    p.advantage = a.advantage[s];
+    p.used = p.slope = 0.0f;
+    if (SUMS && count > 0) {
+        const double d = sum / count;
+        const bool up = p.advantage >= 0.0f, cut = up ? d > a.log_high : d < a.log_low;
+        const float r = expf(float(d));
+        p.used = cut ? (up ? a.used_high : a.used_low) : r;
+        p.slope = cut ? 0.0f : -p.advantage * r;
+        if (cut) p.weight = -p.weight;   // (the sign says so)
+    }
+    return p;
+}
+
+// e^x - 1 - x: its series where the terms cancel (|x| < 1; what is left out is below
+// 2^-28 of the sum).
+__device__ __forceinline__ float excess(float x, float em1) {
+    if (fabsf(x) >= 1.0f) return em1 - x;
+    float s = 1.0f / 39916800.0f;
+    s = fmaf(s, x, 1.0f / 3628800.0f);
+    s = fmaf(s, x, 1.0f / 362880.0f);
+    s = fmaf(s, x, 1.0f / 40320.0f);
+    s = fmaf(s, x, 1.0f / 5040.0f);
+    s = fmaf(s, x, 1.0f / 720.0f);
+    s = fmaf(s, x, 1.0f / 120.0f);
+    s = fmaf(s, x, 1.0f / 24.0f);
+    s = fmaf(s, x, 1.0f / 6.0f);
+    s = fmaf(s, x, 0.5f);
+    return s * x * x;
+}
+
+__device__ __forceinline__ void store8(float *p, int64_t i, uint32_t inside, bool vector, const float (&v)[kE]) {
+    if (vector && inside == (1u << kE) - 1) {
+        reinterpret_cast<float4 *>(p + i)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4 *>(p + i)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+        if (inside >> e & 1) p[i + e] = v[e];
+}
+
+// loss, policy, kl, entropy, clipped from their sums
+__device__ __forceinline__ void write_stats(const PolicyArgs &a, const double (&s)[kSums]) {
+    double loss = s[0];
+    if (a.kl_coef != 0.0f) loss += double(a.kl_coef) * s[1];
+    if (a.entropy_coef != 0.0f) loss -= double(a.entropy_coef) * s[2];
+    a.stats[0] = float(loss);
+    a.stats[1] = float(s[0]);
+    a.stats[2] = float(s[1]);
+    a.stats[3] = float(s[2]);
+    a.stats[4] = float(s[3]);
+}
+
+// ---- the first reading of many tokens: the sums of sequences ----
+
+template <bool SUMS>
+__global__ void __launch_bounds__(kChunkThreads) policy_count_kernel(const PolicyArgs a) {
+    __shared__ ChunkShared<kChunkThreads> sh;
+    const int tid = threadIdx.x;
+    const int64_t c = blockIdx.x, c0 = c * kChunkTokens, i = c0 + tid * kE;
+    pdl_wait_previous();
+    // after the wait, so that the next kernel may read the inputs before it waits for this one
+    pdl_launch_dependents();
+    uint32_t on = load_mask(a.mask, i, a.n, a.vector);
+    float lp[kE] = {}, old[kE] = {};
+    if (SUMS) {
+        load8(a.logprob, i, a.n, a.vector, lp);
+        load8(a.old, i, a.n, a.vector, old);
+    }
+    if (c == 0 && tid == 0) *a.w.ticket = 0, *a.w.norm = 0;
+    const int first = find_sequences<kChunkThreads>(a, c0, sh);
+    // tokens of no sequence do not count
+    int cur = first;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+        if (sh.start[tid * kE + e] != kNone) cur = tid * kE + e;
+        if (sh.start[cur] == kOutside) on &= ~(1u << e);
+    }
+    const int64_t before = sh.before;
+    sequence_sums<kChunkThreads, SUMS>(a, c0, first, on, lp, old, sh, [&](int start, int count, double sum) {
+        if (start == 0 && before < c0) {
+            a.w.head_count[c] = count;
+            a.w.head_sum[c] = sum;
+        } else {
+            a.w.slot_count[c0 + start] = count;
+            if (SUMS) a.w.slot_sum[c0 + start] = sum;
+        }
+    });
+    if (tid == 0) {
+        const bool head = sh.start[0] >= 0 && before < c0;
+        a.w.head_start[c] = head ? int(max(before, int64_t(-1))) : -1;
+        if (!head) a.w.head_count[c] = 0;
+    }
+    const long long all = block_sum<kChunkThreads>(__popc(on));
+    if (tid == 0) a.w.count[c] = int(all);
+}
+
+__global__ void __launch_bounds__(kChunkThreads) policy_norm_kernel(const PolicyArgs a) {
+    pdl_wait_previous();
+    pdl_launch_dependents();
+    const long long v = block_sum<kChunkThreads>(counted(a, int64_t(blockIdx.x) * kChunkThreads + threadIdx.x, int64_t(gridDim.x) * kChunkThreads));
+    if (threadIdx.x == 0 && v != 0) atomicAdd(reinterpret_cast<unsigned long long *>(a.w.norm), static_cast<unsigned long long>(v));
+}
+
+// ---- the loss and its gradients ----
+
+// The sum of a sequence over all chunks that it spans, by one warp.
+template <bool SUMS>
+__device__ __forceinline__ void across_chunks(const PolicyArgs &a, int64_t lo, int64_t hi, int &count, double &sum) {
+    const int lane = threadIdx.x & 31;
+    int n = 0;
+    double v = 0.0;
+    const int64_t c0 = lo / kChunkTokens + 1, c1 = min((hi - 1) / kChunkTokens, a.chunks - 1);
+    for (int64_t c = c0 + lane; c <= c1; c += 32) {
+        n += a.w.head_count[c];
+        if (SUMS) v += a.w.head_sum[c];
+    }
+    for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(~0u, n, d);
+    if (SUMS) v = warp_sum(v);
+    count = a.w.slot_count[lo] + n;
+    sum = SUMS ? a.w.slot_sum[lo] + v : 0.0;
+}
+
+// SINGLE: all tokens in one CTA, which counts them itself.
+template <int THREADS, bool SINGLE, bool SUMS>
+__global__ void __launch_bounds__(THREADS) policy_kernel(const PolicyArgs a) {
+    constexpr int T = THREADS * kE;
+    extern __shared__ __align__(16) unsigned char raw[];
+    ChunkShared<THREADS> &sh = *reinterpret_cast<ChunkShared<THREADS> *>(raw);
+    Piece *const pieces = reinterpret_cast<Piece *>(raw + (sizeof(ChunkShared<THREADS>) + 15) / 16 * 16);
+    __shared__ float stat_part[kSums][THREADS / 32];
+    __shared__ bool last_cta;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int64_t c = SINGLE ? 0 : blockIdx.x, c0 = c * T, i = c0 + tid * kE;
+    if (SINGLE) {
+        pdl_launch_dependents();
+        pdl_wait_previous();
+    }
+    // (many: whatever filled the inputs was complete when the kernel before this one let it start)
+    uint32_t on = load_mask(a.mask, i, a.n, a.vector);
+    float lp[kE], old[kE], ref[kE], ent[kE];
+    load8(a.logprob, i, a.n, a.vector, lp);
+    load8(a.old, i, a.n, a.vector, old);
+    if (a.ref != nullptr) load8(a.ref, i, a.n, a.vector, ref);
+    if (a.entropy != nullptr) load8(a.entropy, i, a.n, a.vector, ent);
+    const int first = find_sequences<THREADS>(a, c0, sh);
+    uint32_t inside = i >= a.n ? 0u : a.n - i >= kE ? (1u << kE) - 1 : (1u << int(a.n - i)) - 1;
+    {
+        int cur = first;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            if (sh.start[tid * kE + e] != kNone) cur = tid * kE + e;
+            if (sh.start[cur] == kOutside) inside &= ~(1u << e);
+        }
+    }
+    on &= inside;
+    long long norm;
+    if (SINGLE) {
+        // the sums stand in the pieces until what tokens need takes their place
+        sequence_sums<THREADS, SUMS>(a, c0, first, on, lp, old, sh, [&](int start, int count, double sum) {
+            pieces[start].weight = __int_as_float(count);
+            if (SUMS) *reinterpret_cast<double *>(&pieces[start].used) = sum;
+        });
+        __syncthreads();
+        long long mine = 0;
+        if (a.per_sequence) {
+            for (int p = tid; p < T; p += THREADS)
+                if (sh.start[p] >= 0) mine += __float_as_int(pieces[p].weight) > 0;
+        } else {
+            mine = __popc(on);
+        }
+        norm = block_sum<THREADS>(mine);
+        for (int p = tid; p < T; p += THREADS) {
+            const int s = sh.start[p];
+            if (s < 0) continue;
+            const double sum = SUMS ? *reinterpret_cast<const double *>(&pieces[p].used) : 0.0;
+            pieces[p] = piece_of<SUMS>(a, s, __float_as_int(pieces[p].weight), sum, norm);
+        }
+    } else {
+        pdl_launch_dependents();
+        pdl_wait_previous();
+        __syncthreads();
+        norm = a.counted ? *a.w.norm : block_sum<THREADS>(counted(a, tid, THREADS));
+        // the sequences at the chunk's ends may go on beyond it
+        for (int p = tid; p < T; p += THREADS) {
+            const int s = sh.start[p];
+            if (s < 0) continue;
+            const int64_t lo = p > 0 ? c0 + p : sh.before, hi = a.offsets[s + 1];
+            if (lo < c0 || hi > c0 + T) continue;
+            pieces[p] = piece_of<SUMS>(a, s, a.w.slot_count[lo], SUMS ? a.w.slot_sum[lo] : 0.0, norm);
+        }
+        const int p = warp == 0 ? 0 : sh.last;
+        const int s = sh.start[p];
+        if (s >= 0 && warp < 2 && !(warp == 1 && p == 0)) {
+            const int64_t lo = p > 0 ? c0 + p : sh.before, hi = a.offsets[s + 1];
+            if (lo < c0 || hi > c0 + T) {
+                int count;
+                double sum;
+                across_chunks<SUMS>(a, max(lo, int64_t(0)), min(hi, a.n), count, sum);
+                if (lane == 0) pieces[p] = piece_of<SUMS>(a, s, count, sum, norm);
+            }
+        }
+    }
+    __syncthreads();
+
+    float stat[kSums] = {}, d_lp[kE], d_ent[kE];   // policy, kl, entropy, clipped
+    Piece piece = {};
+    int cur = first;
+    if (inside & 1 && sh.start[tid * kE] == kNone) piece = pieces[cur];
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+        d_lp[e] = d_ent[e] = 0.0f;
+        if ((inside >> e & 1) && sh.start[tid * kE + e] != kNone) piece = pieces[tid * kE + e];
+        if (!(on >> e & 1)) continue;
+        const float w = fabsf(piece.weight), adv = piece.advantage;
+        float used, slope;
+        bool cut;
+        if (SUMS) {
+            cut = piece.weight < 0.0f, used = piece.used, slope = piece.slope;
+        } else {
+            float hi, lo;
+            difference(lp[e], old[e], hi, lo);
+            const bool up = adv >= 0.0f;
+            cut = up ? past(hi, lo, a.high, 1.0f) : past(hi, lo, a.low, -1.0f);
+            const float r = expf(hi);
+            used = cut ? (up ? a.used_high : a.used_low) : r;
+            slope = cut ? 0.0f : -adv * r;
+        }
+        float d = slope;
+        stat[0] += w * (-adv * used);
+        if (cut) stat[3] += w;
+        if (a.ref != nullptr) {
+            const float x = ref[e] - lp[e], em1 = expm1f(x);
+            stat[1] += w * excess(x, em1);
+            if (a.kl_coef != 0.0f) d -= a.kl_coef * em1;
+        }
+        if (a.entropy != nullptr) stat[2] += w * ent[e];
+        d_lp[e] = w * d;
+        d_ent[e] = -a.entropy_coef * w;
+    }
+    store8(a.d_logprob, i, inside, a.vector, d_lp);
+    if (a.d_entropy != nullptr) store8(a.d_entropy, i, inside, a.vector, d_ent);
+
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        const float v = warp_sum(stat[k]);
+        if (lane == 0) stat_part[k][warp] = v;
+    }
+    __syncthreads();
+    double sums[kSums];
+    if (tid == 0) {
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) {
+            sums[k] = 0.0;
+            for (int w = 0; w < THREADS / 32; ++w) sums[k] += double(stat_part[k][w]);
+        }
+    }
+    if (SINGLE) {
+        if (tid == 0) write_stats(a, sums);
+        return;
+    }
+    // the CTA that is done last adds the chunks up, in an order that does not depend on which it is
+    if (tid == 0) {
+        for (int k = 0; k < kSums; ++k) a.w.partial[k * a.chunks + c] = sums[k];
+        __threadfence();
+        last_cta = atomicAdd(a.w.ticket, 1) == int(gridDim.x) - 1;
+    }
+    __syncthreads();
+    if (!last_cta) return;
+    __threadfence();
+    __shared__ double wide[kSums][THREADS / 32];
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        double v = 0.0;
+        for (int64_t j = tid; j < a.chunks; j += THREADS) v += __ldcg(a.w.partial + k * a.chunks + j);
+        v = warp_sum(v);
+        if (lane == 0) wide[k][warp] = v;
+    }
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) {
+            sums[k] = 0.0;
+            for (int w = 0; w < THREADS / 32; ++w) sums[k] += wide[k][w];
+        }
+        write_stats(a, sums);
+    }
+}
+
+// ---- host ----
+
+int64_t chunks_of(int64_t n) { return (n + kChunkTokens - 1) / kChunkTokens; }
+
+// The parts of the scratch one after the other; its size.
+int64_t lay_work(char *base, int64_t n, PolicyWork &w) {
+    const int64_t c = chunks_of(n);
+    int64_t at = 0;
+    const auto take = [&](auto *&p, int64_t count) {
+        p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at);
+        at += (count * int64_t(sizeof(*p)) + 15) / 16 * 16;
+    };
+    take(w.slot_sum, n);
+    take(w.head_sum, c);
+    take(w.partial, kSums * c);
+    take(w.slot_count, n);
+    take(w.head_count, c);
+    take(w.head_start, c);
+    take(w.count, c);
+    take(w.norm, 1);
+    take(w.ticket, 1);
+    return at;
+}
+int64_t policy_work(int64_t n) {
+    PolicyWork w;
+    return n <= kFew ? 0 : lay_work(nullptr, n, w);
+}
+
+void split_border(double v, float (&b)[3]) {
+    b[0] = float(v);
+    if (!std::isfinite(v)) {
+        b[1] = b[2] = 0.0f;
+        return;
+    }
+    b[1] = float(v - double(b[0]));
+    b[2] = float(v - double(b[0]) - double(b[1]));
+}
+
+template <int THREADS, bool SINGLE, bool SUMS>
+cudaError_t launch_policy_kernel(const PolicyArgs &a, cudaStream_t stream) {
+    const auto kernel = policy_kernel<THREADS, SINGLE, SUMS>;
+    const size_t smem = (sizeof(ChunkShared<THREADS>) + 15) / 16 * 16 + THREADS * kE * sizeof(Piece);
+    const cudaError_t e = allow_smem(kernel, smem + 4096);
+    if (e != cudaSuccess) return e;
+    return launch_ex(kernel, dim3(unsigned(SINGLE ? 1 : a.chunks)), dim3(THREADS), smem, stream, 1, true, a);
+}
+
+template <bool SUMS>
+cudaError_t launch_policy(PolicyArgs &a, cudaStream_t stream) {
+    if (a.n <= kFew) return launch_policy_kernel<kFew / kE, true, SUMS>(a, stream);
+    cudaError_t e = launch_ex(policy_count_kernel<SUMS>, dim3(unsigned(a.chunks)), dim3(kChunkThreads), 0, stream, 1, true, a);
+    if (e != cudaSuccess) return e;
+    const int64_t sums = a.chunks + (a.per_sequence ? a.sequences : 0);
+    a.counted = sums > kInline;
+    if (a.counted) {
+        e = launch_ex(policy_norm_kernel, dim3(unsigned(std::min<int64_t>((sums + 2047) / 2048, 1024))), dim3(kChunkThreads), 0, stream, 1, true, a);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_policy_kernel<kChunkThreads, false, SUMS>(a, stream);
+}
+
+}  // namespace
+}  // namespace darb
+
+using namespace darb;
+
+extern "C" {
+
+darb_status_t darb_policy_loss_work(int64_t tokens, int64_t *bytes) {
+    DARB_TRACE("darb_policy_loss_work");
+    if (bytes == nullptr || tokens < 0) return DARB_ERR_INVALID_ARG;
+    if (tokens > kMaxTokens) return DARB_ERR_UNSUPPORTED;
+    *bytes = policy_work(tokens);
+    return DARB_OK;
+}
+
+darb_status_t darb_policy_loss(int64_t tokens, int64_t sequences, const float *logprob, const float *old_logprob,
+                               const float *ref_logprob, const float *entropy, const uint8_t *mask, const float *advantage,
+                               const int64_t *offsets, double clip_low, double clip_high, double kl_coef,
+                               double entropy_coef, darb_per_t ratio, darb_per_t mean, float *stats, float *d_logprob,
+                               float *d_entropy, void *work, cudaStream_t stream) {
+    DARB_TRACE("darb_policy_loss");
+    if (tokens < 0 || sequences < 0 || stats == nullptr || offsets == nullptr) return DARB_ERR_INVALID_ARG;
+    if ((ratio != DARB_PER_TOKEN && ratio != DARB_PER_SEQUENCE) || (mean != DARB_PER_TOKEN && mean != DARB_PER_SEQUENCE)) return DARB_ERR_INVALID_ARG;
+    if (!(clip_low >= 0.0 && clip_low <= 1.0) || !(clip_high >= 0.0) || !std::isfinite(kl_coef) || !std::isfinite(entropy_coef))
+        return DARB_ERR_INVALID_ARG;
+    if (tokens > 0 && (logprob == nullptr || old_logprob == nullptr || d_logprob == nullptr)) return DARB_ERR_INVALID_ARG;
+    if (sequences > 0 && advantage == nullptr) return DARB_ERR_INVALID_ARG;
+    if (tokens > 0 && ((kl_coef != 0.0 && ref_logprob == nullptr) || (entropy == nullptr && (entropy_coef != 0.0 || d_entropy != nullptr))))
+        return DARB_ERR_INVALID_ARG;
+    if (tokens > kMaxTokens || sequences > kMaxTokens) return DARB_ERR_UNSUPPORTED;
+    for (const void *p : {static_cast<const void *>(logprob), static_cast<const void *>(old_logprob), static_cast<const void *>(ref_logprob),
+                          static_cast<const void *>(entropy), static_cast<const void *>(advantage), static_cast<const void *>(stats),
+                          static_cast<const void *>(d_logprob), static_cast<const void *>(d_entropy)})
+        if (!aligned_to(p, 4)) return DARB_ERR_INVALID_ARG;
+    if (!aligned_to(offsets, 8) || !aligned_to(work, 16)) return DARB_ERR_INVALID_ARG;
+    const int64_t need = policy_work(tokens), v = tokens * 4;
+    const Range ins[] = {{logprob, v}, {old_logprob, v}, {ref_logprob, v}, {entropy, v}, {mask, tokens}, {advantage, sequences * 4}, {offsets, (sequences + 1) * 8}};
+    const Range outs[] = {{stats, kStats * 4}, {d_logprob, v}, {d_entropy, v}, {work, need}};
+    if (!outputs_apart(outs, ins)) return DARB_ERR_INVALID_ARG;
+
+    PolicyArgs a = {};
+    a.logprob = logprob, a.old = old_logprob, a.ref = ref_logprob, a.entropy = entropy, a.advantage = advantage;
+    a.mask = mask, a.offsets = offsets, a.stats = stats, a.d_logprob = d_logprob, a.d_entropy = d_entropy;
+    a.n = tokens, a.sequences = sequences, a.chunks = chunks_of(tokens);
+    a.log_low = std::log1p(-clip_low), a.log_high = std::log1p(clip_high);
+    split_border(a.log_low, a.low);
+    split_border(a.log_high, a.high);
+    a.used_low = float(1.0 - clip_low), a.used_high = float(1.0 + clip_high);
+    a.kl_coef = float(kl_coef), a.entropy_coef = float(entropy_coef);
+    a.per_sequence = mean == DARB_PER_SEQUENCE;
+    a.vector = aligned_to(mask, 8);
+    for (const float *p : {logprob, old_logprob, ref_logprob, entropy, static_cast<const float *>(d_logprob), static_cast<const float *>(d_entropy)})
+        a.vector = a.vector && aligned_to(p, 16);
+    return enqueue([&] {
+        void *mine = nullptr;
+        if (need > 0 && work == nullptr) {
+            const cudaError_t e = stream_alloc(&mine, size_t(need), stream);
+            if (e != cudaSuccess) return e;
+        }
+        lay_work(static_cast<char *>(work != nullptr ? work : mine), tokens, a.w);
+        cudaError_t e = ratio == DARB_PER_SEQUENCE ? launch_policy<true>(a, stream) : launch_policy<false>(a, stream);
+        if (mine != nullptr) {
+            const cudaError_t f = cudaFreeAsync(mine, stream);
+            if (e == cudaSuccess) e = f;
+        }
+        return e;
+    });
+}
+
+}  // extern "C"

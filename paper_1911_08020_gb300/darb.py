@@ -23,6 +23,7 @@ F32, BF16 = 0, 1
 PATH_AUTO, PATH_CUDA_CORES, PATH_TENSOR_CORES = 0, 1, 2
 TOKEN_ROWS, TOKEN_COLUMNS = 0, 1
 GATES_LOGITS, GATES_VALUES = 0, 1
+PER_TOKEN, PER_SEQUENCE = 0, 1
 MAX_BLOCK = 256
 MAX_TOP = 32
 ADAMW_BLOCK = 256
@@ -91,6 +92,9 @@ def lib():
                                     I64, I64, P, S],
                 "darb_gated_scan_grad": [P, I64, I64, P, I64, I64, P, I64, I64, P, I64, I64, ctypes.c_int, ctypes.c_int,
                                          ctypes.c_int, I64, I64, I64, P, P, P, I64, I64, P, I64, I64, P, S],
+                "darb_policy_loss": [I64, I64, P, P, P, P, P, P, P, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                                     ctypes.c_double, ctypes.c_int, ctypes.c_int, P, P, P, P, S],
+                "darb_policy_loss_work": [I64, P],
                 "darb_adamw_create": [I32, P, P, P, P, P, P, P, ctypes.c_int, P, S],
                 "darb_adamw_step": [P, P, P, I64, ctypes.c_uint64, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                     ctypes.c_double, ctypes.c_double, S],
@@ -430,6 +434,15 @@ def _new(shape, dtype, device, stream):
     return t
 
 
+def _zero(t, stream):
+    """Zeros in a new tensor, in the order of `stream`."""
+    if stream is None:
+        t.zero_()
+        return
+    with _torch.cuda.stream(_torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        t.zero_()
+
+
 def _tokens(t, dim: int, call: str, name: str) -> tuple[int, int, int, int, int]:
     """(layout, steps, tokens, features, ld) of a tensor whose features lie along `dim`: 2-D with
     either axis contiguous, or 3-D (steps, features, tokens) with contiguous tokens."""
@@ -730,6 +743,77 @@ def darb_gated_scan_grad(dh, gate, x, h, h0=None, d_last=None, dim: int = 0, gat
                                       *_scan_operand(d_x, x, oa, sa, call, "d_x"), _vector(d_h0, n, f32, call, "d_h0"),
                                       _stream(stream)), call)
     return d_gate, d_x, d_h0
+
+
+# ---- the loss of drawn answers ----
+
+class PolicyLoss(NamedTuple):
+    """Results of darb_policy_loss: stats, float32 (5,): loss, policy, kl, entropy, share of the clipped weight; the
+    gradients of the loss, float32 (tokens,); and the call's scratch."""
+    stats: object
+    d_logprob: object
+    d_entropy: object
+    work: object
+
+    @staticmethod
+    def empty(tokens: int, device="cuda", entropy: bool = False, stream=None) -> "PolicyLoss":
+        """Buffers for `tokens` tokens, to be passed as `out`."""
+        torch = _torch or _load_torch()
+        need = darb_policy_loss_work(tokens)
+        return PolicyLoss(_new((5,), torch.float32, device, stream), _new((tokens,), torch.float32, device, stream),
+                          _new((tokens,), torch.float32, device, stream) if entropy else None,
+                          _new((need,), torch.uint8, device, stream) if need else None)
+
+
+def darb_policy_loss(logprob, old_logprob, advantage, offsets, ref_logprob=None, entropy=None, mask=None, clip_low: float = 0.2,
+                     clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0, ratio: int = PER_TOKEN,
+                     mean: int = PER_TOKEN, out: PolicyLoss | None = None, stream=None) -> PolicyLoss:
+    """The clipped policy loss of answers that a model drew, with a KL term and an entropy bonus, and its
+    gradients with respect to log probabilities and entropies, as darb_token_logprobs_grad takes them.
+
+    logprob, old_logprob, ref_logprob, entropy: float32 (tokens,), the answers one after the other; advantage:
+    float32 (sequences,); offsets: int64 (sequences + 1,), where each starts; mask: bool or uint8 (tokens,),
+    the tokens that count.  ratio, mean: PER_TOKEN or PER_SEQUENCE.  out: buffers to write; new ones, with the
+    gradients 0 outside of all sequences, if None."""
+    call = "darb_policy_loss"
+    torch = _torch or _load_torch()
+    f32 = torch.float32
+    n, sequences = logprob.numel(), advantage.numel()
+    if out is None:
+        out = PolicyLoss.empty(n, logprob.device, entropy is not None, stream)
+        for t in out[1:3]:
+            if t is not None:
+                _zero(t, stream)
+    if mask is not None and mask.dtype not in (torch.bool, torch.uint8):
+        _refuse(call, "mask must be bool or uint8")
+    work = out.work
+    if work is not None:
+        if n <= 4096:
+            work = None
+        else:
+            need = darb_policy_loss_work(n)
+            if not work.is_cuda or not work.is_contiguous() or work.numel() * work.element_size() < need:
+                _refuse(call, f"work must be a contiguous CUDA tensor of {need} bytes")
+    if out.stats is None or (n and out.d_logprob is None):
+        _refuse(call, "stats and d_logprob must be there")
+    _check(lib().darb_policy_loss(n, sequences, _vector(logprob, n, f32, call, "logprob"),
+                                  _vector(old_logprob, n, f32, call, "old_logprob"),
+                                  _vector(ref_logprob, n, f32, call, "ref_logprob"), _vector(entropy, n, f32, call, "entropy"),
+                                  None if mask is None else _vector(mask, n, mask.dtype, call, "mask"),
+                                  _vector(advantage, sequences, f32, call, "advantage"),
+                                  _vector(offsets, sequences + 1, torch.int64, call, "offsets"), clip_low, clip_high, kl_coef,
+                                  entropy_coef, ratio, mean, _vector(out.stats, 5, f32, call, "stats"),
+                                  _vector(out.d_logprob, n, f32, call, "d_logprob"),
+                                  _vector(out.d_entropy, n, f32, call, "d_entropy"),
+                                  None if work is None else work.data_ptr(), _stream(stream)), call)
+    return out
+
+
+def darb_policy_loss_work(tokens: int) -> int:
+    """Bytes of scratch that darb_policy_loss needs for so many tokens."""
+    need = ctypes.c_int64()
+    _check(lib().darb_policy_loss_work(tokens, ctypes.byref(need)), "darb_policy_loss_work")
+    return need.value
 
 
 class AdamW:
