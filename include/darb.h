@@ -668,6 +668,59 @@ DARB_API darb_status_t darb_adamw_sync_status(darb_adamw_t plan, cudaStream_t st
 /* Release a plan (not its tensors); NULL is a no-op.  Waits for the device.    */
 DARB_API darb_status_t darb_adamw_destroy(darb_adamw_t plan);
 
+typedef struct darb_muon_s *darb_muon_t;
+
+/*
+ * A plan for updates of n weight matrices whose momentum is orthogonalised by
+ * Newton-Schulz products, next to darb_adamw_create (which is left the vectors).  The
+ * matrices are dense, row after row, and the caller's; they have to stay where they are
+ * while the plan lives.
+ *   rows, cols   host int64[n], 0 allowed, 32768 at most
+ *   params   host array of n device pointers, fp32[rows x cols], updated by every step
+ *   m        host array of n device pointers, fp32, the momentum
+ *   copies   host array of n device pointers (NULL entries allowed), bf16: the updated
+ *            parameters rounded, e.g. for darb_reencode; NULL: none
+ *   gtype    type of the gradients
+ * No two of the buffers may overlap.  Allocates tables and scratch on the current device (8
+ * bytes an element and 8 bytes for every pair of the shorter side's), runs on `stream` and
+ * synchronises it.
+ * Errors: DARB_ERR_INVALID_ARG; DARB_ERR_UNSUPPORTED (a longer side); DARB_ERR_OOM;
+ * DARB_ERR_CUDA.
+ */
+DARB_API darb_status_t darb_muon_create(int32_t n, const int64_t *rows, const int64_t *cols, float *const *params,
+                                        float *const *m, void *const *copies, darb_dtype_t gtype, darb_muon_t *out,
+                                        cudaStream_t stream);
+
+/*
+ * One step: with g' = g * *grad_scale and |u| the root of the sum of all squares,
+ *   m = beta m + (1 - beta) g',  u = (1 - beta) g' + beta m (nesterov == 0: m),
+ *   X = u / (|u| + eps), transposed where there are more rows than columns,
+ *   five times  A = X X^T,  X = 3.4445 X + (-4.7750 A + 2.0315 A A) X,
+ *   p = p (1 - lr weight_decay) - lr 0.2 sqrt(max(rows, cols)) X.
+ *   grads    host array of n device pointers of the plan's gradient type, as dense as the
+ *            parameters; a NULL entry leaves its matrix and momentum as they are
+ *   grad_scale  device fp32 scalar (what clipping by the norm gives), or NULL: 1
+ * The products' operands are fp16 with all sums in fp32, and the diagonals of A and its
+ * polynomial are kept in fp32.  With bf16 gradients X is off by about 1e-3 of itself
+ * (its norm), with fp32 gradients, whose operands are two fp16 numbers each, by about
+ * 1e-5.  A NaN or infinity in a gradient makes its whole matrix NaN; zero gradients
+ * and momentum give X = 0.
+ * Asynchronous on `stream`; allocates nothing; 17 launches (two more for every further
+ * 448 matrices).  Results do not depend on the order of anything.  Steps of one plan must
+ * be ordered on one stream.
+ * Errors: DARB_ERR_INVALID_ARG (an unknown plan, lr or weight_decay negative or not finite, beta
+ * outside [0, 1), eps not above 0 or not finite, a gradient or grad_scale that overlaps a
+ * buffer of any of the plan's matrices); DARB_ERR_CUDA.
+ */
+DARB_API darb_status_t darb_muon_step(darb_muon_t plan, const void *const *grads, const float *grad_scale, double lr,
+                                      double beta, double weight_decay, double eps, int nesterov, cudaStream_t stream);
+
+/* As darb_adamw_sync_status: DARB_ERR_TIMEOUT if a bounded device wait gave up. */
+DARB_API darb_status_t darb_muon_sync_status(darb_muon_t plan, cudaStream_t stream);
+
+/* Release a plan (not its matrices); NULL is a no-op.  Waits for the device.   */
+DARB_API darb_status_t darb_muon_destroy(darb_muon_t plan);
+
 typedef struct {
     int64_t rows, cols;
     int64_t nnzb;            /* kept weights = blocks = sum_r ceil(cols / m_r)           */

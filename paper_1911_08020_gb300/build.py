@@ -25,7 +25,7 @@ BASE_LIB = os.path.join(PKG, "libdarb_baselines.so")
 BASE_SOURCES = ["baselines.cu"]
 SOURCES = ["darb_api.cu", "assign.cu", "encode.cu", "spmm.cu", "spmm_batch.cu", "spmm_tc.cu", "rnn.cu", "rnn_batch.cu", "rnn_step.cu",
            "noalloc.cu", "sequence.cu", "logprobs.cu",
-           "layer_norm.cu", "adamw.cu", "scan.cu", "policy.cu"]
+           "layer_norm.cu", "adamw.cu", "scan.cu", "policy.cu", "muon.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

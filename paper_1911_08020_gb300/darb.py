@@ -100,6 +100,11 @@ def lib():
                                     ctypes.c_double, ctypes.c_double, S],
                 "darb_adamw_sync_status": [P, S],
                 "darb_adamw_destroy": [P],
+                "darb_muon_create": [I32, P, P, P, P, P, ctypes.c_int, P, S],
+                "darb_muon_step": [P, P, P, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_int,
+                                   S],
+                "darb_muon_sync_status": [P, S],
+                "darb_muon_destroy": [P],
             }
             for name, args in sig.items():
                 fn = getattr(L, name)
@@ -872,12 +877,8 @@ def darb_adamw_create(params, m, v, m_scale=None, v_scale=None, copies=None, gra
     return AdamW(out.value, lists, numels, grad_dtype)
 
 
-def darb_adamw_step(plan: AdamW, grads, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
-                    weight_decay: float = 0.01, grad_scale=None, seed: int | None = None, stream=None):
-    """One step (step >= 1) with the gradients `grads` of the plan's tensors (None: that tensor is left as it
-    is).  grad_scale: float32 CUDA scalar that multiplies every gradient.  seed: of the rounding of states in
-    8 bits, the step itself if None."""
-    call = "darb_adamw_step"
+def _gradient_pointers(plan, grads, call: str):
+    """The gradients of a plan's tensors (None where there is none) as an array of pointers."""
     pointers, dtype = plan.pointers, plan.grad_dtype
     if len(grads) != len(plan.numels):
         _refuse(call, "one gradient for every parameter")
@@ -888,6 +889,16 @@ def darb_adamw_step(plan: AdamW, grads, step: int, lr: float, beta1: float = 0.9
         if g.dtype != dtype or not g.is_cuda or g.numel() != n or not g.is_contiguous():
             _refuse(call, f"gradient {i} must be a contiguous CUDA {dtype} tensor of {n} values")
         pointers[i] = g.data_ptr()
+    return pointers
+
+
+def darb_adamw_step(plan: AdamW, grads, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                    weight_decay: float = 0.01, grad_scale=None, seed: int | None = None, stream=None):
+    """One step (step >= 1) with the gradients `grads` of the plan's tensors (None: that tensor is left as it
+    is).  grad_scale: float32 CUDA scalar that multiplies every gradient.  seed: of the rounding of states in
+    8 bits, the step itself if None."""
+    call = "darb_adamw_step"
+    pointers = _gradient_pointers(plan, grads, call)
     _check(lib().darb_adamw_step(plan.ptr, pointers, _vector(grad_scale, 1, (_torch or _load_torch()).float32, call, "grad_scale"),
                                  step, (step if seed is None else seed) & 0xFFFFFFFFFFFFFFFF, lr, beta1, beta2, eps,
                                  weight_decay, _stream(stream)), call)
@@ -902,4 +913,69 @@ def darb_adamw_destroy(plan: AdamW | None):
     if plan is None or plan.ptr is None:
         return
     _check(lib().darb_adamw_destroy(plan.ptr), "darb_adamw_destroy")
+    plan.ptr = None
+
+
+class Muon:
+    """A plan of darb_muon_create (owned; free with darb_muon_destroy).  Holds on to its tensors."""
+
+    def __init__(self, ptr: int, tensors, numels, grad_dtype):
+        self.ptr, self.tensors, self.numels, self.grad_dtype = ptr, tensors, numels, grad_dtype
+        self.pointers = (ctypes.c_void_p * len(numels))()
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        darb_muon_destroy(self)
+
+
+def darb_muon_create(params, m, copies=None, grad_dtype=None, stream=None) -> Muon:
+    """A plan for updates with orthogonalised momentum of the float32 CUDA matrices `params`, all contiguous.
+
+    m: the momentum, float32 of the parameters' shapes.  copies: bfloat16 tensors (or None) that receive the
+    rounded parameters, e.g. for darb_reencode.  grad_dtype: float32 (default) or bfloat16."""
+    call = "darb_muon_create"
+    torch = _torch or _load_torch()
+    params, m = list(params), list(m)
+    copies = None if copies is None else list(copies)
+    n = len(params)
+    if len(m) != n or (copies is not None and len(copies) != n):
+        _refuse(call, "one momentum (and copy) for every parameter")
+    grad_dtype = torch.float32 if grad_dtype is None else grad_dtype
+    if grad_dtype not in (torch.float32, torch.bfloat16):
+        _refuse(call, "grad_dtype must be float32 or bfloat16")
+    for name, tensors, dtype in (("params", params, torch.float32), ("m", m, torch.float32), ("copies", copies or (), torch.bfloat16)):
+        for t, p in zip(tensors, params):
+            if t is None and name == "copies":
+                continue
+            if t.dim() != 2 or not t.is_cuda or t.dtype != dtype or t.shape != p.shape or not t.is_contiguous():
+                _refuse(call, f"{name} must be contiguous CUDA matrices of {dtype}, of the parameters' shapes")
+    array = lambda ts: (ctypes.c_void_p * n)(*[None if t is None else t.data_ptr() for t in ts])  # noqa: E731
+    sides = [(ctypes.c_int64 * n)(*[p.shape[i] for p in params]) for i in range(2)]
+    out = ctypes.c_void_p()
+    _check(lib().darb_muon_create(n, *sides, array(params), array(m), None if copies is None else array(copies),
+                                  BF16 if grad_dtype == torch.bfloat16 else F32, ctypes.byref(out), _stream(stream)), call)
+    return Muon(out.value, [params, m, copies], [p.numel() for p in params], grad_dtype)
+
+
+def darb_muon_step(plan: Muon, grads, lr: float, beta: float = 0.95, weight_decay: float = 0.01, eps: float = 1e-7,
+                   nesterov: bool = True, grad_scale=None, stream=None):
+    """One step with the gradients `grads` of the plan's matrices (None: that matrix is left as it is).
+    grad_scale: float32 CUDA scalar that multiplies every gradient."""
+    call = "darb_muon_step"
+    pointers = _gradient_pointers(plan, grads, call)
+    _check(lib().darb_muon_step(plan.ptr, pointers, _vector(grad_scale, 1, (_torch or _load_torch()).float32, call, "grad_scale"),
+                                lr, beta, weight_decay, eps, bool(nesterov), _stream(stream)), call)
+
+
+def darb_muon_sync_status(plan: Muon, stream=None):
+    """Synchronise and raise if a step's bounded wait gave up."""
+    _check(lib().darb_muon_sync_status(plan.ptr, _stream(stream)), "darb_muon_sync_status")
+
+
+def darb_muon_destroy(plan: Muon | None):
+    if plan is None or plan.ptr is None:
+        return
+    _check(lib().darb_muon_destroy(plan.ptr), "darb_muon_destroy")
     plan.ptr = None
