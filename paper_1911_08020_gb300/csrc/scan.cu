@@ -96,11 +96,9 @@ struct Word<T, 1> {
 template <bool LOGITS>
 __device__ __forceinline__ void open_gate(float gate, float &a, float &rest) {
     if (LOGITS) {
-        const float e = exp2_fast(-kLog2e * fabsf(gate));
-        const float near = __fdividef(1.0f, 1.0f + e), far = e * near;
-        const bool up = gate >= 0.0f;
-        a = up ? near : far;
-        rest = up ? far : near;
+        const float e = exp2_fast(-kLog2e * gate);
+        a = __fdividef(1.0f, 1.0f + e);
+        rest = gate >= 0.0f ? e * a : 1.0f - a;
     } else {
         a = gate;
         rest = 1.0f - gate;
@@ -117,20 +115,441 @@ __device__ __forceinline__ void cluster_meet() {
     cluster_arrive();
     cluster_wait();
 }
-__device__ __forceinline__ void store_remote(float *here, uint32_t rank, float v) {
+__device__ __forceinline__ uint32_t remote(const void *here, uint32_t rank) {
     uint32_t to;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(here)), "r"(rank));
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v) : "memory");
+    return to;
 }
+__device__ __forceinline__ void store_remote(float *here, uint32_t rank, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote(here, rank)), "f"(v) : "memory");
+}
+__device__ __forceinline__ void store_remote(float2 *here, uint32_t rank, float2 v) {
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(remote(here, rank)), "f"(v.x), "f"(v.y) : "memory");
+}
+__device__ __forceinline__ void store_remote(float4 *here, uint32_t rank, float4 v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(remote(here, rank)), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
+                 : "memory");
+}
+
+// Four channels' states after a map, and a map after the one before it.
+__device__ __forceinline__ void state_through(float4 A, float4 H, float4 &c) {
+    c = make_float4(through(A.x, H.x, c.x), through(A.y, H.y, c.y), through(A.z, H.z, c.z), through(A.w, H.w, c.w));
+}
+__device__ __forceinline__ void map_through(float4 A, float4 H, float4 &CA, float4 &CH) {
+    state_through(A, H, CH);
+    CA = make_float4(CA.x * A.x, CA.y * A.y, CA.z * A.z, CA.w * A.w);
+}
+
+// An asynchronous copy of 8 or 16 bytes to shared memory (zeros where it is not `on`).
+template <int BYTES>
+__device__ __forceinline__ void cp_async_word(uint32_t dst, const void *src, bool on) {
+    if (BYTES == 16) cp_async16(dst, src, on);
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(on ? 8 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// ---- channels four at a time ----
+
+// A round's inputs wait in shared memory, each thread's in places of its own: loads
+// are on their way for one or two rounds without holding registers, and no barrier
+// goes with them.
+template <int LC>
+constexpr int kStages = LC == 32 ? 2 : 3;
+constexpr int kStageBytes = 128;   // of a thread and round
+
+// LC lanes of a warp have neighbouring channels, the other lanes later steps.
+template <typename T, bool BACK, int LC, bool LOGITS>
+__global__ void __launch_bounds__(kScanThreads, 2) channel_kernel(const ScanArgs s, const int cluster) {
+    constexpr int V = 4, IN = BACK ? 4 : 2, OUT = BACK ? 2 : 1;
+    constexpr int S = kStageBytes / (IN * V * int(sizeof(T)));   // steps of a thread in a round
+    constexpr int TL = 32 / LC, NS = kStages<LC>;
+    using Raw = Word<T, V>;
+    __shared__ float4 s_A[2][kScanWarps][LC], s_H[2][kScanWarps][LC], s_carry[2][kScanWarps][LC];
+    __shared__ float4 s_rA[LC < 32 ? 2 : 1][LC < 32 ? kMaxCluster : 1][LC], s_rH[LC < 32 ? 2 : 1][LC < 32 ? kMaxCluster : 1][LC];
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    Raw *const slots = reinterpret_cast<Raw *>(s_raw) + threadIdx.x;   // [stage][tensor][step][thread]
+
+    pdl_launch_dependents();
+    if (LC < 32 && cluster > 1) cluster_arrive();   // (the others' shared memory is there once they run)
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int cl = lane % LC, tl = lane / LC;
+    const int tg = 1 << s.groups_log, group = warp & (tg - 1), ct = warp >> s.groups_log;
+    const int rank = LC < 32 && cluster > 1 ? int(blockIdx.x) % cluster : 0;
+    const int64_t tile = blockIdx.x / unsigned(cluster);
+    const int64_t steps = s.steps, stride = int64_t(tg) * (TL * S) * cluster;
+    const int64_t c = ((tile * (kScanWarps >> s.groups_log) + ct) * LC + cl) * V;
+    const bool valid = c < s.channels;
+    const int64_t co = valid ? c / s.inner : 0, ci = valid ? c - co * s.inner : 0;
+    int64_t t0 = (int64_t(rank) * tg + group) * (TL * S) + tl * S;   // the thread's first step
+
+    const Operand *const ins[4] = {&s.gate, &s.x, &s.dh, &s.before};
+    const T *in[IN];
+    T *out[OUT];
+#pragma unroll
+    for (int k = 0; k < IN; ++k) in[k] = static_cast<const T *>(ins[k]->p) + co * ins[k]->ld + ci;
+#pragma unroll
+    for (int k = 0; k < OUT; ++k) out[k] = static_cast<T *>(const_cast<void *>(s.out[k].p)) + co * s.out[k].ld + ci;
+
+    const int64_t rounds = (steps + stride - 1) / stride;
+    auto load = [&](int64_t round) {
+        const int64_t t = t0 + round * stride;
+        Raw *const to = slots + (round % NS) * (IN * S * kScanThreads);
+#pragma unroll
+        for (int k = 0; k < IN; ++k) {
+            const T *p = in[k] + t * ins[k]->step;
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
+                // (no state before step 0 in memory: state0)
+                const bool on = round < rounds && valid && t + j < steps - (BACK && k == 3 ? 1 : 0);
+                cp_async_word<sizeof(Raw)>(smem_addr(to + (k * S + j) * kScanThreads), on ? p : static_cast<const T *>(s.gate.p), on);
+                p += ins[k]->step;
+            }
+        }
+        cp_async_commit();
+    };
+
+    pdl_wait_previous();
+#pragma unroll
+    for (int r = 0; r < NS - 1; ++r) load(r);
+    float carry[V], state0[V];   // state0: backward, the state before step 0, in 32 bits
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        carry[v] = valid && s.first != nullptr ? s.first[c + v] : 0.0f;
+        state0[v] = BACK && valid && s.h0 != nullptr ? s.h0[c + v] : 0.0f;
+    }
+    if (LC < 32 && cluster > 1) cluster_wait();
+
+    for (int64_t round = 0; round < rounds; ++round) {
+        const int buf = int(round & 1);
+        load(round + NS - 1);
+        cp_async_wait<NS - 1>();
+        const Raw *const from = slots + (round % NS) * (IN * S * kScanThreads);
+        const int64_t t1 = t0 + round * stride;
+        const int live = t1 >= steps ? 0 : steps - t1 < S ? int(steps - t1) : S;   // of the thread's steps
+
+        // the maps of the steps.  Forward: p = u.  Backward: p = dh, q = what g is
+        // multiplied by in d_gate, rest in d_x
+        float a[S][V], p[S][V], q[BACK ? S : 1][V], rest[BACK ? S : 1][V];
+        float A[V], H[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = 1.0f, H[v] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < S; ++j) {
+            float gate[V], x[V], dh[V], hp[V];
+            const Raw g = from[j * kScanThreads], xr = from[(S + j) * kScanThreads];
+            g.get(gate);
+            xr.get(x);
+            if (BACK) {
+                const Raw d = from[(2 * S + j) * kScanThreads], h = from[((IN - 1) * S + j) * kScanThreads];
+                d.get(dh);
+                h.get(hp);
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float r;
+                open_gate<LOGITS>(gate[v], a[j][v], r);
+                if (BACK) {
+                    const float h = t1 + j == steps - 1 ? state0[v] : hp[v];
+                    const float slope = LOGITS ? a[j][v] * r : 1.0f;
+                    q[j][v] = (s.coupled ? h - x[v] : h) * slope;
+                    rest[j][v] = s.coupled ? r : 1.0f;
+                    p[j][v] = dh[v];
+                } else {
+                    p[j][v] = s.coupled ? r * x[v] : x[v];
+                }
+                if (j >= live) a[j][v] = 1.0f, p[j][v] = 0.0f;
+                H[v] = BACK ? a[j][v] * (H[v] + p[j][v]) : fmaf(a[j][v], H[v], p[j][v]);
+                A[v] *= a[j][v];
+            }
+        }
+
+        // the maps of the lanes before, then all of the warp's
+        float Ae[V], He[V];
+        if (TL > 1) {
+#pragma unroll
+            for (int d = 1; d < TL; d <<= 1) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float pa = __shfl_up_sync(~0u, A[v], d * LC), ph = __shfl_up_sync(~0u, H[v], d * LC);
+                    if (tl >= d) H[v] = through(A[v], H[v], ph), A[v] *= pa;
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                Ae[v] = __shfl_up_sync(~0u, A[v], LC), He[v] = __shfl_up_sync(~0u, H[v], LC);
+                if (tl == 0) Ae[v] = 1.0f, He[v] = 0.0f;
+            }
+        }
+        // the carry into the warp's steps
+        float in_c[V];
+        if (tg > 1) {
+            if (tl == TL - 1) {
+                s_A[buf][warp][cl] = make_float4(A[0], A[1], A[2], A[3]);
+                s_H[buf][warp][cl] = make_float4(H[0], H[1], H[2], H[3]);
+            }
+            __syncthreads();
+            if (LC < 32 && cluster > 1) {
+                // the map of all steps of this CTA, to every CTA
+                if (warp < cluster && tl == 0) {
+                    float4 CA = make_float4(1.0f, 1.0f, 1.0f, 1.0f), CH = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int w = 0; w < kScanWarps; ++w) map_through(s_A[buf][w][cl], s_H[buf][w][cl], CA, CH);
+                    store_remote(&s_rA[buf][rank][cl], warp, CA);
+                    store_remote(&s_rH[buf][rank][cl], warp, CH);
+                }
+                cluster_meet();   // (the slots of a round are written again two meetings later)
+                float4 at = make_float4(carry[0], carry[1], carry[2], carry[3]), mine = at;
+                for (int k = 0; k < cluster; ++k) {
+                    if (k == rank) mine = at;
+                    state_through(s_rA[buf][k][cl], s_rH[buf][k][cl], at);
+                }
+                carry[0] = at.x, carry[1] = at.y, carry[2] = at.z, carry[3] = at.w;
+                in_c[0] = mine.x, in_c[1] = mine.y, in_c[2] = mine.z, in_c[3] = mine.w;
+            } else if (round == 0) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) in_c[v] = carry[v];
+            } else {
+                const float4 at = s_carry[buf ^ 1][ct][cl];
+                in_c[0] = at.x, in_c[1] = at.y, in_c[2] = at.z, in_c[3] = at.w;
+            }
+            const int w0 = warp - group;   // the first warp of these channels
+            for (int w = 0; w < group; ++w) {
+                float4 at = make_float4(in_c[0], in_c[1], in_c[2], in_c[3]);
+                state_through(s_A[buf][w0 + w][cl], s_H[buf][w0 + w][cl], at);
+                in_c[0] = at.x, in_c[1] = at.y, in_c[2] = at.z, in_c[3] = at.w;
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) in_c[v] = carry[v];
+        }
+        if (TL > 1) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) in_c[v] = through(Ae[v], He[v], in_c[v]);
+        }
+
+        // the steps again, from that carry
+        T *to[OUT];
+#pragma unroll
+        for (int k = 0; k < OUT; ++k) to[k] = out[k] + t1 * s.out[k].step;
+#pragma unroll
+        for (int j = 0; j < S; ++j) {
+            float o0[V], o1[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (BACK) {
+                    const float g = p[j][v] + in_c[v];
+                    o0[v] = g * q[j][v];
+                    o1[v] = g * rest[j][v];
+                    in_c[v] = a[j][v] * g;
+                } else {
+                    in_c[v] = fmaf(a[j][v], in_c[v], p[j][v]);
+                    o0[v] = in_c[v];
+                }
+            }
+            if (valid && j < live) {
+                Raw w;
+                w.set(o0);
+                *reinterpret_cast<Raw *>(to[0]) = w;
+                if (BACK) {
+                    w.set(o1);
+                    *reinterpret_cast<Raw *>(to[OUT - 1]) = w;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < OUT; ++k) to[k] += s.out[k].step;
+        }
+        // the carry out of the round, with the lanes that have its last steps
+        if (tg > 1) {
+            if (cluster == 1 && group == tg - 1 && tl == TL - 1) s_carry[buf][ct][cl] = make_float4(in_c[0], in_c[1], in_c[2], in_c[3]);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) carry[v] = TL > 1 ? __shfl_sync(~0u, in_c[v], (TL - 1) * LC + cl) : in_c[v];
+        }
+        if (round + 1 == rounds && s.last != nullptr && valid) {
+            const bool split = LC < 32 && cluster > 1;   // (then all threads have the carry)
+            if (split ? rank == 0 && warp == 0 && tl == 0 : group == tg - 1 && tl == TL - 1) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) s.last[c + v] = split ? carry[v] : in_c[v];
+            }
+        }
+    }
+    cp_async_wait<0>();
+}
+
+// ---- time as the contiguous axis ----
+
+// A row is cut into granules of 16 aligned bytes; the rows of all tensors start equally
+// far past such a boundary.  Granules are numbered in the order of the walk, from
+// the row's last one backward.  A thread takes J of them, 32 apart, so that a warp reads
+// 512 bytes side by side; lanes are put together by shuffles, warps and CTAs as above.
+template <typename T, bool BACK, bool LOGITS>
+__global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, const int cluster) {
+    constexpr int V = kPerGranule<T>, IN = BACK ? 4 : 2, J = 16 / V / (BACK ? 2 : 1);
+    __shared__ float2 s_map[2][kScanWarps], s_remote[2][kMaxCluster];
+
+    pdl_launch_dependents();
+    if (cluster > 1) cluster_arrive();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tg = 1 << s.groups_log, group = warp & (tg - 1), w0 = warp - group;
+    const int rank = cluster > 1 ? int(blockIdx.x) % cluster : 0;
+    const int64_t row = (blockIdx.x / unsigned(cluster)) * int64_t(kScanWarps >> s.groups_log) + (warp >> s.groups_log);
+    const bool valid = row < s.channels;
+    const int64_t steps = s.steps;
+    const Operand *const ins[4] = {&s.gate, &s.x, &s.dh, &s.before};
+    const T *in[IN];
+#pragma unroll
+    for (int k = 0; k < IN; ++k) in[k] = static_cast<const T *>(ins[k]->p) + (valid ? row * ins[k]->ld : 0);
+    T *const out0 = static_cast<T *>(const_cast<void *>(s.out[0].p)) + (valid ? row * s.out[0].ld : 0);
+    T *const out1 = BACK ? static_cast<T *>(const_cast<void *>(s.out[1].p)) + (valid ? row * s.out[1].ld : 0) : nullptr;
+    const int head = row_head<T>(in[0]);
+    const int64_t granules = valid ? row_granules<T>(head, steps) : 0;
+    const int64_t most = (steps + V - 1) / V + 1;   // of any row
+    const int64_t stride = int64_t(tg) * (32 * J) * cluster, rounds = (most + stride - 1) / stride;
+    // the first step of the thread's j-th granule in a round
+    auto first_step = [&](int64_t round, int j) {
+        const int64_t w = round * stride + (int64_t(rank) * tg + group) * (32 * J) + j * 32 + lane;
+        return (w >= granules ? steps : (BACK ? granules - 1 - w : w) * V - head);
+    };
+
+    uint4 raw[IN][J];
+    float edge[J];   // backward: the state before the granule's first step
+    auto load = [&](int64_t round) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int64_t t = first_step(round, j);
+            if (t >= steps) continue;
+#pragma unroll
+            for (int k = 0; k < IN; ++k) raw[k][j] = load_granule<T, false>(in[k], t, steps, 0.0f);
+            if (BACK) edge[j] = t > 0 ? widen(in[IN - 1][t - 1]) : 0.0f;
+        }
+    };
+    pdl_wait_previous();
+    load(0);
+    float carry = valid && s.first != nullptr ? s.first[row] : 0.0f;
+    const float state0 = BACK && valid && s.h0 != nullptr ? s.h0[row] : 0.0f;
+    if (cluster > 1) cluster_wait();
+
+    for (int64_t round = 0; round < rounds; ++round) {
+        const int buf = int(round & 1);
+        float a[J][V], p[J][V], q[BACK ? J : 1][V], rest[BACK ? J : 1][V];
+        float Ae[J], He[J], At[J], Ht[J];   // of the lanes before, of the 32 granules
+        float CA = 1.0f, CH = 0.0f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int64_t t = first_step(round, j);
+            float gate[V], x[V], dh[V], h[V];
+            unpack(raw[0][j], gate);
+            unpack(raw[1][j], x);
+            if (BACK) {
+                unpack(raw[IN - 2][j], dh);
+                unpack(raw[IN - 1][j], h);
+            }
+            float A = 1.0f, H = 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int e = BACK ? V - 1 - i : i;
+                const bool on = t + e >= 0 && t + e < steps;
+                float r;
+                open_gate<LOGITS>(gate[e], a[j][e], r);
+                if (BACK) {
+                    const float before = t + e == 0 ? state0 : e > 0 ? h[e > 0 ? e - 1 : 0] : edge[j];
+                    const float slope = LOGITS ? a[j][e] * r : 1.0f;
+                    q[j][e] = (s.coupled ? before - x[e] : before) * slope;
+                    rest[j][e] = s.coupled ? r : 1.0f;
+                    p[j][e] = dh[e];
+                } else {
+                    p[j][e] = s.coupled ? r * x[e] : x[e];
+                }
+                if (!on) a[j][e] = 1.0f, p[j][e] = 0.0f;
+                H = BACK ? a[j][e] * (H + p[j][e]) : fmaf(a[j][e], H, p[j][e]);
+                A *= a[j][e];
+            }
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const float pa = __shfl_up_sync(~0u, A, d), ph = __shfl_up_sync(~0u, H, d);
+                if (lane >= d) H = through(A, H, ph), A *= pa;
+            }
+            Ae[j] = __shfl_up_sync(~0u, A, 1), He[j] = __shfl_up_sync(~0u, H, 1);
+            if (lane == 0) Ae[j] = 1.0f, He[j] = 0.0f;
+            At[j] = __shfl_sync(~0u, A, 31), Ht[j] = __shfl_sync(~0u, H, 31);
+            CH = through(At[j], Ht[j], CH);
+            CA *= At[j];
+        }
+        if (round + 1 < rounds) load(round + 1);
+
+        float in_c = carry;
+        if (tg > 1) {
+            if (lane == 0) s_map[buf][warp] = make_float2(CA, CH);
+            __syncthreads();
+            if (cluster > 1) {
+                if (tid < cluster) {
+                    float2 all = make_float2(1.0f, 0.0f);
+                    for (int w = 0; w < kScanWarps; ++w) {
+                        const float2 m = s_map[buf][w];
+                        all = make_float2(all.x * m.x, through(m.x, m.y, all.y));
+                    }
+                    store_remote(&s_remote[buf][rank], tid, all);
+                }
+                cluster_meet();   // (the slots of a round are written again two meetings later)
+                for (int k = 0; k < cluster; ++k) {
+                    if (k == rank) in_c = carry;
+                    const float2 m = s_remote[buf][k];
+                    carry = through(m.x, m.y, carry);
+                }
+                for (int w = 0; w < group; ++w) {
+                    const float2 m = s_map[buf][w];
+                    in_c = through(m.x, m.y, in_c);
+                }
+            } else {
+                for (int w = 0; w < tg; ++w) {
+                    if (w == group) in_c = carry;
+                    const float2 m = s_map[buf][w0 + w];
+                    carry = through(m.x, m.y, carry);
+                }
+            }
+        } else {
+            carry = through(CA, CH, carry);
+        }
+
+        // the steps again, from that carry
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int64_t t = first_step(round, j);
+            float at = through(Ae[j], He[j], in_c), o0[V], o1[V];
+            in_c = through(At[j], Ht[j], in_c);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int e = BACK ? V - 1 - i : i;
+                if (BACK) {
+                    const float g = p[j][e] + at;
+                    o0[e] = g * q[j][e];
+                    o1[e] = g * rest[j][e];
+                    at = a[j][e] * g;
+                } else {
+                    at = fmaf(a[j][e], at, p[j][e]);
+                    o0[e] = at;
+                }
+            }
+            if (t >= steps) continue;
+            store_granule(out0, t, steps, o0);
+            if (BACK) store_granule(out1, t, steps, o1);
+        }
+    }
+    if (s.last != nullptr && valid && rank == 0 && group == 0 && lane == 0) s.last[row] = carry;
+}
+
+// ---- anything else, an element at a time ----
 
 // STAGED: fewer than kNarrow channels lie together, so that a warp's loads would
 // touch a sector for every lane.  There a CTA takes 32 / inner rows of kRun steps
 // each, read and written along the rows, and turns them through shared memory (rows
 // `inner` floats longer than their steps: a warp's 32 channels hit 32 banks).
-template <typename T, bool BACK, int V, bool STAGED, bool LOGITS>
+template <typename T, bool BACK, bool STAGED, bool LOGITS>
 __global__ void __launch_bounds__(kScanThreads, BACK ? 1 : 2)
-scan_kernel(const ScanArgs s, const int cluster) {
-    constexpr int S = kElems / V;          // steps of a thread in a round
+strided_kernel(const ScanArgs s, const int cluster) {
+    constexpr int V = 1, S = kElems;       // steps of a thread in a round
     constexpr int IN = BACK ? 4 : 2;       // tensors read
     constexpr int OUT = BACK ? 2 : 1;
     constexpr int W = 32 * V;
@@ -392,10 +811,60 @@ scan_kernel(const ScanArgs s, const int cluster) {
 
 // ---- host ----
 
-template <typename T, bool BACK, int V, bool STAGED, bool LOGITS>
-cudaError_t launch_scan_kernel(ScanArgs &s, cudaStream_t stream) {
-    constexpr int S = kElems / V;
-    const auto kernel = scan_kernel<T, BACK, V, STAGED, LOGITS>;
+// Warps that share a channel: as many as the steps go round, a warp taking `per` of
+// them in a round.  The logarithm.
+int groups_for(int64_t steps, int64_t per) {
+    int log = 0;
+    while (log < 3 && (per << log) < steps) ++log;
+    return log;
+}
+// CTAs that share channels: while the GPU holds two of `tiles` CTAs on an SM, and the
+// steps go round.
+int cluster_for(int64_t tiles, int64_t steps, int64_t per) {
+    int cluster = 1;
+    while (cluster < kMaxCluster && tiles * cluster <= sm_count() && per * cluster < steps) cluster *= 2;
+    return cluster;
+}
+
+template <typename T, bool BACK, int LC, bool LOGITS>
+cudaError_t launch_channels(ScanArgs &s, int64_t tiles, int cluster, cudaStream_t stream) {
+    const auto kernel = channel_kernel<T, BACK, LC, LOGITS>;
+    constexpr size_t smem = size_t(kStages<LC>) * kStageBytes * kScanThreads;
+    const cudaError_t e = allow_smem(kernel, smem);
+    if (e != cudaSuccess) return e;
+    if (tiles * cluster > INT32_MAX) return cudaErrorNotSupported;
+    return launch_ex(kernel, dim3(unsigned(tiles * cluster)), dim3(kScanThreads), smem, stream, unsigned(cluster), true, s, cluster);
+}
+template <typename T, bool BACK, bool LOGITS>
+cudaError_t launch_channels(ScanArgs &s, cudaStream_t stream) {
+    constexpr int S = kStageBytes / ((BACK ? 4 : 2) * 4 * int(sizeof(T)));
+    const auto tiles = [&](int lanes) {
+        s.groups_log = groups_for(s.steps, S * (32 / lanes));
+        const int64_t per = int64_t(lanes) * 4 * (kScanWarps >> s.groups_log);
+        return (s.channels + per - 1) / per;
+    };
+    // whole warps side by side where that fills the GPU; else 8 lanes (64 or 128 bytes side
+    // by side) and later steps in the others
+    const int64_t wide = tiles(32);
+    if (wide >= int64_t(3) * sm_count()) return launch_channels<T, BACK, 32, LOGITS>(s, wide, 1, stream);
+    const int64_t narrow = tiles(8);
+    return launch_channels<T, BACK, 8, LOGITS>(s, narrow, cluster_for(narrow, s.steps, int64_t(S * 4) << s.groups_log), stream);
+}
+
+template <typename T, bool BACK, bool LOGITS>
+cudaError_t launch_rows(ScanArgs &s, cudaStream_t stream) {
+    constexpr int64_t per = 32 * 16 / (BACK ? 2 : 1);
+    s.groups_log = 0;
+    while (s.groups_log < 3 && (per << s.groups_log) < s.steps && (s.channels << s.groups_log) < int64_t(4) * kScanWarps * sm_count()) ++s.groups_log;
+    const int64_t rows = kScanWarps >> s.groups_log, tiles = (s.channels + rows - 1) / rows;
+    const int cluster = s.groups_log < 3 ? 1 : cluster_for(tiles, s.steps, per << s.groups_log);
+    if (tiles * cluster > INT32_MAX) return cudaErrorNotSupported;
+    return launch_ex(row_kernel<T, BACK, LOGITS>, dim3(unsigned(tiles * cluster)), dim3(kScanThreads), 0, stream, unsigned(cluster), true, s, cluster);
+}
+
+template <typename T, bool BACK, bool STAGED, bool LOGITS>
+cudaError_t launch_strided(ScanArgs &s, cudaStream_t stream) {
+    const auto kernel = strided_kernel<T, BACK, STAGED, LOGITS>;
     int64_t tiles;
     size_t smem = 0;
     if (STAGED) {
@@ -406,27 +875,32 @@ cudaError_t launch_scan_kernel(ScanArgs &s, cudaStream_t stream) {
         const cudaError_t e = allow_smem(kernel, size_t(BACK ? 4 : 2) * 32 * (kRun + 1) * sizeof(float) + 48 * 1024);
         if (e != cudaSuccess) return e;
     } else {
-        // warps of one channel as far as the steps go round, the others take channels of their own
-        s.groups_log = 0;
-        while (s.groups_log < 3 && (int64_t(S) << s.groups_log) < s.steps) ++s.groups_log;
-        const int64_t per = int64_t(32 * V) * (kScanWarps >> s.groups_log);
+        s.groups_log = groups_for(s.steps, kElems);
+        const int64_t per = int64_t(32) * (kScanWarps >> s.groups_log);
         tiles = (s.channels + per - 1) / per;
     }
-    // time over a cluster's CTAs while the GPU has room for three of them an SM
-    int cluster = 1;
-    while (cluster < kMaxCluster && tiles * cluster * 2 <= int64_t(3) * sm_count() && (int64_t(S) << s.groups_log) * cluster < s.steps)
-        cluster *= 2;
+    const int cluster = s.groups_log < 3 ? 1 : cluster_for(tiles, s.steps, int64_t(kElems) << s.groups_log);
     if (tiles * cluster > INT32_MAX) return cudaErrorNotSupported;
     return launch_ex(kernel, dim3(unsigned(tiles * cluster)), dim3(kScanThreads), smem, stream, unsigned(cluster), true, s, cluster);
 }
 
-template <typename T, bool BACK>
-cudaError_t launch_scan(ScanArgs &s, bool logits, bool vector, cudaStream_t stream) {
-    if (vector)
-        return logits ? launch_scan_kernel<T, BACK, 4, false, true>(s, stream) : launch_scan_kernel<T, BACK, 4, false, false>(s, stream);
-    if (s.inner < kNarrow)
-        return logits ? launch_scan_kernel<T, BACK, 1, true, true>(s, stream) : launch_scan_kernel<T, BACK, 1, true, false>(s, stream);
-    return logits ? launch_scan_kernel<T, BACK, 1, false, true>(s, stream) : launch_scan_kernel<T, BACK, 1, false, false>(s, stream);
+enum Form { kChannels, kRows, kStaged, kStrided };
+
+template <typename T, bool BACK, bool LOGITS>
+cudaError_t launch_scan(ScanArgs &s, Form form, cudaStream_t stream) {
+    switch (form) {
+        case kChannels: return launch_channels<T, BACK, LOGITS>(s, stream);
+        case kRows: return launch_rows<T, BACK, LOGITS>(s, stream);
+        case kStaged: return launch_strided<T, BACK, true, LOGITS>(s, stream);
+        default: return launch_strided<T, BACK, false, LOGITS>(s, stream);
+    }
+}
+template <bool BACK>
+darb_status_t enqueue_scan(ScanArgs &s, darb_dtype_t dtype, bool logits, Form form, cudaStream_t stream) {
+    return enqueue([&] {
+        if (dtype == DARB_BF16) return logits ? launch_scan<__nv_bfloat16, BACK, true>(s, form, stream) : launch_scan<__nv_bfloat16, BACK, false>(s, form, stream);
+        return logits ? launch_scan<float, BACK, true>(s, form, stream) : launch_scan<float, BACK, false>(s, form, stream);
+    });
 }
 
 struct Shape {
@@ -456,8 +930,18 @@ Range operand_range(const Operand &o, const Shape &n, size_t es) {
     return {o.p, bytes};
 }
 
-bool vectors(const Operand &o, const Shape &n, size_t es) {
-    return aligned_to(o.p, 4 * es) && (n.outer == 1 || o.ld % 4 == 0) && (n.steps == 1 || o.step % 4 == 0);
+// Which kernel takes these operands.
+template <int N>
+Form form_of(const Operand (&all)[N], const Shape &n, size_t es) {
+    bool vectors = n.inner % 4 == 0, rows = n.inner == 1;
+    for (const Operand &o : all) {
+        vectors = vectors && aligned_to(o.p, 4 * es) && (n.outer == 1 || o.ld % 4 == 0) && (n.steps == 1 || o.step % 4 == 0);
+        // rows of consecutive steps, all of which start equally far past 16 bytes
+        const auto past = [&](int64_t row) { return (reinterpret_cast<uintptr_t>(o.p) + uintptr_t(row * o.ld) * es) % 16; };
+        const auto past0 = [&](int64_t row) { return (reinterpret_cast<uintptr_t>(all[0].p) + uintptr_t(row * all[0].ld) * es) % 16; };
+        rows = rows && (n.steps == 1 || o.step == 1) && past(0) == past0(0) && (n.outer == 1 || past(1) == past0(1));
+    }
+    return vectors ? kChannels : rows ? kRows : n.inner < kNarrow ? kStaged : kStrided;
 }
 
 bool same(const Operand &a, const Operand &b) { return a.p == b.p && a.ld == b.ld && a.step == b.step; }
@@ -507,11 +991,10 @@ darb_status_t darb_gated_scan(const void *gate, int64_t ld_gate, int64_t step_ga
     const size_t es = dtype_size(dtype);
     ScanArgs s = {};
     s.gate = {gate, ld_gate, step_gate}, s.x = {x, ld_x, step_x}, s.out[0] = {h, ld_h, step_h};
-    bool vector = inner % 4 == 0;
-    for (const Operand &o : {s.gate, s.x, s.out[0]}) {
+    const Operand all[] = {s.gate, s.x, s.out[0]};
+    for (const Operand &o : all) {
         st = check_operand(o, n, es);
         if (st != DARB_OK) return st;
-        vector = vector && vectors(o, n, es);
     }
     const Range outs[] = {operand_range(s.out[0], n, es), {h_last, states}};
     Range ins[] = {operand_range(s.gate, n, es), operand_range(s.x, n, es), {h0, states}};
@@ -520,10 +1003,7 @@ darb_status_t darb_gated_scan(const void *gate, int64_t ld_gate, int64_t step_ga
     if (!outputs_apart(outs, ins) || (h0 == h_last && buffers_overlap(outs[0], {h0, states}))) return DARB_ERR_INVALID_ARG;
     s.first = h0, s.last = h_last, s.steps = steps, s.channels = outer * inner;
     s.outer = int32_t(outer), s.inner = int32_t(inner), s.coupled = coupled != 0;
-    const bool logits = gates == DARB_GATES_LOGITS;
-    return enqueue([&] {
-        return dtype == DARB_BF16 ? launch_scan<__nv_bfloat16, false>(s, logits, vector, stream) : launch_scan<float, false>(s, logits, vector, stream);
-    });
+    return enqueue_scan<false>(s, dtype, gates == DARB_GATES_LOGITS, form_of(all, n, es), stream);
 }
 
 darb_status_t darb_gated_scan_grad(const void *dh, int64_t ld_dh, int64_t step_dh, const void *gate, int64_t ld_gate,
@@ -545,11 +1025,10 @@ darb_status_t darb_gated_scan_grad(const void *dh, int64_t ld_dh, int64_t step_d
     const size_t es = dtype_size(dtype);
     const Operand in[4] = {{gate, ld_gate, step_gate}, {x, ld_x, step_x}, {dh, ld_dh, step_dh}, {h, ld_h, step_h}};
     const Operand out[2] = {{d_gate, ld_dgate, step_dgate}, {d_x, ld_dx, step_dx}};
-    bool vector = inner % 4 == 0;
-    for (const Operand &o : {in[0], in[1], in[2], in[3], out[0], out[1]}) {
+    const Operand all[] = {in[0], in[1], in[2], in[3], out[0], out[1]};
+    for (const Operand &o : all) {
         st = check_operand(o, n, es);
         if (st != DARB_OK) return st;
-        vector = vector && vectors(o, n, es);
     }
     // an output may take the place of its input: d_gate the gate's, d_x that of x
     Range ins[] = {operand_range(in[0], n, es), operand_range(in[1], n, es), operand_range(in[2], n, es),
@@ -563,16 +1042,18 @@ darb_status_t darb_gated_scan_grad(const void *dh, int64_t ld_dh, int64_t step_d
         buffers_overlap(outs[2], x_in))
         return DARB_ERR_INVALID_ARG;
     ScanArgs s = {};
-    const int64_t last = steps - 1;
-    s.gate = reversed(in[0], last, es), s.x = reversed(in[1], last, es), s.dh = reversed(in[2], last, es);
-    s.before = reversed(in[3], last - 1, es);   // the state before each step
-    s.out[0] = reversed(out[0], last, es), s.out[1] = reversed(out[1], last, es);
+    const Form form = form_of(all, n, es);
+    if (form == kRows) {
+        s.gate = in[0], s.x = in[1], s.dh = in[2], s.before = in[3], s.out[0] = out[0], s.out[1] = out[1];
+    } else {   // the steps are walked with negative strides
+        const int64_t last = steps - 1;
+        s.gate = reversed(in[0], last, es), s.x = reversed(in[1], last, es), s.dh = reversed(in[2], last, es);
+        s.before = reversed(in[3], last - 1, es);   // the state before each step
+        s.out[0] = reversed(out[0], last, es), s.out[1] = reversed(out[1], last, es);
+    }
     s.first = d_last, s.h0 = h0, s.last = d_h0, s.steps = steps, s.channels = outer * inner;
     s.outer = int32_t(outer), s.inner = int32_t(inner), s.coupled = coupled != 0;
-    const bool logits = gates == DARB_GATES_LOGITS;
-    return enqueue([&] {
-        return dtype == DARB_BF16 ? launch_scan<__nv_bfloat16, true>(s, logits, vector, stream) : launch_scan<float, true>(s, logits, vector, stream);
-    });
+    return enqueue_scan<true>(s, dtype, gates == DARB_GATES_LOGITS, form, stream);
 }
 
 }  // extern "C"
