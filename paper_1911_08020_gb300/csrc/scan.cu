@@ -31,6 +31,7 @@
 #include "trace.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace darb {
 
@@ -69,18 +70,18 @@ struct Word;
 template <>
 struct Word<float, 4> {
     float4 w;
-    __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w; }
-    __device__ __forceinline__ void set(const float (&v)[4]) { w = make_float4(v[0], v[1], v[2], v[3]); }
+    __device__ __forceinline__ void get(Pair (&v)[2]) const { v[0] = pair(w.x, w.y), v[1] = pair(w.z, w.w); }
+    __device__ __forceinline__ void set(const Pair (&v)[2]) { w = make_float4(low(v[0]), high(v[0]), low(v[1]), high(v[1])); }
 };
 template <>
 struct Word<__nv_bfloat16, 4> {
     uint2 w;
-    __device__ __forceinline__ void get(float (&v)[4]) const {
+    __device__ __forceinline__ void get(Pair (&v)[2]) const {
         const float2 a = widen2(w.x), b = widen2(w.y);
-        v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+        v[0] = pair(a.x, a.y), v[1] = pair(b.x, b.y);
     }
-    __device__ __forceinline__ void set(const float (&v)[4]) {
-        const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+    __device__ __forceinline__ void set(const Pair (&v)[2]) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(low(v[0]), high(v[0])), b = __floats2bfloat162_rn(low(v[1]), high(v[1]));
         w = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
     }
 };
@@ -91,13 +92,20 @@ struct Word<T, 1> {
     __device__ __forceinline__ void set(const float (&v)[1]) { w = narrow<T>(v[0]); }
 };
 
+// 1 / x, one instruction (off by one unit; of infinity 0).
+__device__ __forceinline__ float reciprocal(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // a and 1 - a from a gate, each to the last places of its own (a sigmoid near 1
 // leaves its distance from 1 exact); +-inf give exactly 1 and 0.
 template <bool LOGITS>
 __device__ __forceinline__ void open_gate(float gate, float &a, float &rest) {
     if (LOGITS) {
         const float e = exp2_fast(-kLog2e * gate);
-        a = __fdividef(1.0f, 1.0f + e);
+        a = reciprocal(1.0f + e);
         rest = gate >= 0.0f ? e * a : 1.0f - a;
     } else {
         a = gate;
@@ -105,9 +113,29 @@ __device__ __forceinline__ void open_gate(float gate, float &a, float &rest) {
     }
 }
 
-// The state after a map, from the one before.  Nothing comes of a state of 0, even
-// where the product of gates above 1 has overflown.
-__device__ __forceinline__ float through(float A, float H, float c) { return c == 0.0f ? H : fmaf(A, c, H); }
+// The same of two gates.
+template <bool LOGITS>
+__device__ __forceinline__ void open_gates(Pair gate, Pair &a, Pair &rest) {
+    if (LOGITS) {
+        const Pair z = mul2(gate, both(-kLog2e)), e = pair(exp2_fast(low(z)), exp2_fast(high(z))), d = add2(e, both(1.0f));
+        a = pair(reciprocal(low(d)), reciprocal(high(d)));
+        const Pair near = mul2(e, a), far = fma2(a, both(-1.0f), both(1.0f));
+        rest = pair(low(gate) >= 0.0f ? low(near) : low(far), high(gate) >= 0.0f ? high(near) : high(far));
+    } else {
+        a = gate;
+        rest = fma2(a, both(-1.0f), both(1.0f));
+    }
+}
+
+// The state after a map, from the one before.  Where gates may be above 1 nothing
+// comes of a state of 0, even where the product of the gates has overflown.
+template <bool LOGITS>
+__device__ __forceinline__ float through(float A, float H, float c) { return !LOGITS && c == 0.0f ? H : fmaf(A, c, H); }
+template <bool LOGITS>
+__device__ __forceinline__ Pair through(Pair A, Pair H, Pair c) {
+    const Pair r = fma2(A, c, H);
+    return LOGITS ? r : pair(low(c) == 0.0f ? low(H) : low(r), high(c) == 0.0f ? high(H) : high(r));
+}
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -131,20 +159,42 @@ __device__ __forceinline__ void store_remote(float4 *here, uint32_t rank, float4
                  : "memory");
 }
 
-// Four channels' states after a map, and a map after the one before it.
-__device__ __forceinline__ void state_through(float4 A, float4 H, float4 &c) {
-    c = make_float4(through(A.x, H.x, c.x), through(A.y, H.y, c.y), through(A.z, H.z, c.z), through(A.w, H.w, c.w));
+// Four channels as two pairs.
+struct Quad {
+    Pair p[2];
+};
+__device__ __forceinline__ Quad quad(float4 v) { return {pair(v.x, v.y), pair(v.z, v.w)}; }
+__device__ __forceinline__ float4 floats(const Quad &q) { return make_float4(low(q.p[0]), high(q.p[0]), low(q.p[1]), high(q.p[1])); }
+template <bool LOGITS>
+__device__ __forceinline__ void state_through(const Quad &A, const Quad &H, Quad &c) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) c.p[h] = through<LOGITS>(A.p[h], H.p[h], c.p[h]);
 }
-__device__ __forceinline__ void map_through(float4 A, float4 H, float4 &CA, float4 &CH) {
-    state_through(A, H, CH);
-    CA = make_float4(CA.x * A.x, CA.y * A.y, CA.z * A.z, CA.w * A.w);
+// A map, and another after it.
+template <bool LOGITS>
+__device__ __forceinline__ void map_through(const Quad &A, const Quad &H, Quad &CA, Quad &CH) {
+    state_through<LOGITS>(A, H, CH);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) CA.p[h] = mul2(CA.p[h], A.p[h]);
+}
+// A carry goes from warp to warp, and from the last one to the first one's next round:
+// a named barrier for each warp that takes one, at which the giver does not wait.  (A
+// warp gives again when the carry has been round all the others, so that one place and
+// one barrier do.)
+__device__ __forceinline__ void take_carry(int warp) { asm volatile("bar.sync %0, 64;" ::"r"(warp + 1) : "memory"); }
+__device__ __forceinline__ void give_carry(int warp) { asm volatile("bar.arrive %0, 64;" ::"r"(warp + 1) : "memory"); }
+
+__device__ __forceinline__ Pair shuffle_up(Pair v, int d) {
+    Pair r;
+    r.bits = __shfl_up_sync(~0u, v.bits, d);
+    return r;
 }
 
-// An asynchronous copy of 8 or 16 bytes to shared memory (zeros where it is not `on`).
+// An asynchronous copy of 8 or 16 bytes to shared memory.
 template <int BYTES>
-__device__ __forceinline__ void cp_async_word(uint32_t dst, const void *src, bool on) {
-    if (BYTES == 16) cp_async16(dst, src, on);
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(on ? 8 : 0) : "memory");
+__device__ __forceinline__ void cp_async_word(uint32_t dst, const void *src) {
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -153,10 +203,9 @@ __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_gr
 // ---- channels four at a time ----
 
 // A round's inputs wait in shared memory, each thread's in places of its own: loads
-// are on their way for one or two rounds without holding registers, and no barrier
+// are on their way for two rounds without holding registers, and no barrier
 // goes with them.
-template <int LC>
-constexpr int kStages = LC == 32 ? 2 : 3;
+constexpr int kStages = 3;
 constexpr int kStageBytes = 128;   // of a thread and round
 
 // LC lanes of a warp have neighbouring channels, the other lanes later steps.
@@ -164,214 +213,227 @@ template <typename T, bool BACK, int LC, bool LOGITS>
 __global__ void __launch_bounds__(kScanThreads, 2) channel_kernel(const ScanArgs s, const int cluster) {
     constexpr int V = 4, IN = BACK ? 4 : 2, OUT = BACK ? 2 : 1;
     constexpr int S = kStageBytes / (IN * V * int(sizeof(T)));   // steps of a thread in a round
-    constexpr int TL = 32 / LC, NS = kStages<LC>;
+    constexpr int TL = 32 / LC, NS = kStages;
+    constexpr bool kMayCluster = LC < 32;
     using Raw = Word<T, V>;
-    __shared__ float4 s_A[2][kScanWarps][LC], s_H[2][kScanWarps][LC], s_carry[2][kScanWarps][LC];
-    __shared__ float4 s_rA[LC < 32 ? 2 : 1][LC < 32 ? kMaxCluster : 1][LC], s_rH[LC < 32 ? 2 : 1][LC < 32 ? kMaxCluster : 1][LC];
+    constexpr int CW = kMayCluster ? kScanWarps : 1, CC = kMayCluster ? kMaxCluster : 1;
+    __shared__ Quad s_carry[kScanWarps][LC], s_A[2][CW][LC], s_H[2][CW][LC];
+    __shared__ float4 s_rA[2][CC][LC], s_rH[2][CC][LC];
     extern __shared__ __align__(16) unsigned char s_raw[];
     Raw *const slots = reinterpret_cast<Raw *>(s_raw) + threadIdx.x;   // [stage][tensor][step][thread]
 
     pdl_launch_dependents();
-    if (LC < 32 && cluster > 1) cluster_arrive();   // (the others' shared memory is there once they run)
+    if (kMayCluster && cluster > 1) cluster_arrive();   // (the others' shared memory is there once they run)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int cl = lane % LC, tl = lane / LC;
     const int tg = 1 << s.groups_log, group = warp & (tg - 1), ct = warp >> s.groups_log;
-    const int rank = LC < 32 && cluster > 1 ? int(blockIdx.x) % cluster : 0;
+    const int rank = kMayCluster && cluster > 1 ? int(blockIdx.x) % cluster : 0;
     const int64_t tile = blockIdx.x / unsigned(cluster);
     const int64_t steps = s.steps, stride = int64_t(tg) * (TL * S) * cluster;
     const int64_t c = ((tile * (kScanWarps >> s.groups_log) + ct) * LC + cl) * V;
     const bool valid = c < s.channels;
     const int64_t co = valid ? c / s.inner : 0, ci = valid ? c - co * s.inner : 0;
-    int64_t t0 = (int64_t(rank) * tg + group) * (TL * S) + tl * S;   // the thread's first step
+    const int64_t t0 = (int64_t(rank) * tg + group) * (TL * S) + tl * S;   // the thread's first step
 
     const Operand *const ins[4] = {&s.gate, &s.x, &s.dh, &s.before};
-    const T *in[IN];
-    T *out[OUT];
+    const T *in[IN];     // at the first step of the next round to load
+    T *out[OUT];         // at the first step of the round
 #pragma unroll
-    for (int k = 0; k < IN; ++k) in[k] = static_cast<const T *>(ins[k]->p) + co * ins[k]->ld + ci;
+    for (int k = 0; k < IN; ++k) in[k] = static_cast<const T *>(ins[k]->p) + co * ins[k]->ld + ci + t0 * ins[k]->step;
 #pragma unroll
-    for (int k = 0; k < OUT; ++k) out[k] = static_cast<T *>(const_cast<void *>(s.out[k].p)) + co * s.out[k].ld + ci;
+    for (int k = 0; k < OUT; ++k) out[k] = static_cast<T *>(const_cast<void *>(s.out[k].p)) + co * s.out[k].ld + ci + t0 * s.out[k].step;
+
+    int64_t in_round[IN], out_round[OUT];
+#pragma unroll
+    for (int k = 0; k < IN; ++k) in_round[k] = stride * ins[k]->step;
+#pragma unroll
+    for (int k = 0; k < OUT; ++k) out_round[k] = stride * s.out[k].step;
 
     const int64_t rounds = (steps + stride - 1) / stride;
-    auto load = [&](int64_t round) {
-        const int64_t t = t0 + round * stride;
-        Raw *const to = slots + (round % NS) * (IN * S * kScanThreads);
+    int64_t left_to_load = valid ? steps - t0 : 0;   // steps from the first of the next round to load
+    int in_slot = 0;
+    auto load = [&]() {
+        const uint32_t to = smem_addr(slots + in_slot * (IN * S * kScanThreads));
+        constexpr uint32_t kWord = kScanThreads * sizeof(Raw);
+        if (left_to_load > S) {
 #pragma unroll
-        for (int k = 0; k < IN; ++k) {
-            const T *p = in[k] + t * ins[k]->step;
+            for (int k = 0; k < IN; ++k) {
+                const T *p = in[k];
 #pragma unroll
-            for (int j = 0; j < S; ++j) {
-                // (no state before step 0 in memory: state0)
-                const bool on = round < rounds && valid && t + j < steps - (BACK && k == 3 ? 1 : 0);
-                cp_async_word<sizeof(Raw)>(smem_addr(to + (k * S + j) * kScanThreads), on ? p : static_cast<const T *>(s.gate.p), on);
-                p += ins[k]->step;
+                for (int j = 0; j < S; ++j, p += ins[k]->step) cp_async_word<sizeof(Raw)>(to + (k * S + j) * kWord, p);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < IN; ++k) {
+                const T *p = in[k];
+#pragma unroll
+                for (int j = 0; j < S; ++j, p += ins[k]->step) {
+                    // (no state before step 0 in memory: state0)
+                    if (j < left_to_load - (BACK && k == 3 ? 1 : 0)) cp_async_word<sizeof(Raw)>(to + (k * S + j) * kWord, p);
+                }
             }
         }
         cp_async_commit();
+#pragma unroll
+        for (int k = 0; k < IN; ++k) in[k] += in_round[k];
+        left_to_load -= stride;
+        in_slot = in_slot + 1 == NS ? 0 : in_slot + 1;
     };
 
     pdl_wait_previous();
 #pragma unroll
-    for (int r = 0; r < NS - 1; ++r) load(r);
-    float carry[V], state0[V];   // state0: backward, the state before step 0, in 32 bits
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        carry[v] = valid && s.first != nullptr ? s.first[c + v] : 0.0f;
-        state0[v] = BACK && valid && s.h0 != nullptr ? s.h0[c + v] : 0.0f;
-    }
-    if (LC < 32 && cluster > 1) cluster_wait();
+    for (int r = 0; r < NS - 1; ++r) load();
+    Quad carry = {{both(0.0f), both(0.0f)}}, state0 = carry;   // state0: backward, the state before step 0, in 32 bits
+    if (valid && s.first != nullptr) carry = {pair(s.first[c], s.first[c + 1]), pair(s.first[c + 2], s.first[c + 3])};
+    if (BACK && valid && s.h0 != nullptr) state0 = {pair(s.h0[c], s.h0[c + 1]), pair(s.h0[c + 2], s.h0[c + 3])};
+    if (kMayCluster && cluster > 1) cluster_wait();
 
-    for (int64_t round = 0; round < rounds; ++round) {
+    int slot = 0;
+    int64_t left = valid ? steps - t0 : 0;   // steps from the thread's first of the round
+    for (int64_t round = 0; round < rounds; ++round, left -= stride) {
         const int buf = int(round & 1);
-        load(round + NS - 1);
+        load();
         cp_async_wait<NS - 1>();
-        const Raw *const from = slots + (round % NS) * (IN * S * kScanThreads);
-        const int64_t t1 = t0 + round * stride;
-        const int live = t1 >= steps ? 0 : steps - t1 < S ? int(steps - t1) : S;   // of the thread's steps
+        const Raw *const from = slots + slot * (IN * S * kScanThreads);
+        slot = slot + 1 == NS ? 0 : slot + 1;
 
         // the maps of the steps.  Forward: p = u.  Backward: p = dh, q = what g is
         // multiplied by in d_gate, rest in d_x
-        float a[S][V], p[S][V], q[BACK ? S : 1][V], rest[BACK ? S : 1][V];
-        float A[V], H[V];
+        Quad a[S], p[S], q[BACK ? S : 1], rest[BACK ? S : 1];
+        Quad A = {{both(1.0f), both(1.0f)}}, H = {{both(0.0f), both(0.0f)}};
+        auto maps = [&](auto full) {
+            constexpr bool all = decltype(full)::value;
 #pragma unroll
-        for (int v = 0; v < V; ++v) A[v] = 1.0f, H[v] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < S; ++j) {
-            float gate[V], x[V], dh[V], hp[V];
-            const Raw g = from[j * kScanThreads], xr = from[(S + j) * kScanThreads];
-            g.get(gate);
-            xr.get(x);
-            if (BACK) {
-                const Raw d = from[(2 * S + j) * kScanThreads], h = from[((IN - 1) * S + j) * kScanThreads];
-                d.get(dh);
-                h.get(hp);
-            }
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float r;
-                open_gate<LOGITS>(gate[v], a[j][v], r);
+            for (int j = 0; j < S; ++j) {
+                Pair gate[2], x[2], dh[2], hp[2];
+                const Raw g = from[j * kScanThreads], xr = from[(S + j) * kScanThreads];
+                g.get(gate);
+                xr.get(x);
                 if (BACK) {
-                    const float h = t1 + j == steps - 1 ? state0[v] : hp[v];
-                    const float slope = LOGITS ? a[j][v] * r : 1.0f;
-                    q[j][v] = (s.coupled ? h - x[v] : h) * slope;
-                    rest[j][v] = s.coupled ? r : 1.0f;
-                    p[j][v] = dh[v];
-                } else {
-                    p[j][v] = s.coupled ? r * x[v] : x[v];
+                    const Raw d = from[(2 * S + j) * kScanThreads], h = from[((IN - 1) * S + j) * kScanThreads];
+                    d.get(dh);
+                    h.get(hp);
+                    if (!all && j == left - 1) hp[0] = state0.p[0], hp[1] = state0.p[1];
                 }
-                if (j >= live) a[j][v] = 1.0f, p[j][v] = 0.0f;
-                H[v] = BACK ? a[j][v] * (H[v] + p[j][v]) : fmaf(a[j][v], H[v], p[j][v]);
-                A[v] *= a[j][v];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    Pair r;
+                    open_gates<LOGITS>(gate[h], a[j].p[h], r);
+                    if (BACK) {
+                        const Pair d = s.coupled ? fma2(x[h], both(-1.0f), hp[h]) : hp[h];
+                        q[j].p[h] = LOGITS ? mul2(d, mul2(a[j].p[h], r)) : d;
+                        rest[j].p[h] = s.coupled ? r : both(1.0f);
+                        p[j].p[h] = dh[h];
+                    } else {
+                        p[j].p[h] = s.coupled ? mul2(r, x[h]) : x[h];
+                    }
+                    if (!all && j >= left) a[j].p[h] = both(1.0f), p[j].p[h] = both(0.0f);
+                    H.p[h] = BACK ? mul2(a[j].p[h], add2(H.p[h], p[j].p[h])) : fma2(a[j].p[h], H.p[h], p[j].p[h]);
+                    A.p[h] = mul2(A.p[h], a[j].p[h]);
+                }
             }
-        }
+        };
+        if (left > S) maps(std::true_type());
+        else maps(std::false_type());
 
         // the maps of the lanes before, then all of the warp's
-        float Ae[V], He[V];
+        Quad Ae, He;
         if (TL > 1) {
 #pragma unroll
-            for (int d = 1; d < TL; d <<= 1) {
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float pa = __shfl_up_sync(~0u, A[v], d * LC), ph = __shfl_up_sync(~0u, H[v], d * LC);
-                    if (tl >= d) H[v] = through(A[v], H[v], ph), A[v] *= pa;
+                for (int d = 1; d < TL; d <<= 1) {
+                    const Pair pa = shuffle_up(A.p[h], d * LC), ph = shuffle_up(H.p[h], d * LC);
+                    if (tl >= d) H.p[h] = through<LOGITS>(A.p[h], H.p[h], ph), A.p[h] = mul2(A.p[h], pa);
                 }
-            }
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                Ae[v] = __shfl_up_sync(~0u, A[v], LC), He[v] = __shfl_up_sync(~0u, H[v], LC);
-                if (tl == 0) Ae[v] = 1.0f, He[v] = 0.0f;
+                Ae.p[h] = shuffle_up(A.p[h], LC), He.p[h] = shuffle_up(H.p[h], LC);
+                if (tl == 0) Ae.p[h] = both(1.0f), He.p[h] = both(0.0f);
             }
         }
         // the carry into the warp's steps
-        float in_c[V];
-        if (tg > 1) {
-            if (tl == TL - 1) {
-                s_A[buf][warp][cl] = make_float4(A[0], A[1], A[2], A[3]);
-                s_H[buf][warp][cl] = make_float4(H[0], H[1], H[2], H[3]);
-            }
+        Quad in_c = carry;
+        const bool split = kMayCluster && cluster > 1;
+        if (split) {
+            if (tl == TL - 1) s_A[buf][warp][cl] = A, s_H[buf][warp][cl] = H;
             __syncthreads();
-            if (LC < 32 && cluster > 1) {
-                // the map of all steps of this CTA, to every CTA
-                if (warp < cluster && tl == 0) {
-                    float4 CA = make_float4(1.0f, 1.0f, 1.0f, 1.0f), CH = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            // the map of all steps of this CTA, to every CTA
+            if (warp < cluster && tl == 0) {
+                Quad CA = s_A[buf][0][cl], CH = s_H[buf][0][cl];
 #pragma unroll
-                    for (int w = 0; w < kScanWarps; ++w) map_through(s_A[buf][w][cl], s_H[buf][w][cl], CA, CH);
-                    store_remote(&s_rA[buf][rank][cl], warp, CA);
-                    store_remote(&s_rH[buf][rank][cl], warp, CH);
-                }
-                cluster_meet();   // (the slots of a round are written again two meetings later)
-                float4 at = make_float4(carry[0], carry[1], carry[2], carry[3]), mine = at;
-                for (int k = 0; k < cluster; ++k) {
-                    if (k == rank) mine = at;
-                    state_through(s_rA[buf][k][cl], s_rH[buf][k][cl], at);
-                }
-                carry[0] = at.x, carry[1] = at.y, carry[2] = at.z, carry[3] = at.w;
-                in_c[0] = mine.x, in_c[1] = mine.y, in_c[2] = mine.z, in_c[3] = mine.w;
-            } else if (round == 0) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) in_c[v] = carry[v];
-            } else {
-                const float4 at = s_carry[buf ^ 1][ct][cl];
-                in_c[0] = at.x, in_c[1] = at.y, in_c[2] = at.z, in_c[3] = at.w;
+                for (int w = 1; w < CW; ++w) map_through<LOGITS>(s_A[buf][w][cl], s_H[buf][w][cl], CA, CH);
+                store_remote(&s_rA[buf][rank][cl], warp, floats(CA));
+                store_remote(&s_rH[buf][rank][cl], warp, floats(CH));
             }
-            const int w0 = warp - group;   // the first warp of these channels
-            for (int w = 0; w < group; ++w) {
-                float4 at = make_float4(in_c[0], in_c[1], in_c[2], in_c[3]);
-                state_through(s_A[buf][w0 + w][cl], s_H[buf][w0 + w][cl], at);
-                in_c[0] = at.x, in_c[1] = at.y, in_c[2] = at.z, in_c[3] = at.w;
+            cluster_meet();   // (the slots of a round are written again two meetings later)
+            for (int k = 0; k < cluster; ++k) {
+                if (k == rank) in_c = carry;
+                state_through<LOGITS>(quad(s_rA[buf][k][cl]), quad(s_rH[buf][k][cl]), carry);
             }
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) in_c[v] = carry[v];
+            for (int w = 0; w < group; ++w) state_through<LOGITS>(s_A[buf][w][cl], s_H[buf][w][cl], in_c);
+        } else if (tg > 1) {
+            if (round > 0 || group > 0) {
+                take_carry(warp);
+                in_c = s_carry[warp][cl];
+            }
+            if (round + 1 < rounds || group < tg - 1) {
+                const int next = warp - group + ((group + 1) & (tg - 1));
+                if (tl == TL - 1) {
+                    Quad out_c = in_c;
+                    state_through<LOGITS>(A, H, out_c);
+                    s_carry[next][cl] = out_c;
+                }
+                give_carry(next);
+            }
         }
-        if (TL > 1) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) in_c[v] = through(Ae[v], He[v], in_c[v]);
-        }
+        if (TL > 1) state_through<LOGITS>(Ae, He, in_c);
 
         // the steps again, from that carry
-        T *to[OUT];
+        auto steps_again = [&](auto full) {
+            constexpr bool all = decltype(full)::value;
+            T *to[OUT];
 #pragma unroll
-        for (int k = 0; k < OUT; ++k) to[k] = out[k] + t1 * s.out[k].step;
+            for (int k = 0; k < OUT; ++k) to[k] = out[k];
 #pragma unroll
-        for (int j = 0; j < S; ++j) {
-            float o0[V], o1[V];
+            for (int j = 0; j < S; ++j) {
+                Pair o0[2], o1[2];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (BACK) {
-                    const float g = p[j][v] + in_c[v];
-                    o0[v] = g * q[j][v];
-                    o1[v] = g * rest[j][v];
-                    in_c[v] = a[j][v] * g;
-                } else {
-                    in_c[v] = fmaf(a[j][v], in_c[v], p[j][v]);
-                    o0[v] = in_c[v];
+                for (int h = 0; h < 2; ++h) {
+                    if (BACK) {
+                        const Pair g = add2(p[j].p[h], in_c.p[h]);
+                        o0[h] = mul2(g, q[j].p[h]);
+                        o1[h] = mul2(g, rest[j].p[h]);
+                        in_c.p[h] = mul2(a[j].p[h], g);
+                    } else {
+                        o0[h] = in_c.p[h] = fma2(a[j].p[h], in_c.p[h], p[j].p[h]);
+                    }
                 }
-            }
-            if (valid && j < live) {
-                Raw w;
-                w.set(o0);
-                *reinterpret_cast<Raw *>(to[0]) = w;
-                if (BACK) {
-                    w.set(o1);
-                    *reinterpret_cast<Raw *>(to[OUT - 1]) = w;
+                if (all || j < left) {
+                    Raw w;
+                    w.set(o0);
+                    *reinterpret_cast<Raw *>(to[0]) = w;
+                    if (BACK) {
+                        w.set(o1);
+                        *reinterpret_cast<Raw *>(to[OUT - 1]) = w;
+                    }
                 }
-            }
 #pragma unroll
-            for (int k = 0; k < OUT; ++k) to[k] += s.out[k].step;
-        }
+                for (int k = 0; k < OUT; ++k) to[k] += s.out[k].step;
+            }
+        };
+        if (left >= S) steps_again(std::true_type());
+        else steps_again(std::false_type());
+#pragma unroll
+        for (int k = 0; k < OUT; ++k) out[k] += out_round[k];
         // the carry out of the round, with the lanes that have its last steps
-        if (tg > 1) {
-            if (cluster == 1 && group == tg - 1 && tl == TL - 1) s_carry[buf][ct][cl] = make_float4(in_c[0], in_c[1], in_c[2], in_c[3]);
-        } else {
+        if (tg == 1) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = TL > 1 ? __shfl_sync(~0u, in_c[v], (TL - 1) * LC + cl) : in_c[v];
+            for (int h = 0; h < 2; ++h) carry.p[h].bits = TL > 1 ? __shfl_sync(~0u, in_c.p[h].bits, (TL - 1) * LC + cl) : in_c.p[h].bits;
         }
         if (round + 1 == rounds && s.last != nullptr && valid) {
-            const bool split = LC < 32 && cluster > 1;   // (then all threads have the carry)
+            // (split: all threads have the carry)
             if (split ? rank == 0 && warp == 0 && tl == 0 : group == tg - 1 && tl == TL - 1) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) s.last[c + v] = split ? carry[v] : in_c[v];
+                const float4 v = floats(split ? carry : in_c);
+                s.last[c] = v.x, s.last[c + 1] = v.y, s.last[c + 2] = v.z, s.last[c + 3] = v.w;
             }
         }
     }
@@ -388,11 +450,12 @@ template <typename T, bool BACK, bool LOGITS>
 __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, const int cluster) {
     constexpr int V = kPerGranule<T>, IN = BACK ? 4 : 2, J = 16 / V / (BACK ? 2 : 1);
     __shared__ float2 s_map[2][kScanWarps], s_remote[2][kMaxCluster];
+    __shared__ float s_carry[kScanWarps];
 
     pdl_launch_dependents();
     if (cluster > 1) cluster_arrive();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int tg = 1 << s.groups_log, group = warp & (tg - 1), w0 = warp - group;
+    const int tg = 1 << s.groups_log, group = warp & (tg - 1);
     const int rank = cluster > 1 ? int(blockIdx.x) % cluster : 0;
     const int64_t row = (blockIdx.x / unsigned(cluster)) * int64_t(kScanWarps >> s.groups_log) + (warp >> s.groups_log);
     const bool valid = row < s.channels;
@@ -419,10 +482,14 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int64_t t = first_step(round, j);
-            if (t >= steps) continue;
+            if (t >= 0 && t + V <= steps) {
 #pragma unroll
-            for (int k = 0; k < IN; ++k) raw[k][j] = load_granule<T, false>(in[k], t, steps, 0.0f);
-            if (BACK) edge[j] = t > 0 ? widen(in[IN - 1][t - 1]) : 0.0f;
+                for (int k = 0; k < IN; ++k) raw[k][j] = *reinterpret_cast<const uint4 *>(in[k] + t);
+            } else if (t < steps) {
+#pragma unroll
+                for (int k = 0; k < IN; ++k) raw[k][j] = load_granule<T, false>(in[k], t, steps, 0.0f);
+            }
+            if (BACK && t < steps) edge[j] = t > 0 ? widen(in[IN - 1][t - 1]) : 0.0f;
         }
     };
     pdl_wait_previous();
@@ -439,86 +506,99 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int64_t t = first_step(round, j);
-            float gate[V], x[V], dh[V], h[V];
+            Pair gate[V / 2], x[V / 2];
+            float dh[V], h[V];
             unpack(raw[0][j], gate);
             unpack(raw[1][j], x);
             if (BACK) {
                 unpack(raw[IN - 2][j], dh);
                 unpack(raw[IN - 1][j], h);
+#pragma unroll
+                for (int e = V - 1; e > 0; --e) h[e] = t + e == 0 ? state0 : h[e - 1];   // the states before
+                h[0] = t == 0 ? state0 : edge[j];
+            }
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+                Pair ga, r;
+                open_gates<LOGITS>(gate[e / 2], ga, r);
+                a[j][e] = low(ga), a[j][e + 1] = high(ga);
+                if (BACK) {
+                    const Pair before = pair(h[e], h[e + 1]), d = s.coupled ? fma2(x[e / 2], both(-1.0f), before) : before;
+                    const Pair qe = LOGITS ? mul2(d, mul2(ga, r)) : d;
+                    q[j][e] = low(qe), q[j][e + 1] = high(qe);
+                    rest[j][e] = s.coupled ? low(r) : 1.0f, rest[j][e + 1] = s.coupled ? high(r) : 1.0f;
+                    p[j][e] = dh[e], p[j][e + 1] = dh[e + 1];
+                } else {
+                    const Pair u = s.coupled ? mul2(r, x[e / 2]) : x[e / 2];
+                    p[j][e] = low(u), p[j][e + 1] = high(u);
+                }
+            }
+            if (t < 0 || t + V > steps) {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (t + e < 0 || t + e >= steps) a[j][e] = 1.0f, p[j][e] = 0.0f;
             }
             float A = 1.0f, H = 0.0f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int e = BACK ? V - 1 - i : i;
-                const bool on = t + e >= 0 && t + e < steps;
-                float r;
-                open_gate<LOGITS>(gate[e], a[j][e], r);
-                if (BACK) {
-                    const float before = t + e == 0 ? state0 : e > 0 ? h[e > 0 ? e - 1 : 0] : edge[j];
-                    const float slope = LOGITS ? a[j][e] * r : 1.0f;
-                    q[j][e] = (s.coupled ? before - x[e] : before) * slope;
-                    rest[j][e] = s.coupled ? r : 1.0f;
-                    p[j][e] = dh[e];
-                } else {
-                    p[j][e] = s.coupled ? r * x[e] : x[e];
-                }
-                if (!on) a[j][e] = 1.0f, p[j][e] = 0.0f;
                 H = BACK ? a[j][e] * (H + p[j][e]) : fmaf(a[j][e], H, p[j][e]);
                 A *= a[j][e];
             }
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const float pa = __shfl_up_sync(~0u, A, d), ph = __shfl_up_sync(~0u, H, d);
-                if (lane >= d) H = through(A, H, ph), A *= pa;
+                if (lane >= d) H = through<LOGITS>(A, H, ph), A *= pa;
             }
             Ae[j] = __shfl_up_sync(~0u, A, 1), He[j] = __shfl_up_sync(~0u, H, 1);
             if (lane == 0) Ae[j] = 1.0f, He[j] = 0.0f;
             At[j] = __shfl_sync(~0u, A, 31), Ht[j] = __shfl_sync(~0u, H, 31);
-            CH = through(At[j], Ht[j], CH);
+            CH = through<LOGITS>(At[j], Ht[j], CH);
             CA *= At[j];
         }
         if (round + 1 < rounds) load(round + 1);
 
         float in_c = carry;
-        if (tg > 1) {
+        if (cluster > 1) {
             if (lane == 0) s_map[buf][warp] = make_float2(CA, CH);
             __syncthreads();
-            if (cluster > 1) {
-                if (tid < cluster) {
-                    float2 all = make_float2(1.0f, 0.0f);
-                    for (int w = 0; w < kScanWarps; ++w) {
-                        const float2 m = s_map[buf][w];
-                        all = make_float2(all.x * m.x, through(m.x, m.y, all.y));
-                    }
-                    store_remote(&s_remote[buf][rank], tid, all);
-                }
-                cluster_meet();   // (the slots of a round are written again two meetings later)
-                for (int k = 0; k < cluster; ++k) {
-                    if (k == rank) in_c = carry;
-                    const float2 m = s_remote[buf][k];
-                    carry = through(m.x, m.y, carry);
-                }
-                for (int w = 0; w < group; ++w) {
+            if (tid < cluster) {
+                float2 all = make_float2(1.0f, 0.0f);
+                for (int w = 0; w < kScanWarps; ++w) {
                     const float2 m = s_map[buf][w];
-                    in_c = through(m.x, m.y, in_c);
+                    all = make_float2(all.x * m.x, through<LOGITS>(m.x, m.y, all.y));
                 }
-            } else {
-                for (int w = 0; w < tg; ++w) {
-                    if (w == group) in_c = carry;
-                    const float2 m = s_map[buf][w0 + w];
-                    carry = through(m.x, m.y, carry);
-                }
+                store_remote(&s_remote[buf][rank], tid, all);
+            }
+            cluster_meet();   // (the slots of a round are written again two meetings later)
+            for (int k = 0; k < cluster; ++k) {
+                if (k == rank) in_c = carry;
+                const float2 m = s_remote[buf][k];
+                carry = through<LOGITS>(m.x, m.y, carry);
+            }
+            for (int w = 0; w < group; ++w) {
+                const float2 m = s_map[buf][w];
+                in_c = through<LOGITS>(m.x, m.y, in_c);
             }
         } else {
-            carry = through(CA, CH, carry);
+            if (tg > 1 && (round > 0 || group > 0)) {
+                take_carry(warp);
+                in_c = s_carry[warp];
+            }
+            carry = through<LOGITS>(CA, CH, in_c);
+            if (tg > 1 && (round + 1 < rounds || group < tg - 1)) {
+                const int next = warp - group + ((group + 1) & (tg - 1));
+                if (lane == 0) s_carry[next] = carry;
+                give_carry(next);
+            }
         }
 
         // the steps again, from that carry
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int64_t t = first_step(round, j);
-            float at = through(Ae[j], He[j], in_c), o0[V], o1[V];
-            in_c = through(At[j], Ht[j], in_c);
+            float at = through<LOGITS>(Ae[j], He[j], in_c), o0[V], o1[V];
+            in_c = through<LOGITS>(At[j], Ht[j], in_c);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int e = BACK ? V - 1 - i : i;
@@ -537,7 +617,8 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
             if (BACK) store_granule(out1, t, steps, o1);
         }
     }
-    if (s.last != nullptr && valid && rank == 0 && group == 0 && lane == 0) s.last[row] = carry;
+    // (of the last warp's steps, or with a cluster everyone's)
+    if (s.last != nullptr && valid && rank == 0 && group == tg - 1 && lane == 0) s.last[row] = carry;
 }
 
 // ---- anything else, an element at a time ----
@@ -717,7 +798,7 @@ strided_kernel(const ScanArgs s, const int cluster) {
                 float CA = 1.0f, CH = 0.0f;
                 for (int w = 0; w < kScanWarps; ++w) {
                     const float wa = s_A[buf][w][v * 32 + lane];
-                    CH = through(wa, s_H[buf][w][v * 32 + lane], CH);
+                    CH = through<LOGITS>(wa, s_H[buf][w][v * 32 + lane], CH);
                     CA *= wa;
                 }
                 for (int k = warp / V; k < cluster; k += kScanWarps / V) {
@@ -730,7 +811,7 @@ strided_kernel(const ScanArgs s, const int cluster) {
                     for (int v = 0; v < V; ++v) {
                         for (int k = 0; k < cluster; ++k) {
                             if (k == rank) s_start[v * 32 + lane] = carry[v];
-                            carry[v] = through(s_rA[buf][k][v * 32 + lane], s_rH[buf][k][v * 32 + lane], carry[v]);
+                            carry[v] = through<LOGITS>(s_rA[buf][k][v * 32 + lane], s_rH[buf][k][v * 32 + lane], carry[v]);
                         }
                     }
                 }
@@ -739,19 +820,19 @@ strided_kernel(const ScanArgs s, const int cluster) {
                 for (int v = 0; v < V; ++v) in_c[v] = s_start[v * 32 + lane];
                 for (int w = 0; w < group; ++w)
 #pragma unroll
-                    for (int v = 0; v < V; ++v) in_c[v] = through(s_A[buf][w][v * 32 + lane], s_H[buf][w][v * 32 + lane], in_c[v]);
+                    for (int v = 0; v < V; ++v) in_c[v] = through<LOGITS>(s_A[buf][w][v * 32 + lane], s_H[buf][w][v * 32 + lane], in_c[v]);
             } else {
                 for (int w = 0; w < tg; ++w) {
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
                         if (w == group) in_c[v] = carry[v];
-                        carry[v] = through(s_A[buf][w0 + w][v * 32 + lane], s_H[buf][w0 + w][v * 32 + lane], carry[v]);
+                        carry[v] = through<LOGITS>(s_A[buf][w0 + w][v * 32 + lane], s_H[buf][w0 + w][v * 32 + lane], carry[v]);
                     }
                 }
             }
         } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) in_c[v] = carry[v], carry[v] = through(A[v], H[v], carry[v]);
+            for (int v = 0; v < V; ++v) in_c[v] = carry[v], carry[v] = through<LOGITS>(A[v], H[v], carry[v]);
         }
 
         // the steps again, from that carry
@@ -829,7 +910,7 @@ int cluster_for(int64_t tiles, int64_t steps, int64_t per) {
 template <typename T, bool BACK, int LC, bool LOGITS>
 cudaError_t launch_channels(ScanArgs &s, int64_t tiles, int cluster, cudaStream_t stream) {
     const auto kernel = channel_kernel<T, BACK, LC, LOGITS>;
-    constexpr size_t smem = size_t(kStages<LC>) * kStageBytes * kScanThreads;
+    constexpr size_t smem = size_t(kStages) * kStageBytes * kScanThreads;
     const cudaError_t e = allow_smem(kernel, smem);
     if (e != cudaSuccess) return e;
     if (tiles * cluster > INT32_MAX) return cudaErrorNotSupported;
