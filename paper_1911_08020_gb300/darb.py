@@ -8,6 +8,7 @@ the library's CUDA kernels; if ``libdarb.so`` is missing or a call fails, a
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 from dataclasses import dataclass
@@ -656,37 +657,45 @@ def darb_layer_norm_grad_work(layout: int, steps: int, tokens: int, features: in
 
 # ---- a gated linear recurrence ----
 
-def _channel_axes(like, others, dim: int, call: str) -> tuple[int, int, int, int, int]:
-    """(outer, steps, inner, outer axis, step axis) of tensors whose steps lie along `dim`: their other axes are
-    one run of contiguous channels where that holds for all of them, else a strided axis and a contiguous one.
-    The outer axis is -1 where there is none."""
-    shape = like.shape
+def _channel_axes(shape, strides, dim: int, call: str) -> tuple[int, int, int, int, int]:
+    """(outer, steps, inner, outer axis, step axis) of tensors of one shape and these strides whose steps lie along
+    `dim`: their other axes are one run of contiguous channels where that holds for all of them, else a strided
+    axis and a contiguous one.  The outer axis is -1 where there is none."""
     nd = len(shape)
     if nd not in (2, 3) or not -nd <= dim < nd:
         _refuse(call, "x must be 2-D or 3-D, with its steps along dim")
-    dim %= nd
-    axes = [a for a in range(nd) if a != dim]
-    n = [shape[a] for a in axes]
-    channels = n[0] * (n[1] if nd == 3 else 1)
-    tensors = (like, *others)
-    if nd == 3:
-        if n[0] == 1 or n[1] == 1:
-            axes = axes[n[0] == 1:][:1]
-        elif channels and any(t.stride(axes[0]) != n[1] * t.stride(axes[1]) for t in tensors):
-            if any(t.stride(axes[1]) != 1 for t in tensors):
-                _refuse(call, "the last axis of the channels must be contiguous, or all channels equally far apart")
-            return n[0], shape[dim], n[1], axes[0], dim
-    if channels <= 1 or all(t.stride(axes[-1]) == 1 for t in tensors):
-        return 1, shape[dim], channels, -1, dim
-    return channels, shape[dim], 1, axes[-1], dim
+    if dim < 0:
+        dim += nd
+    if nd == 2:
+        axis = 1 - dim
+        channels = shape[axis]
+    else:
+        a, axis = ((1, 2), (0, 2), (0, 1))[dim]
+        na, nb = shape[a], shape[axis]
+        channels = na * nb
+        if nb == 1:
+            axis = a
+        elif na > 1 and channels:
+            for s in strides:
+                if s[a] != nb * s[axis]:
+                    if any(t[axis] != 1 for t in strides):
+                        _refuse(call, "the last axis of the channels must be contiguous, or all channels equally far apart")
+                    return na, shape[dim], nb, a, dim
+    if channels > 1:
+        for s in strides:
+            if s[axis] != 1:
+                return channels, shape[dim], 1, axis, dim
+    return 1, shape[dim], channels, -1, dim
 
 
-def _scan_operand(t, like, outer: int, step: int, call: str, name: str) -> tuple[int, int, int]:
-    """(pointer, leading dimension, step) of a tensor of x's shape and type."""
-    if t.dtype != like.dtype or not t.is_cuda or t.shape != like.shape:
-        _refuse(call, f"{name} must be a CUDA tensor of x's shape and type")
-    strides = t.stride()
-    return t.data_ptr(), strides[outer] if outer >= 0 else 0, strides[step]
+def _scan_operands(call: str, like, outer: int, step: int, operands, strides):
+    """Pointer, leading dimension and step of every (name, tensor) of x's shape, checked to be of its type."""
+    dtype, out = like.dtype, []
+    for (name, t), s in zip(operands, strides):
+        if t.dtype != dtype or not t.is_cuda:
+            _refuse(call, f"{name} must be a CUDA tensor of x's type")
+        out += (t.data_ptr(), s[outer] if outer >= 0 else 0, s[step])
+    return out
 
 
 def _state_shape(x, dim: int):
@@ -706,19 +715,19 @@ def darb_gated_scan(gate, x, h0=None, dim: int = 0, gates: int = GATES_LOGITS, c
     `dim`, the state before the first step (None: 0).  h: as x, and may be x; h_last: as h0, and may be h0."""
     call = "darb_gated_scan"
     code = _value_code(x, call, "x")
-    f32 = _torch.float32
+    f32, shape = _torch.float32, x.shape
     if h is None:
-        h = _new(x.shape, x.dtype, x.device, stream)
-    if gate.shape != x.shape or h.shape != x.shape:
+        h = _new(shape, x.dtype, x.device, stream)
+    if gate.shape != shape or h.shape != shape:
         _refuse(call, "gate and h must have x's shape")
-    outer, steps, inner, oa, sa = _channel_axes(x, (gate, h), dim, call)
+    strides = (gate.stride(), x.stride(), h.stride())
+    outer, steps, inner, oa, sa = _channel_axes(shape, strides, dim, call)
     if h_last is None:
         h_last = _new(_state_shape(x, sa), f32, x.device, stream)
     n = outer * inner
-    _check(lib().darb_gated_scan(*_scan_operand(gate, x, oa, sa, call, "gate"), *_scan_operand(x, x, oa, sa, call, "x"), code,
-                                 gates, bool(coupled), outer, steps, inner, _vector(h0, n, f32, call, "h0"),
-                                 *_scan_operand(h, x, oa, sa, call, "h"), _vector(h_last, n, f32, call, "h_last"),
-                                 _stream(stream)), call)
+    at = _scan_operands(call, x, oa, sa, (("gate", gate), ("x", x), ("h", h)), strides)
+    _check(lib().darb_gated_scan(*at[:6], code, gates, bool(coupled), outer, steps, inner, _vector(h0, n, f32, call, "h0"),
+                                 *at[6:], _vector(h_last, n, f32, call, "h_last"), _stream(stream)), call)
     return h, h_last
 
 
@@ -729,24 +738,24 @@ def darb_gated_scan_grad(dh, gate, x, h, h0=None, d_last=None, dim: int = 0, gat
     h0 there is no d_h0 (None) unless a buffer for it is given."""
     call = "darb_gated_scan_grad"
     code = _value_code(x, call, "x")
-    f32 = _torch.float32
+    f32, shape = _torch.float32, x.shape
     if d_gate is None:
-        d_gate = _new(x.shape, x.dtype, x.device, stream)
+        d_gate = _new(shape, x.dtype, x.device, stream)
     if d_x is None:
-        d_x = _new(x.shape, x.dtype, x.device, stream)
-    others = (gate, dh, h, d_gate, d_x)
-    if any(t.shape != x.shape for t in others):
-        _refuse(call, "dh, gate, h, d_gate and d_x must have x's shape")
-    outer, steps, inner, oa, sa = _channel_axes(x, others, dim, call)
+        d_x = _new(shape, x.dtype, x.device, stream)
+    tensors = (dh, gate, x, h, d_gate, d_x)
+    for t in tensors:
+        if t.shape != shape:
+            _refuse(call, "dh, gate, h, d_gate and d_x must have x's shape")
+    strides = [t.stride() for t in tensors]
+    outer, steps, inner, oa, sa = _channel_axes(shape, strides, dim, call)
     if d_h0 is None and h0 is not None:
         d_h0 = _new(_state_shape(x, sa), f32, x.device, stream)
     n = outer * inner
-    at = [_scan_operand(t, x, oa, sa, call, name) for t, name in ((dh, "dh"), (gate, "gate"), (x, "x"), (h, "h"))]
-    _check(lib().darb_gated_scan_grad(*at[0], *at[1], *at[2], *at[3], code, gates, bool(coupled), outer, steps, inner,
-                                      _vector(h0, n, f32, call, "h0"), _vector(d_last, n, f32, call, "d_last"),
-                                      *_scan_operand(d_gate, x, oa, sa, call, "d_gate"),
-                                      *_scan_operand(d_x, x, oa, sa, call, "d_x"), _vector(d_h0, n, f32, call, "d_h0"),
-                                      _stream(stream)), call)
+    at = _scan_operands(call, x, oa, sa, zip(("dh", "gate", "x", "h", "d_gate", "d_x"), tensors), strides)
+    _check(lib().darb_gated_scan_grad(*at[:12], code, gates, bool(coupled), outer, steps, inner,
+                                      _vector(h0, n, f32, call, "h0"), _vector(d_last, n, f32, call, "d_last"), *at[12:],
+                                      _vector(d_h0, n, f32, call, "d_h0"), _stream(stream)), call)
     return d_gate, d_x, d_h0
 
 
@@ -814,6 +823,7 @@ def darb_policy_loss(logprob, old_logprob, advantage, offsets, ref_logprob=None,
     return out
 
 
+@functools.lru_cache(maxsize=64)
 def darb_policy_loss_work(tokens: int) -> int:
     """Bytes of scratch that darb_policy_loss needs for so many tokens."""
     need = ctypes.c_int64()
