@@ -56,6 +56,7 @@ constexpr int kPointers = 448;              // gradients of a launch
 constexpr int kParts = 304;                 // CTAs of a matrix in the elementwise kernels, at most
 constexpr int kPartElems = 4096;            // elements of one, at least
 constexpr int kElemThreads = 256;
+constexpr int kUnroll = 4;                  // times four elements of a thread whose loads are on their way together
 constexpr int64_t kMaxSide = 32768;         // rows and columns: elements fit 32 bits
 
 constexpr int kBM = 128, kBK = 64;          // rows of a tile; depth of a stage
@@ -74,6 +75,8 @@ struct alignas(128) Matrix {
     int32_t rows, cols, n;                  // n: the shorter side
     int32_t ldx, lda;                       // of the fp16 numbers
     int32_t tall, parts, part_elems;
+    int32_t shift;                          // e / cols = e * reciprocal >> shift for e < 2^31
+    uint64_t reciprocal;
     float size;                             // 0.2 sqrt(max(rows, cols))
 };
 struct Part {
@@ -103,15 +106,10 @@ __device__ __forceinline__ bool aligned16(const void *p) { return (reinterpret_c
 
 __device__ __forceinline__ float direction(const StepArgs &a, float g, float m) { return a.nesterov ? a.rest * g + a.beta * m : m; }
 
-// Elements [e0, e1) of a matrix, four at a time where `vector`: f(index, count).
-template <typename F>
-__device__ __forceinline__ void each_quad(int64_t e0, int64_t e1, F f) {
-    for (int64_t e = e0 + int64_t(threadIdx.x) * 4; e < e1; e += kElemThreads * 4) f(int(e), int(e1 - e < 4 ? e1 - e : 4));
-}
-
+// Elements e .. e + 4 of those before `end`.
 template <typename G>
-__device__ __forceinline__ void load4(const G *p, int e, int count, bool vector, float (&v)[4]) {
-    if (vector && count == 4) {
+__device__ __forceinline__ void load4(const G *p, int64_t e, int64_t end, bool vector, float (&v)[4]) {
+    if (vector && e + 4 <= end) {
         if constexpr (sizeof(G) == 4) {
             const float4 q = *reinterpret_cast<const float4 *>(p + e);
             v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
@@ -123,7 +121,16 @@ __device__ __forceinline__ void load4(const G *p, int e, int count, bool vector,
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = i < count ? widen(p[e + i]) : 0.0f;
+    for (int i = 0; i < 4; ++i) v[i] = e + i < end ? widen(p[e + i]) : 0.0f;
+}
+__device__ __forceinline__ void store4(float *p, int64_t e, int64_t end, bool vector, const float (&v)[4]) {
+    if (vector && e + 4 <= end) {
+        *reinterpret_cast<float4 *>(p + e) = make_float4(v[0], v[1], v[2], v[3]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (e + i < end) p[e + i] = v[i];
 }
 
 __device__ __forceinline__ double block_total(double v) {
@@ -150,32 +157,40 @@ __global__ void __launch_bounds__(kElemThreads) momentum_kernel(const StepArgs a
     const bool vector = aligned16(x.m) && (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) == 0;
     float *const m = x.m;
     double sum = 0.0;
-    each_quad(e0, e1, [&](int e, int count) {
-        float gv[4], mv[4], top = 0.0f, squares = 0.0f;
-        load4(g, e, count, vector, gv);
-        load4(m, e, count, vector, mv);
+    for (int64_t b0 = e0 + int64_t(threadIdx.x) * 4; b0 < e1; b0 += kUnroll * kElemThreads * 4) {
+        float gv[kUnroll][4], mv[kUnroll][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            gv[i] *= scale;
-            mv[i] = mv[i] * a.beta + gv[i] * a.rest;
-            gv[i] = direction(a, gv[i], mv[i]);
-            top = fmaxf(top, fabsf(gv[i]));
-            squares = fmaf(gv[i], gv[i], squares);
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t e = b0 + u * kElemThreads * 4;
+            load4(g, e, e1, vector, gv[u]);
+            load4(m, e, e1, vector, mv[u]);
         }
-        if (vector && count == 4) {
-            *reinterpret_cast<float4 *>(m + e) = make_float4(mv[0], mv[1], mv[2], mv[3]);
-        } else {
-            for (int i = 0; i < count; ++i) m[e + i] = mv[i];
+        float top = 0.0f, squares = 0.0f;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t e = b0 + u * kElemThreads * 4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float gs = gv[u][i] * scale;
+                mv[u][i] = mv[u][i] * a.beta + gs * a.rest;
+                gv[u][i] = direction(a, gs, mv[u][i]);
+                top = fmaxf(top, fabsf(gv[u][i]));
+                squares = fmaf(gv[u][i], gv[u][i], squares);
+            }
+            store4(m, e, e1, vector, mv[u]);
         }
         // squares that 32 bits do not hold
         if (top > 1e15f || (top < 1e-15f && top > 0.0f)) {
-            double s = 0.0;
-            for (int i = 0; i < 4; ++i) s += double(gv[i]) * gv[i];
-            sum += s;
+            double d = 0.0;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d += double(gv[u][i]) * gv[u][i];
+            sum += d;
         } else {
             sum += double(squares);
         }
-    });
+    }
     sum = block_total(sum);
     if (threadIdx.x == 0) x.partial[part.part] = sum;
 }
@@ -198,32 +213,47 @@ __global__ void __launch_bounds__(kElemThreads) start_kernel(const StepArgs a, c
     for (int i = threadIdx.x; i < x.parts; i += kElemThreads) sum += x.partial[i];
     sum = block_total(sum);
     const float norm = float(sqrt(sum)) + a.eps, scale = a.grad_scale != nullptr ? *a.grad_scale : 1.0f;
+    const float factor = kScaleX / norm;
+    const bool divide = !(factor < INFINITY);   // (a norm too small for its reciprocal)
     const int64_t all = int64_t(x.rows) * x.cols, e0 = int64_t(part.part) * x.part_elems, e1 = min(e0 + x.part_elems, all);
     const bool vector = aligned16(x.m) && (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) == 0;
     const float *const m = x.m;
     __half *const hi = x.xp[0][0], *const lo = x.xp[0][1];
-    const int cols = x.cols;
+    const int cols = x.cols, ldx = x.ldx, shift = x.shift;
+    const uint64_t reciprocal = x.reciprocal;
     const bool quads = cols % 4 == 0;
-    each_quad(e0, e1, [&](int e, int count) {
-        float gv[4], mv[4];
-        load4(g, e, count, vector, gv);
-        load4(m, e, count, vector, mv);
-        alignas(8) __half h[4], l[4];
+    for (int64_t b0 = e0 + int64_t(threadIdx.x) * 4; b0 < e1; b0 += kUnroll * kElemThreads * 4) {
+        float gv[kUnroll][4], mv[kUnroll][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) split(direction(a, gv[i] * scale, mv[i]) / norm * kScaleX, h[i], l[i]);
-        int row = e / cols, col = e - row * cols;
-        if (quads) {   // (then count is 4: parts are multiples of 4 elements)
-            const int64_t at = int64_t(row) * x.ldx + col;
-            *reinterpret_cast<uint2 *>(hi + at) = *reinterpret_cast<const uint2 *>(h);
-            *reinterpret_cast<uint2 *>(lo + at) = *reinterpret_cast<const uint2 *>(l);
-            return;
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t e = b0 + u * kElemThreads * 4;
+            load4(g, e, e1, vector, gv[u]);
+            load4(m, e, e1, vector, mv[u]);
         }
-        for (int i = 0; i < count; ++i) {
-            const int64_t at = int64_t(row) * x.ldx + col;
-            hi[at] = h[i], lo[at] = l[i];
-            if (++col == cols) col = 0, ++row;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t e = b0 + u * kElemThreads * 4;
+            if (e >= e1) break;
+            alignas(8) __half h[4], l[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float d = direction(a, gv[u][i] * scale, mv[u][i]);
+                split(divide ? d / norm * kScaleX : d * factor, h[i], l[i]);
+            }
+            int row = int(uint64_t(e) * reciprocal >> shift), col = int(e) - row * cols;
+            if (quads) {   // (then all four are there: parts are multiples of 4 elements)
+                const int64_t at = int64_t(row) * ldx + col;
+                *reinterpret_cast<uint2 *>(hi + at) = *reinterpret_cast<const uint2 *>(h);
+                *reinterpret_cast<uint2 *>(lo + at) = *reinterpret_cast<const uint2 *>(l);
+                continue;
+            }
+            for (int i = 0; i < 4 && e + i < e1; ++i) {
+                const int64_t at = int64_t(row) * ldx + col;
+                hi[at] = h[i], lo[at] = l[i];
+                if (++col == cols) col = 0, ++row;
+            }
         }
-    });
+    }
 }
 
 // ---- products ----
@@ -236,14 +266,79 @@ __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, bool a_mn, bool b
     return (1u << 4) | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16) | (uint32_t(N >> 3) << 17) | (uint32_t(M >> 4) << 24);
 }
 
-template <int P, int BN>
+// P: products of fp16 numbers that make one of the operands.  BN: columns of a tile.
+// CG: CTAs of a tile, each with 128 of its rows; a pair reads half of the columns each,
+// which halves what the copies write to a shared memory.
+template <int P, int BN, int CG>
 struct Geo {
     static constexpr int kParts = P == 1 ? 1 : 2;                 // fp16 numbers of an operand
-    static constexpr int kABytes = kBM / 64 * kBox, kBBytes = BN / 64 * kBox;
+    static constexpr int kABytes = kBM / 64 * kBox, kBBytes = BN / CG / 64 * kBox;
     static constexpr int kStage = kParts * (kABytes + kBBytes);
-    static constexpr int kStages = (220 * 1024) / kStage < 6 ? (220 * 1024) / kStage : 6;
-    static constexpr size_t kSmem = 2048 + size_t(kStages) * kStage;
+    static constexpr int kTurn = 4 * 32 * 64 * 4;                 // 32 rows x 64 columns of each writing warp
+    static constexpr int kFit = (227 * 1024 - 2048 - kTurn) / kStage;
+    static constexpr int kStages = kFit < 6 ? kFit : 6;
+    static constexpr size_t kSmem = 2048 + size_t(kStages) * kStage + kTurn;
 };
+
+// tcgen05 for one CTA or a pair.
+template <int CG>
+__device__ __forceinline__ void pair_alloc(uint32_t *dst, uint32_t ncols) {
+    if (CG == 1) {
+        tmem_alloc(dst, ncols);
+        tmem_relinquish();
+        return;
+    }
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst)), "r"(ncols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+template <int CG>
+__device__ __forceinline__ void pair_dealloc(uint32_t taddr, uint32_t ncols) {
+    if (CG == 1) tmem_dealloc(taddr, ncols);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    if (CG == 1) {
+        mma_bf16(d, a, b, idesc, acc);   // (the type is the descriptor's)
+        return;
+    }
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+// Arrive on `bar` (of both CTAs) when every product issued so far is complete.
+template <int CG>
+__device__ __forceinline__ void pair_commit(uint64_t *bar) {
+    if (CG == 1) mma_commit(bar);
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)),
+                     "h"(uint16_t(3))
+                     : "memory");
+}
+// A box into this CTA's shared memory that completes on a barrier of the pair's first CTA.
+template <int CG>
+__device__ __forceinline__ void pair_copy(void *dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    if (CG == 1)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_addr(dst)),
+                     "l"(map), "r"(x), "r"(y), "r"(bar)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                         smem_addr(dst)),
+                     "l"(map), "r"(x), "r"(y), "r"(bar)
+                     : "memory");
+}
+__device__ __forceinline__ uint32_t shared_of(const void *p, uint32_t rank) {
+    uint32_t to;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(p)), "r"(rank));
+    return to;
+}
+__device__ __forceinline__ void pair_meet() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 // The product's operands of a matrix, and how they lie.
 struct Operands {
@@ -259,109 +354,225 @@ __device__ __forceinline__ Operands operands(const Matrix &x, int buf) {
     return x.tall ? Operands{x.x[buf], x.b, false, false, x.n} : Operands{x.b, x.x[buf], false, true, x.n};
 }
 
-// 32 numbers of a row, 16 bytes at a time
-__device__ __forceinline__ void store32(__half *p, const __half (&v)[32]) {
+// A warp has 32 rows x 64 columns of a product as 64 numbers of a row in each lane; it
+// turns them through shared memory, so that eight lanes share a row, eight neighbouring
+// columns each, and 4 rows of 128 bytes of fp16 are read or written at once.  The 16
+// bytes c of row r stand at c ^ (r % 8).
+struct Turn {
+    float4 *at;   // 32 x 16
+
+    __device__ __forceinline__ void put(int lane, int c0, const uint32_t (&v)[32]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(v)[i];
+        for (int i = 0; i < 8; ++i)
+            at[lane * 16 + ((c0 + i) ^ (lane & 7))] =
+                make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+    }
+    __device__ __forceinline__ void get(int row, int oct, float (&v)[8]) const {
+        const float4 x = at[row * 16 + ((2 * oct) ^ (row & 7))], y = at[row * 16 + ((2 * oct + 1) ^ (row & 7))];
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+    }
+    __device__ __forceinline__ void set(int row, int oct, const float (&v)[8]) const {
+        at[row * 16 + ((2 * oct) ^ (row & 7))] = make_float4(v[0], v[1], v[2], v[3]);
+        at[row * 16 + ((2 * oct + 1) ^ (row & 7))] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+    __device__ __forceinline__ float one(int row, int col) const {
+        return reinterpret_cast<const float *>(&at[row * 16 + ((col >> 2) ^ (row & 7))])[col & 3];
+    }
+};
+
+__device__ __forceinline__ void halves(const uint4 &q, float (&v)[8]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+        v[2 * i] = f.x, v[2 * i + 1] = f.y;
+    }
 }
-__device__ __forceinline__ void load32(const __half *p, __half (&v)[32]) {
+// Eight numbers as the sums of two fp16 numbers.
+__device__ __forceinline__ void split8(const float (&v)[8], uint4 &hi, uint4 &lo) {
+    uint32_t h[4], l[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) reinterpret_cast<uint4 *>(v)[i] = reinterpret_cast<const uint4 *>(p)[i];
+    for (int i = 0; i < 4; ++i) {
+        const __half2 a = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        const float2 f = __half22float2(a);
+        const __half2 b = __floats2half2_rn(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+        h[i] = *reinterpret_cast<const uint32_t *>(&a), l[i] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]), lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
-// What becomes of 32 columns from j0 on of row i of a product.
+// What becomes of rows i0 .. i0 + 32 and columns j0 .. j0 + 64 of a product, `acc` being
+// the accumulator's address.
 template <int P, int OP>
-__device__ __forceinline__ void finish(const StepArgs &s, const Matrix &x, int buf, bool last, int i, int j0, const uint32_t (&acc)[32]) {
+__device__ __forceinline__ void finish(const StepArgs &s, const Matrix &x, int buf, bool last, int i0, int j0, uint32_t acc, const Turn &turn) {
     constexpr bool two = P == 3;
+    const int lane = threadIdx.x & 31, oct = lane & 7, sub = lane >> 3;
+    const int rows = OP == kApply ? x.rows : x.n, cols = OP == kApply ? x.cols : x.n;
+    if (i0 >= rows || j0 >= cols || (OP != kApply && j0 > i0 + 31)) return;
+    const int ld = OP == kApply ? x.ldx : x.lda;
+    const int j = j0 + 8 * oct;                            // this lane's columns after the turn
+    const bool inside = j < ld;                            // (rows are as long as a multiple of 64 numbers)
+    const __half *const in_hi = OP == kApply ? x.xp[buf][0] : x.ap[0], *const in_lo = OP == kApply ? x.xp[buf][1] : x.ap[1];
+    uint4 hi[8], lo[8];
+    if (OP != kGram) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int i = i0 + 4 * q + sub;
+            if (i >= rows || !inside) continue;
+            const int64_t at = int64_t(i) * ld + j;
+            hi[q] = *reinterpret_cast<const uint4 *>(in_hi + at);
+            if (OP == kApply || two) lo[q] = *reinterpret_cast<const uint4 *>(in_lo + at);
+        }
+    }
+    uint32_t v[32];
+#pragma unroll
+    for (int c = 0; c < 64; c += 32) {
+        tmem_ld32(acc + c, v);
+        tmem_ld_wait();
+        turn.put(lane, c / 4, v);
+    }
+    __syncwarp();
+
     if (OP != kApply) {
-        const int n = x.n;
-        if (i >= n || j0 > i) return;
-        __half *const hi = OP == kGram ? x.ap[0] : x.bp[0], *const lo = OP == kGram ? x.ap[1] : x.bp[1];
-        const int64_t at = int64_t(i) * x.lda + j0;
-        const float di = OP == kSquare ? x.d[i] : 0.0f;
-        alignas(16) __half ah[32], al[32];
+        __half *const out_hi = OP == kGram ? x.ap[0] : x.bp[0], *const out_lo = OP == kGram ? x.ap[1] : x.bp[1];
+        float dj[8];
         if (OP == kSquare) {
-            load32(x.ap[0] + at, ah);
-            if (two) load32(x.ap[1] + at, al);
-        }
-        alignas(16) __half h[32], l[32];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            const int j = j0 + e;
-            const float raw = __uint_as_float(acc[e]);
-            float v = raw * (1.0f / kScaleX);
-            if (OP == kSquare) {
-                const float sq = raw * (1.0f / (kScaleX * kScaleX));
-                const float old = (__half2float(ah[e]) + (two ? __half2float(al[e]) : 0.0f)) * (1.0f / kScaleX);
-                const float dj = j <= i ? x.d[j] : 0.0f;
-                v = (kB * old + kC * fmaf(di + dj, old, sq)) * kScaleB;
-                if (j == i) x.D[i] = kA + kB * di + kC * fmaf(di, di, sq);
-            } else if (j == i) {
-                x.d[i] = raw * (1.0f / (kScaleX * kScaleX));
-            }
-            split(v, h[e], l[e]);
-            if (j < i) {   // across the diagonal: neighbouring lanes are neighbouring places
-                hi[int64_t(j) * x.lda + i] = h[e];
-                if (two) lo[int64_t(j) * x.lda + i] = l[e];
-            }
+            for (int e = 0; e < 8; ++e) dj[e] = j + e < cols ? x.d[j + e] : 0.0f;
         }
-        if (j0 + 31 < i) {
-            store32(hi + at, h);
-            if (two) store32(lo + at, l);
-        } else {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                if (j0 + e >= i) continue;
-                hi[at + e] = h[e];
-                if (two) lo[at + e] = l[e];
+        for (int q = 0; q < 8; ++q) {
+            const int i = i0 + 4 * q + sub;
+            float r[8], w[8];
+            turn.get(4 * q + sub, oct, r);
+            if (i < rows && inside) {
+                if (OP == kSquare) {
+                    const float di = x.d[i];
+                    float old[8], more[8];
+                    halves(hi[q], old);
+                    if (two) halves(lo[q], more);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float sq = r[e] * (1.0f / (kScaleX * kScaleX)), A = (two ? old[e] + more[e] : old[e]) * (1.0f / kScaleX);
+                        w[e] = (kB * A + kC * fmaf(di + dj[e], A, sq)) * kScaleB;
+                        if (j + e == i) x.D[i] = kA + kB * di + kC * fmaf(di, di, sq);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        w[e] = r[e] * (1.0f / kScaleX);
+                        if (j + e == i) x.d[i] = r[e] * (1.0f / (kScaleX * kScaleX));
+                    }
+                }
+                uint4 h, l;
+                split8(w, h, l);
+                const int64_t at = int64_t(i) * ld + j;
+                if (j + 8 <= i) {
+                    *reinterpret_cast<uint4 *>(out_hi + at) = h;
+                    if (two) *reinterpret_cast<uint4 *>(out_lo + at) = l;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (j + e >= i) continue;
+                        __half a, b;
+                        split(w[e], a, b);
+                        out_hi[at + e] = a;
+                        if (two) out_lo[at + e] = b;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = 0.0f;
+            }
+            turn.set(4 * q + sub, oct, w);
+        }
+        __syncwarp();
+        // across the diagonal: a lane has two rows of half of the columns
+        const int i = i0 + 2 * (lane & 15);
+#pragma unroll 4
+        for (int c = lane >> 4; c < 64; c += 2) {
+            const int jj = j0 + c;
+            if (jj >= cols || i >= rows || jj > i) continue;
+            const float v0 = turn.one(2 * (lane & 15), c), v1 = turn.one(2 * (lane & 15) + 1, c);
+            const __half2 h = __floats2half2_rn(v0, v1);
+            const float2 f = __half22float2(h);
+            const __half2 l = __floats2half2_rn(v0 - f.x, v1 - f.y);
+            const int64_t at = int64_t(jj) * ld + i;
+            if (jj < i && i + 1 < rows) {
+                *reinterpret_cast<__half2 *>(out_hi + at) = h;
+                if (two) *reinterpret_cast<__half2 *>(out_lo + at) = l;
+            } else {
+                if (jj < i) {
+                    out_hi[at] = __low2half(h);
+                    if (two) out_lo[at] = __low2half(l);
+                }
+                if (jj < i + 1 && i + 1 < rows) {
+                    out_hi[at + 1] = __high2half(h);
+                    if (two) out_lo[at + 1] = __high2half(l);
+                }
             }
         }
+        __syncwarp();
         return;
     }
-    if (i >= x.rows || j0 >= x.cols) return;
-    const int64_t at = int64_t(i) * x.ldx + j0;   // (rows are as long as a multiple of 64 numbers)
-    const float Di = x.tall ? 0.0f : x.D[i];
-    alignas(16) __half h[32], l[32];
-    load32(x.xp[buf][0] + at, h);
-    load32(x.xp[buf][1] + at, l);
-    float v[32];
+
+    float dj[8];
+    if (x.tall) {
 #pragma unroll
-    for (int e = 0; e < 32; ++e) {
-        const int j = min(j0 + e, x.cols - 1);
-        const float D = x.tall ? x.D[j] : Di;
-        v[e] = fmaf(D, (__half2float(h[e]) + __half2float(l[e])) * (1.0f / kScaleX), __uint_as_float(acc[e]) * (1.0f / (kScaleX * kScaleB)));
-    }
-    if (!last) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) split(v[e] * kScaleX, h[e], l[e]);
-        store32(x.xp[buf ^ 1][0] + at, h);
-        store32(x.xp[buf ^ 1][1] + at, l);
-        return;
+        for (int e = 0; e < 8; ++e) dj[e] = j + e < cols ? x.D[j + e] : 0.0f;
     }
     const float size = s.lr * x.size;
-    const int64_t to = int64_t(i) * x.cols + j0;
-    float *const p = x.p + to;
-    __nv_bfloat16 *const copy = x.copy != nullptr ? x.copy + to : nullptr;
-    if (j0 + 32 <= x.cols && x.cols % 4 == 0 && aligned16(x.p) && (reinterpret_cast<uintptr_t>(x.copy) & 7) == 0) {
+    const bool vector = x.cols % 8 == 0 && aligned16(x.p) && aligned16(x.copy);
 #pragma unroll
-        for (int e = 0; e < 32; e += 4) {
-            float4 q = *reinterpret_cast<float4 *>(p + e);
-            q = make_float4(q.x * s.decay - size * v[e], q.y * s.decay - size * v[e + 1], q.z * s.decay - size * v[e + 2],
-                            q.w * s.decay - size * v[e + 3]);
-            *reinterpret_cast<float4 *>(p + e) = q;
-            if (copy != nullptr) {
-                const __nv_bfloat162 c0 = __floats2bfloat162_rn(q.x, q.y), c1 = __floats2bfloat162_rn(q.z, q.w);
-                *reinterpret_cast<uint2 *>(copy + e) = make_uint2(*reinterpret_cast<const uint32_t *>(&c0), *reinterpret_cast<const uint32_t *>(&c1));
+    for (int q = 0; q < 8; ++q) {
+        const int i = i0 + 4 * q + sub;
+        if (i >= rows || !inside) continue;
+        float r[8], a[8], b[8];
+        turn.get(4 * q + sub, oct, r);
+        halves(hi[q], a);
+        halves(lo[q], b);
+        const float di = x.tall ? 0.0f : x.D[i];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            r[e] = fmaf(x.tall ? dj[e] : di, (a[e] + b[e]) * (1.0f / kScaleX), r[e] * (1.0f / (kScaleX * kScaleB)));
+        if (!last) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[e] *= kScaleX;
+            uint4 h, l;
+            split8(r, h, l);
+            const int64_t at = int64_t(i) * ld + j;
+            *reinterpret_cast<uint4 *>(x.xp[buf ^ 1][0] + at) = h;
+            *reinterpret_cast<uint4 *>(x.xp[buf ^ 1][1] + at) = l;
+        } else if (!vector) {
+            turn.set(4 * q + sub, oct, r);
+        } else if (j < cols) {
+            const int64_t at = int64_t(i) * x.cols + j;
+            float4 p0 = reinterpret_cast<const float4 *>(x.p + at)[0], p1 = reinterpret_cast<const float4 *>(x.p + at)[1];
+            p0 = make_float4(p0.x * s.decay - size * r[0], p0.y * s.decay - size * r[1], p0.z * s.decay - size * r[2], p0.w * s.decay - size * r[3]);
+            p1 = make_float4(p1.x * s.decay - size * r[4], p1.y * s.decay - size * r[5], p1.z * s.decay - size * r[6], p1.w * s.decay - size * r[7]);
+            reinterpret_cast<float4 *>(x.p + at)[0] = p0;
+            reinterpret_cast<float4 *>(x.p + at)[1] = p1;
+            if (x.copy != nullptr) {
+                const float c[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+                *reinterpret_cast<uint4 *>(x.copy + at) = pack(c);
             }
         }
-        return;
     }
+    __syncwarp();
+    if (last && !vector) {
+#pragma unroll 4
+        for (int r = 0; r < 32; ++r) {
+            if (i0 + r >= rows) break;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) {
-        if (j0 + e >= x.cols) continue;
-        const float q = p[e] * s.decay - size * v[e];
-        p[e] = q;
-        if (copy != nullptr) copy[e] = __float2bfloat16_rn(q);
+            for (int c = lane; c < 64; c += 32) {
+                if (j0 + c >= cols) continue;
+                const int64_t at = int64_t(i0 + r) * x.cols + j0 + c;
+                const float p = x.p[at] * s.decay - size * turn.one(r, c);
+                x.p[at] = p;
+                if (x.copy != nullptr) x.copy[at] = __float2bfloat16_rn(p);
+            }
+        }
+        __syncwarp();
     }
 }
 
@@ -370,10 +581,10 @@ __device__ __forceinline__ void acquire_map(const CUtensorMap *map) {
     asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" ::"l"(map) : "memory");
 }
 
-// The tiles of CTA b are tiles[first[b]] .. tiles[first[b + 1] - 1].
-template <int P, int BN, int OP>
+// The tiles of CTA (or pair) b are tiles[first[b]] .. tiles[first[b + 1] - 1].
+template <int P, int BN, int CG, int OP>
 __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs s, const Tile *tiles, const int32_t *first, int buf, int last) {
-    using G = Geo<P, BN>;
+    using G = Geo<P, BN, CG>;
     constexpr int NS = G::kStages, NP = G::kParts;
     extern __shared__ unsigned char sm_raw[];
     unsigned char *const sm = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
@@ -382,24 +593,23 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
     uint32_t *const s_tmem = reinterpret_cast<uint32_t *>(done + 1);
     unsigned char *const stages = sm + 1024;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = CG == 2 ? int(blockIdx.x) & 1 : 0, unit = CG == 2 ? int(blockIdx.x) >> 1 : int(blockIdx.x);
     constexpr uint32_t kColumns = 2 * BN;
 
     pdl_launch_dependents();
     if (tid == 0) {
         for (int i = 0; i < NS; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-        for (int i = 0; i < 2; ++i) mbar_init(&ready[i], 1), mbar_init(&read[i], 4);
+        for (int i = 0; i < 2; ++i) mbar_init(&ready[i], 1), mbar_init(&read[i], 4 * CG);
         mbar_init(done, 1);
         fence_mbar_init();
     }
-    if (warp == 1) {
-        tmem_alloc(s_tmem, kColumns);
-        tmem_relinquish();
-    }
+    if (warp == 1) pair_alloc<CG>(s_tmem, kColumns);
     tc_fence_before_sync();
     __syncthreads();
+    if (CG == 2) pair_meet();   // the other CTA's barriers stand before anything arrives there
     tc_fence_after_sync();
     const uint32_t tmem = *s_tmem;
-    const int t0 = first[blockIdx.x], t1 = first[blockIdx.x + 1];
+    const int t0 = first[unit], t1 = first[unit + 1];
     bool ok = true;
     pdl_wait_previous();
 
@@ -415,6 +625,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                 const Matrix &x = s.matrices[tile.matrix];
                 if (!s.active[tile.matrix]) continue;
                 const Operands o = operands<OP>(x, buf);
+                const int row = tile.row + rank * kBM, col = tile.col + rank * (BN / CG);
                 if (tile.matrix != known) {
                     for (int q = 0; q < NP; ++q) acquire_map(&o.a[q]), acquire_map(&o.b[q]);
                     known = tile.matrix;
@@ -424,26 +635,29 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                         ok = false;
                         break;
                     }
-                    mbar_arrive_expect_tx(&full[stage], G::kStage);
+                    // the first CTA's barrier counts the bytes of both
+                    if (rank == 0) mbar_arrive_expect_tx(&full[stage], CG * G::kStage);
+                    const uint32_t bar = CG == 2 ? shared_of(&full[stage], 0) : smem_addr(&full[stage]);
                     unsigned char *to = stages + stage * G::kStage;
 #pragma unroll
                     for (int q = 0; q < NP; ++q)
                         for (int b = 0; b < kBM; b += 64, to += kBox)
-                            tensor2d_g2s(to, &o.a[q], o.a_mn ? tile.row + b : k, o.a_mn ? k : tile.row + b, &full[stage]);
+                            pair_copy<CG>(to, &o.a[q], o.a_mn ? row + b : k, o.a_mn ? k : row + b, bar);
 #pragma unroll
                     for (int q = 0; q < NP; ++q)
-                        for (int b = 0; b < BN; b += 64, to += kBox)
-                            tensor2d_g2s(to, &o.b[q], o.b_mn ? tile.col + b : k, o.b_mn ? k : tile.col + b, &full[stage]);
+                        for (int b = 0; b < BN / CG; b += 64, to += kBox)
+                            pair_copy<CG>(to, &o.b[q], o.b_mn ? col + b : k, o.b_mn ? k : col + b, bar);
                     if (++stage == NS) stage = 0, parity ^= 1u;
                 }
             }
-            if (!ok) {   // what is still on its way lands before the CTA leaves
+            // what is still on its way lands before the CTA leaves (in the second CTA: when the pair's products have
+            // been waited for, below)
+            if (!ok && rank == 0)
                 for (int64_t i = issued > NS ? issued - NS : 0; i < issued; ++i) mbar_wait(&full[i % NS], uint32_t(i / NS) & 1u);
-            }
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (lane == 0 && rank == 0) {
             int stage = 0, used = 0;
             uint32_t parity = 0;
             for (int t = t0; t < t1 && ok; ++t) {
@@ -451,12 +665,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                 const Matrix &x = s.matrices[tile.matrix];
                 if (!s.active[tile.matrix]) continue;
                 const Operands o = operands<OP>(x, buf);
-                const uint32_t idesc = idesc_f16(kBM, BN, o.a_mn, o.b_mn);
+                const uint32_t idesc = idesc_f16(CG * kBM, BN, o.a_mn, o.b_mn);
                 // along the depth: rows of 128 bytes; along the tile: boxes of 64 columns, 8 deep atoms one after the other
                 const uint32_t a_lbo = o.a_mn ? kBox : 16, b_lbo = o.b_mn ? kBox : 16;
                 const uint32_t a_step = (o.a_mn ? 2048 : 32) >> 4, b_step = (o.b_mn ? 2048 : 32) >> 4;
                 const int half = used & 1;
-                if (used >= 2 && !mbar_wait(&read[half], uint32_t(used / 2 - 1) & 1u)) {
+                if (used >= 2 && !mbar_wait_acq_cluster(&read[half], uint32_t(used / 2 - 1) & 1u)) {
                     ok = false;
                     break;
                 }
@@ -474,24 +688,26 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
 #pragma unroll
                     for (int kk = 0; kk < kBK / 16; ++kk) {
                         const uint64_t ao = kk * a_step, bo = kk * b_step;
-                        mma_bf16(d, ah + ao, bh + bo, idesc, (k | kk) != 0);
+                        pair_mma<CG>(d, ah + ao, bh + bo, idesc, (k | kk) != 0);
                         if (P == 3) {
-                            mma_bf16(d, ah + ao, bl + bo, idesc, 1u);
-                            mma_bf16(d, al + ao, bh + bo, idesc, 1u);
+                            pair_mma<CG>(d, ah + ao, bl + bo, idesc, 1u);
+                            pair_mma<CG>(d, al + ao, bh + bo, idesc, 1u);
                         }
                     }
-                    mma_commit(&empty[stage]);
+                    pair_commit<CG>(&empty[stage]);
                     if (++stage == NS) stage = 0, parity ^= 1u;
                 }
-                mma_commit(&ready[half]);
+                pair_commit<CG>(&ready[half]);
                 ++used;
             }
-            mma_commit(done);
-            if (!mbar_wait(done, 0)) ok = false;   // no product is in flight when the memory is given back
+            pair_commit<CG>(done);
         }
+        // no product is in flight when the memory is given back
+        if (lane == 0 && !mbar_wait(done, 0)) ok = false;
         __syncwarp();
     } else {
         const int quarter = warp & 3;
+        const Turn turn = {reinterpret_cast<float4 *>(stages + NS * G::kStage) + quarter * (32 * 16)};
         int used = 0;
         for (int t = t0; t < t1; ++t) {
             const Tile tile = tiles[t];
@@ -504,18 +720,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
             }
             tc_fence_after_sync();
             const uint32_t at = tmem + half * BN + (uint32_t(quarter * 32) << 16);
-            const int i = tile.row + quarter * 32 + lane;
+            const int i0 = tile.row + rank * kBM + quarter * 32;
 #pragma unroll 1
-            for (int c = 0; c < BN; c += 32) {
-                uint32_t acc[32];
-                tmem_ld32(at + c, acc);
-                tmem_ld_wait();
-                if (c + 32 == BN) {   // the accumulator has been read
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&read[half]);
-                }
-                finish<P, OP>(s, x, buf, last != 0, i, tile.col + c, acc);
+            for (int c = 0; c < BN; c += 64) finish<P, OP>(s, x, buf, last != 0, i0, tile.col + c, at + c, turn);
+            // the accumulator has been read
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 1) mbar_arrive(&read[half]);
+                else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(shared_of(&read[half], 0)) : "memory");
             }
             ++used;
         }
@@ -523,9 +736,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
     if (!ok) atomicOr(s.status, kStatusTimeout);
     tc_fence_before_sync();
     __syncthreads();
+    if (CG == 2) pair_meet();   // neither CTA leaves while the other may reach into it
     if (warp == 1) {
         tc_fence_after_sync();
-        tmem_dealloc(tmem, kColumns);
+        pair_dealloc<CG>(tmem, kColumns);
     }
 }
 
@@ -535,17 +749,26 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
 struct Schedule {
     std::vector<Tile> tiles;
     std::vector<int32_t> first;
-    int bn = 0;
+    int cg = 1;
     int64_t longest = 0;
     int64_t o_tiles = 0, o_first = 0;   // in the plan's memory
-    int32_t ctas() const { return int32_t(first.size()) - 1; }
+    int32_t units() const { return int32_t(first.size()) - 1; }
 };
 
-// A tile costs its depth (in stages), for the width of its columns and for what a
-// stage and a tile cost at any width.
-int64_t tile_cost(int64_t depth, int bn) { return (depth + kBK - 1) / kBK * (bn + 32) + 6 * (bn + 32); }
+// The forms of a product: tiles of 256 x 256 by pairs of CTAs, or of 128 x 128 by one.
+struct Form {
+    int bm, bn, cg;
+};
+constexpr Form kPairs = {256, 256, 2}, kSingles = {128, 128, 1};
 
-Schedule make_schedule(const std::vector<Matrix> &all, Op op, int bn, int ctas) {
+// Clocks of a tile, about: a stage by what it moves through shared memory and the
+// products that it feeds (measured), and what a tile waits for at its ends.
+int64_t tile_cost(int64_t depth, bool three, int cg) {
+    const int64_t stages = (depth + kBK - 1) / kBK;
+    return cg == 2 ? stages * (three ? 1600 : 560) + 5000 : stages * (three ? 1350 : 600) + 3500;
+}
+
+Schedule make_schedule(const std::vector<Matrix> &all, Op op, const Form &form, bool three, int units) {
     struct Item {
         int64_t cost;
         Tile tile;
@@ -555,19 +778,19 @@ Schedule make_schedule(const std::vector<Matrix> &all, Op op, int bn, int ctas) 
         const Matrix &x = all[t];
         if (x.n == 0) continue;
         const int rows = op == kApply ? x.rows : x.n, cols = op == kApply ? x.cols : x.n;
-        const int64_t depth = op == kGram ? std::max(x.rows, x.cols) : x.n, cost = tile_cost(depth, bn);
-        for (int col = 0; col < cols; col += bn)
-            for (int row = 0; row < rows; row += kBM)
-                if (op == kApply || col < row + kBM) items.push_back({cost, {int32_t(t), row, col}});
+        const int64_t depth = op == kGram ? std::max(x.rows, x.cols) : x.n, cost = tile_cost(depth, three, form.cg);
+        for (int col = 0; col < cols; col += form.bn)
+            for (int row = 0; row < rows; row += form.bm)
+                if (op == kApply || col < row + form.bm) items.push_back({cost, {int32_t(t), row, col}});
     }
     std::stable_sort(items.begin(), items.end(), [](const Item &a, const Item &b) { return a.cost > b.cost; });
     Schedule s;
-    s.bn = bn;
-    ctas = int(std::min<int64_t>(ctas, int64_t(items.size())));
-    std::vector<std::vector<Tile>> mine(ctas);
+    s.cg = form.cg;
+    units = int(std::min<int64_t>(units, int64_t(items.size())));
+    std::vector<std::vector<Tile>> mine(units);
     using Load = std::pair<int64_t, int>;
     std::priority_queue<Load, std::vector<Load>, std::greater<Load>> queue;
-    for (int c = 0; c < ctas; ++c) queue.push({0, c});
+    for (int c = 0; c < units; ++c) queue.push({0, c});
     for (const Item &i : items) {
         Load l = queue.top();
         queue.pop();
@@ -584,21 +807,28 @@ Schedule make_schedule(const std::vector<Matrix> &all, Op op, int bn, int ctas) 
     return s;
 }
 
-template <int P, int BN, int OP>
-cudaError_t launch_product(const StepArgs &s, const Tile *tiles, const int32_t *first, int ctas, int buf, bool last, cudaStream_t stream) {
-    const auto kernel = product_kernel<P, BN, OP>;
-    const cudaError_t e = allow_smem(kernel, Geo<P, BN>::kSmem);
+template <int P, int BN, int CG, int OP>
+cudaError_t launch_product(const StepArgs &s, const Schedule &sch, const char *memory, int buf, bool last, cudaStream_t stream) {
+    const auto kernel = product_kernel<P, BN, CG, OP>;
+    constexpr size_t smem = Geo<P, BN, CG>::kSmem;
+    const cudaError_t e = allow_smem(kernel, smem);
     if (e != cudaSuccess) return e;
-    return launch_ex(kernel, dim3(unsigned(ctas)), dim3(kGemmThreads), Geo<P, BN>::kSmem, stream, 1, true, s, tiles, first, buf, int(last));
+    return launch_ex(kernel, dim3(unsigned(CG * sch.units())), dim3(kGemmThreads), smem, stream, CG, true, s, reinterpret_cast<const Tile *>(memory + sch.o_tiles),
+                     reinterpret_cast<const int32_t *>(memory + sch.o_first), buf, int(last));
 }
 template <int OP>
 cudaError_t launch_product(const StepArgs &s, const Schedule &sch, const char *memory, bool three, int buf, bool last, cudaStream_t stream) {
-    const Tile *tiles = reinterpret_cast<const Tile *>(memory + sch.o_tiles);
-    const int32_t *first = reinterpret_cast<const int32_t *>(memory + sch.o_first);
-    const int ctas = sch.ctas();
-    if (sch.bn == 256)
-        return three ? launch_product<3, 256, OP>(s, tiles, first, ctas, buf, last, stream) : launch_product<1, 256, OP>(s, tiles, first, ctas, buf, last, stream);
-    return three ? launch_product<3, 128, OP>(s, tiles, first, ctas, buf, last, stream) : launch_product<1, 128, OP>(s, tiles, first, ctas, buf, last, stream);
+    if (sch.cg == 2) return three ? launch_product<3, 256, 2, OP>(s, sch, memory, buf, last, stream) : launch_product<1, 256, 2, OP>(s, sch, memory, buf, last, stream);
+    return three ? launch_product<3, 128, 1, OP>(s, sch, memory, buf, last, stream) : launch_product<1, 128, 1, OP>(s, sch, memory, buf, last, stream);
+}
+
+// Pairs of CTAs that the device holds at a time.
+int pair_room(bool three) {
+    const auto kernel1 = product_kernel<1, 256, 2, kApply>;
+    const auto kernel3 = product_kernel<3, 256, 2, kApply>;
+    const size_t smem = three ? Geo<3, 256, 2>::kSmem : Geo<1, 256, 2>::kSmem;
+    if ((three ? allow_smem(kernel3, smem) : allow_smem(kernel1, smem)) != cudaSuccess) return 1;
+    return cluster_room(three ? kernel3 : kernel1, kGemmThreads, smem).of[1];
 }
 
 bool encode_map(CUtensorMap &map, const void *base, int64_t rows, int64_t cols, int64_t ld) {
@@ -676,6 +906,10 @@ darb_status_t build_plan(darb_muon_s *plan, int32_t n, const int64_t *rows, cons
         x.parts = int32_t((e + x.part_elems - 1) / x.part_elems);
         x.ldx = (x.cols + 63) / 64 * 64;
         x.lda = (x.n + 63) / 64 * 64;
+        int bits = 0;
+        while ((int64_t(1) << bits) < x.cols) ++bits;
+        x.shift = 31 + bits;
+        x.reciprocal = ((uint64_t(1) << x.shift) + x.cols - 1) / x.cols;
         x.size = float(0.2 * std::sqrt(double(std::max(x.rows, x.cols))));
         for (int32_t p = 0; p < x.parts; ++p) parts.push_back({i, p});
     }
@@ -683,10 +917,11 @@ darb_status_t build_plan(darb_muon_s *plan, int32_t n, const int64_t *rows, cons
     if (parts.empty()) return DARB_OK;
     const char *fail = std::getenv("DARB_FAIL_ALLOC");   // test hook, as for the library's other allocations
     if (fail != nullptr && fail[0] == '1') return DARB_ERR_OOM;
-    const int sms = sm_count();
+    const bool three = plan->gtype == DARB_F32;
+    const int sms = sm_count(), pairs = pair_room(three);
     for (int op = kGram; op <= kApply; ++op) {
-        // the width whose busiest CTA has least to do
-        Schedule wide = make_schedule(plan->matrices, Op(op), 256, sms), narrow = make_schedule(plan->matrices, Op(op), 128, sms);
+        // the form whose busiest CTA has least to do
+        Schedule wide = make_schedule(plan->matrices, Op(op), kPairs, three, pairs), narrow = make_schedule(plan->matrices, Op(op), kSingles, three, sms);
         plan->schedules[op] = wide.longest <= narrow.longest ? std::move(wide) : std::move(narrow);
     }
     // the tables, then the numbers of every matrix
