@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kElemThreads) start_kernel(const StepArgs a, c
 
 // ---- products ----
 
-enum Op : int { kGram, kSquare, kApply };
+enum Op : int { kGram, kSquare, kApply, kLast };   // kLast: the last kApply, which updates the parameters
 
 // Instruction descriptor of tcgen05.mma kind::f16 with fp16 A and B and an fp32
 // accumulator.
@@ -401,28 +401,82 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 &hi, uint4 &lo
     hi = make_uint4(h[0], h[1], h[2], h[3]), lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
+// What the writing of a product needs to know of a matrix, in registers: after a store
+// whatever lies in memory would have to be read again.
+struct Target {
+    const __half *in_hi, *in_lo;   // A or X
+    __half *out_hi, *out_lo;       // A, B or X
+    const float *row, *col;        // the diagonal by rows and by columns, or null
+    float *diagonal;               // of the result, or null
+    float *p;
+    __nv_bfloat16 *copy;
+    int32_t rows, cols, ld;
+    float size;
+    bool vector;                   // parameters eight at a time
+};
+template <int OP>
+__device__ __forceinline__ Target target(const StepArgs &s, const Matrix &x, int buf) {
+    Target t = {};
+    if (OP == kGram || OP == kSquare) {
+        t.in_hi = x.ap[0], t.in_lo = x.ap[1];
+        t.out_hi = OP == kGram ? x.ap[0] : x.bp[0], t.out_lo = OP == kGram ? x.ap[1] : x.bp[1];
+        if (OP == kSquare) t.row = t.col = x.d;
+        t.diagonal = OP == kGram ? x.d : x.D;
+        t.rows = t.cols = x.n, t.ld = x.lda;
+        return t;
+    }
+    t.in_hi = x.xp[buf][0], t.in_lo = x.xp[buf][1], t.out_hi = x.xp[buf ^ 1][0], t.out_lo = x.xp[buf ^ 1][1];
+    if (x.tall) t.col = x.D;
+    else t.row = x.D;
+    t.rows = x.rows, t.cols = x.cols, t.ld = x.ldx;
+    t.p = x.p, t.copy = x.copy, t.size = s.lr * x.size;
+    t.vector = x.cols % 8 == 0 && aligned16(x.p) && aligned16(x.copy);
+    return t;
+}
+
 // What becomes of rows i0 .. i0 + 32 and columns j0 .. j0 + 64 of a product, `acc` being
 // the accumulator's address.
 template <int P, int OP>
-__device__ __forceinline__ void finish(const StepArgs &s, const Matrix &x, int buf, bool last, int i0, int j0, uint32_t acc, const Turn &turn) {
-    constexpr bool two = P == 3;
+__device__ __forceinline__ void finish(const float decay, const Target &x, int i0, int j0, uint32_t acc, const Turn &turn) {
+    constexpr bool two = P == 3, apply = OP == kApply || OP == kLast;
     const int lane = threadIdx.x & 31, oct = lane & 7, sub = lane >> 3;
-    const int rows = OP == kApply ? x.rows : x.n, cols = OP == kApply ? x.cols : x.n;
-    if (i0 >= rows || j0 >= cols || (OP != kApply && j0 > i0 + 31)) return;
-    const int ld = OP == kApply ? x.ldx : x.lda;
-    const int j = j0 + 8 * oct;                            // this lane's columns after the turn
-    const bool inside = j < ld;                            // (rows are as long as a multiple of 64 numbers)
-    const __half *const in_hi = OP == kApply ? x.xp[buf][0] : x.ap[0], *const in_lo = OP == kApply ? x.xp[buf][1] : x.ap[1];
+    const int rows = x.rows, cols = x.cols, ld = x.ld;
+    if (i0 >= rows || j0 >= cols || (!apply && j0 > i0 + 31)) return;
+    const int j = j0 + 8 * oct;   // this lane's columns after the turn (rows are as long as a multiple of 64 numbers)
+    // All loads come before the first store: none can be moved over a store that might
+    // meet it, and waiting for each in turn would take longer than the product.
     uint4 hi[8], lo[8];
+    float di[8], dj[8];              // of the diagonal: of this lane's rows, of its columns
+    float p[OP == kLast ? 64 : 1];   // parameters: of this lane's rows and columns, or (unaligned) of columns lane and lane + 32
     if (OP != kGram) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const int i = i0 + 4 * q + sub;
-            if (i >= rows || !inside) continue;
-            const int64_t at = int64_t(i) * ld + j;
-            hi[q] = *reinterpret_cast<const uint4 *>(in_hi + at);
-            if (OP == kApply || two) lo[q] = *reinterpret_cast<const uint4 *>(in_lo + at);
+            const int i = min(i0 + 4 * q + sub, rows - 1);
+            hi[q] = *reinterpret_cast<const uint4 *>(x.in_hi + int64_t(i) * ld + j);
+            if (apply || two) lo[q] = *reinterpret_cast<const uint4 *>(x.in_lo + int64_t(i) * ld + j);
         }
+        if (x.row != nullptr) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) di[q] = x.row[min(i0 + 4 * q + sub, rows - 1)];
+        }
+        if (x.col != nullptr) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dj[e] = x.col[min(j + e, cols - 1)];
+        }
+    }
+    if (OP == kLast && x.vector) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const float4 *from = reinterpret_cast<const float4 *>(x.p + int64_t(min(i0 + 4 * q + sub, rows - 1)) * cols + min(j, cols - 8));
+            const float4 p0 = from[0], p1 = from[1];
+            float *const to = p + (OP == kLast ? 8 * q : 0);
+            to[0] = p0.x, to[1] = p0.y, to[2] = p0.z, to[3] = p0.w, to[4] = p1.x, to[5] = p1.y, to[6] = p1.z, to[7] = p1.w;
+        }
+    } else if (OP == kLast) {
+#pragma unroll
+        for (int r = 0; r < 32; ++r)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) p[OP == kLast ? 2 * r + c : 0] = x.p[int64_t(min(i0 + r, rows - 1)) * cols + min(j0 + 32 * c + lane, cols - 1)];
     }
     uint32_t v[32];
 #pragma unroll
@@ -433,51 +487,44 @@ __device__ __forceinline__ void finish(const StepArgs &s, const Matrix &x, int b
     }
     __syncwarp();
 
-    if (OP != kApply) {
-        __half *const out_hi = OP == kGram ? x.ap[0] : x.bp[0], *const out_lo = OP == kGram ? x.ap[1] : x.bp[1];
-        float dj[8];
-        if (OP == kSquare) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dj[e] = j + e < cols ? x.d[j + e] : 0.0f;
-        }
+    if (!apply) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             const int i = i0 + 4 * q + sub;
             float r[8], w[8];
             turn.get(4 * q + sub, oct, r);
-            if (i < rows && inside) {
+            if (i < rows) {
                 if (OP == kSquare) {
-                    const float di = x.d[i];
                     float old[8], more[8];
                     halves(hi[q], old);
                     if (two) halves(lo[q], more);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float sq = r[e] * (1.0f / (kScaleX * kScaleX)), A = (two ? old[e] + more[e] : old[e]) * (1.0f / kScaleX);
-                        w[e] = (kB * A + kC * fmaf(di + dj[e], A, sq)) * kScaleB;
-                        if (j + e == i) x.D[i] = kA + kB * di + kC * fmaf(di, di, sq);
+                        w[e] = (kB * A + kC * fmaf(di[q] + dj[e], A, sq)) * kScaleB;
+                        if (j + e == i) x.diagonal[i] = kA + kB * di[q] + kC * fmaf(di[q], di[q], sq);
                     }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         w[e] = r[e] * (1.0f / kScaleX);
-                        if (j + e == i) x.d[i] = r[e] * (1.0f / (kScaleX * kScaleX));
+                        if (j + e == i) x.diagonal[i] = r[e] * (1.0f / (kScaleX * kScaleX));
                     }
                 }
                 uint4 h, l;
                 split8(w, h, l);
                 const int64_t at = int64_t(i) * ld + j;
                 if (j + 8 <= i) {
-                    *reinterpret_cast<uint4 *>(out_hi + at) = h;
-                    if (two) *reinterpret_cast<uint4 *>(out_lo + at) = l;
+                    *reinterpret_cast<uint4 *>(x.out_hi + at) = h;
+                    if (two) *reinterpret_cast<uint4 *>(x.out_lo + at) = l;
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         if (j + e >= i) continue;
                         __half a, b;
                         split(w[e], a, b);
-                        out_hi[at + e] = a;
-                        if (two) out_lo[at + e] = b;
+                        x.out_hi[at + e] = a;
+                        if (two) x.out_lo[at + e] = b;
                     }
                 }
             } else {
@@ -499,16 +546,16 @@ __device__ __forceinline__ void finish(const StepArgs &s, const Matrix &x, int b
             const __half2 l = __floats2half2_rn(v0 - f.x, v1 - f.y);
             const int64_t at = int64_t(jj) * ld + i;
             if (jj < i && i + 1 < rows) {
-                *reinterpret_cast<__half2 *>(out_hi + at) = h;
-                if (two) *reinterpret_cast<__half2 *>(out_lo + at) = l;
+                *reinterpret_cast<__half2 *>(x.out_hi + at) = h;
+                if (two) *reinterpret_cast<__half2 *>(x.out_lo + at) = l;
             } else {
                 if (jj < i) {
-                    out_hi[at] = __low2half(h);
-                    if (two) out_lo[at] = __low2half(l);
+                    x.out_hi[at] = __low2half(h);
+                    if (two) x.out_lo[at] = __low2half(l);
                 }
                 if (jj < i + 1 && i + 1 < rows) {
-                    out_hi[at + 1] = __high2half(h);
-                    if (two) out_lo[at + 1] = __high2half(l);
+                    x.out_hi[at + 1] = __high2half(h);
+                    if (two) x.out_lo[at + 1] = __high2half(l);
                 }
             }
         }
@@ -516,60 +563,49 @@ __device__ __forceinline__ void finish(const StepArgs &s, const Matrix &x, int b
         return;
     }
 
-    float dj[8];
-    if (x.tall) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dj[e] = j + e < cols ? x.D[j + e] : 0.0f;
-    }
-    const float size = s.lr * x.size;
-    const bool vector = x.cols % 8 == 0 && aligned16(x.p) && aligned16(x.copy);
+    const bool by_col = x.col != nullptr;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
         const int i = i0 + 4 * q + sub;
-        if (i >= rows || !inside) continue;
+        if (i >= rows) continue;
         float r[8], a[8], b[8];
         turn.get(4 * q + sub, oct, r);
         halves(hi[q], a);
         halves(lo[q], b);
-        const float di = x.tall ? 0.0f : x.D[i];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            r[e] = fmaf(x.tall ? dj[e] : di, (a[e] + b[e]) * (1.0f / kScaleX), r[e] * (1.0f / (kScaleX * kScaleB)));
-        if (!last) {
+            r[e] = fmaf(by_col ? dj[e] : di[q], (a[e] + b[e]) * (1.0f / kScaleX), r[e] * (1.0f / (kScaleX * kScaleB)));
+        if (OP == kApply) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) r[e] *= kScaleX;
             uint4 h, l;
             split8(r, h, l);
             const int64_t at = int64_t(i) * ld + j;
-            *reinterpret_cast<uint4 *>(x.xp[buf ^ 1][0] + at) = h;
-            *reinterpret_cast<uint4 *>(x.xp[buf ^ 1][1] + at) = l;
-        } else if (!vector) {
+            *reinterpret_cast<uint4 *>(x.out_hi + at) = h;
+            *reinterpret_cast<uint4 *>(x.out_lo + at) = l;
+        } else if (!x.vector) {
             turn.set(4 * q + sub, oct, r);
         } else if (j < cols) {
-            const int64_t at = int64_t(i) * x.cols + j;
-            float4 p0 = reinterpret_cast<const float4 *>(x.p + at)[0], p1 = reinterpret_cast<const float4 *>(x.p + at)[1];
-            p0 = make_float4(p0.x * s.decay - size * r[0], p0.y * s.decay - size * r[1], p0.z * s.decay - size * r[2], p0.w * s.decay - size * r[3]);
-            p1 = make_float4(p1.x * s.decay - size * r[4], p1.y * s.decay - size * r[5], p1.z * s.decay - size * r[6], p1.w * s.decay - size * r[7]);
-            reinterpret_cast<float4 *>(x.p + at)[0] = p0;
-            reinterpret_cast<float4 *>(x.p + at)[1] = p1;
-            if (x.copy != nullptr) {
-                const float c[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
-                *reinterpret_cast<uint4 *>(x.copy + at) = pack(c);
-            }
+            const int64_t at = int64_t(i) * cols + j;
+            float c[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c[e] = p[OP == kLast ? 8 * q + e : 0] * decay - x.size * r[e];
+            reinterpret_cast<float4 *>(x.p + at)[0] = make_float4(c[0], c[1], c[2], c[3]);
+            reinterpret_cast<float4 *>(x.p + at)[1] = make_float4(c[4], c[5], c[6], c[7]);
+            if (x.copy != nullptr) *reinterpret_cast<uint4 *>(x.copy + at) = pack(c);
         }
     }
     __syncwarp();
-    if (last && !vector) {
-#pragma unroll 4
-        for (int r = 0; r < 32; ++r) {
-            if (i0 + r >= rows) break;
+    if (OP == kLast && !x.vector) {
 #pragma unroll
-            for (int c = lane; c < 64; c += 32) {
-                if (j0 + c >= cols) continue;
-                const int64_t at = int64_t(i0 + r) * x.cols + j0 + c;
-                const float p = x.p[at] * s.decay - size * turn.one(r, c);
-                x.p[at] = p;
-                if (x.copy != nullptr) x.copy[at] = __float2bfloat16_rn(p);
+        for (int r = 0; r < 32; ++r) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                if (i0 + r >= rows || j0 + 32 * c + lane >= cols) continue;
+                const int64_t at = int64_t(i0 + r) * cols + j0 + 32 * c + lane;
+                const float v = p[OP == kLast ? 2 * r + c : 0] * decay - x.size * turn.one(r, 32 * c + lane);
+                x.p[at] = v;
+                if (x.copy != nullptr) x.copy[at] = __float2bfloat16_rn(v);
             }
         }
         __syncwarp();
@@ -583,7 +619,7 @@ __device__ __forceinline__ void acquire_map(const CUtensorMap *map) {
 
 // The tiles of CTA (or pair) b are tiles[first[b]] .. tiles[first[b + 1] - 1].
 template <int P, int BN, int CG, int OP>
-__global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs s, const Tile *tiles, const int32_t *first, int buf, int last) {
+__global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs s, const Tile *tiles, const int32_t *first, int buf) {
     using G = Geo<P, BN, CG>;
     constexpr int NS = G::kStages, NP = G::kParts;
     extern __shared__ unsigned char sm_raw[];
@@ -721,8 +757,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
             tc_fence_after_sync();
             const uint32_t at = tmem + half * BN + (uint32_t(quarter * 32) << 16);
             const int i0 = tile.row + rank * kBM + quarter * 32;
+            const Target to = target<OP>(s, x, buf);
 #pragma unroll 1
-            for (int c = 0; c < BN; c += 64) finish<P, OP>(s, x, buf, last != 0, i0, tile.col + c, at + c, turn);
+            for (int c = 0; c < BN; c += 64) finish<P, OP>(s.decay, to, i0, tile.col + c, at + c, turn);
             // the accumulator has been read
             tc_fence_before_sync();
             __syncwarp();
@@ -808,18 +845,18 @@ Schedule make_schedule(const std::vector<Matrix> &all, Op op, const Form &form, 
 }
 
 template <int P, int BN, int CG, int OP>
-cudaError_t launch_product(const StepArgs &s, const Schedule &sch, const char *memory, int buf, bool last, cudaStream_t stream) {
+cudaError_t launch_product(const StepArgs &s, const Schedule &sch, const char *memory, int buf, cudaStream_t stream) {
     const auto kernel = product_kernel<P, BN, CG, OP>;
     constexpr size_t smem = Geo<P, BN, CG>::kSmem;
     const cudaError_t e = allow_smem(kernel, smem);
     if (e != cudaSuccess) return e;
     return launch_ex(kernel, dim3(unsigned(CG * sch.units())), dim3(kGemmThreads), smem, stream, CG, true, s, reinterpret_cast<const Tile *>(memory + sch.o_tiles),
-                     reinterpret_cast<const int32_t *>(memory + sch.o_first), buf, int(last));
+                     reinterpret_cast<const int32_t *>(memory + sch.o_first), buf);
 }
 template <int OP>
-cudaError_t launch_product(const StepArgs &s, const Schedule &sch, const char *memory, bool three, int buf, bool last, cudaStream_t stream) {
-    if (sch.cg == 2) return three ? launch_product<3, 256, 2, OP>(s, sch, memory, buf, last, stream) : launch_product<1, 256, 2, OP>(s, sch, memory, buf, last, stream);
-    return three ? launch_product<3, 128, 1, OP>(s, sch, memory, buf, last, stream) : launch_product<1, 128, 1, OP>(s, sch, memory, buf, last, stream);
+cudaError_t launch_product(const StepArgs &s, const Schedule &sch, const char *memory, bool three, int buf, cudaStream_t stream) {
+    if (sch.cg == 2) return three ? launch_product<3, 256, 2, OP>(s, sch, memory, buf, stream) : launch_product<1, 256, 2, OP>(s, sch, memory, buf, stream);
+    return three ? launch_product<3, 128, 1, OP>(s, sch, memory, buf, stream) : launch_product<1, 128, 1, OP>(s, sch, memory, buf, stream);
 }
 
 // Pairs of CTAs that the device holds at a time.
@@ -1015,10 +1052,11 @@ cudaError_t launch_step(const darb_muon_s &plan, StepArgs s, const void *const *
     const char *memory = static_cast<const char *>(plan.dmem);
     for (int k = 0; k < kIterations; ++k) {
         const int buf = k & 1;
-        const bool last = k == kIterations - 1;
-        cudaError_t e = launch_product<kGram>(s, plan.schedules[kGram], memory, three, buf, last, stream);
-        if (e == cudaSuccess) e = launch_product<kSquare>(s, plan.schedules[kSquare], memory, three, buf, last, stream);
-        if (e == cudaSuccess) e = launch_product<kApply>(s, plan.schedules[kApply], memory, three, buf, last, stream);
+        cudaError_t e = launch_product<kGram>(s, plan.schedules[kGram], memory, three, buf, stream);
+        if (e == cudaSuccess) e = launch_product<kSquare>(s, plan.schedules[kSquare], memory, three, buf, stream);
+        if (e == cudaSuccess)
+            e = k + 1 < kIterations ? launch_product<kApply>(s, plan.schedules[kApply], memory, three, buf, stream)
+                                    : launch_product<kLast>(s, plan.schedules[kApply], memory, three, buf, stream);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
