@@ -25,7 +25,7 @@
 // One launch a product for all matrices of the plan.  A CTA walks the tiles that the
 // plan's schedule gives it (longest first, to the CTA that is done first): one warp
 // copies boxes of 64 x 64 numbers (TMA, 128-byte swizzle), one issues tcgen05.mma
-// into one of two accumulators in tensor memory, four write the tile before.
+// into one of two accumulators in tensor memory, eight write the tile before.
 #include "launch.cuh"
 #include "tcgen05.cuh"
 #include "tma.cuh"
@@ -61,7 +61,8 @@ constexpr int64_t kMaxSide = 32768;         // rows and columns: elements fit 32
 
 constexpr int kBM = 128, kBK = 64;          // rows of a tile; depth of a stage
 constexpr int kBox = 64 * 64 * 2;           // bytes of a box
-constexpr int kGemmThreads = 192;           // copies, products, four warps that write
+constexpr int kWriters = 8;                  // warps that write a product
+constexpr int kGemmThreads = 32 * (2 + kWriters);   // copies, products, writing
 constexpr float kScaleX = 32768.0f, kScaleB = 16384.0f;
 
 // One matrix of a plan.
@@ -274,7 +275,7 @@ struct Geo {
     static constexpr int kParts = P == 1 ? 1 : 2;                 // fp16 numbers of an operand
     static constexpr int kABytes = kBM / 64 * kBox, kBBytes = BN / CG / 64 * kBox;
     static constexpr int kStage = kParts * (kABytes + kBBytes);
-    static constexpr int kTurn = 4 * 32 * 64 * 4;                 // 32 rows x 64 columns of each writing warp
+    static constexpr int kTurn = kWriters * 32 * 32 * 4;          // 32 rows x 32 columns of each writing warp
     static constexpr int kFit = (227 * 1024 - 2048 - kTurn) / kStage;
     static constexpr int kStages = kFit < 6 ? kFit : 6;
     static constexpr size_t kSmem = 2048 + size_t(kStages) * kStage + kTurn;
@@ -354,29 +355,29 @@ __device__ __forceinline__ Operands operands(const Matrix &x, int buf) {
     return x.tall ? Operands{x.x[buf], x.b, false, false, x.n} : Operands{x.b, x.x[buf], false, true, x.n};
 }
 
-// A warp has 32 rows x 64 columns of a product as 64 numbers of a row in each lane; it
-// turns them through shared memory, so that eight lanes share a row, eight neighbouring
-// columns each, and 4 rows of 128 bytes of fp16 are read or written at once.  The 16
+// A warp has 32 rows x 32 columns of a product as the numbers of a row in each lane; it
+// turns them through shared memory, so that four lanes share a row, eight neighbouring
+// columns each, and 8 rows of 64 bytes of fp16 are read or written at once.  The 16
 // bytes c of row r stand at c ^ (r % 8).
 struct Turn {
-    float4 *at;   // 32 x 16
+    float4 *at;   // 32 x 8
 
-    __device__ __forceinline__ void put(int lane, int c0, const uint32_t (&v)[32]) const {
+    __device__ __forceinline__ void put(int lane, const uint32_t (&v)[32]) const {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            at[lane * 16 + ((c0 + i) ^ (lane & 7))] =
+            at[lane * 8 + (i ^ (lane & 7))] =
                 make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
     }
     __device__ __forceinline__ void get(int row, int oct, float (&v)[8]) const {
-        const float4 x = at[row * 16 + ((2 * oct) ^ (row & 7))], y = at[row * 16 + ((2 * oct + 1) ^ (row & 7))];
+        const float4 x = at[row * 8 + ((2 * oct) ^ (row & 7))], y = at[row * 8 + ((2 * oct + 1) ^ (row & 7))];
         v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
     }
     __device__ __forceinline__ void set(int row, int oct, const float (&v)[8]) const {
-        at[row * 16 + ((2 * oct) ^ (row & 7))] = make_float4(v[0], v[1], v[2], v[3]);
-        at[row * 16 + ((2 * oct + 1) ^ (row & 7))] = make_float4(v[4], v[5], v[6], v[7]);
+        at[row * 8 + ((2 * oct) ^ (row & 7))] = make_float4(v[0], v[1], v[2], v[3]);
+        at[row * 8 + ((2 * oct + 1) ^ (row & 7))] = make_float4(v[4], v[5], v[6], v[7]);
     }
     __device__ __forceinline__ float one(int row, int col) const {
-        return reinterpret_cast<const float *>(&at[row * 16 + ((col >> 2) ^ (row & 7))])[col & 3];
+        return reinterpret_cast<const float *>(&at[row * 8 + ((col >> 2) ^ (row & 7))])[col & 3];
     }
 };
 
@@ -434,30 +435,30 @@ __device__ __forceinline__ Target target(const StepArgs &s, const Matrix &x, int
     return t;
 }
 
-// What becomes of rows i0 .. i0 + 32 and columns j0 .. j0 + 64 of a product, `acc` being
+// What becomes of rows i0 .. i0 + 32 and columns j0 .. j0 + 32 of a product, `acc` being
 // the accumulator's address.
 template <int P, int OP>
 __device__ __forceinline__ void finish(const float decay, const Target &x, int i0, int j0, uint32_t acc, const Turn &turn) {
     constexpr bool two = P == 3, apply = OP == kApply || OP == kLast;
-    const int lane = threadIdx.x & 31, oct = lane & 7, sub = lane >> 3;
+    const int lane = threadIdx.x & 31, oct = lane & 3, sub = lane >> 2;
     const int rows = x.rows, cols = x.cols, ld = x.ld;
     if (i0 >= rows || j0 >= cols || (!apply && j0 > i0 + 31)) return;
     const int j = j0 + 8 * oct;   // this lane's columns after the turn (rows are as long as a multiple of 64 numbers)
     // All loads come before the first store: none can be moved over a store that might
     // meet it, and waiting for each in turn would take longer than the product.
-    uint4 hi[8], lo[8];
-    float di[8], dj[8];              // of the diagonal: of this lane's rows, of its columns
-    float p[OP == kLast ? 64 : 1];   // parameters: of this lane's rows and columns, or (unaligned) of columns lane and lane + 32
+    uint4 hi[4], lo[4];
+    float di[4], dj[8];              // of the diagonal: of this lane's rows, of its columns
+    float p[OP == kLast ? 32 : 1];   // parameters: of this lane's rows and columns, or (unaligned) of column `lane`
     if (OP != kGram) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const int i = min(i0 + 4 * q + sub, rows - 1);
+        for (int q = 0; q < 4; ++q) {
+            const int i = min(i0 + 8 * q + sub, rows - 1);
             hi[q] = *reinterpret_cast<const uint4 *>(x.in_hi + int64_t(i) * ld + j);
             if (apply || two) lo[q] = *reinterpret_cast<const uint4 *>(x.in_lo + int64_t(i) * ld + j);
         }
         if (x.row != nullptr) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) di[q] = x.row[min(i0 + 4 * q + sub, rows - 1)];
+            for (int q = 0; q < 4; ++q) di[q] = x.row[min(i0 + 8 * q + sub, rows - 1)];
         }
         if (x.col != nullptr) {
 #pragma unroll
@@ -466,33 +467,28 @@ __device__ __forceinline__ void finish(const float decay, const Target &x, int i
     }
     if (OP == kLast && x.vector) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const float4 *from = reinterpret_cast<const float4 *>(x.p + int64_t(min(i0 + 4 * q + sub, rows - 1)) * cols + min(j, cols - 8));
+        for (int q = 0; q < 4; ++q) {
+            const float4 *from = reinterpret_cast<const float4 *>(x.p + int64_t(min(i0 + 8 * q + sub, rows - 1)) * cols + min(j, cols - 8));
             const float4 p0 = from[0], p1 = from[1];
             float *const to = p + (OP == kLast ? 8 * q : 0);
             to[0] = p0.x, to[1] = p0.y, to[2] = p0.z, to[3] = p0.w, to[4] = p1.x, to[5] = p1.y, to[6] = p1.z, to[7] = p1.w;
         }
     } else if (OP == kLast) {
 #pragma unroll
-        for (int r = 0; r < 32; ++r)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) p[OP == kLast ? 2 * r + c : 0] = x.p[int64_t(min(i0 + r, rows - 1)) * cols + min(j0 + 32 * c + lane, cols - 1)];
+        for (int r = 0; r < 32; ++r) p[OP == kLast ? r : 0] = x.p[int64_t(min(i0 + r, rows - 1)) * cols + min(j0 + lane, cols - 1)];
     }
     uint32_t v[32];
-#pragma unroll
-    for (int c = 0; c < 64; c += 32) {
-        tmem_ld32(acc + c, v);
-        tmem_ld_wait();
-        turn.put(lane, c / 4, v);
-    }
+    tmem_ld32(acc, v);
+    tmem_ld_wait();
+    turn.put(lane, v);
     __syncwarp();
 
     if (!apply) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const int i = i0 + 4 * q + sub;
+        for (int q = 0; q < 4; ++q) {
+            const int i = i0 + 8 * q + sub;
             float r[8], w[8];
-            turn.get(4 * q + sub, oct, r);
+            turn.get(8 * q + sub, oct, r);
             if (i < rows) {
                 if (OP == kSquare) {
                     float old[8], more[8];
@@ -531,13 +527,13 @@ __device__ __forceinline__ void finish(const float decay, const Target &x, int i
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[e] = 0.0f;
             }
-            turn.set(4 * q + sub, oct, w);
+            turn.set(8 * q + sub, oct, w);
         }
         __syncwarp();
         // across the diagonal: a lane has two rows of half of the columns
         const int i = i0 + 2 * (lane & 15);
 #pragma unroll 4
-        for (int c = lane >> 4; c < 64; c += 2) {
+        for (int c = lane >> 4; c < 32; c += 2) {
             const int jj = j0 + c;
             if (jj >= cols || i >= rows || jj > i) continue;
             const float v0 = turn.one(2 * (lane & 15), c), v1 = turn.one(2 * (lane & 15) + 1, c);
@@ -565,11 +561,11 @@ __device__ __forceinline__ void finish(const float decay, const Target &x, int i
 
     const bool by_col = x.col != nullptr;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        const int i = i0 + 4 * q + sub;
+    for (int q = 0; q < 4; ++q) {
+        const int i = i0 + 8 * q + sub;
         if (i >= rows) continue;
         float r[8], a[8], b[8];
-        turn.get(4 * q + sub, oct, r);
+        turn.get(8 * q + sub, oct, r);
         halves(hi[q], a);
         halves(lo[q], b);
 #pragma unroll
@@ -584,7 +580,7 @@ __device__ __forceinline__ void finish(const float decay, const Target &x, int i
             *reinterpret_cast<uint4 *>(x.out_hi + at) = h;
             *reinterpret_cast<uint4 *>(x.out_lo + at) = l;
         } else if (!x.vector) {
-            turn.set(4 * q + sub, oct, r);
+            turn.set(8 * q + sub, oct, r);
         } else if (j < cols) {
             const int64_t at = int64_t(i) * cols + j;
             float c[8];
@@ -599,14 +595,11 @@ __device__ __forceinline__ void finish(const float decay, const Target &x, int i
     if (OP == kLast && !x.vector) {
 #pragma unroll
         for (int r = 0; r < 32; ++r) {
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                if (i0 + r >= rows || j0 + 32 * c + lane >= cols) continue;
-                const int64_t at = int64_t(i0 + r) * cols + j0 + 32 * c + lane;
-                const float v = p[OP == kLast ? 2 * r + c : 0] * decay - x.size * turn.one(r, 32 * c + lane);
-                x.p[at] = v;
-                if (x.copy != nullptr) x.copy[at] = __float2bfloat16_rn(v);
-            }
+            if (i0 + r >= rows || j0 + lane >= cols) continue;
+            const int64_t at = int64_t(i0 + r) * cols + j0 + lane;
+            const float v = p[OP == kLast ? r : 0] * decay - x.size * turn.one(r, lane);
+            x.p[at] = v;
+            if (x.copy != nullptr) x.copy[at] = __float2bfloat16_rn(v);
         }
         __syncwarp();
     }
@@ -635,7 +628,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
     pdl_launch_dependents();
     if (tid == 0) {
         for (int i = 0; i < NS; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-        for (int i = 0; i < 2; ++i) mbar_init(&ready[i], 1), mbar_init(&read[i], 4 * CG);
+        for (int i = 0; i < 2; ++i) mbar_init(&ready[i], 1), mbar_init(&read[i], kWriters * CG);
         mbar_init(done, 1);
         fence_mbar_init();
     }
@@ -742,8 +735,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
         if (lane == 0 && !mbar_wait(done, 0)) ok = false;
         __syncwarp();
     } else {
-        const int quarter = warp & 3;
-        const Turn turn = {reinterpret_cast<float4 *>(stages + NS * G::kStage) + quarter * (32 * 16)};
+        // two warps for each quarter of the accumulator's rows, with half of the columns each
+        const int quarter = warp & 3, c0 = warp < 6 ? 0 : BN / 2;
+        const Turn turn = {reinterpret_cast<float4 *>(stages + NS * G::kStage) + (warp - 2) * (32 * 8)};
         int used = 0;
         for (int t = t0; t < t1; ++t) {
             const Tile tile = tiles[t];
@@ -759,7 +753,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
             const int i0 = tile.row + rank * kBM + quarter * 32;
             const Target to = target<OP>(s, x, buf);
 #pragma unroll 1
-            for (int c = 0; c < BN; c += 64) finish<P, OP>(s.decay, to, i0, tile.col + c, at + c, turn);
+            for (int c = c0; c < c0 + BN / 2; c += 32) finish<P, OP>(s.decay, to, i0, tile.col + c, at + c, turn);
             // the accumulator has been read
             tc_fence_before_sync();
             __syncwarp();
