@@ -41,21 +41,23 @@ cudaError_t stream_alloc(void **p, size_t bytes, cudaStream_t stream);
 namespace {
 
 constexpr int kE = 8;                       // tokens of a thread
-constexpr int kFew = 4096;                  // tokens of the single CTA
+constexpr int kFew = 4096, kVeryFew = 1024;  // tokens of a single CTA of 512 or 128 threads
 constexpr int kChunkThreads = 256;
 constexpr int kChunkTokens = kChunkThreads * kE;
-constexpr int kInline = 8192;               // chunks and sequences that every CTA counts itself
+constexpr int kInline = 4096;               // chunks that every CTA adds up itself
 constexpr int kStats = 5;                   // loss, policy, kl, entropy, clipped
 constexpr int kSums = 4;                    // the sums that they come from
 constexpr int kOutside = -2, kNone = -1;    // in place of a sequence
+
+constexpr int kWhole = 1 << 30;             // a chunk that is all of one sequence that started before
 
 struct PolicyWork {
     double *slot_sum;     // per token: of the sequence that starts there, what its first chunk has of it
     double *head_sum;     // per chunk: of the sequence that started before it
     double *partial;      // per sum and chunk
-    int32_t *slot_count, *head_count;
-    int32_t *head_start;  // where that sequence started; -1: none
-    int32_t *count;       // per chunk: all of its tokens that count
+    int4 *info;           // per chunk: the tokens that count; sequences that start in it and have one of them; of the
+                          // sequence that started before it; of the one that goes on behind it (kWhole: the same one)
+    int32_t *slot_count;
     long long *norm;      // the tokens, or sequences, that count
     int32_t *ticket;
 };
@@ -100,6 +102,7 @@ struct ChunkShared {
     int scan_count[THREADS / 32], scan_flag[THREADS / 32];
     int last;            // where the last sequence of the chunk starts
     int64_t before;      // where the sequence of the first token starts
+    int64_t after;       // where the last one ends
 };
 
 // Which sequences start where in the chunk at c0; where the last one starts before
@@ -108,6 +111,7 @@ template <int THREADS>
 __device__ __forceinline__ int find_sequences(const PolicyArgs &a, int64_t c0, ChunkShared<THREADS> &sh) {
     constexpr int T = THREADS * kE;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+#pragma unroll
     for (int p = tid; p < T; p += THREADS) sh.start[p] = kNone;
     const int64_t s0 = offsets_upto<THREADS>(a.offsets, a.sequences, c0) - 1;   // (its barriers order the writes above)
     if (tid == 0) {
@@ -123,7 +127,11 @@ __device__ __forceinline__ int find_sequences(const PolicyArgs &a, int64_t c0, C
             if (s == a.sequences) sh.start[at] = kOutside;
             else if (a.offsets[s + 1] - c0 > at) sh.start[at] = int(s);
         }
-        if (__syncthreads_count(in) < THREADS) break;
+        const int starts = __syncthreads_count(in);
+        if (starts < THREADS) {
+            if (tid == starts) sh.after = c0 + at;
+            break;
+        }
     }
     int mine = -1;
 #pragma unroll
@@ -277,24 +285,23 @@ __device__ __forceinline__ long long block_sum(long long v) {
 
 // The part of thread `at` of `threads` of the tokens (or sequences) that count.
 __device__ __forceinline__ long long counted(const PolicyArgs &a, int64_t at, int64_t threads) {
-    const PolicyWork &w = a.w;
+    const int4 *const info = a.w.info;
     long long sum = 0;
-    if (!a.per_sequence) {
-        for (int64_t c = at; c < a.chunks; c += threads) sum += w.count[c];
-        return sum;
-    }
-    for (int64_t s = at; s < a.sequences; s += threads) {
-        const int64_t lo = a.offsets[s], hi = a.offsets[s + 1];
-        if (lo >= 0 && lo < hi && lo < a.n) sum += w.slot_count[lo] > 0;
-    }
-    // a sequence none of whose tokens count in its first chunk: the first chunk that has one
+#pragma unroll 4
     for (int64_t c = at; c < a.chunks; c += threads) {
-        const int start = w.head_start[c];
-        if (start < 0 || w.head_count[c] == 0) continue;
-        const int64_t own = start / kChunkTokens;
-        bool first = w.slot_count[start] == 0;
-        for (int64_t b = c - 1; b > own && first; --b) first = w.head_count[b] == 0;
-        sum += first;
+        const int4 here = __ldcg(info + c);
+        const int tail = __ldcg(&info[c > 0 ? c - 1 : 0].w);
+        if (!a.per_sequence) {
+            sum += here.x;
+            continue;
+        }
+        sum += here.y;
+        // a sequence none of whose tokens count before this chunk
+        if (here.z > 0) {
+            bool first = (tail & ~kWhole) == 0;
+            for (int64_t b = c - 1; first && b > 0 && (__ldcg(&info[b].w) & kWhole) != 0; --b) first = (__ldcg(&info[b - 1].w) & ~kWhole) == 0;
+            sum += first;
+        }
     }
     return sum;
 }
@@ -306,11 +313,11 @@ struct Piece {
 };
 
 template <bool SUMS>
-__device__ __forceinline__ Piece piece_of(const PolicyArgs &a, int64_t s, int count, double sum, long long norm) {
+__device__ __forceinline__ Piece piece_of(const PolicyArgs &a, float advantage, int count, double sum, long long norm) {
     Piece p;
     const long long n = a.per_sequence ? norm * count : norm;
     p.weight = count > 0 ? 1.0f / __ll2float_rn(n) : 0.0f;
-    p.advantage = a.advantage[s];
+    p.advantage = advantage;
     p.used = p.slope = 0.0f;
     if (SUMS && count > 0) {
         const double d = sum / count;
@@ -351,18 +358,6 @@ __device__ __forceinline__ void store8(float *p, int64_t i, uint32_t inside, boo
         if (inside >> e & 1) p[i + e] = v[e];
 }
 
-// loss, policy, kl, entropy, clipped from their sums
-__device__ __forceinline__ void write_stats(const PolicyArgs &a, const double (&s)[kSums]) {
-    double loss = s[0];
-    if (a.kl_coef != 0.0f) loss += double(a.kl_coef) * s[1];
-    if (a.entropy_coef != 0.0f) loss -= double(a.entropy_coef) * s[2];
-    a.stats[0] = float(loss);
-    a.stats[1] = float(s[0]);
-    a.stats[2] = float(s[1]);
-    a.stats[3] = float(s[2]);
-    a.stats[4] = float(s[3]);
-}
-
 // ---- the first reading of many tokens: the sums of sequences ----
 
 template <bool SUMS>
@@ -388,23 +383,26 @@ __global__ void __launch_bounds__(kChunkThreads) policy_count_kernel(const Polic
         if (sh.start[tid * kE + e] != kNone) cur = tid * kE + e;
         if (sh.start[cur] == kOutside) on &= ~(1u << e);
     }
-    const int64_t before = sh.before;
+    const int64_t before = sh.before, end = c0 + kChunkTokens;
+    __shared__ int s_head, s_tail, s_starts;
+    if (tid == 0) s_head = s_tail = s_starts = 0;
+    const bool goes_on = sh.after > end;
+    __syncthreads();
     sequence_sums<kChunkThreads, SUMS>(a, c0, first, on, lp, old, sh, [&](int start, int count, double sum) {
-        if (start == 0 && before < c0) {
-            a.w.head_count[c] = count;
-            a.w.head_sum[c] = sum;
+        if (sh.start[start] < 0) return;
+        const bool head = start == 0 && before < c0;
+        if (head) {
+            s_head = count;
+            if (SUMS) a.w.head_sum[c] = sum;
         } else {
+            if (count > 0) atomicAdd(&s_starts, 1);
             a.w.slot_count[c0 + start] = count;
             if (SUMS) a.w.slot_sum[c0 + start] = sum;
         }
+        if (start == sh.last && goes_on) s_tail = count | (head ? kWhole : 0);
     });
-    if (tid == 0) {
-        const bool head = sh.start[0] >= 0 && before < c0;
-        a.w.head_start[c] = head ? int(max(before, int64_t(-1))) : -1;
-        if (!head) a.w.head_count[c] = 0;
-    }
     const long long all = block_sum<kChunkThreads>(__popc(on));
-    if (tid == 0) a.w.count[c] = int(all);
+    if (tid == 0) a.w.info[c] = make_int4(int(all), s_starts, s_head, s_tail);
 }
 
 __global__ void __launch_bounds__(kChunkThreads) policy_norm_kernel(const PolicyArgs a) {
@@ -424,13 +422,35 @@ __device__ __forceinline__ void across_chunks(const PolicyArgs &a, int64_t lo, i
     double v = 0.0;
     const int64_t c0 = lo / kChunkTokens + 1, c1 = min((hi - 1) / kChunkTokens, a.chunks - 1);
     for (int64_t c = c0 + lane; c <= c1; c += 32) {
-        n += a.w.head_count[c];
+        n += __ldcg(&a.w.info[c].z);
         if (SUMS) v += a.w.head_sum[c];
     }
     for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(~0u, n, d);
     if (SUMS) v = warp_sum(v);
     count = a.w.slot_count[lo] + n;
     sum = SUMS ? a.w.slot_sum[lo] + v : 0.0;
+}
+
+// The sums of a CTA's warps, in the first warp: lane 8 k has the k-th.
+template <int THREADS>
+__device__ __forceinline__ double warps_sum(const double (&part)[kSums][THREADS / 32], int lane) {
+    double v = 0.0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; w += 8)
+        if (w + (lane & 7) < THREADS / 32) v += part[lane >> 3][w + (lane & 7)];
+    for (int d = 4; d > 0; d >>= 1) v += __shfl_down_sync(~0u, v, d, 8);
+    return v;
+}
+// loss, policy, kl, entropy, clipped from their sums (lane 8 k has the k-th)
+__device__ __forceinline__ void write_stats(const PolicyArgs &a, double sum, int lane) {
+    const double kl = __shfl_sync(~0u, sum, 8), entropy = __shfl_sync(~0u, sum, 16);
+    if (lane == 0) {
+        double loss = sum;
+        if (a.kl_coef != 0.0f) loss += double(a.kl_coef) * kl;
+        if (a.entropy_coef != 0.0f) loss -= double(a.entropy_coef) * entropy;
+        a.stats[0] = float(loss);
+    }
+    if ((lane & 7) == 0) a.stats[1 + (lane >> 3)] = float(sum);
 }
 
 // SINGLE: all tokens in one CTA, which counts them itself.
@@ -440,10 +460,11 @@ __global__ void __launch_bounds__(THREADS) policy_kernel(const PolicyArgs a) {
     extern __shared__ __align__(16) unsigned char raw[];
     ChunkShared<THREADS> &sh = *reinterpret_cast<ChunkShared<THREADS> *>(raw);
     Piece *const pieces = reinterpret_cast<Piece *>(raw + (sizeof(ChunkShared<THREADS>) + 15) / 16 * 16);
-    __shared__ float stat_part[kSums][THREADS / 32];
+    __shared__ double stat_part[kSums][THREADS / 32];
     __shared__ bool last_cta;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t c = SINGLE ? 0 : blockIdx.x, c0 = c * T, i = c0 + tid * kE;
+    const int live = int(min(a.n - c0, int64_t(T)));
     if (SINGLE) {
         pdl_launch_dependents();
         pdl_wait_previous();
@@ -456,17 +477,50 @@ __global__ void __launch_bounds__(THREADS) policy_kernel(const PolicyArgs a) {
     if (a.ref != nullptr) load8(a.ref, i, a.n, a.vector, ref);
     if (a.entropy != nullptr) load8(a.entropy, i, a.n, a.vector, ent);
     const int first = find_sequences<THREADS>(a, c0, sh);
+#pragma unroll
+    for (int q = 0; q < kE; ++q) {
+        const int p = tid + q * THREADS;
+        if (p < live && sh.start[p] >= 0) pieces[p].advantage = a.advantage[sh.start[p]];
+    }
     uint32_t inside = i >= a.n ? 0u : a.n - i >= kE ? (1u << kE) - 1 : (1u << int(a.n - i)) - 1;
+    int at[kE];   // where the sequence of each token starts
     {
         int cur = first;
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
             if (sh.start[tid * kE + e] != kNone) cur = tid * kE + e;
+            at[e] = cur;
             if (sh.start[cur] == kOutside) inside &= ~(1u << e);
         }
     }
     on &= inside;
-    long long norm;
+    __syncthreads();
+
+    // all that does without the weight
+    float d[kE], excess_of[kE], loss[kE];   // gradient; e^x - 1 - x; -min(..)
+    uint32_t cut = 0;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+        d[e] = excess_of[e] = loss[e] = 0.0f;
+        if (!(on >> e & 1)) continue;
+        if (a.ref != nullptr) {
+            const float x = ref[e] - lp[e], em1 = expm1f(x);
+            excess_of[e] = excess(x, em1);
+            if (a.kl_coef != 0.0f) d[e] = -a.kl_coef * em1;
+        }
+        if (!SUMS) {
+            const float adv = pieces[at[e]].advantage;
+            float hi, lo;
+            difference(lp[e], old[e], hi, lo);
+            const bool up = adv >= 0.0f, clipped = up ? past(hi, lo, a.high, 1.0f) : past(hi, lo, a.low, -1.0f);
+            const float r = expf(hi);
+            loss[e] = -adv * (clipped ? (up ? a.used_high : a.used_low) : r);
+            if (!clipped) d[e] += -adv * r;
+            cut |= uint32_t(clipped) << e;
+        }
+    }
+
+    // what the tokens of a sequence share
     if (SINGLE) {
         // the sums stand in the pieces until what tokens need takes their place
         sequence_sums<THREADS, SUMS>(a, c0, first, on, lp, old, sh, [&](int start, int count, double sum) {
@@ -474,129 +528,117 @@ __global__ void __launch_bounds__(THREADS) policy_kernel(const PolicyArgs a) {
             if (SUMS) *reinterpret_cast<double *>(&pieces[start].used) = sum;
         });
         __syncthreads();
-        long long mine = 0;
+        long long mine = a.per_sequence ? 0 : __popc(on);
         if (a.per_sequence) {
-            for (int p = tid; p < T; p += THREADS)
-                if (sh.start[p] >= 0) mine += __float_as_int(pieces[p].weight) > 0;
-        } else {
-            mine = __popc(on);
+#pragma unroll
+            for (int q = 0; q < kE; ++q) {
+                const int p = tid + q * THREADS;
+                if (p < live && sh.start[p] >= 0) mine += __float_as_int(pieces[p].weight) > 0;
+            }
         }
-        norm = block_sum<THREADS>(mine);
-        for (int p = tid; p < T; p += THREADS) {
-            const int s = sh.start[p];
-            if (s < 0) continue;
+        const long long norm = block_sum<THREADS>(mine);
+#pragma unroll
+        for (int q = 0; q < kE; ++q) {
+            const int p = tid + q * THREADS;
+            if (p >= live || sh.start[p] < 0) continue;
             const double sum = SUMS ? *reinterpret_cast<const double *>(&pieces[p].used) : 0.0;
-            pieces[p] = piece_of<SUMS>(a, s, __float_as_int(pieces[p].weight), sum, norm);
+            pieces[p] = piece_of<SUMS>(a, pieces[p].advantage, __float_as_int(pieces[p].weight), sum, norm);
         }
     } else {
         pdl_launch_dependents();
         pdl_wait_previous();
-        __syncthreads();
-        norm = a.counted ? *a.w.norm : block_sum<THREADS>(counted(a, tid, THREADS));
-        // the sequences at the chunk's ends may go on beyond it
-        for (int p = tid; p < T; p += THREADS) {
-            const int s = sh.start[p];
-            if (s < 0) continue;
-            const int64_t lo = p > 0 ? c0 + p : sh.before, hi = a.offsets[s + 1];
-            if (lo < c0 || hi > c0 + T) continue;
-            pieces[p] = piece_of<SUMS>(a, s, a.w.slot_count[lo], SUMS ? a.w.slot_sum[lo] : 0.0, norm);
+        // every load is on its way before the first of them is waited for
+        int count[kE];
+        double sum[SUMS ? kE : 1];
+        const int64_t before = sh.before;
+        const bool from_before = before < c0, goes_on = sh.after > c0 + T;
+#pragma unroll
+        for (int q = 0; q < kE; ++q) {
+            const int p = tid + q * THREADS;
+            count[q] = -1;
+            // (the sequences at the chunk's ends may go on beyond it)
+            if (p >= live || sh.start[p] < 0 || (p == 0 && from_before) || (p == sh.last && goes_on)) continue;
+            count[q] = __ldcg(a.w.slot_count + c0 + p);
+            if (SUMS) sum[q] = __ldcg(a.w.slot_sum + c0 + p);
         }
-        const int p = warp == 0 ? 0 : sh.last;
-        const int s = sh.start[p];
-        if (s >= 0 && warp < 2 && !(warp == 1 && p == 0)) {
-            const int64_t lo = p > 0 ? c0 + p : sh.before, hi = a.offsets[s + 1];
-            if (lo < c0 || hi > c0 + T) {
-                int count;
-                double sum;
-                across_chunks<SUMS>(a, max(lo, int64_t(0)), min(hi, a.n), count, sum);
-                if (lane == 0) pieces[p] = piece_of<SUMS>(a, s, count, sum, norm);
-            }
+        int n_across = 0;
+        double sum_across = 0.0;
+        const int p_across = warp == 0 ? 0 : sh.last;
+        const bool across = warp < 2 && !(warp == 1 && sh.last == 0) && sh.start[p_across] >= 0 &&
+                            ((p_across == 0 && from_before) || (p_across == sh.last && goes_on));
+        if (across)
+            across_chunks<SUMS>(a, p_across == 0 ? max(before, int64_t(0)) : c0 + p_across, p_across == sh.last ? min(sh.after, a.n) : c0 + T, n_across, sum_across);
+        __syncthreads();   // (the advantages have been read where they are written again)
+        const long long norm = a.counted ? __ldcg(a.w.norm) : block_sum<THREADS>(counted(a, tid, THREADS));
+#pragma unroll
+        for (int q = 0; q < kE; ++q) {
+            const int p = tid + q * THREADS;
+            if (count[q] >= 0) pieces[p] = piece_of<SUMS>(a, pieces[p].advantage, count[q], SUMS ? sum[q] : 0.0, norm);
         }
+        if (across && lane == 0) pieces[p_across] = piece_of<SUMS>(a, pieces[p_across].advantage, n_across, sum_across, norm);
     }
     __syncthreads();
 
-    float stat[kSums] = {}, d_lp[kE], d_ent[kE];   // policy, kl, entropy, clipped
-    Piece piece = {};
-    int cur = first;
-    if (inside & 1 && sh.start[tid * kE] == kNone) piece = pieces[cur];
+    float stat[kSums] = {}, d_ent[kE];   // policy, kl, entropy, clipped
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
-        d_lp[e] = d_ent[e] = 0.0f;
-        if ((inside >> e & 1) && sh.start[tid * kE + e] != kNone) piece = pieces[tid * kE + e];
-        if (!(on >> e & 1)) continue;
-        const float w = fabsf(piece.weight), adv = piece.advantage;
-        float used, slope;
-        bool cut;
+        d_ent[e] = 0.0f;
+        if (!(on >> e & 1)) {
+            d[e] = 0.0f;
+            continue;
+        }
+        const Piece piece = pieces[at[e]];
+        const float w = fabsf(piece.weight);
         if (SUMS) {
-            cut = piece.weight < 0.0f, used = piece.used, slope = piece.slope;
-        } else {
-            float hi, lo;
-            difference(lp[e], old[e], hi, lo);
-            const bool up = adv >= 0.0f;
-            cut = up ? past(hi, lo, a.high, 1.0f) : past(hi, lo, a.low, -1.0f);
-            const float r = expf(hi);
-            used = cut ? (up ? a.used_high : a.used_low) : r;
-            slope = cut ? 0.0f : -adv * r;
+            loss[e] = -piece.advantage * piece.used;
+            d[e] += piece.slope;
+            cut |= uint32_t(piece.weight < 0.0f) << e;
         }
-        float d = slope;
-        stat[0] += w * (-adv * used);
-        if (cut) stat[3] += w;
-        if (a.ref != nullptr) {
-            const float x = ref[e] - lp[e], em1 = expm1f(x);
-            stat[1] += w * excess(x, em1);
-            if (a.kl_coef != 0.0f) d -= a.kl_coef * em1;
-        }
+        stat[0] += w * loss[e];
+        stat[1] += w * excess_of[e];
         if (a.entropy != nullptr) stat[2] += w * ent[e];
-        d_lp[e] = w * d;
+        if (cut >> e & 1) stat[3] += w;
+        d[e] *= w;
         d_ent[e] = -a.entropy_coef * w;
     }
-    store8(a.d_logprob, i, inside, a.vector, d_lp);
+    store8(a.d_logprob, i, inside, a.vector, d);
     if (a.d_entropy != nullptr) store8(a.d_entropy, i, inside, a.vector, d_ent);
 
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
         const float v = warp_sum(stat[k]);
-        if (lane == 0) stat_part[k][warp] = v;
+        if (lane == 0) stat_part[k][warp] = double(v);
     }
     __syncthreads();
-    double sums[kSums];
-    if (tid == 0) {
-#pragma unroll
-        for (int k = 0; k < kSums; ++k) {
-            sums[k] = 0.0;
-            for (int w = 0; w < THREADS / 32; ++w) sums[k] += double(stat_part[k][w]);
-        }
-    }
     if (SINGLE) {
-        if (tid == 0) write_stats(a, sums);
+        if (warp == 0) write_stats(a, warps_sum<THREADS>(stat_part, lane), lane);
         return;
     }
     // the CTA that is done last adds the chunks up, in an order that does not depend on which it is
-    if (tid == 0) {
-        for (int k = 0; k < kSums; ++k) a.w.partial[k * a.chunks + c] = sums[k];
-        __threadfence();
-        last_cta = atomicAdd(a.w.ticket, 1) == int(gridDim.x) - 1;
+    if (warp == 0) {
+        const double v = warps_sum<THREADS>(stat_part, lane);
+        if ((lane & 7) == 0) {
+            a.w.partial[(lane >> 3) * a.chunks + c] = v;
+            __threadfence();
+        }
+        __syncwarp();
+        if (lane == 0) last_cta = atomicAdd(a.w.ticket, 1) == int(gridDim.x) - 1;
     }
     __syncthreads();
     if (!last_cta) return;
     __threadfence();
-    __shared__ double wide[kSums][THREADS / 32];
+    double v[kSums] = {};
+#pragma unroll 4
+    for (int64_t j = tid; j < a.chunks; j += THREADS)
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) v[k] += __ldcg(a.w.partial + k * a.chunks + j);
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
-        double v = 0.0;
-        for (int64_t j = tid; j < a.chunks; j += THREADS) v += __ldcg(a.w.partial + k * a.chunks + j);
-        v = warp_sum(v);
-        if (lane == 0) wide[k][warp] = v;
+        v[k] = warp_sum(v[k]);
+        if (lane == 0) stat_part[k][warp] = v[k];
     }
     __syncthreads();
-    if (tid == 0) {
-#pragma unroll
-        for (int k = 0; k < kSums; ++k) {
-            sums[k] = 0.0;
-            for (int w = 0; w < THREADS / 32; ++w) sums[k] += wide[k][w];
-        }
-        write_stats(a, sums);
-    }
+    if (warp == 0) write_stats(a, warps_sum<THREADS>(stat_part, lane), lane);
 }
 
 // ---- host ----
@@ -614,10 +656,8 @@ int64_t lay_work(char *base, int64_t n, PolicyWork &w) {
     take(w.slot_sum, n);
     take(w.head_sum, c);
     take(w.partial, kSums * c);
+    take(w.info, c);
     take(w.slot_count, n);
-    take(w.head_count, c);
-    take(w.head_start, c);
-    take(w.count, c);
     take(w.norm, 1);
     take(w.ticket, 1);
     return at;
@@ -648,13 +688,13 @@ cudaError_t launch_policy_kernel(const PolicyArgs &a, cudaStream_t stream) {
 
 template <bool SUMS>
 cudaError_t launch_policy(PolicyArgs &a, cudaStream_t stream) {
+    if (a.n <= kVeryFew) return launch_policy_kernel<kVeryFew / kE, true, SUMS>(a, stream);
     if (a.n <= kFew) return launch_policy_kernel<kFew / kE, true, SUMS>(a, stream);
     cudaError_t e = launch_ex(policy_count_kernel<SUMS>, dim3(unsigned(a.chunks)), dim3(kChunkThreads), 0, stream, 1, true, a);
     if (e != cudaSuccess) return e;
-    const int64_t sums = a.chunks + (a.per_sequence ? a.sequences : 0);
-    a.counted = sums > kInline;
+    a.counted = a.chunks > kInline;
     if (a.counted) {
-        e = launch_ex(policy_norm_kernel, dim3(unsigned(std::min<int64_t>((sums + 2047) / 2048, 1024))), dim3(kChunkThreads), 0, stream, 1, true, a);
+        e = launch_ex(policy_norm_kernel, dim3(unsigned((a.chunks + 1023) / 1024)), dim3(kChunkThreads), 0, stream, 1, true, a);
         if (e != cudaSuccess) return e;
     }
     return launch_policy_kernel<kChunkThreads, false, SUMS>(a, stream);

@@ -78,6 +78,17 @@ def test_sizes(n, sequences, ratio, mean):
     check(lp, old, adv, offsets, ref, ent, g.random(n) < 0.9, dict(KW, ratio=ratio, mean=mean))
 
 
+def test_more_chunks_than_a_cta_adds_up():
+    """A sequence of more than a million masked tokens among them."""
+    n = 2048 * 4100 + 5
+    g, lp, old, ref, ent, adv = values(n, 500, 9)
+    offsets = lengths(n, 500, g)
+    mask = g.random(n) < 0.9
+    mask[offsets[100] - 1000000:offsets[100] + 1000000] = False
+    for ratio, mean in ((TOKEN, SEQUENCE), (SEQUENCE, TOKEN)):
+        check(lp, old, adv, offsets, ref, ent, mask, dict(KW, ratio=ratio, mean=mean))
+
+
 @pytest.mark.parametrize("ratio,mean", FORMS)
 @pytest.mark.parametrize("n", [200, 20000])
 @pytest.mark.parametrize("with_ref,with_ent,with_mask", [(False, False, False), (True, False, True), (False, True, False)])
