@@ -96,7 +96,9 @@ __device__ __forceinline__ int64_t offsets_upto(const int64_t *offsets, int64_t 
 template <int THREADS>
 struct ChunkShared {
     static constexpr int T = THREADS * kE;
-    int start[T];        // at the first token of a sequence: the sequence; elsewhere kNone
+    alignas(16) int start[T];   // at the first token of a sequence: the sequence; elsewhere kNone
+    uint16_t places[T];         // where the sequences start, in any order
+    int sequences;              // how many
     int warp_max[THREADS / 32];
     double scan_sum[THREADS / 32];
     int scan_count[THREADS / 32], scan_flag[THREADS / 32];
@@ -105,27 +107,40 @@ struct ChunkShared {
     int64_t after;       // where the last one ends
 };
 
-// Which sequences start where in the chunk at c0; where the last one starts before
-// the thread's tokens (0 in the first thread, where one always stands).
+// What a thread's tokens have to do with sequences.
+struct Tokens {
+    int first;           // where the last sequence before the thread's tokens starts (0 in the first thread)
+    uint32_t starts;     // a bit for each token at which one starts
+    uint32_t inside;     // a bit for each token that belongs to one
+};
+
+// Which sequences start where in the chunk at c0.
 template <int THREADS>
-__device__ __forceinline__ int find_sequences(const PolicyArgs &a, int64_t c0, ChunkShared<THREADS> &sh) {
+__device__ __forceinline__ Tokens find_sequences(const PolicyArgs &a, int64_t c0, ChunkShared<THREADS> &sh) {
     constexpr int T = THREADS * kE;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-#pragma unroll
-    for (int p = tid; p < T; p += THREADS) sh.start[p] = kNone;
+    int4 *const mine = reinterpret_cast<int4 *>(sh.start + tid * kE);
+    mine[0] = mine[1] = make_int4(kNone, kNone, kNone, kNone);
+    if (tid == 0) sh.sequences = 0;
     const int64_t s0 = offsets_upto<THREADS>(a.offsets, a.sequences, c0) - 1;   // (its barriers order the writes above)
     if (tid == 0) {
         const bool inside = s0 >= 0 && s0 < a.sequences;
         sh.start[0] = inside ? int(s0) : kOutside;
         sh.before = inside ? a.offsets[s0] : c0;
+        if (inside) sh.places[atomicAdd(&sh.sequences, 1)] = 0;
     }
     for (int64_t base = s0 + 1;; base += THREADS) {
         const int64_t s = base + tid;
         const int64_t at = s <= a.sequences ? a.offsets[s] - c0 : T;
         const bool in = at < T;
         if (in && at > 0 && c0 + at < a.n) {
-            if (s == a.sequences) sh.start[at] = kOutside;
-            else if (a.offsets[s + 1] - c0 > at) sh.start[at] = int(s);
+            if (s == a.sequences) {
+                sh.start[at] = kOutside;
+            } else if (a.offsets[s + 1] - c0 > at) {
+                sh.start[at] = int(s);
+                const int place = atomicAdd(&sh.sequences, 1);
+                if (place < T) sh.places[place] = uint16_t(at);
+            }
         }
         const int starts = __syncthreads_count(in);
         if (starts < THREADS) {
@@ -133,21 +148,32 @@ __device__ __forceinline__ int find_sequences(const PolicyArgs &a, int64_t c0, C
             break;
         }
     }
-    int mine = -1;
+    const int4 x = mine[0], y = mine[1];
+    const int id[kE] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    Tokens t = {};
 #pragma unroll
-    for (int e = 0; e < kE; ++e)
-        if (sh.start[tid * kE + e] != kNone) mine = tid * kE + e;
+    for (int e = 0; e < kE; ++e) t.starts |= uint32_t(id[e] != kNone) << e;
+    int last = t.starts != 0 ? tid * kE + 31 - __clz(t.starts) : -1;
     for (int d = 1; d < 32; d <<= 1) {
-        const int o = __shfl_up_sync(~0u, mine, d);
-        if (lane >= d) mine = max(mine, o);
+        const int o = __shfl_up_sync(~0u, last, d);
+        if (lane >= d) last = max(last, o);
     }
-    if (lane == 31) sh.warp_max[warp] = mine;
+    if (lane == 31) sh.warp_max[warp] = last;
     __syncthreads();
-    int before = __shfl_up_sync(~0u, mine, 1);
+    int before = __shfl_up_sync(~0u, last, 1);
     if (lane == 0) before = -1;
     for (int w = 0; w < warp; ++w) before = max(before, sh.warp_max[w]);
-    if (tid == THREADS - 1) sh.last = max(mine, before);
-    return tid == 0 ? 0 : before;
+    if (tid == THREADS - 1) sh.last = max(last, before);
+    t.first = tid == 0 ? 0 : before;
+    bool in = sh.start[t.first] >= 0;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+        if (id[e] != kNone) in = id[e] >= 0;
+        t.inside |= uint32_t(in) << e;
+    }
+    const int64_t left = a.n - c0 - tid * kE;
+    t.inside &= left >= kE ? (1u << kE) - 1 : left > 0 ? (1u << int(left)) - 1 : 0u;
+    return t;
 }
 
 // kE tokens from i on (`rest` where n ends before them).
@@ -185,27 +211,31 @@ __device__ __forceinline__ void difference(float a, float b, float &hi, float &l
     lo = __fadd_rn(__fsub_rn(a, __fadd_rn(hi, bb)), __fsub_rn(bb, b));
 }
 
-// Whether hi + lo is above (sign +1) or below (-1) the border.
-__device__ __forceinline__ bool past(float hi, float lo, const float (&border)[3], float sign) {
-    if (hi != border[0]) return sign * hi > sign * border[0];
-    if (lo != border[1]) return sign * lo > sign * border[1];
-    return sign * border[2] < 0.0f;
+// Whether the exact difference a - b is above (UP) or below a border, `d` being the
+// rounded one, which tells unless it is the rounded border.
+template <bool UP>
+__device__ __forceinline__ bool past(float a, float b, float d, const float (&border)[3]) {
+    if (d != border[0]) return UP ? d > border[0] : d < border[0];
+    float hi, lo;
+    difference(a, b, hi, lo);
+    if (lo != border[1]) return UP ? lo > border[1] : lo < border[1];
+    return UP ? border[2] < 0.0f : border[2] > 0.0f;
 }
 
 // Of every sequence in the chunk, how many of its tokens count and the sum of their
 // differences: put(start, count, sum) once for each.
 template <int THREADS, bool SUMS, typename Put>
-__device__ __forceinline__ void sequence_sums(const PolicyArgs &a, int64_t c0, int first, uint32_t on, const float (&lp)[kE],
+__device__ __forceinline__ void sequence_sums(const Tokens &t, uint32_t on, const float (&lp)[kE],
                                               const float (&old)[kE], ChunkShared<THREADS> &sh, Put put) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    int cur = first, count = 0, head_count = 0;
+    int cur = t.first, count = 0, head_count = 0;
     float hi = 0.0f, lo = 0.0f;
     double head_sum = 0.0;
     bool flag = false;
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
         const int p = tid * kE + e;
-        if (sh.start[p] != kNone && p > 0) {
+        if ((t.starts >> e & 1) && p > 0) {
             if (!flag) head_count = count, head_sum = SUMS ? double(hi) + double(lo) : 0.0;
             else put(cur, count, SUMS ? double(hi) + double(lo) : 0.0);
             flag = true;
@@ -251,7 +281,7 @@ __device__ __forceinline__ void sequence_sums(const PolicyArgs &a, int64_t c0, i
     }
     if (!bf) bc += wc, bs = ws + bs;
     // the thread's first start ends the sequence before it, the chunk's end the last one
-    if (flag) put(first, bc + head_count, bs + head_sum);
+    if (flag) put(t.first, bc + head_count, bs + head_sum);
     if (tid == THREADS - 1) {
         if (flag) put(cur, tail_count, tail_sum);
         else put(cur, bc + tail_count, bs + tail_sum);
@@ -330,10 +360,9 @@ __device__ __forceinline__ Piece piece_of(const PolicyArgs &a, float advantage, 
     return p;
 }
 
-// e^x - 1 - x: its series where the terms cancel (|x| < 1; what is left out is below
-// 2^-28 of the sum).
-__device__ __forceinline__ float excess(float x, float em1) {
-    if (fabsf(x) >= 1.0f) return em1 - x;
+// e^x - 1 and e^x - 1 - x: the second by its series where the terms cancel (|x| < 1; what
+// is left out is below 2^-28 of the sum), and the first from it.
+__device__ __forceinline__ void divergence(float x, float &em1, float &excess) {
     float s = 1.0f / 39916800.0f;
     s = fmaf(s, x, 1.0f / 3628800.0f);
     s = fmaf(s, x, 1.0f / 362880.0f);
@@ -344,7 +373,10 @@ __device__ __forceinline__ float excess(float x, float em1) {
     s = fmaf(s, x, 1.0f / 24.0f);
     s = fmaf(s, x, 1.0f / 6.0f);
     s = fmaf(s, x, 0.5f);
-    return s * x * x;
+    const float far = expf(x) - 1.0f;
+    const bool near = fabsf(x) < 1.0f;
+    excess = near ? s * x * x : far - x;
+    em1 = near ? x + s * x * x : far;
 }
 
 __device__ __forceinline__ void store8(float *p, int64_t i, uint32_t inside, bool vector, const float (&v)[kE]) {
@@ -375,20 +407,14 @@ __global__ void __launch_bounds__(kChunkThreads) policy_count_kernel(const Polic
         load8(a.old, i, a.n, a.vector, old);
     }
     if (c == 0 && tid == 0) *a.w.ticket = 0, *a.w.norm = 0;
-    const int first = find_sequences<kChunkThreads>(a, c0, sh);
-    // tokens of no sequence do not count
-    int cur = first;
-#pragma unroll
-    for (int e = 0; e < kE; ++e) {
-        if (sh.start[tid * kE + e] != kNone) cur = tid * kE + e;
-        if (sh.start[cur] == kOutside) on &= ~(1u << e);
-    }
+    const Tokens t = find_sequences<kChunkThreads>(a, c0, sh);
+    on &= t.inside;
     const int64_t before = sh.before, end = c0 + kChunkTokens;
     __shared__ int s_head, s_tail, s_starts;
     if (tid == 0) s_head = s_tail = s_starts = 0;
     const bool goes_on = sh.after > end;
     __syncthreads();
-    sequence_sums<kChunkThreads, SUMS>(a, c0, first, on, lp, old, sh, [&](int start, int count, double sum) {
+    sequence_sums<kChunkThreads, SUMS>(t, on, lp, old, sh, [&](int start, int count, double sum) {
         if (sh.start[start] < 0) return;
         const bool head = start == 0 && before < c0;
         if (head) {
@@ -455,16 +481,15 @@ __device__ __forceinline__ void write_stats(const PolicyArgs &a, double sum, int
 
 // SINGLE: all tokens in one CTA, which counts them itself.
 template <int THREADS, bool SINGLE, bool SUMS>
-__global__ void __launch_bounds__(THREADS) policy_kernel(const PolicyArgs a) {
+__global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const PolicyArgs a) {
     constexpr int T = THREADS * kE;
     extern __shared__ __align__(16) unsigned char raw[];
     ChunkShared<THREADS> &sh = *reinterpret_cast<ChunkShared<THREADS> *>(raw);
-    Piece *const pieces = reinterpret_cast<Piece *>(raw + (sizeof(ChunkShared<THREADS>) + 15) / 16 * 16);
+    Piece *const pieces = reinterpret_cast<Piece *>(raw + (sizeof(ChunkShared<THREADS>) + 15) / 16 * 16);   // by the place of the start
     __shared__ double stat_part[kSums][THREADS / 32];
     __shared__ bool last_cta;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t c = SINGLE ? 0 : blockIdx.x, c0 = c * T, i = c0 + tid * kE;
-    const int live = int(min(a.n - c0, int64_t(T)));
     if (SINGLE) {
         pdl_launch_dependents();
         pdl_wait_previous();
@@ -476,131 +501,110 @@ __global__ void __launch_bounds__(THREADS) policy_kernel(const PolicyArgs a) {
     load8(a.old, i, a.n, a.vector, old);
     if (a.ref != nullptr) load8(a.ref, i, a.n, a.vector, ref);
     if (a.entropy != nullptr) load8(a.entropy, i, a.n, a.vector, ent);
-    const int first = find_sequences<THREADS>(a, c0, sh);
-#pragma unroll
-    for (int q = 0; q < kE; ++q) {
-        const int p = tid + q * THREADS;
-        if (p < live && sh.start[p] >= 0) pieces[p].advantage = a.advantage[sh.start[p]];
-    }
-    uint32_t inside = i >= a.n ? 0u : a.n - i >= kE ? (1u << kE) - 1 : (1u << int(a.n - i)) - 1;
-    int at[kE];   // where the sequence of each token starts
-    {
-        int cur = first;
-#pragma unroll
-        for (int e = 0; e < kE; ++e) {
-            if (sh.start[tid * kE + e] != kNone) cur = tid * kE + e;
-            at[e] = cur;
-            if (sh.start[cur] == kOutside) inside &= ~(1u << e);
-        }
-    }
-    on &= inside;
+    const Tokens t = find_sequences<THREADS>(a, c0, sh);
+    const int sequences = min(sh.sequences, T);
+    for (int k = tid; k < sequences; k += THREADS) pieces[sh.places[k]].advantage = a.advantage[sh.start[sh.places[k]]];
+    on &= t.inside;
     __syncthreads();
 
-    // all that does without the weight
-    float d[kE], excess_of[kE], loss[kE];   // gradient; e^x - 1 - x; -min(..)
+    // all that does without the weight, of tokens that do not count as of differences of 0
+    float d[kE], excess[kE], loss[kE];   // gradient; e^x - 1 - x; -min(..)
     uint32_t cut = 0;
+    float adv = pieces[t.first].advantage;
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
-        d[e] = excess_of[e] = loss[e] = 0.0f;
-        if (!(on >> e & 1)) continue;
+        const bool counts = on >> e & 1;
+        d[e] = excess[e] = loss[e] = 0.0f;
         if (a.ref != nullptr) {
-            const float x = ref[e] - lp[e], em1 = expm1f(x);
-            excess_of[e] = excess(x, em1);
+            float em1;
+            divergence(counts ? ref[e] - lp[e] : 0.0f, em1, excess[e]);
             if (a.kl_coef != 0.0f) d[e] = -a.kl_coef * em1;
         }
         if (!SUMS) {
-            const float adv = pieces[at[e]].advantage;
-            float hi, lo;
-            difference(lp[e], old[e], hi, lo);
-            const bool up = adv >= 0.0f, clipped = up ? past(hi, lo, a.high, 1.0f) : past(hi, lo, a.low, -1.0f);
-            const float r = expf(hi);
+            if (t.starts >> e & 1) adv = pieces[tid * kE + e].advantage;
+            const float diff = counts ? lp[e] - old[e] : 0.0f;
+            const bool up = adv >= 0.0f, clipped = up ? past<true>(lp[e], old[e], diff, a.high) : past<false>(lp[e], old[e], diff, a.low);
+            const float r = expf(diff);
             loss[e] = -adv * (clipped ? (up ? a.used_high : a.used_low) : r);
             if (!clipped) d[e] += -adv * r;
             cut |= uint32_t(clipped) << e;
         }
+        if (!counts) ent[e] = 0.0f;
     }
 
     // what the tokens of a sequence share
     if (SINGLE) {
         // the sums stand in the pieces until what tokens need takes their place
-        sequence_sums<THREADS, SUMS>(a, c0, first, on, lp, old, sh, [&](int start, int count, double sum) {
+        sequence_sums<THREADS, SUMS>(t, on, lp, old, sh, [&](int start, int count, double sum) {
             pieces[start].weight = __int_as_float(count);
             if (SUMS) *reinterpret_cast<double *>(&pieces[start].used) = sum;
         });
         __syncthreads();
         long long mine = a.per_sequence ? 0 : __popc(on);
-        if (a.per_sequence) {
-#pragma unroll
-            for (int q = 0; q < kE; ++q) {
-                const int p = tid + q * THREADS;
-                if (p < live && sh.start[p] >= 0) mine += __float_as_int(pieces[p].weight) > 0;
-            }
-        }
+        if (a.per_sequence)
+            for (int k = tid; k < sequences; k += THREADS) mine += __float_as_int(pieces[sh.places[k]].weight) > 0;
         const long long norm = block_sum<THREADS>(mine);
-#pragma unroll
-        for (int q = 0; q < kE; ++q) {
-            const int p = tid + q * THREADS;
-            if (p >= live || sh.start[p] < 0) continue;
-            const double sum = SUMS ? *reinterpret_cast<const double *>(&pieces[p].used) : 0.0;
-            pieces[p] = piece_of<SUMS>(a, pieces[p].advantage, __float_as_int(pieces[p].weight), sum, norm);
+        for (int k = tid; k < sequences; k += THREADS) {
+            Piece &p = pieces[sh.places[k]];
+            const double sum = SUMS ? *reinterpret_cast<const double *>(&p.used) : 0.0;
+            p = piece_of<SUMS>(a, p.advantage, __float_as_int(p.weight), sum, norm);
         }
     } else {
         pdl_launch_dependents();
         pdl_wait_previous();
-        // every load is on its way before the first of them is waited for
-        int count[kE];
-        double sum[SUMS ? kE : 1];
+        __syncthreads();   // (the advantages have been read where they are written again)
         const int64_t before = sh.before;
+        const int last = sh.last;
         const bool from_before = before < c0, goes_on = sh.after > c0 + T;
-#pragma unroll
-        for (int q = 0; q < kE; ++q) {
-            const int p = tid + q * THREADS;
-            count[q] = -1;
-            // (the sequences at the chunk's ends may go on beyond it)
-            if (p >= live || sh.start[p] < 0 || (p == 0 && from_before) || (p == sh.last && goes_on)) continue;
-            count[q] = __ldcg(a.w.slot_count + c0 + p);
-            if (SUMS) sum[q] = __ldcg(a.w.slot_sum + c0 + p);
-        }
         int n_across = 0;
         double sum_across = 0.0;
-        const int p_across = warp == 0 ? 0 : sh.last;
-        const bool across = warp < 2 && !(warp == 1 && sh.last == 0) && sh.start[p_across] >= 0 &&
-                            ((p_across == 0 && from_before) || (p_across == sh.last && goes_on));
+        // the sequences at the chunk's ends may go on beyond it
+        const int p_across = warp == 0 ? 0 : last;
+        const bool across = warp < 2 && !(warp == 1 && last == 0) && sh.start[p_across] >= 0 &&
+                            ((p_across == 0 && from_before) || (p_across == last && goes_on));
         if (across)
-            across_chunks<SUMS>(a, p_across == 0 ? max(before, int64_t(0)) : c0 + p_across, p_across == sh.last ? min(sh.after, a.n) : c0 + T, n_across, sum_across);
-        __syncthreads();   // (the advantages have been read where they are written again)
+            across_chunks<SUMS>(a, p_across == 0 ? max(before, int64_t(0)) : c0 + p_across, p_across == last ? min(sh.after, a.n) : c0 + T, n_across, sum_across);
+        const int place = tid < sequences ? sh.places[tid] : 0;
+        int n_mine = 0;
+        double sum_mine = 0.0;
+        if (tid < sequences && c0 + place < a.n) {   // (on its way while the chunks are added up)
+            n_mine = __ldcg(a.w.slot_count + c0 + place);
+            if (SUMS) sum_mine = __ldcg(a.w.slot_sum + c0 + place);
+        }
         const long long norm = a.counted ? __ldcg(a.w.norm) : block_sum<THREADS>(counted(a, tid, THREADS));
-#pragma unroll
-        for (int q = 0; q < kE; ++q) {
-            const int p = tid + q * THREADS;
-            if (count[q] >= 0) pieces[p] = piece_of<SUMS>(a, pieces[p].advantage, count[q], SUMS ? sum[q] : 0.0, norm);
+        for (int k = tid; k < sequences; k += THREADS) {
+            const int p = sh.places[k];
+            if ((p == 0 && from_before) || (p == last && goes_on)) continue;
+            if (k != tid) {
+                n_mine = __ldcg(a.w.slot_count + c0 + p);
+                if (SUMS) sum_mine = __ldcg(a.w.slot_sum + c0 + p);
+            }
+            pieces[p] = piece_of<SUMS>(a, pieces[p].advantage, n_mine, sum_mine, norm);
         }
         if (across && lane == 0) pieces[p_across] = piece_of<SUMS>(a, pieces[p_across].advantage, n_across, sum_across, norm);
     }
     __syncthreads();
 
     float stat[kSums] = {}, d_ent[kE];   // policy, kl, entropy, clipped
+    Piece piece = pieces[t.first];
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
-        d_ent[e] = 0.0f;
-        if (!(on >> e & 1)) {
-            d[e] = 0.0f;
-            continue;
-        }
-        const Piece piece = pieces[at[e]];
-        const float w = fabsf(piece.weight);
+        if (t.starts >> e & 1) piece = pieces[tid * kE + e];
+        const float w = on >> e & 1 ? fabsf(piece.weight) : 0.0f;
         if (SUMS) {
             loss[e] = -piece.advantage * piece.used;
             d[e] += piece.slope;
             cut |= uint32_t(piece.weight < 0.0f) << e;
         }
-        stat[0] += w * loss[e];
-        stat[1] += w * excess_of[e];
+        // (of what does not count nothing is taken: 0 times it might not be 0)
+        stat[0] += w != 0.0f ? w * loss[e] : 0.0f;
+        stat[1] += w * excess[e];
         if (a.entropy != nullptr) stat[2] += w * ent[e];
         if (cut >> e & 1) stat[3] += w;
-        d[e] *= w;
-        d_ent[e] = -a.entropy_coef * w;
+        d[e] = w != 0.0f ? w * d[e] : 0.0f;
+        d_ent[e] = w != 0.0f ? -a.entropy_coef * w : 0.0f;
     }
+    const uint32_t inside = t.inside;
     store8(a.d_logprob, i, inside, a.vector, d);
     if (a.d_entropy != nullptr) store8(a.d_entropy, i, inside, a.vector, d_ent);
 
