@@ -379,6 +379,26 @@ __device__ __forceinline__ void divergence(float x, float &em1, float &excess) {
     em1 = near ? x + s * x * x : far;
 }
 
+// e^x of two numbers between -80 and 80, to two units: 2^t with t = x log2 e rounded, and
+// what that rounding left taken to first order.
+__device__ __forceinline__ Pair exp_pair(Pair x) {
+    constexpr float kLog2eRest = 1.925963033500e-08f;   // log2 e - kLog2e
+    const Pair t = mul2(x, both(kLog2e)), r = fma2(x, both(kLog2eRest), fma2(x, both(kLog2e), mul2(t, both(-1.0f))));
+    const Pair e = pair(exp2_fast(low(t)), exp2_fast(high(t)));
+    return fma2(e, mul2(r, both(kLn2)), e);
+}
+// divergence() of two of them.
+__device__ __forceinline__ void divergence_pair(Pair x, Pair &em1, Pair &excess) {
+    Pair s = both(1.0f / 39916800.0f);
+    constexpr float terms[] = {1.0f / 3628800.0f, 1.0f / 362880.0f, 1.0f / 40320.0f, 1.0f / 5040.0f, 1.0f / 720.0f, 1.0f / 120.0f, 1.0f / 24.0f, 1.0f / 6.0f, 0.5f};
+#pragma unroll
+    for (int i = 0; i < 9; ++i) s = fma2(s, x, both(terms[i]));
+    const Pair near = mul2(s, mul2(x, x)), far = add2(exp_pair(x), both(-1.0f)), rest = fma2(x, both(-1.0f), far), em1_near = add2(x, near);
+    const bool n0 = fabsf(low(x)) < 1.0f, n1 = fabsf(high(x)) < 1.0f;
+    excess = pair(n0 ? low(near) : low(rest), n1 ? high(near) : high(rest));
+    em1 = pair(n0 ? low(em1_near) : low(far), n1 ? high(em1_near) : high(far));
+}
+
 __device__ __forceinline__ void store8(float *p, int64_t i, uint32_t inside, bool vector, const float (&v)[kE]) {
     if (vector && inside == (1u << kE) - 1) {
         reinterpret_cast<float4 *>(p + i)[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -479,6 +499,26 @@ __device__ __forceinline__ void write_stats(const PolicyArgs &a, double sum, int
     if ((lane & 7) == 0) a.stats[1 + (lane >> 3)] = float(sum);
 }
 
+// The same for one token, whatever it holds.
+template <bool SUMS>
+__device__ __noinline__ void rarely_one(const PolicyArgs &a, float lp, float old, float ref, float adv, float &d, float &excess, float &loss, bool &cut) {
+    d = excess = loss = 0.0f;
+    cut = false;
+    if (a.ref != nullptr) {
+        float em1;
+        divergence(ref - lp, em1, excess);
+        if (a.kl_coef != 0.0f) d = -a.kl_coef * em1;
+    }
+    if (!SUMS) {
+        const float diff = lp - old;
+        const bool up = adv >= 0.0f;
+        cut = up ? past<true>(lp, old, diff, a.high) : past<false>(lp, old, diff, a.low);
+        const float r = expf(diff);
+        loss = -adv * (cut ? (up ? a.used_high : a.used_low) : r);
+        if (!cut) d += -adv * r;
+    }
+}
+
 // SINGLE: all tokens in one CTA, which counts them itself.
 template <int THREADS, bool SINGLE, bool SUMS>
 __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const PolicyArgs a) {
@@ -508,28 +548,56 @@ __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const P
     __syncthreads();
 
     // all that does without the weight, of tokens that do not count as of differences of 0
-    float d[kE], excess[kE], loss[kE];   // gradient; e^x - 1 - x; -min(..)
+    float d[kE], excess[kE], loss[kE], advantage[kE];   // gradient; e^x - 1 - x; -min(..)
     uint32_t cut = 0;
-    float adv = pieces[t.first].advantage;
+    if (!SUMS) {
+        float adv = pieces[t.first].advantage;
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
-        const bool counts = on >> e & 1;
-        d[e] = excess[e] = loss[e] = 0.0f;
-        if (a.ref != nullptr) {
-            float em1;
-            divergence(counts ? ref[e] - lp[e] : 0.0f, em1, excess[e]);
-            if (a.kl_coef != 0.0f) d[e] = -a.kl_coef * em1;
-        }
-        if (!SUMS) {
+        for (int e = 0; e < kE; ++e) {
             if (t.starts >> e & 1) adv = pieces[tid * kE + e].advantage;
-            const float diff = counts ? lp[e] - old[e] : 0.0f;
-            const bool up = adv >= 0.0f, clipped = up ? past<true>(lp[e], old[e], diff, a.high) : past<false>(lp[e], old[e], diff, a.low);
-            const float r = expf(diff);
-            loss[e] = -adv * (clipped ? (up ? a.used_high : a.used_low) : r);
-            if (!clipped) d[e] += -adv * r;
-            cut |= uint32_t(clipped) << e;
+            advantage[e] = on >> e & 1 ? adv : 0.0f;
         }
-        if (!counts) ent[e] = 0.0f;
+    }
+    // two tokens at a time; `rare`: a difference on a border, whose exact value decides,
+    // or one too large for exp_pair
+    bool rare = false;
+#pragma unroll
+    for (int e = 0; e < kE; e += 2) {
+        const bool c0 = on >> e & 1, c1 = on >> (e + 1) & 1;
+        Pair grad = both(0.0f), far_off = both(0.0f);
+        if (a.ref != nullptr) {
+            const Pair x = pair(c0 ? ref[e] - lp[e] : 0.0f, c1 ? ref[e + 1] - lp[e + 1] : 0.0f);
+            rare |= !(fmaxf(fabsf(low(x)), fabsf(high(x))) < 80.0f);
+            Pair em1;
+            divergence_pair(x, em1, far_off);
+            if (a.kl_coef != 0.0f) grad = mul2(em1, both(-a.kl_coef));
+        }
+        excess[e] = low(far_off), excess[e + 1] = high(far_off);
+        if (!SUMS) {
+            const Pair diff = pair(c0 ? lp[e] - old[e] : 0.0f, c1 ? lp[e + 1] - old[e + 1] : 0.0f);
+            rare |= !(fmaxf(fabsf(low(diff)), fabsf(high(diff))) < 80.0f);
+            const bool up0 = advantage[e] >= 0.0f, up1 = advantage[e + 1] >= 0.0f;
+            const float b0 = up0 ? a.high[0] : a.low[0], b1 = up1 ? a.high[0] : a.low[0];
+            const bool k0 = up0 ? low(diff) > b0 : low(diff) < b0, k1 = up1 ? high(diff) > b1 : high(diff) < b1;
+            rare |= low(diff) == b0 || high(diff) == b1;
+            const Pair gain = mul2(exp_pair(diff), pair(-advantage[e], -advantage[e + 1]));
+            loss[e] = k0 ? -advantage[e] * (up0 ? a.used_high : a.used_low) : low(gain);
+            loss[e + 1] = k1 ? -advantage[e + 1] * (up1 ? a.used_high : a.used_low) : high(gain);
+            grad = add2(grad, pair(k0 ? 0.0f : low(gain), k1 ? 0.0f : high(gain)));
+            cut |= uint32_t(k0) << e | uint32_t(k1) << (e + 1);
+        }
+        d[e] = low(grad), d[e + 1] = high(grad);
+        if (!c0) ent[e] = 0.0f;
+        if (!c1) ent[e + 1] = 0.0f;
+    }
+    if (rare) {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            if (!(on >> e & 1)) continue;
+            bool k;
+            rarely_one<SUMS>(a, lp[e], old[e], a.ref != nullptr ? ref[e] : 0.0f, SUMS ? 0.0f : advantage[e], d[e], excess[e], loss[e], k);
+            cut = (cut & ~(1u << e)) | uint32_t(k) << e;
+        }
     }
 
     // what the tokens of a sequence share
@@ -585,25 +653,33 @@ __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const P
     }
     __syncthreads();
 
-    float stat[kSums] = {}, d_ent[kE];   // policy, kl, entropy, clipped
+    float d_ent[kE];
+    Pair sum_loss = both(0.0f), sum_excess = both(0.0f), sum_ent = both(0.0f);
+    float sum_cut = 0.0f;
     Piece piece = pieces[t.first];
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
-        if (t.starts >> e & 1) piece = pieces[tid * kE + e];
-        const float w = on >> e & 1 ? fabsf(piece.weight) : 0.0f;
-        if (SUMS) {
-            loss[e] = -piece.advantage * piece.used;
-            d[e] += piece.slope;
-            cut |= uint32_t(piece.weight < 0.0f) << e;
+    for (int e = 0; e < kE; e += 2) {
+        float w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (t.starts >> (e + i) & 1) piece = pieces[tid * kE + e + i];
+            const bool counts = on >> (e + i) & 1;
+            w[i] = counts ? fabsf(piece.weight) : 0.0f;
+            if (SUMS) {
+                loss[e + i] = counts ? -piece.advantage * piece.used : 0.0f;
+                d[e + i] += counts ? piece.slope : 0.0f;
+                cut |= uint32_t(piece.weight < 0.0f) << (e + i);
+            }
+            sum_cut += cut >> (e + i) & 1 ? w[i] : 0.0f;
         }
-        // (of what does not count nothing is taken: 0 times it might not be 0)
-        stat[0] += w != 0.0f ? w * loss[e] : 0.0f;
-        stat[1] += w * excess[e];
-        if (a.entropy != nullptr) stat[2] += w * ent[e];
-        if (cut >> e & 1) stat[3] += w;
-        d[e] = w != 0.0f ? w * d[e] : 0.0f;
-        d_ent[e] = w != 0.0f ? -a.entropy_coef * w : 0.0f;
+        const Pair ww = pair(w[0], w[1]), dd = mul2(ww, pair(d[e], d[e + 1])), ee = mul2(ww, both(-a.entropy_coef));
+        sum_loss = fma2(ww, pair(loss[e], loss[e + 1]), sum_loss);
+        sum_excess = fma2(ww, pair(excess[e], excess[e + 1]), sum_excess);
+        if (a.entropy != nullptr) sum_ent = fma2(ww, pair(ent[e], ent[e + 1]), sum_ent);
+        d[e] = low(dd), d[e + 1] = high(dd);
+        d_ent[e] = low(ee), d_ent[e + 1] = high(ee);
     }
+    const float stat[kSums] = {across(sum_loss), across(sum_excess), across(sum_ent), sum_cut};   // policy, kl, entropy, clipped
     const uint32_t inside = t.inside;
     store8(a.d_logprob, i, inside, a.vector, d);
     if (a.d_entropy != nullptr) store8(a.d_entropy, i, inside, a.vector, d_ent);
