@@ -54,7 +54,7 @@ constexpr int kWhole = 1 << 30;             // a chunk that is all of one sequen
 struct PolicyWork {
     double *slot_sum;     // per token: of the sequence that starts there, what its first chunk has of it
     double *head_sum;     // per chunk: of the sequence that started before it
-    double *partial;      // per sum and chunk
+    double *partial;      // per chunk and sum
     int4 *info;           // per chunk: the tokens that count; sequences that start in it and have one of them; of the
                           // sequence that started before it; of the one that goes on behind it (kWhole: the same one)
     int32_t *slot_count;
@@ -131,12 +131,12 @@ __device__ __forceinline__ Tokens find_sequences(const PolicyArgs &a, int64_t c0
     }
     for (int64_t base = s0 + 1;; base += THREADS) {
         const int64_t s = base + tid;
-        const int64_t at = s <= a.sequences ? a.offsets[s] - c0 : T;
+        const int64_t at = s <= a.sequences ? a.offsets[s] - c0 : T, next = s < a.sequences ? a.offsets[s + 1] - c0 : 0;
         const bool in = at < T;
         if (in && at > 0 && c0 + at < a.n) {
             if (s == a.sequences) {
                 sh.start[at] = kOutside;
-            } else if (a.offsets[s + 1] - c0 > at) {
+            } else if (next > at) {
                 sh.start[at] = int(s);
                 const int place = atomicAdd(&sh.sequences, 1);
                 if (place < T) sh.places[place] = uint16_t(at);
@@ -680,30 +680,30 @@ __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const P
         d_ent[e] = low(ee), d_ent[e + 1] = high(ee);
     }
     const float stat[kSums] = {across(sum_loss), across(sum_excess), across(sum_ent), sum_cut};   // policy, kl, entropy, clipped
-    const uint32_t inside = t.inside;
-    store8(a.d_logprob, i, inside, a.vector, d);
-    if (a.d_entropy != nullptr) store8(a.d_entropy, i, inside, a.vector, d_ent);
-
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
         const float v = warp_sum(stat[k]);
         if (lane == 0) stat_part[k][warp] = double(v);
     }
     __syncthreads();
-    if (SINGLE) {
-        if (warp == 0) write_stats(a, warps_sum<THREADS>(stat_part, lane), lane);
-        return;
-    }
-    // the CTA that is done last adds the chunks up, in an order that does not depend on which it is
+    // the CTA that is done last adds the chunks up, in an order that does not depend on
+    // which it is (it is told before the gradients are written: the fence would wait for them)
     if (warp == 0) {
         const double v = warps_sum<THREADS>(stat_part, lane);
-        if ((lane & 7) == 0) {
-            a.w.partial[(lane >> 3) * a.chunks + c] = v;
-            __threadfence();
+        if (SINGLE) {
+            write_stats(a, v, lane);
+        } else {
+            if ((lane & 7) == 0) {
+                a.w.partial[c * kSums + (lane >> 3)] = v;
+                __threadfence();
+            }
+            __syncwarp();
+            if (lane == 0) last_cta = atomicAdd(a.w.ticket, 1) == int(gridDim.x) - 1;
         }
-        __syncwarp();
-        if (lane == 0) last_cta = atomicAdd(a.w.ticket, 1) == int(gridDim.x) - 1;
     }
+    store8(a.d_logprob, i, t.inside, a.vector, d);
+    if (a.d_entropy != nullptr) store8(a.d_entropy, i, t.inside, a.vector, d_ent);
+    if (SINGLE) return;
     __syncthreads();
     if (!last_cta) return;
     __threadfence();
@@ -711,7 +711,7 @@ __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const P
 #pragma unroll 4
     for (int64_t j = tid; j < a.chunks; j += THREADS)
 #pragma unroll
-        for (int k = 0; k < kSums; ++k) v[k] += __ldcg(a.w.partial + k * a.chunks + j);
+        for (int k = 0; k < kSums; ++k) v[k] += __ldcg(a.w.partial + j * kSums + k);
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
         v[k] = warp_sum(v[k]);
