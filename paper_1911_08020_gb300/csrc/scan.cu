@@ -180,9 +180,11 @@ __device__ __forceinline__ void map_through(const Quad &A, const Quad &H, Quad &
 // A carry goes from warp to warp, and from the last one to the first one's next round:
 // a named barrier for each warp that takes one, at which the giver does not wait.  (A
 // warp gives again when the carry has been round all the others, so that one place and
-// one barrier do.)
-__device__ __forceinline__ void take_carry(int warp) { asm volatile("bar.sync %0, 64;" ::"r"(warp + 1) : "memory"); }
-__device__ __forceinline__ void give_carry(int warp) { asm volatile("bar.arrive %0, 64;" ::"r"(warp + 1) : "memory"); }
+// one barrier do.  16 warps use the barrier of __syncthreads too, which they do without.)
+template <int WARPS>
+__device__ __forceinline__ void take_carry(int warp) { asm volatile("bar.sync %0, 64;" ::"r"(warp + (WARPS < 16)) : "memory"); }
+template <int WARPS>
+__device__ __forceinline__ void give_carry(int warp) { asm volatile("bar.arrive %0, 64;" ::"r"(warp + (WARPS < 16)) : "memory"); }
 
 __device__ __forceinline__ Pair shuffle_up(Pair v, int d) {
     Pair r;
@@ -209,15 +211,16 @@ constexpr int kStages = 3;
 constexpr int kStageBytes = 128;   // of a thread and round
 
 // LC lanes of a warp have neighbouring channels, the other lanes later steps.
-template <typename T, bool BACK, int LC, bool LOGITS>
-__global__ void __launch_bounds__(kScanThreads, 2) channel_kernel(const ScanArgs s, const int cluster) {
+template <typename T, bool BACK, int LC, int WARPS, bool LOGITS>
+__global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) channel_kernel(const ScanArgs s, const int cluster) {
     constexpr int V = 4, IN = BACK ? 4 : 2, OUT = BACK ? 2 : 1;
     constexpr int S = kStageBytes / (IN * V * int(sizeof(T)));   // steps of a thread in a round
     constexpr int TL = 32 / LC, NS = kStages;
-    constexpr bool kMayCluster = LC < 32;
+    constexpr bool kMayCluster = LC < 16;
+    constexpr int kThreads = WARPS * 32;
     using Raw = Word<T, V>;
-    constexpr int CW = kMayCluster ? kScanWarps : 1, CC = kMayCluster ? kMaxCluster : 1;
-    __shared__ Quad s_carry[kScanWarps][LC], s_A[2][CW][LC], s_H[2][CW][LC];
+    constexpr int CW = kMayCluster ? WARPS : 1, CC = kMayCluster ? kMaxCluster : 1;
+    __shared__ Quad s_carry[WARPS][LC], s_A[2][CW][LC], s_H[2][CW][LC];
     __shared__ float4 s_rA[2][CC][LC], s_rH[2][CC][LC];
     extern __shared__ __align__(16) unsigned char s_raw[];
     Raw *const slots = reinterpret_cast<Raw *>(s_raw) + threadIdx.x;   // [stage][tensor][step][thread]
@@ -230,7 +233,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) channel_kernel(const ScanArgs
     const int rank = kMayCluster && cluster > 1 ? int(blockIdx.x) % cluster : 0;
     const int64_t tile = blockIdx.x / unsigned(cluster);
     const int64_t steps = s.steps, stride = int64_t(tg) * (TL * S) * cluster;
-    const int64_t c = ((tile * (kScanWarps >> s.groups_log) + ct) * LC + cl) * V;
+    const int64_t c = ((tile * (WARPS >> s.groups_log) + ct) * LC + cl) * V;
     const bool valid = c < s.channels;
     const int64_t co = valid ? c / s.inner : 0, ci = valid ? c - co * s.inner : 0;
     const int64_t t0 = (int64_t(rank) * tg + group) * (TL * S) + tl * S;   // the thread's first step
@@ -253,8 +256,8 @@ __global__ void __launch_bounds__(kScanThreads, 2) channel_kernel(const ScanArgs
     int64_t left_to_load = valid ? steps - t0 : 0;   // steps from the first of the next round to load
     int in_slot = 0;
     auto load = [&]() {
-        const uint32_t to = smem_addr(slots + in_slot * (IN * S * kScanThreads));
-        constexpr uint32_t kWord = kScanThreads * sizeof(Raw);
+        const uint32_t to = smem_addr(slots + in_slot * (IN * S * kThreads));
+        constexpr uint32_t kWord = kThreads * sizeof(Raw);
         if (left_to_load > S) {
 #pragma unroll
             for (int k = 0; k < IN; ++k) {
@@ -294,7 +297,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) channel_kernel(const ScanArgs
         const int buf = int(round & 1);
         load();
         cp_async_wait<NS - 1>();
-        const Raw *const from = slots + slot * (IN * S * kScanThreads);
+        const Raw *const from = slots + slot * (IN * S * kThreads);
         slot = slot + 1 == NS ? 0 : slot + 1;
 
         // the maps of the steps.  Forward: p = u.  Backward: p = dh, q = what g is
@@ -306,11 +309,11 @@ __global__ void __launch_bounds__(kScanThreads, 2) channel_kernel(const ScanArgs
 #pragma unroll
             for (int j = 0; j < S; ++j) {
                 Pair gate[2], x[2], dh[2], hp[2];
-                const Raw g = from[j * kScanThreads], xr = from[(S + j) * kScanThreads];
+                const Raw g = from[j * kThreads], xr = from[(S + j) * kThreads];
                 g.get(gate);
                 xr.get(x);
                 if (BACK) {
-                    const Raw d = from[(2 * S + j) * kScanThreads], h = from[((IN - 1) * S + j) * kScanThreads];
+                    const Raw d = from[(2 * S + j) * kThreads], h = from[((IN - 1) * S + j) * kThreads];
                     d.get(dh);
                     h.get(hp);
                     if (!all && j == left - 1) hp[0] = state0.p[0], hp[1] = state0.p[1];
@@ -372,7 +375,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) channel_kernel(const ScanArgs
             for (int w = 0; w < group; ++w) state_through<LOGITS>(s_A[buf][w][cl], s_H[buf][w][cl], in_c);
         } else if (tg > 1) {
             if (round > 0 || group > 0) {
-                take_carry(warp);
+                take_carry<WARPS>(warp);
                 in_c = s_carry[warp][cl];
             }
             if (round + 1 < rounds || group < tg - 1) {
@@ -382,7 +385,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) channel_kernel(const ScanArgs
                     state_through<LOGITS>(A, H, out_c);
                     s_carry[next][cl] = out_c;
                 }
-                give_carry(next);
+                give_carry<WARPS>(next);
             }
         }
         if (TL > 1) state_through<LOGITS>(Ae, He, in_c);
@@ -582,14 +585,14 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
             }
         } else {
             if (tg > 1 && (round > 0 || group > 0)) {
-                take_carry(warp);
+                take_carry<kScanWarps>(warp);
                 in_c = s_carry[warp];
             }
             carry = through<LOGITS>(CA, CH, in_c);
             if (tg > 1 && (round + 1 < rounds || group < tg - 1)) {
                 const int next = warp - group + ((group + 1) & (tg - 1));
                 if (lane == 0) s_carry[next] = carry;
-                give_carry(next);
+                give_carry<kScanWarps>(next);
             }
         }
 
@@ -894,9 +897,9 @@ strided_kernel(const ScanArgs s, const int cluster) {
 
 // Warps that share a channel: as many as the steps go round, a warp taking `per` of
 // them in a round.  The logarithm.
-int groups_for(int64_t steps, int64_t per) {
+int groups_for(int64_t steps, int64_t per, int warps = kScanWarps) {
     int log = 0;
-    while (log < 3 && (per << log) < steps) ++log;
+    while ((1 << log) < warps && (per << log) < steps) ++log;
     return log;
 }
 // CTAs that share channels: while the GPU holds two of `tiles` CTAs on an SM, and the
@@ -907,29 +910,34 @@ int cluster_for(int64_t tiles, int64_t steps, int64_t per) {
     return cluster;
 }
 
-template <typename T, bool BACK, int LC, bool LOGITS>
+template <typename T, bool BACK, int LC, int WARPS, bool LOGITS>
 cudaError_t launch_channels(ScanArgs &s, int64_t tiles, int cluster, cudaStream_t stream) {
-    const auto kernel = channel_kernel<T, BACK, LC, LOGITS>;
-    constexpr size_t smem = size_t(kStages) * kStageBytes * kScanThreads;
+    const auto kernel = channel_kernel<T, BACK, LC, WARPS, LOGITS>;
+    constexpr size_t smem = size_t(kStages) * kStageBytes * WARPS * 32;
     const cudaError_t e = allow_smem(kernel, smem);
     if (e != cudaSuccess) return e;
     if (tiles * cluster > INT32_MAX) return cudaErrorNotSupported;
-    return launch_ex(kernel, dim3(unsigned(tiles * cluster)), dim3(kScanThreads), smem, stream, unsigned(cluster), true, s, cluster);
+    return launch_ex(kernel, dim3(unsigned(tiles * cluster)), dim3(WARPS * 32), smem, stream, unsigned(cluster), true, s, cluster);
 }
 template <typename T, bool BACK, bool LOGITS>
 cudaError_t launch_channels(ScanArgs &s, cudaStream_t stream) {
     constexpr int S = kStageBytes / ((BACK ? 4 : 2) * 4 * int(sizeof(T)));
-    const auto tiles = [&](int lanes) {
-        s.groups_log = groups_for(s.steps, S * (32 / lanes));
-        const int64_t per = int64_t(lanes) * 4 * (kScanWarps >> s.groups_log);
+    const auto tiles = [&](int lanes, int warps) {
+        s.groups_log = groups_for(s.steps, S * (32 / lanes), warps);
+        const int64_t per = int64_t(lanes) * 4 * (warps >> s.groups_log);
         return (s.channels + per - 1) / per;
     };
-    // whole warps side by side where that fills the GPU; else 8 lanes (64 or 128 bytes side
-    // by side) and later steps in the others
-    const int64_t wide = tiles(32);
-    if (wide >= int64_t(3) * sm_count()) return launch_channels<T, BACK, 32, LOGITS>(s, wide, 1, stream);
-    const int64_t narrow = tiles(8);
-    return launch_channels<T, BACK, 8, LOGITS>(s, narrow, cluster_for(narrow, s.steps, int64_t(S * 4) << s.groups_log), stream);
+    // whole warps side by side where that fills the GPU
+    const int64_t wide = tiles(32, kScanWarps);
+    if (wide >= int64_t(3) * sm_count()) return launch_channels<T, BACK, 32, kScanWarps, LOGITS>(s, wide, 1, stream);
+    // else fewer lanes, and later steps in the others: 128 bytes side by side (of 64 at a
+    // time memory gives two thirds as much: 4 x 16384 x 2048 bf16 270 us against 172)
+    if (sizeof(T) == 2) {
+        const int64_t middle = tiles(16, 16);
+        if (middle * 5 >= int64_t(4) * sm_count()) return launch_channels<T, BACK, 16, 16, LOGITS>(s, middle, 1, stream);
+    }
+    const int64_t narrow = tiles(8, kScanWarps);
+    return launch_channels<T, BACK, 8, kScanWarps, LOGITS>(s, narrow, cluster_for(narrow, s.steps, int64_t(S * 4) << s.groups_log), stream);
 }
 
 template <typename T, bool BACK, bool LOGITS>
