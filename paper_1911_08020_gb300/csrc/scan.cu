@@ -451,9 +451,11 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) channel_kernel(const S
 // 512 bytes side by side; lanes are put together by shuffles, warps and CTAs as above.
 template <typename T, bool BACK, bool LOGITS>
 __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, const int cluster) {
-    constexpr int V = kPerGranule<T>, IN = BACK ? 4 : 2, J = 16 / V / (BACK ? 2 : 1);
+    constexpr int V = kPerGranule<T>, IN = BACK ? 4 : 2, J = kStageBytes / (IN * 16), NS = kStages;
     __shared__ float2 s_map[2][kScanWarps], s_remote[2][kMaxCluster];
     __shared__ float s_carry[kScanWarps];
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    uint4 *const slots = reinterpret_cast<uint4 *>(s_raw) + threadIdx.x;   // [stage][tensor][granule][thread]
 
     pdl_launch_dependents();
     if (cluster > 1) cluster_arrive();
@@ -462,7 +464,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
     const int rank = cluster > 1 ? int(blockIdx.x) % cluster : 0;
     const int64_t row = (blockIdx.x / unsigned(cluster)) * int64_t(kScanWarps >> s.groups_log) + (warp >> s.groups_log);
     const bool valid = row < s.channels;
-    const int64_t steps = s.steps;
+    const int steps = int(s.steps);   // (2^30 at most)
     const Operand *const ins[4] = {&s.gate, &s.x, &s.dh, &s.before};
     const T *in[IN];
 #pragma unroll
@@ -470,45 +472,70 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
     T *const out0 = static_cast<T *>(const_cast<void *>(s.out[0].p)) + (valid ? row * s.out[0].ld : 0);
     T *const out1 = BACK ? static_cast<T *>(const_cast<void *>(s.out[1].p)) + (valid ? row * s.out[1].ld : 0) : nullptr;
     const int head = row_head<T>(in[0]);
-    const int64_t granules = valid ? row_granules<T>(head, steps) : 0;
-    const int64_t most = (steps + V - 1) / V + 1;   // of any row
-    const int64_t stride = int64_t(tg) * (32 * J) * cluster, rounds = (most + stride - 1) / stride;
-    // the first step of the thread's j-th granule in a round
-    auto first_step = [&](int64_t round, int j) {
-        const int64_t w = round * stride + (int64_t(rank) * tg + group) * (32 * J) + j * 32 + lane;
-        return (w >= granules ? steps : (BACK ? granules - 1 - w : w) * V - head);
+    const int granules = valid ? int(row_granules<T>(head, steps)) : 0;
+    const int most = (steps + V - 1) / V + 1;   // of any row
+    const int stride = tg * (32 * J) * cluster, rounds = (most + stride - 1) / stride;
+    const int w0 = (rank * tg + group) * (32 * J) + lane;
+    // the first step of the thread's j-th granule in a round (`steps`: there is none)
+    auto first_step = [&](int round, int j) {
+        const int w = w0 + round * stride + j * 32;
+        return w >= granules ? steps : (BACK ? granules - 1 - w : w) * V - head;
     };
-
-    uint4 raw[IN][J];
-    float edge[J];   // backward: the state before the granule's first step
-    auto load = [&](int64_t round) {
+    auto whole = [&](int t) { return t >= 0 && t <= steps - V; };
+    int next = 0, in_slot = 0;   // the next round to load, and where to
+    auto load = [&]() {
+        const uint32_t to = smem_addr(slots + in_slot * (IN * J * kScanThreads));
+        if (next < rounds) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int64_t t = first_step(round, j);
-            if (t >= 0 && t + V <= steps) {
+            for (int j = 0; j < J; ++j) {
+                const int t = first_step(next, j);
+                if (!whole(t)) continue;
 #pragma unroll
-                for (int k = 0; k < IN; ++k) raw[k][j] = *reinterpret_cast<const uint4 *>(in[k] + t);
-            } else if (t < steps) {
-#pragma unroll
-                for (int k = 0; k < IN; ++k) raw[k][j] = load_granule<T, false>(in[k], t, steps, 0.0f);
+                for (int k = 0; k < IN; ++k) cp_async_word<16>(to + (k * J + j) * (kScanThreads * 16), in[k] + t);
             }
-            if (BACK && t < steps) edge[j] = t > 0 ? widen(in[IN - 1][t - 1]) : 0.0f;
         }
+        cp_async_commit();
+        ++next;
+        in_slot = in_slot + 1 == NS ? 0 : in_slot + 1;
     };
     pdl_wait_previous();
-    load(0);
+#pragma unroll
+    for (int r = 0; r < NS - 1; ++r) load();
     float carry = valid && s.first != nullptr ? s.first[row] : 0.0f;
     const float state0 = BACK && valid && s.h0 != nullptr ? s.h0[row] : 0.0f;
     if (cluster > 1) cluster_wait();
 
-    for (int64_t round = 0; round < rounds; ++round) {
-        const int buf = int(round & 1);
+    int slot = 0;
+    for (int round = 0; round < rounds; ++round) {
+        const int buf = round & 1;
+        // backward, the state before a warp's last granule, which another warp has
+        float edge = 0.0f;
+        if (BACK && lane == 31) {
+            const int t = first_step(round, J - 1);
+            if (t > 0 && t < steps) edge = widen(in[IN - 1][t - 1]);
+        }
+        load();
+        cp_async_wait<NS - 1>();
+        uint4 raw[IN][J];
+        {
+            const uint4 *const from = slots + slot * (IN * J * kScanThreads);
+            slot = slot + 1 == NS ? 0 : slot + 1;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int t = first_step(round, j);
+#pragma unroll
+                for (int k = 0; k < IN; ++k) {
+                    raw[k][j] = from[(k * J + j) * kScanThreads];
+                    if (!whole(t) && t < steps) raw[k][j] = load_granule<T, false>(in[k], t, steps, 0.0f);
+                }
+            }
+        }
         float a[J][V], p[J][V], q[BACK ? J : 1][V], rest[BACK ? J : 1][V];
         float Ae[J], He[J], At[J], Ht[J];   // of the lanes before, of the 32 granules
         float CA = 1.0f, CH = 0.0f;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            const int64_t t = first_step(round, j);
+            const int t = first_step(round, j);
             Pair gate[V / 2], x[V / 2];
             float dh[V], h[V];
             unpack(raw[0][j], gate);
@@ -516,9 +543,21 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
             if (BACK) {
                 unpack(raw[IN - 2][j], dh);
                 unpack(raw[IN - 1][j], h);
+                // the states before: the last of the granule before is the next lane's
+                float last[2];
+                {
+                    float all[V];
+                    unpack(raw[IN - 1][j], all);
+                    last[0] = all[V - 1];
+                    unpack(raw[IN - 1][j + 1 < J ? j + 1 : j], all);
+                    last[1] = all[V - 1];
+                }
+                const float across = __shfl_sync(~0u, last[1], 0);
+                float before = __shfl_down_sync(~0u, last[0], 1);
+                if (lane == 31) before = j + 1 < J ? across : edge;
 #pragma unroll
-                for (int e = V - 1; e > 0; --e) h[e] = t + e == 0 ? state0 : h[e - 1];   // the states before
-                h[0] = t == 0 ? state0 : edge[j];
+                for (int e = V - 1; e > 0; --e) h[e] = t + e == 0 ? state0 : h[e - 1];
+                h[0] = t == 0 ? state0 : before;
             }
 #pragma unroll
             for (int e = 0; e < V; e += 2) {
@@ -536,10 +575,10 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
                     p[j][e] = low(u), p[j][e + 1] = high(u);
                 }
             }
-            if (t < 0 || t + V > steps) {
+            if (!whole(t)) {
 #pragma unroll
                 for (int e = 0; e < V; ++e)
-                    if (t + e < 0 || t + e >= steps) a[j][e] = 1.0f, p[j][e] = 0.0f;
+                    if (t + e < 0 || t >= steps - e) a[j][e] = 1.0f, p[j][e] = 0.0f;
             }
             float A = 1.0f, H = 0.0f;
 #pragma unroll
@@ -559,8 +598,6 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
             CH = through<LOGITS>(At[j], Ht[j], CH);
             CA *= At[j];
         }
-        if (round + 1 < rounds) load(round + 1);
-
         float in_c = carry;
         if (cluster > 1) {
             if (lane == 0) s_map[buf][warp] = make_float2(CA, CH);
@@ -599,7 +636,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
         // the steps again, from that carry
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            const int64_t t = first_step(round, j);
+            const int t = first_step(round, j);
             float at = through<LOGITS>(Ae[j], He[j], in_c), o0[V], o1[V];
             in_c = through<LOGITS>(At[j], Ht[j], in_c);
 #pragma unroll
@@ -622,6 +659,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
     }
     // (of the last warp's steps, or with a cluster everyone's)
     if (s.last != nullptr && valid && rank == 0 && group == tg - 1 && lane == 0) s.last[row] = carry;
+    cp_async_wait<0>();
 }
 
 // ---- anything else, an element at a time ----
@@ -942,13 +980,23 @@ cudaError_t launch_channels(ScanArgs &s, cudaStream_t stream) {
 
 template <typename T, bool BACK, bool LOGITS>
 cudaError_t launch_rows(ScanArgs &s, cudaStream_t stream) {
-    constexpr int64_t per = 32 * 16 / (BACK ? 2 : 1);
-    s.groups_log = 0;
-    while (s.groups_log < 3 && (per << s.groups_log) < s.steps && (s.channels << s.groups_log) < int64_t(4) * kScanWarps * sm_count()) ++s.groups_log;
-    const int64_t rows = kScanWarps >> s.groups_log, tiles = (s.channels + rows - 1) / rows;
+    constexpr int64_t per = 32 * (kStageBytes / ((BACK ? 4 : 2) * 16)) * kPerGranule<T>;   // steps of a warp in a round
+    constexpr size_t smem = size_t(kStages) * kStageBytes * kScanThreads;
+    const auto kernel = row_kernel<T, BACK, LOGITS>;
+    const cudaError_t e = allow_smem(kernel, smem);
+    if (e != cudaSuccess) return e;
+    // warps that share a row: the fewest rounds of all CTAs one after the other, with two
+    // rounds' time for a CTA to begin
+    const auto tiles_of = [&](int log) { return (s.channels + (kScanWarps >> log) - 1) / (kScanWarps >> log); };
+    int64_t least = INT64_MAX;
+    for (int log = 0; log < 4; ++log) {
+        const int64_t waves = (tiles_of(log) + 2 * sm_count() - 1) / (2 * sm_count()), rounds = (s.steps + (per << log) - 1) / (per << log);
+        if (waves * (rounds + 2) < least) least = waves * (rounds + 2), s.groups_log = log;
+    }
+    const int64_t tiles = tiles_of(s.groups_log);
     const int cluster = s.groups_log < 3 ? 1 : cluster_for(tiles, s.steps, per << s.groups_log);
     if (tiles * cluster > INT32_MAX) return cudaErrorNotSupported;
-    return launch_ex(row_kernel<T, BACK, LOGITS>, dim3(unsigned(tiles * cluster)), dim3(kScanThreads), 0, stream, unsigned(cluster), true, s, cluster);
+    return launch_ex(kernel, dim3(unsigned(tiles * cluster)), dim3(kScanThreads), smem, stream, unsigned(cluster), true, s, cluster);
 }
 
 template <typename T, bool BACK, bool STAGED, bool LOGITS>
