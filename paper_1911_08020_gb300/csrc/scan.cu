@@ -692,6 +692,10 @@ strided_kernel(const ScanArgs s, const int cluster) {
     const int inner = s.inner;
     const int rows = STAGED ? 32 / inner : 0;                  // rows of a tile
     const int run = kRun * inner, pitch = run + inner;
+    // e / inner for e < 4096 and inner < 8: 65536 / inner rounded up is off by less than one
+    // part in 4096 * 7 / 65536 of the quotient's unit
+    const uint32_t part = STAGED ? (65536u + inner - 1) / inner : 0;
+    auto over_inner = [&](int e) { return int(uint32_t(e) * part >> 16); };
 
     // the thread's channels
     int64_t c;
@@ -722,10 +726,8 @@ strided_kernel(const ScanArgs s, const int cluster) {
         if (STAGED) {
 #pragma unroll
             for (int j = 0; j < S; ++j) {
-                const int e = tid + j * kScanThreads;
-                const int r = inner == 1 ? e / kRun : e / run, q = e - r * run;
-                const int tl = inner == 1 ? q : q / inner, i = q - tl * inner;
-                const int64_t t = first + tl, o = tile * rows + r;
+                const int e = tid + j * kScanThreads, f = over_inner(e), r = f / kRun, i = e - f * inner;
+                const int64_t t = first + f % kRun, o = tile * rows + r;
                 const bool on = r < rows && o < s.outer && t < steps;
 #pragma unroll
                 for (int k = 0; k < IN; ++k) {
@@ -771,8 +773,7 @@ strided_kernel(const ScanArgs s, const int cluster) {
             if (round > 0) __syncthreads();   // the tile has been written out
 #pragma unroll
             for (int j = 0; j < S; ++j) {
-                const int e = tid + j * kScanThreads;
-                const int r = inner == 1 ? e / kRun : e / run, q = e - r * run;
+                const int e = tid + j * kScanThreads, r = over_inner(e) / kRun, q = e - r * run;
                 if (r < rows) {
 #pragma unroll
                     for (int k = 0; k < IN; ++k) {
@@ -913,10 +914,8 @@ strided_kernel(const ScanArgs s, const int cluster) {
             const int64_t first = (round * cluster + rank) * L;
 #pragma unroll 4
             for (int j = 0; j < S; ++j) {
-                const int e = tid + j * kScanThreads;
-                const int r = inner == 1 ? e / kRun : e / run, q1 = e - r * run;
-                const int tl = inner == 1 ? q1 : q1 / inner, i = q1 - tl * inner;
-                const int64_t t = first + tl, o = tile * rows + r;
+                const int e = tid + j * kScanThreads, f = over_inner(e), r = f / kRun, i = e - f * inner, q1 = e - r * run;
+                const int64_t t = first + f % kRun, o = tile * rows + r;
                 if (r < rows && o < s.outer && t < steps) {
 #pragma unroll
                     for (int k = 0; k < OUT; ++k)
