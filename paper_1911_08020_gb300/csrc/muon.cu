@@ -435,21 +435,21 @@ __device__ __forceinline__ Target target(const StepArgs &s, const Matrix &x, int
     return t;
 }
 
-// What becomes of rows i0 .. i0 + 32 and columns j0 .. j0 + 32 of a product, `acc` being
-// the accumulator's address.
+// What rows i0 .. i0 + 32 and columns j0 .. j0 + 32 of a product are put together with.
+// All of it is loaded before the first store: no load can be moved over a store that
+// might meet it, and waiting for each in turn would take longer than the product.
 template <int P, int OP>
-__device__ __forceinline__ void finish(const float decay, const Target &x, int i0, int j0, uint32_t acc, const Turn &turn) {
-    constexpr bool two = P == 3, apply = OP == kApply || OP == kLast;
-    const int lane = threadIdx.x & 31, oct = lane & 3, sub = lane >> 2;
-    const int rows = x.rows, cols = x.cols, ld = x.ld;
-    if (i0 >= rows || j0 >= cols || (!apply && j0 > i0 + 31)) return;
-    const int j = j0 + 8 * oct;   // this lane's columns after the turn (rows are as long as a multiple of 64 numbers)
-    // All loads come before the first store: none can be moved over a store that might
-    // meet it, and waiting for each in turn would take longer than the product.
+struct Loads {
     uint4 hi[4], lo[4];
     float di[4], dj[8];              // of the diagonal: of this lane's rows, of its columns
     float p[OP == kLast ? 32 : 1];   // parameters: of this lane's rows and columns, or (unaligned) of column `lane`
-    if (OP != kGram) {
+
+    __device__ __forceinline__ void get(const Target &x, int i0, int j0) {
+        constexpr bool two = P == 3, apply = OP == kApply || OP == kLast;
+        const int lane = threadIdx.x & 31, oct = lane & 3, sub = lane >> 2;
+        const int rows = x.rows, cols = x.cols, ld = x.ld;
+        if (OP == kGram || i0 >= rows || j0 >= cols || (!apply && j0 > i0 + 31)) return;
+        const int j = j0 + 8 * oct;   // this lane's columns (rows are as long as a multiple of 64 numbers)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int i = min(i0 + 8 * q + sub, rows - 1);
@@ -464,19 +464,31 @@ __device__ __forceinline__ void finish(const float decay, const Target &x, int i
 #pragma unroll
             for (int e = 0; e < 8; ++e) dj[e] = x.col[min(j + e, cols - 1)];
         }
-    }
-    if (OP == kLast && x.vector) {
+        if (OP == kLast && x.vector) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float4 *from = reinterpret_cast<const float4 *>(x.p + int64_t(min(i0 + 8 * q + sub, rows - 1)) * cols + min(j, cols - 8));
-            const float4 p0 = from[0], p1 = from[1];
-            float *const to = p + (OP == kLast ? 8 * q : 0);
-            to[0] = p0.x, to[1] = p0.y, to[2] = p0.z, to[3] = p0.w, to[4] = p1.x, to[5] = p1.y, to[6] = p1.z, to[7] = p1.w;
+            for (int q = 0; q < 4; ++q) {
+                const float4 *from = reinterpret_cast<const float4 *>(x.p + int64_t(min(i0 + 8 * q + sub, rows - 1)) * cols + min(j, cols - 8));
+                const float4 p0 = from[0], p1 = from[1];
+                float *const to = p + (OP == kLast ? 8 * q : 0);
+                to[0] = p0.x, to[1] = p0.y, to[2] = p0.z, to[3] = p0.w, to[4] = p1.x, to[5] = p1.y, to[6] = p1.z, to[7] = p1.w;
+            }
+        } else if (OP == kLast) {
+#pragma unroll
+            for (int r = 0; r < 32; ++r) p[OP == kLast ? r : 0] = x.p[int64_t(min(i0 + r, rows - 1)) * cols + min(j0 + lane, cols - 1)];
         }
-    } else if (OP == kLast) {
-#pragma unroll
-        for (int r = 0; r < 32; ++r) p[OP == kLast ? r : 0] = x.p[int64_t(min(i0 + r, rows - 1)) * cols + min(j0 + lane, cols - 1)];
     }
+};
+
+// What becomes of them, `acc` being the accumulator's address.
+template <int P, int OP>
+__device__ __forceinline__ void finish(const float decay, const Target &x, const Loads<P, OP> &in, int i0, int j0, uint32_t acc, const Turn &turn) {
+    constexpr bool two = P == 3, apply = OP == kApply || OP == kLast;
+    const int lane = threadIdx.x & 31, oct = lane & 3, sub = lane >> 2;
+    const int rows = x.rows, cols = x.cols, ld = x.ld;
+    if (i0 >= rows || j0 >= cols || (!apply && j0 > i0 + 31)) return;
+    const int j = j0 + 8 * oct;   // this lane's columns after the turn
+    const uint4 (&hi)[4] = in.hi, (&lo)[4] = in.lo;
+    const float (&di)[4] = in.di, (&dj)[8] = in.dj;
     uint32_t v[32];
     tmem_ld32(acc, v);
     tmem_ld_wait();
@@ -585,7 +597,7 @@ __device__ __forceinline__ void finish(const float decay, const Target &x, int i
             const int64_t at = int64_t(i) * cols + j;
             float c[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) c[e] = p[OP == kLast ? 8 * q + e : 0] * decay - x.size * r[e];
+            for (int e = 0; e < 8; ++e) c[e] = in.p[OP == kLast ? 8 * q + e : 0] * decay - x.size * r[e];
             reinterpret_cast<float4 *>(x.p + at)[0] = make_float4(c[0], c[1], c[2], c[3]);
             reinterpret_cast<float4 *>(x.p + at)[1] = make_float4(c[4], c[5], c[6], c[7]);
             if (x.copy != nullptr) *reinterpret_cast<uint4 *>(x.copy + at) = pack(c);
@@ -597,7 +609,7 @@ __device__ __forceinline__ void finish(const float decay, const Target &x, int i
         for (int r = 0; r < 32; ++r) {
             if (i0 + r >= rows || j0 + lane >= cols) continue;
             const int64_t at = int64_t(i0 + r) * cols + j0 + lane;
-            const float v = p[OP == kLast ? r : 0] * decay - x.size * turn.one(r, lane);
+            const float v = in.p[OP == kLast ? r : 0] * decay - x.size * turn.one(r, lane);
             x.p[at] = v;
             if (x.copy != nullptr) x.copy[at] = __float2bfloat16_rn(v);
         }
@@ -638,8 +650,18 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
     if (CG == 2) pair_meet();   // the other CTA's barriers stand before anything arrives there
     tc_fence_after_sync();
     const uint32_t tmem = *s_tmem;
+    // (the plan's tables do not change: what a CTA begins with is fetched while the kernel before ends)
     const int t0 = first[unit], t1 = first[unit + 1];
     bool ok = true;
+    int known = -1;   // the matrix whose maps the copying thread has at hand
+    if (tid == 0 && t0 < t1) {
+        known = tiles[t0].matrix;
+        const Operands o = operands<OP>(s.matrices[known], buf);
+        for (int q = 0; q < NP; ++q) {
+            acquire_map(&o.a[q]), acquire_map(&o.b[q]);
+            prefetch_tensormap(&o.a[q]), prefetch_tensormap(&o.b[q]);
+        }
+    }
     pdl_wait_previous();
 
     if (warp == 0) {
@@ -648,7 +670,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
             int stage = 0;
             uint32_t parity = 0;
             int64_t issued = 0;
-            int known = -1;   // the matrix of the last tile
             for (int t = t0; t < t1 && ok; ++t) {
                 const Tile tile = tiles[t];
                 const Matrix &x = s.matrices[tile.matrix];
@@ -743,17 +764,21 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
             const Tile tile = tiles[t];
             const Matrix &x = s.matrices[tile.matrix];
             if (!s.active[tile.matrix]) continue;
-            const int half = used & 1;
+            const int half = used & 1, i0 = tile.row + rank * kBM + quarter * 32;
+            const Target to = target<OP>(s, x, buf);
+            Loads<P, OP> in;
+            in.get(to, i0, tile.col + c0);   // (while the product is made)
             if (!__all_sync(~0u, mbar_wait(&ready[half], uint32_t(used / 2) & 1u))) {
                 ok = false;
                 break;
             }
             tc_fence_after_sync();
             const uint32_t at = tmem + half * BN + (uint32_t(quarter * 32) << 16);
-            const int i0 = tile.row + rank * kBM + quarter * 32;
-            const Target to = target<OP>(s, x, buf);
 #pragma unroll 1
-            for (int c = c0; c < c0 + BN / 2; c += 32) finish<P, OP>(s.decay, to, i0, tile.col + c, at + c, turn);
+            for (int c = c0; c < c0 + BN / 2; c += 32) {
+                if (c > c0) in.get(to, i0, tile.col + c);
+                finish<P, OP>(s.decay, to, in, i0, tile.col + c, at + c, turn);
+            }
             // the accumulator has been read
             tc_fence_before_sync();
             __syncwarp();
@@ -780,23 +805,25 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
 struct Schedule {
     std::vector<Tile> tiles;
     std::vector<int32_t> first;
-    int cg = 1;
+    int bn = 0;
     int64_t longest = 0;
     int64_t o_tiles = 0, o_first = 0;   // in the plan's memory
     int32_t units() const { return int32_t(first.size()) - 1; }
 };
 
-// The forms of a product: tiles of 256 x 256 by pairs of CTAs, or of 128 x 128 by one.
+// The forms of a product: tiles of 256 x 256 by pairs of CTAs, or of 128 x 128 or 64 by one.
 struct Form {
     int bm, bn, cg;
 };
-constexpr Form kPairs = {256, 256, 2}, kSingles = {128, 128, 1};
+constexpr Form kForms[] = {{256, 256, 2}, {128, 128, 1}, {128, 64, 1}};
 
 // Clocks of a tile, about: a stage by what it moves through shared memory and the
 // products that it feeds (measured), and what a tile waits for at its ends.
-int64_t tile_cost(int64_t depth, bool three, int cg) {
+int64_t tile_cost(int64_t depth, bool three, int bn) {
     const int64_t stages = (depth + kBK - 1) / kBK;
-    return cg == 2 ? stages * (three ? 1600 : 560) + 5000 : stages * (three ? 1350 : 600) + 3500;
+    if (bn == 256) return stages * (three ? 1600 : 560) + 5000;
+    if (bn == 128) return stages * (three ? 1350 : 600) + 3500;
+    return stages * (three ? 950 : 420) + 2500;
 }
 
 Schedule make_schedule(const std::vector<Matrix> &all, Op op, const Form &form, bool three, int units) {
@@ -809,14 +836,14 @@ Schedule make_schedule(const std::vector<Matrix> &all, Op op, const Form &form, 
         const Matrix &x = all[t];
         if (x.n == 0) continue;
         const int rows = op == kApply ? x.rows : x.n, cols = op == kApply ? x.cols : x.n;
-        const int64_t depth = op == kGram ? std::max(x.rows, x.cols) : x.n, cost = tile_cost(depth, three, form.cg);
+        const int64_t depth = op == kGram ? std::max(x.rows, x.cols) : x.n, cost = tile_cost(depth, three, form.bn);
         for (int col = 0; col < cols; col += form.bn)
             for (int row = 0; row < rows; row += form.bm)
                 if (op == kApply || col < row + form.bm) items.push_back({cost, {int32_t(t), row, col}});
     }
     std::stable_sort(items.begin(), items.end(), [](const Item &a, const Item &b) { return a.cost > b.cost; });
     Schedule s;
-    s.cg = form.cg;
+    s.bn = form.bn;
     units = int(std::min<int64_t>(units, int64_t(items.size())));
     std::vector<std::vector<Tile>> mine(units);
     using Load = std::pair<int64_t, int>;
@@ -849,8 +876,9 @@ cudaError_t launch_product(const StepArgs &s, const Schedule &sch, const char *m
 }
 template <int OP>
 cudaError_t launch_product(const StepArgs &s, const Schedule &sch, const char *memory, bool three, int buf, cudaStream_t stream) {
-    if (sch.cg == 2) return three ? launch_product<3, 256, 2, OP>(s, sch, memory, buf, stream) : launch_product<1, 256, 2, OP>(s, sch, memory, buf, stream);
-    return three ? launch_product<3, 128, 1, OP>(s, sch, memory, buf, stream) : launch_product<1, 128, 1, OP>(s, sch, memory, buf, stream);
+    if (sch.bn == 256) return three ? launch_product<3, 256, 2, OP>(s, sch, memory, buf, stream) : launch_product<1, 256, 2, OP>(s, sch, memory, buf, stream);
+    if (sch.bn == 128) return three ? launch_product<3, 128, 1, OP>(s, sch, memory, buf, stream) : launch_product<1, 128, 1, OP>(s, sch, memory, buf, stream);
+    return three ? launch_product<3, 64, 1, OP>(s, sch, memory, buf, stream) : launch_product<1, 64, 1, OP>(s, sch, memory, buf, stream);
 }
 
 // Pairs of CTAs that the device holds at a time.
@@ -952,8 +980,10 @@ darb_status_t build_plan(darb_muon_s *plan, int32_t n, const int64_t *rows, cons
     const int sms = sm_count(), pairs = pair_room(three);
     for (int op = kGram; op <= kApply; ++op) {
         // the form whose busiest CTA has least to do
-        Schedule wide = make_schedule(plan->matrices, Op(op), kPairs, three, pairs), narrow = make_schedule(plan->matrices, Op(op), kSingles, three, sms);
-        plan->schedules[op] = wide.longest <= narrow.longest ? std::move(wide) : std::move(narrow);
+        for (const Form &f : kForms) {
+            Schedule s = make_schedule(plan->matrices, Op(op), f, three, f.cg == 2 ? pairs : sms);
+            if (plan->schedules[op].bn == 0 || s.longest < plan->schedules[op].longest) plan->schedules[op] = std::move(s);
+        }
     }
     // the tables, then the numbers of every matrix
     int64_t size = 0;
