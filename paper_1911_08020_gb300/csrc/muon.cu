@@ -203,7 +203,7 @@ __device__ __forceinline__ void split(float v, __half &hi, __half &lo) {
 }
 
 template <typename G>
-__global__ void __launch_bounds__(kElemThreads) start_kernel(const StepArgs a, const __grid_constant__ GradArgs grads) {
+__global__ void __launch_bounds__(kElemThreads, sizeof(G) == 4 ? 4 : 3) start_kernel(const StepArgs a, const __grid_constant__ GradArgs grads) {
     pdl_launch_dependents();
     const Part part = a.parts[blockIdx.x];
     const Matrix &x = a.matrices[part.matrix];
@@ -413,7 +413,7 @@ struct Target {
     __nv_bfloat16 *copy;
     int32_t rows, cols, ld;
     float size;
-    bool vector;                   // parameters eight at a time
+    bool vector;                   // parameters four at a time
 };
 template <int OP>
 __device__ __forceinline__ Target target(const StepArgs &s, const Matrix &x, int buf) {
@@ -431,7 +431,7 @@ __device__ __forceinline__ Target target(const StepArgs &s, const Matrix &x, int
     else t.row = x.D;
     t.rows = x.rows, t.cols = x.cols, t.ld = x.ldx;
     t.p = x.p, t.copy = x.copy, t.size = s.lr * x.size;
-    t.vector = x.cols % 8 == 0 && aligned16(x.p) && aligned16(x.copy);
+    t.vector = x.cols % 4 == 0 && aligned16(x.p) && (reinterpret_cast<uintptr_t>(x.copy) & 7) == 0;
     return t;
 }
 
@@ -467,8 +467,8 @@ struct Loads {
         if (OP == kLast && x.vector) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float4 *from = reinterpret_cast<const float4 *>(x.p + int64_t(min(i0 + 8 * q + sub, rows - 1)) * cols + min(j, cols - 8));
-                const float4 p0 = from[0], p1 = from[1];
+                const float *from = x.p + int64_t(min(i0 + 8 * q + sub, rows - 1)) * cols;
+                const float4 p0 = *reinterpret_cast<const float4 *>(from + min(j, cols - 4)), p1 = *reinterpret_cast<const float4 *>(from + min(j + 4, cols - 4));
                 float *const to = p + (OP == kLast ? 8 * q : 0);
                 to[0] = p0.x, to[1] = p0.y, to[2] = p0.z, to[3] = p0.w, to[4] = p1.x, to[5] = p1.y, to[6] = p1.z, to[7] = p1.w;
             }
@@ -593,14 +593,20 @@ __device__ __forceinline__ void finish(const float decay, const Target &x, const
             *reinterpret_cast<uint4 *>(x.out_lo + at) = l;
         } else if (!x.vector) {
             turn.set(8 * q + sub, oct, r);
-        } else if (j < cols) {
-            const int64_t at = int64_t(i) * cols + j;
-            float c[8];
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) c[e] = in.p[OP == kLast ? 8 * q + e : 0] * decay - x.size * r[e];
-            reinterpret_cast<float4 *>(x.p + at)[0] = make_float4(c[0], c[1], c[2], c[3]);
-            reinterpret_cast<float4 *>(x.p + at)[1] = make_float4(c[4], c[5], c[6], c[7]);
-            if (x.copy != nullptr) *reinterpret_cast<uint4 *>(x.copy + at) = pack(c);
+            for (int h = 0; h < 8; h += 4) {
+                if (j + h >= cols) continue;
+                const int64_t at = int64_t(i) * cols + j + h;
+                float c[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c[e] = in.p[OP == kLast ? 8 * q + h + e : 0] * decay - x.size * r[h + e];
+                *reinterpret_cast<float4 *>(x.p + at) = make_float4(c[0], c[1], c[2], c[3]);
+                if (x.copy != nullptr) {
+                    const __nv_bfloat162 b0 = __floats2bfloat162_rn(c[0], c[1]), b1 = __floats2bfloat162_rn(c[2], c[3]);
+                    *reinterpret_cast<uint2 *>(x.copy + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&b0), *reinterpret_cast<const uint32_t *>(&b1));
+                }
+            }
         }
     }
     __syncwarp();
