@@ -85,6 +85,7 @@ struct Part {
 };
 struct Tile {
     int32_t matrix, row, col;               // first row and column
+    int32_t width;                          // columns
 };
 
 struct StepArgs {
@@ -681,7 +682,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                 const Matrix &x = s.matrices[tile.matrix];
                 if (!s.active[tile.matrix]) continue;
                 const Operands o = operands<OP>(x, buf);
-                const int row = tile.row + rank * kBM, col = tile.col + rank * (BN / CG);
+                const bool wide = CG == 1 || tile.width == BN;   // (else half of the columns)
+                const int row = tile.row + rank * kBM, col = tile.col + rank * (wide ? BN / CG : BN / CG / 2);
                 if (tile.matrix != known) {
                     for (int q = 0; q < NP; ++q) acquire_map(&o.a[q]), acquire_map(&o.b[q]);
                     known = tile.matrix;
@@ -692,7 +694,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                         break;
                     }
                     // the first CTA's barrier counts the bytes of both
-                    if (rank == 0) mbar_arrive_expect_tx(&full[stage], CG * G::kStage);
+                    if (rank == 0) mbar_arrive_expect_tx(&full[stage], wide ? CG * G::kStage : CG * NP * (G::kABytes + G::kBBytes / 2));
                     const uint32_t bar = CG == 2 ? shared_of(&full[stage], 0) : smem_addr(&full[stage]);
                     unsigned char *to = stages + stage * G::kStage;
 #pragma unroll
@@ -701,8 +703,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                             pair_copy<CG>(to, &o.a[q], o.a_mn ? row + b : k, o.a_mn ? k : row + b, bar);
 #pragma unroll
                     for (int q = 0; q < NP; ++q)
+#pragma unroll
                         for (int b = 0; b < BN / CG; b += 64, to += kBox)
-                            pair_copy<CG>(to, &o.b[q], o.b_mn ? col + b : k, o.b_mn ? k : col + b, bar);
+                            if (wide || b < BN / CG / 2) pair_copy<CG>(to, &o.b[q], o.b_mn ? col + b : k, o.b_mn ? k : col + b, bar);
                     if (++stage == NS) stage = 0, parity ^= 1u;
                 }
             }
@@ -721,7 +724,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                 const Matrix &x = s.matrices[tile.matrix];
                 if (!s.active[tile.matrix]) continue;
                 const Operands o = operands<OP>(x, buf);
-                const uint32_t idesc = idesc_f16(CG * kBM, BN, o.a_mn, o.b_mn);
+                const uint32_t idesc = idesc_f16(CG * kBM, CG == 1 ? BN : tile.width, o.a_mn, o.b_mn);
                 // along the depth: rows of 128 bytes; along the tile: boxes of 64 columns, 8 deep atoms one after the other
                 const uint32_t a_lbo = o.a_mn ? kBox : 16, b_lbo = o.b_mn ? kBox : 16;
                 const uint32_t a_step = (o.a_mn ? 2048 : 32) >> 4, b_step = (o.b_mn ? 2048 : 32) >> 4;
@@ -763,14 +766,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
         __syncwarp();
     } else {
         // two warps for each quarter of the accumulator's rows, with half of the columns each
-        const int quarter = warp & 3, c0 = warp < 6 ? 0 : BN / 2;
+        const int quarter = warp & 3;
         const Turn turn = {reinterpret_cast<float4 *>(stages + NS * G::kStage) + (warp - 2) * (32 * 8)};
         int used = 0;
         for (int t = t0; t < t1; ++t) {
             const Tile tile = tiles[t];
             const Matrix &x = s.matrices[tile.matrix];
             if (!s.active[tile.matrix]) continue;
-            const int half = used & 1, i0 = tile.row + rank * kBM + quarter * 32;
+            const int half = used & 1, i0 = tile.row + rank * kBM + quarter * 32, columns = CG == 1 ? BN / 2 : tile.width / 2, c0 = warp < 6 ? 0 : columns;
             const Target to = target<OP>(s, x, buf);
             Loads<P, OP> in;
             in.get(to, i0, tile.col + c0);   // (while the product is made)
@@ -781,7 +784,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
             tc_fence_after_sync();
             const uint32_t at = tmem + half * BN + (uint32_t(quarter * 32) << 16);
 #pragma unroll 1
-            for (int c = c0; c < c0 + BN / 2; c += 32) {
+            for (int c = c0; c < c0 + columns; c += 32) {
                 if (c > c0) in.get(to, i0, tile.col + c);
                 finish<P, OP>(s.decay, to, in, i0, tile.col + c, at + c, turn);
             }
@@ -817,7 +820,8 @@ struct Schedule {
     int32_t units() const { return int32_t(first.size()) - 1; }
 };
 
-// The forms of a product: tiles of 256 x 256 by pairs of CTAs, or of 128 x 128 or 64 by one.
+// The forms of a product: tiles of 256 x 256 by pairs of CTAs (256 x 128 where that
+// evens out what the pairs have to do), or of 128 x 128 or 64 by one.
 struct Form {
     int bm, bn, cg;
 };
@@ -825,44 +829,82 @@ constexpr Form kForms[] = {{256, 256, 2}, {128, 128, 1}, {128, 64, 1}};
 
 // Clocks of a tile, about: a stage by what it moves through shared memory and the
 // products that it feeds (measured), and what a tile waits for at its ends.
-int64_t tile_cost(int64_t depth, bool three, int bn) {
+int64_t tile_cost(int64_t depth, bool three, int cg, int width) {
     const int64_t stages = (depth + kBK - 1) / kBK;
-    if (bn == 256) return stages * (three ? 1600 : 560) + 5000;
-    if (bn == 128) return stages * (three ? 1350 : 600) + 3500;
-    return stages * (three ? 950 : 420) + 2500;
+    if (cg == 2) return width == 256 ? stages * (three ? 1600 : 560) + 5000 : stages * (three ? 950 : 400) + 3500;
+    return width == 128 ? stages * (three ? 1350 : 600) + 3500 : stages * (three ? 950 : 420) + 2500;
+}
+
+struct Item {
+    int64_t cost, depth;
+    Tile tile;
+    int64_t unit = 0;
+};
+
+// Items, the longest first, each to the unit that is done first; the longest load.
+int64_t assign(std::vector<Item> &items, int units, std::vector<int64_t> &load) {
+    std::stable_sort(items.begin(), items.end(), [](const Item &a, const Item &b) { return a.cost > b.cost; });
+    load.assign(units, 0);
+    using Load = std::pair<int64_t, int>;
+    std::priority_queue<Load, std::vector<Load>, std::greater<Load>> queue;
+    for (int c = 0; c < units; ++c) queue.push({0, c});
+    int64_t longest = 0;
+    for (Item &i : items) {
+        Load l = queue.top();
+        queue.pop();
+        i.unit = l.second;
+        load[l.second] = l.first += i.cost;
+        longest = std::max(longest, l.first);
+        queue.push(l);
+    }
+    return longest;
 }
 
 Schedule make_schedule(const std::vector<Matrix> &all, Op op, const Form &form, bool three, int units) {
-    struct Item {
-        int64_t cost;
-        Tile tile;
-    };
     std::vector<Item> items;
     for (size_t t = 0; t < all.size(); ++t) {
         const Matrix &x = all[t];
         if (x.n == 0) continue;
         const int rows = op == kApply ? x.rows : x.n, cols = op == kApply ? x.cols : x.n;
-        const int64_t depth = op == kGram ? std::max(x.rows, x.cols) : x.n, cost = tile_cost(depth, three, form.bn);
+        const int64_t depth = op == kGram ? std::max(x.rows, x.cols) : x.n;
         for (int col = 0; col < cols; col += form.bn)
             for (int row = 0; row < rows; row += form.bm)
-                if (op == kApply || col < row + form.bm) items.push_back({cost, {int32_t(t), row, col}});
+                if (op == kApply || col < row + form.bm)
+                    items.push_back({tile_cost(depth, three, form.cg, form.bn), depth, {int32_t(t), row, col, form.bn}});
     }
-    std::stable_sort(items.begin(), items.end(), [](const Item &a, const Item &b) { return a.cost > b.cost; });
     Schedule s;
     s.bn = form.bn;
-    units = int(std::min<int64_t>(units, int64_t(items.size())));
-    std::vector<std::vector<Tile>> mine(units);
-    using Load = std::pair<int64_t, int>;
-    std::priority_queue<Load, std::vector<Load>, std::greater<Load>> queue;
-    for (int c = 0; c < units; ++c) queue.push({0, c});
-    for (const Item &i : items) {
-        Load l = queue.top();
-        queue.pop();
-        mine[l.second].push_back(i.tile);
-        l.first += i.cost;
-        s.longest = std::max(s.longest, l.first);
-        queue.push(l);
+    const int most = units;
+    std::vector<int64_t> load;
+    auto shared = [&] { return int(std::min<int64_t>(most, int64_t(items.size()))); };
+    s.longest = assign(items, shared(), load);
+    // the last tiles of the busiest pairs in halves, as long as that helps
+    for (int64_t tries = 0; form.cg == 2 && tries < 64 && tries * int64_t(items.size()) < 2000000; ++tries) {
+        std::vector<Item> next;
+        std::vector<char> halved(load.size(), 0);
+        for (auto i = items.rbegin(); i != items.rend(); ++i) {   // the shortest first
+            const int cols = op == kApply ? all[i->tile.matrix].cols : all[i->tile.matrix].n;
+            const bool busy = load[i->unit] * 100 > s.longest * 98 && !halved[i->unit] && i->tile.width == 256;
+            if (!busy) {
+                next.push_back(*i);
+                continue;
+            }
+            halved[i->unit] = 1;
+            for (int h = 0; h < 256; h += 128) {
+                Item half = *i;
+                half.cost = tile_cost(i->depth, three, 2, 128);
+                half.tile.col += h, half.tile.width = 128;
+                if (half.tile.col < cols && (op == kApply || half.tile.col < half.tile.row + form.bm)) next.push_back(half);
+            }
+        }
+        if (std::find(halved.begin(), halved.end(), 1) == halved.end()) break;
+        std::vector<int64_t> next_load;
+        const int64_t longest = assign(next, int(std::min<int64_t>(most, int64_t(next.size()))), next_load);
+        if (longest >= s.longest) break;
+        items = std::move(next), load = std::move(next_load), s.longest = longest;
     }
+    std::vector<std::vector<Tile>> mine(load.size());
+    for (const Item &i : items) mine[i.unit].push_back(i.tile);
     s.first.push_back(0);
     for (const auto &m : mine) {
         s.tiles.insert(s.tiles.end(), m.begin(), m.end());

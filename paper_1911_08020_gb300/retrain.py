@@ -7,6 +7,7 @@ back, one AdamW step updates the dense weights, and the layer is encoded again:
     darb_layer_norm -> darb_spmm -> darb_token_logprobs -> darb_token_logprobs_grad
       -> darb_layer_norm_grad -> darb_adamw_step -> darb_reencode
 
+(``states="muon"``: the weights take darb_muon_step, whose momentum is orthogonalised, and AdamW the vectors.)
 The products of the backward pass are plain dense ones (library calls).  The gradient of the layer's input
 is that of the pruned layer, whose dense form is the product with the identity.  The gradient of the weights
 passes the pruning straight through: that of a pruned weight is that of the weight at its place, so that
@@ -23,7 +24,8 @@ from . import darb
 
 
 class Head:
-    """Layer norm and a pruned output layer, trained with AdamW (states in 8 bits, or fp32)."""
+    """Layer norm and a pruned output layer, trained with AdamW (states in 8 bits, or fp32), or the weights with
+    orthogonalised momentum."""
 
     def __init__(self, vocab: int, features: int, block: int, lr: float = 2e-3, states: str = "e4m3", seed: int = 0):
         gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -32,7 +34,10 @@ class Head:
         self.gamma, self.beta = torch.ones(features, device="cuda"), torch.zeros(features, device="cuda")
         self.stored = self.W.to(torch.bfloat16)   # what is encoded
         self.handle = darb.darb_encode(self.stored, np.full(vocab, block, np.int32))
-        params = [self.W, self.gamma, self.beta]
+        params, copies, self.muon = [self.W, self.gamma, self.beta], [self.stored, None, None], None
+        if states == "muon":
+            self.muon = darb.darb_muon_create(params[:1], [torch.zeros_like(self.W)], copies=copies[:1])
+            params, copies = params[1:], None
         if states == "e4m3":
             def codes(p):
                 return torch.zeros(p.numel(), device=p.device).to(torch.float8_e4m3fn)
@@ -43,7 +48,7 @@ class Head:
             moments = [[codes(p) for p in params] for _ in range(2)] + [[scales(p) for p in params] for _ in range(2)]
         else:
             moments = [[torch.zeros_like(p) for p in params] for _ in range(2)]
-        self.plan = darb.darb_adamw_create(params, *moments, copies=[self.stored, None, None])
+        self.plan = darb.darb_adamw_create(params, *moments, copies=copies)
         self.lr, self.step = lr, 0
 
     def forward(self, h):
@@ -64,12 +69,15 @@ class Head:
         dW, dx = d_logits @ x.t(), darb.darb_spmm(self.handle, self.eye).t() @ d_logits
         _, d_gamma, d_beta = darb.darb_layer_norm_grad(dx, h, self.gamma, mean, rstd, dim=0, dx=dx)
         self.step += 1
-        darb.darb_adamw_step(self.plan, [dW, d_gamma, d_beta], self.step, self.lr)
+        if self.muon is not None:
+            darb.darb_muon_step(self.muon, [dW], self.lr)
+        darb.darb_adamw_step(self.plan, [d_gamma, d_beta] if self.muon is not None else [dW, d_gamma, d_beta], self.step, self.lr)
         darb.darb_reencode(self.handle, self.stored)
         return scores.logprob
 
     def close(self):
         darb.darb_adamw_destroy(self.plan)
+        darb.darb_muon_destroy(self.muon)
         darb.darb_destroy(self.handle)
 
 
@@ -97,5 +105,5 @@ def retrain(steps: int = 200, vocab: int = 2000, features: int = 256, tokens: in
 
 
 if __name__ == "__main__":
-    for kind in ("f32", "e4m3"):
-        print("states in %s: perplexity %.1f -> %.1f" % ((kind,) + retrain(states=kind)))
+    for kind in ("f32", "e4m3", "muon"):
+        print("states %s: perplexity %.1f -> %.1f" % ((kind,) + retrain(states=kind)))
