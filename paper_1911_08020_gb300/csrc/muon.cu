@@ -83,9 +83,13 @@ struct alignas(128) Matrix {
 struct Part {
     int32_t matrix, part;
 };
+// A tile of a product, or one of the parts of its depth that several CTAs take.
 struct Tile {
     int32_t matrix, row, col;               // first row and column
     int32_t width;                          // columns
+    int32_t k0, k1;                         // depth
+    int32_t slot, parts;                    // where the parts' sums go (slot + part), and how many there are
+    int32_t part, pad[3];
 };
 
 struct StepArgs {
@@ -94,6 +98,8 @@ struct StepArgs {
     int32_t *active;                        // per matrix: has a gradient in this step
     const float *grad_scale;
     int32_t *status;
+    float *partial;                         // sums of parts of tiles
+    int32_t *arrived;                       // per slot: parts that are done, 0 between launches
     float beta, rest, eps, decay, lr;       // rest: 1 - beta; decay: 1 - lr decay
     int32_t nesterov;
 };
@@ -480,9 +486,9 @@ struct Loads {
     }
 };
 
-// What becomes of them, `acc` being the accumulator's address.
+// What becomes of them, `v` being a row of the product in each lane.
 template <int P, int OP>
-__device__ __forceinline__ void finish(const float decay, const Target &x, const Loads<P, OP> &in, int i0, int j0, uint32_t acc, const Turn &turn) {
+__device__ __forceinline__ void finish(const float decay, const Target &x, const Loads<P, OP> &in, int i0, int j0, const uint32_t (&v)[32], const Turn &turn) {
     constexpr bool two = P == 3, apply = OP == kApply || OP == kLast;
     const int lane = threadIdx.x & 31, oct = lane & 3, sub = lane >> 2;
     const int rows = x.rows, cols = x.cols, ld = x.ld;
@@ -490,9 +496,6 @@ __device__ __forceinline__ void finish(const float decay, const Target &x, const
     const int j = j0 + 8 * oct;   // this lane's columns after the turn
     const uint4 (&hi)[4] = in.hi, (&lo)[4] = in.lo;
     const float (&di)[4] = in.di, (&dj)[8] = in.dj;
-    uint32_t v[32];
-    tmem_ld32(acc, v);
-    tmem_ld_wait();
     turn.put(lane, v);
     __syncwarp();
 
@@ -629,6 +632,9 @@ __device__ __forceinline__ void acquire_map(const CUtensorMap *map) {
     asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" ::"l"(map) : "memory");
 }
 
+// The writing warps among themselves.
+__device__ __forceinline__ void writers_meet() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWriters) : "memory"); }
+
 // The tiles of CTA (or pair) b are tiles[first[b]] .. tiles[first[b + 1] - 1].
 template <int P, int BN, int CG, int OP>
 __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs s, const Tile *tiles, const int32_t *first, int buf) {
@@ -639,6 +645,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
     uint64_t *const full = reinterpret_cast<uint64_t *>(sm), *const empty = full + NS, *const ready = empty + NS, *const read = ready + 2,
                     *const done = read + 2;
     uint32_t *const s_tmem = reinterpret_cast<uint32_t *>(done + 1);
+    volatile uint32_t *const s_last = s_tmem + 1;
     unsigned char *const stages = sm + 1024;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = CG == 2 ? int(blockIdx.x) & 1 : 0, unit = CG == 2 ? int(blockIdx.x) >> 1 : int(blockIdx.x);
@@ -688,7 +695,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                     for (int q = 0; q < NP; ++q) acquire_map(&o.a[q]), acquire_map(&o.b[q]);
                     known = tile.matrix;
                 }
-                for (int k = 0; k < o.depth; k += kBK, ++issued) {
+                for (int k = tile.k0; k < tile.k1; k += kBK, ++issued) {
                     if (issued >= NS && !mbar_wait(&empty[stage], parity ^ 1u)) {
                         ok = false;
                         break;
@@ -735,7 +742,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                 }
                 tc_fence_after_sync();
                 const uint32_t d = tmem + half * BN;
-                for (int k = 0; k < o.depth; k += kBK) {
+                for (int k = tile.k0; k < tile.k1; k += kBK) {
                     if (!mbar_wait(&full[stage], parity)) {
                         ok = false;
                         break;
@@ -747,7 +754,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
 #pragma unroll
                     for (int kk = 0; kk < kBK / 16; ++kk) {
                         const uint64_t ao = kk * a_step, bo = kk * b_step;
-                        pair_mma<CG>(d, ah + ao, bh + bo, idesc, (k | kk) != 0);
+                        pair_mma<CG>(d, ah + ao, bh + bo, idesc, (k - tile.k0 | kk) != 0);
                         if (P == 3) {
                             pair_mma<CG>(d, ah + ao, bl + bo, idesc, 1u);
                             pair_mma<CG>(d, al + ao, bh + bo, idesc, 1u);
@@ -775,18 +782,30 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
             if (!s.active[tile.matrix]) continue;
             const int half = used & 1, i0 = tile.row + rank * kBM + quarter * 32, columns = CG == 1 ? BN / 2 : tile.width / 2, c0 = warp < 6 ? 0 : columns;
             const Target to = target<OP>(s, x, buf);
+            const bool whole = OP != kGram || CG == 2 || tile.parts == 1;
             Loads<P, OP> in;
-            in.get(to, i0, tile.col + c0);   // (while the product is made)
-            if (!__all_sync(~0u, mbar_wait(&ready[half], uint32_t(used / 2) & 1u))) {
+            if (whole) in.get(to, i0, tile.col + c0);   // (while the product is made)
+            const bool here = __all_sync(~0u, mbar_wait(&ready[half], uint32_t(used / 2) & 1u));
+            if (!here) {
                 ok = false;
-                break;
+                if (OP != kGram || CG == 2) break;   // (else the other warps wait for this one below)
             }
             tc_fence_after_sync();
             const uint32_t at = tmem + half * BN + (uint32_t(quarter * 32) << 16);
+            // the sums of a part: a column's rows side by side
+            float *const mine = s.partial + (int64_t(tile.slot) * BN + c0) * kBM + quarter * 32 + lane;
 #pragma unroll 1
-            for (int c = c0; c < c0 + columns; c += 32) {
-                if (c > c0) in.get(to, i0, tile.col + c);
-                finish<P, OP>(s.decay, to, in, i0, tile.col + c, at + c, turn);
+            for (int c = 0; c < columns && here; c += 32) {
+                uint32_t v[32];
+                tmem_ld32(at + c0 + c, v);
+                tmem_ld_wait();
+                if (whole) {
+                    if (c > 0) in.get(to, i0, tile.col + c0 + c);
+                    finish<P, OP>(s.decay, to, in, i0, tile.col + c0 + c, v, turn);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) mine[(int64_t(tile.part) * BN + c + e) * kBM] = __uint_as_float(v[e]);
+                }
             }
             // the accumulator has been read
             tc_fence_before_sync();
@@ -796,6 +815,33 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                 else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(shared_of(&read[half], 0)) : "memory");
             }
             ++used;
+            if (whole) continue;
+            // whoever is done last adds the parts up, in their order
+            __threadfence();
+            writers_meet();
+            if (warp == 2 && lane == 0) {
+                const bool last = atomicAdd(s.arrived + tile.slot, 1) == tile.parts - 1;
+                if (last) s.arrived[tile.slot] = 0;
+                *s_last = last;
+            }
+            writers_meet();
+            if (!*s_last) continue;
+            __threadfence();
+#pragma unroll 1
+            for (int c = 0; c < columns; c += 32) {
+                if (i0 >= to.rows || tile.col + c0 + c > i0 + 31) continue;   // (nothing is made of these)
+                float sum[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) sum[e] = __ldcg(mine + int64_t(c + e) * kBM);
+#pragma unroll 1
+                for (int q = 1; q < tile.parts; ++q)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sum[e] += __ldcg(mine + (int64_t(q) * BN + c + e) * kBM);
+                uint32_t v[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(sum[e]);
+                finish<P, OP>(s.decay, to, in, i0, tile.col + c0 + c, v, turn);
+            }
         }
     }
     if (!ok) atomicOr(s.status, kStatusTimeout);
@@ -816,6 +862,7 @@ struct Schedule {
     std::vector<int32_t> first;
     int bn = 0;
     int64_t longest = 0;
+    int64_t slots = 0;                  // of parts of tiles
     int64_t o_tiles = 0, o_first = 0;   // in the plan's memory
     int32_t units() const { return int32_t(first.size()) - 1; }
 };
@@ -860,6 +907,38 @@ int64_t assign(std::vector<Item> &items, int units, std::vector<int64_t> &load) 
     return longest;
 }
 
+// Few tiles are divided along their depth until there is one part for every unit, or
+// none has more than twelve stages (parts of five cost more than they save: three of 600 x
+// 301 170 us against 164); the slots that this takes.
+int64_t divide(std::vector<Item> &items, bool three, const Form &form, int units) {
+    std::vector<int64_t> parts(items.size(), 1);
+    const auto stages = [&](size_t i) { return (items[i].depth + kBK - 1) / kBK; };
+    for (int64_t total = int64_t(items.size()); total < units; ++total) {
+        size_t most = 0;
+        for (size_t i = 1; i < items.size(); ++i)
+            if (stages(i) * parts[most] > stages(most) * parts[i]) most = i;
+        if (stages(most) <= 12 * parts[most]) break;
+        ++parts[most];
+    }
+    std::vector<Item> all;
+    int64_t slots = 0;
+    for (size_t i = 0; i < items.size(); ++i) {
+        const int64_t n = parts[i], each = (stages(i) + n - 1) / n * kBK;
+        const int64_t used = (items[i].depth + each - 1) / each;
+        for (int64_t q = 0; q < used; ++q) {
+            Item part = items[i];
+            part.tile.k0 = int32_t(q * each), part.tile.k1 = int32_t(std::min(part.depth, (q + 1) * each));
+            if (used > 1) part.tile.slot = int32_t(slots), part.tile.parts = int32_t(used), part.tile.part = int32_t(q);
+            // (what the last part does more is about what a tile waits for at its end)
+            part.cost = tile_cost(part.tile.k1 - part.tile.k0, three, form.cg, form.bn) + (used > 1 ? 4000 + 300 * used : 0);
+            all.push_back(part);
+        }
+        if (used > 1) slots += used;
+    }
+    items = std::move(all);
+    return slots;
+}
+
 Schedule make_schedule(const std::vector<Matrix> &all, Op op, const Form &form, bool three, int units) {
     std::vector<Item> items;
     for (size_t t = 0; t < all.size(); ++t) {
@@ -870,10 +949,11 @@ Schedule make_schedule(const std::vector<Matrix> &all, Op op, const Form &form, 
         for (int col = 0; col < cols; col += form.bn)
             for (int row = 0; row < rows; row += form.bm)
                 if (op == kApply || col < row + form.bm)
-                    items.push_back({tile_cost(depth, three, form.cg, form.bn), depth, {int32_t(t), row, col, form.bn}});
+                    items.push_back({tile_cost(depth, three, form.cg, form.bn), depth, {int32_t(t), row, col, form.bn, 0, int32_t(depth), 0, 1, 0, {}}});
     }
     Schedule s;
     s.bn = form.bn;
+    if (op == kGram && form.cg == 1 && int64_t(items.size()) < units) s.slots = divide(items, three, form, units);
     const int most = units;
     std::vector<int64_t> load;
     auto shared = [&] { return int(std::min<int64_t>(most, int64_t(items.size()))); };
@@ -960,7 +1040,8 @@ struct darb_muon_s {
     void *dmem = nullptr;
     const darb::Matrix *d_matrices = nullptr;
     const darb::Part *d_parts = nullptr;
-    int32_t *d_active = nullptr, *d_status = nullptr;
+    int32_t *d_active = nullptr, *d_status = nullptr, *d_arrived = nullptr;
+    float *d_partial = nullptr;
     darb::Schedule schedules[3];
 };
 
@@ -1041,6 +1122,8 @@ darb_status_t build_plan(darb_muon_s *plan, int32_t n, const int64_t *rows, cons
         return at;
     };
     const int64_t o_status = take(4), o_active = take(n * 4), o_parts = take(int64_t(parts.size() * sizeof(Part))), o_matrices = take(int64_t(n * sizeof(Matrix)));
+    const Schedule &gram = plan->schedules[kGram];
+    const int64_t o_arrived = take(gram.slots * 4), o_partial = take(gram.slots * gram.bn * kBM * 4);
     for (Schedule &s : plan->schedules) {
         s.o_tiles = take(int64_t(s.tiles.size() * sizeof(Tile)));
         s.o_first = take(int64_t(s.first.size() * 4));
@@ -1079,6 +1162,8 @@ darb_status_t build_plan(darb_muon_s *plan, int32_t n, const int64_t *rows, cons
     }
     plan->d_status = reinterpret_cast<int32_t *>(d + o_status);
     plan->d_active = reinterpret_cast<int32_t *>(d + o_active);
+    plan->d_arrived = reinterpret_cast<int32_t *>(d + o_arrived);
+    plan->d_partial = reinterpret_cast<float *>(d + o_partial);
     plan->d_parts = reinterpret_cast<const Part *>(d + o_parts);
     plan->d_matrices = reinterpret_cast<const Matrix *>(d + o_matrices);
     // zeros: the diagonals of A and B are never written
@@ -1187,6 +1272,7 @@ darb_status_t darb_muon_step(darb_muon_t plan, const void *const *grads, const f
     s.active = plan->d_active;
     s.grad_scale = grad_scale;
     s.status = plan->d_status;
+    s.partial = plan->d_partial, s.arrived = plan->d_arrived;
     s.beta = float(beta), s.rest = float(1.0 - beta), s.eps = float(eps);
     s.decay = float(1.0 - lr * weight_decay), s.lr = float(lr);
     s.nesterov = nesterov != 0;

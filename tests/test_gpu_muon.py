@@ -95,6 +95,13 @@ def test_many_matrices(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shapes", [[(64, 6000)], [(5999, 65)], [(1, 30000)], [(200, 4000), (33, 2500), (3000, 130), (7, 7)], [(513, 513)]])
+def test_long_products_of_few_tiles(shapes, dtype):
+    """Whose depth several CTAs share; twice, as the second step finds what the first one left."""
+    check(shapes, dtype, steps=2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_enough_for_every_tile_width(dtype):
     check([(2100, 4300), (1700, 1500)], dtype)
 
