@@ -24,14 +24,14 @@
  *    and any scratch it allocates, and releases both in darb_destroy.
  *  - Work is enqueued on the caller's stream.  Only darb_encode, darb_import,
  *    darb_export, darb_sync_status, darb_rnn_reserve, darb_adamw_create,
- *    darb_adamw_sync_status and the two destroy calls synchronise; the others are
- *    asynchronous.
+ *    darb_muon_create, the two _sync_status of their plans and the destroy calls
+ *    synchronise; the others are asynchronous.
  *    darb_spmm allocates nothing; the step calls on large matrices or batches
  *    use scratch owned by the handle (darb_rnn_reserve sizes it up front).
  *  - Only these calls take scratch from the device's stream-ordered memory
  *    pool: darb_spmm_ex with DARB_PATH_TENSOR_CORES, the sequence calls, and
- *    darb_layer_norm_grad where it is given none.  They return it to the pool on the same stream.  The first such
- *    call on a device raises the release threshold of the device's current
+ *    darb_layer_norm_grad and darb_policy_loss where they are given none.  They
+ *    return it to the pool on the same stream.  The first such call on a device raises the release threshold of the device's current
  *    pool to 1 GiB if it is lower, so that freed scratch stays mapped across
  *    synchronisations; darb_spmm never touches the pool.
  *  - There is no CPU fallback: without a usable CUDA device the GPU calls
@@ -518,8 +518,8 @@ typedef enum { DARB_GATES_LOGITS = 0, DARB_GATES_VALUES = 1 } darb_gates_t;
  * be x itself (same pointer and strides); no other overlap is allowed.  A logit of -inf
  * starts anew (a = 0), one of +inf keeps the state (a = 1; steps are put together in a fixed
  * order of their own, so that its last place may change); a NaN, or an infinite state that
- * meets a = 0, makes its channel NaN from there on.  Gates above 1 in magnitude are
- * allowed as long as their products over 512 steps (or until the state is 0) stay finite.
+ * meets a = 0, makes its channel NaN from there on.  Gates above 1 in magnitude are allowed
+ * as long as their products over any 8192 steps stay finite.
  * No channels: nothing is done; steps == 0: h_last is h0.
  * Asynchronous on `stream`; allocates nothing; one launch (steps == 0: a copy).
  * Errors: DARB_ERR_INVALID_ARG; DARB_ERR_UNSUPPORTED (more than 2^30 steps or channels,

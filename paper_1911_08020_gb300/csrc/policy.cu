@@ -12,19 +12,24 @@
 // many, so the formula is the same with one ratio a sequence.
 //
 // w needs how many tokens count in a sequence, and in all: the inputs are read twice
-// (mask, and log probabilities where the ratio is the sequence's; then everything).
-// A CTA takes a chunk of consecutive tokens.  Its sequences are found once, by a
-// search of 256 offsets at a time; the place where a sequence starts in the chunk
-// stands for it from then on, so that scratch goes by tokens and any number of empty
-// sequences costs nothing but reading their offsets.  A chunk's sums of a sequence
-// go to that place, those of a sequence from an earlier chunk to the chunk, and who
-// needs the sum of a sequence that spans chunks adds the chunks up, in their order.
-// Up to 4096 tokens are one chunk: one CTA, one launch, no scratch.
+// (the mask, and log probabilities where the ratio is the sequence's; then everything).
+// A CTA takes a chunk of consecutive tokens.  It finds the sequences in it by a search
+// among the offsets in which all its threads take part; the place where a sequence starts
+// in the chunk stands for it from then on, so that scratch goes by tokens and any
+// number of empty sequences costs nothing but reading their offsets.  A chunk's sums of
+// a sequence go to that place, those of a sequence from an earlier chunk to the chunk,
+// and who needs the sum of a sequence that spans chunks adds the chunks up, in their
+// order.  Up to 4096 tokens are one chunk: one CTA, one launch, no scratch.
 //
-// What bounds it: latency for few tokens, memory for many (25 bytes a token with
-// every term; 64-bit arithmetic is too slow to spend on a token, one operation takes
-// as long as 6 bytes, so differences are pairs of 32-bit numbers where a border needs
-// them exact, and 64 bits hold the sums from a warp on).
+// What bounds it is latency.  A token costs 25 bytes, and 80 instructions with the 64-bit
+// arithmetic left out: that is too slow to spend on a token (one operation takes as long
+// as 6 bytes), so that a border is decided in 32 bits, and by the exact difference in
+// the rare thread that meets one, and 64 bits hold sums from a warp on.  But a chunk is
+// a chain of ten loads and barriers that need one another: 1.5 million tokens of 1000
+// sequences take 29 us (37 MB: 5.5 us), of which the first reading is 7 and the last
+// CTA's sum of all chunks 4.  So all that does without the weights -- exponentials,
+// gradients but for a factor -- comes before the wait for the first reading, and the
+// chunk's sums go out before its gradients.  300 tokens take 5.6 us, 4096 take 8.
 #include "launch.cuh"
 #include "tma.cuh"
 #include "tokens.cuh"
@@ -543,7 +548,10 @@ __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const P
     if (a.entropy != nullptr) load8(a.entropy, i, a.n, a.vector, ent);
     const Tokens t = find_sequences<THREADS>(a, c0, sh);
     const int sequences = min(sh.sequences, T);
-    for (int k = tid; k < sequences; k += THREADS) pieces[sh.places[k]].advantage = a.advantage[sh.start[sh.places[k]]];
+    for (int k = tid; k < sequences; k += THREADS) {
+        const int id = sh.start[sh.places[k]];
+        if (id >= 0) pieces[sh.places[k]].advantage = a.advantage[id];   // (below 0 only where offsets fall)
+    }
     on &= t.inside;
     __syncthreads();
 

@@ -14,17 +14,24 @@
 // kernel does both; the backward pass walks the steps with negative strides.
 //
 // Steps are maps h -> A h + H, and maps compose: (A2, H2) after (A1, H1) is
-// (A2 A1, A2 H1 + H2).  A thread takes 16 elements -- 4 steps of 4 neighbouring
-// channels, or 16 steps of one -- composes its steps' maps, and learns the state
-// before them from the threads (of the CTA, of the cluster) that have the steps
-// before.  Then it runs its steps again from registers.  Inputs are read once and
-// outputs written once, with no scratch and no waiting on other CTAs but at the
-// cluster's barrier; the order of all sums is fixed by the sizes.
+// (A2 A1, A2 H1 + H2).  A thread takes a run of steps of one channel or of four
+// neighbouring ones, composes its steps' maps, and learns the state before them from the
+// lanes, warps and CTAs that have the steps before.  Then it runs its steps again from
+// registers.  Inputs are read once and outputs written once, with no scratch; the order
+// of all sums is fixed by the sizes.
 //
-// What bounds it: memory (12 bytes an element in fp32, 24 backward).  Everything
-// else follows from keeping loads in flight: time is split over the 8 warps of a CTA
-// and, where the channels alone do not fill the GPU, over the 2 to 8 CTAs of a
-// cluster; a thread's next 16 elements are on their way while it works on these.
+// What bounds it is memory (12 bytes an element in fp32, 24 backward): the arithmetic
+// alone, with no loads, takes 123 us where 4 x 16384 x 2048 bf16 take 172 (floor 119).
+// So what counts is how many loads are on their way and how they lie:
+//  * loads go to shared memory asynchronously, two rounds ahead, into places that only
+//    their own thread reads, so that they cost neither registers nor barriers;
+//  * time is split over lanes (shuffles), then over the 8 or 16 warps of a CTA, which hand the
+//    carry on one by one without a barrier of all (a CTA barrier a round: 292 us against
+//    269), then, where channels are few, over the 2 to 8 CTAs of a cluster;
+//  * 128 bytes lie side by side wherever the channels allow it.
+// Three kernels, by how the operands lie (form_of): channels four at a time; rows of
+// consecutive steps, by aligned granules; and anything else, an element at a time, through
+// shared memory where fewer than 8 channels lie together.
 #include "launch.cuh"
 #include "tma.cuh"
 #include "tokens.cuh"
@@ -1055,15 +1062,34 @@ darb_status_t check_operand(const Operand &o, const Shape &n, size_t es) {
     return (n.outer - 1) * ld + rows > kMaxSpan ? DARB_ERR_UNSUPPORTED : DARB_OK;
 }
 
-// The bytes of an operand as lines of one pitch, where it is that regular.
-Range operand_range(const Operand &o, const Shape &n, size_t es) {
+// The bytes of an operand as lines of one pitch, in two ways: short lines, and the long
+// ones that they lie in.  Two operands share no byte if either way tells them apart
+// (slices of rows side by side; rows or elements that take turns).
+struct Place {
+    Range fine, coarse;
+};
+Place place_of(const Operand &o, const Shape &n, size_t es) {
     const int64_t size = int64_t(es), ld = n.outer > 1 ? o.ld : 0, step = n.steps > 1 ? o.step : 0;
-    const int64_t bytes = ((n.outer - 1) * ld + (n.steps - 1) * step + n.inner) * size;
-    if (n.outer == 1 && n.steps == 1) return {o.p, bytes};
-    if (n.outer == 1 || (n.steps > 1 && ld == n.steps * step)) return {o.p, bytes, step * size, n.inner * size};
-    if (n.steps == 1 || step == n.outer * ld) return {o.p, bytes, ld * size, n.inner * size};
-    if (step == n.inner) return {o.p, bytes, ld * size, n.steps * n.inner * size};
-    return {o.p, bytes};
+    const int64_t row = (n.steps - 1) * step + n.inner, bytes = ((n.outer - 1) * ld + row) * size;
+    const Range whole = {o.p, bytes}, steps = {o.p, bytes, step * size, n.inner * size}, rows = {o.p, bytes, ld * size, row * size};
+    if (n.outer == 1) return {n.steps == 1 ? whole : steps, whole};
+    if (n.steps == 1) return {rows, whole};
+    // rows of steps; or steps of rows
+    if (ld >= row) return {ld % step == 0 ? steps : rows, rows};
+    const Range columns = {o.p, bytes, ld * size, n.inner * size}, all_rows = {o.p, bytes, step * size, ((n.outer - 1) * ld + n.inner) * size};
+    return {step % ld == 0 ? columns : all_rows, all_rows};
+}
+Place place_of(const void *p, int64_t bytes) { return {{p, bytes}, {p, bytes}}; }
+bool meet(const Place &a, const Place &b) { return buffers_overlap(a.fine, b.fine) && buffers_overlap(a.coarse, b.coarse); }
+template <int NO, int NI>
+bool apart(const Place (&outs)[NO], const Place (&ins)[NI]) {
+    for (int o = 0; o < NO; ++o) {
+        for (const Place &i : ins)
+            if (meet(outs[o], i)) return false;
+        for (int p = 0; p < o; ++p)
+            if (meet(outs[o], outs[p])) return false;
+    }
+    return true;
 }
 
 // Which kernel takes these operands.
@@ -1132,11 +1158,11 @@ darb_status_t darb_gated_scan(const void *gate, int64_t ld_gate, int64_t step_ga
         st = check_operand(o, n, es);
         if (st != DARB_OK) return st;
     }
-    const Range outs[] = {operand_range(s.out[0], n, es), {h_last, states}};
-    Range ins[] = {operand_range(s.gate, n, es), operand_range(s.x, n, es), {h0, states}};
-    if (same(s.x, s.out[0])) ins[1].p = nullptr;
-    if (h0 == h_last) ins[2].p = nullptr;
-    if (!outputs_apart(outs, ins) || (h0 == h_last && buffers_overlap(outs[0], {h0, states}))) return DARB_ERR_INVALID_ARG;
+    const Place outs[] = {place_of(s.out[0], n, es), place_of(h_last, states)}, nowhere = place_of(nullptr, 0);
+    Place ins[] = {place_of(s.gate, n, es), place_of(s.x, n, es), place_of(h0, states)};
+    if (same(s.x, s.out[0])) ins[1] = nowhere;
+    if (h0 == h_last) ins[2] = nowhere;
+    if (!apart(outs, ins) || (h0 == h_last && meet(outs[0], place_of(h0, states)))) return DARB_ERR_INVALID_ARG;
     s.first = h0, s.last = h_last, s.steps = steps, s.channels = outer * inner;
     s.outer = int32_t(outer), s.inner = int32_t(inner), s.coupled = coupled != 0;
     return enqueue_scan<false>(s, dtype, gates == DARB_GATES_LOGITS, form_of(all, n, es), stream);
@@ -1167,15 +1193,14 @@ darb_status_t darb_gated_scan_grad(const void *dh, int64_t ld_dh, int64_t step_d
         if (st != DARB_OK) return st;
     }
     // an output may take the place of its input: d_gate the gate's, d_x that of x
-    Range ins[] = {operand_range(in[0], n, es), operand_range(in[1], n, es), operand_range(in[2], n, es),
-                   operand_range(in[3], n, es), {h0, states}, {d_last, states}};
-    const Range outs[] = {operand_range(out[0], n, es), operand_range(out[1], n, es), {d_h0, states}};
-    const Range gate_in = ins[0], x_in = ins[1];
-    if (same(in[0], out[0])) ins[0].p = nullptr;
-    if (same(in[1], out[1])) ins[1].p = nullptr;
-    if (d_last == d_h0) ins[5].p = nullptr;
-    if (!outputs_apart(outs, ins) || buffers_overlap(outs[1], gate_in) || buffers_overlap(outs[0], x_in) || buffers_overlap(outs[2], gate_in) ||
-        buffers_overlap(outs[2], x_in))
+    Place ins[] = {place_of(in[0], n, es), place_of(in[1], n, es), place_of(in[2], n, es), place_of(in[3], n, es), place_of(h0, states), place_of(d_last, states)};
+    const Place outs[] = {place_of(out[0], n, es), place_of(out[1], n, es), place_of(d_h0, states)}, nowhere = place_of(nullptr, 0);
+    const Place gate_in = ins[0], x_in = ins[1];
+    if (same(in[0], out[0])) ins[0] = nowhere;
+    if (same(in[1], out[1])) ins[1] = nowhere;
+    if (d_last == d_h0) ins[5] = nowhere;
+    if (!apart(outs, ins) || meet(outs[1], gate_in) || meet(outs[0], x_in) || meet(outs[2], gate_in) ||
+        meet(outs[2], x_in))
         return DARB_ERR_INVALID_ARG;
     ScanArgs s = {};
     const Form form = form_of(all, n, es);

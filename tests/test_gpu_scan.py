@@ -269,6 +269,52 @@ def test_refusals():
         darb.darb_gated_scan_grad(x, gate, x, x.clone(), d_gate=(d := torch.empty_like(x)), d_x=d)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,cols", [(0, slice(0, 64)), (0, slice(3, 40)), (1, slice(0, 100)), (1, slice(0, 100, 2))])
+def test_offsets_past_32_bits(dim, cols, dtype):
+    """Slices of a buffer whose rows lie 2^29 elements apart."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("not enough device memory")
+    buf = torch.empty(6, 1 << 29, dtype=DTYPES[dtype], device="cuda")
+    parts = [buf[:, 1024 * k:1024 * (k + 1)][:, cols] for k in range(6)]
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    for t in parts:
+        t.copy_(2 * torch.randn(t.shape, generator=gen, device="cuda"))
+    gate, x, dh, h, d_gate, d_x = parts
+    small = [t.clone() for t in (gate, x, dh)]   # dense, and so by another kernel
+    darb.darb_gated_scan(gate, x, dim=dim, h=h)
+    darb.darb_gated_scan_grad(dh, gate, x, h, dim=dim, d_gate=d_gate, d_x=d_x)
+    a = [t.double().cpu().numpy() if dim == 0 else t.double().cpu().numpy().T for t in (small[0], small[1], small[2], h, d_gate, d_x)]
+    zero = np.zeros(a[0].shape[1])
+    want, bound = forward(a[0], a[1], zero, True, True)
+    within(a[3], want, bound, DTYPES[dtype], "h")
+    wants = back(a[2], a[0], a[1], a[3], zero, zero, True, True)
+    within(a[4], wants[0], wants[3], DTYPES[dtype], "d_gate")
+    within(a[5], wants[1], wants[4], DTYPES[dtype], "d_x")
+    assert torch.equal(gate, small[0]) and torch.equal(x, small[1])
+    del buf, parts, gate, x, dh, h, d_gate, d_x, t
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_parts_of_one_buffer(dtype):
+    """Halves of rows, neighbouring columns, and steps that take turns: no byte is shared, and all are taken."""
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    fresh = lambda *s: (2 * torch.randn(*s, generator=gen, device="cuda")).to(DTYPES[dtype])  # noqa: E731
+    rows, turns, columns = fresh(3, 50, 6 * 8), fresh(5, 90 * 3), fresh(70, 4, 3 * 16)
+    for parts, dim in ((rows.split(8, dim=2), 1), ([turns[:, k::3] for k in range(3)], 1), (columns.split(16, dim=2), 0)):
+        gate, x, h = parts[:3]
+        want = darb.darb_gated_scan(gate.clone(), x.clone(), dim=dim)[0]
+        keep = [t.clone() for t in parts]
+        darb.darb_gated_scan(gate, x, dim=dim, h=h)
+        a = [t.double().cpu().numpy().swapaxes(0, dim).reshape(t.shape[dim], -1) for t in (keep[0], keep[1], h, want)]
+        zero = np.zeros(a[0].shape[1])
+        ref, bound = forward(a[0], a[1], zero, True, True)
+        within(a[2], ref, bound, DTYPES[dtype], "h")
+        within(a[3], ref, bound, DTYPES[dtype], "dense h")
+        assert all(torch.equal(t, k) for t, k in zip((*parts[:2], *parts[3:]), (*keep[:2], *keep[3:])))
+
+
 def test_deterministic():
     lay = Layout("product", 5000, 64, 1, "f32")
     gate, x, _ = inputs(lay, True)

@@ -47,6 +47,17 @@ def test_scan_refusals(L):
         assert scan(L, **kw) == UNSUPPORTED, kw
 
 
+def test_slices_that_meet(L):
+    """Slices of one buffer that share bytes with an input (those that share none are in test_gpu_scan.py)."""
+    two = dict(outer=2, steps=3, inner=4)
+    for kw in (dict(gate=A, x=A + 16, h=A + 20, ldg=36, sg=12, ldx=36, sx=12, ldh=36, sh=12, **two),
+               dict(gate=A, x=A + 400, h=A + 404, ldg=1000, sg=4, ldx=1000, sx=4, ldh=1000, sh=4, **two),
+               dict(gate=A, x=A + 400, h=A, ldg=1000, sg=4, ldx=1000, sx=4, ldh=1000, sh=4, **two),
+               dict(gate=A, x=A + 4, h=A + 12, outer=6, steps=50, inner=1, ldg=300, sg=3, ldx=300, sx=3, ldh=300, sh=3),
+               dict(gate=A, x=A + 4, h=A + 8, outer=6, steps=50, inner=1, ldg=300, sg=3, ldx=300, sx=3, ldh=300, sh=2)):
+        assert scan(L, **kw) == INVALID, kw
+
+
 def test_scan_grad_refusals(L):
     for kw in (*(({k: None}) for k in ("dh", "gate", "x", "h", "dg", "dx")), dict(dt=7), dict(gates=-1), dict(inner=-1),
                dict(ld={"h": 9}), dict(st={"dg": 49}), dict(dg=C), dict(dx=B), dict(dg=A), dict(dx=A), dict(dx=D), dict(dg=E, dx=E),
