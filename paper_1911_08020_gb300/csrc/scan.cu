@@ -973,7 +973,17 @@ cudaError_t launch_channels(ScanArgs &s, cudaStream_t stream) {
     };
     // whole warps side by side where that fills the GPU
     const int64_t wide = tiles(32, kScanWarps);
-    if (wide >= int64_t(3) * sm_count()) return launch_channels<T, BACK, 32, kScanWarps, LOGITS>(s, wide, 1, stream);
+    if (wide >= int64_t(3) * sm_count()) {
+        // and no more of them to a channel than that needs (100 steps of 200 x 4096 bf16:
+        // 106 us with one, 134 with eight)
+        int64_t tiles_now = wide;
+        while (s.groups_log > 0) {
+            const int64_t per = int64_t(32) * 4 * (kScanWarps >> (s.groups_log - 1)), fewer = (s.channels + per - 1) / per;
+            if (fewer < int64_t(3) * sm_count()) break;
+            --s.groups_log, tiles_now = fewer;
+        }
+        return launch_channels<T, BACK, 32, kScanWarps, LOGITS>(s, tiles_now, 1, stream);
+    }
     // else fewer lanes, and later steps in the others: 128 bytes side by side (of 64 at a
     // time memory gives two thirds as much: 4 x 16384 x 2048 bf16 270 us against 172)
     if (sizeof(T) == 2) {
