@@ -688,14 +688,11 @@ def _channel_axes(shape, strides, dim: int, call: str) -> tuple[int, int, int, i
     return 1, shape[dim], channels, -1, dim
 
 
-def _scan_operands(call: str, like, outer: int, step: int, operands, strides):
-    """Pointer, leading dimension and step of every (name, tensor) of x's shape, checked to be of its type."""
-    dtype, out = like.dtype, []
-    for (name, t), s in zip(operands, strides):
-        if t.dtype != dtype or not t.is_cuda:
-            _refuse(call, f"{name} must be a CUDA tensor of x's type")
-        out += (t.data_ptr(), s[outer] if outer >= 0 else 0, s[step])
-    return out
+def _scan_operand(t, dtype, s, outer: int, step: int, call: str, name: str):
+    """(pointer, leading dimension, step) of a tensor with strides s, checked to be of x's type."""
+    if t.dtype is not dtype or not t.is_cuda:
+        _refuse(call, f"{name} must be a CUDA tensor of x's type")
+    return t.data_ptr(), s[outer] if outer >= 0 else 0, s[step]
 
 
 def _state_shape(x, dim: int):
@@ -720,14 +717,15 @@ def darb_gated_scan(gate, x, h0=None, dim: int = 0, gates: int = GATES_LOGITS, c
         h = _new(shape, x.dtype, x.device, stream)
     if gate.shape != shape or h.shape != shape:
         _refuse(call, "gate and h must have x's shape")
-    strides = (gate.stride(), x.stride(), h.stride())
-    outer, steps, inner, oa, sa = _channel_axes(shape, strides, dim, call)
+    gs, xs, hs = gate.stride(), x.stride(), h.stride()
+    outer, steps, inner, oa, sa = _channel_axes(shape, (xs,) if gs == xs == hs else (gs, xs, hs), dim, call)
     if h_last is None:
         h_last = _new(_state_shape(x, sa), f32, x.device, stream)
-    n = outer * inner
-    at = _scan_operands(call, x, oa, sa, (("gate", gate), ("x", x), ("h", h)), strides)
-    _check(lib().darb_gated_scan(*at[:6], code, gates, bool(coupled), outer, steps, inner, _vector(h0, n, f32, call, "h0"),
-                                 *at[6:], _vector(h_last, n, f32, call, "h_last"), _stream(stream)), call)
+    n, dtype = outer * inner, x.dtype
+    _check(lib().darb_gated_scan(*_scan_operand(gate, dtype, gs, oa, sa, call, "gate"), x.data_ptr(), xs[oa] if oa >= 0 else 0, xs[sa],
+                                 code, gates, bool(coupled), outer, steps, inner, _vector(h0, n, f32, call, "h0"),
+                                 *_scan_operand(h, dtype, hs, oa, sa, call, "h"), _vector(h_last, n, f32, call, "h_last"),
+                                 _stream(stream)), call)
     return h, h_last
 
 
@@ -745,14 +743,18 @@ def darb_gated_scan_grad(dh, gate, x, h, h0=None, d_last=None, dim: int = 0, gat
         d_x = _new(shape, x.dtype, x.device, stream)
     tensors = (dh, gate, x, h, d_gate, d_x)
     for t in tensors:
-        if t.shape != shape:
+        if t is not x and t.shape != shape:
             _refuse(call, "dh, gate, h, d_gate and d_x must have x's shape")
     strides = [t.stride() for t in tensors]
-    outer, steps, inner, oa, sa = _channel_axes(shape, strides, dim, call)
+    xs = strides[2]
+    outer, steps, inner, oa, sa = _channel_axes(shape, (xs,) if strides.count(xs) == 6 else strides, dim, call)
     if d_h0 is None and h0 is not None:
         d_h0 = _new(_state_shape(x, sa), f32, x.device, stream)
-    n = outer * inner
-    at = _scan_operands(call, x, oa, sa, zip(("dh", "gate", "x", "h", "d_gate", "d_x"), tensors), strides)
+    n, dtype, at = outer * inner, x.dtype, []
+    for t, s, name in zip(tensors, strides, ("dh", "gate", "x", "h", "d_gate", "d_x")):
+        if t.dtype is not dtype or not t.is_cuda:
+            _refuse(call, f"{name} must be a CUDA tensor of x's type")
+        at += (t.data_ptr(), s[oa] if oa >= 0 else 0, s[sa])
     _check(lib().darb_gated_scan_grad(*at[:12], code, gates, bool(coupled), outer, steps, inner,
                                       _vector(h0, n, f32, call, "h0"), _vector(d_last, n, f32, call, "d_last"), *at[12:],
                                       _vector(d_h0, n, f32, call, "d_h0"), _stream(stream)), call)
