@@ -26,10 +26,10 @@
 // as 6 bytes), so that a border is decided in 32 bits, and by the exact difference in
 // the rare thread that meets one, and 64 bits hold sums from a warp on.  But a chunk is
 // a chain of ten loads and barriers that need one another: 1.5 million tokens of 1000
-// sequences take 29 us (37 MB: 5.5 us), of which the first reading is 7 and the last
-// CTA's sum of all chunks 4.  So all that does without the weights -- exponentials,
+// sequences take 27 us (37 MB: 5.5 us), of which the first reading is 7.  So all that does without the weights -- exponentials,
 // gradients but for a factor -- comes before the wait for the first reading, and the
-// chunk's sums go out before its gradients.  300 tokens take 5.6 us, 4096 take 8.
+// chunks' sums are added up by a launch of its own (a ticket, and the last CTA: 29 us).
+// 300 tokens take 5.4 us, 4096 take 8.
 #include "launch.cuh"
 #include "tma.cuh"
 #include "tokens.cuh"
@@ -64,7 +64,6 @@ struct PolicyWork {
                           // sequence that started before it; of the one that goes on behind it (kWhole: the same one)
     int32_t *slot_count;
     long long *norm;      // the tokens, or sequences, that count
-    int32_t *ticket;
 };
 
 struct PolicyArgs {
@@ -431,7 +430,7 @@ __global__ void __launch_bounds__(kChunkThreads) policy_count_kernel(const Polic
         load8(a.logprob, i, a.n, a.vector, lp);
         load8(a.old, i, a.n, a.vector, old);
     }
-    if (c == 0 && tid == 0) *a.w.ticket = 0, *a.w.norm = 0;
+    if (c == 0 && tid == 0) *a.w.norm = 0;
     const Tokens t = find_sequences<kChunkThreads>(a, c0, sh);
     on &= t.inside;
     const int64_t before = sh.before, end = c0 + kChunkTokens;
@@ -532,7 +531,6 @@ __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const P
     ChunkShared<THREADS> &sh = *reinterpret_cast<ChunkShared<THREADS> *>(raw);
     Piece *const pieces = reinterpret_cast<Piece *>(raw + (sizeof(ChunkShared<THREADS>) + 15) / 16 * 16);   // by the place of the start
     __shared__ double stat_part[kSums][THREADS / 32];
-    __shared__ bool last_cta;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t c = SINGLE ? 0 : blockIdx.x, c0 = c * T, i = c0 + tid * kE;
     if (SINGLE) {
@@ -694,30 +692,24 @@ __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const P
         if (lane == 0) stat_part[k][warp] = double(v);
     }
     __syncthreads();
-    // the CTA that is done last adds the chunks up, in an order that does not depend on
-    // which it is (it is told before the gradients are written: the fence would wait for them)
     if (warp == 0) {
         const double v = warps_sum<THREADS>(stat_part, lane);
-        if (SINGLE) {
-            write_stats(a, v, lane);
-        } else {
-            if ((lane & 7) == 0) {
-                a.w.partial[c * kSums + (lane >> 3)] = v;
-                __threadfence();
-            }
-            __syncwarp();
-            if (lane == 0) last_cta = atomicAdd(a.w.ticket, 1) == int(gridDim.x) - 1;
-        }
+        if (SINGLE) write_stats(a, v, lane);
+        else if ((lane & 7) == 0) a.w.partial[c * kSums + (lane >> 3)] = v;
     }
     store8(a.d_logprob, i, t.inside, a.vector, d);
     if (a.d_entropy != nullptr) store8(a.d_entropy, i, t.inside, a.vector, d_ent);
-    if (SINGLE) return;
-    __syncthreads();
-    if (!last_cta) return;
-    __threadfence();
+}
+
+// The chunks' sums, in their order.
+__global__ void __launch_bounds__(kChunkThreads) policy_stats_kernel(const PolicyArgs a) {
+    __shared__ double stat_part[kSums][kChunkThreads / 32];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    pdl_launch_dependents();
+    pdl_wait_previous();
     double v[kSums] = {};
 #pragma unroll 4
-    for (int64_t j = tid; j < a.chunks; j += THREADS)
+    for (int64_t j = tid; j < a.chunks; j += kChunkThreads)
 #pragma unroll
         for (int k = 0; k < kSums; ++k) v[k] += __ldcg(a.w.partial + j * kSums + k);
 #pragma unroll
@@ -726,7 +718,7 @@ __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const P
         if (lane == 0) stat_part[k][warp] = v[k];
     }
     __syncthreads();
-    if (warp == 0) write_stats(a, warps_sum<THREADS>(stat_part, lane), lane);
+    if (warp == 0) write_stats(a, warps_sum<kChunkThreads>(stat_part, lane), lane);
 }
 
 // ---- host ----
@@ -747,7 +739,6 @@ int64_t lay_work(char *base, int64_t n, PolicyWork &w) {
     take(w.info, c);
     take(w.slot_count, n);
     take(w.norm, 1);
-    take(w.ticket, 1);
     return at;
 }
 int64_t policy_work(int64_t n) {
@@ -785,7 +776,9 @@ cudaError_t launch_policy(PolicyArgs &a, cudaStream_t stream) {
         e = launch_ex(policy_norm_kernel, dim3(unsigned((a.chunks + 1023) / 1024)), dim3(kChunkThreads), 0, stream, 1, true, a);
         if (e != cudaSuccess) return e;
     }
-    return launch_policy_kernel<kChunkThreads, false, SUMS>(a, stream);
+    e = launch_policy_kernel<kChunkThreads, false, SUMS>(a, stream);
+    if (e != cudaSuccess) return e;
+    return launch_ex(policy_stats_kernel, dim3(1), dim3(kChunkThreads), 0, stream, 1, true, a);
 }
 
 }  // namespace
