@@ -189,9 +189,15 @@ __device__ __forceinline__ void map_through(const Quad &A, const Quad &H, Quad &
 // warp gives again when the carry has been round all the others, so that one place and
 // one barrier do.  16 warps use the barrier of __syncthreads too, which they do without.)
 template <int WARPS>
-__device__ __forceinline__ void take_carry(int warp) { asm volatile("bar.sync %0, 64;" ::"r"(warp + (WARPS < 16)) : "memory"); }
+__device__ __forceinline__ void take_carry(int warp) {
+    __syncwarp();
+    asm volatile("bar.sync %0, 64;" ::"r"(warp + (WARPS < 16)) : "memory");
+}
 template <int WARPS>
-__device__ __forceinline__ void give_carry(int warp) { asm volatile("bar.arrive %0, 64;" ::"r"(warp + (WARPS < 16)) : "memory"); }
+__device__ __forceinline__ void give_carry(int warp) {
+    __syncwarp();
+    asm volatile("bar.arrive %0, 64;" ::"r"(warp + (WARPS < 16)) : "memory");
+}
 
 __device__ __forceinline__ Pair shuffle_up(Pair v, int d) {
     Pair r;
@@ -966,32 +972,30 @@ cudaError_t launch_channels(ScanArgs &s, int64_t tiles, int cluster, cudaStream_
 template <typename T, bool BACK, bool LOGITS>
 cudaError_t launch_channels(ScanArgs &s, cudaStream_t stream) {
     constexpr int S = kStageBytes / ((BACK ? 4 : 2) * 4 * int(sizeof(T)));
-    const auto tiles = [&](int lanes, int warps) {
-        s.groups_log = groups_for(s.steps, S * (32 / lanes), warps);
-        const int64_t per = int64_t(lanes) * 4 * (warps >> s.groups_log);
-        return (s.channels + per - 1) / per;
-    };
-    // whole warps side by side where that fills the GPU
-    const int64_t wide = tiles(32, kScanWarps);
-    if (wide >= int64_t(3) * sm_count()) {
-        // and no more of them to a channel than that needs (100 steps of 200 x 4096 bf16:
-        // 106 us with one, 134 with eight)
-        int64_t tiles_now = wide;
-        while (s.groups_log > 0) {
-            const int64_t per = int64_t(32) * 4 * (kScanWarps >> (s.groups_log - 1)), fewer = (s.channels + per - 1) / per;
-            if (fewer < int64_t(3) * sm_count()) break;
-            --s.groups_log, tiles_now = fewer;
+    // How many lanes have neighbouring channels, and how many warps share a channel: the fewest
+    // rounds of all CTAs one after the other, with one round's time for a CTA to begin
+    // (35 steps of 1500 x 20 fp32, backward: 32 lanes 5.6 us, 8 lanes 10.6; 1000 steps of
+    // 40 x 1024: 84 and 76; 100 steps of 200 x 4096 bf16: one warp 106, eight 134).  Of 64 bytes at
+    // a time memory gives two thirds as much (8 lanes of bf16: 4 x 16384 x 2048 270 us, 16 lanes 172).
+    int lanes = 0;
+    int64_t tiles = 0, least = INT64_MAX;
+    const auto consider = [&](int with, int warps, int price) {
+        for (int log = 0; (1 << log) <= warps; ++log) {
+            const int64_t per = int64_t(with) * 4 * (warps >> log), n = (s.channels + per - 1) / per, room = int64_t(16 / warps) * sm_count();
+            const int64_t rounds = (s.steps + (int64_t(S * (32 / with)) << log) - 1) / (int64_t(S * (32 / with)) << log);
+            const int64_t cost = (n + room - 1) / room * (rounds + 1) * price;
+            if (cost < least) least = cost, lanes = with, tiles = n, s.groups_log = log;
         }
-        return launch_channels<T, BACK, 32, kScanWarps, LOGITS>(s, tiles_now, 1, stream);
-    }
-    // else fewer lanes, and later steps in the others: 128 bytes side by side (of 64 at a
-    // time memory gives two thirds as much: 4 x 16384 x 2048 bf16 270 us against 172)
-    if (sizeof(T) == 2) {
-        const int64_t middle = tiles(16, 16);
-        if (middle * 5 >= int64_t(4) * sm_count()) return launch_channels<T, BACK, 16, 16, LOGITS>(s, middle, 1, stream);
-    }
-    const int64_t narrow = tiles(8, kScanWarps);
-    return launch_channels<T, BACK, 8, kScanWarps, LOGITS>(s, narrow, cluster_for(narrow, s.steps, int64_t(S * 4) << s.groups_log), stream);
+    };
+    consider(32, kScanWarps, 2);
+    if (sizeof(T) == 2) consider(16, 16, 2);
+    consider(8, kScanWarps, sizeof(T) == 2 ? 3 : 2);
+    // (so few channels that a cluster shares them: 8 lanes)
+    if (tiles * 2 <= sm_count()) least = INT64_MAX, consider(8, kScanWarps, 2);
+    if (lanes == 32) return launch_channels<T, BACK, 32, kScanWarps, LOGITS>(s, tiles, 1, stream);
+    if (sizeof(T) == 2 && lanes == 16) return launch_channels<T, BACK, sizeof(T) == 2 ? 16 : 8, sizeof(T) == 2 ? 16 : kScanWarps, LOGITS>(s, tiles, 1, stream);
+    const int cluster = s.groups_log < 3 ? 1 : cluster_for(tiles, s.steps, int64_t(S * 4) << s.groups_log);
+    return launch_channels<T, BACK, 8, kScanWarps, LOGITS>(s, tiles, cluster, stream);
 }
 
 template <typename T, bool BACK, bool LOGITS>
