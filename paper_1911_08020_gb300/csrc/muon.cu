@@ -480,9 +480,9 @@ struct Loads {
 #pragma unroll
             for (int q = 0; q < 4; ++q) di[q] = x.row[min(i0 + 8 * q + sub, rows - 1)];
         }
-        if (x.col != nullptr) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dj[e] = x.col[min(j + e, cols - 1)];
+        if (x.col != nullptr) {   // (as long as a row, and 0 past its end)
+            const float4 d0 = reinterpret_cast<const float4 *>(x.col + j)[0], d1 = reinterpret_cast<const float4 *>(x.col + j)[1];
+            dj[0] = d0.x, dj[1] = d0.y, dj[2] = d0.z, dj[3] = d0.w, dj[4] = d1.x, dj[5] = d1.y, dj[6] = d1.z, dj[7] = d1.w;
         }
         if (OP == kLast && x.vector) {
 #pragma unroll
