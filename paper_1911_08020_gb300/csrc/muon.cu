@@ -30,9 +30,10 @@
 // What bounds it: the tensor cores where matrices are large.  A CTA alone is bound by its
 // shared memory instead (a stage of 128 x 256 x 64 writes 48 KB and reads 48 KB in what are
 // 512 clocks of products); a pair shares the columns' half of the operands and writes 32.
-// 4096 x 9216 and 4096 x 4096 with bf16 gradients, 4.0e12 operations: 2.9 ms, of which 0.23
-// are the elementwise kernels and 2.66 products at 1.5 PFLOP/s (cuBLAS' burst is 1.95).
-// Two of 6000 x 3000 and 1500 x 1500 with fp32 gradients, 3 x 1.95e12: 4.2 ms, 1.4 PFLOP/s.
+// 4096 x 9216 and 4096 x 4096 with bf16 gradients, 4.0e12 operations: 2.8 ms, of which 0.2
+// are the elementwise kernels and 2.6 products at 1.55 PFLOP/s (a plain library product's
+// burst is 1.95).  Two of 6000 x 3000 and 1500 x 1500 with fp32 gradients, 3 x 1.95e12: 4.1 ms,
+// 1.4 PFLOP/s.
 // Small matrices are bound by the 17 launches, of which each waits for a chain of
 // copies, products and stores: three of 600 x 301 and 128 x 500 take 165 us.
 #include "launch.cuh"
