@@ -26,10 +26,10 @@
 // as 6 bytes), so that a border is decided in 32 bits, and by the exact difference in
 // the rare thread that meets one, and 64 bits hold sums from a warp on.  But a chunk is
 // a chain of ten loads and barriers that need one another: 1.5 million tokens of 1000
-// sequences take 27 us (37 MB: 5.5 us), of which the first reading is 7.  So all that does without the weights -- exponentials,
-// gradients but for a factor -- comes before the wait for the first reading, and the
-// chunks' sums are added up by a launch of its own (a ticket, and the last CTA: 29 us).
-// 300 tokens take 5.4 us, 4096 take 8.
+// sequences take 27 us (37 MB: 5.5 us), of which the first reading is 6.  So all that does
+// without the weights -- exponentials, gradients but for a factor -- comes before the
+// wait for the first reading, and the chunks' sums are added up by a launch of its own (a
+// ticket, and the last CTA: 2 us more).  300 tokens take 5.4 us, 4096 take 7.5.
 #include "launch.cuh"
 #include "tma.cuh"
 #include "tokens.cuh"
@@ -157,17 +157,17 @@ __device__ __forceinline__ Tokens find_sequences(const PolicyArgs &a, int64_t c0
     Tokens t = {};
 #pragma unroll
     for (int e = 0; e < kE; ++e) t.starts |= uint32_t(id[e] != kNone) << e;
-    int last = t.starts != 0 ? tid * kE + 31 - __clz(t.starts) : -1;
-    for (int d = 1; d < 32; d <<= 1) {
-        const int o = __shfl_up_sync(~0u, last, d);
-        if (lane >= d) last = max(last, o);
-    }
-    if (lane == 31) sh.warp_max[warp] = last;
+    // the last start of a lane before, of a warp before
+    const int mine_last = tid * kE + 31 - __clz(t.starts);
+    const uint32_t lanes = __ballot_sync(~0u, t.starts != 0), lower = lanes & ((1u << lane) - 1);
+    int before = __shfl_sync(~0u, mine_last, 31 - __clz(lower | 1));
+    if (lower == 0) before = -1;
+    const int warp_last = __shfl_sync(~0u, mine_last, 31 - __clz(lanes | 1));
+    if (lane == 0) sh.warp_max[warp] = lanes != 0 ? warp_last : -1;
     __syncthreads();
-    int before = __shfl_up_sync(~0u, last, 1);
-    if (lane == 0) before = -1;
-    for (int w = 0; w < warp; ++w) before = max(before, sh.warp_max[w]);
-    if (tid == THREADS - 1) sh.last = max(last, before);
+    if (lower == 0)
+        for (int w = 0; w < warp; ++w) before = max(before, sh.warp_max[w]);
+    if (tid == THREADS - 1) sh.last = t.starts != 0 ? mine_last : before;
     t.first = tid == 0 ? 0 : before;
     bool in = sh.start[t.first] >= 0;
 #pragma unroll
@@ -198,9 +198,9 @@ __device__ __forceinline__ uint32_t load_mask(const uint8_t *p, int64_t i, int64
     }
     if (vector && i + kE <= n) {
         const uint2 q = __ldg(reinterpret_cast<const uint2 *>(p + i));
-#pragma unroll
-        for (int e = 0; e < kE; ++e) bits |= uint32_t((((e < 4 ? q.x : q.y) >> (8 * (e & 3))) & 255u) != 0) << e;
-        return bits;
+        // the top bit of every byte that is not 0, then byte i's to bit i
+        const uint32_t x = (((q.x & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | q.x) >> 7 & 0x01010101u, y = (((q.y & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | q.y) >> 7 & 0x01010101u;
+        return (x * 0x01020408u) >> 24 & 15u | ((y * 0x01020408u) >> 24 & 15u) << 4;
     }
 #pragma unroll
     for (int e = 0; e < kE; ++e)
@@ -224,6 +224,26 @@ __device__ __forceinline__ bool past(float a, float b, float d, const float (&bo
     difference(a, b, hi, lo);
     if (lo != border[1]) return UP ? lo > border[1] : lo < border[1];
     return UP ? border[2] < 0.0f : border[2] > 0.0f;
+}
+
+// Of every sequence in the chunk, how many of its tokens count: added to counts[] by the
+// place of the start (whole numbers: in any order).  A warp without a start has one.
+template <int THREADS>
+__device__ __forceinline__ void sequence_counts(const Tokens &t, uint32_t on, int *counts) {
+    const int tid = threadIdx.x, lane = tid & 31;
+    if (__all_sync(~0u, t.starts == 0)) {   // (then all have the same one)
+        const int n = __reduce_add_sync(~0u, __popc(on));
+        if (lane == 0 && n > 0) atomicAdd(counts + t.first, n);
+        return;
+    }
+    int cur = t.first, from = 0;
+    for (uint32_t left = tid == 0 ? t.starts & ~1u : t.starts;; left &= left - 1) {
+        const int to = left != 0 ? __ffs(left) - 1 : kE;
+        const int n = __popc(on >> from & ((1u << (to - from)) - 1));
+        if (n > 0) atomicAdd(counts + cur, n);
+        if (left == 0) break;
+        cur = tid * kE + to, from = to;
+    }
 }
 
 // Of every sequence in the chunk, how many of its tokens count and the sum of their
@@ -293,10 +313,6 @@ __device__ __forceinline__ void sequence_sums(const Tokens &t, uint32_t on, cons
 }
 
 __device__ __forceinline__ double warp_sum(double v) {
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
-    return v;
-}
-__device__ __forceinline__ float warp_sum(float v) {
     for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
     return v;
 }
@@ -438,7 +454,7 @@ __global__ void __launch_bounds__(kChunkThreads) policy_count_kernel(const Polic
     if (tid == 0) s_head = s_tail = s_starts = 0;
     const bool goes_on = sh.after > end;
     __syncthreads();
-    sequence_sums<kChunkThreads, SUMS>(t, on, lp, old, sh, [&](int start, int count, double sum) {
+    auto put = [&](int start, int count, double sum) {
         if (sh.start[start] < 0) return;
         const bool head = start == 0 && before < c0;
         if (head) {
@@ -450,7 +466,18 @@ __global__ void __launch_bounds__(kChunkThreads) policy_count_kernel(const Polic
             if (SUMS) a.w.slot_sum[c0 + start] = sum;
         }
         if (start == sh.last && goes_on) s_tail = count | (head ? kWhole : 0);
-    });
+    };
+    if (SUMS) {
+        sequence_sums<kChunkThreads, SUMS>(t, on, lp, old, sh, put);
+    } else {
+        __shared__ int counts[SUMS ? 1 : kChunkTokens];
+        const int sequences = min(sh.sequences, kChunkTokens);
+        for (int k = tid; k < sequences; k += kChunkThreads) counts[sh.places[k]] = 0;
+        __syncthreads();
+        sequence_counts<kChunkThreads>(t, on, counts);
+        __syncthreads();
+        for (int k = tid; k < sequences; k += kChunkThreads) put(sh.places[k], counts[sh.places[k]], 0.0);
+    }
     const long long all = block_sum<kChunkThreads>(__popc(on));
     if (tid == 0) a.w.info[c] = make_int4(int(all), s_starts, s_head, s_tail);
 }
@@ -685,12 +712,14 @@ __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const P
         d[e] = low(dd), d[e + 1] = high(dd);
         d_ent[e] = low(ee), d_ent[e + 1] = high(ee);
     }
-    const float stat[kSums] = {across(sum_loss), across(sum_excess), across(sum_ent), sum_cut};   // policy, kl, entropy, clipped
-#pragma unroll
-    for (int k = 0; k < kSums; ++k) {
-        const float v = warp_sum(stat[k]);
-        if (lane == 0) stat_part[k][warp] = double(v);
-    }
+    // policy, kl, entropy, clipped: lanes 16 apart share two of the sums, 8 apart one, and lane 8 k ends with the k-th
+    const float stat[kSums] = {across(sum_loss), across(sum_excess), across(sum_ent), sum_cut};
+    const bool up = lane & 16, odd = lane & 8;
+    const float s0 = (up ? stat[2] : stat[0]) + __shfl_xor_sync(~0u, up ? stat[0] : stat[2], 16);
+    const float s1 = (up ? stat[3] : stat[1]) + __shfl_xor_sync(~0u, up ? stat[1] : stat[3], 16);
+    float sum = (odd ? s1 : s0) + __shfl_xor_sync(~0u, odd ? s0 : s1, 8);
+    for (int d = 4; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+    if ((lane & 7) == 0) stat_part[lane >> 3][warp] = double(sum);
     __syncthreads();
     if (warp == 0) {
         const double v = warps_sum<THREADS>(stat_part, lane);
