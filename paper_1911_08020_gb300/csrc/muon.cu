@@ -110,7 +110,8 @@ struct StepArgs {
     const float *grad_scale;
     int32_t *status;
     float *partial;                         // sums of parts of tiles
-    int32_t *arrived;                       // per slot: parts that are done, 0 between launches
+    int32_t *arrived;                       // per slot: parts that are done, 0 between steps (the momentum kernel sets it so)
+    int32_t slots;
     float beta, rest, eps, decay, lr;       // rest: 1 - beta; decay: 1 - lr decay
     int32_t nesterov;
 };
@@ -170,6 +171,8 @@ __global__ void __launch_bounds__(kElemThreads) momentum_kernel(const StepArgs a
     const G *g = static_cast<const G *>(grads.p[part.matrix - grads.first]);
     pdl_wait_previous();
     if (part.part == 0 && threadIdx.x == 0) a.active[part.matrix] = g != nullptr;
+    if (blockIdx.x == 0)   // (a step whose waits gave up may have left some)
+        for (int i = threadIdx.x; i < a.slots; i += kElemThreads) a.arrived[i] = 0;
     if (g == nullptr) return;
     const float scale = a.grad_scale != nullptr ? *a.grad_scale : 1.0f;
     const int64_t all = int64_t(x.rows) * x.cols, e0 = int64_t(part.part) * x.part_elems, e1 = min(e0 + x.part_elems, all);
@@ -1291,7 +1294,7 @@ darb_status_t darb_muon_step(darb_muon_t plan, const void *const *grads, const f
     s.active = plan->d_active;
     s.grad_scale = grad_scale;
     s.status = plan->d_status;
-    s.partial = plan->d_partial, s.arrived = plan->d_arrived;
+    s.partial = plan->d_partial, s.arrived = plan->d_arrived, s.slots = int32_t(plan->schedules[kGram].slots);
     s.beta = float(beta), s.rest = float(1.0 - beta), s.eps = float(eps);
     s.decay = float(1.0 - lr * weight_decay), s.lr = float(lr);
     s.nesterov = nesterov != 0;
