@@ -97,10 +97,6 @@ __device__ __forceinline__ int64_t offsets_upto(const int64_t *offsets, int64_t 
     return lo;
 }
 
-// Where a sequence starts, as a place in the tokens (or their end) whatever the offset holds: what
-// is looked up by it later stays inside the scratch.
-__device__ __forceinline__ int64_t start_of(const PolicyArgs &a, int64_t s) { return min(max(a.offsets[s], int64_t(0)), a.n); }
-
 template <int THREADS>
 struct ChunkShared {
     static constexpr int T = THREADS * kE;
@@ -134,12 +130,13 @@ __device__ __forceinline__ Tokens find_sequences(const PolicyArgs &a, int64_t c0
     if (tid == 0) {
         const bool inside = s0 >= 0 && s0 < a.sequences;
         sh.start[0] = inside ? int(s0) : kOutside;
-        sh.before = inside ? min(start_of(a, s0), c0) : c0;   // (behind c0 only where offsets fall)
+        // (outside of 0 .. c0 only where offsets are wrong: it is a place in the scratch)
+        sh.before = inside ? min(max(a.offsets[s0], int64_t(0)), c0) : c0;
         if (inside) sh.places[atomicAdd(&sh.sequences, 1)] = 0;
     }
     for (int64_t base = s0 + 1;; base += THREADS) {
         const int64_t s = base + tid;
-        const int64_t at = s <= a.sequences ? start_of(a, s) - c0 : T, next = s < a.sequences ? start_of(a, s + 1) - c0 : 0;
+        const int64_t at = s <= a.sequences ? a.offsets[s] - c0 : T, next = s < a.sequences ? a.offsets[s + 1] - c0 : 0;
         const bool in = at < T;
         if (in && at > 0 && c0 + at < a.n) {
             if (s == a.sequences) {
@@ -668,7 +665,7 @@ __global__ void __launch_bounds__(THREADS, SINGLE ? 1 : 3) policy_kernel(const P
         const bool across = warp < 2 && !(warp == 1 && last == 0) && sh.start[p_across] >= 0 &&
                             ((p_across == 0 && from_before) || (p_across == last && goes_on));
         if (across)
-            across_chunks<SUMS>(a, p_across == 0 ? before : c0 + p_across, p_across == last ? sh.after : c0 + T, n_across, sum_across);
+            across_chunks<SUMS>(a, p_across == 0 ? before : c0 + p_across, p_across == last ? min(sh.after, a.n) : c0 + T, n_across, sum_across);
         const int place = tid < sequences ? sh.places[tid] : 0;
         int n_mine = 0;
         double sum_mine = 0.0;
