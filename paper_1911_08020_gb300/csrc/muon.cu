@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kElemThreads, 4) start_kernel(const StepArgs a
     const int parts = x.parts;
     const double *const partial = x.partial;
 #pragma unroll 8
-    for (int i = threadIdx.x; i < parts; i += kElemThreads) sum += __ldg(partial + i);
+    for (int i = threadIdx.x; i < parts; i += kElemThreads) sum += partial[i];
     sum = block_total(sum);
     const float norm = float(sqrt(sum)) + a.eps, scale = a.grad_scale != nullptr ? *a.grad_scale : 1.0f;
     const float factor = kScaleX / norm;

@@ -184,12 +184,12 @@ __device__ __forceinline__ Tokens find_sequences(const PolicyArgs &a, int64_t c0
 // kE tokens from i on (`rest` where n ends before them).
 __device__ __forceinline__ void load8(const float *p, int64_t i, int64_t n, bool vector, float (&v)[kE]) {
     if (vector && i + kE <= n) {
-        const float4 x = __ldg(reinterpret_cast<const float4 *>(p + i)), y = __ldg(reinterpret_cast<const float4 *>(p + i) + 1);
+        const float4 x = reinterpret_cast<const float4 *>(p + i)[0], y = reinterpret_cast<const float4 *>(p + i)[1];
         v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
         return;
     }
 #pragma unroll
-    for (int e = 0; e < kE; ++e) v[e] = i + e < n ? __ldg(p + i + e) : 0.0f;
+    for (int e = 0; e < kE; ++e) v[e] = i + e < n ? p[i + e] : 0.0f;
 }
 // The mask of kE tokens, a bit each.
 __device__ __forceinline__ uint32_t load_mask(const uint8_t *p, int64_t i, int64_t n, bool vector) {
@@ -198,14 +198,14 @@ __device__ __forceinline__ uint32_t load_mask(const uint8_t *p, int64_t i, int64
         return i >= n ? 0u : n - i >= kE ? (1u << kE) - 1 : (1u << int(n - i)) - 1;
     }
     if (vector && i + kE <= n) {
-        const uint2 q = __ldg(reinterpret_cast<const uint2 *>(p + i));
+        const uint2 q = *reinterpret_cast<const uint2 *>(p + i);
         // the top bit of every byte that is not 0, then byte i's to bit i
         const uint32_t x = (((q.x & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | q.x) >> 7 & 0x01010101u, y = (((q.y & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | q.y) >> 7 & 0x01010101u;
         return (x * 0x01020408u) >> 24 & 15u | ((y * 0x01020408u) >> 24 & 15u) << 4;
     }
 #pragma unroll
     for (int e = 0; e < kE; ++e)
-        if (i + e < n && __ldg(p + i + e) != 0) bits |= 1u << e;
+        if (i + e < n && p[i + e] != 0) bits |= 1u << e;
     return bits;
 }
 
