@@ -62,8 +62,8 @@ struct NormArgs {
 // granule, in whole granules.
 __host__ __device__ __forceinline__ int64_t partial_width(int32_t features) { return (int64_t(features) + 7 + 7) / 8 * 8; }
 
-__device__ __forceinline__ float gamma_at(const NormArgs &a, int32_t f) { return a.gamma ? __ldg(a.gamma + f) : 1.0f; }
-__device__ __forceinline__ float beta_at(const NormArgs &a, int32_t f) { return a.beta ? __ldg(a.beta + f) : 0.0f; }
+__device__ __forceinline__ float gamma_at(const NormArgs &a, int32_t f) { return a.gamma ? a.gamma[f] : 1.0f; }
+__device__ __forceinline__ float beta_at(const NormArgs &a, int32_t f) { return a.beta ? a.beta[f] : 0.0f; }
 __device__ __forceinline__ float inverse_root(float v) { return __fdiv_rn(1.0f, __fsqrt_rn(v)); }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -170,7 +170,7 @@ struct Owned {
                 if (partial(u)) unpack(*reinterpret_cast<const uint4 *>(stage + u * step * int(sizeof(T))), v[u]);
                 clear_outside(u, v[u]);
             } else {
-                unpack(load_granule<T, false>(rows.base + r * rows.ld, feature(u), n, 0.0f), v[u]);
+                unpack(load_granule(rows.base + r * rows.ld, feature(u), n, 0.0f), v[u]);
             }
         }
         if (!arrived) v[0][0] = both(__uint_as_float(0x7FC00000u));   // a copy that never came: the row is NaN
@@ -204,12 +204,12 @@ struct Owned {
             if (p != nullptr && whole(u) && (reinterpret_cast<uintptr_t>(p + feature(u)) & 15) == 0) {
 #pragma unroll
                 for (int e = 0; e < V; e += 4) {
-                    const float4 q = __ldg(reinterpret_cast<const float4 *>(p + feature(u) + e));
+                    const float4 q = *reinterpret_cast<const float4 *>(p + feature(u) + e);
                     v[u][e / 2] = pair(q.x, q.y);
                     v[u][e / 2 + 1] = pair(q.z, q.w);
                 }
             } else {
-                const auto at = [&](int e) { return !in(u, e) ? 0.0f : p == nullptr ? none : __ldg(p + feature(u) + e); };
+                const auto at = [&](int e) { return !in(u, e) ? 0.0f : p == nullptr ? none : p[feature(u) + e]; };
 #pragma unroll
                 for (int e = 0; e < V; e += 2) v[u][e / 2] = pair(at(e), at(e + 1));
             }
@@ -222,14 +222,21 @@ struct Owned {
 constexpr int kRowThreads = 512, kHalfThreads = 288;
 constexpr int ctas_of(int most) { return most > kHalfThreads ? 1 : 2; }
 
+enum When : int { kBeforeRow, kAfterRow, kAtUse };
+
 // The mean first, then the squares about it, from registers: two sums over the
 // CTA a row.  A wait that gives up (after a second, and once more so that the
 // copy can land) makes the row NaN; the CTA then copies and waits no more.
-//   8191 x 4096 bf16: 30 us (4.5 TB/s; 6.1 a row, and 6 us to start and drain)
+//   8191 x 4096 bf16: 29 us (4.6 TB/s; 6.1 a row, and 6 us to start and drain)
 //   2700 x 12288 fp32: 49 us (5.4 TB/s), 16384 x 1024 fp32: 24 us (5.6 TB/s)
 template <typename T, int VPT, int STAGES, int MOST>
 __global__ void __launch_bounds__(MOST, ctas_of(MOST)) norm_rows_kernel(const NormArgs a, int32_t stage_bytes) {
     constexpr int V = kPerGranule<T>, H = V / 2;
+    // Gain and offset are needed at the end of the first row.  Where they are loaded: before the
+    // wait for that row, after it has been taken, or where they are used.  (Before anything else, after
+    // the row, at their use: 8191 x 4096 bf16 31.3, 29.7, 28.9 us; 2700 x 12288 fp32 53.9, 49.8, 51.8;
+    // before the wait for the row, at their use: 16 x 1024 fp32 3.0 and 3.2.)
+    constexpr int kWhen = sizeof(T) == 2 ? kAtUse : VPT == 4 ? kBeforeRow : kAfterRow;
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ __align__(16) float buf[2 * kSumWarps];
     __shared__ uint64_t full[STAGES];
@@ -255,8 +262,6 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) norm_rows_kernel(const No
     // all rows of this CTA start alike
     const Owned<T, VPT> own = {t * V - row_head<T>(rows.base + r0 * a.ld_x), threads * V, n};
     Pair gm[VPT][H], bt[VPT][H];
-    own.gather(a.gamma, 1.0f, gm);
-    own.gather(a.beta, 0.0f, bt);
     clear_sums(buf, 2 * kSumWarps);
     T *y = static_cast<T *>(a.out);
     int turn = 0, stage = 0;
@@ -264,8 +269,10 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) norm_rows_kernel(const No
     bool arrived = true;
     for (int64_t r = r0; r < a.tokens; r += stride) {
         Pair v[VPT][H], s2 = both(0.0f);
+        if (kWhen == kBeforeRow && r == r0) own.gather(a.gamma, 1.0f, gm), own.gather(a.beta, 0.0f, bt);
         arrived = arrived && (mbar_wait(&full[stage], parity) || mbar_wait(&full[stage], parity));
         own.load(rows, r, ring + stage * stage_bytes + t * 16, arrived, v);
+        if (kWhen == kAfterRow && r == r0) own.gather(a.gamma, 1.0f, gm), own.gather(a.beta, 0.0f, bt);
 #pragma unroll
         for (int u = 0; u < VPT; ++u)
 #pragma unroll
@@ -291,6 +298,7 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) norm_rows_kernel(const No
             if (a.mean) a.mean[r] = mean;
             if (a.rstd) a.rstd[r] = rstd;
         }
+        if (kWhen == kAtUse && r == r0) own.gather(a.gamma, 1.0f, gm), own.gather(a.beta, 0.0f, bt);
 #pragma unroll
         for (int u = 0; u < VPT; ++u)
 #pragma unroll
@@ -324,6 +332,11 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const No
     const int32_t n = a.features, half = stage_bytes / 2;
     const RowCopies<T> xs(a.x, a.ld_x, a.tokens, n), ds(a.dy, a.ld_dy, a.tokens, n);
     const int64_t stride = gridDim.x, r0 = blockIdx.x;
+    const Owned<T, VPT> own = {t * V - row_head<T>(xs.base + r0 * a.ld_x), threads * V, n};
+    Pair gm[VPT][H];
+    float mean_next = 0.0f, rstd_next = 0.0f;
+    if (r0 < a.tokens) mean_next = a.mean[r0], rstd_next = a.rstd[r0];
+    own.gather(a.gamma, 1.0f, gm);
     const auto issue = [&](int64_t r, int s) {
         mbar_arrive_expect_tx(&full[s], xs.bytes(r) + ds.bytes(r));
         xs.copy(r, ring + s * stage_bytes, &full[s]);
@@ -333,9 +346,7 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const No
         for (int s = 0; s < STAGES; ++s)
             if (r0 + s * stride < a.tokens) issue(r0 + s * stride, s);
     const float inv_n = __fdiv_rn(1.0f, float(n));
-    const Owned<T, VPT> own = {t * V - row_head<T>(xs.base + r0 * a.ld_x), threads * V, n};
-    Pair gm[VPT][H], sg[REGISTERS ? VPT : 1][H], sb[REGISTERS ? VPT : 1][H];
-    own.gather(a.gamma, 1.0f, gm);
+    Pair sg[REGISTERS ? VPT : 1][H], sb[REGISTERS ? VPT : 1][H];
     // granule g of the row: V sums for dgamma, V for dbeta, at 16 bytes a thread
     float4 *sums = reinterpret_cast<float4 *>(ring + STAGES * stage_bytes) + t;
     const auto place = [&](int u, int q) { return (u * (V / 2) + q) * threads; };   // q: V / 4 words of one sum, V / 4 of the other
@@ -356,12 +367,10 @@ __global__ void __launch_bounds__(MOST, ctas_of(MOST)) back_rows_kernel(const No
     int turn = 0, stage = 0;
     uint32_t parity = 0;
     bool arrived = true;
-    float mean_next = 0.0f, rstd_next = 0.0f;
-    if (r0 < a.tokens) mean_next = __ldg(a.mean + r0), rstd_next = __ldg(a.rstd + r0);
     for (int64_t r = r0; r < a.tokens; r += stride) {
         Pair xh[VPT][H], d[VPT][H], s0 = both(0.0f), s1 = both(0.0f);
         const float mean = mean_next, rstd = rstd_next;
-        if (r + stride < a.tokens) mean_next = __ldg(a.mean + r + stride), rstd_next = __ldg(a.rstd + r + stride);
+        if (r + stride < a.tokens) mean_next = a.mean[r + stride], rstd_next = a.rstd[r + stride];
         arrived = arrived && (mbar_wait(&full[stage], parity) || mbar_wait(&full[stage], parity));
         const unsigned char *at = ring + stage * stage_bytes + t * 16;
         own.load(xs, r, at, arrived, xh);
@@ -552,8 +561,8 @@ __global__ void __launch_bounds__(kAnyThreads) row_sums_kernel(const NormArgs a)
             const bool in = at < a.tokens;
             qx[u] = in ? load_granule(x + at * a.ld_x, f, n, 0.0f) : make_uint4(0, 0, 0, 0);
             qd[u] = in ? load_granule(dy + at * a.ld_dy, f, n, 0.0f) : make_uint4(0, 0, 0, 0);   // 0 adds nothing
-            mean[u] = in ? __ldg(a.mean + at) : 0.0f;
-            rstd[u] = in ? __ldg(a.rstd + at) : 0.0f;
+            mean[u] = in ? a.mean[at] : 0.0f;
+            rstd[u] = in ? a.rstd[at] : 0.0f;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -594,7 +603,7 @@ __global__ void __launch_bounds__(kAnyThreads) any_sums_kernel(const NormArgs a)
 #pragma unroll 8
         for (int64_t r = r0; r < end; r += stride) {
             const float d = widen(dy[r * a.ld_dy]);
-            bg = fmaf(d, (widen(x[r * a.ld_x]) - __ldg(a.mean + r)) * __ldg(a.rstd + r), bg);
+            bg = fmaf(d, (widen(x[r * a.ld_x]) - a.mean[r]) * a.rstd[r], bg);
             bb += d;
         }
         sg += bg;
@@ -636,7 +645,7 @@ __global__ void __launch_bounds__(kNarrowThreads) norm_narrow_kernel(const NormA
     own.gather(a.beta, 0.0f, bt);
     const int64_t rounds = (a.tokens - 1) / stride + 1;   // the same for all lanes of a warp
     const auto fetch = [&](int64_t r) {
-        return r < a.tokens ? load_granule<T, false>(x + r * a.ld_x, own.f0, n, 0.0f) : make_uint4(0, 0, 0, 0);
+        return r < a.tokens ? load_granule(x + r * a.ld_x, own.f0, n, 0.0f) : make_uint4(0, 0, 0, 0);
     };
     uint4 next = fetch(r0);
     int64_t r = r0;
@@ -690,9 +699,9 @@ __global__ void __launch_bounds__(kNarrowThreads) back_narrow_kernel(const NormA
     const auto fetch = [&](int64_t r) {
         const bool in = r < a.tokens;
         nx = in ? load_granule(x + r * a.ld_x, own.f0, n, 0.0f) : make_uint4(0, 0, 0, 0);
-        nd = in ? load_granule<T, false>(dy + r * a.ld_dy, own.f0, n, 0.0f) : make_uint4(0, 0, 0, 0);   // 0 adds nothing
-        mean_next = in ? __ldg(a.mean + r) : 0.0f;
-        rstd_next = in ? __ldg(a.rstd + r) : 0.0f;
+        nd = in ? load_granule(dy + r * a.ld_dy, own.f0, n, 0.0f) : make_uint4(0, 0, 0, 0);   // 0 adds nothing
+        mean_next = in ? a.mean[r] : 0.0f;
+        rstd_next = in ? a.rstd[r] : 0.0f;
     };
     fetch(r0);
     int64_t r = r0;
@@ -772,10 +781,10 @@ struct ColShare {
             for (int u = 0; u < U; ++u) v[u] = none;
         } else if (full(batch)) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = __ldg(p + u * SLOTS);
+            for (int u = 0; u < U; ++u) v[u] = p[u * SLOTS];
         } else {
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = feature(batch, u) < end ? __ldg(p + u * SLOTS) : 0.0f;
+            for (int u = 0; u < U; ++u) v[u] = feature(batch, u) < end ? p[u * SLOTS] : 0.0f;
         }
     }
     __device__ __forceinline__ void store(T *y, int64_t ld, int batch, const float (&v)[U]) const {

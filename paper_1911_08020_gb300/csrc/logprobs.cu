@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(THREADS) score_rows_kernel(const ScoreArgs a, 
     const auto fetch = [&](uint4 (&q)[U], int32_t g) {
         if (g >= whole0 && g + THREADS * U <= min(g1, whole1)) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) q[u] = __ldg(aligned + g + u * THREADS + tid);
+            for (int u = 0; u < U; ++u) q[u] = aligned[g + u * THREADS + tid];
             return;
         }
 #pragma unroll
@@ -961,7 +961,7 @@ __device__ __noinline__ void wide_row(Args a, int64_t token, const T *row, T *ou
     const int head = row_head<T>(row);
     const int32_t n = a.vocab, granules = int32_t(row_granules<T>(head, n));
     const bool alike = row_head<T>(out) == head;
-    const auto fetch = [&](int32_t g, float (&v)[V]) { unpack(load_granule<T, false>(row, int64_t(g) * V - head, n, -INFINITY), v); };
+    const auto fetch = [&](int32_t g, float (&v)[V]) { unpack(load_granule(row, int64_t(g) * V - head, n, -INFINITY), v); };
     float m = -INFINITY, s = 0.0f;
     for (int32_t g = threadIdx.x; g < granules; g += blockDim.x) {
         float v[V];
@@ -1112,7 +1112,7 @@ __global__ void __launch_bounds__(THREADS) grad_rows_kernel(const __grid_constan
 #pragma unroll
         for (int u = 0; u < B; ++u) {
             const int32_t g = at + u * THREADS;
-            if (g < granules) q[u] = load_granule<T, false>(row, int64_t(g) * V - head, n, -INFINITY);
+            if (g < granules) q[u] = load_granule(row, int64_t(g) * V - head, n, -INFINITY);
         }
         const GradToken own = B == 1 ? t : grad_token(a, token);   // (after the loads)
         if (is_wide_lse(own.lse)) {   // (in the first round, and for all threads)

@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
 #pragma unroll
                 for (int k = 0; k < IN; ++k) {
                     raw[k][j] = from[(k * J + j) * kScanThreads];
-                    if (!whole(t) && t < steps) raw[k][j] = load_granule<T, false>(in[k], t, steps, 0.0f);
+                    if (!whole(t) && t < steps) raw[k][j] = load_granule(in[k], t, steps, 0.0f);
                 }
             }
         }

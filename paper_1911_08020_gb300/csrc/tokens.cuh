@@ -73,14 +73,13 @@ __host__ __device__ __forceinline__ int64_t row_granules(int head, int64_t n) {
 }
 
 // Elements j0 .. j0 + V of a row (j0 = granule * V - head, so that row + j0 is
-// 16-byte aligned), `fill` outside [0, n).  READ_ONLY: nothing writes the row
-// while the kernel runs.
-template <typename T, bool READ_ONLY = true>
+// 16-byte aligned), `fill` outside [0, n).  (Not through the read-only path: the
+// kernel ahead may write the row while this one is resident.)
+template <typename T>
 __device__ __forceinline__ uint4 load_granule(const T *row, int64_t j0, int64_t n, float fill) {
     constexpr int V = kPerGranule<T>;
     if (j0 >= 0 && j0 + V <= n) {
-        const uint4 *p = reinterpret_cast<const uint4 *>(row + j0);
-        return READ_ONLY ? __ldg(p) : *p;
+        return *reinterpret_cast<const uint4 *>(row + j0);
     }
     float v[V];
 #pragma unroll

@@ -12,7 +12,7 @@ import pytest
 from paper_1911_08020_gb300.build import CSRC
 
 
-@pytest.mark.parametrize("name", ["policy.cu", "muon.cu"])
+@pytest.mark.parametrize("name", ["adamw.cu", "layer_norm.cu", "logprobs.cu", "muon.cu", "policy.cu", "scan.cu", "tokens.cuh"])
 def test_no_read_only_loads(name):
     with open(os.path.join(CSRC, name)) as f:
         code = re.sub(r"//[^\n]*|/\*.*?\*/", "", f.read(), flags=re.S)
