@@ -709,8 +709,8 @@ DARB_API darb_status_t darb_muon_create(int32_t n, const int64_t *rows, const in
  * Asynchronous on `stream`; allocates nothing; 17 launches (two more for every further
  * 448 matrices).  Results do not depend on the order of anything.  Steps of one plan must
  * be ordered on one stream.
- * Errors: DARB_ERR_INVALID_ARG (an unknown plan, lr or weight_decay negative or not finite, beta
- * outside [0, 1), eps not above 0 or not finite, a gradient or grad_scale that overlaps a
+ * Errors: DARB_ERR_INVALID_ARG (an unknown plan; lr or weight_decay negative; lr, eps or 1 - lr weight_decay
+ * not finite in 32 bits; beta outside [0, 1); an eps that is not above 0 in 32 bits; a gradient or grad_scale that overlaps a
  * buffer of any of the plan's matrices); DARB_ERR_CUDA.
  */
 DARB_API darb_status_t darb_muon_step(darb_muon_t plan, const void *const *grads, const float *grad_scale, double lr,

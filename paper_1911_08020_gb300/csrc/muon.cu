@@ -1276,8 +1276,9 @@ darb_status_t darb_muon_step(darb_muon_t plan, const void *const *grads, const f
                              double eps, int nesterov, cudaStream_t stream) {
     DARB_TRACE("darb_muon_step");
     if (!live_plan(plan) || grads == nullptr || !aligned_to(grad_scale, 4)) return DARB_ERR_INVALID_ARG;
-    if (!(lr >= 0.0 && std::isfinite(lr)) || !(beta >= 0.0 && beta < 1.0) || !(eps > 0.0 && std::isfinite(eps)) ||
-        !(weight_decay >= 0.0 && std::isfinite(weight_decay)))
+    // (what counts is what the kernels get: an eps that 32 bits round to 0 would make 0 / 0 of zero gradients)
+    if (!(lr >= 0.0 && std::isfinite(float(lr))) || !(beta >= 0.0 && beta < 1.0) || !(float(eps) > 0.0f && std::isfinite(float(eps))) ||
+        !(weight_decay >= 0.0 && std::isfinite(float(1.0 - lr * weight_decay))))
         return DARB_ERR_INVALID_ARG;
     if (grad_scale != nullptr && meets_written(*plan, grad_scale, 4)) return DARB_ERR_INVALID_ARG;
     const size_t es = dtype_size(plan->gtype);
