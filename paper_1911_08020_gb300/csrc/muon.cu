@@ -237,8 +237,10 @@ __global__ void __launch_bounds__(kElemThreads, 4) start_kernel(const StepArgs a
 #pragma unroll 8
     for (int i = threadIdx.x; i < parts; i += kElemThreads) sum += partial[i];
     sum = block_total(sum);
-    const float norm = float(sqrt(sum)) + a.eps, scale = a.grad_scale != nullptr ? *a.grad_scale : 1.0f;
-    const float factor = kScaleX / norm;
+    const double root = sqrt(sum);
+    const float norm = float(root) + a.eps, scale = a.grad_scale != nullptr ? *a.grad_scale : 1.0f;
+    // (numbers that 32 bits hold may have a norm that they do not)
+    const float factor = norm < INFINITY ? kScaleX / norm : float(double(kScaleX) / (root + double(a.eps)));
     const bool divide = !(factor < INFINITY);   // (a norm too small for its reciprocal)
     const int64_t all = int64_t(x.rows) * x.cols, e0 = int64_t(part.part) * x.part_elems, e1 = min(e0 + x.part_elems, all);
     const bool vector = aligned16(x.m) && (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) == 0;

@@ -1,8 +1,12 @@
 """Orthogonalised momentum at the ends of what 32 bits hold (the refusals: test_muon_numbers.py)."""
+import math
+
+import numpy as np
 import pytest
 import torch
 
 from paper_1911_08020_gb300 import darb
+from tests.muon_reference import COEFFICIENTS, step
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -26,3 +30,33 @@ def test_zero_gradients_at_any_eps(dtype, eps):
         darb.darb_muon_sync_status(plan)
     for t, k in zip(p, keep):
         assert bool(((t.double() - 0.95 * k.double()).abs() <= 2 * U * k.double().abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("size,eps", [(2e38, 1e-7), (2e38, 3e38), (1e38, 3e38)])
+def test_a_norm_past_32_bits(dtype, size, eps):
+    """The norm of numbers that 32 bits hold, and its sum with eps, may be past their range.
+
+    The matrix has one number in a row, none in a column twice: all of its singular values are the same s, X keeps its
+    form, and every product has one term.  So a step is s' = a s + b s^3 + c s^5, whose terms have up to five factors
+    that are off by e relative to themselves: 2^-12 (bf16 gradients: one fp16 number) or 2^-21 (two of them).  What a
+    step is off by goes through the derivatives of the steps after it; s at the start, by 5 e."""
+    n = 600
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    g = torch.zeros(n, n + 7, device="cuda", dtype=dtype)
+    g[torch.arange(n, device="cuda"), torch.randperm(n + 7, generator=gen, device="cuda")[:n]] = size
+    p, m = [torch.zeros(n, n + 7, device="cuda")], [torch.zeros(n, n + 7, device="cuda")]
+    with darb.darb_muon_create(p, m, grad_dtype=dtype) as plan:
+        darb.darb_muon_step(plan, [g], 0.1, weight_decay=0.0, eps=eps)
+        darb.darb_muon_sync_status(plan)
+    _, _, x = step(np.zeros(g.shape), np.zeros(g.shape), g.double().cpu().numpy(), 0.1, eps=eps)
+    got = p[0].double().cpu().numpy() / -(0.1 * 0.2 * math.sqrt(max(g.shape)))
+    a, b, c = COEFFICIENTS
+    u = g.max().item() * 0.05 * 1.95
+    s = u / (math.sqrt(n) * u + eps)
+    off, e = 5 * s, 2.0 ** -12 if dtype == torch.bfloat16 else 2.0 ** -21
+    for _ in range(5):
+        off = abs(a + 3 * b * s ** 2 + 5 * c * s ** 4) * off + 5 * (a * s + abs(b) * s ** 3 + c * s ** 5)
+        s = a * s + b * s ** 3 + c * s ** 5
+    assert abs(np.abs(x).max() - s) < 1e-9 and off * 2.0 ** -12 < 0.1 * s   # (the bound tells X from 0)
+    assert np.abs(got - x).max() <= off * e
