@@ -736,7 +736,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
                 }
             }
             // what is still on its way lands before the CTA leaves (in the second CTA: when the pair's products have
-            // been waited for, below)
+            // been waited for, at the end)
             if (!ok && rank == 0)
                 for (int64_t i = issued > NS ? issued - NS : 0; i < issued; ++i) mbar_wait(&full[i % NS], uint32_t(i / NS) & 1u);
         }
@@ -787,8 +787,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
             }
             pair_commit<CG>(done);
         }
-        // no product is in flight when the memory is given back
-        if (lane == 0 && !mbar_wait(done, 0)) ok = false;
         __syncwarp();
     } else {
         // two warps for each quarter of the accumulator's rows, with half of the columns each
@@ -863,9 +861,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
             }
         }
     }
-    if (!ok) atomicOr(s.status, kStatusTimeout);
     tc_fence_before_sync();
     __syncthreads();
+    // No product is in flight when the memory is given back.  (Waited for when this CTA's tiles have been written:
+    // a pair's second CTA issues none, and from its start this would be a wait for the whole launch.)
+    if (warp == 1) {
+        if (lane == 0 && !mbar_wait(done, 0)) ok = false;
+        __syncwarp();
+    }
+    if (!ok) atomicOr(s.status, kStatusTimeout);
     if (CG == 2) pair_meet();   // neither CTA leaves while the other may reach into it
     if (warp == 1) {
         tc_fence_after_sync();

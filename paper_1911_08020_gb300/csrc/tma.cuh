@@ -10,7 +10,10 @@
 
 namespace darb {
 
-constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // 1 s
+#ifndef DARB_WAIT_LIMIT_NS   // (a test builds a kernel with a shorter one)
+#define DARB_WAIT_LIMIT_NS 1000000000   // 1 s
+#endif
+constexpr unsigned long long kWaitLimitNs = DARB_WAIT_LIMIT_NS;
 
 // Device status word bits (sticky until read by darb_sync_status).
 constexpr int kStatusNaN = 1;
