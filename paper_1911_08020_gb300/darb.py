@@ -931,9 +931,10 @@ def darb_adamw_destroy(plan: AdamW | None):
 class Muon:
     """A plan of darb_muon_create (owned; free with darb_muon_destroy).  Holds on to its tensors."""
 
-    def __init__(self, ptr: int, tensors, numels, grad_dtype):
-        self.ptr, self.tensors, self.numels, self.grad_dtype = ptr, tensors, numels, grad_dtype
-        self.pointers = (ctypes.c_void_p * len(numels))()
+    def __init__(self, ptr: int, tensors, shapes, grad_dtype):
+        self.ptr, self.tensors, self.shapes, self.grad_dtype = ptr, tensors, shapes, grad_dtype
+        self.numels = [s.numel() for s in shapes]
+        self.pointers = (ctypes.c_void_p * len(shapes))()
 
     def __enter__(self):
         return self
@@ -968,15 +969,18 @@ def darb_muon_create(params, m, copies=None, grad_dtype=None, stream=None) -> Mu
     out = ctypes.c_void_p()
     _check(lib().darb_muon_create(n, *sides, array(params), array(m), None if copies is None else array(copies),
                                   BF16 if grad_dtype == torch.bfloat16 else F32, ctypes.byref(out), _stream(stream)), call)
-    return Muon(out.value, [params, m, copies], [p.numel() for p in params], grad_dtype)
+    return Muon(out.value, [params, m, copies], [p.shape for p in params], grad_dtype)
 
 
 def darb_muon_step(plan: Muon, grads, lr: float, beta: float = 0.95, weight_decay: float = 0.01, eps: float = 1e-7,
                    nesterov: bool = True, grad_scale=None, stream=None):
-    """One step with the gradients `grads` of the plan's matrices (None: that matrix is left as it is).
-    grad_scale: float32 CUDA scalar that multiplies every gradient."""
+    """One step with the gradients `grads` of the plan's matrices, of their shapes (None: that matrix is left as it
+    is).  grad_scale: float32 CUDA scalar that multiplies every gradient."""
     call = "darb_muon_step"
     pointers = _gradient_pointers(plan, grads, call)
+    for i, (g, shape) in enumerate(zip(grads, plan.shapes)):   # rows and columns matter here
+        if g is not None and g.shape != shape:
+            _refuse(call, f"gradient {i} must have its matrix's shape")
     _check(lib().darb_muon_step(plan.ptr, pointers, _vector(grad_scale, 1, (_torch or _load_torch()).float32, call, "grad_scale"),
                                 lr, beta, weight_decay, eps, bool(nesterov), _stream(stream)), call)
 

@@ -60,3 +60,20 @@ def test_a_norm_past_32_bits(dtype, size, eps):
         s = a * s + b * s ** 3 + c * s ** 5
     assert abs(np.abs(x).max() - s) < 1e-9 and off * 2.0 ** -12 < 0.1 * s   # (the bound tells X from 0)
     assert np.abs(got - x).max() <= off * e
+
+
+def test_a_gradient_of_another_shape_is_refused():
+    """As many numbers, side by side, but other rows: the transpose's, a vector's.  Nothing is written."""
+    p = [torch.randn(8, 6, device="cuda"), torch.randn(5, 5, device="cuda")]
+    keep, m = [t.clone() for t in p], [torch.zeros_like(t) for t in p]
+    g = [torch.randn_like(t) for t in p]
+    with darb.darb_muon_create(p, m) as plan:
+        for bad in (g[0].t().contiguous(), g[0].view(-1), g[0].view(4, 12), g[0].view(1, 8, 6)):
+            with pytest.raises(darb.DarbError):
+                darb.darb_muon_step(plan, [bad, g[1]], 0.1)
+            with pytest.raises(darb.DarbError):
+                darb.darb_muon_step(plan, [bad, None], 0.1)
+        darb.darb_muon_sync_status(plan)
+        assert all(torch.equal(t, k) for t, k in zip(p, keep)) and not any(t.any() for t in m)
+        darb.darb_muon_step(plan, g, 0.1)
+        assert not torch.equal(p[0], keep[0])
