@@ -580,6 +580,7 @@ typedef enum { DARB_PER_TOKEN = 0, DARB_PER_SEQUENCE = 1 } darb_per_t;
  *            (else results are not defined, but nothing outside the buffers is touched).
  *            Tokens before the first and behind the last sequence do not count
  *   clip_low   0 .. 1 (1: r is not clipped from below); clip_high >= 0 (+inf: not from above)
+ *   kl_coef, entropy_coef   finite as 32 bits hold them
  *   stats    device fp32[5]: loss, policy, kl, entropy, and the share of the weight whose
  *            ratio is clipped; terms without their buffers are 0
  *   d_logprob, d_entropy   device fp32[tokens]: the gradients of the loss; d_entropy NULL: not

@@ -834,7 +834,8 @@ darb_status_t darb_policy_loss(int64_t tokens, int64_t sequences, const float *l
     DARB_TRACE("darb_policy_loss");
     if (tokens < 0 || sequences < 0 || stats == nullptr || offsets == nullptr) return DARB_ERR_INVALID_ARG;
     if ((ratio != DARB_PER_TOKEN && ratio != DARB_PER_SEQUENCE) || (mean != DARB_PER_TOKEN && mean != DARB_PER_SEQUENCE)) return DARB_ERR_INVALID_ARG;
-    if (!(clip_low >= 0.0 && clip_low <= 1.0) || !(clip_high >= 0.0) || !std::isfinite(kl_coef) || !std::isfinite(entropy_coef))
+    // (the kernels get the coefficients in 32 bits)
+    if (!(clip_low >= 0.0 && clip_low <= 1.0) || !(clip_high >= 0.0) || !std::isfinite(float(kl_coef)) || !std::isfinite(float(entropy_coef)))
         return DARB_ERR_INVALID_ARG;
     if (tokens > 0 && (logprob == nullptr || old_logprob == nullptr || d_logprob == nullptr)) return DARB_ERR_INVALID_ARG;
     if (sequences > 0 && advantage == nullptr) return DARB_ERR_INVALID_ARG;
