@@ -590,7 +590,7 @@ typedef enum { DARB_PER_TOKEN = 0, DARB_PER_SEQUENCE = 1 } darb_per_t;
  * Where nothing counts the stats and gradients are 0.  A border is decided as the exact
  * difference decides it; sums are in a fixed order, over more than 256 tokens in 64 bits.
  * No output may overlap another buffer.  Asynchronous on `stream`; allocates nothing but work;
- * one launch up to 4096 tokens, else three (past 8 million, four).
+ * one launch up to 4096 tokens, else three (past 1.6 million, four).
  * Errors: DARB_ERR_INVALID_ARG; DARB_ERR_UNSUPPORTED (more than 2^27 tokens or sequences);
  * DARB_ERR_OOM; DARB_ERR_CUDA.
  */
