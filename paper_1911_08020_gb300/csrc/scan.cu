@@ -50,7 +50,10 @@ constexpr int kScanThreads = 256;
 constexpr int kScanWarps = kScanThreads / 32;
 constexpr int kElems = 16;          // elements of a thread in a round
 constexpr int kMaxCluster = 8;
-constexpr int kNarrow = 8;          // fewer contiguous channels than this: runs of steps go through shared memory
+// Fewer contiguous channels than this: runs of steps go through shared memory.  fp32, us with that and without, forward
+// and backward: 40000 x 1000 x 1 (unaligned) 277 and 313, 396 and 620; 30000 x 1000 x 2 393 and 287, 568 and 640;
+// 100 x 20000 x 3 152 and 106, 128 and 137 (but 30000 x 1000 x 3 backward 855 and 749); x 5 977 and 438, 1422 and 922.
+constexpr int kNarrow = 2, kNarrowBack = 4;
 constexpr int kRun = kScanWarps * kElems;   // steps of a CTA in a round there
 
 // The element (outer o, step t, inner i) of a tensor is at o * ld + t * step + i.
@@ -677,7 +680,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
 
 // ---- anything else, an element at a time ----
 
-// STAGED: fewer than kNarrow channels lie together, so that a warp's loads would
+// STAGED: few channels lie together (kNarrow), so that a warp's loads would
 // touch a sector for every lane.  There a CTA takes 32 / inner rows of kRun steps
 // each, read and written along the rows, and turns them through shared memory (rows
 // `inner` floats longer than their steps: a warp's 32 channels hit 32 banks).
@@ -705,8 +708,8 @@ strided_kernel(const ScanArgs s, const int cluster) {
     const int inner = s.inner;
     const int rows = STAGED ? 32 / inner : 0;                  // rows of a tile
     const int run = kRun * inner, pitch = run + inner;
-    // e / inner for e < 4096 and inner < 8: 65536 / inner rounded up is off by less than one
-    // part in 4096 * 7 / 65536 of the quotient's unit
+    // e / inner for e < 4096 and inner < 4: 65536 / inner rounded up is off by less than one
+    // part in 4096 * 3 / 65536 of the quotient's unit
     const uint32_t part = STAGED ? (65536u + inner - 1) / inner : 0;
     auto over_inner = [&](int e) { return int(uint32_t(e) * part >> 16); };
 
@@ -953,7 +956,8 @@ int groups_for(int64_t steps, int64_t per, int warps = kScanWarps) {
     return log;
 }
 // CTAs that share channels: while the GPU holds two of `tiles` CTAs on an SM, and the
-// steps go round.
+// steps go round.  (With it, without, to half and to twice as many CTAs, us: 64 rows of 20011 fp32 8.7, 11.9, 11.5, 10.9;
+// 4 x 16384 x 256 bf16 52, 124, 72, 49, backward 99, 279, 154, 98; 16384 x 4 x 64 fp32 37, 102, 38, 38.)
 int cluster_for(int64_t tiles, int64_t steps, int64_t per) {
     int cluster = 1;
     while (cluster < kMaxCluster && tiles * cluster <= sm_count() && per * cluster < steps) cluster *= 2;
@@ -1117,7 +1121,7 @@ Form form_of(const Operand (&all)[N], const Shape &n, size_t es) {
         const auto past0 = [&](int64_t row) { return (reinterpret_cast<uintptr_t>(all[0].p) + uintptr_t(row * all[0].ld) * es) % 16; };
         rows = rows && (n.steps == 1 || o.step == 1) && past(0) == past0(0) && (n.outer == 1 || past(1) == past0(1));
     }
-    return vectors ? kChannels : rows ? kRows : n.inner < kNarrow ? kStaged : kStrided;
+    return vectors ? kChannels : rows ? kRows : n.inner < (N > 3 ? kNarrowBack : kNarrow) ? kStaged : kStrided;   // (backward: six operands)
 }
 
 bool same(const Operand &a, const Operand &b) { return a.p == b.p && a.ld == b.ld && a.step == b.step; }
