@@ -51,9 +51,9 @@ constexpr int kE = 8;                       // tokens of a thread
 constexpr int kFew = 4096, kVeryFew = 1024;
 constexpr int kChunkThreads = 256;
 constexpr int kChunkTokens = kChunkThreads * kE;
-// Chunks that every CTA adds up itself instead of a launch of its own: tokens and, mean of sequences, us with it
-// and without: 400000 11.5 and 15.9, 11.7 and 15.3; 1.5 million 24.0 and 25.5, 25.5 and 25.2; 1.8 million 27.2 and 27.2, 29.7
-// and 27.3; 8 million 116 and 92, 148 and 92.
+// Chunks that every CTA adds up itself, not a launch of its own.  Us without that launch and with it, every token counting
+// the same, and every sequence: 400000 tokens 11.5 and 15.9, 11.7 and 15.3; 1.5 million 24.0 and 25.5, 25.5 and 25.2;
+// 1.8 million 27.2 and 27.2, 29.7 and 27.3; 8 million 116 and 92, 148 and 92.
 constexpr int kInline = 800;
 constexpr int kStats = 5;                   // loss, policy, kl, entropy, clipped
 constexpr int kSums = 4;                    // the sums that they come from

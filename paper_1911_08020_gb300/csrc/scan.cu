@@ -74,17 +74,17 @@ struct ScanArgs {
     int32_t coupled;
 };
 
-// V neighbouring elements as they lie in memory.
-template <typename T, int V>
+// Four neighbouring elements as they lie in memory.
+template <typename T>
 struct Word;
 template <>
-struct Word<float, 4> {
+struct Word<float> {
     float4 w;
     __device__ __forceinline__ void get(Pair (&v)[2]) const { v[0] = pair(w.x, w.y), v[1] = pair(w.z, w.w); }
     __device__ __forceinline__ void set(const Pair (&v)[2]) { w = make_float4(low(v[0]), high(v[0]), low(v[1]), high(v[1])); }
 };
 template <>
-struct Word<__nv_bfloat16, 4> {
+struct Word<__nv_bfloat16> {
     uint2 w;
     __device__ __forceinline__ void get(Pair (&v)[2]) const {
         const float2 a = widen2(w.x), b = widen2(w.y);
@@ -95,13 +95,6 @@ struct Word<__nv_bfloat16, 4> {
         w = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
     }
 };
-template <typename T>
-struct Word<T, 1> {
-    T w;
-    __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = widen(w); }
-    __device__ __forceinline__ void set(const float (&v)[1]) { w = narrow<T>(v[0]); }
-};
-
 // 1 / x, one instruction (off by one unit; of infinity 0).
 __device__ __forceinline__ float reciprocal(float x) {
     float y;
@@ -234,7 +227,7 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) channel_kernel(const S
     constexpr int TL = 32 / LC, NS = kStages;
     constexpr bool kMayCluster = LC < 16;
     constexpr int kThreads = WARPS * 32;
-    using Raw = Word<T, V>;
+    using Raw = Word<T>;
     constexpr int CW = kMayCluster ? WARPS : 1, CC = kMayCluster ? kMaxCluster : 1;
     __shared__ Quad s_carry[WARPS][LC], s_A[2][CW][LC], s_H[2][CW][LC];
     __shared__ float4 s_rA[2][CC][LC], s_rH[2][CC][LC];
@@ -687,14 +680,12 @@ __global__ void __launch_bounds__(kScanThreads, 2) row_kernel(const ScanArgs s, 
 template <typename T, bool BACK, bool STAGED, bool LOGITS>
 __global__ void __launch_bounds__(kScanThreads, BACK ? 1 : 2)
 strided_kernel(const ScanArgs s, const int cluster) {
-    constexpr int V = 1, S = kElems;       // steps of a thread in a round
+    constexpr int S = kElems;              // steps of a thread in a round
     constexpr int IN = BACK ? 4 : 2;       // tensors read
     constexpr int OUT = BACK ? 2 : 1;
-    constexpr int W = 32 * V;
-    using Raw = Word<T, V>;
-    __shared__ float s_A[2][kScanWarps][W], s_H[2][kScanWarps][W];
-    __shared__ float s_rA[2][kMaxCluster][W], s_rH[2][kMaxCluster][W];
-    __shared__ float s_start[W];
+    __shared__ float s_A[2][kScanWarps][32], s_H[2][kScanWarps][32];
+    __shared__ float s_rA[2][kMaxCluster][32], s_rH[2][kMaxCluster][32];
+    __shared__ float s_start[32];
     extern __shared__ float s_tile[];
 
     pdl_launch_dependents();
@@ -720,7 +711,7 @@ strided_kernel(const ScanArgs s, const int cluster) {
         c = tile * (rows * inner) + lane;
         valid = lane < rows * inner && c < s.channels;
     } else {
-        c = ((tile * (kScanWarps >> s.groups_log) + ct) * 32 + lane) * V;
+        c = (tile * (kScanWarps >> s.groups_log) + ct) * 32 + lane;
         valid = c < s.channels;
     }
     const int64_t co = valid ? c / inner : 0, ci = valid ? c - co * inner : 0;
@@ -736,7 +727,7 @@ strided_kernel(const ScanArgs s, const int cluster) {
 #pragma unroll
     for (int k = 0; k < OUT; ++k) out[k] = static_cast<T *>(const_cast<void *>(s.out[k].p)) + (STAGED ? 0 : co * s.out[k].ld + ci);
 
-    Raw raw[IN][S];      // not STAGED: the thread's steps; STAGED: elements of the tile, 256 apart
+    T raw[IN][S];      // not STAGED: the thread's steps; STAGED: elements of the tile, 256 apart
     auto load = [&](int64_t round) {
         const int64_t first = (round * cluster + rank) * L;
         if (STAGED) {
@@ -747,10 +738,9 @@ strided_kernel(const ScanArgs s, const int cluster) {
                 const bool on = r < rows && o < s.outer && t < steps;
 #pragma unroll
                 for (int k = 0; k < IN; ++k) {
-                    const float zero[V] = {};
-                    raw[k][j].set(zero);
+                    raw[k][j] = narrow<T>(0.0f);
                     if (!on || (BACK && k == 3 && t == steps - 1)) continue;   // (before step 0: state0)
-                    raw[k][j] = *reinterpret_cast<const Raw *>(in[k] + o * ins[k]->ld + t * ins[k]->step + i);
+                    raw[k][j] = in[k][o * ins[k]->ld + t * ins[k]->step + i];
                 }
             }
             return;
@@ -761,22 +751,15 @@ strided_kernel(const ScanArgs s, const int cluster) {
             const int64_t t = t0 + j;
 #pragma unroll
             for (int k = 0; k < IN; ++k) {
-                const float zero[V] = {};
-                raw[k][j].set(zero);
-                if (valid && t < steps - (BACK && k == 3 ? 1 : 0))
-                    raw[k][j] = *reinterpret_cast<const Raw *>(in[k] + t * ins[k]->step);
+                raw[k][j] = valid && t < steps - (BACK && k == 3 ? 1 : 0) ? in[k][t * ins[k]->step] : narrow<T>(0.0f);
             }
         }
     };
 
     pdl_wait_previous();
     load(0);
-    float carry[V], state0[V];   // state0: backward, the state before step 0, in 32 bits
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        carry[v] = valid && s.first != nullptr ? s.first[c + v] : 0.0f;
-        state0[v] = BACK && valid && s.h0 != nullptr ? s.h0[c + v] : 0.0f;
-    }
+    float carry = valid && s.first != nullptr ? s.first[c] : 0.0f;
+    const float state0 = BACK && valid && s.h0 != nullptr ? s.h0[c] : 0.0f;   // backward: the state before step 0, in 32 bits
 
     if (cluster > 1) cluster_wait();
     const int64_t rounds = (steps + int64_t(cluster) * L - 1) / (int64_t(cluster) * L);
@@ -792,11 +775,7 @@ strided_kernel(const ScanArgs s, const int cluster) {
                 const int e = tid + j * kScanThreads, r = over_inner(e) / kRun, q = e - r * run;
                 if (r < rows) {
 #pragma unroll
-                    for (int k = 0; k < IN; ++k) {
-                        float v[V];
-                        raw[k][j].get(v);
-                        s_tile[k * plane + r * pitch + q] = v[0];
-                    }
+                    for (int k = 0; k < IN; ++k) s_tile[k * plane + r * pitch + q] = widen(raw[k][j]);
                 }
             }
             __syncthreads();
@@ -804,125 +783,94 @@ strided_kernel(const ScanArgs s, const int cluster) {
 
         // the maps of the steps.  Forward: p = u.  Backward: p = dh, q = what g is
         // multiplied by in d_gate, rest in d_x
-        float a[S][V], p[S][V], q[BACK ? S : 1][V], rest[BACK ? S : 1][V];
-        float A[V], H[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) A[v] = 1.0f, H[v] = 0.0f;
+        float a[S], p[S], q[BACK ? S : 1], rest[BACK ? S : 1];
+        float A = 1.0f, H = 0.0f;
 #pragma unroll
         for (int j = 0; j < S; ++j) {
-            float gate[V], x[V], dh[V], hp[V];
+            float gate, x, dh = 0.0f, h = 0.0f;
             if (STAGED) {
-                gate[0] = at[j * inner], x[0] = at[plane + j * inner];
-                if (BACK) dh[0] = at[2 * plane + j * inner], hp[0] = at[3 * plane + j * inner];
+                gate = at[j * inner], x = at[plane + j * inner];
+                if (BACK) dh = at[2 * plane + j * inner], h = at[3 * plane + j * inner];
             } else {
-                raw[0][j].get(gate);
-                raw[1][j].get(x);
-                if (BACK) {
-                    raw[IN - 2][j].get(dh);
-                    raw[IN - 1][j].get(hp);
-                }
+                gate = widen(raw[0][j]), x = widen(raw[1][j]);
+                if (BACK) dh = widen(raw[IN - 2][j]), h = widen(raw[IN - 1][j]);
             }
-            const bool on = t0 + j < steps;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float r;
-                open_gate<LOGITS>(gate[v], a[j][v], r);
-                if (BACK) {
-                    const float h = t0 + j == steps - 1 ? state0[v] : hp[v];
-                    const float slope = LOGITS ? a[j][v] * r : 1.0f;
-                    q[j][v] = (s.coupled ? h - x[v] : h) * slope;
-                    rest[j][v] = s.coupled ? r : 1.0f;
-                    p[j][v] = dh[v];
-                } else {
-                    p[j][v] = s.coupled ? r * x[v] : x[v];
-                }
-                if (!on) a[j][v] = 1.0f, p[j][v] = 0.0f;
-                H[v] = BACK ? a[j][v] * (H[v] + p[j][v]) : fmaf(a[j][v], H[v], p[j][v]);
-                A[v] *= a[j][v];
+            float r;
+            open_gate<LOGITS>(gate, a[j], r);
+            if (BACK) {
+                if (t0 + j == steps - 1) h = state0;
+                const float slope = LOGITS ? a[j] * r : 1.0f;
+                q[j] = (s.coupled ? h - x : h) * slope;
+                rest[j] = s.coupled ? r : 1.0f;
+                p[j] = dh;
+            } else {
+                p[j] = s.coupled ? r * x : x;
             }
+            if (t0 + j >= steps) a[j] = 1.0f, p[j] = 0.0f;
+            H = BACK ? a[j] * (H + p[j]) : fmaf(a[j], H, p[j]);
+            A *= a[j];
         }
         if (round + 1 < rounds) load(round + 1);
 
         // the carry into the thread's steps
-        float in_c[V];
+        float in_c = carry;
         if (tg > 1 || cluster > 1) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) s_A[buf][warp][v * 32 + lane] = A[v], s_H[buf][warp][v * 32 + lane] = H[v];
+            s_A[buf][warp][lane] = A, s_H[buf][warp][lane] = H;
             __syncthreads();
             const int w0 = warp & ~(tg - 1);   // the first warp of these channels
             if (cluster > 1) {
-                // the map of all steps of this CTA, to every CTA: a warp folds one of the V channels of a lane
-                const int v = warp % V;
+                // the map of all steps of this CTA, to every CTA
                 float CA = 1.0f, CH = 0.0f;
                 for (int w = 0; w < kScanWarps; ++w) {
-                    const float wa = s_A[buf][w][v * 32 + lane];
-                    CH = through<LOGITS>(wa, s_H[buf][w][v * 32 + lane], CH);
+                    const float wa = s_A[buf][w][lane];
+                    CH = through<LOGITS>(wa, s_H[buf][w][lane], CH);
                     CA *= wa;
                 }
-                for (int k = warp / V; k < cluster; k += kScanWarps / V) {
-                    store_remote(&s_rA[buf][rank][v * 32 + lane], k, CA);
-                    store_remote(&s_rH[buf][rank][v * 32 + lane], k, CH);
+                for (int k = warp; k < cluster; k += kScanWarps) {
+                    store_remote(&s_rA[buf][rank][lane], k, CA);
+                    store_remote(&s_rH[buf][rank][lane], k, CH);
                 }
                 cluster_meet();   // (the slots of a round are written again two meetings later)
                 if (warp == 0) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        for (int k = 0; k < cluster; ++k) {
-                            if (k == rank) s_start[v * 32 + lane] = carry[v];
-                            carry[v] = through<LOGITS>(s_rA[buf][k][v * 32 + lane], s_rH[buf][k][v * 32 + lane], carry[v]);
-                        }
+                    for (int k = 0; k < cluster; ++k) {
+                        if (k == rank) s_start[lane] = carry;
+                        carry = through<LOGITS>(s_rA[buf][k][lane], s_rH[buf][k][lane], carry);
                     }
                 }
                 __syncthreads();
-#pragma unroll
-                for (int v = 0; v < V; ++v) in_c[v] = s_start[v * 32 + lane];
-                for (int w = 0; w < group; ++w)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) in_c[v] = through<LOGITS>(s_A[buf][w][v * 32 + lane], s_H[buf][w][v * 32 + lane], in_c[v]);
+                in_c = s_start[lane];
+                for (int w = 0; w < group; ++w) in_c = through<LOGITS>(s_A[buf][w][lane], s_H[buf][w][lane], in_c);
             } else {
                 for (int w = 0; w < tg; ++w) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        if (w == group) in_c[v] = carry[v];
-                        carry[v] = through<LOGITS>(s_A[buf][w0 + w][v * 32 + lane], s_H[buf][w0 + w][v * 32 + lane], carry[v]);
-                    }
+                    if (w == group) in_c = carry;
+                    carry = through<LOGITS>(s_A[buf][w0 + w][lane], s_H[buf][w0 + w][lane], carry);
                 }
             }
         } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) in_c[v] = carry[v], carry[v] = through<LOGITS>(A[v], H[v], carry[v]);
+            carry = through<LOGITS>(A, H, carry);
         }
 
         // the steps again, from that carry
 #pragma unroll
         for (int j = 0; j < S; ++j) {
             const int64_t t = t0 + j;
-            float o0[V], o1[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (BACK) {
-                    const float g = p[j][v] + in_c[v];
-                    o0[v] = g * q[j][v];
-                    o1[v] = g * rest[j][v];
-                    in_c[v] = a[j][v] * g;
-                } else {
-                    in_c[v] = fmaf(a[j][v], in_c[v], p[j][v]);
-                    o0[v] = in_c[v];
-                }
+            float o0, o1 = 0.0f;
+            if (BACK) {
+                const float g = p[j] + in_c;
+                o0 = g * q[j];
+                o1 = g * rest[j];
+                in_c = a[j] * g;
+            } else {
+                o0 = in_c = fmaf(a[j], in_c, p[j]);
             }
             if (STAGED) {
                 if (staged) {
-                    at[j * inner] = o0[0];
-                    if (BACK) at[plane + j * inner] = o1[0];
+                    at[j * inner] = o0;
+                    if (BACK) at[plane + j * inner] = o1;
                 }
             } else if (valid && t < steps) {
-                Raw w;
-                w.set(o0);
-                *reinterpret_cast<Raw *>(out[0] + t * s.out[0].step) = w;
-                if (BACK) {
-                    w.set(o1);
-                    *reinterpret_cast<Raw *>(out[OUT - 1] + t * s.out[1].step) = w;
-                }
+                out[0][t * s.out[0].step] = narrow<T>(o0);
+                if (BACK) out[OUT - 1][t * s.out[1].step] = narrow<T>(o1);
             }
         }
         if (STAGED) {
@@ -940,10 +888,7 @@ strided_kernel(const ScanArgs s, const int cluster) {
             }
         }
     }
-    if (s.last != nullptr && valid && rank == 0 && (cluster > 1 ? warp == 0 : group == 0)) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) s.last[c + v] = carry[v];
-    }
+    if (s.last != nullptr && valid && rank == 0 && (cluster > 1 ? warp == 0 : group == 0)) s.last[c] = carry;
 }
 
 // ---- host ----
