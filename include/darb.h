@@ -517,8 +517,9 @@ typedef enum { DARB_GATES_LOGITS = 0, DARB_GATES_VALUES = 1 } darb_gates_t;
  * The state is fp32 from step to step; h is rounded to its type as it is written.  h may
  * be x itself (same pointer and strides); no other overlap is allowed.  A logit of -inf
  * starts anew (a = 0), one of +inf keeps the state (a = 1; steps are put together in a fixed
- * order of their own, so that its last place may change); a NaN, or an infinite state that
- * meets a = 0, makes its channel NaN from there on.  Gates above 1 in magnitude are allowed
+ * order of their own, so that its last place may change); a NaN makes its channel NaN from
+ * there on, and so may an infinite state, as soon as the product of the gates since is 0 in
+ * 32 bits.  Gates above 1 in magnitude are allowed
  * as long as their products over any 8192 steps stay finite.
  * No channels: nothing is done; steps == 0: h_last is h0.
  * Asynchronous on `stream`; allocates nothing; one launch (steps == 0: a copy).

@@ -31,7 +31,7 @@
 //  * 128 bytes lie side by side wherever the channels allow it.
 // Three kernels, by how the operands lie (form_of): channels four at a time; rows of
 // consecutive steps, by aligned granules; and anything else, an element at a time, through
-// shared memory where fewer than 8 channels lie together.
+// shared memory where few channels lie together.
 #include "launch.cuh"
 #include "tma.cuh"
 #include "tokens.cuh"
@@ -95,6 +95,7 @@ struct Word<__nv_bfloat16> {
         w = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
     }
 };
+
 // 1 / x, one instruction (off by one unit; of infinity 0).
 __device__ __forceinline__ float reciprocal(float x) {
     float y;
@@ -102,8 +103,10 @@ __device__ __forceinline__ float reciprocal(float x) {
     return y;
 }
 
-// a and 1 - a from a gate, each to the last places of its own (a sigmoid near 1
-// leaves its distance from 1 exact); +-inf give exactly 1 and 0.
+// a and 1 - a from a gate, neither as the other's difference from 1 where it is the smaller (a
+// sigmoid near 1 keeps its distance from 1).  The exponential's argument is rounded, so that the
+// smaller one is off by about |gate| 2^-24 of itself beside its last places (gates of 4 to 8: 8,
+// 17 to 30: 29 of these units); +-inf give exactly 1 and 0.
 template <bool LOGITS>
 __device__ __forceinline__ void open_gate(float gate, float &a, float &rest) {
     if (LOGITS) {
