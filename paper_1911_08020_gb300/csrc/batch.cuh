@@ -205,8 +205,8 @@ __device__ __forceinline__ void chunk_rows(const unsigned char *s_vals, const ui
 
 template <bool BF16, int LPR, int CPL, int MODE>
 __global__ void __launch_bounds__(kThreads, 2)
-batch_kernel(Format f, const WorkItem *__restrict__ items, const float *__restrict__ X, int64_t ldx, int64_t batch,
-       float *__restrict__ Y, int64_t ldy, const __grid_constant__ CUtensorMap xmap,
+batch_kernel(Format f, const WorkItem *__restrict__ items, const float *X, int64_t ldx, int64_t batch,
+       float *Y, int64_t ldy, const __grid_constant__ CUtensorMap xmap,
        const __grid_constant__ CUtensorMap hmap, RnnArgs ra, int use_tma, int early) {
     constexpr bool kStacked = MODE != kModeY;
     constexpr bool kSplit = MODE == kModeGru;

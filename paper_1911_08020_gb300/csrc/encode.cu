@@ -161,8 +161,8 @@ encode_kernel(EncodeTarget t, const void *W, int64_t ldw, int32_t *status, int s
         const int ehead = (g.blo - g.off0) / kEsz, etail = (g.bhi - g.off0) / kEsz;
         if (ehead > 0 || etail < padded) {   // the same for every thread
             const elem_t *src = reinterpret_cast<const elem_t *>(g.gaddr);
-            for (int c = tid; c < ehead && c < padded; c += kEncThreads) e[c] = c < d.span ? __ldg(src + c) : elem_t(0);
-            for (int c = etail + tid; c < padded; c += kEncThreads) e[c] = c < d.span ? __ldg(src + c) : elem_t(0);
+            for (int c = tid; c < ehead && c < padded; c += kEncThreads) e[c] = c < d.span ? src[c] : elem_t(0);
+            for (int c = etail + tid; c < padded; c += kEncThreads) e[c] = c < d.span ? src[c] : elem_t(0);
             __syncthreads();
         }
         // ---- general path: one block per thread

@@ -57,14 +57,14 @@ template <bool BF16>
 __device__ __forceinline__ void load_chunk_rec(const Format &f, const Group &g, int c, int lane, ChunkData<BF16> &d) {
     const int64_t rec = int64_t(c) * kSlots + lane;
     if constexpr (BF16) {
-        d.v[0] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(f.vals) + g.val_off + rec * kChunk));
+        d.v[0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(f.vals) + g.val_off + rec * kChunk);
     } else {
         const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const float *>(f.vals) + g.val_off + rec * kChunk);
-        d.v[0] = __ldg(p);
-        d.v[1] = __ldg(p + 1);
+        d.v[0] = p[0];
+        d.v[1] = p[1];
     }
-    if (g.nib) d.o = make_uint2(__ldg(f.offs + g.off_off + rec), 0u);
-    else d.o = __ldg(reinterpret_cast<const uint2 *>(f.offs + g.off_off) + rec);
+    if (g.nib) d.o = make_uint2(f.offs[g.off_off + rec], 0u);
+    else d.o = reinterpret_cast<const uint2 *>(f.offs + g.off_off)[rec];
 }
 
 // A chunk's products for one slot (lane): block e selects xb[e m + offset],
@@ -162,10 +162,10 @@ gemv_kernel(Format f, const float *X, int64_t ldx, float *Y, int64_t ldy, int ea
     if (ldx == 1 && (reinterpret_cast<uintptr_t>(X) & 15) == 0) {
         const int64_t nq = cols / 4;
         for (int64_t i = tid; i < nq; i += kThreadsG)
-            reinterpret_cast<float4 *>(s_x)[i] = __ldg(reinterpret_cast<const float4 *>(X) + i);
-        for (int64_t k = nq * 4 + tid; k < cols; k += kThreadsG) s_x[k] = __ldg(X + k);
+            reinterpret_cast<float4 *>(s_x)[i] = reinterpret_cast<const float4 *>(X)[i];
+        for (int64_t k = nq * 4 + tid; k < cols; k += kThreadsG) s_x[k] = X[k];
     } else {
-        for (int64_t k = tid; k < cols; k += kThreadsG) s_x[k] = __ldg(X + k * ldx);
+        for (int64_t k = tid; k < cols; k += kThreadsG) s_x[k] = X[k * ldx];
     }
     __syncthreads();
     float acc = 0.0f;
@@ -217,8 +217,9 @@ gemv_bulk_kernel(Format f, const float *X, int64_t ldx, float *Y, int64_t ldy, i
     const uint32_t vbytes = uint32_t(nch) * kSlots * kChunk * kEsz;
     const uint32_t obytes = uint32_t(nch) * kSlots * (g.nib ? 4u : 8u);
     const int64_t cols = f.cols;
-    // x in one copy when it is one aligned run of whole 16-byte units
-    const bool xbulk = ldx == 1 && (reinterpret_cast<uintptr_t>(X) & 15) == 0 && (cols & 3) == 0;
+    // x, or all but its last three elements at most, in one copy when it is one aligned run
+    const int xcopied = ldx == 1 && (reinterpret_cast<uintptr_t>(X) & 15) == 0 ? int(cols) & ~3 : 0;
+    const bool xbulk = xcopied > 0;
     auto copy_w = [&] {
         mbar_arrive_expect_tx(&bar[0], vbytes + obytes);
         bulk_g2s(s_val, static_cast<const unsigned char *>(f.vals) + g.val_off * kEsz, vbytes, &bar[0]);
@@ -236,12 +237,11 @@ gemv_bulk_kernel(Format f, const float *X, int64_t ldx, float *Y, int64_t ldy, i
     if (tid == 0) {
         if (!early) copy_w();
         if (xbulk) {
-            mbar_arrive_expect_tx(&bar[1], uint32_t(cols) * 4u);
-            bulk_g2s(s_x, X, uint32_t(cols) * 4u, &bar[1]);
+            mbar_arrive_expect_tx(&bar[1], uint32_t(xcopied) * 4u);
+            bulk_g2s(s_x, X, uint32_t(xcopied) * 4u, &bar[1]);
         }
     }
-    if (!xbulk)
-        for (int64_t k = tid; k < cols; k += kThreadsB) s_x[k] = __ldg(X + k * ldx);
+    for (int k = xcopied + tid; k < int(cols); k += kThreadsB) s_x[k] = X[k * ldx];
     __syncthreads();   // the barriers' initialisation and the plain copy of x are seen by all threads
     const bool ok = __syncthreads_and(mbar_wait(&bar[0], 0) && (!xbulk || mbar_wait(&bar[1], 0)));
     float acc = 0.0f;

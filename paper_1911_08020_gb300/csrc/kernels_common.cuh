@@ -40,7 +40,7 @@ __device__ __forceinline__ void fma4(float4 &acc, float v, const float4 &x) {
 template <bool BF16>
 __device__ __forceinline__ void load_chunk(const void *vals, int64_t idx, float (&v)[kChunk]) {
     if constexpr (BF16) {
-        const uint4 q = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(vals) + idx));
+        const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(vals) + idx);
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -49,7 +49,7 @@ __device__ __forceinline__ void load_chunk(const void *vals, int64_t idx, float 
         }
     } else {
         const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(vals) + idx);
-        const float4 a = __ldg(p), b = __ldg(p + 1);
+        const float4 a = p[0], b = p[1];
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
         v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
@@ -59,9 +59,9 @@ __device__ __forceinline__ void load_chunk(const void *vals, int64_t idx, float 
 template <bool NIB>
 __device__ __forceinline__ uint2 load_offsets(const uint32_t *offs, int64_t rec) {
     if constexpr (NIB) {
-        return make_uint2(__ldg(offs + rec), 0u);
+        return make_uint2(offs[rec], 0u);
     } else {
-        return __ldg(reinterpret_cast<const uint2 *>(offs) + rec);
+        return reinterpret_cast<const uint2 *>(offs)[rec];
     }
 }
 
@@ -117,7 +117,7 @@ __device__ __forceinline__ void rowlane_accumulate(const Format &f, const Group 
 #pragma unroll
                 for (int t = 0; t < BT; ++t) {
                     if (t < nb) {
-                        const float xv = __ldg(xr + t);
+                        const float xv = xr[t];
                         if (p1) acc[t] = fmaf(v[e], xv, acc[t]);
                         else acc2[t] = fmaf(v[e], xv, acc2[t]);
                     }

@@ -215,18 +215,18 @@ step_kernel(Format f, RnnArgs ra, const __grid_constant__ CUtensorMap mx, const 
         b.kb = c * kChunk * m;
         b.whole = b.kb >= row.klo && b.kb + kChunk * m <= row.khi;
         const uint4 *pv = static_cast<const uint4 *>(f.vals) + int64_t(row.rec + uint32_t(c) * kSlots) * (BF16 ? 1 : 2);
-        const uint4 w0 = __ldg(pv);
+        const uint4 w0 = pv[0];
         b.vw[0] = w0.x; b.vw[1] = w0.y; b.vw[2] = w0.z; b.vw[3] = w0.w;
         if constexpr (!BF16) {
-            const uint4 w1 = __ldg(pv + 1);
+            const uint4 w1 = pv[1];
             b.vw[4] = w1.x; b.vw[5] = w1.y; b.vw[6] = w1.z; b.vw[7] = w1.w;
         }
         if (nib) {
-            const uint32_t w = __ldg(f.offs + row.off + uint32_t(c) * kSlots);
+            const uint32_t w = f.offs[row.off + uint32_t(c) * kSlots];
             const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
             b.ow = make_uint2(__byte_perm(even, odd, 0x5140), __byte_perm(even, odd, 0x7362));
         } else {
-            b.ow = __ldg(reinterpret_cast<const uint2 *>(f.offs + row.off + uint32_t(c) * (2 * kSlots)));
+            b.ow = *reinterpret_cast<const uint2 *>(f.offs + row.off + uint32_t(c) * (2 * kSlots));
         }
     };
     if (p.early) {

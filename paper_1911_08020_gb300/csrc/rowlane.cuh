@@ -92,7 +92,7 @@ __device__ __forceinline__ void chunks(const Group &g, int rc0, int lc_begin, in
 
 template <bool BF16, int BT, int MODE>
 __global__ void __launch_bounds__(kWarps * 32)
-rowlane_kernel(Format f, const float *__restrict__ X, int64_t ldx, int64_t batch, float *__restrict__ Y, int64_t ldy,
+rowlane_kernel(Format f, const float *X, int64_t ldx, int64_t batch, float *Y, int64_t ldy,
        RnnArgs ra, int early, int x_contig) {
     constexpr int kEsz = BF16 ? 2 : 4;
     constexpr int kParts = MODE == kModeGru ? 2 : 1;
@@ -167,7 +167,7 @@ rowlane_kernel(Format f, const float *__restrict__ X, int64_t ldx, int64_t batch
             if (nbulk > 0) bulk_g2s(s_x, X + int64_t(k0) * BT, uint32_t(nbulk) * 4, bar);
         }
         if (MODE == kModeY && x_contig) {
-            for (int idx = nbulk + tid; idx < nx; idx += kWarps * 32) s_x[idx] = __ldg(X + int64_t(k0) * BT + idx);
+            for (int idx = nbulk + tid; idx < nx; idx += kWarps * 32) s_x[idx] = X[int64_t(k0) * BT + idx];
         } else {
             // strided X or the stacked RNN input: 8 independent loads in flight per thread
             for (int base = 0; base < nx; base += 8 * kWarps * 32) {
@@ -178,8 +178,8 @@ rowlane_kernel(Format f, const float *__restrict__ X, int64_t ldx, int64_t batch
                     const int k = k0 + idx / BT, t = idx % BT;
                     float v = 0.0f;
                     if (idx < nx && t < nb) {
-                        if constexpr (MODE == kModeY) v = __ldg(X + int64_t(k) * ldx + t);
-                        else v = k < ra.I ? __ldg(ra.x + int64_t(k) * ra.B + t) : __ldg(ra.h + int64_t(k - ra.I) * ra.B + t);
+                        if constexpr (MODE == kModeY) v = X[int64_t(k) * ldx + t];
+                        else v = k < ra.I ? ra.x[int64_t(k) * ra.B + t] : ra.h[int64_t(k - ra.I) * ra.B + t];
                     }
                     tmp[u] = v;
                 }

@@ -159,12 +159,12 @@ split_kernel(const float *X, int64_t ldx, int64_t batch, int64_t cols, uint16_t 
                 const int k = i / q4, b = (i - k * q4) * 4;
                 const float *x = X + int64_t(k) * ldx + b;
                 if (vec && b + 4 <= nb) {
-                    v[u] = __ldg(reinterpret_cast<const float4 *>(x));
+                    v[u] = *reinterpret_cast<const float4 *>(x);
                 } else {
-                    v[u].x = __ldg(x);
-                    if (b + 1 < nb) v[u].y = __ldg(x + 1);
-                    if (b + 2 < nb) v[u].z = __ldg(x + 2);
-                    if (b + 3 < nb) v[u].w = __ldg(x + 3);
+                    v[u].x = x[0];
+                    if (b + 1 < nb) v[u].y = x[1];
+                    if (b + 2 < nb) v[u].z = x[2];
+                    if (b + 3 < nb) v[u].w = x[3];
                 }
             }
         }
@@ -255,9 +255,9 @@ tc_kernel(const __grid_constant__ CUtensorMap hmap, const __grid_constant__ CUte
         auto load_chunk = [&](int c, uint4 &v, uint2 &o) {
             const int64_t rec = int64_t(c) * kSlots + lane;
             if (valid && c * kChunk < n) {
-                v = __ldg(reinterpret_cast<const uint4 *>(vals + val_off + rec * kChunk));
-                if (nib) o = make_uint2(__ldg(f.offs + off_off + rec), 0u);
-                else o = __ldg(reinterpret_cast<const uint2 *>(f.offs + off_off) + rec);
+                v = *reinterpret_cast<const uint4 *>(vals + val_off + rec * kChunk);
+                if (nib) o = make_uint2(f.offs[off_off + rec], 0u);
+                else o = reinterpret_cast<const uint2 *>(f.offs + off_off)[rec];
             }
         };
         // blocks of this warp's first stage start at jb = floor(k0 / m), rem = k0 - jb*m;

@@ -151,7 +151,7 @@ struct Set {
 
 template <bool BF16, int T, bool PLAIN>
 __global__ void __launch_bounds__(kThreads, 1)
-xres_kernel(Format f, const float *__restrict__ X, int64_t ldx, int64_t batch, float *__restrict__ Y, int64_t ldy,
+xres_kernel(Format f, const float *X, int64_t ldx, int64_t batch, float *Y, int64_t ldy,
             const __grid_constant__ CUtensorMap xmap, const __grid_constant__ Plan p) {
     static_assert(T == 32, "the consumer layouts assume 32-column tiles (128-byte activation rows)");
     constexpr int kEsz = BF16 ? 2 : 4;
