@@ -787,6 +787,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
             }
             pair_commit<CG>(done);
         }
+        // no product is in flight when the memory is given back
+        if (lane == 0 && rank == 0 && !mbar_wait(done, 0)) ok = false;
         __syncwarp();
     } else {
         // two warps for each quarter of the accumulator's rows, with half of the columns each
@@ -863,9 +865,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) product_kernel(const StepArgs
     }
     tc_fence_before_sync();
     __syncthreads();
-    // No product is in flight when the memory is given back.  (Waited for when this CTA's tiles have been written:
-    // a pair's second CTA issues none, and from its start this would be a wait for the whole launch.)
-    if (warp == 1) {
+    // (A pair's second CTA issues none: from its start this would be a wait for the whole launch, not for a tile.)
+    if (CG == 2 && rank == 1 && warp == 1) {
         if (lane == 0 && !mbar_wait(done, 0)) ok = false;
         __syncwarp();
     }
